@@ -403,6 +403,104 @@ slicegcn_status_t slicegcn_train_epochs_host(const slicegcn_model* m, const slic
                                              int64_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Embedding lookup -- features of nodes that are given by an id (a learned vector per node, a categorical field) instead
+ * of a dense row.  The paper starts from dense features; these calls produce them, and take their gradient
+ * (slicegcn_layer_backward's dH_in) back to the table.
+ *   forward    out[i, 0:width] = scale * table[ids[i], 0:width]
+ *   backward   dtable[v, 0:width] = sum over i with ids[i] = v of scale * dout[i, 0:width]
+ * An id of -1 means "none": a row of zeros forward, no gradient.  Any other id outside [0, vocab) is treated the same way
+ * and reported: *status [device, one int32, caller-owned, may be NULL] receives SLICEGCN_DEVSTATUS_BAD_ID (the word is
+ * only ever set, never cleared).  Several fields side by side are several calls whose out / dout start at the field's
+ * first column, with the leading dimension of the whole matrix.
+ */
+enum { SLICEGCN_DEVSTATUS_BAD_ID = 33 };
+typedef struct slicegcn_embed_desc {
+    int64_t n;             /* ids, >= 0 */
+    int64_t vocab;         /* rows of the table, 1 .. 2^31 - 2 */
+    int32_t width;         /* columns, >= 1 */
+    int32_t table_dtype;   /* forward: storage type of the table ... */
+    int32_t out_dtype;     /* ... and of out (fp32 arithmetic, one rounding) */
+    int32_t accumulate;    /* backward: 0 overwrites the whole of dtable (rows of absent ids become zero), 1 adds to it */
+    double scale;
+    int64_t table_ld, out_ld;       /* leading dimensions; forward only */
+    int64_t dout_ld, dtable_ld;     /* backward only */
+} slicegcn_embed_desc;
+/* ids [device, int32 n], table [device, vocab x width], out [device, n x width].  Errors: INVALID_ARG, OVERFLOW, CUDA. */
+slicegcn_status_t slicegcn_embed_forward(const slicegcn_embed_desc* d, const int32_t* ids, const void* table, void* out,
+                                         int32_t* status, void* stream);
+/* dout [device, fp32 n x width], dtable [device, fp32 vocab x width].  Deterministic: the ids are sorted (stable) and every
+ * row is summed in a fixed order; no floating-point atomics.  workspace [device, 16-byte aligned], at least
+ * slicegcn_embed_workspace_bytes(d) bytes, contents undefined before and after.
+ * Errors: INVALID_ARG, OVERFLOW, ALLOC (workspace too small), CUDA. */
+slicegcn_status_t slicegcn_embed_workspace_bytes(const slicegcn_embed_desc* d, int64_t* bytes);
+slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const int32_t* ids, const float* dout, float* dtable,
+                                          int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Residual step between sliced layers -- the norms before and after a block, its gate and its residual scale in one pass
+ * (deep models; the paper's layers have neither norms nor residuals).  Statistics are taken per slice: every block of h_s
+ * columns of a row is normalised by itself, so that the slices still never interact (num_slices = 1: the whole row).
+ *   h = x + residual_scale * sigmoid(gate) * (N(y) * w_post + b_post)
+ *   u = N(h) * w_pre + b_pre
+ *   N(t) = t / sqrt(mean(t^2) + eps)  (ROWNORM_RMS)    or    (t - mean(t)) / sqrt(var(t) + eps)  (ROWNORM_LAYER)
+ * x is the residual stream, y the block's output (slicegcn_layer_forward), h the new residual stream and u the next
+ * block's input.  u is computed from h before h is rounded to its storage type.  What is NULL is left out: gate = NULL
+ * no gate; x = NULL no residual; y = NULL a norm before a block alone (h = x, u = N(x) ...); u = NULL after the last block
+ * (h alone); h = NULL when only u is wanted; a NULL weight is a vector of ones, a NULL bias of zeros.
+ */
+enum { SLICEGCN_ROWNORM_RMS = 0, SLICEGCN_ROWNORM_LAYER = 1 };
+#define SLICEGCN_MAX_NORM_WIDTH 16384
+typedef struct slicegcn_residual_norm_desc {
+    int64_t n;                   /* rows, >= 0 */
+    int32_t num_slices;          /* 1 .. SLICEGCN_MAX_SLICES */
+    int32_t h_s;                 /* columns per slice, 1 .. SLICEGCN_MAX_NORM_WIDTH */
+    int32_t kind;                /* SLICEGCN_ROWNORM_* */
+    int32_t dtype;               /* storage type of x, y, gate, h and u; gradients are always fp32 */
+    double eps;                  /* > 0 */
+    double residual_scale;
+    int64_t x_ld, y_ld, gate_ld, h_ld, u_ld;              /* leading dimensions of the matrices a call is given */
+    int64_t dh_ld, du_ld, dx_ld, dy_ld, dgate_ld;         /* (>= num_slices * h_s; those of others are ignored) */
+    const float *w_post, *b_post, *w_pre, *b_pre;         /* [device, num_slices * h_s] or NULL */
+} slicegcn_residual_norm_desc;
+/* Matrices [device, n x num_slices*h_s].  h may be x (same pointer and leading dimension); no other overlap.
+ * Errors: INVALID_ARG, OVERFLOW, UNSUPPORTED (more slices or wider ones), CUDA. */
+slicegcn_status_t slicegcn_residual_norm_forward(const slicegcn_residual_norm_desc* d, const void* x, const void* y,
+                                                 const void* gate, void* h, void* u, void* stream);
+/* Gradient of the same step from y, gate and h as the forward call took and stored them (nothing else is kept).
+ *   dh [device, fp32, n x cols]: gradient of the loss w.r.t. h from everything but u, NULL = 0;  du: w.r.t. u, NULL when
+ *   there was no u (h may then be NULL as well).
+ * Outputs (fp32, OVERWRITTEN, each may be NULL to skip): dx, dy, dgate [n x cols]; dw_post, db_post, dw_pre, db_pre
+ * [num_slices * h_s].  dx may be dh (same pointer and leading dimension); no other overlap.  Deterministic.
+ * workspace [device, 16-byte aligned]: at least slicegcn_residual_norm_workspace_bytes(d) bytes, contents undefined before
+ * and after.  Errors: INVALID_ARG, OVERFLOW, UNSUPPORTED, ALLOC, CUDA. */
+slicegcn_status_t slicegcn_residual_norm_workspace_bytes(const slicegcn_residual_norm_desc* d, int64_t* bytes);
+slicegcn_status_t slicegcn_residual_norm_backward(const slicegcn_residual_norm_desc* d, const void* y, const void* gate,
+                                                  const void* h, const float* dh, const float* du, float* dx, float* dy,
+                                                  float* dgate, float* dw_post, float* db_post, float* dw_pre, float* db_pre,
+                                                  void* workspace, int64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Global gradient norm over a list of tensors, and clipping by it:
+ *   norm = sqrt(sum of the squares of all elements of all tensors)  (squares and sums in 64 bits, fixed order)
+ *   dst[i] = src[i] * max_norm / norm   if norm > max_norm and norm is finite, else src[i]
+ * A norm that is infinite or NaN leaves the gradients as they are; *norm_out says so.  Nothing is read back to the host.
+ */
+#define SLICEGCN_MAX_TENSORS 512
+typedef struct slicegcn_tensor_list {
+    int32_t count;               /* 0 .. SLICEGCN_MAX_TENSORS */
+    const void* const* src;      /* [host, count] device pointers, each tensor dense */
+    void* const* dst;            /* [host, count]; dst[i] may be src[i]; NULL: only the norm */
+    const int64_t* elems;        /* [host, count], 0 allowed */
+    const int32_t* dtypes;       /* [host, count] SLICEGCN_F32 / SLICEGCN_BF16, or NULL = all fp32 */
+} slicegcn_tensor_list;
+/* norm_out [device, one float] or NULL; max_norm > 0 (infinity: nothing is clipped).  workspace [device, 16-byte aligned]:
+ * slicegcn_clip_workspace_bytes() bytes, contents undefined before and after.  Apart from dst[i] = src[i] the tensors must
+ * not overlap.  Errors: INVALID_ARG, UNSUPPORTED (too many tensors), ALLOC, CUDA. */
+slicegcn_status_t slicegcn_clip_workspace_bytes(int64_t* bytes);
+slicegcn_status_t slicegcn_clip_grads(const slicegcn_tensor_list* list, double max_norm, float* norm_out, void* workspace,
+                                      int64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Instrumentation for benchmarks (the paper reports only end-to-end epochs per second, Table IV;
  * this splits out the aggregation kernel).  Between profile_begin and profile_end every SpMM call
  * is bracketed by CUDA events on its stream and kernel launches are counted.  profile_end

@@ -24,7 +24,9 @@ ORDER_AUTO, AGG_FIRST, XFORM_FIRST = 0, 1, 2
 RULE_CEIL, RULE_FLOOR_PLUS_1 = 0, 1
 SYMMETRIZE, ADD_SELF_LOOPS, INPUT_ON_DEVICE, NORM_MEAN, NORM_SUM = 1, 2, 4, 8, 16
 MAX_SLICES = 64
-DEVSTATUS_BAD_LABEL = 32
+DEVSTATUS_BAD_LABEL, DEVSTATUS_BAD_ID = 32, 33
+ROWNORM_RMS, ROWNORM_LAYER = 0, 1
+MAX_NORM_WIDTH, MAX_TENSORS = 16384, 512
 
 EXPORTS = [
     "slicegcn_last_error", "slicegcn_slice_strategy", "slicegcn_graph_create", "slicegcn_graph_create_from_csr",
@@ -33,8 +35,21 @@ EXPORTS = [
     "slicegcn_layer_backward", "slicegcn_model_create", "slicegcn_model_destroy", "slicegcn_model_invalidate_caches", "slicegcn_model_param_count",
     "slicegcn_model_param_elems", "slicegcn_model_num_tensors", "slicegcn_model_tensor_info", "slicegcn_model_slices",
     "slicegcn_model_layer_order", "slicegcn_train_workspace_bytes", "slicegcn_train_epoch", "slicegcn_train_epoch_dropout", "slicegcn_train_epoch_sliced", "slicegcn_forward_logits", "slicegcn_train_epoch_host", "slicegcn_train_epochs_host", "slicegcn_profile_begin", "slicegcn_profile_begin_sampled",
-    "slicegcn_profile_end",
+    "slicegcn_profile_end", "slicegcn_embed_forward", "slicegcn_embed_workspace_bytes", "slicegcn_embed_backward",
+    "slicegcn_residual_norm_forward", "slicegcn_residual_norm_workspace_bytes", "slicegcn_residual_norm_backward",
+    "slicegcn_clip_workspace_bytes", "slicegcn_clip_grads",
 ]
+
+
+# declared argument types let ctypes take plain ints, which keeps short calls short
+_P = c_void_p
+ARGTYPES = {
+    "slicegcn_embed_forward": [_P, _P, _P, _P, _P, _P],
+    "slicegcn_embed_backward": [_P, _P, _P, _P, _P, _P, c_int64, _P],
+    "slicegcn_residual_norm_forward": [_P] * 7,
+    "slicegcn_residual_norm_backward": [_P] * 14 + [c_int64, _P],
+    "slicegcn_clip_grads": [_P, c_double, _P, _P, c_int64, _P],
+}
 
 
 class SliceGCNError(RuntimeError):
@@ -65,6 +80,24 @@ class DropoutDesc(ctypes.Structure):
     _fields_ = [("rate", c_double), ("masks", POINTER(c_void_p)), ("mask_ld", c_int64)]
 
 
+class EmbedDesc(ctypes.Structure):
+    _fields_ = [("n", c_int64), ("vocab", c_int64), ("width", c_int32), ("table_dtype", c_int32), ("out_dtype", c_int32),
+                ("accumulate", c_int32), ("scale", c_double), ("table_ld", c_int64), ("out_ld", c_int64), ("dout_ld", c_int64),
+                ("dtable_ld", c_int64)]
+
+
+class ResidualNormDesc(ctypes.Structure):
+    _fields_ = [("n", c_int64), ("num_slices", c_int32), ("h_s", c_int32), ("kind", c_int32), ("dtype", c_int32), ("eps", c_double),
+                ("residual_scale", c_double)] + [(k + "_ld", c_int64) for k in
+                                                 ("x", "y", "gate", "h", "u", "dh", "du", "dx", "dy", "dgate")] + \
+               [(k, c_void_p) for k in ("w_post", "b_post", "w_pre", "b_pre")]
+
+
+class TensorList(ctypes.Structure):
+    _fields_ = [("count", c_int32), ("src", POINTER(c_void_p)), ("dst", POINTER(c_void_p)), ("elems", POINTER(c_int64)),
+                ("dtypes", POINTER(c_int32))]
+
+
 def make_dropout_desc(rate: float, masks: Sequence, mask_ld: int) -> DropoutDesc:
     """masks: one device tensor (bytes, n x mask_ld) per layer but the last."""
     d = DropoutDesc()
@@ -83,6 +116,8 @@ def _load() -> ctypes.CDLL:
     for name in EXPORTS:
         if name != "slicegcn_last_error":
             getattr(lib, name).restype = c_int32
+    for name, args in ARGTYPES.items():
+        getattr(lib, name).argtypes = args
     return lib
 
 
@@ -105,6 +140,12 @@ def _ptr(x) -> Optional[int]:
 
 def _vp(x) -> c_void_p:
     return c_void_p(_ptr(x))
+
+
+def _with_address(d: ctypes.Structure) -> ctypes.Structure:
+    """The struct with its own address as an int beside it (its memory stays where it is)."""
+    d.address = ctypes.addressof(d)
+    return d
 
 
 def _check(status: int):
@@ -391,6 +432,89 @@ def slicegcn_profile_end() -> Dict[str, float]:
     calls, launches = c_int64(), c_int64()
     _check(_lib.slicegcn_profile_end(byref(ms), byref(calls), byref(by), byref(launches)))
     return {"spmm_ms": ms.value, "spmm_calls": calls.value, "spmm_bytes": by.value, "kernel_launches": launches.value}
+
+
+# ------------------------------------------------------------------------------------------ embedding
+
+def make_embed_desc(n: int, vocab: int, width: int, scale: float = 1.0, table_dtype: int = F32, out_dtype: int = F32,
+                    accumulate: bool = False, table_ld: int = 0, out_ld: int = 0, dout_ld: int = 0, dtable_ld: int = 0) -> EmbedDesc:
+    """Leading dimensions left at 0 are `width` (dense rows)."""
+    return _with_address(EmbedDesc(n, vocab, width, table_dtype, out_dtype, int(accumulate), scale, table_ld or width,
+                                   out_ld or width, dout_ld or width, dtable_ld or width))
+
+
+def slicegcn_embed_forward(d: EmbedDesc, ids, table, out, status=None, stream=None) -> None:
+    _check(_lib.slicegcn_embed_forward(d.address, _ptr(ids), _ptr(table), _ptr(out), _ptr(status), _ptr(stream)))
+
+
+def slicegcn_embed_workspace_bytes(d: EmbedDesc) -> int:
+    b = c_int64()
+    _check(_lib.slicegcn_embed_workspace_bytes(byref(d), byref(b)))
+    return b.value
+
+
+def slicegcn_embed_backward(d: EmbedDesc, ids, dout, dtable, status, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(_lib.slicegcn_embed_backward(d.address, _ptr(ids), _ptr(dout), _ptr(dtable), _ptr(status), _ptr(workspace),
+                                        workspace_bytes, _ptr(stream)))
+
+
+# ------------------------------------------------------------------------------------------ residual step, clipping
+
+def make_residual_norm_desc(n: int, num_slices: int, h_s: int, kind: int = ROWNORM_RMS, dtype: int = F32, eps: float = 1e-5,
+                            residual_scale: float = 1.0, w_post=None, b_post=None, w_pre=None, b_pre=None,
+                            **leading_dims: int) -> ResidualNormDesc:
+    """leading_dims: x_ld, y_ld, gate_ld, h_ld, u_ld, dh_ld, du_ld, dx_ld, dy_ld, dgate_ld; left out = num_slices * h_s."""
+    d = ResidualNormDesc(n, num_slices, h_s, kind, dtype, eps, residual_scale)
+    for k, _ in ResidualNormDesc._fields_[7:17]:
+        setattr(d, k, leading_dims.pop(k, 0) or num_slices * h_s)
+    if leading_dims:
+        raise TypeError(f"unknown leading dimensions {sorted(leading_dims)}")
+    d.w_post, d.b_post, d.w_pre, d.b_pre = _ptr(w_post), _ptr(b_post), _ptr(w_pre), _ptr(b_pre)
+    d._keep = (w_post, b_post, w_pre, b_pre)
+    return _with_address(d)
+
+
+def slicegcn_residual_norm_forward(d: ResidualNormDesc, x, y, gate, h, u, stream=None) -> None:
+    _check(_lib.slicegcn_residual_norm_forward(d.address, _ptr(x), _ptr(y), _ptr(gate), _ptr(h), _ptr(u), _ptr(stream)))
+
+
+def slicegcn_residual_norm_workspace_bytes(d: ResidualNormDesc) -> int:
+    b = c_int64()
+    _check(_lib.slicegcn_residual_norm_workspace_bytes(byref(d), byref(b)))
+    return b.value
+
+
+def slicegcn_residual_norm_backward(d: ResidualNormDesc, y, gate, h, dh, du, dx, dy, dgate, dw_post, db_post, dw_pre, db_pre,
+                                    workspace, workspace_bytes: int, stream=None) -> None:
+    _check(_lib.slicegcn_residual_norm_backward(d.address, _ptr(y), _ptr(gate), _ptr(h), _ptr(dh), _ptr(du), _ptr(dx), _ptr(dy),
+                                                _ptr(dgate), _ptr(dw_post), _ptr(db_post), _ptr(dw_pre), _ptr(db_pre),
+                                                _ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+def make_tensor_list(src: Sequence, dst: Optional[Sequence] = None) -> TensorList:
+    """src, dst: dense device tensors of fp32 or bf16 (dst[i] of src[i]'s type and size; dst=None: only the norm is wanted)."""
+    n = len(src)
+    if dst is not None and [(t.dtype, t.numel()) for t in dst] != [(t.dtype, t.numel()) for t in src]:
+        raise ValueError("dst must match src in number, types and sizes")
+    if not all(t.is_contiguous() for t in list(src) + list(dst or [])):
+        raise ValueError("the tensors of a list must be dense")
+    codes = {"torch.float32": F32, "torch.bfloat16": BF16}
+    arrays = ((c_void_p * max(n, 1))(*[_ptr(t) for t in src]), (c_void_p * max(n, 1))(*[_ptr(t) for t in dst]) if dst is not None else None,
+              (c_int64 * max(n, 1))(*[t.numel() for t in src]), (c_int32 * max(n, 1))(*[codes[str(t.dtype)] for t in src]))
+    d = TensorList(n, ctypes.cast(arrays[0], POINTER(c_void_p)), ctypes.cast(arrays[1], POINTER(c_void_p)) if dst is not None else None,
+                   ctypes.cast(arrays[2], POINTER(c_int64)), ctypes.cast(arrays[3], POINTER(c_int32)))
+    d._keep = (arrays, list(src), list(dst) if dst is not None else None)      # pointer arrays and tensors live with the struct
+    return _with_address(d)
+
+
+def slicegcn_clip_workspace_bytes() -> int:
+    b = c_int64()
+    _check(_lib.slicegcn_clip_workspace_bytes(byref(b)))
+    return b.value
+
+
+def slicegcn_clip_grads(tensors: TensorList, max_norm: float, norm_out, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(_lib.slicegcn_clip_grads(tensors.address, max_norm, _ptr(norm_out), _ptr(workspace), workspace_bytes, _ptr(stream)))
 
 
 # ------------------------------------------------------------------------------------------ parameter marshalling
