@@ -10,9 +10,9 @@
 namespace sgcn {
 namespace {
 
-constexpr int kSortThreads = 256;
+constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortTile = 4096;   // positions per CTA and digit pass
+constexpr int kSMs = 148;
 
 __device__ __forceinline__ float ld_elem(const float* p) { return __ldg(p); }
 __device__ __forceinline__ float ld_elem(const __nv_bfloat16* p) { return __bfloat162float(*p); }
@@ -38,68 +38,99 @@ __global__ void embed_forward_kernel(int64_t n, int64_t vocab, int width, const 
     }
 }
 
-// Sort keys: the id, or `vocab` (sorted last) for positions that take no part.
+// ---- stable sort of the ids -------------------------------------------------------------------
+// Keys run from 0 to `vocab`: the id, or `vocab` (sorted last) for positions that take no part.  Per digit two launches:
+// sort_count_kernel counts every tile's digits, sort_scatter_kernel turns the counts into offsets (each CTA reads the whole
+// table of tiles x digits, a few hundred KB that stay in L2, so no scan launch stands between the two) and moves the pairs.
 __device__ __forceinline__ uint32_t sort_key(int32_t id, int64_t vocab, int32_t* status) {
     const int32_t v = checked_id(id, vocab, status);
     return v < 0 ? (uint32_t)vocab : (uint32_t)v;
 }
 
-__global__ void sort_init_kernel(int64_t n, int64_t vocab, const int32_t* ids, uint2* pairs, int32_t* status) {
-    for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x)
-        pairs[i] = make_uint2(sort_key(ids[i], vocab, status), (uint32_t)i);
+struct SortArgs {
+    int32_t n;
+    int64_t vocab;
+    const int32_t* ids;      // read by the first digit's pass
+    const uint2* in;         // (key, position), read by the others
+    uint2* out;
+    uint32_t* counts;        // [tiles][bins]
+    uint8_t* present;        // [vocab] 1 where an id occurs; cleared by the first count, set by the first scatter
+    int32_t* status;
+    int shift, bits, tiles;
+    int32_t tile;            // positions per tile, a multiple of kSortWarps * 32
+};
+
+template <bool FIRST>
+__device__ __forceinline__ uint2 sort_load(const SortArgs& a, int32_t i) {
+    if (FIRST) return make_uint2(sort_key(a.ids[i], a.vocab, a.status), (uint32_t)i);
+    return a.in[i];
 }
 
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(int64_t n, const uint2* pairs, int shift, int tiles, uint32_t* counts) {
+template <bool FIRST>
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
     __shared__ uint32_t hist[256];
-    hist[threadIdx.x] = 0;
+    if (FIRST)
+        for (int64_t i = (blockIdx.x * (int64_t)kSortThreads + threadIdx.x) * 16; i < a.vocab; i += (int64_t)gridDim.x * kSortThreads * 16)
+            *reinterpret_cast<uint4*>(a.present + i) = make_uint4(0, 0, 0, 0);   // (rounded up to 16 bytes)
+    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * kSortTile, i1 = min(n, i0 + kSortTile);
-    for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads) atomicAdd(&hist[(pairs[i].x >> shift) & 255u], 1u);
+    const uint32_t mask = (1u << a.bits) - 1u;
+    const int64_t i0 = (int64_t)blockIdx.x * a.tile, i1 = min((int64_t)a.n, i0 + a.tile);
+    for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads)
+        atomicAdd(&hist[(sort_load<FIRST>(a, (int32_t)i).x >> a.shift) & mask], 1u);
     __syncthreads();
-    counts[(int64_t)threadIdx.x * tiles + blockIdx.x] = hist[threadIdx.x];
+    if (threadIdx.x <= mask) a.counts[((int64_t)blockIdx.x << a.bits) + threadIdx.x] = hist[threadIdx.x];
 }
 
-__global__ void __launch_bounds__(1024) sort_scan_kernel(int64_t m, uint32_t* counts) {   // exclusive scan by one CTA
-    __shared__ uint32_t warp_sum[32];
-    __shared__ uint32_t carry;
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    if (threadIdx.x == 0) carry = 0;
-    __syncthreads();
-    for (int64_t base = 0; base < m; base += 1024) {
-        const int64_t i = base + threadIdx.x;
-        const uint32_t v = i < m ? counts[i] : 0;
-        uint32_t s = v;
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t t = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) s += t;
-        }
-        if (lane == 31) warp_sum[w] = s;
-        __syncthreads();
-        uint32_t before = carry;
-        for (int k = 0; k < w; ++k) before += warp_sum[k];
-        if (i < m) counts[i] = before + s - v;
-        __syncthreads();
-        if (threadIdx.x == 1023) carry = before + s;
-        __syncthreads();
-    }
-}
-
-// Stable scatter: each warp owns a contiguous run of the tile and walks it 32 positions at a time.
-__global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(int64_t n, const uint2* in, int shift, int tiles, const uint32_t* offsets,
-                                                                    uint2* out) {
+// Each warp owns a contiguous run of the tile and walks it 32 positions at a time; lanes with the same digit are ranked by
+// one match, so the order of equal digits is kept.
+template <bool FIRST>
+__global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortArgs a) {
     __shared__ uint32_t next[kSortWarps][256];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    for (int k = threadIdx.x; k < kSortWarps * 256; k += kSortThreads) (&next[0][0])[k] = 0;
+    __shared__ uint32_t part_before[kSortThreads], part_total[kSortThreads];
+    __shared__ uint32_t warp_total[8];
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    const int bins = 1 << a.bits;
+    const uint32_t mask = (uint32_t)bins - 1u;
+    for (int k = tid; k < kSortWarps * 256; k += kSortThreads) (&next[0][0])[k] = 0;
     __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * kSortTile + (int64_t)w * (kSortTile / kSortWarps);
-    const int64_t i1 = min(n, i0 + kSortTile / kSortWarps);
-    for (int64_t i = i0 + lane; i < i1; i += 32) atomicAdd(&next[w][(in[i].x >> shift) & 255u], 1u);
+    const int64_t i0 = (int64_t)blockIdx.x * a.tile + (int64_t)w * (a.tile / kSortWarps);
+    const int64_t i1 = min((int64_t)a.n, i0 + a.tile / kSortWarps);
+    for (int64_t i = i0 + lane; i < i1; i += 32) atomicAdd(&next[w][(sort_load<FIRST>(a, (int32_t)i).x >> a.shift) & mask], 1u);
+    {   // tiles before this one, and all tiles, per digit: thread t takes digit t % bins and every (threads / bins)-th tile
+        const int bin = tid & (int)mask, part = tid >> a.bits, parts = kSortThreads >> a.bits;
+        uint32_t before = 0, total = 0;
+#pragma unroll 8
+        for (int t = part; t < a.tiles; t += parts) {
+            const uint32_t c = a.counts[((int64_t)t << a.bits) + bin];
+            total += c;
+            before += t < (int)blockIdx.x ? c : 0;
+        }
+        part_before[tid] = before;
+        part_total[tid] = total;
+    }
     __syncthreads();
-    {
-        uint32_t at = offsets[(int64_t)threadIdx.x * tiles + blockIdx.x];
+    uint32_t at = 0, total = 0, incl = 0;
+    if (tid < 256) {
+        if (tid < bins)
+            for (int q = tid; q < kSortThreads; q += bins) {
+                at += part_before[q];
+                total += part_total[q];
+            }
+        incl = total;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        if (lane == 31) warp_total[w] = incl;
+    }
+    __syncthreads();
+    if (tid < bins) {
+        at += incl - total;
+        for (int k = 0; k < w; ++k) at += warp_total[k];
         for (int k = 0; k < kSortWarps; ++k) {
-            const uint32_t c = next[k][threadIdx.x];
-            next[k][threadIdx.x] = at;
+            const uint32_t c = next[k][tid];
+            next[k][tid] = at;
             at += c;
         }
     }
@@ -107,46 +138,215 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(int64_t n, c
     for (int64_t b = i0; b < i1; b += 32) {
         const int64_t i = b + lane;
         const bool live = i < i1;
-        const uint2 p = live ? in[i] : make_uint2(0, 0);
-        const uint32_t d = live ? (p.x >> shift) & 255u : 256u + lane;   // idle lanes match nobody
+        const uint2 p = live ? sort_load<FIRST>(a, (int32_t)i) : make_uint2(0, 0);
+        if (FIRST && live && p.x < (uint32_t)a.vocab) a.present[p.x] = 1;
+        const uint32_t d = live ? (p.x >> a.shift) & mask : 256u + lane;   // idle lanes match nobody
         const uint32_t peers = __match_any_sync(0xffffffffu, d);
         const uint32_t rank = __popc(peers & ((1u << lane) - 1u));
-        uint32_t at = 0;
-        if (live) at = next[w][d] + rank;
+        uint32_t to = 0;
+        if (live) to = next[w][d] + rank;
         __syncwarp();
         if (live && rank == 0) next[w][d] += __popc(peers);
         __syncwarp();
-        if (live) out[at] = p;
+        if (live) a.out[to] = p;
     }
 }
 
-__device__ int64_t lower_bound_key(const uint2* pairs, int64_t n, uint32_t key) {
-    int64_t lo = 0, hi = n;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (pairs[mid].x < key)
-            lo = mid + 1;
-        else
-            hi = mid;
+// ---- sums over the sorted positions -----------------------------------------------------------
+// A unit of L lanes takes R consecutive sorted positions and up to 4 L columns, gathers the rows of dout and adds them up
+// in registers.  An id whose positions lie inside the unit is finished there.  The sum of an id that reaches over the
+// unit's edges is left in shared memory; the CTA joins its units' sums in order, and what reaches over the CTA's edges goes
+// to the workspace, where embed_join_kernel joins it, again in order.  Work is split by positions, so an id that holds
+// half of them costs no more than others.
+constexpr int kSumThreads = 512;
+
+struct SumArgs {
+    int32_t n;
+    int64_t vocab;
+    int width, accumulate;
+    const uint2* pairs;
+    const float* dout;
+    int64_t dout_ld;
+    float* dtable;
+    int64_t dtable_ld;
+    float scale;
+    const uint8_t* present;
+    int32_t per_unit;        // R
+    int sum_ctas, zero_ctas;
+    float* head;             // [sum_ctas][width] sum of the id that comes in from the CTA before
+    float* tail;             // [sum_ctas][width] sum of the id that starts here and goes on in the next one
+    int4* info;              // [sum_ctas] {head present, head ends here, tail present, tail's id}
+};
+
+template <bool VEC>
+__device__ __forceinline__ void load4(const float* row, int col, int stride, int width, float (&v)[4]) {
+    if (VEC) {
+        const float4 t = __ldg(reinterpret_cast<const float4*>(row + col));
+        v[0] = t.x, v[1] = t.y, v[2] = t.z, v[3] = t.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = col + j * stride < width ? __ldg(row + col + j * stride) : 0.f;
     }
-    return lo;
+}
+template <bool VEC>
+__device__ __forceinline__ void store4(float* row, int col, int stride, int width, int accumulate, const float (&v)[4]) {
+    if (VEC) {
+        float4 t = make_float4(v[0], v[1], v[2], v[3]);
+        if (accumulate) {
+            const float4 o = *reinterpret_cast<const float4*>(row + col);
+            t.x += o.x, t.y += o.y, t.z += o.z, t.w += o.w;
+        }
+        *reinterpret_cast<float4*>(row + col) = t;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (col + j * stride < width) row[col + j * stride] = v[j] + (accumulate ? row[col + j * stride] : 0.f);
+    }
 }
 
-// One warp per row of dtable: the positions of its id, summed in order.
-__global__ void embed_reduce_kernel(int64_t n, int64_t vocab, int width, const uint2* pairs, const float* dout, int64_t dout_ld,
-                                    float* dtable, int64_t dtable_ld, float scale, int accumulate) {
-    const int lane = threadIdx.x & 31;
-    const int64_t v = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5;
-    if (v >= vocab) return;
-    const int64_t a = lower_bound_key(pairs, n, (uint32_t)v), b = lower_bound_key(pairs, n, (uint32_t)v + 1);
-    for (int c = lane; c < width; c += 32) {
-        float s = 0.f;
-        for (int64_t i = a; i < b; ++i) s += scale * __ldg(dout + (int64_t)pairs[i].y * dout_ld + c);
-        float* t = dtable + v * dtable_ld + c;
-        if (!accumulate)
-            *t = s;
-        else if (b > a)
-            *t += s;
+// VEC: lane l holds columns 4 l .. 4 l + 3 of the tile (16-byte accesses); else columns l, l + L, l + 2 L, l + 3 L
+template <int L, bool VEC>
+__global__ void __launch_bounds__(kSumThreads, 2) embed_sum_kernel(const SumArgs a) {
+    constexpr int U = kSumThreads / L;
+    __shared__ float sums[U][2][4 * L];
+    __shared__ int4 unit_info[U];   // {head present, head ends here, tail's id or -1, head's id}
+    const int tid = threadIdx.x, l = tid & (L - 1), unit = tid / L;
+    const int c0 = blockIdx.y * 4 * L;
+    const int col = c0 + (VEC ? 4 * l : l);
+    const bool live_col = col < a.width;
+    if ((int)blockIdx.x >= a.sum_ctas) {   // rows of ids that do not occur
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int64_t v = (int64_t)(blockIdx.x - a.sum_ctas) * U + unit; v < a.vocab; v += (int64_t)a.zero_ctas * U)
+            if (live_col && !a.present[v]) store4<VEC>(a.dtable + v * a.dtable_ld, col, L, a.width, 0, zero);
+        return;
+    }
+    const int64_t s = ((int64_t)blockIdx.x * U + unit) * a.per_unit, e = min((int64_t)a.n, s + a.per_unit);
+    const unsigned group = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((tid & 31) & ~(L - 1));
+    const uint32_t none = (uint32_t)a.vocab;
+    const uint32_t before = s > 0 && s < e ? a.pairs[s - 1].x : 0xffffffffu;
+    uint32_t key = 0xffffffffu;
+    bool first = true;             // still in the unit's first run
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    bool head = false, head_ends = false;
+    int head_id = -1, tail_id = -1;
+    auto put = [&](int which) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[unit][which][VEC ? 4 * l + j : l + j * L] = acc[j];
+    };
+    auto finish = [&](bool goes_on) {   // the run of `key` ends, or the unit does
+        if (key >= none) return;
+        if (first && key == before) {
+            head = true, head_ends = !goes_on, head_id = (int)key;
+            put(0);
+        } else if (goes_on) {
+            tail_id = (int)key;
+            put(1);
+        } else if (live_col) {
+            store4<VEC>(a.dtable + (int64_t)key * a.dtable_ld, col, L, a.width, a.accumulate, acc);
+        }
+    };
+    for (int64_t b = s; b < e; b += L) {
+        const uint2 mine = b + l < e ? a.pairs[b + l] : make_uint2(none, 0);
+        const int m = (int)min((int64_t)L, e - b);
+        for (int q = 0; q < m; q += 4) {
+            uint32_t k[4];
+            float v[4][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int src = min(q + j, m - 1);
+                k[j] = __shfl_sync(group, mine.x, src, L);
+                const uint32_t pos = __shfl_sync(group, mine.y, src, L);
+                if (q + j >= m) k[j] = none;
+                v[j][0] = v[j][1] = v[j][2] = v[j][3] = 0.f;
+                if (live_col && k[j] < none) load4<VEC>(a.dout + (int64_t)pos * a.dout_ld, col, L, a.width, v[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (q + j >= m) break;
+                if (k[j] != key) {
+                    if (key != 0xffffffffu) {
+                        finish(false);
+                        first = false;
+                    }
+                    key = k[j];
+                    acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[c] = fmaf(a.scale, v[j][c], acc[c]);
+            }
+        }
+    }
+    if (s < e) finish(e < a.n && a.pairs[e].x == key);
+    if (l == 0) unit_info[unit] = make_int4(head, head_ends, tail_id, head_id);
+    __syncthreads();
+    // one thread per column joins the units' sums in order
+    if (tid >= 4 * L || c0 + tid >= a.width) return;
+    float sum = 0.f;
+    bool open = false, started = false, any_head = false, ended = false;
+    int id = -1;
+    auto write = [&](int to, float v) {
+        float* t = a.dtable + (int64_t)to * a.dtable_ld + c0 + tid;
+        *t = v + (a.accumulate ? *t : 0.f);
+    };
+#pragma unroll 8
+    for (int k = 0; k < U; ++k) {
+        const int4 f = unit_info[k];
+        if (f.x) {
+            if (!open) open = true, started = false, sum = 0.f, any_head = true;
+            sum += sums[k][0][tid];
+            if (f.y) {
+                if (started)
+                    write(id, sum);
+                else
+                    a.head[(int64_t)blockIdx.x * a.width + c0 + tid] = sum, ended = true;
+                open = false;
+            }
+        }
+        if (f.z >= 0) open = true, started = true, sum = sums[k][1][tid], id = f.z;
+    }
+    const bool tail = open && started;
+    if (tail) a.tail[(int64_t)blockIdx.x * a.width + c0 + tid] = sum;
+    if (open && !started) a.head[(int64_t)blockIdx.x * a.width + c0 + tid] = sum;
+    if (tid == 0 && blockIdx.y == 0) a.info[blockIdx.x] = make_int4(any_head, ended, tail, id);
+}
+
+// The ids that reach over the edges of CTAs: eight groups of 32 columns each add a share of the CTAs in order, then the
+// shares are added in order.
+__global__ void __launch_bounds__(256) embed_join_kernel(const SumArgs a) {
+    __shared__ float part[8][32];
+    __shared__ int last;
+    const int4 f = a.info[blockIdx.x];
+    if (!f.z) return;
+    const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
+    if (threadIdx.x < 32) {   // the CTA in which the id ends
+        int c = blockIdx.x + 1;
+        for (;; c += 32) {
+            const int k = c + lane;
+            const bool stop = k >= a.sum_ctas || !a.info[k].x || a.info[k].y;
+            const unsigned hit = __ballot_sync(0xffffffffu, stop);
+            if (hit) {
+                c += __ffs(hit) - 1;
+                break;
+            }
+        }
+        if (lane == 0) last = min(c, a.sum_ctas - 1);
+    }
+    __syncthreads();
+    const int c = blockIdx.y * 32 + lane;
+    const int lo = blockIdx.x + 1, count = last - lo + 1, share = (count + 7) / 8;
+    float s = 0.f;
+    if (c < a.width) {
+        const int k1 = min(last + 1, lo + (g + 1) * share);
+#pragma unroll 8
+        for (int k = lo + g * share; k < k1; ++k) s += a.head[(int64_t)k * a.width + c];
+    }
+    part[g][lane] = s;
+    __syncthreads();
+    if (g == 0 && c < a.width) {
+        float t = a.tail[(int64_t)blockIdx.x * a.width + c];
+        for (int k = 0; k < 8; ++k) t += part[k][lane];
+        float* to = a.dtable + (int64_t)f.w * a.dtable_ld + c;
+        *to = t + (a.accumulate ? *to : 0.f);
     }
 }
 
@@ -160,16 +360,63 @@ slicegcn_status_t check_desc(const slicegcn_embed_desc* d, const char* who) {
 
 int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 
-struct SortLayout {
-    int64_t tiles, pairs_bytes, counts_bytes, total;
+// How the gradient is cut, and where its parts lie in the workspace.
+struct GradPlan {
+    int passes, bits, tiles;     // digit passes and bits per digit; CTAs of a pass
+    int32_t tile;                // positions per CTA of a pass
+    int lanes;                   // lanes per row of dout, four columns each
+    int col_tiles, sum_ctas, zero_ctas;
+    int32_t per_unit;            // sorted positions per unit of lanes
+    int64_t counts, present, head, tail, info, pairs[2], total;   // byte offsets
 };
-SortLayout sort_layout(const slicegcn_embed_desc* d) {
-    SortLayout L;
-    L.tiles = std::max<int64_t>(1, (d->n + kSortTile - 1) / kSortTile);
-    L.pairs_bytes = align256(d->n * (int64_t)sizeof(uint2));
-    L.counts_bytes = align256(L.tiles * 256 * (int64_t)sizeof(uint32_t));
-    L.total = 2 * L.pairs_bytes + L.counts_bytes;
-    return L;
+GradPlan grad_plan(const slicegcn_embed_desc* d) {
+    GradPlan p;
+    int key_bits = 1;
+    while ((d->vocab >> key_bits) > 0) ++key_bits;   // keys run up to vocab itself
+    p.passes = (key_bits + 7) / 8;
+    p.bits = (key_bits + p.passes - 1) / p.passes;
+    // one CTA per SM at most: every CTA of a pass reads all tiles' counts
+    const int64_t granule = kSortWarps * 32;
+    int64_t tile = (d->n + kSMs - 1) / kSMs;
+    tile = std::max<int64_t>(granule, (tile + granule - 1) / granule * granule);
+    p.tile = (int32_t)std::min<int64_t>(tile, (int64_t)1 << 30);
+    p.tiles = (int)std::max<int64_t>(1, (d->n + p.tile - 1) / p.tile);
+    const int quads = (d->width + 3) / 4;
+    p.lanes = 1;
+    while (p.lanes < 32 && p.lanes < quads) p.lanes *= 2;
+    p.col_tiles = (quads + p.lanes - 1) / p.lanes;
+    const int units = kSumThreads / p.lanes;
+    const int64_t want = std::max<int64_t>(1, kSMs * 2 / p.col_tiles);   // CTAs resident at once, over the column tiles
+    p.per_unit = (int32_t)std::max<int64_t>(8, (d->n + want * units - 1) / (want * units));
+    p.sum_ctas = (int)((d->n + (int64_t)p.per_unit * units - 1) / ((int64_t)p.per_unit * units));
+    p.zero_ctas = d->accumulate ? 0 : (int)std::min<int64_t>((d->vocab + units - 1) / units, kSMs * 2);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += align256(bytes);
+        return here;
+    };
+    p.counts = take(((int64_t)p.tiles << p.bits) * 4);
+    p.present = take(d->vocab + 16);
+    p.head = take((int64_t)p.sum_ctas * d->width * 4);
+    p.tail = take((int64_t)p.sum_ctas * d->width * 4);
+    p.info = take((int64_t)p.sum_ctas * 16);
+    p.pairs[0] = take(d->n * 8);
+    p.pairs[1] = take(d->n * 8);
+    p.total = at;
+    return p;
+}
+
+template <int L>
+slicegcn_status_t launch_sum(const SumArgs& a, bool vec, int col_tiles, cudaStream_t st) {
+    const dim3 grid(a.sum_ctas + a.zero_ctas, col_tiles);
+    if (vec)
+        embed_sum_kernel<L, true><<<grid, kSumThreads, 0, st>>>(a);
+    else
+        embed_sum_kernel<L, false><<<grid, kSumThreads, 0, st>>>(a);
+    SGCN_LAUNCH_CHECK();
+    count_launch();
+    return SLICEGCN_OK;
 }
 
 template <typename TT, typename TO>
@@ -210,7 +457,7 @@ slicegcn_status_t slicegcn_embed_forward(const slicegcn_embed_desc* d, const int
 slicegcn_status_t slicegcn_embed_workspace_bytes(const slicegcn_embed_desc* d, int64_t* bytes) {
     SGCN_TRY(check_desc(d, "embed_workspace_bytes"));
     if (!bytes) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "embed_workspace_bytes: NULL argument");
-    *bytes = sort_layout(d).total;
+    *bytes = grad_plan(d).total;
     return SLICEGCN_OK;
 }
 
@@ -221,33 +468,70 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
     if (!dtable || (d->n > 0 && (!ids || !dout))) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "embed_backward: NULL argument");
     if ((uintptr_t)ids % 4 || (uintptr_t)status % 4 || (uintptr_t)dout % 4 || (uintptr_t)dtable % 4 || (uintptr_t)workspace % 16)
         SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "embed_backward: a pointer is not aligned to its element type (workspace: 16 bytes)");
-    const SortLayout L = sort_layout(d);
-    if (!workspace || workspace_bytes < L.total)
-        SGCN_FAIL(SLICEGCN_ERR_ALLOC, "embed_backward: workspace too small (%lld < %lld bytes)", (long long)workspace_bytes, (long long)L.total);
+    const GradPlan p = grad_plan(d);
+    if (!workspace || workspace_bytes < p.total)
+        SGCN_FAIL(SLICEGCN_ERR_ALLOC, "embed_backward: workspace too small (%lld < %lld bytes)", (long long)workspace_bytes, (long long)p.total);
     cudaStream_t st = (cudaStream_t)stream;
     char* ws = static_cast<char*>(workspace);
-    uint2* a = reinterpret_cast<uint2*>(ws);
-    uint2* b = reinterpret_cast<uint2*>(ws + L.pairs_bytes);
-    uint32_t* counts = reinterpret_cast<uint32_t*>(ws + 2 * L.pairs_bytes);
-    if (d->n > 0) {
-        sort_init_kernel<<<(unsigned)std::min<int64_t>((d->n + 255) / 256, 148 * 16), 256, 0, st>>>(d->n, d->vocab, ids, a, status);
+    SortArgs a;
+    a.n = (int32_t)d->n;
+    a.vocab = d->vocab;
+    a.ids = ids;
+    a.counts = reinterpret_cast<uint32_t*>(ws + p.counts);
+    a.present = reinterpret_cast<uint8_t*>(ws + p.present);
+    a.status = status;
+    a.bits = p.bits;
+    a.tiles = p.tiles;
+    a.tile = p.tile;
+    uint2* buf[2] = {reinterpret_cast<uint2*>(ws + p.pairs[0]), reinterpret_cast<uint2*>(ws + p.pairs[1])};
+    for (int k = 0; k < p.passes; ++k) {
+        a.shift = k * p.bits;
+        a.in = buf[(k + 1) & 1];
+        a.out = buf[k & 1];
+        if (k == 0) {
+            sort_count_kernel<true><<<p.tiles, kSortThreads, 0, st>>>(a);
+            sort_scatter_kernel<true><<<p.tiles, kSortThreads, 0, st>>>(a);
+        } else {
+            sort_count_kernel<false><<<p.tiles, kSortThreads, 0, st>>>(a);
+            sort_scatter_kernel<false><<<p.tiles, kSortThreads, 0, st>>>(a);
+        }
         SGCN_LAUNCH_CHECK();
-        count_launch();
-        for (int shift = 0; (d->vocab >> shift) > 0; shift += 8) {   // keys run up to vocab itself
-            sort_count_kernel<<<(unsigned)L.tiles, kSortThreads, 0, st>>>(d->n, a, shift, (int)L.tiles, counts);
-            SGCN_LAUNCH_CHECK();
-            sort_scan_kernel<<<1, 1024, 0, st>>>(L.tiles * 256, counts);
-            SGCN_LAUNCH_CHECK();
-            sort_scatter_kernel<<<(unsigned)L.tiles, kSortThreads, 0, st>>>(d->n, a, shift, (int)L.tiles, counts, b);
-            SGCN_LAUNCH_CHECK();
-            count_launch(3);
-            std::swap(a, b);
+        count_launch(2);
+    }
+    SumArgs t;
+    t.n = (int32_t)d->n;
+    t.vocab = d->vocab;
+    t.width = d->width;
+    t.accumulate = d->accumulate;
+    t.pairs = buf[(p.passes + 1) & 1];
+    t.dout = dout;
+    t.dout_ld = d->dout_ld;
+    t.dtable = dtable;
+    t.dtable_ld = d->dtable_ld;
+    t.scale = (float)d->scale;
+    t.present = a.present;
+    t.per_unit = p.per_unit;
+    t.sum_ctas = p.sum_ctas;
+    t.zero_ctas = p.zero_ctas;
+    t.head = reinterpret_cast<float*>(ws + p.head);
+    t.tail = reinterpret_cast<float*>(ws + p.tail);
+    t.info = reinterpret_cast<int4*>(ws + p.info);
+    if (p.sum_ctas + p.zero_ctas > 0) {
+        const bool vec = d->width % 4 == 0 && d->dout_ld % 4 == 0 && d->dtable_ld % 4 == 0 && (uintptr_t)dout % 16 == 0 && (uintptr_t)dtable % 16 == 0;
+        switch (p.lanes) {
+            case 1: SGCN_TRY(launch_sum<1>(t, vec, p.col_tiles, st)); break;
+            case 2: SGCN_TRY(launch_sum<2>(t, vec, p.col_tiles, st)); break;
+            case 4: SGCN_TRY(launch_sum<4>(t, vec, p.col_tiles, st)); break;
+            case 8: SGCN_TRY(launch_sum<8>(t, vec, p.col_tiles, st)); break;
+            case 16: SGCN_TRY(launch_sum<16>(t, vec, p.col_tiles, st)); break;
+            default: SGCN_TRY(launch_sum<32>(t, vec, p.col_tiles, st)); break;
         }
     }
-    embed_reduce_kernel<<<(unsigned)((d->vocab + 7) / 8), 256, 0, st>>>(d->n, d->vocab, d->width, a, dout, d->dout_ld, dtable, d->dtable_ld,
-                                                                        (float)d->scale, d->accumulate);
-    SGCN_LAUNCH_CHECK();
-    count_launch();
+    if (p.sum_ctas > 1) {
+        embed_join_kernel<<<dim3(p.sum_ctas, (d->width + 31) / 32), 256, 0, st>>>(t);
+        SGCN_LAUNCH_CHECK();
+        count_launch();
+    }
     return SLICEGCN_OK;
 }
 
