@@ -54,7 +54,7 @@ struct SortArgs {
     const uint2* in;         // (key, position), read by the others
     uint2* out;
     uint32_t* counts;        // [tiles][bins]
-    uint8_t* present;        // [vocab] 1 where an id occurs; cleared by the first count, set by the first scatter
+    uint8_t* present;        // [vocab] cleared by the first count, see SumArgs
     int32_t* status;
     int shift, bits, tiles;
     int32_t tile;            // positions per tile, a multiple of kSortWarps * 32
@@ -139,7 +139,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
         const int64_t i = b + lane;
         const bool live = i < i1;
         const uint2 p = live ? sort_load<FIRST>(a, (int32_t)i) : make_uint2(0, 0);
-        if (FIRST && live && p.x < (uint32_t)a.vocab) a.present[p.x] = 1;
         const uint32_t d = live ? (p.x >> a.shift) & mask : 256u + lane;   // idle lanes match nobody
         const uint32_t peers = __match_any_sync(0xffffffffu, d);
         const uint32_t rank = __popc(peers & ((1u << lane) - 1u));
@@ -159,6 +158,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
 // to the workspace, where embed_join_kernel joins it, again in order.  Work is split by positions, so an id that holds
 // half of them costs no more than others.
 constexpr int kSumThreads = 512;
+constexpr int kAhead = 8;   // rows of dout requested before they are added
 
 struct SumArgs {
     int32_t n;
@@ -170,9 +170,10 @@ struct SumArgs {
     float* dtable;
     int64_t dtable_ld;
     float scale;
-    const uint8_t* present;
+    uint8_t* present;        // [vocab] set where an id occurs: once per run and unit, as setting it per position would
+                             // queue the positions of a frequent id up on one byte (200 us for 2.4 M positions)
     int32_t per_unit;        // R
-    int sum_ctas, zero_ctas;
+    int sum_ctas;
     float* head;             // [sum_ctas][width] sum of the id that comes in from the CTA before
     float* tail;             // [sum_ctas][width] sum of the id that starts here and goes on in the next one
     int4* info;              // [sum_ctas] {head present, head ends here, tail present, tail's id}
@@ -214,12 +215,6 @@ __global__ void __launch_bounds__(kSumThreads, 2) embed_sum_kernel(const SumArgs
     const int c0 = blockIdx.y * 4 * L;
     const int col = c0 + (VEC ? 4 * l : l);
     const bool live_col = col < a.width;
-    if ((int)blockIdx.x >= a.sum_ctas) {   // rows of ids that do not occur
-        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int64_t v = (int64_t)(blockIdx.x - a.sum_ctas) * U + unit; v < a.vocab; v += (int64_t)a.zero_ctas * U)
-            if (live_col && !a.present[v]) store4<VEC>(a.dtable + v * a.dtable_ld, col, L, a.width, 0, zero);
-        return;
-    }
     const int64_t s = ((int64_t)blockIdx.x * U + unit) * a.per_unit, e = min((int64_t)a.n, s + a.per_unit);
     const unsigned group = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((tid & 31) & ~(L - 1));
     const uint32_t none = (uint32_t)a.vocab;
@@ -238,7 +233,10 @@ __global__ void __launch_bounds__(kSumThreads, 2) embed_sum_kernel(const SumArgs
         if (first && key == before) {
             head = true, head_ends = !goes_on, head_id = (int)key;
             put(0);
-        } else if (goes_on) {
+            return;
+        }
+        if (a.present && l == 0 && blockIdx.y == 0) a.present[key] = 1;
+        if (goes_on) {
             tail_id = (int)key;
             put(1);
         } else if (live_col) {
@@ -248,20 +246,19 @@ __global__ void __launch_bounds__(kSumThreads, 2) embed_sum_kernel(const SumArgs
     for (int64_t b = s; b < e; b += L) {
         const uint2 mine = b + l < e ? a.pairs[b + l] : make_uint2(none, 0);
         const int m = (int)min((int64_t)L, e - b);
-        for (int q = 0; q < m; q += 4) {
-            uint32_t k[4];
-            float v[4][4];
+        for (int q = 0; q < m; q += kAhead) {
+            uint32_t k[kAhead];
+            float v[kAhead][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int src = min(q + j, m - 1);
+            for (int j = 0; j < kAhead; ++j) {
+                const int src = min(q + j, L - 1);             // lanes past m hold `none`
                 k[j] = __shfl_sync(group, mine.x, src, L);
                 const uint32_t pos = __shfl_sync(group, mine.y, src, L);
-                if (q + j >= m) k[j] = none;
                 v[j][0] = v[j][1] = v[j][2] = v[j][3] = 0.f;
                 if (live_col && k[j] < none) load4<VEC>(a.dout + (int64_t)pos * a.dout_ld, col, L, a.width, v[j]);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < kAhead; ++j) {
                 if (q + j >= m) break;
                 if (k[j] != key) {
                     if (key != 0xffffffffu) {
@@ -308,6 +305,17 @@ __global__ void __launch_bounds__(kSumThreads, 2) embed_sum_kernel(const SumArgs
     if (tail) a.tail[(int64_t)blockIdx.x * a.width + c0 + tid] = sum;
     if (open && !started) a.head[(int64_t)blockIdx.x * a.width + c0 + tid] = sum;
     if (tid == 0 && blockIdx.y == 0) a.info[blockIdx.x] = make_int4(any_head, ended, tail, id);
+}
+
+// Rows of ids that do not occur, as lane groups like those above.
+template <int L, bool VEC>
+__global__ void __launch_bounds__(256) embed_zero_kernel(const SumArgs a) {
+    const int l = threadIdx.x & (L - 1);
+    const int col = blockIdx.y * 4 * L + (VEC ? 4 * l : l);
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+    if (col >= a.width) return;
+    for (int64_t v = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L; v < a.vocab; v += (int64_t)gridDim.x * (256 / L))
+        if (!a.present[v]) store4<VEC>(a.dtable + v * a.dtable_ld, col, L, a.width, 0, zero);
 }
 
 // The ids that reach over the edges of CTAs: eight groups of 32 columns each add a share of the CTAs in order, then the
@@ -365,7 +373,7 @@ struct GradPlan {
     int passes, bits, tiles;     // digit passes and bits per digit; CTAs of a pass
     int32_t tile;                // positions per CTA of a pass
     int lanes;                   // lanes per row of dout, four columns each
-    int col_tiles, sum_ctas, zero_ctas;
+    int col_tiles, sum_ctas;
     int32_t per_unit;            // sorted positions per unit of lanes
     int64_t counts, present, head, tail, info, pairs[2], total;   // byte offsets
 };
@@ -389,7 +397,6 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
     const int64_t want = std::max<int64_t>(1, kSMs * 2 / p.col_tiles);   // CTAs resident at once, over the column tiles
     p.per_unit = (int32_t)std::max<int64_t>(8, (d->n + want * units - 1) / (want * units));
     p.sum_ctas = (int)((d->n + (int64_t)p.per_unit * units - 1) / ((int64_t)p.per_unit * units));
-    p.zero_ctas = d->accumulate ? 0 : (int)std::min<int64_t>((d->vocab + units - 1) / units, kSMs * 2);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -407,16 +414,32 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
     return p;
 }
 
-template <int L>
-slicegcn_status_t launch_sum(const SumArgs& a, bool vec, int col_tiles, cudaStream_t st) {
-    const dim3 grid(a.sum_ctas + a.zero_ctas, col_tiles);
-    if (vec)
-        embed_sum_kernel<L, true><<<grid, kSumThreads, 0, st>>>(a);
-    else
-        embed_sum_kernel<L, false><<<grid, kSumThreads, 0, st>>>(a);
-    SGCN_LAUNCH_CHECK();
-    count_launch();
+template <int L, bool VEC>
+slicegcn_status_t launch_sum(const SumArgs& a, int col_tiles, cudaStream_t st) {
+    if (a.sum_ctas > 0) {
+        embed_sum_kernel<L, VEC><<<dim3(a.sum_ctas, col_tiles), kSumThreads, 0, st>>>(a);
+        SGCN_LAUNCH_CHECK();
+        count_launch();
+    }
+    if (!a.accumulate) {
+        const unsigned blocks = (unsigned)std::min<int64_t>((a.vocab * L + 255) / 256, kSMs * 8);
+        embed_zero_kernel<L, VEC><<<dim3(blocks, col_tiles), 256, 0, st>>>(a);
+        SGCN_LAUNCH_CHECK();
+        count_launch();
+    }
     return SLICEGCN_OK;
+}
+
+template <bool VEC>
+slicegcn_status_t launch_sums(const SumArgs& a, int lanes, int col_tiles, cudaStream_t st) {
+    switch (lanes) {
+        case 1: return launch_sum<1, VEC>(a, col_tiles, st);
+        case 2: return launch_sum<2, VEC>(a, col_tiles, st);
+        case 4: return launch_sum<4, VEC>(a, col_tiles, st);
+        case 8: return launch_sum<8, VEC>(a, col_tiles, st);
+        case 16: return launch_sum<16, VEC>(a, col_tiles, st);
+        default: return launch_sum<32, VEC>(a, col_tiles, st);
+    }
 }
 
 template <typename TT, typename TO>
@@ -512,21 +535,11 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
     t.present = a.present;
     t.per_unit = p.per_unit;
     t.sum_ctas = p.sum_ctas;
-    t.zero_ctas = p.zero_ctas;
     t.head = reinterpret_cast<float*>(ws + p.head);
     t.tail = reinterpret_cast<float*>(ws + p.tail);
     t.info = reinterpret_cast<int4*>(ws + p.info);
-    if (p.sum_ctas + p.zero_ctas > 0) {
-        const bool vec = d->width % 4 == 0 && d->dout_ld % 4 == 0 && d->dtable_ld % 4 == 0 && (uintptr_t)dout % 16 == 0 && (uintptr_t)dtable % 16 == 0;
-        switch (p.lanes) {
-            case 1: SGCN_TRY(launch_sum<1>(t, vec, p.col_tiles, st)); break;
-            case 2: SGCN_TRY(launch_sum<2>(t, vec, p.col_tiles, st)); break;
-            case 4: SGCN_TRY(launch_sum<4>(t, vec, p.col_tiles, st)); break;
-            case 8: SGCN_TRY(launch_sum<8>(t, vec, p.col_tiles, st)); break;
-            case 16: SGCN_TRY(launch_sum<16>(t, vec, p.col_tiles, st)); break;
-            default: SGCN_TRY(launch_sum<32>(t, vec, p.col_tiles, st)); break;
-        }
-    }
+    const bool vec = d->width % 4 == 0 && d->dout_ld % 4 == 0 && d->dtable_ld % 4 == 0 && (uintptr_t)dout % 16 == 0 && (uintptr_t)dtable % 16 == 0;
+    SGCN_TRY(vec ? launch_sums<true>(t, p.lanes, p.col_tiles, st) : launch_sums<false>(t, p.lanes, p.col_tiles, st));
     if (p.sum_ctas > 1) {
         embed_join_kernel<<<dim3(p.sum_ctas, (d->width + 31) / 32), 256, 0, st>>>(t);
         SGCN_LAUNCH_CHECK();
