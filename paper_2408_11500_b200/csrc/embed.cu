@@ -157,8 +157,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
 // unit's edges is left in shared memory; the CTA joins its units' sums in order, and what reaches over the CTA's edges goes
 // to the workspace, where embed_join_kernel joins it, again in order.  Work is split by positions, so an id that holds
 // half of them costs no more than others.
-constexpr int kSumThreads = 512;
-constexpr int kAhead = 8;   // rows of dout requested before they are added
+constexpr int kSumThreads = 256;
+constexpr int kSumPerSM = 5;   // CTAs of them that fit an SM (41 KB of shared memory each)
+constexpr int kAhead = 8;      // rows of dout on their way per unit
 
 struct SumArgs {
     int32_t n;
@@ -179,14 +180,17 @@ struct SumArgs {
     int4* info;              // [sum_ctas] {head present, head ends here, tail present, tail's id}
 };
 
+// Four columns of a row on their way to shared memory, asynchronously; then from there.  A thread reads back only what it
+// asked for itself, so its own count of finished copies is all the waiting there is.
 template <bool VEC>
-__device__ __forceinline__ void load4(const float* row, int col, int stride, int width, float (&v)[4]) {
+__device__ __forceinline__ void request4(uint32_t slot, const float* row, int col, int stride, int width) {
     if (VEC) {
-        const float4 t = __ldg(reinterpret_cast<const float4*>(row + col));
-        v[0] = t.x, v[1] = t.y, v[2] = t.z, v[3] = t.w;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot), "l"(row + col) : "memory");
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = col + j * stride < width ? __ldg(row + col + j * stride) : 0.f;
+        for (int j = 0; j < 4; ++j)
+            if (col + j * stride < width)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(slot + 4 * j), "l"(row + col + j * stride) : "memory");
     }
 }
 template <bool VEC>
@@ -207,23 +211,27 @@ __device__ __forceinline__ void store4(float* row, int col, int stride, int widt
 
 // VEC: lane l holds columns 4 l .. 4 l + 3 of the tile (16-byte accesses); else columns l, l + L, l + 2 L, l + 3 L
 template <int L, bool VEC>
-__global__ void __launch_bounds__(kSumThreads, 2) embed_sum_kernel(const SumArgs a) {
+__global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const SumArgs a) {
     constexpr int U = kSumThreads / L;
+    constexpr int A = L < kAhead ? L : kAhead;   // rows on their way at any time, and positions per batch
+    __shared__ __align__(16) float ring[A][kSumThreads][4];
     __shared__ float sums[U][2][4 * L];
-    __shared__ int4 unit_info[U];   // {head present, head ends here, tail's id or -1, head's id}
+    __shared__ int4 unit_info[U];   // {head present, head ends here, tail's id or -1, unused}
     const int tid = threadIdx.x, l = tid & (L - 1), unit = tid / L;
     const int c0 = blockIdx.y * 4 * L;
     const int col = c0 + (VEC ? 4 * l : l);
     const bool live_col = col < a.width;
-    const int64_t s = ((int64_t)blockIdx.x * U + unit) * a.per_unit, e = min((int64_t)a.n, s + a.per_unit);
+    const int64_t s64 = ((int64_t)blockIdx.x * U + unit) * a.per_unit;
+    const int s = (int)min((int64_t)a.n, s64), e = (int)min((int64_t)a.n, s64 + a.per_unit);
     const unsigned group = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((tid & 31) & ~(L - 1));
     const uint32_t none = (uint32_t)a.vocab;
     const uint32_t before = s > 0 && s < e ? a.pairs[s - 1].x : 0xffffffffu;
+    const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(&ring[0][tid][0]);
     uint32_t key = 0xffffffffu;
     bool first = true;             // still in the unit's first run
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
     bool head = false, head_ends = false;
-    int head_id = -1, tail_id = -1;
+    int tail_id = -1;
     auto put = [&](int which) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) sums[unit][which][VEC ? 4 * l + j : l + j * L] = acc[j];
@@ -231,7 +239,7 @@ __global__ void __launch_bounds__(kSumThreads, 2) embed_sum_kernel(const SumArgs
     auto finish = [&](bool goes_on) {   // the run of `key` ends, or the unit does
         if (key >= none) return;
         if (first && key == before) {
-            head = true, head_ends = !goes_on, head_id = (int)key;
+            head = true, head_ends = !goes_on;
             put(0);
             return;
         }
@@ -243,38 +251,50 @@ __global__ void __launch_bounds__(kSumThreads, 2) embed_sum_kernel(const SumArgs
             store4<VEC>(a.dtable + (int64_t)key * a.dtable_ld, col, L, a.width, a.accumulate, acc);
         }
     };
-    for (int64_t b = s; b < e; b += L) {
-        const uint2 mine = b + l < e ? a.pairs[b + l] : make_uint2(none, 0);
-        const int m = (int)min((int64_t)L, e - b);
-        for (int q = 0; q < m; q += kAhead) {
-            uint32_t k[kAhead];
-            float v[kAhead][4];
+    auto batch = [&](int b) { return l < A && b + l < e ? a.pairs[b + l] : make_uint2(none, 0); };
+    auto request = [&](int i, const uint2& p) {   // row i of a batch into slot i
+        const uint32_t k = __shfl_sync(group, p.x, i, L), pos = __shfl_sync(group, p.y, i, L);
+        if (live_col && k < none)
+            request4<VEC>(my_ring + i * (int)sizeof(ring[0]), a.dout + (int64_t)pos * a.dout_ld, col, L, a.width);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    uint2 cur = batch(s), next = batch(s + A);
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const int src = min(q + j, L - 1);             // lanes past m hold `none`
-                k[j] = __shfl_sync(group, mine.x, src, L);
-                const uint32_t pos = __shfl_sync(group, mine.y, src, L);
-                v[j][0] = v[j][1] = v[j][2] = v[j][3] = 0.f;
-                if (live_col && k[j] < none) load4<VEC>(a.dout + (int64_t)pos * a.dout_ld, col, L, a.width, v[j]);
-            }
+    for (int i = 0; i < A - 1; ++i) request(i, cur);
+    for (int b = s; b < e; b += A) {
+        const uint2 later = batch(b + 2 * A);
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                if (q + j >= m) break;
-                if (k[j] != key) {
-                    if (key != 0xffffffffu) {
-                        finish(false);
-                        first = false;
-                    }
-                    key = k[j];
-                    acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+        for (int i = 0; i < A; ++i) {
+            // the slot read in the step before is free: the last row of this batch, then the next batch's rows
+            if (i == 0)
+                request(A - 1, cur);
+            else
+                request(i - 1, next);
+            if (b + i >= e) continue;
+            asm volatile("cp.async.wait_group %0;" ::"n"(A - 1) : "memory");
+            const uint32_t k = __shfl_sync(group, cur.x, i, L);
+            if (k != key) {
+                if (key != 0xffffffffu) {
+                    finish(false);
+                    first = false;
                 }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) acc[c] = fmaf(a.scale, v[j][c], acc[c]);
+                key = k;
+                acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+            }
+            if (live_col && k < none) {
+                const float4 v = *reinterpret_cast<const float4*>(&ring[i][tid][0]);
+                acc[0] = fmaf(a.scale, v.x, acc[0]);
+                if (VEC || col + L < a.width) acc[1] = fmaf(a.scale, v.y, acc[1]);
+                if (VEC || col + 2 * L < a.width) acc[2] = fmaf(a.scale, v.z, acc[2]);
+                if (VEC || col + 3 * L < a.width) acc[3] = fmaf(a.scale, v.w, acc[3]);
             }
         }
+        cur = next;
+        next = later;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (s < e) finish(e < a.n && a.pairs[e].x == key);
-    if (l == 0) unit_info[unit] = make_int4(head, head_ends, tail_id, head_id);
+    if (l == 0) unit_info[unit] = make_int4(head, head_ends, tail_id, 0);
     __syncthreads();
     // one thread per column joins the units' sums in order
     if (tid >= 4 * L || c0 + tid >= a.width) return;
@@ -390,11 +410,11 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
     p.tile = (int32_t)std::min<int64_t>(tile, (int64_t)1 << 30);
     p.tiles = (int)std::max<int64_t>(1, (d->n + p.tile - 1) / p.tile);
     const int quads = (d->width + 3) / 4;
-    p.lanes = 1;
+    p.lanes = 2;
     while (p.lanes < 32 && p.lanes < quads) p.lanes *= 2;
     p.col_tiles = (quads + p.lanes - 1) / p.lanes;
     const int units = kSumThreads / p.lanes;
-    const int64_t want = std::max<int64_t>(1, kSMs * 2 / p.col_tiles);   // CTAs resident at once, over the column tiles
+    const int64_t want = std::max<int64_t>(1, kSMs * kSumPerSM / p.col_tiles);   // CTAs resident at once, over the column tiles
     p.per_unit = (int32_t)std::max<int64_t>(8, (d->n + want * units - 1) / (want * units));
     p.sum_ctas = (int)((d->n + (int64_t)p.per_unit * units - 1) / ((int64_t)p.per_unit * units));
     int64_t at = 0;
@@ -433,7 +453,6 @@ slicegcn_status_t launch_sum(const SumArgs& a, int col_tiles, cudaStream_t st) {
 template <bool VEC>
 slicegcn_status_t launch_sums(const SumArgs& a, int lanes, int col_tiles, cudaStream_t st) {
     switch (lanes) {
-        case 1: return launch_sum<1, VEC>(a, col_tiles, st);
         case 2: return launch_sum<2, VEC>(a, col_tiles, st);
         case 4: return launch_sum<4, VEC>(a, col_tiles, st);
         case 8: return launch_sum<8, VEC>(a, col_tiles, st);
