@@ -12,6 +12,8 @@ namespace {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortItems = 8;       // positions a lane loads ahead
+constexpr int kMaxDigitBits = 9;    // 512 digits: one pass less for 17 and 18 key bits, 64 KB of counters per CTA
 constexpr int kSMs = 148;
 
 __device__ __forceinline__ float ld_elem(const float* p) { return __ldg(p); }
@@ -42,11 +44,6 @@ __global__ void embed_forward_kernel(int64_t n, int64_t vocab, int width, const 
 // Keys run from 0 to `vocab`: the id, or `vocab` (sorted last) for positions that take no part.  Per digit two launches:
 // sort_count_kernel counts every tile's digits, sort_scatter_kernel turns the counts into offsets (each CTA reads the whole
 // table of tiles x digits, a few hundred KB that stay in L2, so no scan launch stands between the two) and moves the pairs.
-__device__ __forceinline__ uint32_t sort_key(int32_t id, int64_t vocab, int32_t* status) {
-    const int32_t v = checked_id(id, vocab, status);
-    return v < 0 ? (uint32_t)vocab : (uint32_t)v;
-}
-
 struct SortArgs {
     int32_t n;
     int64_t vocab;
@@ -62,41 +59,54 @@ struct SortArgs {
 
 template <bool FIRST>
 __device__ __forceinline__ uint2 sort_load(const SortArgs& a, int32_t i) {
-    if (FIRST) return make_uint2(sort_key(a.ids[i], a.vocab, a.status), (uint32_t)i);
+    if (FIRST) return make_uint2(min((uint32_t)a.ids[i], (uint32_t)a.vocab), (uint32_t)i);   // a negative id is a large number
     return a.in[i];
 }
 
 template <bool FIRST>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
-    __shared__ uint32_t hist[256];
+    __shared__ uint32_t hist[1 << kMaxDigitBits];
     if (FIRST)
         for (int64_t i = (blockIdx.x * (int64_t)kSortThreads + threadIdx.x) * 16; i < a.vocab; i += (int64_t)gridDim.x * kSortThreads * 16)
             *reinterpret_cast<uint4*>(a.present + i) = make_uint4(0, 0, 0, 0);   // (rounded up to 16 bytes)
-    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+    if (threadIdx.x < 1 << kMaxDigitBits) hist[threadIdx.x] = 0;
     __syncthreads();
     const uint32_t mask = (1u << a.bits) - 1u;
     const int64_t i0 = (int64_t)blockIdx.x * a.tile, i1 = min((int64_t)a.n, i0 + a.tile);
-    for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads)
-        atomicAdd(&hist[(sort_load<FIRST>(a, (int32_t)i).x >> a.shift) & mask], 1u);
+#pragma unroll 4
+    for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads) {
+        const uint32_t key = sort_load<FIRST>(a, (int32_t)i).x;
+        if (FIRST && key == (uint32_t)a.vocab && a.status && a.ids[i] != -1) atomicExch(a.status, SLICEGCN_DEVSTATUS_BAD_ID);
+        atomicAdd(&hist[(key >> a.shift) & mask], 1u);
+    }
     __syncthreads();
     if (threadIdx.x <= mask) a.counts[((int64_t)blockIdx.x << a.bits) + threadIdx.x] = hist[threadIdx.x];
 }
 
 // Each warp owns a contiguous run of the tile and walks it 32 positions at a time; lanes with the same digit are ranked by
-// one match, so the order of equal digits is kept.
+// ballots, so the order of equal digits is kept.
 template <bool FIRST>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortArgs a) {
-    __shared__ uint32_t next[kSortWarps][256];
+    extern __shared__ uint32_t next[];   // [kSortWarps][bins] counts of each warp's run, then where its next pair goes
     __shared__ uint32_t part_before[kSortThreads], part_total[kSortThreads];
-    __shared__ uint32_t warp_total[8];
+    __shared__ uint32_t warp_total[kSortWarps];
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int bins = 1 << a.bits;
     const uint32_t mask = (uint32_t)bins - 1u;
-    for (int k = tid; k < kSortWarps * 256; k += kSortThreads) (&next[0][0])[k] = 0;
-    __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * a.tile + (int64_t)w * (a.tile / kSortWarps);
+    uint32_t* mine = next + w * bins;
+    for (int k = lane; k < bins; k += 32) mine[k] = 0;
+    __syncwarp();
+    const int64_t i0 = min((int64_t)a.n, (int64_t)blockIdx.x * a.tile + (int64_t)w * (a.tile / kSortWarps));
     const int64_t i1 = min((int64_t)a.n, i0 + a.tile / kSortWarps);
-    for (int64_t i = i0 + lane; i < i1; i += 32) atomicAdd(&next[w][(sort_load<FIRST>(a, (int32_t)i).x >> a.shift) & mask], 1u);
+    uint2 item[kSortItems];
+    for (int64_t b = i0; b < i1; b += 32 * kSortItems) {
+#pragma unroll
+        for (int j = 0; j < kSortItems; ++j)
+            if (b + 32 * j + lane < i1) item[j] = sort_load<FIRST>(a, (int32_t)(b + 32 * j + lane));
+#pragma unroll
+        for (int j = 0; j < kSortItems; ++j)
+            if (b + 32 * j + lane < i1) atomicAdd(&mine[(item[j].x >> a.shift) & mask], 1u);
+    }
     {   // tiles before this one, and all tiles, per digit: thread t takes digit t % bins and every (threads / bins)-th tile
         const int bin = tid & (int)mask, part = tid >> a.bits, parts = kSortThreads >> a.bits;
         uint32_t before = 0, total = 0;
@@ -110,44 +120,56 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
         part_total[tid] = total;
     }
     __syncthreads();
-    uint32_t at = 0, total = 0, incl = 0;
-    if (tid < 256) {
-        if (tid < bins)
-            for (int q = tid; q < kSortThreads; q += bins) {
-                at += part_before[q];
-                total += part_total[q];
-            }
-        incl = total;
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += t;
+    uint32_t at = 0, total = 0;
+    if (tid < bins)
+        for (int q = tid; q < kSortThreads; q += bins) {
+            at += part_before[q];
+            total += part_total[q];
         }
-        if (lane == 31) warp_total[w] = incl;
+    uint32_t incl = total;
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += t;
     }
+    if (lane == 31) warp_total[w] = incl;
     __syncthreads();
     if (tid < bins) {
         at += incl - total;
         for (int k = 0; k < w; ++k) at += warp_total[k];
+#pragma unroll 8
         for (int k = 0; k < kSortWarps; ++k) {
-            const uint32_t c = next[k][tid];
-            next[k][tid] = at;
+            const uint32_t c = next[k * bins + tid];
+            next[k * bins + tid] = at;
             at += c;
         }
     }
     __syncthreads();
-    for (int64_t b = i0; b < i1; b += 32) {
-        const int64_t i = b + lane;
-        const bool live = i < i1;
-        const uint2 p = live ? sort_load<FIRST>(a, (int32_t)i) : make_uint2(0, 0);
-        const uint32_t d = live ? (p.x >> a.shift) & mask : 256u + lane;   // idle lanes match nobody
-        const uint32_t peers = __match_any_sync(0xffffffffu, d);
-        const uint32_t rank = __popc(peers & ((1u << lane) - 1u));
-        uint32_t to = 0;
-        if (live) to = next[w][d] + rank;
-        __syncwarp();
-        if (live && rank == 0) next[w][d] += __popc(peers);
-        __syncwarp();
-        if (live) a.out[to] = p;
+    const bool whole = i1 - i0 <= 32 * kSortItems;   // the run still sits in registers
+    for (int64_t b = i0; b < i1; b += 32 * kSortItems) {
+        if (!whole)
+#pragma unroll
+            for (int j = 0; j < kSortItems; ++j)
+                if (b + 32 * j + lane < i1) item[j] = sort_load<FIRST>(a, (int32_t)(b + 32 * j + lane));
+#pragma unroll
+        for (int j = 0; j < kSortItems; ++j) {
+            if (b + 32 * j >= i1) break;
+            const bool live = b + 32 * j + lane < i1;
+            const uint32_t d = (item[j].x >> a.shift) & mask;
+            uint32_t peers = __ballot_sync(0xffffffffu, live);   // lanes with the same digit, bit by bit
+#pragma unroll
+            for (int k = 0; k < kMaxDigitBits; ++k) {
+                const bool set = (d >> k) & 1u;
+                const uint32_t with = __ballot_sync(0xffffffffu, set);
+                peers &= set ? with : ~with;
+            }
+            const uint32_t rank = __popc(peers & ((1u << lane) - 1u));
+            uint32_t to = 0;
+            if (live) to = mine[d] + rank;
+            __syncwarp();
+            if (live && rank == 0) mine[d] += __popc(peers);
+            __syncwarp();
+            if (live) a.out[to] = item[j];
+        }
     }
 }
 
@@ -401,7 +423,7 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
     GradPlan p;
     int key_bits = 1;
     while ((d->vocab >> key_bits) > 0) ++key_bits;   // keys run up to vocab itself
-    p.passes = (key_bits + 7) / 8;
+    p.passes = (key_bits + kMaxDigitBits - 1) / kMaxDigitBits;
     p.bits = (key_bits + p.passes - 1) / p.passes;
     // one CTA per SM at most: every CTA of a pass reads all tiles' counts
     const int64_t granule = kSortWarps * 32;
@@ -525,17 +547,21 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
     a.bits = p.bits;
     a.tiles = p.tiles;
     a.tile = p.tile;
+    constexpr int kMaxSmem = kSortWarps * 4 << kMaxDigitBits;
+    SGCN_CUDA(cudaFuncSetAttribute(sort_scatter_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem));
+    SGCN_CUDA(cudaFuncSetAttribute(sort_scatter_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem));
     uint2* buf[2] = {reinterpret_cast<uint2*>(ws + p.pairs[0]), reinterpret_cast<uint2*>(ws + p.pairs[1])};
     for (int k = 0; k < p.passes; ++k) {
         a.shift = k * p.bits;
         a.in = buf[(k + 1) & 1];
         a.out = buf[k & 1];
+        const size_t smem = (size_t)kSortWarps * 4 << p.bits;
         if (k == 0) {
             sort_count_kernel<true><<<p.tiles, kSortThreads, 0, st>>>(a);
-            sort_scatter_kernel<true><<<p.tiles, kSortThreads, 0, st>>>(a);
+            sort_scatter_kernel<true><<<p.tiles, kSortThreads, smem, st>>>(a);
         } else {
             sort_count_kernel<false><<<p.tiles, kSortThreads, 0, st>>>(a);
-            sort_scatter_kernel<false><<<p.tiles, kSortThreads, 0, st>>>(a);
+            sort_scatter_kernel<false><<<p.tiles, kSortThreads, smem, st>>>(a);
         }
         SGCN_LAUNCH_CHECK();
         count_launch(2);
