@@ -8,6 +8,7 @@
 //   dgate = D * s * v * sigmoid'(gate),  dy = J_N(y)^T (w_post * dt)
 //   dw_post = sum(dt * N(y)), db_post = sum(dt), dw_pre = sum(du * N(h)), db_pre = sum(du)   over the rows
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -20,19 +21,21 @@ struct NormArgs {
     float eps, s;
     int64_t x_ld, y_ld, gate_ld, h_ld, u_ld, dh_ld, du_ld, dx_ld, dy_ld, dgate_ld;
     const float *w_post, *b_post, *w_pre, *b_pre;
-    int64_t lanes_rows;   // rows that are worked on at a time: groups / p
+    int64_t lanes_rows;   // rows that are worked on at a time
     float* partial;       // gradient: [partial rows][4][p * w] column sums, or NULL when none is asked for
     int whole_rows;       // a CTA's groups cover whole rows: it leaves one partial row, not one per group
 };
 
-// ---- four columns of a slice row, as one access (VEC) or as four columns L apart ---------------
-// VEC needs rows whose slices start on boundaries of four elements; the last four columns may then reach past the slice
-// (one slice of 602 columns): what is read there is ignored, and such a quad is stored element by element.
-template <typename T>
-struct Quad;
+// ---- E columns of a slice row, neighbouring ones (VEC) or ones that lie L apart -----------------
+// VEC needs rows whose slices start on boundaries of E elements and takes 16 bytes of fp32 (E = 4), 8 or 16 of bf16 (E = 4,
+// 8) per access.  The last columns may reach past the slice (one slice of 602 columns): what is read there counts as zero,
+// and such a chunk is stored element by element.
+template <typename T, int E>
+struct Chunk;
 template <>
-struct Quad<float> {
+struct Chunk<float, 4> {
     float4 v;
+    __device__ __forceinline__ void clear() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w; }
     __device__ __forceinline__ void load(const float* p) { v = __ldcs(reinterpret_cast<const float4*>(p)); }
     static __device__ __forceinline__ void store(float* p, const float (&f)[4]) {
@@ -40,22 +43,44 @@ struct Quad<float> {
     }
     __device__ __forceinline__ void set(int j, float x) { (&v.x)[j] = x; }
 };
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t o;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(hi), "f"(lo));
+    return o;
+}
+template <int W>
+struct Words;   // W 32-bit words, one access
 template <>
-struct Quad<__nv_bfloat16> {
-    uint2 v;
-    __device__ __forceinline__ void get(float (&f)[4]) const {
-        f[0] = __uint_as_float(v.x << 16), f[1] = __uint_as_float(v.x & 0xffff0000u);
-        f[2] = __uint_as_float(v.y << 16), f[3] = __uint_as_float(v.y & 0xffff0000u);
+struct Words<2> {
+    using type = uint2;
+};
+template <>
+struct Words<4> {
+    using type = uint4;
+};
+template <int E>
+struct Chunk<__nv_bfloat16, E> {
+    using V = typename Words<E / 2>::type;
+    V v;
+    __device__ __forceinline__ const uint32_t& word(int k) const { return (&v.x)[k]; }
+    __device__ __forceinline__ uint32_t& word(int k) { return (&v.x)[k]; }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k) word(k) = 0;
     }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint2*>(p)); }
-    static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&f)[4]) {
-        uint2 o;
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.x) : "f"(f[1]), "f"(f[0]));
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o.y) : "f"(f[3]), "f"(f[2]));
-        __stcs(reinterpret_cast<uint2*>(p), o);
+    __device__ __forceinline__ void get(float (&f)[E]) const {
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k) f[2 * k] = __uint_as_float(word(k) << 16), f[2 * k + 1] = __uint_as_float(word(k) & 0xffff0000u);
+    }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const V*>(p)); }
+    static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&f)[E]) {
+        Chunk o;
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k) o.word(k) = pack_bf16(f[2 * k], f[2 * k + 1]);
+        __stcs(reinterpret_cast<V*>(p), o.v);
     }
     __device__ __forceinline__ void set(int j, float x) {   // x is a bf16 value
-        uint32_t& t = j < 2 ? v.x : v.y;
+        uint32_t& t = word(j >> 1);
         t = j & 1 ? (t & 0xffffu) | (__float_as_uint(x) & 0xffff0000u) : (t & 0xffff0000u) | (__float_as_uint(x) >> 16);
     }
 };
@@ -64,374 +89,788 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162f
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// `left` columns of the slice are at or after the first of the four
-template <typename T, bool VEC>
-__device__ __forceinline__ Quad<T> quad_load(const T* p, int step, int left) {
-    Quad<T> q;
-    q.v = {};
-    if (VEC) {
-        if (left > 0) q.load(p);
-    } else {
+// Columns of a thread: chunk i holds columns at(i), at(i) + step, ...; `left` columns of the slice follow the first one.
+template <bool VEC, int E>
+struct Columns {
+    int first, hop, step, left;   // of chunk 0; chunks lie `hop` apart
+    __device__ __forceinline__ Columns(int lane, int lanes, int w, bool idle)
+        : first(VEC ? E * lane : lane), hop(E * lanes), step(VEC ? 1 : lanes), left(idle ? 0 : w - first) {}
+    __device__ __forceinline__ int at(int i) const { return first + i * hop; }
+    __device__ __forceinline__ bool inside(int i, int j) const { return j * step < left - i * hop; }
+    template <typename T>
+    __device__ __forceinline__ void load(Chunk<T, E>& q, const T* row, int i, bool live) const {
+        q.clear();
+        if (VEC) {
+            if (live && inside(i, 0)) q.load(row + at(i));
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j * step < left) q.set(j, to_float(p[j * step]));
+            for (int j = 0; j < E; ++j)
+                if (live && inside(i, j)) q.set(j, to_float(row[at(i) + j * step]));
+        }
     }
-    return q;
-}
-template <typename T, bool VEC>
-__device__ __forceinline__ void quad_store(T* p, int step, int left, const float (&f)[4]) {
-    if (VEC && left >= 4) {
-        Quad<T>::store(p, f);
-    } else {
+    // what a chunk read past the slice becomes zero (VEC alone reads there)
+    __device__ __forceinline__ void trim(float (&f)[E], int i, bool ragged) const {
+        if (VEC && ragged)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j * (VEC ? 1 : step) < left) put(p + j * (VEC ? 1 : step), f[j]);
+            for (int j = 1; j < E; ++j) f[j] = inside(i, j) ? f[j] : 0.f;
     }
-}
-template <bool VEC>
-__device__ __forceinline__ void vector_load(const float* p, int step, int left, float otherwise, float (&f)[4]) {
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, int i, const float (&f)[E], bool ragged) const {
+        if (VEC && (!ragged || inside(i, E - 1))) {
+            if (inside(i, 0)) Chunk<T, E>::store(row + at(i), f);
+        } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = p && j * (VEC ? 1 : step) < left ? __ldg(p + j * (VEC ? 1 : step)) : otherwise;
-}
-
-// ---- sums over the lanes of one slice row -------------------------------------------------------
-// L = 1 .. 32: L neighbouring lanes of a warp (every lane of the warp takes part in the shuffles).  L = 0: the whole CTA;
-// two buffers in turn, so that one barrier per sum is enough.
-constexpr int kMaxNormWarps = 32;
+            for (int j = 0; j < E; ++j)
+                if (inside(i, j)) put(row + at(i) + j * step, f[j]);
+        }
+    }
+    // a vector of the columns (weight, bias), `otherwise` where there is none; zero past the slice
+    __device__ __forceinline__ void vector(const float* v, int i, float otherwise, float (&f)[E]) const {
+#pragma unroll
+        for (int j = 0; j < E; ++j) f[j] = !inside(i, j) ? 0.f : v ? __ldg(v + at(i) + j * step) : otherwise;
+    }
+};
+// sums over the L neighbouring lanes of one slice row (every lane of the warp takes part in the shuffles)
 template <int L, int K>
-__device__ __forceinline__ void group_sum(float (&v)[K], float (*smem)[kMaxNormWarps][4], int& turn) {
+__device__ __forceinline__ void group_sum(float (&v)[K]) {
 #pragma unroll
-    for (int o = (L ? L : 32) / 2; o > 0; o >>= 1)
+    for (int o = L / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-    if (L == 0) {
-        const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-        if (warps == 1) return;
-        if (lane == 0)
-#pragma unroll
-            for (int k = 0; k < K; ++k) smem[turn][threadIdx.x >> 5][k] = v[k];
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            v[k] = lane < warps ? smem[turn][lane][k] : 0.f;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-        }
-        turn ^= 1;
-    }
 }
 
-// sigmoid(g) = 1 / (1 + e^-g).  The hardware's exponential and division are good to a few units in the last place of fp32;
+// 2^x and 1 / x by the hardware's approximations (a few units in the last place of fp32, denormals as zero):
+// sigmoid(g) = 1 / (1 + e^-g) costs four instructions, where the exact forms would make the forward step issue-bound.
 // e^-g overflows to infinity for very negative g, which gives the right 0.
-__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float recip_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ __forceinline__ float sigmoid(float g) { return recip_fast(1.f + exp2_fast(-kLog2e * g)); }
 
-// Where a thread works: its group's slice, first row, and the columns of its quads.
+// Where a thread works: its group's slice and first row (then every lanes_rows-th).
 template <int L>
 struct Place {
     int lane, slice;
-    int64_t row;        // first row; then every lanes_rows-th
+    int64_t row;
     bool idle;
-    int64_t partial_row;
     __device__ __forceinline__ Place(const NormArgs& a) {
-        const int per_cta = L ? (int)blockDim.x / (L ? L : 1) : 1;
-        lane = L ? (int)threadIdx.x & (L - 1) : (int)threadIdx.x;
-        const int64_t g = (int64_t)blockIdx.x * per_cta + (L ? (int)threadIdx.x / (L ? L : 1) : 0);
+        lane = (int)threadIdx.x & (L - 1);
+        const int64_t g = (int64_t)blockIdx.x * (blockDim.x / L) + threadIdx.x / L;
         row = g / a.p;
         slice = (int)(g - row * a.p);
         idle = row >= a.lanes_rows;
-        partial_row = row;
     }
 };
 
+// Columns past the slice hold zeros in every array below, so that sums need no tests; a mean is taken off with a factor
+// that is zero there.
+template <typename T, bool VEC, int E, int L, int NV>
+__device__ __forceinline__ float centre_and_scale(float (&t)[NV][E], const float (&in)[NV][E], const NormArgs& a, float inv_w) {
+    float sum[1] = {0.f};
+    if (a.layer) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < E; ++j) sum[0] += t[i][j];
+        group_sum<L>(sum);
+        const float mean = sum[0] * inv_w;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < E; ++j) t[i][j] = fmaf(-mean, in[i][j], t[i][j]);
+        sum[0] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum[0] = fmaf(t[i][j], t[i][j], sum[0]);
+    group_sum<L>(sum);
+    return rsqrtf(fmaf(sum[0], inv_w, a.eps));
+}
+
 // Bound by HBM: x, y and gate are read once, h and u written once.  A slice row lives in the registers of its lanes from
-// the first load to the last store, so both norms cost shuffles and no second pass; the next row is requested before this
-// one is worked on.  NV = 1: four columns per lane, whose weights stay in registers over all rows.
-template <typename T, bool VEC, int L, int NV>
-__global__ void __launch_bounds__(L ? 256 : 1024) norm_forward_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
-    __shared__ float smem[2][kMaxNormWarps][4];
-    int turn = 0;
-    const Place<L> at(a);
-    const int lanes = L ? L : blockDim.x;
-    const int c0 = at.slice * a.w, c = VEC ? 4 * at.lane : at.lane, step = lanes, hop = 4 * lanes;   // quad i: columns c + i hop ...
+// the first load to the last store, so both norms cost shuffles and no second pass; with one chunk per lane the next row is
+// requested before this one is worked on, and the weights stay in registers over all rows.
+template <typename T, bool VEC, int E, int L, int NV>
+__global__ void __launch_bounds__(256) norm_forward_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
+    const Place<L> place(a);
+    const Columns<VEC, E> cols(place.lane, L, a.w, place.idle);
+    const int c0 = place.slice * a.w;
     const float inv_w = 1.f / (float)a.w;
-    const int left = at.idle ? 0 : a.w - c;
-    float wp[4], bp[4], wq[4], bq[4];
+    const bool ragged = a.w % E != 0;
+    float wp[E], bp[E], wq[E], bq[E], in[NV][E];
     auto weights_post = [&](int i) {
-        vector_load<VEC>(a.w_post ? a.w_post + c0 + c + i * hop : nullptr, step, left - i * hop, 1.f, wp);
-        vector_load<VEC>(a.b_post ? a.b_post + c0 + c + i * hop : nullptr, step, left - i * hop, 0.f, bp);
+        cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, wp);
+        cols.vector(a.b_post ? a.b_post + c0 : nullptr, i, 0.f, bp);
     };
     auto weights_pre = [&](int i) {
-        vector_load<VEC>(a.w_pre ? a.w_pre + c0 + c + i * hop : nullptr, step, left - i * hop, 1.f, wq);
-        vector_load<VEC>(a.b_pre ? a.b_pre + c0 + c + i * hop : nullptr, step, left - i * hop, 0.f, bq);
+        cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, wq);
+        cols.vector(a.b_pre ? a.b_pre + c0 : nullptr, i, 0.f, bq);
     };
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < E; ++j) in[i][j] = cols.inside(i, j) ? 1.f : 0.f;
     if (NV == 1) weights_post(0), weights_pre(0);
-    Quad<T> qx[NV], qy[NV], qg[NV];
+    Chunk<T, E> qx[NV], qy[NV], qg[NV];
     auto request = [&](int64_t row) {
         const bool live = row < a.n;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int rest = live ? left - i * hop : 0;
-            const int64_t k = c0 + c + i * hop;
-            if (y) qy[i] = quad_load<T, VEC>(y + row * a.y_ld + k, step, rest);
-            if (gate) qg[i] = quad_load<T, VEC>(gate + row * a.gate_ld + k, step, rest);
-            if (x) qx[i] = quad_load<T, VEC>(x + row * a.x_ld + k, step, rest);
+            if (y) cols.load(qy[i], y + row * a.y_ld + c0, i, live);
+            if (gate) cols.load(qg[i], gate + row * a.gate_ld + c0, i, live);
+            if (x) cols.load(qx[i], x + row * a.x_ld + c0, i, live);
         }
     };
-    request(at.row);
+    if (NV == 1) request(place.row);
     const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;   // the same for all lanes
     for (int64_t r = 0; r < rounds; ++r) {
-        const int64_t row = at.row + r * a.lanes_rows;
+        const int64_t row = place.row + r * a.lanes_rows;
         const bool live = row < a.n;
-        float v[NV][4], t[NV][4], gt[NV][4];
+        if (NV > 1) request(row);
+        float v[NV][E], t[NV][E], gt[NV][E];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (x)
-                qx[i].get(v[i]);
-            else
-                v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0.f;
-            if (y) qy[i].get(t[i]);
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[i][j] = 0.f;
+            if (x) qx[i].get(v[i]), cols.trim(v[i], i, ragged);
+            if (y) qy[i].get(t[i]), cols.trim(t[i], i, ragged);
             if (gate) qg[i].get(gt[i]);
         }
-        if (r + 1 < rounds) request(row + a.lanes_rows);
+        if (NV == 1 && r + 1 < rounds) request(row + a.lanes_rows);
         if (y) {
-            float sum[1] = {0.f}, mean = 0.f;
-            if (a.layer) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (j * (VEC ? 1 : step) < left - i * hop) sum[0] += t[i][j];
-                group_sum<L>(sum, smem, turn);
-                mean = sum[0] * inv_w;
-                sum[0] = 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    t[i][j] -= mean;
-                    if (j * (VEC ? 1 : step) < left - i * hop) sum[0] = fmaf(t[i][j], t[i][j], sum[0]);
-                }
-            group_sum<L>(sum, smem, turn);
-            const float ry = rsqrtf(fmaf(sum[0], inv_w, a.eps));
+            const float ry = centre_and_scale<T, VEC, E, L, NV>(t, in, a, inv_w);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 if (NV > 1) weights_post(i);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < E; ++j) {
                     float b = fmaf(t[i][j] * ry, wp[j], bp[j]);
                     if (gate) b *= sigmoid(gt[i][j]);
                     v[i][j] = fmaf(a.s, b, v[i][j]);
                 }
             }
+            if (gate) {   // a gate read past the slice is anything: 0 * NaN must not come into the sums
+#pragma unroll
+                for (int i = 0; i < NV; ++i) cols.trim(v[i], i, ragged);
+            }
         }
         if (h && live)
 #pragma unroll
-            for (int i = 0; i < NV; ++i) quad_store<T, VEC>(h + row * a.h_ld + c0 + c + i * hop, step, left - i * hop, v[i]);
+            for (int i = 0; i < NV; ++i) cols.store(h + row * a.h_ld + c0, i, v[i], ragged);
         if (!u) continue;
-        float sum[1] = {0.f}, mean = 0.f;
-        if (a.layer) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j * (VEC ? 1 : step) < left - i * hop) sum[0] += v[i][j];
-            group_sum<L>(sum, smem, turn);
-            mean = sum[0] * inv_w;
-            sum[0] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[i][j] -= mean;
-                if (j * (VEC ? 1 : step) < left - i * hop) sum[0] = fmaf(v[i][j], v[i][j], sum[0]);
-            }
-        group_sum<L>(sum, smem, turn);
-        const float rh = rsqrtf(fmaf(sum[0], inv_w, a.eps));
+        const float rh = centre_and_scale<T, VEC, E, L, NV>(v, in, a, inv_w);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (NV > 1) weights_pre(i);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[i][j] = fmaf(v[i][j] * rh, wq[j], bq[j]);
-            if (live) quad_store<T, VEC>(u + row * a.u_ld + c0 + c + i * hop, step, left - i * hop, v[i]);
+            for (int j = 0; j < E; ++j) v[i][j] = fmaf(v[i][j] * rh, wq[j], bq[j]);
+            if (live) cols.store(u + row * a.u_ld + c0, i, v[i], ragged);
         }
     }
 }
 
+// Slices of more than 1024 columns: a warp per slice row passes over it three times (four for the layer norm), and finds it
+// in L2 from the second time on.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) norm_forward_wide_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
+    constexpr int E = 4;
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (item >= a.n * a.p) return;
+    const int64_t row = item / a.p;
+    const int c0 = (int)(item - row * a.p) * a.w;
+    const Columns<VEC, E> cols(threadIdx.x & 31, 32, a.w, false);
+    const bool ragged = a.w % E != 0;
+    const float inv_w = 1.f / (float)a.w;
+    const int chunks = (a.w + 127) / 128;
+    auto get = [&](const T* from, int i, float(&f)[E]) {
+        Chunk<T, E> q;
+        cols.load(q, from, i, true);
+        q.get(f);
+        cols.trim(f, i, ragged);
+    };
+    float my = 0.f, ry = 0.f, sum[1];
+    if (y) {
+        if (a.layer) {
+            sum[0] = 0.f;
+#pragma unroll 4
+            for (int i = 0; i < chunks; ++i) {
+                float f[E];
+                get(y + row * a.y_ld + c0, i, f);
+#pragma unroll
+                for (int j = 0; j < E; ++j) sum[0] += f[j];
+            }
+            group_sum<32>(sum);
+            my = sum[0] * inv_w;
+        }
+        sum[0] = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < chunks; ++i) {
+            float f[E];
+            get(y + row * a.y_ld + c0, i, f);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float t = cols.inside(i, j) ? f[j] - my : 0.f;
+                sum[0] = fmaf(t, t, sum[0]);
+            }
+        }
+        group_sum<32>(sum);
+        ry = rsqrtf(fmaf(sum[0], inv_w, a.eps));
+    }
+    auto step = [&](int i, float(&v)[E]) {   // unrounded h, zero past the slice
+        float t[E], g[E], wp[E], bp[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = 0.f;
+        if (x) get(x + row * a.x_ld + c0, i, v);
+        if (!y) return;
+        get(y + row * a.y_ld + c0, i, t);
+        if (gate) get(gate + row * a.gate_ld + c0, i, g);
+        cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, wp);
+        cols.vector(a.b_post ? a.b_post + c0 : nullptr, i, 0.f, bp);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            float b = fmaf((t[j] - my) * ry, wp[j], bp[j]);
+            if (gate) b *= sigmoid(g[j]);
+            v[j] = cols.inside(i, j) ? fmaf(a.s, b, v[j]) : 0.f;
+        }
+    };
+    float mh = 0.f, rh = 0.f;
+    if (u) {
+        if (a.layer) {
+            sum[0] = 0.f;
+#pragma unroll 2
+            for (int i = 0; i < chunks; ++i) {
+                float v[E];
+                step(i, v);
+#pragma unroll
+                for (int j = 0; j < E; ++j) sum[0] += v[j];
+            }
+            group_sum<32>(sum);
+            mh = sum[0] * inv_w;
+        }
+        sum[0] = 0.f;
+#pragma unroll 2
+        for (int i = 0; i < chunks; ++i) {
+            float v[E];
+            step(i, v);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float t = cols.inside(i, j) ? v[j] - mh : 0.f;
+                sum[0] = fmaf(t, t, sum[0]);
+            }
+        }
+        group_sum<32>(sum);
+        rh = rsqrtf(fmaf(sum[0], inv_w, a.eps));
+    }
+#pragma unroll 2
+    for (int i = 0; i < chunks; ++i) {   // h may be x: an element is read before it is written, and by the same lane
+        float v[E];
+        step(i, v);
+        if (h) cols.store(h + row * a.h_ld + c0, i, v, ragged);
+        if (u) {
+            float wq[E], bq[E];
+            cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, wq);
+            cols.vector(a.b_pre ? a.b_pre + c0 : nullptr, i, 0.f, bq);
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[j] = fmaf((v[j] - mh) * rh, wq[j], bq[j]);
+            cols.store(u + row * a.u_ld + c0, i, v, ragged);
+        }
+    }
+}
+
+// sigmoid(g) and its slope e / (1 + e)^2 from e = e^-|g|: neither cancels
+__device__ __forceinline__ void gate_and_slope(float g, float& open, float& slope) {
+    const float e = exp2_fast(-kLog2e * fabsf(g)), f = recip_fast(1.f + e);
+    open = g < 0.f ? e * f : f;
+    slope = e * f * f;
+}
+
 // Bound by HBM as well: y, gate, h, dh and du are read once, dx, dy and dgate written once.  The sums over a slice are
 // taken together as far as they can be: (means), then squares of h and y with the products of du w_pre, then the
-// products of dt w_post.  The columns' sums over the rows stay in registers until the end.
-template <typename T, bool VEC, int L, int NV>
-__global__ void __launch_bounds__(L ? 256 : NV == 1 ? 1024 : 1024) norm_backward_kernel(const NormArgs a, const T* y, const T* gate, const T* h,
-                                                                                     const float* dh, const float* du, float* dx,
-                                                                                     float* dy, float* dgate) {
-    __shared__ float smem[2][kMaxNormWarps][4];
-    int turn = 0;
-    const Place<L> at(a);
-    const int lanes = L ? L : blockDim.x;
-    const int c0 = at.slice * a.w, c = VEC ? 4 * at.lane : at.lane, step = lanes, hop = 4 * lanes;
+// products of dt w_post.  Slices of up to 128 columns: four per lane, whose sums over the rows stay in registers until the
+// end, as do the weights; the next row is requested before this one is worked on.
+template <typename T, bool VEC, int L>
+__global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a, const T* y, const T* gate, const T* h, const float* dh,
+                                                               const float* du, float* dx, float* dy, float* dgate) {
+    constexpr int E = 4;
+    const Place<L> place(a);
+    const Columns<VEC, E> cols(place.lane, L, a.w, place.idle);
+    const int c0 = place.slice * a.w;
     const float inv_w = 1.f / (float)a.w;
-    const int left = at.idle ? 0 : a.w - c;
-    float wp[4], bp[4], wq[4];
-    auto weights = [&](int i) {
-        vector_load<VEC>(a.w_post ? a.w_post + c0 + c + i * hop : nullptr, step, left - i * hop, 1.f, wp);
-        vector_load<VEC>(a.b_post ? a.b_post + c0 + c + i * hop : nullptr, step, left - i * hop, 0.f, bp);
-        vector_load<VEC>(a.w_pre ? a.w_pre + c0 + c + i * hop : nullptr, step, left - i * hop, 1.f, wq);
-    };
-    if (NV == 1) weights(0);
-    float acc[4][NV][4];   // dw_post, db_post, dw_pre, db_pre
+    const bool ragged = a.w % E != 0;
+    const int all = a.p * a.w;
+    float wp[E], bp[E], wq[E], in[E];
+    cols.vector(a.w_post ? a.w_post + c0 : nullptr, 0, 1.f, wp);
+    cols.vector(a.b_post ? a.b_post + c0 : nullptr, 0, 0.f, bp);
+    cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, 0, 1.f, wq);
+    float acc[4][E];   // dw_post, db_post, dw_pre, db_pre
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[k][i][j] = 0.f;
-    Quad<T> qy[NV], qg[NV], qh[NV];
-    Quad<float> qd[NV], qu[NV];
+    for (int j = 0; j < E; ++j) {
+        in[j] = cols.inside(0, j) ? 1.f : 0.f;
+        acc[0][j] = acc[1][j] = acc[2][j] = acc[3][j] = 0.f;
+    }
+    Chunk<T, E> qy, qg, qh;
+    Chunk<float, E> qd, qu;
     auto request = [&](int64_t row) {
         const bool live = row < a.n;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int rest = live ? left - i * hop : 0;
-            const int64_t k = c0 + c + i * hop;
-            if (du) qh[i] = quad_load<T, VEC>(h + row * a.h_ld + k, step, rest);
-            if (du) qu[i] = quad_load<float, VEC>(du + row * a.du_ld + k, step, rest);
-            if (y) qy[i] = quad_load<T, VEC>(y + row * a.y_ld + k, step, rest);
-            if (dh) qd[i] = quad_load<float, VEC>(dh + row * a.dh_ld + k, step, rest);
-            if (gate) qg[i] = quad_load<T, VEC>(gate + row * a.gate_ld + k, step, rest);
-        }
+        if (du) cols.load(qh, h + row * a.h_ld + c0, 0, live);
+        if (du) cols.load(qu, du + row * a.du_ld + c0, 0, live);
+        if (y) cols.load(qy, y + row * a.y_ld + c0, 0, live);
+        if (dh) cols.load(qd, dh + row * a.dh_ld + c0, 0, live);
+        if (gate) cols.load(qg, gate + row * a.gate_ld + c0, 0, live);
     };
-    auto inside = [&](int i, int j) { return j * (VEC ? 1 : step) < left - i * hop; };
-    request(at.row);
+    request(place.row);
     const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;
     for (int64_t r = 0; r < rounds; ++r) {
-        const int64_t row = at.row + r * a.lanes_rows;
-        const bool live = row < a.n && !at.idle;
-        float hv[NV][4], uv[NV][4], yv[NV][4], d[NV][4], gv[NV][4];
+        const int64_t row = place.row + r * a.lanes_rows;
+        const bool live = row < a.n && !place.idle;
+        float hv[E], uv[E], yv[E], d[E], gv[E];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) hv[i][j] = uv[i][j] = yv[i][j] = d[i][j] = gv[i][j] = 0.f;
-            if (du) qh[i].get(hv[i]), qu[i].get(uv[i]);
-            if (y) qy[i].get(yv[i]);
-            if (dh) qd[i].get(d[i]);
-            if (gate) qg[i].get(gv[i]);
-        }
+        for (int j = 0; j < E; ++j) hv[j] = uv[j] = yv[j] = d[j] = gv[j] = 0.f;
+        if (du) qh.get(hv), qu.get(uv), cols.trim(hv, 0, ragged), cols.trim(uv, 0, ragged);
+        if (y) qy.get(yv), cols.trim(yv, 0, ragged);
+        if (dh) qd.get(d), cols.trim(d, 0, ragged);
+        if (gate) qg.get(gv), cols.trim(gv, 0, ragged);
         if (r + 1 < rounds) request(row + a.lanes_rows);
         if (a.layer) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int j = 0; j < E; ++j) m[0] += hv[j], m[1] += yv[j];
+            group_sum<L>(m);
+            m[0] *= inv_w, m[1] *= inv_w;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (inside(i, j)) m[0] += hv[i][j], m[1] += yv[i][j];
-            group_sum<L>(m, smem, turn);
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) hv[i][j] -= m[0] * inv_w, yv[i][j] -= m[1] * inv_w;
+            for (int j = 0; j < E; ++j) hv[j] = fmaf(-m[0], in[j], hv[j]), yv[j] = fmaf(-m[1], in[j], yv[j]);
         }
         float q[4] = {0.f, 0.f, 0.f, 0.f};   // squares of h and y, sum of du w_pre, of its product with h
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (NV > 1) weights(i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (inside(i, j)) {
-                    const float g = uv[i][j] * wq[j];
-                    q[0] = fmaf(hv[i][j], hv[i][j], q[0]);
-                    q[1] = fmaf(yv[i][j], yv[i][j], q[1]);
-                    q[2] += g;
-                    q[3] = fmaf(g, hv[i][j], q[3]);
-                }
+        for (int j = 0; j < E; ++j) {
+            const float g = uv[j] * wq[j];
+            q[0] = fmaf(hv[j], hv[j], q[0]);
+            q[1] = fmaf(yv[j], yv[j], q[1]);
+            q[2] += g;
+            q[3] = fmaf(g, hv[j], q[3]);
         }
-        group_sum<L>(q, smem, turn);
+        group_sum<L>(q);
         const float rh = rsqrtf(fmaf(q[0], inv_w, a.eps)), ry = rsqrtf(fmaf(q[1], inv_w, a.eps));
         const float mg = a.layer ? q[2] * inv_w : 0.f, mgh = q[3] * inv_w * rh;
         float z[2] = {0.f, 0.f};             // sum of dt w_post, of its product with y
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (NV > 1) weights(i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (du) {
-                    const float hhat = hv[i][j] * rh;
-                    d[i][j] = fmaf(rh, uv[i][j] * wq[j] - mg - hhat * mgh, d[i][j]);
-                    if (live && inside(i, j)) {
-                        acc[2][i][j] = fmaf(uv[i][j], hhat, acc[2][i][j]);
-                        acc[3][i][j] += uv[i][j];
-                    }
-                }
-                if (y) {
-                    // sigmoid and its slope e / (1 + e)^2 from e = e^-|g|: neither cancels
-                    float open = 1.f, slope = 0.f;
-                    if (gate) {
-                        const float e = __expf(-fabsf(gv[i][j])), f = __fdividef(1.f, 1.f + e);
-                        open = gv[i][j] >= 0.f ? f : e * f;
-                        slope = e * f * f;
-                        if (gv[i][j] != gv[i][j]) open = slope = gv[i][j];
-                    }
-                    const float ds = d[i][j] * a.s, yhat = yv[i][j] * ry, dt = ds * open;
-                    gv[i][j] = ds * slope * fmaf(yhat, wp[j], bp[j]);
-                    uv[i][j] = dt * wp[j];
-                    if (inside(i, j)) {
-                        z[0] += uv[i][j];
-                        z[1] = fmaf(uv[i][j], yv[i][j], z[1]);
-                        if (live) {
-                            acc[0][i][j] = fmaf(dt, yhat, acc[0][i][j]);
-                            acc[1][i][j] += dt;
-                        }
-                    }
-                }
+        for (int j = 0; j < E; ++j) {
+            if (du) {
+                const float hhat = hv[j] * rh;
+                d[j] = fmaf(rh, fmaf(-mg, in[j], uv[j] * wq[j]) - hhat * mgh, d[j]);
+                acc[2][j] = fmaf(uv[j], hhat, acc[2][j]);
+                acc[3][j] += uv[j];
             }
-            const int64_t k = c0 + c + i * hop;
-            if (dx && live) quad_store<float, VEC>(dx + row * a.dx_ld + k, step, left - i * hop, d[i]);
-            if (dgate && live) quad_store<float, VEC>(dgate + row * a.dgate_ld + k, step, left - i * hop, gv[i]);
+            if (y) {
+                float open = 1.f, slope = 0.f;
+                if (gate) gate_and_slope(gv[j], open, slope);
+                const float ds = d[j] * a.s, yhat = yv[j] * ry, dt = ds * open;
+                gv[j] = ds * slope * fmaf(yhat, wp[j], bp[j]);
+                uv[j] = dt * wp[j];
+                z[0] += uv[j];
+                z[1] = fmaf(uv[j], yv[j], z[1]);
+                acc[0][j] = fmaf(dt, yhat, acc[0][j]);
+                acc[1][j] += dt;
+            }
         }
+        if (dx && live) cols.store(dx + row * a.dx_ld + c0, 0, d, ragged);
+        if (dgate && live) cols.store(dgate + row * a.dgate_ld + c0, 0, gv, ragged);
         if (!dy) continue;
-        group_sum<L>(z, smem, turn);
+        group_sum<L>(z);
         const float mt = a.layer ? z[0] * inv_w : 0.f, mty = z[1] * inv_w * ry;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) yv[i][j] = ry * (uv[i][j] - mt - yv[i][j] * ry * mty);
-            if (live) quad_store<float, VEC>(dy + row * a.dy_ld + c0 + c + i * hop, step, left - i * hop, yv[i]);
-        }
+        for (int j = 0; j < E; ++j) yv[j] = ry * (uv[j] - mt - yv[j] * ry * mty);
+        if (live) cols.store(dy + row * a.dy_ld + c0, 0, yv, ragged);
     }
     if (!a.partial) return;
-    const int cols = a.p * a.w;
-    if (L && a.whole_rows) {
+    if (a.whole_rows) {
         // the CTA's groups of one slice lie p apart: their sums are added in order, and one partial row is left
-        __shared__ float sums[256][4];
-        const int per_slice = a.p * (L ? L : 1);
+        __shared__ float sums[256][E];
+        const int per_slice = a.p * L;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sums[threadIdx.x][j] = acc[k][0][j];
+            for (int j = 0; j < E; ++j) sums[threadIdx.x][j] = acc[k][j];
             __syncthreads();
             if ((int)threadIdx.x < per_slice) {
-                float t[4] = {0.f, 0.f, 0.f, 0.f};
+                float t[E] = {0.f, 0.f, 0.f, 0.f};
                 for (int o = threadIdx.x; o < 256; o += per_slice)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) t[j] += sums[o][j];
-                float* out = a.partial + ((int64_t)blockIdx.x * 4 + k) * cols + c0 + c;
+                    for (int j = 0; j < E; ++j) t[j] += sums[o][j];
+                float* out = a.partial + ((int64_t)blockIdx.x * 4 + k) * all + c0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (inside(0, j)) out[j * (VEC ? 1 : step)] = t[j];
+                for (int j = 0; j < E; ++j)
+                    if (cols.inside(0, j)) out[cols.at(0) + j * cols.step] = t[j];
             }
         }
         return;
     }
-    if (at.idle) return;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 4; ++k) {
+        float* out = a.partial + (place.row * 4 + k) * all + c0;
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (cols.inside(0, j)) out[cols.at(0) + j * cols.step] = acc[k][j];
+    }
+}
+
+// Slices of 129 to 1024 columns that allow accesses of four elements: a warp per slice row, whose five inputs are copied to
+// shared memory asynchronously one row ahead.  Every lane copies, and reads back, its own columns only (4 lane + 128 i), so
+// no barrier stands in the loop.  The row is read from shared memory in each of the passes over it, which leaves the
+// registers to the columns' sums (BIAS: those of the biases too).  A CTA works on one slice: its warps' sums are added in
+// order at the end.
+constexpr int kStagedWarps = 8;
+__device__ __forceinline__ void copy_async(uint32_t to, const float* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async(uint32_t to, const __nv_bfloat16* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void staged_get(const unsigned char* at, float (&f)[4]) {
+    Chunk<T, 4> q;
+    q.v = *reinterpret_cast<const decltype(q.v)*>(at);
+    q.get(f);
+}
+// bytes of one row of a warp: dh, du in fp32 and y, gate, h in T, 32 lanes x NV chunks each
+template <typename T, int NV>
+struct Staged {
+    static constexpr int kF = NV * 32 * 16, kT = NV * 32 * 4 * (int)sizeof(T);
+    static constexpr int kDh = 0, kDu = kF, kY = 2 * kF, kGate = kY + kT, kH = kGate + kT, kRow = kH + kT;
+    static constexpr int kVectors = 3 * NV * 32 * 16;                             // w_post, b_post, w_pre
+    static constexpr int smem(int warps) { return kVectors + warps * 2 * kRow; }
+};
+template <typename T, int NV, bool BIAS>
+__global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel(const NormArgs a, const T* y, const T* gate, const T* h,
+                                                                                 const float* dh, const float* du, float* dx, float* dy,
+                                                                                 float* dgate) {
+    using S = Staged<T, NV>;
+    constexpr int E = 4;
+    extern __shared__ __align__(16) unsigned char stage[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int slice = blockIdx.x % a.p;
+    const int64_t first = (int64_t)(blockIdx.x / a.p) * warps + warp;             // then every lanes_rows-th row
+    const int c0 = slice * a.w;
+    const Columns<true, E> cols(lane, 32, a.w, false);
+    const bool ragged = a.w % E != 0;
+    const float inv_w = 1.f / (float)a.w;
+    float(*vec)[NV][32][E] = reinterpret_cast<float(*)[NV][32][E]>(stage);
+    unsigned char* mine = stage + S::kVectors + warp * 2 * S::kRow;
+    const uint32_t mine_u = (uint32_t)__cvta_generic_to_shared(mine);
+    if (warp == 0)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float f[E];
+            cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, f);
+#pragma unroll
+            for (int j = 0; j < E; ++j) vec[0][i][lane][j] = f[j];
+            cols.vector(a.b_post ? a.b_post + c0 : nullptr, i, 0.f, f);
+#pragma unroll
+            for (int j = 0; j < E; ++j) vec[1][i][lane][j] = f[j];
+            cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, f);
+#pragma unroll
+            for (int j = 0; j < E; ++j) vec[2][i][lane][j] = f[j];
+        }
+    // columns past the slice are never copied: they stay zero
+    for (int k = lane * 16; k < 2 * S::kRow; k += 512) *reinterpret_cast<uint4*>(mine + k) = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    auto request = [&](int64_t row, int buf) {
+        if (row < a.n) {
+            const uint32_t to = mine_u + buf * S::kRow;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (cols.inside(i, 0)) {
+                    const int o = i * 32 + lane, c = c0 + cols.at(i);
+                    if (du) copy_async(to + S::kH + o * E * (int)sizeof(T), h + row * a.h_ld + c);
+                    if (y) copy_async(to + S::kY + o * E * (int)sizeof(T), y + row * a.y_ld + c);
+                    if (du) copy_async(to + S::kDu + o * 16, du + row * a.du_ld + c);
+                    if (dh) copy_async(to + S::kDh + o * 16, dh + row * a.dh_ld + c);
+                    if (gate) copy_async(to + S::kGate + o * E * (int)sizeof(T), gate + row * a.gate_ld + c);
+                }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    float acc[BIAS ? 4 : 2][NV][E];   // dw_post, dw_pre, db_post, db_pre
+#pragma unroll
+    for (int k = 0; k < (BIAS ? 4 : 2); ++k)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (inside(i, j)) a.partial[(at.partial_row * 4 + k) * cols + c0 + c + i * hop + j * (VEC ? 1 : step)] = acc[k][i][j];
+            for (int j = 0; j < E; ++j) acc[k][i][j] = 0.f;
+    request(first, 0);
+    int buf = 0;
+    for (int64_t row = first; row < a.n; row += a.lanes_rows, buf ^= 1) {
+        request(row + a.lanes_rows, buf ^ 1);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        const unsigned char* in = mine + buf * S::kRow;
+        const unsigned char* own_f = in + lane * 16;
+        const unsigned char* own_t = in + lane * E * sizeof(T);
+        constexpr int HF = 512, HT = 32 * E * (int)sizeof(T);   // bytes from one chunk of a lane to its next
+        float mh = 0.f, my = 0.f, f[E];
+        if (a.layer) {
+            float m[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                staged_get<T>(own_t + S::kH + i * HT, f), cols.trim(f, i, ragged);
+#pragma unroll
+                for (int j = 0; j < E; ++j) m[0] += f[j];
+                staged_get<T>(own_t + S::kY + i * HT, f), cols.trim(f, i, ragged);
+#pragma unroll
+                for (int j = 0; j < E; ++j) m[1] += f[j];
+            }
+            group_sum<32>(m);
+            mh = m[0] * inv_w, my = m[1] * inv_w;
+        }
+        float q[4] = {0.f, 0.f, 0.f, 0.f};   // squares of h and y, sum of du w_pre, of its product with h
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float hv[E], uv[E], yv[E];
+            staged_get<T>(own_t + S::kH + i * HT, hv);
+            staged_get<float>(own_f + S::kDu + i * HF, uv);
+            staged_get<T>(own_t + S::kY + i * HT, yv);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                if (!cols.inside(i, j)) continue;
+                const float g = uv[j] * vec[2][i][lane][j], hc = hv[j] - mh, yc = yv[j] - my;
+                q[0] = fmaf(hc, hc, q[0]);
+                q[1] = fmaf(yc, yc, q[1]);
+                q[2] += g;
+                q[3] = fmaf(g, hc, q[3]);
+            }
+        }
+        group_sum<32>(q);
+        const float rh = rsqrtf(fmaf(q[0], inv_w, a.eps)), ry = rsqrtf(fmaf(q[1], inv_w, a.eps));
+        const float mg = a.layer ? q[2] * inv_w : 0.f, mgh = q[3] * inv_w * rh;
+        float t[NV][E], z[2] = {0.f, 0.f};   // dt w_post; its sum, and that of its product with y
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float hv[E], uv[E], yv[E], d[E], gv[E];
+            staged_get<T>(own_t + S::kH + i * HT, hv);
+            staged_get<float>(own_f + S::kDu + i * HF, uv);
+            staged_get<T>(own_t + S::kY + i * HT, yv);
+            staged_get<float>(own_f + S::kDh + i * HF, d);
+            staged_get<T>(own_t + S::kGate + i * HT, gv);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const bool is = cols.inside(i, j);
+                t[i][j] = 0.f;
+                if (du) {
+                    const float hhat = (hv[j] - mh) * rh;
+                    d[j] = fmaf(rh, fmaf(uv[j], vec[2][i][lane][j], -mg) - hhat * mgh, d[j]);
+                    if (is) {
+                        acc[1][i][j] = fmaf(uv[j], hhat, acc[1][i][j]);
+                        if (BIAS) acc[BIAS ? 3 : 1][i][j] += uv[j];
+                    }
+                }
+                if (y) {
+                    float open = 1.f, slope = 0.f;
+                    if (gate) gate_and_slope(gv[j], open, slope);
+                    const float ds = d[j] * a.s, yc = yv[j] - my, yhat = yc * ry, dt = ds * open, w = vec[0][i][lane][j];
+                    gv[j] = ds * slope * fmaf(yhat, w, vec[1][i][lane][j]);
+                    t[i][j] = dt * w;
+                    if (is) {
+                        z[0] += t[i][j];
+                        z[1] = fmaf(t[i][j], yc, z[1]);
+                        acc[0][i][j] = fmaf(dt, yhat, acc[0][i][j]);
+                        if (BIAS) acc[BIAS ? 2 : 0][i][j] += dt;
+                    }
+                }
+            }
+            if (dx) cols.store(dx + row * a.dx_ld + c0, i, d, ragged);
+            if (dgate) cols.store(dgate + row * a.dgate_ld + c0, i, gv, ragged);
+        }
+        if (!dy) continue;
+        group_sum<32>(z);
+        const float mt = a.layer ? z[0] * inv_w : 0.f, mty = z[1] * inv_w * ry;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float yv[E];
+            staged_get<T>(own_t + S::kY + i * HT, yv);
+#pragma unroll
+            for (int j = 0; j < E; ++j) yv[j] = ry * (t[i][j] - mt - (yv[j] - my) * ry * mty);
+            cols.store(dy + row * a.dy_ld + c0, i, yv, ragged);
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!a.partial) return;
+    const int all = a.p * a.w;
+    float(*sums)[NV][32][E] = reinterpret_cast<float(*)[NV][32][E]>(stage + S::kVectors);   // [warp]
+#pragma unroll
+    for (int k = 0; k < (BIAS ? 4 : 2); ++k) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < E; ++j) sums[warp][i][lane][j] = acc[k][i][j];
+        __syncthreads();
+        const int which = BIAS ? (k == 0 ? 0 : k == 1 ? 2 : k == 2 ? 1 : 3) : 2 * k;   // order of the partial rows
+        float* out = a.partial + ((int64_t)(blockIdx.x / a.p) * 4 + which) * all + c0;
+        for (int c = threadIdx.x; c < a.w; c += blockDim.x) {
+            float s = 0.f;
+            for (int v = 0; v < warps; ++v) s += (&sums[v][0][0][0])[c];   // chunk i of lane l holds columns 128 i + 4 l ...
+            out[c] = s;
+        }
+    }
+}
+
+// All other slices (wider ones, or wide ones that allow no accesses of four elements).  First a warp per slice row takes
+// the sums over the row, reading it twice (the second time from L2); then every thread applies them to columns of its own
+// for many rows, whose sums it keeps in registers.
+struct RowStats {
+    float mh, rh, mg, mgh, my, ry, mt, mty;
+};
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) norm_stats_kernel(const NormArgs a, const T* y, const T* gate, const T* h, const float* dh,
+                                                         const float* du, RowStats* stats) {
+    constexpr int E = 4;
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (item >= a.n * a.p) return;
+    const int64_t row = item / a.p;
+    const int c0 = (int)(item - row * a.p) * a.w, lane = threadIdx.x & 31;
+    const Columns<VEC, E> cols(lane, 32, a.w, false);
+    const bool ragged = a.w % E != 0;
+    const float inv_w = 1.f / (float)a.w;
+    const int chunks = (a.w + 127) / 128;
+    auto get = [&](auto* from, int i, float(&f)[E]) {
+        Chunk<typename std::remove_cv<typename std::remove_pointer<decltype(from)>::type>::type, E> q;
+        cols.load(q, from, i, true);
+        q.get(f);
+        cols.trim(f, i, ragged);
+    };
+    RowStats s{};
+    if (a.layer) {
+        float m[2] = {0.f, 0.f};
+        for (int i = 0; i < chunks; ++i) {
+            float f[E];
+            if (du) {
+                get(h + row * a.h_ld + c0, i, f);
+                for (int j = 0; j < E; ++j) m[0] += f[j];
+            }
+            if (y) {
+                get(y + row * a.y_ld + c0, i, f);
+                for (int j = 0; j < E; ++j) m[1] += f[j];
+            }
+        }
+        group_sum<32>(m);
+        s.mh = m[0] * inv_w, s.my = m[1] * inv_w;
+    }
+    float q[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+    for (int i = 0; i < chunks; ++i) {
+        float hv[E] = {0.f, 0.f, 0.f, 0.f}, uv[E] = {0.f, 0.f, 0.f, 0.f}, yv[E] = {0.f, 0.f, 0.f, 0.f}, wq[E];
+        if (du) get(h + row * a.h_ld + c0, i, hv), get(du + row * a.du_ld + c0, i, uv);
+        if (y) get(y + row * a.y_ld + c0, i, yv);
+        cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, wq);
+        for (int j = 0; j < E; ++j) {
+            if (!cols.inside(i, j)) continue;
+            const float g = uv[j] * wq[j], hc = hv[j] - s.mh, yc = yv[j] - s.my;
+            q[0] = fmaf(hc, hc, q[0]);
+            q[1] = fmaf(yc, yc, q[1]);
+            q[2] += g;
+            q[3] = fmaf(g, hc, q[3]);
+        }
+    }
+    group_sum<32>(q);
+    s.rh = rsqrtf(fmaf(q[0], inv_w, a.eps)), s.ry = rsqrtf(fmaf(q[1], inv_w, a.eps));
+    s.mg = a.layer ? q[2] * inv_w : 0.f, s.mgh = q[3] * inv_w * s.rh;
+    if (y) {
+        float z[2] = {0.f, 0.f};
+#pragma unroll 2
+        for (int i = 0; i < chunks; ++i) {
+            float hv[E] = {0.f, 0.f, 0.f, 0.f}, uv[E] = {0.f, 0.f, 0.f, 0.f}, d[E] = {0.f, 0.f, 0.f, 0.f}, yv[E], gv[E], wq[E], wp[E];
+            if (du) get(h + row * a.h_ld + c0, i, hv), get(du + row * a.du_ld + c0, i, uv);
+            if (dh) get(dh + row * a.dh_ld + c0, i, d);
+            get(y + row * a.y_ld + c0, i, yv);
+            if (gate) get(gate + row * a.gate_ld + c0, i, gv);
+            cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, wq);
+            cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, wp);
+            for (int j = 0; j < E; ++j) {
+                if (!cols.inside(i, j)) continue;
+                if (du) d[j] = fmaf(s.rh, fmaf(uv[j], wq[j], -s.mg) - (hv[j] - s.mh) * s.rh * s.mgh, d[j]);
+                const float t = d[j] * a.s * (gate ? sigmoid(gv[j]) : 1.f) * wp[j];
+                z[0] += t;
+                z[1] = fmaf(t, yv[j] - s.my, z[1]);
+            }
+        }
+        group_sum<32>(z);
+        s.mt = a.layer ? z[0] * inv_w : 0.f, s.mty = z[1] * inv_w * s.ry;
+    }
+    if (lane == 0) stats[item] = s;
+}
+
+// blockIdx.x: 128 columns of one slice per warp; blockIdx.y: every gridDim.y-th row
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) norm_apply_kernel(const NormArgs a, const T* y, const T* gate, const T* h, const float* dh,
+                                                         const float* du, float* dx, float* dy, float* dgate, const RowStats* stats) {
+    constexpr int E = 4;
+    const int per_slice = (a.w + 127) / 128;
+    const int tile = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (tile >= per_slice * a.p) return;
+    const int slice = tile / per_slice, i = tile - slice * per_slice, c0 = slice * a.w;
+    const Columns<VEC, E> cols(threadIdx.x & 31, 32, a.w, false);
+    const bool ragged = a.w % E != 0;
+    float wp[E], bp[E], wq[E], acc[4][E];
+    cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, wp);
+    cols.vector(a.b_post ? a.b_post + c0 : nullptr, i, 0.f, bp);
+    cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, wq);
+#pragma unroll
+    for (int j = 0; j < E; ++j) acc[0][j] = acc[1][j] = acc[2][j] = acc[3][j] = 0.f;
+#pragma unroll 2
+    for (int64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
+        Chunk<T, E> qy, qg, qh;
+        Chunk<float, E> qd, qu;
+        const RowStats s = stats[row * a.p + slice];
+        if (du) cols.load(qh, h + row * a.h_ld + c0, i, true), cols.load(qu, du + row * a.du_ld + c0, i, true);
+        if (y) cols.load(qy, y + row * a.y_ld + c0, i, true);
+        if (dh) cols.load(qd, dh + row * a.dh_ld + c0, i, true);
+        if (gate) cols.load(qg, gate + row * a.gate_ld + c0, i, true);
+        float hv[E], uv[E], yv[E], d[E] = {0.f, 0.f, 0.f, 0.f}, gv[E] = {0.f, 0.f, 0.f, 0.f};
+        if (dh) qd.get(d);
+        if (gate) qg.get(gv);
+        if (du) {
+            qh.get(hv), qu.get(uv);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float hhat = (hv[j] - s.mh) * s.rh;
+                d[j] = fmaf(s.rh, fmaf(uv[j], wq[j], -s.mg) - hhat * s.mgh, d[j]);
+                acc[2][j] = fmaf(uv[j], hhat, acc[2][j]);
+                acc[3][j] += uv[j];
+            }
+        }
+        if (dx) cols.store(dx + row * a.dx_ld + c0, i, d, ragged);
+        if (!y) continue;
+        qy.get(yv);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            float open = 1.f, slope = 0.f;
+            if (gate) gate_and_slope(gv[j], open, slope);
+            const float ds = d[j] * a.s, yhat = (yv[j] - s.my) * s.ry, dt = ds * open;
+            gv[j] = ds * slope * fmaf(yhat, wp[j], bp[j]);
+            yv[j] = s.ry * (dt * wp[j] - s.mt - yhat * s.mty);
+            acc[0][j] = fmaf(dt, yhat, acc[0][j]);
+            acc[1][j] += dt;
+        }
+        if (dgate) cols.store(dgate + row * a.dgate_ld + c0, i, gv, ragged);
+        if (dy) cols.store(dy + row * a.dy_ld + c0, i, yv, ragged);
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float* out = a.partial + ((int64_t)blockIdx.y * 4 + k) * (a.p * a.w) + c0;
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (cols.inside(i, j)) out[cols.at(i) + j * cols.step] = acc[k][j];
+    }
 }
 
 // partial rows -> column sums: 32 columns per CTA, 32 warps that take every 32nd row, then the warps in order
@@ -491,97 +930,173 @@ NormArgs make_args(const slicegcn_residual_norm_desc* d) {
     return a;
 }
 
-// How a call is cut: lanes per slice row (0: a CTA per slice row), quads per lane, threads and CTAs.
 constexpr int kSMs = 148;
-struct NormPlan {
-    int lanes, quads, threads;
+constexpr int kMaxWarpWidth = 1024;   // columns of a slice that one warp holds (forward: in registers, gradient: in shared memory)
+
+// Forward, up to 1024 columns.  E: columns per chunk; lanes per slice row and chunks per lane.
+struct ForwardPlan {
+    int lanes, chunks;
+    int64_t ctas, lanes_rows;
+};
+int64_t rows_at_a_time(int64_t ctas, int groups, int p) { return ctas * groups / p; }
+int lanes_for(int need) {
+    int lanes = 1;
+    while (lanes < 32 && lanes < need) lanes *= 2;
+    return lanes;
+}
+ForwardPlan forward_plan(const slicegcn_residual_norm_desc* d, int E) {
+    ForwardPlan p;
+    const int need = (d->h_s + E - 1) / E;
+    p.lanes = lanes_for(need);
+    p.chunks = 1;
+    while (p.chunks * p.lanes < need) p.chunks *= 2;
+    const int groups = 256 / p.lanes;
+    const int64_t items = d->n * d->num_slices;
+    p.ctas = std::max<int64_t>(std::min<int64_t>((items + groups - 1) / groups, 8 * kSMs), (d->num_slices + groups - 1) / groups);
+    p.lanes_rows = rows_at_a_time(p.ctas, groups, d->num_slices);
+    return p;
+}
+
+// Gradient.  The workspace holds the partial rows of the columns' sums and, for the third form, the rows' statistics.  Its
+// size must not depend on the matrices' alignment, which decides between the second and the third.
+enum { kByLanes, kStaged, kTwoPasses };
+struct BackwardPlan {
+    int form;
+    int lanes;                         // kByLanes: lanes per slice row
+    int chunks, warps, smem;           // kStaged: chunks per lane, warps per CTA
     int64_t ctas, lanes_rows;
     int whole_rows;
-    int64_t partial_rows;
+    int64_t partial_rows, stats_bytes;
 };
-NormPlan norm_plan(const slicegcn_residual_norm_desc* d, bool backward) {
-    NormPlan p;
-    const int need = (d->h_s + 3) / 4;   // quads per slice row
-    p.quads = 1;
-    p.lanes = 1;
-    while (p.lanes < 32 && p.lanes < need) p.lanes *= 2;
-    p.threads = 256;
-    if (need > 32) {
-        if (!backward && need <= 256) {
-            // a warp per slice row, up to eight quads per lane: no barriers
-            while (p.quads * 32 < need) p.quads *= 2;
-        } else {
-            p.lanes = 0;
-            // the gradient keeps four column sums per column in registers: few columns per thread
-            const int per = backward ? 1024 : 256;
-            while (p.quads < 4 && need > per * p.quads) p.quads *= 2;
-            p.threads = ((need + p.quads - 1) / p.quads + 31) / 32 * 32;
-        }
+constexpr int kApplyRows = 4 * kSMs;   // kTwoPasses: partial rows at most
+template <typename T, int NV>
+int staged_smem(int warps) { return Staged<T, NV>::smem(warps); }
+int staged_smem_for(int dtype, int chunks, int warps) {
+    const bool bf = dtype == SLICEGCN_BF16;
+    switch (chunks) {
+        case 2: return bf ? staged_smem<__nv_bfloat16, 2>(warps) : staged_smem<float, 2>(warps);
+        case 4: return bf ? staged_smem<__nv_bfloat16, 4>(warps) : staged_smem<float, 4>(warps);
+        case 5: return bf ? staged_smem<__nv_bfloat16, 5>(warps) : staged_smem<float, 5>(warps);
+        default: return bf ? staged_smem<__nv_bfloat16, 8>(warps) : staged_smem<float, 8>(warps);
     }
-    const int groups = p.lanes ? p.threads / p.lanes : 1;   // per CTA
+}
+constexpr int kStagedSmem = 227 * 1024;
+BackwardPlan backward_plan(const slicegcn_residual_norm_desc* d, bool vec) {
+    BackwardPlan p{};
     const int64_t items = d->n * d->num_slices;
-    const int64_t resident = (backward ? 2 : 8) * kSMs * std::max(1, 256 / p.threads);
-    int64_t ctas = std::min((items + groups - 1) / groups, resident);
-    p.ctas = std::max<int64_t>(ctas, (d->num_slices + groups - 1) / groups);   // at least one row at a time
-    p.lanes_rows = p.ctas * groups / d->num_slices;
-    p.whole_rows = p.lanes && p.quads == 1 && groups % d->num_slices == 0;
-    p.partial_rows = p.whole_rows ? p.ctas : p.lanes_rows;
+    if (d->h_s <= 128) {
+        p.form = kByLanes;
+        p.lanes = lanes_for((d->h_s + 3) / 4);
+        const int groups = 256 / p.lanes;
+        p.ctas = std::max<int64_t>(std::min<int64_t>((items + groups - 1) / groups, 2 * kSMs), (d->num_slices + groups - 1) / groups);
+        p.lanes_rows = rows_at_a_time(p.ctas, groups, d->num_slices);
+        p.whole_rows = groups % d->num_slices == 0;
+        p.partial_rows = p.whole_rows ? p.ctas : p.lanes_rows;
+    } else if (d->h_s <= kMaxWarpWidth && vec) {
+        p.form = kStaged;
+        p.chunks = d->h_s <= 256 ? 2 : d->h_s <= 512 ? 4 : d->h_s <= 640 ? 5 : 8;
+        p.warps = kStagedWarps;
+        while (staged_smem_for(d->dtype, p.chunks, p.warps) > kStagedSmem) --p.warps;
+        p.smem = staged_smem_for(d->dtype, p.chunks, p.warps);
+        const int per_sm = std::max(1, std::min(2, kStagedSmem / (p.smem + 1024)));
+        const int64_t row_ctas = std::min<int64_t>((d->n + p.warps - 1) / p.warps, std::max<int64_t>(1, per_sm * kSMs / d->num_slices));
+        p.partial_rows = std::max<int64_t>(1, row_ctas);
+        p.ctas = p.partial_rows * d->num_slices;
+        p.lanes_rows = p.partial_rows * p.warps;
+    } else {
+        p.form = kTwoPasses;
+        p.partial_rows = std::max<int64_t>(1, std::min<int64_t>(d->n, kApplyRows));
+        p.stats_bytes = items * (int64_t)sizeof(RowStats);
+    }
     return p;
+}
+int64_t backward_bytes(const slicegcn_residual_norm_desc* d, const BackwardPlan& p) {
+    return p.stats_bytes + p.partial_rows * 4 * d->num_slices * d->h_s * (int64_t)sizeof(float);
 }
 
 template <typename T>
 struct ForwardCall {
-    const NormPlan& pl;
+    const ForwardPlan& pl;
     const NormArgs& a;
     const T *x, *y, *gate;
     T *h, *u;
     cudaStream_t st;
-    template <bool VEC, int L, int NV>
-    void go() const { norm_forward_kernel<T, VEC, L, NV><<<(unsigned)pl.ctas, pl.threads, 0, st>>>(a, x, y, gate, h, u); }
-    template <bool VEC>
+    template <bool VEC, int E, int L, int NV>
+    void go() const { norm_forward_kernel<T, VEC, E, L, NV><<<(unsigned)pl.ctas, 256, 0, st>>>(a, x, y, gate, h, u); }
+    template <bool VEC, int E>
     void pick() const {
         switch (pl.lanes) {
-            case 0: pl.quads == 1 ? go<VEC, 0, 1>() : pl.quads == 2 ? go<VEC, 0, 2>() : go<VEC, 0, 4>(); break;
-            case 1: go<VEC, 1, 1>(); break;
-            case 2: go<VEC, 2, 1>(); break;
-            case 4: go<VEC, 4, 1>(); break;
-            case 8: go<VEC, 8, 1>(); break;
-            case 16: go<VEC, 16, 1>(); break;
-            default: pl.quads == 1 ? go<VEC, 32, 1>() : pl.quads == 2 ? go<VEC, 32, 2>() : pl.quads == 4 ? go<VEC, 32, 4>() : go<VEC, 32, 8>(); break;
+            case 1: go<VEC, E, 1, 1>(); break;
+            case 2: go<VEC, E, 2, 1>(); break;
+            case 4: go<VEC, E, 4, 1>(); break;
+            case 8: go<VEC, E, 8, 1>(); break;
+            case 16: go<VEC, E, 16, 1>(); break;
+            default:
+                pl.chunks == 1 ? go<VEC, E, 32, 1>() : pl.chunks == 2 ? go<VEC, E, 32, 2>() : pl.chunks * E == 16 ? go<VEC, E, 32, 16 / E>()
+                                                                                                           : go<VEC, E, 32, 32 / E>();
         }
+    }
+    template <bool VEC>
+    void wide() const {
+        norm_forward_wide_kernel<T, VEC><<<(unsigned)((a.n * a.p + 7) / 8), 256, 0, st>>>(a, x, y, gate, h, u);
     }
 };
 
 template <typename T>
 struct BackwardCall {
-    const NormPlan& pl;
+    const BackwardPlan& pl;
     const NormArgs& a;
     const T *y, *gate, *h;
     const float *dh, *du;
     float *dx, *dy, *dgate;
+    RowStats* stats;
     cudaStream_t st;
-    template <bool VEC, int L, int NV>
-    void go() const { norm_backward_kernel<T, VEC, L, NV><<<(unsigned)pl.ctas, pl.threads, 0, st>>>(a, y, gate, h, dh, du, dx, dy, dgate); }
+    template <bool VEC, int L>
+    void go() const { norm_backward_kernel<T, VEC, L><<<(unsigned)pl.ctas, 256, 0, st>>>(a, y, gate, h, dh, du, dx, dy, dgate); }
+    template <int NV, bool BIAS>
+    slicegcn_status_t staged() const {
+        SGCN_CUDA(cudaFuncSetAttribute(norm_backward_staged_kernel<T, NV, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem));
+        norm_backward_staged_kernel<T, NV, BIAS><<<(unsigned)pl.ctas, pl.warps * 32, pl.smem, st>>>(a, y, gate, h, dh, du, dx, dy, dgate);
+        return SLICEGCN_OK;
+    }
+    template <bool BIAS>
+    slicegcn_status_t staged_for() const {
+        return pl.chunks == 2 ? staged<2, BIAS>() : pl.chunks == 4 ? staged<4, BIAS>() : pl.chunks == 5 ? staged<5, BIAS>() : staged<8, BIAS>();
+    }
     template <bool VEC>
-    void pick() const {
-        switch (pl.lanes) {
-            case 0: pl.quads == 1 ? go<VEC, 0, 1>() : pl.quads == 2 ? go<VEC, 0, 2>() : go<VEC, 0, 4>(); break;
-            case 1: go<VEC, 1, 1>(); break;
-            case 2: go<VEC, 2, 1>(); break;
-            case 4: go<VEC, 4, 1>(); break;
-            case 8: go<VEC, 8, 1>(); break;
-            case 16: go<VEC, 16, 1>(); break;
-            default: go<VEC, 32, 1>(); break;
+    slicegcn_status_t run(bool bias) const {
+        if (pl.form == kByLanes) {
+            switch (pl.lanes) {
+                case 1: go<VEC, 1>(); break;
+                case 2: go<VEC, 2>(); break;
+                case 4: go<VEC, 4>(); break;
+                case 8: go<VEC, 8>(); break;
+                case 16: go<VEC, 16>(); break;
+                default: go<VEC, 32>(); break;
+            }
+        } else if (pl.form == kStaged) {
+            SGCN_TRY(bias ? staged_for<true>() : staged_for<false>());
+        } else {
+            norm_stats_kernel<T, VEC><<<(unsigned)((a.n * a.p + 7) / 8), 256, 0, st>>>(a, y, gate, h, dh, du, stats);
+            SGCN_LAUNCH_CHECK();
+            count_launch();
+            const int tiles = (a.w + 127) / 128 * a.p;
+            const dim3 grid((tiles + 7) / 8, (unsigned)pl.partial_rows);
+            norm_apply_kernel<T, VEC><<<grid, 256, 0, st>>>(a, y, gate, h, dh, du, dx, dy, dgate, stats);
         }
+        SGCN_LAUNCH_CHECK();
+        count_launch();
+        return SLICEGCN_OK;
     }
 };
 
-// four elements at a time: every matrix that is given allows it
+// Whether every matrix that is given allows accesses of E elements at once.
 struct VecCheck {
+    int E;
     bool ok;
-    explicit VecCheck(const slicegcn_residual_norm_desc* d) : ok(d->num_slices == 1 || d->h_s % 4 == 0) {}
+    VecCheck(const slicegcn_residual_norm_desc* d, int e) : E(e), ok(d->num_slices == 1 || d->h_s % e == 0) {}
     VecCheck& with(const void* p, int64_t ld, int esz) {
-        if (p) ok = ok && ld % 4 == 0 && (uintptr_t)p % (4 * esz) == 0;
+        if (p) ok = ok && ld % E == 0 && (uintptr_t)p % std::min(E * esz, 16) == 0;
         return *this;
     }
 };
@@ -608,18 +1123,27 @@ slicegcn_status_t slicegcn_residual_norm_forward(const slicegcn_residual_norm_de
     if (gate && !y) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: a gate without y", who);
     if (!h && !u) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: neither h nor u is asked for", who);
     NormArgs a = make_args(d);
-    const NormPlan pl = norm_plan(d, false);
-    a.lanes_rows = pl.lanes_rows;
     cudaStream_t st = (cudaStream_t)stream;
-    const bool vec = VecCheck(d).with(x, d->x_ld, esz).with(y, d->y_ld, esz).with(gate, d->gate_ld, esz).with(h, d->h_ld, esz).with(u, d->u_ld, esz).ok;
+    auto check = [&](int E) {
+        return VecCheck(d, E).with(x, d->x_ld, esz).with(y, d->y_ld, esz).with(gate, d->gate_ld, esz).with(h, d->h_ld, esz).with(u, d->u_ld, esz).ok;
+    };
+    const bool vec4 = check(4), vec8 = esz == 2 && check(8), wide = d->h_s > kMaxWarpWidth;
+    const ForwardPlan pl = forward_plan(d, vec8 ? 8 : 4);
+    a.lanes_rows = pl.lanes_rows;
     if (d->dtype == SLICEGCN_BF16) {
         using T = __nv_bfloat16;
         const ForwardCall<T> call{pl, a, (const T*)x, (const T*)y, (const T*)gate, (T*)h, (T*)u, st};
-        vec ? call.template pick<true>() : call.template pick<false>();
+        if (wide)
+            vec4 ? call.template wide<true>() : call.template wide<false>();
+        else
+            vec8 ? call.template pick<true, 8>() : vec4 ? call.template pick<true, 4>() : call.template pick<false, 4>();
     } else {
         using T = float;
         const ForwardCall<T> call{pl, a, (const T*)x, (const T*)y, (const T*)gate, (T*)h, (T*)u, st};
-        vec ? call.template pick<true>() : call.template pick<false>();
+        if (wide)
+            vec4 ? call.template wide<true>() : call.template wide<false>();
+        else
+            vec4 ? call.template pick<true, 4>() : call.template pick<false, 4>();
     }
     SGCN_LAUNCH_CHECK();
     count_launch();
@@ -629,7 +1153,7 @@ slicegcn_status_t slicegcn_residual_norm_forward(const slicegcn_residual_norm_de
 slicegcn_status_t slicegcn_residual_norm_workspace_bytes(const slicegcn_residual_norm_desc* d, int64_t* bytes) {
     SGCN_TRY(check_desc(d, "residual_norm_workspace_bytes"));
     if (!bytes) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "residual_norm_workspace_bytes: NULL argument");
-    *bytes = norm_plan(d, true).partial_rows * 4 * d->num_slices * d->h_s * (int64_t)sizeof(float);
+    *bytes = std::max(backward_bytes(d, backward_plan(d, true)), backward_bytes(d, backward_plan(d, false)));
     return SLICEGCN_OK;
 }
 
@@ -661,31 +1185,31 @@ slicegcn_status_t slicegcn_residual_norm_backward(const slicegcn_residual_norm_d
     if (!y && (dw_post || db_post) && d->n > 0) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: dw_post / db_post without y", who);
     if (!du && (dw_pre || db_pre) && d->n > 0) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: dw_pre / db_pre without du", who);
     const bool sums = dw_post || db_post || dw_pre || db_pre;
-    const NormPlan pl = norm_plan(d, true);
+    const bool fours = VecCheck(d, 4).with(y, d->y_ld, esz).with(gate, d->gate_ld, esz).with(h, d->h_ld, esz).with(dh, d->dh_ld, 4)
+                         .with(du, d->du_ld, 4).with(dx, d->dx_ld, 4).with(dy, d->dy_ld, 4).with(dgate, d->dgate_ld, 4).ok;
+    const BackwardPlan pl = backward_plan(d, fours);
     const int cols = d->num_slices * d->h_s;
-    const int64_t need = pl.partial_rows * 4 * cols * (int64_t)sizeof(float);
-    if (sums && (!workspace || workspace_bytes < need))
+    const int64_t need = std::max(backward_bytes(d, backward_plan(d, true)), backward_bytes(d, backward_plan(d, false)));
+    if ((sums || pl.form == kTwoPasses) && (!workspace || workspace_bytes < need))
         SGCN_FAIL(SLICEGCN_ERR_ALLOC, "%s: workspace too small (%lld < %lld bytes)", who, (long long)workspace_bytes, (long long)need);
     if ((uintptr_t)workspace % 16) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: the workspace is not aligned to 16 bytes", who);
     NormArgs a = make_args(d);
     a.lanes_rows = pl.lanes_rows;
     a.whole_rows = pl.whole_rows;
-    a.partial = sums ? static_cast<float*>(workspace) : nullptr;
+    RowStats* stats = static_cast<RowStats*>(workspace);
+    a.partial = sums ? reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.stats_bytes) : nullptr;
     cudaStream_t st = (cudaStream_t)stream;
     if (a.n > 0) {
-        const bool vec = VecCheck(d).with(y, d->y_ld, esz).with(gate, d->gate_ld, esz).with(h, d->h_ld, esz).with(dh, d->dh_ld, 4)
-                             .with(du, d->du_ld, 4).with(dx, d->dx_ld, 4).with(dy, d->dy_ld, 4).with(dgate, d->dgate_ld, 4).ok;
+        const bool bias = db_post || db_pre;
         if (d->dtype == SLICEGCN_BF16) {
             using T = __nv_bfloat16;
-            const BackwardCall<T> call{pl, a, (const T*)y, (const T*)gate, (const T*)h, dh, du, dx, dy, dgate, st};
-            vec ? call.template pick<true>() : call.template pick<false>();
+            const BackwardCall<T> call{pl, a, (const T*)y, (const T*)gate, (const T*)h, dh, du, dx, dy, dgate, stats, st};
+            SGCN_TRY(fours ? call.template run<true>(bias) : call.template run<false>(bias));
         } else {
             using T = float;
-            const BackwardCall<T> call{pl, a, (const T*)y, (const T*)gate, (const T*)h, dh, du, dx, dy, dgate, st};
-            vec ? call.template pick<true>() : call.template pick<false>();
+            const BackwardCall<T> call{pl, a, (const T*)y, (const T*)gate, (const T*)h, dh, du, dx, dy, dgate, stats, st};
+            SGCN_TRY(fours ? call.template run<true>(bias) : call.template run<false>(bias));
         }
-        SGCN_LAUNCH_CHECK();
-        count_launch();
     }
     if (sums) {
         norm_join_kernel<<<dim3((cols + 31) / 32, 4), 1024, 0, st>>>(a.n > 0 ? pl.partial_rows : 0, cols, a.partial, dw_post, db_post, dw_pre, db_pre);
