@@ -35,57 +35,49 @@ struct Chunk;
 template <>
 struct Chunk<float, 4> {
     float4 v;
-    __device__ __forceinline__ void clear() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w; }
     __device__ __forceinline__ void load(const float* p) { v = __ldcs(reinterpret_cast<const float4*>(p)); }
     static __device__ __forceinline__ void store(float* p, const float (&f)[4]) {
         __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3]));
     }
-    __device__ __forceinline__ void set(int j, float x) { (&v.x)[j] = x; }
+    __device__ __forceinline__ void set(int j, float x) {
+        if (j == 0) v.x = x;
+        if (j == 1) v.y = x;
+        if (j == 2) v.z = x;
+        if (j == 3) v.w = x;
+    }
 };
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t o;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(hi), "f"(lo));
     return o;
 }
-template <int W>
-struct Words;   // W 32-bit words, one access
-template <>
-struct Words<2> {
-    using type = uint2;
-};
-template <>
-struct Words<4> {
-    using type = uint4;
-};
 template <int E>
 struct Chunk<__nv_bfloat16, E> {
-    using V = typename Words<E / 2>::type;
-    V v;
-    __device__ __forceinline__ const uint32_t& word(int k) const { return (&v.x)[k]; }
-    __device__ __forceinline__ uint32_t& word(int k) { return (&v.x)[k]; }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int k = 0; k < E / 2; ++k) word(k) = 0;
-    }
+    uint32_t word[E / 2];
     __device__ __forceinline__ void get(float (&f)[E]) const {
 #pragma unroll
-        for (int k = 0; k < E / 2; ++k) f[2 * k] = __uint_as_float(word(k) << 16), f[2 * k + 1] = __uint_as_float(word(k) & 0xffff0000u);
+        for (int k = 0; k < E / 2; ++k) f[2 * k] = __uint_as_float(word[k] << 16), f[2 * k + 1] = __uint_as_float(word[k] & 0xffff0000u);
     }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const V*>(p)); }
+    __device__ __forceinline__ void take(const uint2& v) { word[0] = v.x, word[1] = v.y; }
+    __device__ __forceinline__ void take(const uint4& v) { word[0] = v.x, word[1] = v.y, word[E / 2 - 2] = v.z, word[E / 2 - 1] = v.w; }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        if constexpr (E == 8)
+            take(__ldcs(reinterpret_cast<const uint4*>(p)));
+        else
+            take(__ldcs(reinterpret_cast<const uint2*>(p)));
+    }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&f)[E]) {
-        Chunk o;
-#pragma unroll
-        for (int k = 0; k < E / 2; ++k) o.word(k) = pack_bf16(f[2 * k], f[2 * k + 1]);
-        __stcs(reinterpret_cast<V*>(p), o.v);
+        if constexpr (E == 8)
+            __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])));
+        else
+            __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])));
     }
-    __device__ __forceinline__ void set(int j, float x) {   // x is a bf16 value
-        uint32_t& t = word(j >> 1);
-        t = j & 1 ? (t & 0xffffu) | (__float_as_uint(x) & 0xffff0000u) : (t & 0xffff0000u) | (__float_as_uint(x) >> 16);
+    __device__ __forceinline__ void set(int j, __nv_bfloat16 x) {
+        const uint32_t b = __bfloat16_as_ushort(x);
+        word[j >> 1] = j & 1 ? word[j >> 1] | b << 16 : b;   // even ones come first
     }
 };
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
@@ -97,22 +89,21 @@ struct Columns {
         : first(VEC ? E * lane : lane), hop(E * lanes), step(VEC ? 1 : lanes), left(idle ? 0 : w - first) {}
     __device__ __forceinline__ int at(int i) const { return first + i * hop; }
     __device__ __forceinline__ bool inside(int i, int j) const { return j * step < left - i * hop; }
+    // Loads are unconditional: a condition on each would make the compiler wait for the value where its two cases meet, and
+    // nothing would be on its way ahead.  What lies past the slice is read at its start instead, and made zero by keep().
     template <typename T>
-    __device__ __forceinline__ void load(Chunk<T, E>& q, const T* row, int i, bool live) const {
-        q.clear();
+    __device__ __forceinline__ void load(Chunk<T, E>& q, const T* row, int i) const {
         if (VEC) {
-            if (live && inside(i, 0)) q.load(row + at(i));
+            q.load(row + (inside(i, 0) ? at(i) : 0));
         } else {
 #pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (live && inside(i, j)) q.set(j, to_float(row[at(i) + j * step]));
+            for (int j = 0; j < E; ++j) q.set(j, row[inside(i, j) ? at(i) + j * step : 0]);
         }
     }
-    // what a chunk read past the slice becomes zero (VEC alone reads there)
-    __device__ __forceinline__ void trim(float (&f)[E], int i, bool ragged) const {
-        if (VEC && ragged)
+    __device__ __forceinline__ void keep(float (&f)[E], int i, bool full) const {
+        if (full) return;
 #pragma unroll
-            for (int j = 1; j < E; ++j) f[j] = inside(i, j) ? f[j] : 0.f;
+        for (int j = 0; j < E; ++j) f[j] = inside(i, j) ? f[j] : 0.f;
     }
     template <typename T>
     __device__ __forceinline__ void store(T* row, int i, const float (&f)[E], bool ragged) const {
@@ -205,7 +196,7 @@ __global__ void __launch_bounds__(256) norm_forward_kernel(const NormArgs a, con
     const Columns<VEC, E> cols(place.lane, L, a.w, place.idle);
     const int c0 = place.slice * a.w;
     const float inv_w = 1.f / (float)a.w;
-    const bool ragged = a.w % E != 0;
+    const bool ragged = a.w % E != 0, full = a.w == NV * E * L;
     float wp[E], bp[E], wq[E], bq[E], in[NV][E];
     auto weights_post = [&](int i) {
         cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, wp);
@@ -222,12 +213,12 @@ __global__ void __launch_bounds__(256) norm_forward_kernel(const NormArgs a, con
     if (NV == 1) weights_post(0), weights_pre(0);
     Chunk<T, E> qx[NV], qy[NV], qg[NV];
     auto request = [&](int64_t row) {
-        const bool live = row < a.n;
+        const int64_t at = min(row, a.n - 1);   // a row past the end is worked on, and not stored
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (y) cols.load(qy[i], y + row * a.y_ld + c0, i, live);
-            if (gate) cols.load(qg[i], gate + row * a.gate_ld + c0, i, live);
-            if (x) cols.load(qx[i], x + row * a.x_ld + c0, i, live);
+            if (y) cols.load(qy[i], y + at * a.y_ld + c0, i);
+            if (gate) cols.load(qg[i], gate + at * a.gate_ld + c0, i);
+            if (x) cols.load(qx[i], x + at * a.x_ld + c0, i);
         }
     };
     if (NV == 1) request(place.row);
@@ -241,9 +232,9 @@ __global__ void __launch_bounds__(256) norm_forward_kernel(const NormArgs a, con
         for (int i = 0; i < NV; ++i) {
 #pragma unroll
             for (int j = 0; j < E; ++j) v[i][j] = 0.f;
-            if (x) qx[i].get(v[i]), cols.trim(v[i], i, ragged);
-            if (y) qy[i].get(t[i]), cols.trim(t[i], i, ragged);
-            if (gate) qg[i].get(gt[i]);
+            if (x) qx[i].get(v[i]), cols.keep(v[i], i, full);
+            if (y) qy[i].get(t[i]), cols.keep(t[i], i, full);
+            if (gate) qg[i].get(gt[i]), cols.keep(gt[i], i, full);
         }
         if (NV == 1 && r + 1 < rounds) request(row + a.lanes_rows);
         if (y) {
@@ -257,10 +248,6 @@ __global__ void __launch_bounds__(256) norm_forward_kernel(const NormArgs a, con
                     if (gate) b *= sigmoid(gt[i][j]);
                     v[i][j] = fmaf(a.s, b, v[i][j]);
                 }
-            }
-            if (gate) {   // a gate read past the slice is anything: 0 * NaN must not come into the sums
-#pragma unroll
-                for (int i = 0; i < NV; ++i) cols.trim(v[i], i, ragged);
             }
         }
         if (h && live)
@@ -293,9 +280,9 @@ __global__ void __launch_bounds__(256) norm_forward_wide_kernel(const NormArgs a
     const int chunks = (a.w + 127) / 128;
     auto get = [&](const T* from, int i, float(&f)[E]) {
         Chunk<T, E> q;
-        cols.load(q, from, i, true);
+        cols.load(q, from, i);
         q.get(f);
-        cols.trim(f, i, ragged);
+        cols.keep(f, i, false);
     };
     float my = 0.f, ry = 0.f, sum[1];
     if (y) {
@@ -405,7 +392,7 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
     const Columns<VEC, E> cols(place.lane, L, a.w, place.idle);
     const int c0 = place.slice * a.w;
     const float inv_w = 1.f / (float)a.w;
-    const bool ragged = a.w % E != 0;
+    const bool ragged = a.w % E != 0, full = a.w == E * L;
     const int all = a.p * a.w;
     float wp[E], bp[E], wq[E], in[E];
     cols.vector(a.w_post ? a.w_post + c0 : nullptr, 0, 1.f, wp);
@@ -420,12 +407,12 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
     Chunk<T, E> qy, qg, qh;
     Chunk<float, E> qd, qu;
     auto request = [&](int64_t row) {
-        const bool live = row < a.n;
-        if (du) cols.load(qh, h + row * a.h_ld + c0, 0, live);
-        if (du) cols.load(qu, du + row * a.du_ld + c0, 0, live);
-        if (y) cols.load(qy, y + row * a.y_ld + c0, 0, live);
-        if (dh) cols.load(qd, dh + row * a.dh_ld + c0, 0, live);
-        if (gate) cols.load(qg, gate + row * a.gate_ld + c0, 0, live);
+        const int64_t at = min(row, a.n - 1);
+        if (du) cols.load(qh, h + at * a.h_ld + c0, 0);
+        if (du) cols.load(qu, du + at * a.du_ld + c0, 0);
+        if (y) cols.load(qy, y + at * a.y_ld + c0, 0);
+        if (dh) cols.load(qd, dh + at * a.dh_ld + c0, 0);
+        if (gate) cols.load(qg, gate + at * a.gate_ld + c0, 0);
     };
     request(place.row);
     const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;
@@ -435,10 +422,10 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
         float hv[E], uv[E], yv[E], d[E], gv[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) hv[j] = uv[j] = yv[j] = d[j] = gv[j] = 0.f;
-        if (du) qh.get(hv), qu.get(uv), cols.trim(hv, 0, ragged), cols.trim(uv, 0, ragged);
-        if (y) qy.get(yv), cols.trim(yv, 0, ragged);
-        if (dh) qd.get(d), cols.trim(d, 0, ragged);
-        if (gate) qg.get(gv), cols.trim(gv, 0, ragged);
+        if (du) qh.get(hv), qu.get(uv), cols.keep(hv, 0, full), cols.keep(uv, 0, full);
+        if (y) qy.get(yv), cols.keep(yv, 0, full);
+        if (dh) qd.get(d), cols.keep(d, 0, full);
+        if (gate) qg.get(gv), cols.keep(gv, 0, full);
         if (r + 1 < rounds) request(row + a.lanes_rows);
         if (a.layer) {
             float m[2] = {0.f, 0.f};
@@ -467,8 +454,10 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
             if (du) {
                 const float hhat = hv[j] * rh;
                 d[j] = fmaf(rh, fmaf(-mg, in[j], uv[j] * wq[j]) - hhat * mgh, d[j]);
-                acc[2][j] = fmaf(uv[j], hhat, acc[2][j]);
-                acc[3][j] += uv[j];
+                if (live) {
+                    acc[2][j] = fmaf(uv[j], hhat, acc[2][j]);
+                    acc[3][j] += uv[j];
+                }
             }
             if (y) {
                 float open = 1.f, slope = 0.f;
@@ -478,8 +467,10 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
                 uv[j] = dt * wp[j];
                 z[0] += uv[j];
                 z[1] = fmaf(uv[j], yv[j], z[1]);
-                acc[0][j] = fmaf(dt, yhat, acc[0][j]);
-                acc[1][j] += dt;
+                if (live) {
+                    acc[0][j] = fmaf(dt, yhat, acc[0][j]);
+                    acc[1][j] += dt;
+                }
             }
         }
         if (dx && live) cols.store(dx + row * a.dx_ld + c0, 0, d, ragged);
@@ -538,9 +529,14 @@ __device__ __forceinline__ void copy_async(uint32_t to, const __nv_bfloat16* fro
 }
 template <typename T>
 __device__ __forceinline__ void staged_get(const unsigned char* at, float (&f)[4]) {
-    Chunk<T, 4> q;
-    q.v = *reinterpret_cast<const decltype(q.v)*>(at);
-    q.get(f);
+    if constexpr (sizeof(T) == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(at);
+        f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+    } else {
+        Chunk<T, 4> q;
+        q.take(*reinterpret_cast<const uint2*>(at));
+        q.get(f);
+    }
 }
 // bytes of one row of a warp: dh, du in fp32 and y, gate, h in T, 32 lanes x NV chunks each
 template <typename T, int NV>
@@ -621,10 +617,10 @@ __global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                staged_get<T>(own_t + S::kH + i * HT, f), cols.trim(f, i, ragged);
+                staged_get<T>(own_t + S::kH + i * HT, f), cols.keep(f, i, !ragged);
 #pragma unroll
                 for (int j = 0; j < E; ++j) m[0] += f[j];
-                staged_get<T>(own_t + S::kY + i * HT, f), cols.trim(f, i, ragged);
+                staged_get<T>(own_t + S::kY + i * HT, f), cols.keep(f, i, !ragged);
 #pragma unroll
                 for (int j = 0; j < E; ++j) m[1] += f[j];
             }
@@ -738,14 +734,13 @@ __global__ void __launch_bounds__(256) norm_stats_kernel(const NormArgs a, const
     const int64_t row = item / a.p;
     const int c0 = (int)(item - row * a.p) * a.w, lane = threadIdx.x & 31;
     const Columns<VEC, E> cols(lane, 32, a.w, false);
-    const bool ragged = a.w % E != 0;
     const float inv_w = 1.f / (float)a.w;
     const int chunks = (a.w + 127) / 128;
     auto get = [&](auto* from, int i, float(&f)[E]) {
         Chunk<typename std::remove_cv<typename std::remove_pointer<decltype(from)>::type>::type, E> q;
-        cols.load(q, from, i, true);
+        cols.load(q, from, i);
         q.get(f);
-        cols.trim(f, i, ragged);
+        cols.keep(f, i, false);
     };
     RowStats s{};
     if (a.layer) {
@@ -830,10 +825,10 @@ __global__ void __launch_bounds__(256) norm_apply_kernel(const NormArgs a, const
         Chunk<T, E> qy, qg, qh;
         Chunk<float, E> qd, qu;
         const RowStats s = stats[row * a.p + slice];
-        if (du) cols.load(qh, h + row * a.h_ld + c0, i, true), cols.load(qu, du + row * a.du_ld + c0, i, true);
-        if (y) cols.load(qy, y + row * a.y_ld + c0, i, true);
-        if (dh) cols.load(qd, dh + row * a.dh_ld + c0, i, true);
-        if (gate) cols.load(qg, gate + row * a.gate_ld + c0, i, true);
+        if (du) cols.load(qh, h + row * a.h_ld + c0, i), cols.load(qu, du + row * a.du_ld + c0, i);
+        if (y) cols.load(qy, y + row * a.y_ld + c0, i);
+        if (dh) cols.load(qd, dh + row * a.dh_ld + c0, i);
+        if (gate) cols.load(qg, gate + row * a.gate_ld + c0, i);
         float hv[E], uv[E], yv[E], d[E] = {0.f, 0.f, 0.f, 0.f}, gv[E] = {0.f, 0.f, 0.f, 0.f};
         if (dh) qd.get(d);
         if (gate) qg.get(gv);
