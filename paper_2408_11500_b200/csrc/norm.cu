@@ -146,6 +146,36 @@ __device__ __forceinline__ float recip_fast(float x) {
 constexpr float kLog2e = 1.44269504088896341f;
 __device__ __forceinline__ float sigmoid(float g) { return recip_fast(1.f + exp2_fast(-kLog2e * g)); }
 
+// An asynchronous copy of one chunk to shared memory, and its values from there.  The thread that copies a chunk is the one
+// that reads it, so its own count of finished copies is all the waiting there is.
+__device__ __forceinline__ void copy_async16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async8(uint32_t to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
+template <int E, typename T>
+__device__ __forceinline__ void copy_chunk(uint32_t to, const T* from) {
+    if constexpr (E * sizeof(T) == 16)
+        copy_async16(to, from);
+    else
+        copy_async8(to, from);
+}
+template <typename T, int E>
+__device__ __forceinline__ void staged_get(const unsigned char* at, float (&f)[E]) {
+    if constexpr (sizeof(T) == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(at);
+        f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+    } else {
+        Chunk<T, E> q;
+        if constexpr (E == 8)
+            q.take(*reinterpret_cast<const uint4*>(at));
+        else
+            q.take(*reinterpret_cast<const uint2*>(at));
+        q.get(f);
+    }
+}
+
 // Where a thread works: its group's slice and first row (then every lanes_rows-th).
 template <int L>
 struct Place {
@@ -188,10 +218,15 @@ __device__ __forceinline__ float centre_and_scale(float (&t)[NV][E], const float
 }
 
 // Bound by HBM: x, y and gate are read once, h and u written once.  A slice row lives in the registers of its lanes from
-// the first load to the last store, so both norms cost shuffles and no second pass; with one chunk per lane the next row is
-// requested before this one is worked on, and the weights stay in registers over all rows.
+// the first use to the last store, so both norms cost shuffles and no second pass.  What decides is how much is on its way:
+// with one chunk per lane (up to 256 columns of bf16, 128 of fp32) kForwardAhead rows are copied to shared memory ahead,
+// and the weights stay in registers over all rows.
+constexpr int kForwardAhead = 4;
 template <typename T, bool VEC, int E, int L, int NV>
-__global__ void __launch_bounds__(256) norm_forward_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
+__global__ void __launch_bounds__(256, VEC && NV == 1 ? 2 : 1) norm_forward_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
+    constexpr bool RING = VEC && NV == 1;
+    constexpr int S = kForwardAhead;
+    extern __shared__ __align__(16) unsigned char ring[];   // [S][x, y, gate][thread] chunks
     const Place<L> place(a);
     const Columns<VEC, E> cols(place.lane, L, a.w, place.idle);
     const int c0 = place.slice * a.w;
@@ -210,33 +245,64 @@ __global__ void __launch_bounds__(256) norm_forward_kernel(const NormArgs a, con
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < E; ++j) in[i][j] = cols.inside(i, j) ? 1.f : 0.f;
-    if (NV == 1) weights_post(0), weights_pre(0);
+    const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;   // the same for all lanes
+    constexpr int kChunk = E * (int)sizeof(T), kTensor = 256 * kChunk;
+    const uint32_t ring_u = RING ? (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * kChunk : 0;
     Chunk<T, E> qx[NV], qy[NV], qg[NV];
-    auto request = [&](int64_t row) {
-        const int64_t at = min(row, a.n - 1);   // a row past the end is worked on, and not stored
+    int next_in = 0, next_out = 0;   // ring stages
+    auto request = [&](int64_t r) {
+        const int64_t at = min(place.row + r * a.lanes_rows, a.n - 1);   // a row past the end is worked on, and not stored
+        if (RING) {
+            const uint32_t to = ring_u + next_in * 3 * kTensor;
+            next_in = next_in + 1 == S ? 0 : next_in + 1;
+            const int c = cols.inside(0, 0) ? cols.at(0) : 0;
+            if (r < rounds) {
+                if (x) copy_chunk<E>(to, x + at * a.x_ld + c0 + c);
+                if (y) copy_chunk<E>(to + kTensor, y + at * a.y_ld + c0 + c);
+                if (gate) copy_chunk<E>(to + 2 * kTensor, gate + at * a.gate_ld + c0 + c);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        } else {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (y) cols.load(qy[i], y + at * a.y_ld + c0, i);
-            if (gate) cols.load(qg[i], gate + at * a.gate_ld + c0, i);
-            if (x) cols.load(qx[i], x + at * a.x_ld + c0, i);
+            for (int i = 0; i < NV; ++i) {
+                if (y) cols.load(qy[i], y + at * a.y_ld + c0, i);
+                if (gate) cols.load(qg[i], gate + at * a.gate_ld + c0, i);
+                if (x) cols.load(qx[i], x + at * a.x_ld + c0, i);
+            }
         }
     };
-    if (NV == 1) request(place.row);
-    const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;   // the same for all lanes
+    if (RING)
+#pragma unroll
+        for (int r = 0; r < S - 1; ++r) request(r);
+    else if (NV == 1)
+        request(0);
+    if (NV == 1) weights_post(0), weights_pre(0);
     for (int64_t r = 0; r < rounds; ++r) {
         const int64_t row = place.row + r * a.lanes_rows;
         const bool live = row < a.n;
-        if (NV > 1) request(row);
         float v[NV][E], t[NV][E], gt[NV][E];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < E; ++j) v[i][j] = 0.f;
-            if (x) qx[i].get(v[i]), cols.keep(v[i], i, full);
-            if (y) qy[i].get(t[i]), cols.keep(t[i], i, full);
-            if (gate) qg[i].get(gt[i]), cols.keep(gt[i], i, full);
+        if (RING) {
+            request(r + S - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+            const unsigned char* from = ring + threadIdx.x * kChunk + next_out * 3 * kTensor;
+            next_out = next_out + 1 == S ? 0 : next_out + 1;
+            if (x) staged_get<T>(from, v[0]), cols.keep(v[0], 0, full);
+            if (y) staged_get<T>(from + kTensor, t[0]), cols.keep(t[0], 0, full);
+            if (gate) staged_get<T>(from + 2 * kTensor, gt[0]), cols.keep(gt[0], 0, full);
+        } else {
+            if (NV > 1) request(r);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (x) qx[i].get(v[i]), cols.keep(v[i], i, full);
+                if (y) qy[i].get(t[i]), cols.keep(t[i], i, full);
+                if (gate) qg[i].get(gt[i]), cols.keep(gt[i], i, full);
+            }
+            if (NV == 1 && r + 1 < rounds) request(r + 1);
         }
-        if (NV == 1 && r + 1 < rounds) request(row + a.lanes_rows);
         if (y) {
             const float ry = centre_and_scale<T, VEC, E, L, NV>(t, in, a, inv_w);
 #pragma unroll
@@ -383,17 +449,55 @@ __device__ __forceinline__ void gate_and_slope(float g, float& open, float& slop
 // Bound by HBM as well: y, gate, h, dh and du are read once, dx, dy and dgate written once.  The sums over a slice are
 // taken together as far as they can be: (means), then squares of h and y with the products of du w_pre, then the
 // products of dt w_post.  Slices of up to 128 columns: four per lane, whose sums over the rows stay in registers until the
-// end, as do the weights; the next row is requested before this one is worked on.
+// end, as do the weights; kBackwardAhead rows are copied to shared memory ahead.
+constexpr int kBackwardAhead = 3;
+// bytes of a CTA's chunks of one row each: dh, du, then h, y, gate
+template <typename T>
+struct BackwardRing {
+    static constexpr int kF = 256 * 16, kT = 256 * 4 * (int)sizeof(T), kStage = 2 * kF + 3 * kT;
+};
 template <typename T, bool VEC, int L>
 __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a, const T* y, const T* gate, const T* h, const float* dh,
                                                                const float* du, float* dx, float* dy, float* dgate) {
-    constexpr int E = 4;
+    using R = BackwardRing<T>;
+    constexpr int E = 4, S = kBackwardAhead;
+    extern __shared__ __align__(16) unsigned char ring[];
     const Place<L> place(a);
     const Columns<VEC, E> cols(place.lane, L, a.w, place.idle);
     const int c0 = place.slice * a.w;
     const float inv_w = 1.f / (float)a.w;
     const bool ragged = a.w % E != 0, full = a.w == E * L;
     const int all = a.p * a.w;
+    const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;
+    const uint32_t ring_u = VEC ? (uint32_t)__cvta_generic_to_shared(ring) : 0;
+    const int at_f = threadIdx.x * 16, at_t = 2 * R::kF + threadIdx.x * 4 * (int)sizeof(T);
+    Chunk<T, E> qy, qg, qh;
+    Chunk<float, E> qd, qu;
+    int next_in = 0, next_out = 0;   // ring stages
+    auto request = [&](int64_t r) {
+        const int64_t at = min(place.row + r * a.lanes_rows, a.n - 1);   // a row past the end is worked on, and not kept
+        if (VEC) {
+            const uint32_t to = ring_u + next_in * R::kStage;
+            next_in = next_in + 1 == S ? 0 : next_in + 1;
+            const int c = c0 + (cols.inside(0, 0) ? cols.at(0) : 0);
+            if (r < rounds) {
+                if (du) copy_chunk<E>(to + at_t, h + at * a.h_ld + c);
+                if (du) copy_chunk<E>(to + R::kF + at_f, du + at * a.du_ld + c);
+                if (y) copy_chunk<E>(to + at_t + R::kT, y + at * a.y_ld + c);
+                if (dh) copy_chunk<E>(to + at_f, dh + at * a.dh_ld + c);
+                if (gate) copy_chunk<E>(to + at_t + 2 * R::kT, gate + at * a.gate_ld + c);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        } else {
+            if (du) cols.load(qh, h + at * a.h_ld + c0, 0);
+            if (du) cols.load(qu, du + at * a.du_ld + c0, 0);
+            if (y) cols.load(qy, y + at * a.y_ld + c0, 0);
+            if (dh) cols.load(qd, dh + at * a.dh_ld + c0, 0);
+            if (gate) cols.load(qg, gate + at * a.gate_ld + c0, 0);
+        }
+    };
+#pragma unroll
+    for (int r = 0; r < (VEC ? S - 1 : 1); ++r) request(r);
     float wp[E], bp[E], wq[E], in[E];
     cols.vector(a.w_post ? a.w_post + c0 : nullptr, 0, 1.f, wp);
     cols.vector(a.b_post ? a.b_post + c0 : nullptr, 0, 0.f, bp);
@@ -404,29 +508,29 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
         in[j] = cols.inside(0, j) ? 1.f : 0.f;
         acc[0][j] = acc[1][j] = acc[2][j] = acc[3][j] = 0.f;
     }
-    Chunk<T, E> qy, qg, qh;
-    Chunk<float, E> qd, qu;
-    auto request = [&](int64_t row) {
-        const int64_t at = min(row, a.n - 1);
-        if (du) cols.load(qh, h + at * a.h_ld + c0, 0);
-        if (du) cols.load(qu, du + at * a.du_ld + c0, 0);
-        if (y) cols.load(qy, y + at * a.y_ld + c0, 0);
-        if (dh) cols.load(qd, dh + at * a.dh_ld + c0, 0);
-        if (gate) cols.load(qg, gate + at * a.gate_ld + c0, 0);
-    };
-    request(place.row);
-    const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;
     for (int64_t r = 0; r < rounds; ++r) {
         const int64_t row = place.row + r * a.lanes_rows;
         const bool live = row < a.n && !place.idle;
         float hv[E], uv[E], yv[E], d[E], gv[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) hv[j] = uv[j] = yv[j] = d[j] = gv[j] = 0.f;
-        if (du) qh.get(hv), qu.get(uv), cols.keep(hv, 0, full), cols.keep(uv, 0, full);
-        if (y) qy.get(yv), cols.keep(yv, 0, full);
-        if (dh) qd.get(d), cols.keep(d, 0, full);
-        if (gate) qg.get(gv), cols.keep(gv, 0, full);
-        if (r + 1 < rounds) request(row + a.lanes_rows);
+        if (VEC) {
+            request(r + S - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+            const unsigned char* from = ring + next_out * R::kStage;
+            next_out = next_out + 1 == S ? 0 : next_out + 1;
+            if (du) staged_get<T>(from + at_t, hv), staged_get<float>(from + R::kF + at_f, uv);
+            if (y) staged_get<T>(from + at_t + R::kT, yv);
+            if (dh) staged_get<float>(from + at_f, d);
+            if (gate) staged_get<T>(from + at_t + 2 * R::kT, gv);
+        } else {
+            if (du) qh.get(hv), qu.get(uv);
+            if (y) qy.get(yv);
+            if (dh) qd.get(d);
+            if (gate) qg.get(gv);
+        }
+        cols.keep(hv, 0, full), cols.keep(uv, 0, full), cols.keep(yv, 0, full), cols.keep(d, 0, full), cols.keep(gv, 0, full);
+        if (!VEC && r + 1 < rounds) request(r + 1);
         if (a.layer) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
@@ -521,23 +625,6 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
 // registers to the columns' sums (BIAS: those of the biases too).  A CTA works on one slice: its warps' sums are added in
 // order at the end.
 constexpr int kStagedWarps = 8;
-__device__ __forceinline__ void copy_async(uint32_t to, const float* from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copy_async(uint32_t to, const __nv_bfloat16* from) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
-}
-template <typename T>
-__device__ __forceinline__ void staged_get(const unsigned char* at, float (&f)[4]) {
-    if constexpr (sizeof(T) == 4) {
-        const float4 v = *reinterpret_cast<const float4*>(at);
-        f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
-    } else {
-        Chunk<T, 4> q;
-        q.take(*reinterpret_cast<const uint2*>(at));
-        q.get(f);
-    }
-}
 // bytes of one row of a warp: dh, du in fp32 and y, gate, h in T, 32 lanes x NV chunks each
 template <typename T, int NV>
 struct Staged {
@@ -587,11 +674,11 @@ __global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel
             for (int i = 0; i < NV; ++i)
                 if (cols.inside(i, 0)) {
                     const int o = i * 32 + lane, c = c0 + cols.at(i);
-                    if (du) copy_async(to + S::kH + o * E * (int)sizeof(T), h + row * a.h_ld + c);
-                    if (y) copy_async(to + S::kY + o * E * (int)sizeof(T), y + row * a.y_ld + c);
-                    if (du) copy_async(to + S::kDu + o * 16, du + row * a.du_ld + c);
-                    if (dh) copy_async(to + S::kDh + o * 16, dh + row * a.dh_ld + c);
-                    if (gate) copy_async(to + S::kGate + o * E * (int)sizeof(T), gate + row * a.gate_ld + c);
+                    if (du) copy_chunk<E>(to + S::kH + o * E * (int)sizeof(T), h + row * a.h_ld + c);
+                    if (y) copy_chunk<E>(to + S::kY + o * E * (int)sizeof(T), y + row * a.y_ld + c);
+                    if (du) copy_chunk<E>(to + S::kDu + o * 16, du + row * a.du_ld + c);
+                    if (dh) copy_chunk<E>(to + S::kDh + o * 16, dh + row * a.dh_ld + c);
+                    if (gate) copy_chunk<E>(to + S::kGate + o * E * (int)sizeof(T), gate + row * a.gate_ld + c);
                 }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -1017,7 +1104,10 @@ struct ForwardCall {
     T *h, *u;
     cudaStream_t st;
     template <bool VEC, int E, int L, int NV>
-    void go() const { norm_forward_kernel<T, VEC, E, L, NV><<<(unsigned)pl.ctas, 256, 0, st>>>(a, x, y, gate, h, u); }
+    void go() const {
+        constexpr int smem = VEC && NV == 1 ? kForwardAhead * 3 * 256 * E * (int)sizeof(T) : 0;   // 48 KB at most
+        norm_forward_kernel<T, VEC, E, L, NV><<<(unsigned)pl.ctas, 256, smem, st>>>(a, x, y, gate, h, u);
+    }
     template <bool VEC, int E>
     void pick() const {
         switch (pl.lanes) {
@@ -1047,7 +1137,12 @@ struct BackwardCall {
     RowStats* stats;
     cudaStream_t st;
     template <bool VEC, int L>
-    void go() const { norm_backward_kernel<T, VEC, L><<<(unsigned)pl.ctas, 256, 0, st>>>(a, y, gate, h, dh, du, dx, dy, dgate); }
+    slicegcn_status_t go() const {
+        constexpr int smem = VEC ? kBackwardAhead * BackwardRing<T>::kStage : 0;
+        if (smem > 48 * 1024) SGCN_CUDA(cudaFuncSetAttribute(norm_backward_kernel<T, VEC, L>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        norm_backward_kernel<T, VEC, L><<<(unsigned)pl.ctas, 256, smem, st>>>(a, y, gate, h, dh, du, dx, dy, dgate);
+        return SLICEGCN_OK;
+    }
     template <int NV, bool BIAS>
     slicegcn_status_t staged() const {
         SGCN_CUDA(cudaFuncSetAttribute(norm_backward_staged_kernel<T, NV, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem));
@@ -1062,12 +1157,12 @@ struct BackwardCall {
     slicegcn_status_t run(bool bias) const {
         if (pl.form == kByLanes) {
             switch (pl.lanes) {
-                case 1: go<VEC, 1>(); break;
-                case 2: go<VEC, 2>(); break;
-                case 4: go<VEC, 4>(); break;
-                case 8: go<VEC, 8>(); break;
-                case 16: go<VEC, 16>(); break;
-                default: go<VEC, 32>(); break;
+                case 1: SGCN_TRY((go<VEC, 1>())); break;
+                case 2: SGCN_TRY((go<VEC, 2>())); break;
+                case 4: SGCN_TRY((go<VEC, 4>())); break;
+                case 8: SGCN_TRY((go<VEC, 8>())); break;
+                case 16: SGCN_TRY((go<VEC, 16>())); break;
+                default: SGCN_TRY((go<VEC, 32>())); break;
             }
         } else if (pl.form == kStaged) {
             SGCN_TRY(bias ? staged_for<true>() : staged_for<false>());
