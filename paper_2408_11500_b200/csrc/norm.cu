@@ -620,11 +620,14 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
 }
 
 // Slices of 129 to 1024 columns that allow accesses of four elements: a warp per slice row, whose five inputs are copied to
-// shared memory asynchronously one row ahead.  Every lane copies, and reads back, its own columns only (4 lane + 128 i), so
-// no barrier stands in the loop.  The row is read from shared memory in each of the passes over it, which leaves the
-// registers to the columns' sums (BIAS: those of the biases too).  A CTA works on one slice: its warps' sums are added in
-// order at the end.
-constexpr int kStagedWarps = 8;
+// shared memory one row ahead.  Every lane copies, and reads back, its own columns only (4 lane + 128 i), so no barrier
+// stands in the loop.  The row is read from shared memory in each of the passes over it, which leaves the registers to the
+// columns' sums (BIAS: those of the biases too).  A CTA works on one slice: its warps' sums are added in order at the end.
+// What is not given is left in shared memory as values that change nothing (zeros; an infinite gate is an open one).
+// Shared memory (two rows per warp) and registers (the sums) bound the warps per SM, so what counts here is instructions
+// per element: twelve warps of them keep up with HBM at 602 columns.
+template <int NV>
+constexpr int staged_warps() { return NV <= 5 ? 12 : 8; }
 // bytes of one row of a warp: dh, du in fp32 and y, gate, h in T, 32 lanes x NV chunks each
 template <typename T, int NV>
 struct Staged {
@@ -634,11 +637,12 @@ struct Staged {
     static constexpr int smem(int warps) { return kVectors + warps * 2 * kRow; }
 };
 template <typename T, int NV, bool BIAS>
-__global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel(const NormArgs a, const T* y, const T* gate, const T* h,
-                                                                                 const float* dh, const float* du, float* dx, float* dy,
-                                                                                 float* dgate) {
+__global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_kernel(const NormArgs a, const T* y, const T* gate, const T* h,
+                                                                                       const float* dh, const float* du, float* dx,
+                                                                                       float* dy, float* dgate) {
     using S = Staged<T, NV>;
     constexpr int E = 4;
+    constexpr int HF = 512, HT = 32 * E * (int)sizeof(T);   // bytes from one chunk of a lane to its next
     extern __shared__ __align__(16) unsigned char stage[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int slice = blockIdx.x % a.p;
@@ -647,25 +651,29 @@ __global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel
     const Columns<true, E> cols(lane, 32, a.w, false);
     const bool ragged = a.w % E != 0;
     const float inv_w = 1.f / (float)a.w;
-    float(*vec)[NV][32][E] = reinterpret_cast<float(*)[NV][32][E]>(stage);
     unsigned char* mine = stage + S::kVectors + warp * 2 * S::kRow;
     const uint32_t mine_u = (uint32_t)__cvta_generic_to_shared(mine);
+    const unsigned char* vectors = stage + lane * 16;
     if (warp == 0)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float f[E];
+            float4* to = reinterpret_cast<float4*>(stage + lane * 16 + i * HF);
             cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, f);
-#pragma unroll
-            for (int j = 0; j < E; ++j) vec[0][i][lane][j] = f[j];
+            to[0] = make_float4(f[0], f[1], f[2], f[3]);
             cols.vector(a.b_post ? a.b_post + c0 : nullptr, i, 0.f, f);
-#pragma unroll
-            for (int j = 0; j < E; ++j) vec[1][i][lane][j] = f[j];
+            to[NV * 32] = make_float4(f[0], f[1], f[2], f[3]);
             cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, f);
-#pragma unroll
-            for (int j = 0; j < E; ++j) vec[2][i][lane][j] = f[j];
+            to[2 * NV * 32] = make_float4(f[0], f[1], f[2], f[3]);
         }
-    // columns past the slice are never copied: they stay zero
-    for (int k = lane * 16; k < 2 * S::kRow; k += 512) *reinterpret_cast<uint4*>(mine + k) = make_uint4(0, 0, 0, 0);
+    {   // columns past the slice are never copied: they stay as they are here
+        const uint32_t inf = sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u;
+        for (int k = lane * 16; k < 2 * S::kRow; k += 512) {
+            const int in = k < S::kRow ? k : k - S::kRow;
+            const uint32_t fill = !gate && in >= S::kGate && in < S::kH ? inf : 0u;
+            *reinterpret_cast<uint4*>(mine + k) = make_uint4(fill, fill, fill, fill);
+        }
+    }
     __syncthreads();
     auto request = [&](int64_t row, int buf) {
         if (row < a.n) {
@@ -683,6 +691,10 @@ __global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    // zero what a ragged chunk holds past the slice, and what subtracting a mean leaves there
+    auto trim = [&](float(&f)[E], int i) {
+        if (a.w < 128 * (i + 1)) cols.keep(f, i, false);
+    };
     float acc[BIAS ? 4 : 2][NV][E];   // dw_post, dw_pre, db_post, db_pre
 #pragma unroll
     for (int k = 0; k < (BIAS ? 4 : 2); ++k)
@@ -695,21 +707,18 @@ __global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel
     for (int64_t row = first; row < a.n; row += a.lanes_rows, buf ^= 1) {
         request(row + a.lanes_rows, buf ^ 1);
         asm volatile("cp.async.wait_group 1;" ::: "memory");
-        const unsigned char* in = mine + buf * S::kRow;
-        const unsigned char* own_f = in + lane * 16;
-        const unsigned char* own_t = in + lane * E * sizeof(T);
-        constexpr int HF = 512, HT = 32 * E * (int)sizeof(T);   // bytes from one chunk of a lane to its next
-        float mh = 0.f, my = 0.f, f[E];
+        const unsigned char* own_f = mine + buf * S::kRow + lane * 16;
+        const unsigned char* own_t = mine + buf * S::kRow + lane * E * (int)sizeof(T);
+        float mh = 0.f, my = 0.f;
         if (a.layer) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                staged_get<T>(own_t + S::kH + i * HT, f), cols.keep(f, i, !ragged);
+                float hv[E], yv[E];
+                staged_get<T>(own_t + S::kH + i * HT, hv), staged_get<T>(own_t + S::kY + i * HT, yv);
+                trim(hv, i), trim(yv, i);
 #pragma unroll
-                for (int j = 0; j < E; ++j) m[0] += f[j];
-                staged_get<T>(own_t + S::kY + i * HT, f), cols.keep(f, i, !ragged);
-#pragma unroll
-                for (int j = 0; j < E; ++j) m[1] += f[j];
+                for (int j = 0; j < E; ++j) m[0] += hv[j], m[1] += yv[j];
             }
             group_sum<32>(m);
             mh = m[0] * inv_w, my = m[1] * inv_w;
@@ -717,18 +726,21 @@ __global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel
         float q[4] = {0.f, 0.f, 0.f, 0.f};   // squares of h and y, sum of du w_pre, of its product with h
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float hv[E], uv[E], yv[E];
+            float hv[E], uv[E], yv[E], wq[E];
             staged_get<T>(own_t + S::kH + i * HT, hv);
             staged_get<float>(own_f + S::kDu + i * HF, uv);
             staged_get<T>(own_t + S::kY + i * HT, yv);
+            staged_get<float>(vectors + 2 * S::kF + i * HF, wq);
+#pragma unroll
+            for (int j = 0; j < E; ++j) hv[j] -= mh, yv[j] -= my;
+            trim(hv, i), trim(yv, i), trim(uv, i);
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                if (!cols.inside(i, j)) continue;
-                const float g = uv[j] * vec[2][i][lane][j], hc = hv[j] - mh, yc = yv[j] - my;
-                q[0] = fmaf(hc, hc, q[0]);
-                q[1] = fmaf(yc, yc, q[1]);
+                const float g = uv[j] * wq[j];
+                q[0] = fmaf(hv[j], hv[j], q[0]);
+                q[1] = fmaf(yv[j], yv[j], q[1]);
                 q[2] += g;
-                q[3] = fmaf(g, hc, q[3]);
+                q[3] = fmaf(g, hv[j], q[3]);
             }
         }
         group_sum<32>(q);
@@ -737,37 +749,31 @@ __global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel
         float t[NV][E], z[2] = {0.f, 0.f};   // dt w_post; its sum, and that of its product with y
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float hv[E], uv[E], yv[E], d[E], gv[E];
+            float hv[E], uv[E], yv[E], d[E], gv[E], wp[E], bp[E], wq[E];
             staged_get<T>(own_t + S::kH + i * HT, hv);
             staged_get<float>(own_f + S::kDu + i * HF, uv);
             staged_get<T>(own_t + S::kY + i * HT, yv);
             staged_get<float>(own_f + S::kDh + i * HF, d);
             staged_get<T>(own_t + S::kGate + i * HT, gv);
+            staged_get<float>(vectors + i * HF, wp);
+            staged_get<float>(vectors + S::kF + i * HF, bp);
+            staged_get<float>(vectors + 2 * S::kF + i * HF, wq);
+            trim(uv, i), trim(d, i), trim(yv, i), trim(gv, i), trim(hv, i);
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const bool is = cols.inside(i, j);
-                t[i][j] = 0.f;
-                if (du) {
-                    const float hhat = (hv[j] - mh) * rh;
-                    d[j] = fmaf(rh, fmaf(uv[j], vec[2][i][lane][j], -mg) - hhat * mgh, d[j]);
-                    if (is) {
-                        acc[1][i][j] = fmaf(uv[j], hhat, acc[1][i][j]);
-                        if (BIAS) acc[BIAS ? 3 : 1][i][j] += uv[j];
-                    }
-                }
-                if (y) {
-                    float open = 1.f, slope = 0.f;
-                    if (gate) gate_and_slope(gv[j], open, slope);
-                    const float ds = d[j] * a.s, yc = yv[j] - my, yhat = yc * ry, dt = ds * open, w = vec[0][i][lane][j];
-                    gv[j] = ds * slope * fmaf(yhat, w, vec[1][i][lane][j]);
-                    t[i][j] = dt * w;
-                    if (is) {
-                        z[0] += t[i][j];
-                        z[1] = fmaf(t[i][j], yc, z[1]);
-                        acc[0][i][j] = fmaf(dt, yhat, acc[0][i][j]);
-                        if (BIAS) acc[BIAS ? 2 : 0][i][j] += dt;
-                    }
-                }
+                const float hhat = (hv[j] - mh) * rh;
+                d[j] = fmaf(rh, fmaf(uv[j], wq[j], -mg) - hhat * mgh, d[j]);
+                acc[1][i][j] = fmaf(uv[j], hhat, acc[1][i][j]);
+                if (BIAS) acc[BIAS ? 3 : 1][i][j] += uv[j];
+                float open, slope;
+                gate_and_slope(gv[j], open, slope);
+                const float ds = d[j] * a.s, yc = yv[j] - my, yhat = yc * ry, dt = ds * open;
+                gv[j] = ds * slope * fmaf(yhat, wp[j], bp[j]);
+                t[i][j] = dt * wp[j];              // w_post is zero past the slice
+                z[0] += t[i][j];
+                z[1] = fmaf(t[i][j], yc, z[1]);
+                acc[0][i][j] = fmaf(dt, yhat, acc[0][i][j]);
+                if (BIAS) acc[BIAS ? 2 : 0][i][j] += dt;
             }
             if (dx) cols.store(dx + row * a.dx_ld + c0, i, d, ragged);
             if (dgate) cols.store(dgate + row * a.dgate_ld + c0, i, gv, ragged);
@@ -787,21 +793,20 @@ __global__ void __launch_bounds__(kStagedWarps * 32) norm_backward_staged_kernel
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (!a.partial) return;
     const int all = a.p * a.w;
-    float(*sums)[NV][32][E] = reinterpret_cast<float(*)[NV][32][E]>(stage + S::kVectors);   // [warp]
+    unsigned char* sums = stage + S::kVectors;   // [warp][columns]
 #pragma unroll
     for (int k = 0; k < (BIAS ? 4 : 2); ++k) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < E; ++j) sums[warp][i][lane][j] = acc[k][i][j];
+            *reinterpret_cast<float4*>(sums + warp * S::kF + i * HF + lane * 16) = make_float4(acc[k][i][0], acc[k][i][1], acc[k][i][2], acc[k][i][3]);
         __syncthreads();
         const int which = BIAS ? (k == 0 ? 0 : k == 1 ? 2 : k == 2 ? 1 : 3) : 2 * k;   // order of the partial rows
         float* out = a.partial + ((int64_t)(blockIdx.x / a.p) * 4 + which) * all + c0;
         for (int c = threadIdx.x; c < a.w; c += blockDim.x) {
-            float s = 0.f;
-            for (int v = 0; v < warps; ++v) s += (&sums[v][0][0][0])[c];   // chunk i of lane l holds columns 128 i + 4 l ...
-            out[c] = s;
+            float v = 0.f;
+            for (int o = 0; o < warps; ++o) v += *reinterpret_cast<const float*>(sums + o * S::kF + c * 4);
+            out[c] = v;
         }
     }
 }
@@ -1077,7 +1082,7 @@ BackwardPlan backward_plan(const slicegcn_residual_norm_desc* d, bool vec) {
     } else if (d->h_s <= kMaxWarpWidth && vec) {
         p.form = kStaged;
         p.chunks = d->h_s <= 256 ? 2 : d->h_s <= 512 ? 4 : d->h_s <= 640 ? 5 : 8;
-        p.warps = kStagedWarps;
+        p.warps = p.chunks <= 5 ? staged_warps<5>() : staged_warps<8>();
         while (staged_smem_for(d->dtype, p.chunks, p.warps) > kStagedSmem) --p.warps;
         p.smem = staged_smem_for(d->dtype, p.chunks, p.warps);
         const int per_sm = std::max(1, std::min(2, kStagedSmem / (p.smem + 1024)));
