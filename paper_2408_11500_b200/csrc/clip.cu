@@ -10,81 +10,88 @@
 namespace sgcn {
 namespace {
 
-constexpr int kClipChunk = 4096;     // elements per work item: 4 per thread of a large CTA, 16 per thread of a small one
+constexpr int kPieceBytes = 16384;   // of one tensor: the work item of a CTA, 16 bytes per thread and step
 constexpr int kSMs = 148;
 
-struct ClipEntry {
-    const void* src;
-    void* dst;
-    int64_t elems;
-    int64_t first;   // index of the tensor's first chunk
-    int bf16, vec;   // vec: four elements at a time are aligned in src and dst
-};
-// N: room for tensors.  A short list travels as a short kernel argument, which costs less to launch (512 tensors: 20 KB).
-template <int N>
-struct ClipTable {
-    int count;
-    int64_t chunks;
-    ClipEntry e[N];
-};
-constexpr int kShortList = 32;
-
-struct Four {
-    float v[4];
+// A stretch of one tensor of at most kPieceBytes.
+struct Piece {
+    const char* src;
+    char* dst;
+    int bytes;
+    int bf16, vec;   // vec: 16 bytes at a time are aligned in src and dst
 };
 
-// four elements from i (fewer where the tensor ends; the rest zeros)
-__device__ __forceinline__ Four load4(const ClipEntry& e, int64_t i) {
-    Four f{{0.f, 0.f, 0.f, 0.f}};
-    if (i >= e.elems) return f;
-    if (e.vec && i + 4 <= e.elems) {
-        if (e.bf16) {
-            const uint2 t = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(e.src) + i);
-            f.v[0] = __uint_as_float(t.x << 16), f.v[1] = __uint_as_float(t.x & 0xffff0000u);
-            f.v[2] = __uint_as_float(t.y << 16), f.v[3] = __uint_as_float(t.y & 0xffff0000u);
-        } else {
-            const float4 t = *reinterpret_cast<const float4*>(static_cast<const float*>(e.src) + i);
-            f.v[0] = t.x, f.v[1] = t.y, f.v[2] = t.z, f.v[3] = t.w;
-        }
-        return f;
-    }
+// The 16 bytes at `off` of a piece.  The load has no condition on it (past the end it reads the piece's start, and the last
+// 16 bytes may reach past the end, never past an aligned 16-byte unit that the tensor shares): with one, the compiler waits
+// for each value where the cases meet, and a thread has one load on its way instead of several.
+struct Raw {
+    uint32_t w[4];
+};
+__device__ __forceinline__ Raw load16(const Piece& p, int off) {
+    Raw r;
+    if (p.vec) {
+        const uint4 t = *reinterpret_cast<const uint4*>(p.src + (off < p.bytes ? off : 0));
+        r.w[0] = t.x, r.w[1] = t.y, r.w[2] = t.z, r.w[3] = t.w;
+    } else if (p.bf16) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (i + j < e.elems)
-            f.v[j] = e.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(e.src)[i + j]) : static_cast<const float*>(e.src)[i + j];
-    return f;
+        for (int k = 0; k < 4; ++k) {
+            const uint16_t* at = reinterpret_cast<const uint16_t*>(p.src + off) + 2 * k;
+            r.w[k] = off + 4 * k < p.bytes ? at[0] : 0u;
+            if (off + 4 * k + 2 < p.bytes) r.w[k] |= (uint32_t)at[1] << 16;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r.w[k] = off + 4 * k < p.bytes ? reinterpret_cast<const uint32_t*>(p.src + off)[k] : 0u;
+    }
+    return r;
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// The squares are taken and added in 64 bits: the square of any fp32 number fits a double, so neither large nor tiny
+// gradients leave its range, and this GPU's 64-bit rate is above what HBM delivers to it.
+__device__ __forceinline__ double squares(const Piece& p, int off, const Raw& r) {
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int left = p.bytes - off - 4 * k;   // bytes from this word on
+        if (p.bf16) {
+            const double a = left > 0 ? bf16_lo(r.w[k]) : 0.f, b = left > 2 ? bf16_hi(r.w[k]) : 0.f;
+            s = fma(a, a, fma(b, b, s));
+        } else {
+            const double a = left > 0 ? __uint_as_float(r.w[k]) : 0.f;
+            s = fma(a, a, s);
+        }
+    }
+    return s;
 }
 
-__device__ __forceinline__ void store4(const ClipEntry& e, int64_t i, const Four& f, float factor) {
-    if (i >= e.elems) return;
-    const float a = f.v[0] * factor, b = f.v[1] * factor, c = f.v[2] * factor, d = f.v[3] * factor;
-    if (e.vec && i + 4 <= e.elems) {
-        if (e.bf16) {
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(a, b), hi = __floats2bfloat162_rn(c, d);
-            uint2 t;
-            t.x = *reinterpret_cast<const uint32_t*>(&lo), t.y = *reinterpret_cast<const uint32_t*>(&hi);
-            __stcs(reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(e.dst) + i), t);
+__device__ __forceinline__ void store16(const Piece& p, int off, const Raw& r, float f) {
+    if (off >= p.bytes) return;
+    if (p.bf16) {
+        uint32_t o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat162 t = __floats2bfloat162_rn(bf16_lo(r.w[k]) * f, bf16_hi(r.w[k]) * f);
+            o[k] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+        if (p.vec && off + 16 <= p.bytes) {
+            __stcs(reinterpret_cast<uint4*>(p.dst + off), make_uint4(o[0], o[1], o[2], o[3]));
         } else {
-            __stcs(reinterpret_cast<float4*>(static_cast<float*>(e.dst) + i), make_float4(a, b, c, d));
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (off + 2 * k < p.bytes) reinterpret_cast<uint16_t*>(p.dst + off)[k] = (uint16_t)(k & 1 ? o[k / 2] >> 16 : o[k / 2]);
         }
         return;
     }
-    const float o[4] = {a, b, c, d};
+    const float v[4] = {__uint_as_float(r.w[0]) * f, __uint_as_float(r.w[1]) * f, __uint_as_float(r.w[2]) * f, __uint_as_float(r.w[3]) * f};
+    if (p.vec && off + 16 <= p.bytes) {
+        __stcs(reinterpret_cast<float4*>(p.dst + off), make_float4(v[0], v[1], v[2], v[3]));
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (i + j < e.elems) {
-            if (e.bf16)
-                static_cast<__nv_bfloat16*>(e.dst)[i + j] = __float2bfloat16_rn(o[j]);
-            else
-                static_cast<float*>(e.dst)[i + j] = o[j];
-        }
-}
-
-// The squares are taken and added in 64 bits: the square of any fp32 number fits a double, so neither large nor tiny
-// gradients leave its range, and this GPU's 64-bit rate is far above what HBM delivers to it.
-__device__ __forceinline__ double squares(const Four& f) {
-    const double a = f.v[0], b = f.v[1], c = f.v[2], d = f.v[3];
-    return fma(a, a, b * b) + fma(c, c, d * d);
+        for (int k = 0; k < 4; ++k)
+            if (off + 4 * k < p.bytes) reinterpret_cast<float*>(p.dst + off)[k] = v[k];
+    }
 }
 
 // sum over the CTA, the same order every time; every thread gets it
@@ -104,31 +111,29 @@ __device__ __forceinline__ float clip_factor(double norm, double max_norm) {
     return norm > max_norm && isfinite(norm) ? (float)(max_norm / norm) : 1.f;
 }
 
-// Small lists (up to kClusterChunks chunks): one launch of one cluster that keeps every gradient in registers between the
-// sum and the scaling, so each is read once.  The eight sums meet in distributed shared memory.
+// Small lists (up to kClusterPieces pieces, laid out by the host): one launch of one cluster that keeps every gradient in
+// registers between the sum and the scaling, so each is read once.  The CTAs' sums meet in distributed shared memory.
 constexpr int kClusterCtas = 8, kClusterThreads = 1024, kHeld = 8;
-constexpr int kClusterChunks = kClusterCtas * kHeld;
+constexpr int kClusterPieces = kClusterCtas * kHeld;
+struct PieceTable {
+    int count;
+    Piece p[kClusterPieces];
+};
 __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kClusterThreads)
-    clip_cluster_kernel(const __grid_constant__ ClipTable<kShortList> t, double max_norm, float* norm_out) {
+    clip_cluster_kernel(const __grid_constant__ PieceTable t, double max_norm, float* norm_out) {
     namespace cg = cooperative_groups;
     __shared__ double smem[kClusterThreads / 32];
     __shared__ double sums[kClusterCtas];
     const cg::cluster_group cluster = cg::this_cluster();
-    const int rank = blockIdx.x;
-    Four held[kHeld];
-    double s = 0.0;
-    int k = 0;
-#pragma unroll
-    for (int q = 0; q < kHeld; ++q) {
-        const int64_t c = rank + q * kClusterCtas;
-        if (c < t.chunks) {
-            while (k + 1 < t.count && t.e[k + 1].first <= c) ++k;
-            held[q] = load4(t.e[k], (c - t.e[k].first) * kClipChunk + threadIdx.x * 4);
-        }
-    }
+    const int rank = blockIdx.x, off = threadIdx.x * 16;
+    Raw held[kHeld];
 #pragma unroll
     for (int q = 0; q < kHeld; ++q)
-        if (rank + q * kClusterCtas < t.chunks) s += squares(held[q]);
+        if (rank + q * kClusterCtas < t.count) held[q] = load16(t.p[rank + q * kClusterCtas], off);
+    double s = 0.0;
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q)
+        if (rank + q * kClusterCtas < t.count) s += squares(t.p[rank + q * kClusterCtas], off, held[q]);
     s = cta_sum<kClusterThreads>(s, smem);
     if (threadIdx.x < kClusterCtas) *cluster.map_shared_rank(&sums[rank], threadIdx.x) = s;
     cluster.sync();   // hardware barrier; no CTA reads another's memory after it
@@ -138,34 +143,47 @@ __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kClusterT
     const double norm = sqrt(total);
     if (norm_out && rank == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     const float f = clip_factor(norm, max_norm);
-    k = 0;
 #pragma unroll
-    for (int q = 0; q < kHeld; ++q) {
-        const int64_t c = rank + q * kClusterCtas;
-        if (c < t.chunks) {
-            while (k + 1 < t.count && t.e[k + 1].first <= c) ++k;
-            if (t.e[k].dst) store4(t.e[k], (c - t.e[k].first) * kClipChunk + threadIdx.x * 4, held[q], f);
-        }
-    }
+    for (int q = 0; q < kHeld; ++q)
+        if (rank + q * kClusterCtas < t.count && t.p[rank + q * kClusterCtas].dst) store16(t.p[rank + q * kClusterCtas], off, held[q], f);
 }
 
-// Larger lists: two launches bound by HBM.  The second one walks the chunks backwards, since what the first one read last is
+// Larger lists: two launches bound by HBM.  The second one walks the pieces backwards, since what the first one read last is
 // still in L2, and its launch overlaps the end of the first (it waits for the sums on the device).
-constexpr int kThreads = 256, kPer = kClipChunk / kThreads / 4, kMaxCtas = 8 * kSMs;
+struct ClipEntry {
+    const char* src;
+    char* dst;
+    int64_t bytes;
+    int64_t first;   // index of the tensor's first piece
+    int bf16, vec;
+};
+// N: room for tensors.  A short list travels as a short kernel argument, which costs less to launch (512 tensors: 20 KB).
+template <int N>
+struct ClipTable {
+    int count;
+    int64_t pieces;
+    ClipEntry e[N];
+};
+constexpr int kShortList = 32;
+__device__ __forceinline__ Piece piece_of(const ClipEntry& e, int64_t piece) {
+    const int64_t at = (piece - e.first) * kPieceBytes;
+    return Piece{e.src + at, e.dst ? e.dst + at : nullptr, (int)min(e.bytes - at, (int64_t)kPieceBytes), e.bf16, e.vec};
+}
+constexpr int kThreads = 256, kPer = kPieceBytes / kThreads / 16, kMaxCtas = 8 * kSMs;
 template <int N>
 __global__ void __launch_bounds__(kThreads) clip_norm_kernel(const __grid_constant__ ClipTable<N> t, double* partial) {
     __shared__ double smem[kThreads / 32];
     cudaTriggerProgrammaticLaunchCompletion();
     double s = 0.0;
     int k = 0;
-    for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    for (int64_t c = blockIdx.x; c < t.pieces; c += gridDim.x) {
         while (k + 1 < t.count && t.e[k + 1].first <= c) ++k;
-        const int64_t i = (c - t.e[k].first) * kClipChunk + threadIdx.x * 4;
-        Four f[kPer];
+        const Piece p = piece_of(t.e[k], c);
+        Raw r[kPer];
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) f[q] = load4(t.e[k], i + q * kThreads * 4);
+        for (int q = 0; q < kPer; ++q) r[q] = load16(p, (q * kThreads + threadIdx.x) * 16);
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) s += squares(f[q]);
+        for (int q = 0; q < kPer; ++q) s += squares(p, (q * kThreads + threadIdx.x) * 16, r[q]);
     }
     s = cta_sum<kThreads>(s, smem);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -182,15 +200,15 @@ __global__ void __launch_bounds__(kThreads) clip_scale_kernel(const __grid_const
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     const float factor = clip_factor(norm, max_norm);
     int k = t.count - 1;
-    for (int64_t c = t.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
+    for (int64_t c = t.pieces - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
         while (t.e[k].first > c) --k;
-        if (!t.e[k].dst || (factor == 1.f && t.e[k].dst == t.e[k].src)) continue;
-        const int64_t i = (c - t.e[k].first) * kClipChunk + threadIdx.x * 4;
-        Four f[kPer];
+        const Piece p = piece_of(t.e[k], c);
+        if (!p.dst || (factor == 1.f && p.dst == p.src)) continue;
+        Raw r[kPer];
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) f[q] = load4(t.e[k], i + q * kThreads * 4);
+        for (int q = 0; q < kPer; ++q) r[q] = load16(p, (q * kThreads + threadIdx.x) * 16);
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) store4(t.e[k], i + q * kThreads * 4, f[q], factor);
+        for (int q = 0; q < kPer; ++q) store16(p, (q * kThreads + threadIdx.x) * 16, r[q], factor);
     }
 }
 
@@ -199,7 +217,7 @@ constexpr int64_t kClipWorkspace = kMaxCtas * (int64_t)sizeof(double);
 template <int N>
 slicegcn_status_t fill_table(const slicegcn_tensor_list* list, ClipTable<N>& t) {
     t.count = 0;
-    t.chunks = 0;
+    t.pieces = 0;
     for (int i = 0; i < list->count; ++i) {
         const int dt = list->dtypes ? list->dtypes[i] : SLICEGCN_F32;
         if (dt != SLICEGCN_F32 && dt != SLICEGCN_BF16) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "clip_grads: bad dtype of tensor %d", i);
@@ -213,20 +231,20 @@ slicegcn_status_t fill_table(const slicegcn_tensor_list* list, ClipTable<N>& t) 
         if ((uintptr_t)src % esz || (uintptr_t)dst % esz)
             SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "clip_grads: tensor %d is not aligned to its element type", i);
         ClipEntry& e = t.e[t.count++];
-        e.src = src;
-        e.dst = dst;
-        e.elems = elems;
-        e.first = t.chunks;
+        e.src = static_cast<const char*>(src);
+        e.dst = static_cast<char*>(dst);
+        e.bytes = elems * esz;
+        e.first = t.pieces;
         e.bf16 = dt == SLICEGCN_BF16;
-        e.vec = (uintptr_t)src % (4 * esz) == 0 && (uintptr_t)dst % (4 * esz) == 0;
-        t.chunks += (elems + kClipChunk - 1) / kClipChunk;
+        e.vec = (uintptr_t)src % 16 == 0 && (uintptr_t)dst % 16 == 0;
+        t.pieces += (e.bytes + kPieceBytes - 1) / kPieceBytes;
     }
     return SLICEGCN_OK;
 }
 
 template <int N>
 slicegcn_status_t run_two(const ClipTable<N>& t, double max_norm, float* norm_out, double* partial, cudaStream_t st) {
-    const int ctas = (int)std::min<int64_t>(std::max<int64_t>(t.chunks, 1), kMaxCtas);
+    const int ctas = (int)std::min<int64_t>(std::max<int64_t>(t.pieces, 1), kMaxCtas);
     clip_norm_kernel<N><<<ctas, kThreads, 0, st>>>(t, partial);
     SGCN_LAUNCH_CHECK();
     cudaLaunchAttribute attr;
@@ -274,8 +292,14 @@ slicegcn_status_t slicegcn_clip_grads(const slicegcn_tensor_list* list, double m
         SGCN_TRY(fill_table(list, t));
         if (!room)
             SGCN_FAIL(SLICEGCN_ERR_ALLOC, "clip_grads: workspace too small (%lld < %lld bytes)", (long long)workspace_bytes, (long long)kClipWorkspace);
-        if (t.chunks > kClusterChunks) return run_two(t, max_norm, norm_out, partial, st);
-        clip_cluster_kernel<<<kClusterCtas, kClusterThreads, 0, st>>>(t, max_norm, norm_out);
+        if (t.pieces > kClusterPieces) return run_two(t, max_norm, norm_out, partial, st);
+        PieceTable small;
+        small.count = (int)t.pieces;
+        for (int k = 0, c = 0; k < t.count; ++k)
+            for (int64_t at = 0; at < t.e[k].bytes; at += kPieceBytes, ++c)
+                small.p[c] = Piece{t.e[k].src + at, t.e[k].dst ? t.e[k].dst + at : nullptr,
+                                   (int)std::min<int64_t>(t.e[k].bytes - at, kPieceBytes), t.e[k].bf16, t.e[k].vec};
+        clip_cluster_kernel<<<kClusterCtas, kClusterThreads, 0, st>>>(small, max_norm, norm_out);
         SGCN_LAUNCH_CHECK();
         count_launch();
         return SLICEGCN_OK;
