@@ -115,6 +115,19 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(int64_t n, int64_t v
 // Keys run from 0 to `vocab`: the id, or `vocab` (sorted last) for positions that take no part.  Per digit two launches:
 // sort_count_kernel counts every tile's digits, sort_scatter_kernel turns the counts into offsets (each CTA reads the whole
 // table of tiles x digits, a few hundred KB that stay in L2, so no scan launch stands between the two) and moves the pairs.
+// lanes that are live and hold the same digit of at most BITS bits
+template <int BITS>
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, bool live) {
+    uint32_t peers = __ballot_sync(0xffffffffu, live);
+#pragma unroll
+    for (int k = 0; k < BITS; ++k) {
+        const bool set = (d >> k) & 1u;
+        const uint32_t with = __ballot_sync(0xffffffffu, set);
+        peers &= set ? with : ~with;
+    }
+    return peers;
+}
+
 struct SortArgs {
     int32_t n;
     int64_t vocab;
@@ -226,13 +239,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
             if (b + 32 * j >= i1) break;
             const bool live = b + 32 * j + lane < i1;
             const uint32_t d = (item[j].x >> a.shift) & mask;
-            uint32_t peers = __ballot_sync(0xffffffffu, live);   // lanes with the same digit, bit by bit
-#pragma unroll
-            for (int k = 0; k < kMaxDigitBits; ++k) {
-                const bool set = (d >> k) & 1u;
-                const uint32_t with = __ballot_sync(0xffffffffu, set);
-                peers &= set ? with : ~with;
-            }
+            const uint32_t peers = same_digit<kMaxDigitBits>(d, live);
             const uint32_t rank = __popc(peers & ((1u << lane) - 1u));
             uint32_t to = 0;
             if (live) to = mine[d] + rank;
@@ -302,24 +309,45 @@ __device__ __forceinline__ void store4(float* row, int col, int stride, int widt
     }
 }
 
+// Shared memory of a CTA that sums.
+template <int L>
+struct SumShared {
+    static constexpr int U = kSumThreads / L;
+    static constexpr int A = L < kAhead ? L : kAhead;   // rows on their way at any time, and positions per batch
+    float4 ring[A][kSumThreads];
+    float sums[U][2][4 * L];
+    int4 unit_info[U];   // {head present, head ends here, tail's id or -1, unused}
+};
+// The sorted positions: in memory, or (small problems) in the CTA's own shared memory as 12 bits of position under the
+// id's distance from the CTA's first one.
+struct PairsInMemory {
+    const uint2* p;
+    __device__ __forceinline__ uint2 operator()(int i) const { return p[i]; }
+};
+constexpr int kSmallBits = 12, kSmallN = 1 << kSmallBits;
+struct PairsInShared {
+    const uint32_t* p;
+    uint32_t first_id;
+    __device__ __forceinline__ uint2 operator()(int i) const {
+        return make_uint2((p[i] >> kSmallBits) + first_id, p[i] & (kSmallN - 1));
+    }
+};
+
+// One CTA's share: positions cta * U * per_unit and on, of n.  ONE: the CTA holds all positions of its ids.
 // VEC: lane l holds columns 4 l .. 4 l + 3 of the tile (16-byte accesses); else columns l, l + L, l + 2 L, l + 3 L
-template <int L, bool VEC>
-__global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const SumArgs a) {
-    constexpr int U = kSumThreads / L;
-    constexpr int A = L < kAhead ? L : kAhead;   // rows on their way at any time, and positions per batch
-    __shared__ __align__(16) float ring[A][kSumThreads][4];
-    __shared__ float sums[U][2][4 * L];
-    __shared__ int4 unit_info[U];   // {head present, head ends here, tail's id or -1, unused}
+template <int L, bool VEC, bool ONE, typename Pairs>
+__device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, int n, int per_unit, int cta, SumShared<L>& sh) {
+    constexpr int U = SumShared<L>::U, A = SumShared<L>::A;
     const int tid = threadIdx.x, l = tid & (L - 1), unit = tid / L;
     const int c0 = blockIdx.y * 4 * L;
     const int col = c0 + (VEC ? 4 * l : l);
     const bool live_col = col < a.width;
-    const int64_t s64 = ((int64_t)blockIdx.x * U + unit) * a.per_unit;
-    const int s = (int)min((int64_t)a.n, s64), e = (int)min((int64_t)a.n, s64 + a.per_unit);
+    const int64_t s64 = ((int64_t)cta * U + unit) * per_unit;
+    const int s = (int)min((int64_t)n, s64), e = (int)min((int64_t)n, s64 + per_unit);
     const unsigned group = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((tid & 31) & ~(L - 1));
     const uint32_t none = (uint32_t)a.vocab;
-    const uint32_t before = s > 0 && s < e ? a.pairs[s - 1].x : 0xffffffffu;
-    const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(&ring[0][tid][0]);
+    const uint32_t before = s > 0 && s < e ? pairs(s - 1).x : 0xffffffffu;
+    const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(&sh.ring[0][tid]);
     uint32_t key = 0xffffffffu;
     bool first = true;             // still in the unit's first run
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
@@ -327,7 +355,7 @@ __global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const
     int tail_id = -1;
     auto put = [&](int which) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sums[unit][which][VEC ? 4 * l + j : l + j * L] = acc[j];
+        for (int j = 0; j < 4; ++j) sh.sums[unit][which][VEC ? 4 * l + j : l + j * L] = acc[j];
     };
     auto finish = [&](bool goes_on) {   // the run of `key` ends, or the unit does
         if (key >= none) return;
@@ -336,7 +364,7 @@ __global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const
             put(0);
             return;
         }
-        if (a.present && l == 0 && blockIdx.y == 0) a.present[key] = 1;
+        if (!ONE && l == 0 && blockIdx.y == 0) a.present[key] = 1;
         if (goes_on) {
             tail_id = (int)key;
             put(1);
@@ -344,11 +372,11 @@ __global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const
             store4<VEC>(a.dtable + (int64_t)key * a.dtable_ld, col, L, a.width, a.accumulate, acc);
         }
     };
-    auto batch = [&](int b) { return l < A && b + l < e ? a.pairs[b + l] : make_uint2(none, 0); };
+    auto batch = [&](int b) { return l < A && b + l < e ? pairs(b + l) : make_uint2(none, 0); };
     auto request = [&](int i, const uint2& p) {   // row i of a batch into slot i
         const uint32_t k = __shfl_sync(group, p.x, i, L), pos = __shfl_sync(group, p.y, i, L);
         if (live_col && k < none)
-            request4<VEC>(my_ring + i * (int)sizeof(ring[0]), a.dout + (int64_t)pos * a.dout_ld, col, L, a.width);
+            request4<VEC>(my_ring + i * (int)sizeof(sh.ring[0]), a.dout + (int64_t)pos * a.dout_ld, col, L, a.width);
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     uint2 cur = batch(s), next = batch(s + A);
@@ -375,7 +403,7 @@ __global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const
                 acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
             }
             if (live_col && k < none) {
-                const float4 v = *reinterpret_cast<const float4*>(&ring[i][tid][0]);
+                const float4 v = sh.ring[i][tid];
                 acc[0] = fmaf(a.scale, v.x, acc[0]);
                 if (VEC || col + L < a.width) acc[1] = fmaf(a.scale, v.y, acc[1]);
                 if (VEC || col + 2 * L < a.width) acc[2] = fmaf(a.scale, v.z, acc[2]);
@@ -386,8 +414,8 @@ __global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const
         next = later;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-    if (s < e) finish(e < a.n && a.pairs[e].x == key);
-    if (l == 0) unit_info[unit] = make_int4(head, head_ends, tail_id, 0);
+    if (s < e) finish(e < n && pairs(e).x == key);
+    if (l == 0) sh.unit_info[unit] = make_int4(head, head_ends, tail_id, 0);
     __syncthreads();
     // one thread per column joins the units' sums in order
     if (tid >= 4 * L || c0 + tid >= a.width) return;
@@ -400,24 +428,145 @@ __global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const
     };
 #pragma unroll 8
     for (int k = 0; k < U; ++k) {
-        const int4 f = unit_info[k];
+        const int4 f = sh.unit_info[k];
         if (f.x) {
             if (!open) open = true, started = false, sum = 0.f, any_head = true;
-            sum += sums[k][0][tid];
+            sum += sh.sums[k][0][tid];
             if (f.y) {
                 if (started)
                     write(id, sum);
-                else
-                    a.head[(int64_t)blockIdx.x * a.width + c0 + tid] = sum, ended = true;
+                else if (!ONE)
+                    a.head[(int64_t)cta * a.width + c0 + tid] = sum, ended = true;
                 open = false;
             }
         }
-        if (f.z >= 0) open = true, started = true, sum = sums[k][1][tid], id = f.z;
+        if (f.z >= 0) open = true, started = true, sum = sh.sums[k][1][tid], id = f.z;
     }
+    if (ONE) return;
     const bool tail = open && started;
-    if (tail) a.tail[(int64_t)blockIdx.x * a.width + c0 + tid] = sum;
-    if (open && !started) a.head[(int64_t)blockIdx.x * a.width + c0 + tid] = sum;
-    if (tid == 0 && blockIdx.y == 0) a.info[blockIdx.x] = make_int4(any_head, ended, tail, id);
+    if (tail) a.tail[(int64_t)cta * a.width + c0 + tid] = sum;
+    if (open && !started) a.head[(int64_t)cta * a.width + c0 + tid] = sum;
+    if (tid == 0 && blockIdx.y == 0) a.info[cta] = make_int4(any_head, ended, tail, id);
+}
+
+template <int L, bool VEC>
+__global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const SumArgs a) {
+    __shared__ SumShared<L> sh;
+    sum_sorted<L, VEC, false>(a, PairsInMemory{a.pairs}, a.n, a.per_unit, blockIdx.x, sh);
+}
+
+// Small problems (up to kSmallN positions): one launch.  Every CTA owns a stretch of the table, picks the positions of its ids
+// out of all of them, sorts those in shared memory and sums them as above; nothing passes between CTAs.
+constexpr int kSmallRows = 1 << 16;   // rows of the table per CTA at most
+template <int L>
+struct SmallShared {
+    SumShared<L> sum;
+    uint32_t list[2][kSmallN];
+    uint32_t next[8][256];
+    uint32_t warp_total[8];
+    uint32_t before[kSmallN / kSumThreads][8];
+    uint32_t present[kSmallRows / 32];
+};
+template <int L, bool VEC>
+__global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs a, const int32_t* ids, int rows_per_cta, int32_t* status) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    SmallShared<L>& sh = *reinterpret_cast<SmallShared<L>*>(raw);
+    constexpr int K = kSmallN / kSumThreads;
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    const uint32_t v0 = blockIdx.x * (uint32_t)rows_per_cta;
+    const uint32_t rows = (uint32_t)min((int64_t)rows_per_cta, a.vocab - v0);
+    int32_t id[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int i = k * kSumThreads + tid;
+        id[k] = ids[min(i, a.n - 1)];
+        if (i >= a.n) id[k] = -1;
+    }
+    for (int k = tid; k < (int)(rows + 31) / 32; k += kSumThreads) sh.present[k] = 0;
+    uint32_t mine[K];   // lanes of the warp that found one of the CTA's ids
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (blockIdx.x == 0 && blockIdx.y == 0 && status && id[k] != -1 && (uint32_t)id[k] >= (uint32_t)a.vocab) atomicExch(status, SLICEGCN_DEVSTATUS_BAD_ID);
+        mine[k] = __ballot_sync(0xffffffffu, id[k] >= 0 && (uint32_t)id[k] - v0 < rows);
+        if (lane == 0) sh.before[k][w] = __popc(mine[k]);
+    }
+    __syncthreads();
+    if (w == 0) {   // K * 8 counts, four per lane, to exclusive sums
+        uint32_t* c = &sh.before[0][0];
+        uint32_t v[K * 8 / 32], sum = 0;
+#pragma unroll
+        for (int q = 0; q < K * 8 / 32; ++q) v[q] = c[lane * (K * 8 / 32) + q], sum += v[q];
+        uint32_t incl = sum;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        uint32_t at = incl - sum;
+#pragma unroll
+        for (int q = 0; q < K * 8 / 32; ++q) c[lane * (K * 8 / 32) + q] = at, at += v[q];
+        if (lane == 31) sh.warp_total[0] = incl;
+    }
+    __syncthreads();
+    const int m = (int)sh.warp_total[0];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (mine[k] >> lane & 1u) {
+            const uint32_t local = (uint32_t)id[k] - v0;
+            sh.list[0][sh.before[k][w] + __popc(mine[k] & ((1u << lane) - 1u))] = local << kSmallBits | (uint32_t)(k * kSumThreads + tid);
+            atomicOr(&sh.present[local >> 5], 1u << (local & 31));
+        }
+    __syncthreads();
+    // stable sort by the row, eight bits at a time (most CTAs own few rows: one pass, or none)
+    int cur = 0;
+    const int run = ((m + 255) / 256) * 32;   // positions per warp
+    for (int shift = kSmallBits; m > 0 && (rows - 1) >> (shift - kSmallBits); shift += 8, cur ^= 1) {
+        for (int k = lane; k < 256; k += 32) sh.next[w][k] = 0;
+        __syncwarp();
+        const int i0 = min(m, w * run), i1 = min(m, i0 + run);
+        for (int i = i0 + lane; i < i1; i += 32) atomicAdd(&sh.next[w][sh.list[cur][i] >> shift & 255u], 1u);
+        __syncthreads();
+        uint32_t total = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) total += sh.next[k][tid];
+        uint32_t incl = total;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        if (lane == 31) sh.warp_total[w] = incl;
+        __syncthreads();
+        uint32_t at = incl - total;
+        for (int k = 0; k < w; ++k) at += sh.warp_total[k];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t c = sh.next[k][tid];
+            sh.next[k][tid] = at;
+            at += c;
+        }
+        __syncthreads();
+        for (int b = i0; b < i1; b += 32) {
+            const bool live = b + lane < i1;
+            const uint32_t p = live ? sh.list[cur][b + lane] : 0, d = p >> shift & 255u;
+            const uint32_t peers = same_digit<8>(d, live);
+            const uint32_t rank = __popc(peers & ((1u << lane) - 1u));
+            uint32_t to = 0;
+            if (live) to = sh.next[w][d] + rank;
+            __syncwarp();
+            if (live && rank == 0) sh.next[w][d] += __popc(peers);
+            __syncwarp();
+            if (live) sh.list[cur ^ 1][to] = p;
+        }
+        __syncthreads();
+    }
+    constexpr int U = SumShared<L>::U;
+    if (!a.accumulate) {   // rows without an id
+        const int l = tid & (L - 1), col = blockIdx.y * 4 * L + (VEC ? 4 * l : l);
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        if (col < a.width)
+            for (uint32_t r = tid / L; r < rows; r += U)
+                if (!(sh.present[r >> 5] >> (r & 31) & 1u)) store4<VEC>(a.dtable + (int64_t)(v0 + r) * a.dtable_ld, col, L, a.width, 0, zero);
+    }
+    sum_sorted<L, VEC, true>(a, PairsInShared{sh.list[cur], v0}, m, (m + U - 1) / U, 0, sh.sum);
 }
 
 // Rows of ids that do not occur, as lane groups like those above.
@@ -481,6 +630,10 @@ slicegcn_status_t check_desc(const slicegcn_embed_desc* d, const char* who) {
 
 int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 
+// One launch while the picking (every CTA looks at all ids) and an id that holds all positions (one CTA sums them) are
+// cheaper than the sort's launches.
+bool is_small(const slicegcn_embed_desc* d) { return d->n > 0 && d->n <= kSmallN && d->vocab <= (int64_t)kSMs * kSmallRows; }
+
 // How the gradient is cut, and where its parts lie in the workspace.
 struct GradPlan {
     int passes, bits, tiles;     // digit passes and bits per digit; CTAs of a pass
@@ -541,6 +694,28 @@ slicegcn_status_t launch_sum(const SumArgs& a, int col_tiles, cudaStream_t st) {
         count_launch();
     }
     return SLICEGCN_OK;
+}
+
+template <int L, bool VEC>
+slicegcn_status_t launch_small(const SumArgs& a, const int32_t* ids, int32_t* status, int col_tiles, cudaStream_t st) {
+    const int rows = (int)((a.vocab + kSMs - 1) / kSMs);
+    constexpr int smem = (int)sizeof(SmallShared<L>);
+    SGCN_CUDA(cudaFuncSetAttribute(embed_small_kernel<L, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    embed_small_kernel<L, VEC><<<dim3((unsigned)((a.vocab + rows - 1) / rows), col_tiles), kSumThreads, smem, st>>>(a, ids, rows, status);
+    SGCN_LAUNCH_CHECK();
+    count_launch();
+    return SLICEGCN_OK;
+}
+
+template <bool VEC>
+slicegcn_status_t launch_smalls(const SumArgs& a, const int32_t* ids, int32_t* status, int lanes, int col_tiles, cudaStream_t st) {
+    switch (lanes) {
+        case 2: return launch_small<2, VEC>(a, ids, status, col_tiles, st);
+        case 4: return launch_small<4, VEC>(a, ids, status, col_tiles, st);
+        case 8: return launch_small<8, VEC>(a, ids, status, col_tiles, st);
+        case 16: return launch_small<16, VEC>(a, ids, status, col_tiles, st);
+        default: return launch_small<32, VEC>(a, ids, status, col_tiles, st);
+    }
 }
 
 template <bool VEC>
@@ -632,12 +807,30 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
         SGCN_FAIL(SLICEGCN_ERR_ALLOC, "embed_backward: workspace too small (%lld < %lld bytes)", (long long)workspace_bytes, (long long)p.total);
     cudaStream_t st = (cudaStream_t)stream;
     char* ws = static_cast<char*>(workspace);
+    SumArgs t;
+    t.n = (int32_t)d->n;
+    t.vocab = d->vocab;
+    t.width = d->width;
+    t.accumulate = d->accumulate;
+    t.dout = dout;
+    t.dout_ld = d->dout_ld;
+    t.dtable = dtable;
+    t.dtable_ld = d->dtable_ld;
+    t.scale = (float)d->scale;
+    t.present = reinterpret_cast<uint8_t*>(ws + p.present);
+    t.per_unit = p.per_unit;
+    t.sum_ctas = p.sum_ctas;
+    t.head = reinterpret_cast<float*>(ws + p.head);
+    t.tail = reinterpret_cast<float*>(ws + p.tail);
+    t.info = reinterpret_cast<int4*>(ws + p.info);
+    const bool vec = d->width % 4 == 0 && d->dout_ld % 4 == 0 && d->dtable_ld % 4 == 0 && (uintptr_t)dout % 16 == 0 && (uintptr_t)dtable % 16 == 0;
+    if (is_small(d)) return vec ? launch_smalls<true>(t, ids, status, p.lanes, p.col_tiles, st) : launch_smalls<false>(t, ids, status, p.lanes, p.col_tiles, st);
     SortArgs a;
     a.n = (int32_t)d->n;
     a.vocab = d->vocab;
     a.ids = ids;
     a.counts = reinterpret_cast<uint32_t*>(ws + p.counts);
-    a.present = reinterpret_cast<uint8_t*>(ws + p.present);
+    a.present = t.present;
     a.status = status;
     a.bits = p.bits;
     a.tiles = p.tiles;
@@ -661,24 +854,7 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
         SGCN_LAUNCH_CHECK();
         count_launch(2);
     }
-    SumArgs t;
-    t.n = (int32_t)d->n;
-    t.vocab = d->vocab;
-    t.width = d->width;
-    t.accumulate = d->accumulate;
     t.pairs = buf[(p.passes + 1) & 1];
-    t.dout = dout;
-    t.dout_ld = d->dout_ld;
-    t.dtable = dtable;
-    t.dtable_ld = d->dtable_ld;
-    t.scale = (float)d->scale;
-    t.present = a.present;
-    t.per_unit = p.per_unit;
-    t.sum_ctas = p.sum_ctas;
-    t.head = reinterpret_cast<float*>(ws + p.head);
-    t.tail = reinterpret_cast<float*>(ws + p.tail);
-    t.info = reinterpret_cast<int4*>(ws + p.info);
-    const bool vec = d->width % 4 == 0 && d->dout_ld % 4 == 0 && d->dtable_ld % 4 == 0 && (uintptr_t)dout % 16 == 0 && (uintptr_t)dtable % 16 == 0;
     SGCN_TRY(vec ? launch_sums<true>(t, p.lanes, p.col_tiles, st) : launch_sums<false>(t, p.lanes, p.col_tiles, st));
     if (p.sum_ctas > 1) {
         embed_join_kernel<<<dim3(p.sum_ctas, (d->width + 31) / 32), 256, 0, st>>>(t);
