@@ -155,9 +155,11 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
             *reinterpret_cast<uint4*>(a.present + i) = make_uint4(0, 0, 0, 0);   // (rounded up to 16 bytes)
     if (threadIdx.x < 1 << kMaxDigitBits) hist[threadIdx.x] = 0;
     __syncthreads();
+    cudaTriggerProgrammaticLaunchCompletion();
+    if (!FIRST) cudaGridDependencySynchronize();
     const uint32_t mask = (1u << a.bits) - 1u;
     const int64_t i0 = (int64_t)blockIdx.x * a.tile, i1 = min((int64_t)a.n, i0 + a.tile);
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads) {
         const uint32_t key = sort_load<FIRST>(a, (int32_t)i).x;
         if (FIRST && key == (uint32_t)a.vocab && a.status && a.ids[i] != -1) atomicExch(a.status, SLICEGCN_DEVSTATUS_BAD_ID);
@@ -172,7 +174,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
 template <bool FIRST>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortArgs a) {
     extern __shared__ uint32_t next[];   // [kSortWarps][bins] counts of each warp's run, then where its next pair goes
-    __shared__ uint32_t part_before[kSortThreads], part_total[kSortThreads];
+    __shared__ uint4 part_before[kSortThreads], part_total[kSortThreads];   // [part][bins / 4]
     __shared__ uint32_t warp_total[kSortWarps];
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int bins = 1 << a.bits;
@@ -180,6 +182,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     uint32_t* mine = next + w * bins;
     for (int k = lane; k < bins; k += 32) mine[k] = 0;
     __syncwarp();
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
     const int64_t i0 = min((int64_t)a.n, (int64_t)blockIdx.x * a.tile + (int64_t)w * (a.tile / kSortWarps));
     const int64_t i1 = min((int64_t)a.n, i0 + a.tile / kSortWarps);
     uint2 item[kSortItems];
@@ -191,14 +195,17 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
         for (int j = 0; j < kSortItems; ++j)
             if (b + 32 * j + lane < i1) atomicAdd(&mine[(item[j].x >> a.shift) & mask], 1u);
     }
-    {   // tiles before this one, and all tiles, per digit: thread t takes digit t % bins and every (threads / bins)-th tile
-        const int bin = tid & (int)mask, part = tid >> a.bits, parts = kSortThreads >> a.bits;
-        uint32_t before = 0, total = 0;
+    const int quads = bins / 4, parts = kSortThreads / quads;
+    {   // tiles before this one, and all tiles, per digit: thread t takes four digits and every parts-th tile
+        const int quad = tid & (quads - 1), part = tid / quads;
+        const uint4* counts = reinterpret_cast<const uint4*>(a.counts) + quad;
+        uint4 before = make_uint4(0, 0, 0, 0), total = before;
 #pragma unroll 8
         for (int t = part; t < a.tiles; t += parts) {
-            const uint32_t c = a.counts[((int64_t)t << a.bits) + bin];
-            total += c;
-            before += t < (int)blockIdx.x ? c : 0;
+            const uint4 c = counts[(int64_t)t * quads];
+            const uint32_t m = t < (int)blockIdx.x ? 0xffffffffu : 0u;
+            total.x += c.x, total.y += c.y, total.z += c.z, total.w += c.w;
+            before.x += c.x & m, before.y += c.y & m, before.z += c.z & m, before.w += c.w & m;
         }
         part_before[tid] = before;
         part_total[tid] = total;
@@ -206,9 +213,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     __syncthreads();
     uint32_t at = 0, total = 0;
     if (tid < bins)
-        for (int q = tid; q < kSortThreads; q += bins) {
-            at += part_before[q];
-            total += part_total[q];
+#pragma unroll 8
+        for (int q = 0; q < parts; ++q) {
+            at += reinterpret_cast<const uint32_t*>(part_before)[q * bins + tid];
+            total += reinterpret_cast<const uint32_t*>(part_total)[q * bins + tid];
         }
     uint32_t incl = total;
     for (int o = 1; o < 32; o <<= 1) {
@@ -220,11 +228,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     if (tid < bins) {
         at += incl - total;
         for (int k = 0; k < w; ++k) at += warp_total[k];
-#pragma unroll 8
+        uint32_t c[kSortWarps];
+#pragma unroll
+        for (int k = 0; k < kSortWarps; ++k) c[k] = next[k * bins + tid];
+#pragma unroll
         for (int k = 0; k < kSortWarps; ++k) {
-            const uint32_t c = next[k * bins + tid];
             next[k * bins + tid] = at;
-            at += c;
+            at += c[k];
         }
     }
     __syncthreads();
@@ -255,7 +265,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
 // A unit of L lanes takes R consecutive sorted positions and up to 4 L columns, gathers the rows of dout and adds them up
 // in registers.  An id whose positions lie inside the unit is finished there.  The sum of an id that reaches over the
 // unit's edges is left in shared memory; the CTA joins its units' sums in order, and what reaches over the CTA's edges goes
-// to the workspace, where embed_join_kernel joins it, again in order.  Work is split by positions, so an id that holds
+// to the workspace, where embed_finish_kernel joins it, again in order.  Work is split by positions, so an id that holds
 // half of them costs no more than others.
 constexpr int kSumThreads = 256;
 constexpr int kSumPerSM = 5;   // CTAs of them that fit an SM (41 KB of shared memory each)
@@ -452,6 +462,8 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
 template <int L, bool VEC>
 __global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const SumArgs a) {
     __shared__ SumShared<L> sh;
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
     sum_sorted<L, VEC, false>(a, PairsInMemory{a.pairs}, a.n, a.per_unit, blockIdx.x, sh);
 }
 
@@ -569,22 +581,24 @@ __global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs 
     sum_sorted<L, VEC, true>(a, PairsInShared{sh.list[cur], v0}, m, (m + U - 1) / U, 0, sh.sum);
 }
 
-// Rows of ids that do not occur, as lane groups like those above.
+// What is left after the sums.  CTAs 0 .. sum_ctas - 1: the id that starts in that CTA and reaches over its edge; eight
+// groups of 32 lanes each add a share of the CTAs in order, then the shares are added in order.  The others: rows of ids
+// that do not occur, by lane groups like those of the sums.
 template <int L, bool VEC>
-__global__ void __launch_bounds__(256) embed_zero_kernel(const SumArgs a) {
-    const int l = threadIdx.x & (L - 1);
-    const int col = blockIdx.y * 4 * L + (VEC ? 4 * l : l);
-    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-    if (col >= a.width) return;
-    for (int64_t v = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L; v < a.vocab; v += (int64_t)gridDim.x * (256 / L))
-        if (!a.present[v]) store4<VEC>(a.dtable + v * a.dtable_ld, col, L, a.width, 0, zero);
-}
-
-// The ids that reach over the edges of CTAs: eight groups of 32 columns each add a share of the CTAs in order, then the
-// shares are added in order.
-__global__ void __launch_bounds__(256) embed_join_kernel(const SumArgs a) {
-    __shared__ float part[8][32];
+__global__ void __launch_bounds__(256) embed_finish_kernel(const SumArgs a) {
+    __shared__ float part[8][4 * L];
     __shared__ int last;
+    cudaGridDependencySynchronize();
+    const int c0 = blockIdx.y * 4 * L;
+    if ((int)blockIdx.x >= a.sum_ctas) {
+        const int l = threadIdx.x & (L - 1), col = c0 + (VEC ? 4 * l : l);
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        if (col >= a.width) return;
+        const int64_t step = (int64_t)(gridDim.x - a.sum_ctas) * (256 / L);
+        for (int64_t v = ((int64_t)(blockIdx.x - a.sum_ctas) * 256 + threadIdx.x) / L; v < a.vocab; v += step)
+            if (!a.present[v]) store4<VEC>(a.dtable + v * a.dtable_ld, col, L, a.width, 0, zero);
+        return;
+    }
     const int4 f = a.info[blockIdx.x];
     if (!f.z) return;
     const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
@@ -602,22 +616,41 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const SumArgs a) {
         if (lane == 0) last = min(c, a.sum_ctas - 1);
     }
     __syncthreads();
-    const int c = blockIdx.y * 32 + lane;
     const int lo = blockIdx.x + 1, count = last - lo + 1, share = (count + 7) / 8;
-    float s = 0.f;
-    if (c < a.width) {
-        const int k1 = min(last + 1, lo + (g + 1) * share);
+    const int k1 = min(last + 1, lo + (g + 1) * share);
+    for (int c = lane; c < 4 * L; c += 32) {
+        float s = 0.f;
+        if (c0 + c < a.width)
 #pragma unroll 8
-        for (int k = lo + g * share; k < k1; ++k) s += a.head[(int64_t)k * a.width + c];
+            for (int k = lo + g * share; k < k1; ++k) s += a.head[(int64_t)k * a.width + c0 + c];
+        part[g][c] = s;
     }
-    part[g][lane] = s;
     __syncthreads();
-    if (g == 0 && c < a.width) {
-        float t = a.tail[(int64_t)blockIdx.x * a.width + c];
-        for (int k = 0; k < 8; ++k) t += part[k][lane];
-        float* to = a.dtable + (int64_t)f.w * a.dtable_ld + c;
+    if (threadIdx.x < 4 * L && c0 + (int)threadIdx.x < a.width) {
+        const int c = threadIdx.x;
+        float t = a.tail[(int64_t)blockIdx.x * a.width + c0 + c];
+        for (int k = 0; k < 8; ++k) t += part[k][c];
+        float* to = a.dtable + (int64_t)f.w * a.dtable_ld + c0 + c;
         *to = t + (a.accumulate ? *to : 0.f);
     }
+}
+
+// A launch that may start while the one before it ends: its kernel waits on the device for the data.
+template <typename... P, typename... Q>
+slicegcn_status_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const Q&... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    SGCN_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+    count_launch();
+    return SLICEGCN_OK;
 }
 
 slicegcn_status_t check_desc(const slicegcn_embed_desc* d, const char* who) {
@@ -648,7 +681,7 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
     int key_bits = 1;
     while ((d->vocab >> key_bits) > 0) ++key_bits;   // keys run up to vocab itself
     p.passes = (key_bits + kMaxDigitBits - 1) / kMaxDigitBits;
-    p.bits = (key_bits + p.passes - 1) / p.passes;
+    p.bits = std::max(2, (key_bits + p.passes - 1) / p.passes);
     // one CTA per SM at most: every CTA of a pass reads all tiles' counts
     const int64_t granule = kSortWarps * 32;
     int64_t tile = (d->n + kSMs - 1) / kSMs;
@@ -682,17 +715,10 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
 
 template <int L, bool VEC>
 slicegcn_status_t launch_sum(const SumArgs& a, int col_tiles, cudaStream_t st) {
-    if (a.sum_ctas > 0) {
-        embed_sum_kernel<L, VEC><<<dim3(a.sum_ctas, col_tiles), kSumThreads, 0, st>>>(a);
-        SGCN_LAUNCH_CHECK();
-        count_launch();
-    }
-    if (!a.accumulate) {
-        const unsigned blocks = (unsigned)std::min<int64_t>((a.vocab * L + 255) / 256, kSMs * 8);
-        embed_zero_kernel<L, VEC><<<dim3(blocks, col_tiles), 256, 0, st>>>(a);
-        SGCN_LAUNCH_CHECK();
-        count_launch();
-    }
+    if (a.sum_ctas > 0) SGCN_TRY(launch_after(embed_sum_kernel<L, VEC>, dim3(a.sum_ctas, col_tiles), kSumThreads, 0, st, a));
+    const unsigned zero_ctas = a.accumulate ? 0 : (unsigned)std::min<int64_t>((a.vocab * L + 255) / 256, kSMs * 8);
+    if (a.sum_ctas > 1 || zero_ctas > 0)
+        SGCN_TRY(launch_after(embed_finish_kernel<L, VEC>, dim3(a.sum_ctas + zero_ctas, col_tiles), 256, 0, st, a));
     return SLICEGCN_OK;
 }
 
@@ -845,22 +871,16 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
         a.out = buf[k & 1];
         const size_t smem = (size_t)kSortWarps * 4 << p.bits;
         if (k == 0) {
-            sort_count_kernel<true><<<p.tiles, kSortThreads, 0, st>>>(a);
-            sort_scatter_kernel<true><<<p.tiles, kSortThreads, smem, st>>>(a);
+            sort_count_kernel<true><<<p.tiles, kSortThreads, 0, st>>>(a);   // after whatever the stream holds
+            SGCN_LAUNCH_CHECK();
+            count_launch();
         } else {
-            sort_count_kernel<false><<<p.tiles, kSortThreads, 0, st>>>(a);
-            sort_scatter_kernel<false><<<p.tiles, kSortThreads, smem, st>>>(a);
+            SGCN_TRY(launch_after(sort_count_kernel<false>, dim3(p.tiles), kSortThreads, 0, st, a));
         }
-        SGCN_LAUNCH_CHECK();
-        count_launch(2);
+        SGCN_TRY(launch_after(k == 0 ? sort_scatter_kernel<true> : sort_scatter_kernel<false>, dim3(p.tiles), kSortThreads, smem, st, a));
     }
     t.pairs = buf[(p.passes + 1) & 1];
     SGCN_TRY(vec ? launch_sums<true>(t, p.lanes, p.col_tiles, st) : launch_sums<false>(t, p.lanes, p.col_tiles, st));
-    if (p.sum_ctas > 1) {
-        embed_join_kernel<<<dim3(p.sum_ctas, (d->width + 31) / 32), 256, 0, st>>>(t);
-        SGCN_LAUNCH_CHECK();
-        count_launch();
-    }
     return SLICEGCN_OK;
 }
 
