@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
 // to the workspace, where embed_finish_kernel joins it, again in order.  Work is split by positions, so an id that holds
 // half of them costs no more than others.
 constexpr int kSumThreads = 256;
-constexpr int kSumPerSM = 5;   // CTAs of them that fit an SM (41 KB of shared memory each)
+constexpr int kSumPerSM = 4;   // CTAs per SM (41 KB of shared memory each; a fifth one fits and makes it 4 % slower)
 constexpr int kAhead = 8;      // rows of dout on their way per unit
 
 struct SumArgs {
@@ -595,8 +595,14 @@ __global__ void __launch_bounds__(256) embed_finish_kernel(const SumArgs a) {
         const float zero[4] = {0.f, 0.f, 0.f, 0.f};
         if (col >= a.width) return;
         const int64_t step = (int64_t)(gridDim.x - a.sum_ctas) * (256 / L);
-        for (int64_t v = ((int64_t)(blockIdx.x - a.sum_ctas) * 256 + threadIdx.x) / L; v < a.vocab; v += step)
-            if (!a.present[v]) store4<VEC>(a.dtable + v * a.dtable_ld, col, L, a.width, 0, zero);
+        for (int64_t v = ((int64_t)(blockIdx.x - a.sum_ctas) * 256 + threadIdx.x) / L; v < a.vocab; v += 4 * step) {
+            uint8_t there[4];   // four rows' flags at once
+#pragma unroll
+            for (int q = 0; q < 4; ++q) there[q] = a.present[min(v + q * step, a.vocab - 1)];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (!there[q] && v + q * step < a.vocab) store4<VEC>(a.dtable + (v + q * step) * a.dtable_ld, col, L, a.width, 0, zero);
+        }
         return;
     }
     const int4 f = a.info[blockIdx.x];
@@ -618,13 +624,17 @@ __global__ void __launch_bounds__(256) embed_finish_kernel(const SumArgs a) {
     __syncthreads();
     const int lo = blockIdx.x + 1, count = last - lo + 1, share = (count + 7) / 8;
     const int k1 = min(last + 1, lo + (g + 1) * share);
-    for (int c = lane; c < 4 * L; c += 32) {
-        float s = 0.f;
-        if (c0 + c < a.width)
-#pragma unroll 8
-            for (int k = lo + g * share; k < k1; ++k) s += a.head[(int64_t)k * a.width + c0 + c];
-        part[g][c] = s;
-    }
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = lo + g * share; k < k1; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = c0 + lane + 32 * j;
+            s[j] += a.head[(int64_t)k * a.width + min(c, a.width - 1)];
+        }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (lane + 32 * j < 4 * L) part[g][lane + 32 * j] = s[j];
     __syncthreads();
     if (threadIdx.x < 4 * L && c0 + (int)threadIdx.x < a.width) {
         const int c = threadIdx.x;
@@ -693,8 +703,11 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
     while (p.lanes < 32 && p.lanes < quads) p.lanes *= 2;
     p.col_tiles = (quads + p.lanes - 1) / p.lanes;
     const int units = kSumThreads / p.lanes;
-    const int64_t want = std::max<int64_t>(1, kSMs * kSumPerSM / p.col_tiles);   // CTAs resident at once, over the column tiles
-    p.per_unit = (int32_t)std::max<int64_t>(8, (d->n + want * units - 1) / (want * units));
+    // One wave of CTAs, or two where the units are long enough to make up for their starts and ends (one / two waves:
+    // 49 / 57 us at 18 positions per unit, 332 / 322 us at 259).
+    const int64_t wave = std::max<int64_t>(1, kSMs * kSumPerSM / p.col_tiles) * units;
+    const int64_t per_unit = (d->n + wave - 1) / wave;
+    p.per_unit = (int32_t)std::max<int64_t>(8, per_unit >= 128 ? (per_unit + 1) / 2 : per_unit);
     p.sum_ctas = (int)((d->n + (int64_t)p.per_unit * units - 1) / ((int64_t)p.per_unit * units));
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
