@@ -78,6 +78,8 @@ struct Chunk<__nv_bfloat16, E> {
         word[j >> 1] = j & 1 ? word[j >> 1] | b << 16 : b;   // even ones come first
     }
 };
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
@@ -176,6 +178,34 @@ __device__ __forceinline__ void staged_get(const unsigned char* at, float (&f)[E
     }
 }
 
+// Columns that allow no wide accesses go to shared memory as the aligned 4-byte words that hold them; a bf16 row may start in
+// the middle of a word (odd_of: then its element c is element c + 1 there).  Other lanes' words are read as well, so the
+// group's lanes meet (__syncwarp) before they read and before the words are replaced.
+__device__ __forceinline__ void copy_async4(uint32_t to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ int odd_of(const T* row) {
+    return sizeof(T) == 4 ? 0 : (int)((uintptr_t)row >> 1 & 1);
+}
+// the words of `count` elements, every `lanes`-th by one lane; at most MOST per lane
+template <int MOST, typename T>
+__device__ __forceinline__ void copy_words(uint32_t to, const T* row, int count, int lane, int lanes) {
+    constexpr int PER = 4 / (int)sizeof(T);
+    const char* from = reinterpret_cast<const char*>((uintptr_t)row & ~(uintptr_t)3);
+    const int words = (count + odd_of(row) + PER - 1) / PER;
+#pragma unroll
+    for (int q = 0; q < MOST; ++q) {
+        const int k = lane + q * lanes;
+        if (k < words) copy_async4(to + 4 * k, from + 4 * k);
+    }
+}
+template <typename T, int E>
+__device__ __forceinline__ void words_get(const unsigned char* at, int odd, const Columns<false, E>& cols, int i, float (&f)[E]) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) f[j] = to_float(reinterpret_cast<const T*>(at)[odd + (cols.inside(i, j) ? cols.at(i) + j * cols.step : 0)]);
+}
+
 // Where a thread works: its group's slice and first row (then every lanes_rows-th).
 template <int L>
 struct Place {
@@ -192,8 +222,8 @@ struct Place {
 };
 
 // Columns past the slice hold zeros in every array below, so that sums need no tests; a mean is taken off with a factor
-// that is zero there.
-template <typename T, bool VEC, int E, int L, int NV>
+// that is zero there.  t becomes t - mean (layer norm); the result is 1 / the root.
+template <int E, int L, int NV>
 __device__ __forceinline__ float centre_and_scale(float (&t)[NV][E], const float (&in)[NV][E], const NormArgs& a, float inv_w) {
     float sum[1] = {0.f};
     if (a.layer) {
@@ -219,116 +249,219 @@ __device__ __forceinline__ float centre_and_scale(float (&t)[NV][E], const float
 
 // Bound by HBM: x, y and gate are read once, h and u written once.  A slice row lives in the registers of its lanes from
 // the first use to the last store, so both norms cost shuffles and no second pass.  What decides is how much is on its way:
-// with one chunk per lane (up to 256 columns of bf16, 128 of fp32) kForwardAhead rows are copied to shared memory ahead,
-// and the weights stay in registers over all rows.
+// kForwardAhead rows are copied to shared memory ahead.  One chunk per lane (up to 256 columns of bf16, 128 of fp32), whose
+// weights stay in registers over all rows.
 constexpr int kForwardAhead = 4;
-template <typename T, bool VEC, int E, int L, int NV>
-__global__ void __launch_bounds__(256, VEC && NV == 1 ? 2 : 1) norm_forward_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
-    constexpr bool RING = VEC && NV == 1;
-    constexpr int S = kForwardAhead;
-    extern __shared__ __align__(16) unsigned char ring[];   // [S][x, y, gate][thread] chunks
+template <typename T, bool VEC, int E>
+constexpr int kForwardSlot = VEC ? E * (int)sizeof(T) : 16;   // bytes of shared memory per thread, tensor and row
+template <typename T, bool VEC, int E, int L>
+__global__ void __launch_bounds__(256, 2) norm_forward_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
+    constexpr int S = kForwardAhead, kSlot = kForwardSlot<T, VEC, E>, kTensor = 256 * kSlot;
+    extern __shared__ __align__(16) unsigned char ring[];   // [S][x, y, gate][thread] slots
     const Place<L> place(a);
     const Columns<VEC, E> cols(place.lane, L, a.w, place.idle);
     const int c0 = place.slice * a.w;
     const float inv_w = 1.f / (float)a.w;
-    const bool ragged = a.w % E != 0, full = a.w == NV * E * L;
-    float wp[E], bp[E], wq[E], bq[E], in[NV][E];
-    auto weights_post = [&](int i) {
-        cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, wp);
-        cols.vector(a.b_post ? a.b_post + c0 : nullptr, i, 0.f, bp);
+    const bool ragged = a.w % E != 0, full = a.w == E * L;
+    float wp[E], bp[E], wq[E], bq[E], in[1][E];
+    const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;   // the same for all lanes
+    const int slot = (VEC ? threadIdx.x : threadIdx.x & ~(L - 1)) * kSlot;   // the thread's, or its group's
+    const uint32_t ring_u = (uint32_t)__cvta_generic_to_shared(ring) + slot;
+    int next_in = 0, next_out = 0;   // ring stages
+    auto row_of = [&](int64_t r) { return min(place.row + r * a.lanes_rows, a.n - 1); };   // a row past the end is worked on, and not stored
+    auto request = [&](int64_t r) {
+        const int64_t at = row_of(r);
+        const uint32_t to = ring_u + next_in * 3 * kTensor;
+        next_in = next_in + 1 == S ? 0 : next_in + 1;
+        if (r < rounds) {
+            if constexpr (VEC) {
+                const int c = c0 + (cols.inside(0, 0) ? cols.at(0) : 0);
+                if (x) copy_chunk<E>(to, x + at * a.x_ld + c);
+                if (y) copy_chunk<E>(to + kTensor, y + at * a.y_ld + c);
+                if (gate) copy_chunk<E>(to + 2 * kTensor, gate + at * a.gate_ld + c);
+            } else {
+                if (x) copy_words<4>(to, x + at * a.x_ld + c0, a.w, place.lane, L);
+                if (y) copy_words<4>(to + kTensor, y + at * a.y_ld + c0, a.w, place.lane, L);
+                if (gate) copy_words<4>(to + 2 * kTensor, gate + at * a.gate_ld + c0, a.w, place.lane, L);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto weights_pre = [&](int i) {
-        cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, wq);
-        cols.vector(a.b_pre ? a.b_pre + c0 : nullptr, i, 0.f, bq);
+#pragma unroll
+    for (int r = 0; r < S - 1; ++r) request(r);
+    cols.vector(a.w_post ? a.w_post + c0 : nullptr, 0, 1.f, wp);
+    cols.vector(a.b_post ? a.b_post + c0 : nullptr, 0, 0.f, bp);
+    cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, 0, 1.f, wq);
+    cols.vector(a.b_pre ? a.b_pre + c0 : nullptr, 0, 0.f, bq);
+#pragma unroll
+    for (int j = 0; j < E; ++j) in[0][j] = cols.inside(0, j) ? 1.f : 0.f;
+    for (int64_t r = 0; r < rounds; ++r) {
+        const int64_t row = place.row + r * a.lanes_rows;
+        const bool live = row < a.n;
+        float v[1][E], t[1][E], gt[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[0][j] = 0.f;
+        if (!VEC) __syncwarp();
+        request(r + S - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+        const unsigned char* from = ring + slot + next_out * 3 * kTensor;
+        next_out = next_out + 1 == S ? 0 : next_out + 1;
+        if constexpr (VEC) {
+            if (x) staged_get<T>(from, v[0]);
+            if (y) staged_get<T>(from + kTensor, t[0]);
+            if (gate) staged_get<T>(from + 2 * kTensor, gt);
+        } else {
+            __syncwarp();
+            const int64_t at = row_of(r);
+            if (x) words_get<T>(from, odd_of(x + at * a.x_ld + c0), cols, 0, v[0]);
+            if (y) words_get<T>(from + kTensor, odd_of(y + at * a.y_ld + c0), cols, 0, t[0]);
+            if (gate) words_get<T>(from + 2 * kTensor, odd_of(gate + at * a.gate_ld + c0), cols, 0, gt);
+        }
+        cols.keep(v[0], 0, full);
+        if (y) {
+            cols.keep(t[0], 0, full);
+            if (gate) cols.keep(gt, 0, full);
+            const float ry = centre_and_scale<E, L, 1>(t, in, a, inv_w);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                float b = fmaf(t[0][j] * ry, wp[j], bp[j]);
+                if (gate) b *= sigmoid(gt[j]);
+                v[0][j] = fmaf(a.s, b, v[0][j]);
+            }
+        }
+        if (h && live) cols.store(h + row * a.h_ld + c0, 0, v[0], ragged);
+        if (!u) continue;
+        const float rh = centre_and_scale<E, L, 1>(v, in, a, inv_w);
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[0][j] = fmaf(v[0][j] * rh, wq[j], bq[j]);
+        if (live) cols.store(u + row * a.u_ld + c0, 0, v[0], ragged);
+    }
+}
+
+// Slices of up to 1024 columns: a warp per slice row, one row ahead in shared memory, as the gradient below does it (see
+// there).  The weights lie in shared memory; a CTA works on one slice.
+template <typename T, int NV>
+struct StagedForward {
+    static constexpr int kT = NV * 32 * 4 * (int)sizeof(T) + 16, kRow = 3 * kT, kF = NV * 32 * 16, kVectors = 4 * kF;
+    static constexpr int smem(int warps) { return kVectors + warps * 2 * kRow; }
+};
+constexpr int kForwardWarps = 12;
+template <typename T, bool VEC, int NV>
+__global__ void __launch_bounds__(kForwardWarps * 32) norm_forward_staged_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
+    using S = StagedForward<T, NV>;
+    constexpr int E = 4, HF = 512, HT = 32 * E * (int)sizeof(T);
+    extern __shared__ __align__(16) unsigned char ring[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int slice = blockIdx.x % a.p;
+    const int64_t first = (int64_t)(blockIdx.x / a.p) * warps + warp;             // then every lanes_rows-th row
+    const int c0 = slice * a.w;
+    const Columns<VEC, E> cols(lane, 32, a.w, false);
+    const bool ragged = a.w % E != 0;
+    const float inv_w = 1.f / (float)a.w;
+    unsigned char* mine = ring + S::kVectors + warp * 2 * S::kRow;
+    const uint32_t mine_u = (uint32_t)__cvta_generic_to_shared(ring) + S::kVectors + warp * 2 * S::kRow;
+    const unsigned char* vectors = ring + lane * 16;
+    if (warp == 0)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const float* from[4] = {a.w_post, a.b_post, a.w_pre, a.b_pre};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float f[E];
+                cols.vector(from[k] ? from[k] + c0 : nullptr, i, k & 1 ? 0.f : 1.f, f);
+                *reinterpret_cast<float4*>(ring + lane * 16 + i * HF + k * S::kF) = make_float4(f[0], f[1], f[2], f[3]);
+            }
+        }
+    __syncthreads();
+    auto copy = [&](uint32_t to, const T* row) {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (cols.inside(i, 0)) copy_chunk<E>(to + (i * 32 + lane) * E * (int)sizeof(T), row + cols.at(i));
+        } else {
+            copy_words<NV * (int)sizeof(T) + 1>(to, row, a.w, lane, 32);
+        }
     };
+    auto request = [&](int64_t row, int buf) {
+        if (row < a.n) {
+            const uint32_t to = mine_u + buf * S::kRow;
+            if (x) copy(to, x + row * a.x_ld + c0);
+            if (y) copy(to + S::kT, y + row * a.y_ld + c0);
+            if (gate) copy(to + 2 * S::kT, gate + row * a.gate_ld + c0);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // chunk i of a staged row; what lies past the slice becomes zero
+    auto get = [&](const unsigned char* at, int odd, int i, float(&f)[E]) {
+        if constexpr (VEC)
+            staged_get<T>(at + i * HT + lane * E * (int)sizeof(T), f);
+        else
+            words_get<T>(at, odd, cols, i, f);
+        if (a.w < 128 * (i + 1)) cols.keep(f, i, false);
+    };
+    float in[NV][E];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < E; ++j) in[i][j] = cols.inside(i, j) ? 1.f : 0.f;
-    const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;   // the same for all lanes
-    constexpr int kChunk = E * (int)sizeof(T), kTensor = 256 * kChunk;
-    const uint32_t ring_u = RING ? (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * kChunk : 0;
-    Chunk<T, E> qx[NV], qy[NV], qg[NV];
-    int next_in = 0, next_out = 0;   // ring stages
-    auto request = [&](int64_t r) {
-        const int64_t at = min(place.row + r * a.lanes_rows, a.n - 1);   // a row past the end is worked on, and not stored
-        if (RING) {
-            const uint32_t to = ring_u + next_in * 3 * kTensor;
-            next_in = next_in + 1 == S ? 0 : next_in + 1;
-            const int c = cols.inside(0, 0) ? cols.at(0) : 0;
-            if (r < rounds) {
-                if (x) copy_chunk<E>(to, x + at * a.x_ld + c0 + c);
-                if (y) copy_chunk<E>(to + kTensor, y + at * a.y_ld + c0 + c);
-                if (gate) copy_chunk<E>(to + 2 * kTensor, gate + at * a.gate_ld + c0 + c);
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (y) cols.load(qy[i], y + at * a.y_ld + c0, i);
-                if (gate) cols.load(qg[i], gate + at * a.gate_ld + c0, i);
-                if (x) cols.load(qx[i], x + at * a.x_ld + c0, i);
-            }
-        }
-    };
-    if (RING)
-#pragma unroll
-        for (int r = 0; r < S - 1; ++r) request(r);
-    else if (NV == 1)
-        request(0);
-    if (NV == 1) weights_post(0), weights_pre(0);
-    for (int64_t r = 0; r < rounds; ++r) {
-        const int64_t row = place.row + r * a.lanes_rows;
-        const bool live = row < a.n;
-        float v[NV][E], t[NV][E], gt[NV][E];
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < E; ++j) v[i][j] = 0.f;
-        if (RING) {
-            request(r + S - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
-            const unsigned char* from = ring + threadIdx.x * kChunk + next_out * 3 * kTensor;
-            next_out = next_out + 1 == S ? 0 : next_out + 1;
-            if (x) staged_get<T>(from, v[0]), cols.keep(v[0], 0, full);
-            if (y) staged_get<T>(from + kTensor, t[0]), cols.keep(t[0], 0, full);
-            if (gate) staged_get<T>(from + 2 * kTensor, gt[0]), cols.keep(gt[0], 0, full);
-        } else {
-            if (NV > 1) request(r);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (x) qx[i].get(v[i]), cols.keep(v[i], i, full);
-                if (y) qy[i].get(t[i]), cols.keep(t[i], i, full);
-                if (gate) qg[i].get(gt[i]), cols.keep(gt[i], i, full);
-            }
-            if (NV == 1 && r + 1 < rounds) request(r + 1);
-        }
+    request(first, 0);
+    int buf = 0;
+    for (int64_t row = first; row < a.n; row += a.lanes_rows, buf ^= 1) {
+        if (!VEC) __syncwarp();
+        request(row + a.lanes_rows, buf ^ 1);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        if (!VEC) __syncwarp();
+        const unsigned char* at = mine + buf * S::kRow;
+        float v[NV][E];
         if (y) {
-            const float ry = centre_and_scale<T, VEC, E, L, NV>(t, in, a, inv_w);
+            const int odd = odd_of(y + row * a.y_ld + c0);
+            float t[NV][E];
+#pragma unroll
+            for (int i = 0; i < NV; ++i) get(at + S::kT, odd, i, t[i]);
+            const float ry = centre_and_scale<E, 32, NV>(t, in, a, inv_w);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (NV > 1) weights_post(i);
+                float wp[E], bp[E], gt[E];
+                staged_get<float>(vectors + i * HF, wp), staged_get<float>(vectors + S::kF + i * HF, bp);
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    float b = fmaf(t[i][j] * ry, wp[j], bp[j]);
-                    if (gate) b *= sigmoid(gt[i][j]);
-                    v[i][j] = fmaf(a.s, b, v[i][j]);
+                for (int j = 0; j < E; ++j) v[i][j] = fmaf(t[i][j] * ry, wp[j], bp[j]) * a.s;
+                if (gate) {
+                    get(at + 2 * S::kT, odd_of(gate + row * a.gate_ld + c0), i, gt);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) v[i][j] *= sigmoid(gt[j]);
                 }
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < E; ++j) v[i][j] = 0.f;
         }
-        if (h && live)
+        if (x) {
+            const int odd = odd_of(x + row * a.x_ld + c0);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float f[E];
+                get(at, odd, i, f);
+#pragma unroll
+                for (int j = 0; j < E; ++j) v[i][j] += f[j];
+            }
+        }
+        if (h)
 #pragma unroll
             for (int i = 0; i < NV; ++i) cols.store(h + row * a.h_ld + c0, i, v[i], ragged);
         if (!u) continue;
-        const float rh = centre_and_scale<T, VEC, E, L, NV>(v, in, a, inv_w);
+        const float rh = centre_and_scale<E, 32, NV>(v, in, a, inv_w);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (NV > 1) weights_pre(i);
+            float wq[E], bq[E];
+            staged_get<float>(vectors + 2 * S::kF + i * HF, wq), staged_get<float>(vectors + 3 * S::kF + i * HF, bq);
 #pragma unroll
             for (int j = 0; j < E; ++j) v[i][j] = fmaf(v[i][j] * rh, wq[j], bq[j]);
-            if (live) cols.store(u + row * a.u_ld + c0, i, v[i], ragged);
+            cols.store(u + row * a.u_ld + c0, i, v[i], ragged);
         }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // Slices of more than 1024 columns: a warp per slice row passes over it three times (four for the layer norm), and finds it
@@ -452,14 +585,14 @@ __device__ __forceinline__ void gate_and_slope(float g, float& open, float& slop
 // end, as do the weights; kBackwardAhead rows are copied to shared memory ahead.
 constexpr int kBackwardAhead = 3;
 // bytes of a CTA's chunks of one row each: dh, du, then h, y, gate
-template <typename T>
+template <typename T, bool VEC>
 struct BackwardRing {
-    static constexpr int kF = 256 * 16, kT = 256 * 4 * (int)sizeof(T), kStage = 2 * kF + 3 * kT;
+    static constexpr int kSlot = VEC ? 4 * (int)sizeof(T) : 16, kF = 256 * 16, kT = 256 * kSlot, kStage = 2 * kF + 3 * kT;
 };
 template <typename T, bool VEC, int L>
 __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a, const T* y, const T* gate, const T* h, const float* dh,
                                                                const float* du, float* dx, float* dy, float* dgate) {
-    using R = BackwardRing<T>;
+    using R = BackwardRing<T, VEC>;
     constexpr int E = 4, S = kBackwardAhead;
     extern __shared__ __align__(16) unsigned char ring[];
     const Place<L> place(a);
@@ -469,35 +602,32 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
     const bool ragged = a.w % E != 0, full = a.w == E * L;
     const int all = a.p * a.w;
     const int64_t rounds = (a.n + a.lanes_rows - 1) / a.lanes_rows;
-    const uint32_t ring_u = VEC ? (uint32_t)__cvta_generic_to_shared(ring) : 0;
-    const int at_f = threadIdx.x * 16, at_t = 2 * R::kF + threadIdx.x * 4 * (int)sizeof(T);
-    Chunk<T, E> qy, qg, qh;
-    Chunk<float, E> qd, qu;
+    const uint32_t ring_u = (uint32_t)__cvta_generic_to_shared(ring);
+    const int owner = VEC ? threadIdx.x : threadIdx.x & ~(L - 1);   // whose slots: the thread's, or its group's
+    const int at_f = owner * 16, at_t = 2 * R::kF + owner * R::kSlot;
     int next_in = 0, next_out = 0;   // ring stages
+    auto row_of = [&](int64_t r) { return min(place.row + r * a.lanes_rows, a.n - 1); };   // a row past the end is worked on, and not kept
     auto request = [&](int64_t r) {
-        const int64_t at = min(place.row + r * a.lanes_rows, a.n - 1);   // a row past the end is worked on, and not kept
-        if (VEC) {
-            const uint32_t to = ring_u + next_in * R::kStage;
-            next_in = next_in + 1 == S ? 0 : next_in + 1;
-            const int c = c0 + (cols.inside(0, 0) ? cols.at(0) : 0);
-            if (r < rounds) {
-                if (du) copy_chunk<E>(to + at_t, h + at * a.h_ld + c);
-                if (du) copy_chunk<E>(to + R::kF + at_f, du + at * a.du_ld + c);
-                if (y) copy_chunk<E>(to + at_t + R::kT, y + at * a.y_ld + c);
-                if (dh) copy_chunk<E>(to + at_f, dh + at * a.dh_ld + c);
-                if (gate) copy_chunk<E>(to + at_t + 2 * R::kT, gate + at * a.gate_ld + c);
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        } else {
-            if (du) cols.load(qh, h + at * a.h_ld + c0, 0);
-            if (du) cols.load(qu, du + at * a.du_ld + c0, 0);
-            if (y) cols.load(qy, y + at * a.y_ld + c0, 0);
-            if (dh) cols.load(qd, dh + at * a.dh_ld + c0, 0);
-            if (gate) cols.load(qg, gate + at * a.gate_ld + c0, 0);
+        const int64_t at = row_of(r);
+        const uint32_t to = ring_u + next_in * R::kStage;
+        next_in = next_in + 1 == S ? 0 : next_in + 1;
+        if (r < rounds) {
+            auto copy = [&](uint32_t slot, const auto* row) {
+                if constexpr (VEC)
+                    copy_chunk<E>(slot, row + (cols.inside(0, 0) ? cols.at(0) : 0));
+                else
+                    copy_words<4>(slot, row, a.w, place.lane, L);
+            };
+            if (du) copy(to + at_t, h + at * a.h_ld + c0);
+            if (du) copy(to + R::kF + at_f, du + at * a.du_ld + c0);
+            if (y) copy(to + at_t + R::kT, y + at * a.y_ld + c0);
+            if (dh) copy(to + at_f, dh + at * a.dh_ld + c0);
+            if (gate) copy(to + at_t + 2 * R::kT, gate + at * a.gate_ld + c0);
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
-    for (int r = 0; r < (VEC ? S - 1 : 1); ++r) request(r);
+    for (int r = 0; r < S - 1; ++r) request(r);
     float wp[E], bp[E], wq[E], in[E];
     cols.vector(a.w_post ? a.w_post + c0 : nullptr, 0, 1.f, wp);
     cols.vector(a.b_post ? a.b_post + c0 : nullptr, 0, 0.f, bp);
@@ -514,23 +644,25 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
         float hv[E], uv[E], yv[E], d[E], gv[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) hv[j] = uv[j] = yv[j] = d[j] = gv[j] = 0.f;
-        if (VEC) {
-            request(r + S - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
-            const unsigned char* from = ring + next_out * R::kStage;
-            next_out = next_out + 1 == S ? 0 : next_out + 1;
+        if (!VEC) __syncwarp();
+        request(r + S - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+        const unsigned char* from = ring + next_out * R::kStage;
+        next_out = next_out + 1 == S ? 0 : next_out + 1;
+        if constexpr (VEC) {
             if (du) staged_get<T>(from + at_t, hv), staged_get<float>(from + R::kF + at_f, uv);
             if (y) staged_get<T>(from + at_t + R::kT, yv);
             if (dh) staged_get<float>(from + at_f, d);
             if (gate) staged_get<T>(from + at_t + 2 * R::kT, gv);
         } else {
-            if (du) qh.get(hv), qu.get(uv);
-            if (y) qy.get(yv);
-            if (dh) qd.get(d);
-            if (gate) qg.get(gv);
+            __syncwarp();
+            const int64_t at = row_of(r);
+            if (du) words_get<T>(from + at_t, odd_of(h + at * a.h_ld + c0), cols, 0, hv), words_get<float>(from + R::kF + at_f, 0, cols, 0, uv);
+            if (y) words_get<T>(from + at_t + R::kT, odd_of(y + at * a.y_ld + c0), cols, 0, yv);
+            if (dh) words_get<float>(from + at_f, 0, cols, 0, d);
+            if (gate) words_get<T>(from + at_t + 2 * R::kT, odd_of(gate + at * a.gate_ld + c0), cols, 0, gv);
         }
         cols.keep(hv, 0, full), cols.keep(uv, 0, full), cols.keep(yv, 0, full), cols.keep(d, 0, full), cols.keep(gv, 0, full);
-        if (!VEC && r + 1 < rounds) request(r + 1);
         if (a.layer) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
@@ -619,9 +751,9 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
     }
 }
 
-// Slices of 129 to 1024 columns that allow accesses of four elements: a warp per slice row, whose five inputs are copied to
-// shared memory one row ahead.  Every lane copies, and reads back, its own columns only (4 lane + 128 i), so no barrier
-// stands in the loop.  The row is read from shared memory in each of the passes over it, which leaves the registers to the
+// Slices of 129 to 1024 columns: a warp per slice row, whose five inputs are copied to shared memory one row ahead.  With
+// accesses of four elements every lane copies, and reads back, its own columns only (4 lane + 128 i).  No barrier of the
+// CTA stands in the loop.  The row is read from shared memory in each of the passes over it, which leaves the registers to the
 // columns' sums (BIAS: those of the biases too).  A CTA works on one slice: its warps' sums are added in order at the end.
 // What is not given is left in shared memory as values that change nothing (zeros; an infinite gate is an open one).
 // Shared memory (two rows per warp) and registers (the sums) bound the warps per SM, so what counts here is instructions
@@ -631,12 +763,12 @@ constexpr int staged_warps() { return NV <= 5 ? 12 : 8; }
 // bytes of one row of a warp: dh, du in fp32 and y, gate, h in T, 32 lanes x NV chunks each
 template <typename T, int NV>
 struct Staged {
-    static constexpr int kF = NV * 32 * 16, kT = NV * 32 * 4 * (int)sizeof(T);
+    static constexpr int kF = NV * 32 * 16, kT = NV * 32 * 4 * (int)sizeof(T) + 16;   // (a bf16 row may start in a word)
     static constexpr int kDh = 0, kDu = kF, kY = 2 * kF, kGate = kY + kT, kH = kGate + kT, kRow = kH + kT;
     static constexpr int kVectors = 3 * NV * 32 * 16;                             // w_post, b_post, w_pre
     static constexpr int smem(int warps) { return kVectors + warps * 2 * kRow; }
 };
-template <typename T, int NV, bool BIAS>
+template <typename T, bool VEC, int NV, bool BIAS>
 __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_kernel(const NormArgs a, const T* y, const T* gate, const T* h,
                                                                                        const float* dh, const float* du, float* dx,
                                                                                        float* dy, float* dgate) {
@@ -648,7 +780,7 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
     const int slice = blockIdx.x % a.p;
     const int64_t first = (int64_t)(blockIdx.x / a.p) * warps + warp;             // then every lanes_rows-th row
     const int c0 = slice * a.w;
-    const Columns<true, E> cols(lane, 32, a.w, false);
+    const Columns<VEC, E> cols(lane, 32, a.w, false);
     const bool ragged = a.w % E != 0;
     const float inv_w = 1.f / (float)a.w;
     unsigned char* mine = stage + S::kVectors + warp * 2 * S::kRow;
@@ -678,16 +810,21 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
     auto request = [&](int64_t row, int buf) {
         if (row < a.n) {
             const uint32_t to = mine_u + buf * S::kRow;
+            auto copy = [&](uint32_t at, const auto* from) {
+                using F = typename std::remove_cv<typename std::remove_reference<decltype(*from)>::type>::type;
+                if constexpr (VEC) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (cols.inside(i, 0)) {
-                    const int o = i * 32 + lane, c = c0 + cols.at(i);
-                    if (du) copy_chunk<E>(to + S::kH + o * E * (int)sizeof(T), h + row * a.h_ld + c);
-                    if (y) copy_chunk<E>(to + S::kY + o * E * (int)sizeof(T), y + row * a.y_ld + c);
-                    if (du) copy_chunk<E>(to + S::kDu + o * 16, du + row * a.du_ld + c);
-                    if (dh) copy_chunk<E>(to + S::kDh + o * 16, dh + row * a.dh_ld + c);
-                    if (gate) copy_chunk<E>(to + S::kGate + o * E * (int)sizeof(T), gate + row * a.gate_ld + c);
+                    for (int i = 0; i < NV; ++i)
+                        if (cols.inside(i, 0)) copy_chunk<E>(at + (i * 32 + lane) * E * (int)sizeof(F), from + cols.at(i));
+                } else {
+                    copy_words<NV * (int)sizeof(F) + 1>(at, from, a.w, lane, 32);
                 }
+            };
+            if (du) copy(to + S::kH, h + row * a.h_ld + c0);
+            if (du) copy(to + S::kDu, du + row * a.du_ld + c0);
+            if (y) copy(to + S::kY, y + row * a.y_ld + c0);
+            if (dh) copy(to + S::kDh, dh + row * a.dh_ld + c0);
+            if (gate) copy(to + S::kGate, gate + row * a.gate_ld + c0);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -705,17 +842,32 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
     request(first, 0);
     int buf = 0;
     for (int64_t row = first; row < a.n; row += a.lanes_rows, buf ^= 1) {
+        if (!VEC) __syncwarp();
         request(row + a.lanes_rows, buf ^ 1);
         asm volatile("cp.async.wait_group 1;" ::: "memory");
-        const unsigned char* own_f = mine + buf * S::kRow + lane * 16;
-        const unsigned char* own_t = mine + buf * S::kRow + lane * E * (int)sizeof(T);
+        if (!VEC) __syncwarp();
+        const unsigned char* at = mine + buf * S::kRow;
+        const int odd_h = du ? odd_of(h + row * a.h_ld + c0) : 0, odd_y = y ? odd_of(y + row * a.y_ld + c0) : 0;
+        const int odd_gate = gate ? odd_of(gate + row * a.gate_ld + c0) : 0;
+        auto get_t = [&](int tensor, int odd, int i, float(&f)[E]) {
+            if constexpr (VEC)
+                staged_get<T>(at + tensor + i * HT + lane * E * (int)sizeof(T), f);
+            else
+                words_get<T>(at + tensor, odd, cols, i, f);
+        };
+        auto get_f = [&](int tensor, int i, float(&f)[E]) {
+            if constexpr (VEC)
+                staged_get<float>(at + tensor + i * HF + lane * 16, f);
+            else
+                words_get<float>(at + tensor, 0, cols, i, f);
+        };
         float mh = 0.f, my = 0.f;
         if (a.layer) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 float hv[E], yv[E];
-                staged_get<T>(own_t + S::kH + i * HT, hv), staged_get<T>(own_t + S::kY + i * HT, yv);
+                get_t(S::kH, odd_h, i, hv), get_t(S::kY, odd_y, i, yv);
                 trim(hv, i), trim(yv, i);
 #pragma unroll
                 for (int j = 0; j < E; ++j) m[0] += hv[j], m[1] += yv[j];
@@ -727,9 +879,9 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float hv[E], uv[E], yv[E], wq[E];
-            staged_get<T>(own_t + S::kH + i * HT, hv);
-            staged_get<float>(own_f + S::kDu + i * HF, uv);
-            staged_get<T>(own_t + S::kY + i * HT, yv);
+            get_t(S::kH, odd_h, i, hv);
+            get_f(S::kDu, i, uv);
+            get_t(S::kY, odd_y, i, yv);
             staged_get<float>(vectors + 2 * S::kF + i * HF, wq);
 #pragma unroll
             for (int j = 0; j < E; ++j) hv[j] -= mh, yv[j] -= my;
@@ -750,11 +902,11 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float hv[E], uv[E], yv[E], d[E], gv[E], wp[E], bp[E], wq[E];
-            staged_get<T>(own_t + S::kH + i * HT, hv);
-            staged_get<float>(own_f + S::kDu + i * HF, uv);
-            staged_get<T>(own_t + S::kY + i * HT, yv);
-            staged_get<float>(own_f + S::kDh + i * HF, d);
-            staged_get<T>(own_t + S::kGate + i * HT, gv);
+            get_t(S::kH, odd_h, i, hv);
+            get_f(S::kDu, i, uv);
+            get_t(S::kY, odd_y, i, yv);
+            get_f(S::kDh, i, d);
+            get_t(S::kGate, odd_gate, i, gv);
             staged_get<float>(vectors + i * HF, wp);
             staged_get<float>(vectors + S::kF + i * HF, bp);
             staged_get<float>(vectors + 2 * S::kF + i * HF, wq);
@@ -784,7 +936,7 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float yv[E];
-            staged_get<T>(own_t + S::kY + i * HT, yv);
+            get_t(S::kY, odd_y, i, yv);
 #pragma unroll
             for (int j = 0; j < E; ++j) yv[j] = ry * (t[i][j] - mt - (yv[j] - my) * ry * mty);
             cols.store(dy + row * a.dy_ld + c0, i, yv, ragged);
@@ -799,7 +951,8 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            *reinterpret_cast<float4*>(sums + warp * S::kF + i * HF + lane * 16) = make_float4(acc[k][i][0], acc[k][i][1], acc[k][i][2], acc[k][i][3]);
+#pragma unroll
+            for (int j = 0; j < E; ++j) reinterpret_cast<float*>(sums + warp * S::kF)[cols.at(i) + j * cols.step] = acc[k][i][j];
         __syncthreads();
         const int which = BIAS ? (k == 0 ? 0 : k == 1 ? 2 : k == 2 ? 1 : 3) : 2 * k;   // order of the partial rows
         float* out = a.partial + ((int64_t)(blockIdx.x / a.p) * 4 + which) * all + c0;
@@ -811,7 +964,7 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
     }
 }
 
-// All other slices (wider ones, or wide ones that allow no accesses of four elements).  First a warp per slice row takes
+// Wider slices.  First a warp per slice row takes
 // the sums over the row, reading it twice (the second time from L2); then every thread applies them to columns of its own
 // for many rows, whose sums it keeps in registers.
 struct RowStats {
@@ -1020,32 +1173,60 @@ NormArgs make_args(const slicegcn_residual_norm_desc* d) {
 constexpr int kSMs = 148;
 constexpr int kMaxWarpWidth = 1024;   // columns of a slice that one warp holds (forward: in registers, gradient: in shared memory)
 
-// Forward, up to 1024 columns.  E: columns per chunk; lanes per slice row and chunks per lane.
+// Forward, up to 1024 columns.  By lanes (one chunk of E columns each), or staged with a warp per slice row.
 struct ForwardPlan {
-    int lanes, chunks;
+    int lanes;                 // 0: staged
+    int chunks, warps, smem;   // staged: chunks per lane, warps per CTA
     int64_t ctas, lanes_rows;
 };
+constexpr int kStagedSmem = 227 * 1024;
 int64_t rows_at_a_time(int64_t ctas, int groups, int p) { return ctas * groups / p; }
 int lanes_for(int need) {
     int lanes = 1;
     while (lanes < 32 && lanes < need) lanes *= 2;
     return lanes;
 }
+int staged_chunks(int w) { return w <= 256 ? 2 : w <= 512 ? 4 : w <= 640 ? 5 : 8; }
+template <template <typename, int> class S>
+int smem_for(int dtype, int chunks, int warps) {
+    const bool bf = dtype == SLICEGCN_BF16;
+    switch (chunks) {
+        case 2: return bf ? S<__nv_bfloat16, 2>::smem(warps) : S<float, 2>::smem(warps);
+        case 4: return bf ? S<__nv_bfloat16, 4>::smem(warps) : S<float, 4>::smem(warps);
+        case 5: return bf ? S<__nv_bfloat16, 5>::smem(warps) : S<float, 5>::smem(warps);
+        default: return bf ? S<__nv_bfloat16, 8>::smem(warps) : S<float, 8>::smem(warps);
+    }
+}
+// Warps per CTA: as many as fit, but no more than leave every SM a CTA when there are few rows.  Row CTAs per slice.
+template <template <typename, int> class S>
+void staged_shape(const slicegcn_residual_norm_desc* d, int chunks, int most, int per_sm, int* warps, int* smem, int64_t* row_ctas) {
+    *warps = most;
+    while (smem_for<S>(d->dtype, chunks, *warps) > kStagedSmem / per_sm - 1024) --*warps;
+    const int64_t share = (d->n * d->num_slices + kSMs * per_sm - 1) / (kSMs * per_sm);
+    *warps = (int)std::max<int64_t>(1, std::min<int64_t>(*warps, share));
+    *smem = smem_for<S>(d->dtype, chunks, *warps);
+    *row_ctas = std::max<int64_t>(1, std::min<int64_t>((d->n + *warps - 1) / *warps, kSMs * per_sm / d->num_slices));
+}
 ForwardPlan forward_plan(const slicegcn_residual_norm_desc* d, int E) {
-    ForwardPlan p;
+    ForwardPlan p{};
     const int need = (d->h_s + E - 1) / E;
-    p.lanes = lanes_for(need);
-    p.chunks = 1;
-    while (p.chunks * p.lanes < need) p.chunks *= 2;
-    const int groups = 256 / p.lanes;
     const int64_t items = d->n * d->num_slices;
-    p.ctas = std::max<int64_t>(std::min<int64_t>((items + groups - 1) / groups, 8 * kSMs), (d->num_slices + groups - 1) / groups);
-    p.lanes_rows = rows_at_a_time(p.ctas, groups, d->num_slices);
+    if (need <= 32) {
+        p.lanes = lanes_for(need);
+        const int groups = 256 / p.lanes;
+        p.ctas = std::max<int64_t>(std::min<int64_t>((items + groups - 1) / groups, 8 * kSMs), (d->num_slices + groups - 1) / groups);
+        p.lanes_rows = rows_at_a_time(p.ctas, groups, d->num_slices);
+    } else {
+        p.chunks = staged_chunks(d->h_s);
+        int64_t row_ctas;
+        staged_shape<StagedForward>(d, p.chunks, kForwardWarps, 1, &p.warps, &p.smem, &row_ctas);
+        p.ctas = row_ctas * d->num_slices;
+        p.lanes_rows = row_ctas * p.warps;
+    }
     return p;
 }
 
-// Gradient.  The workspace holds the partial rows of the columns' sums and, for the third form, the rows' statistics.  Its
-// size must not depend on the matrices' alignment, which decides between the second and the third.
+// Gradient.  The workspace holds the partial rows of the columns' sums and, for the third form, the rows' statistics.
 enum { kByLanes, kStaged, kTwoPasses };
 struct BackwardPlan {
     int form;
@@ -1056,19 +1237,7 @@ struct BackwardPlan {
     int64_t partial_rows, stats_bytes;
 };
 constexpr int kApplyRows = 4 * kSMs;   // kTwoPasses: partial rows at most
-template <typename T, int NV>
-int staged_smem(int warps) { return Staged<T, NV>::smem(warps); }
-int staged_smem_for(int dtype, int chunks, int warps) {
-    const bool bf = dtype == SLICEGCN_BF16;
-    switch (chunks) {
-        case 2: return bf ? staged_smem<__nv_bfloat16, 2>(warps) : staged_smem<float, 2>(warps);
-        case 4: return bf ? staged_smem<__nv_bfloat16, 4>(warps) : staged_smem<float, 4>(warps);
-        case 5: return bf ? staged_smem<__nv_bfloat16, 5>(warps) : staged_smem<float, 5>(warps);
-        default: return bf ? staged_smem<__nv_bfloat16, 8>(warps) : staged_smem<float, 8>(warps);
-    }
-}
-constexpr int kStagedSmem = 227 * 1024;
-BackwardPlan backward_plan(const slicegcn_residual_norm_desc* d, bool vec) {
+BackwardPlan backward_plan(const slicegcn_residual_norm_desc* d) {
     BackwardPlan p{};
     const int64_t items = d->n * d->num_slices;
     if (d->h_s <= 128) {
@@ -1079,15 +1248,11 @@ BackwardPlan backward_plan(const slicegcn_residual_norm_desc* d, bool vec) {
         p.lanes_rows = rows_at_a_time(p.ctas, groups, d->num_slices);
         p.whole_rows = groups % d->num_slices == 0;
         p.partial_rows = p.whole_rows ? p.ctas : p.lanes_rows;
-    } else if (d->h_s <= kMaxWarpWidth && vec) {
+    } else if (d->h_s <= kMaxWarpWidth) {
         p.form = kStaged;
-        p.chunks = d->h_s <= 256 ? 2 : d->h_s <= 512 ? 4 : d->h_s <= 640 ? 5 : 8;
-        p.warps = p.chunks <= 5 ? staged_warps<5>() : staged_warps<8>();
-        while (staged_smem_for(d->dtype, p.chunks, p.warps) > kStagedSmem) --p.warps;
-        p.smem = staged_smem_for(d->dtype, p.chunks, p.warps);
-        const int per_sm = std::max(1, std::min(2, kStagedSmem / (p.smem + 1024)));
-        const int64_t row_ctas = std::min<int64_t>((d->n + p.warps - 1) / p.warps, std::max<int64_t>(1, per_sm * kSMs / d->num_slices));
-        p.partial_rows = std::max<int64_t>(1, row_ctas);
+        p.chunks = staged_chunks(d->h_s);
+        const int most = p.chunks <= 5 ? staged_warps<5>() : staged_warps<8>();
+        staged_shape<Staged>(d, p.chunks, most, 1, &p.warps, &p.smem, &p.partial_rows);
         p.ctas = p.partial_rows * d->num_slices;
         p.lanes_rows = p.partial_rows * p.warps;
     } else {
@@ -1108,22 +1273,28 @@ struct ForwardCall {
     const T *x, *y, *gate;
     T *h, *u;
     cudaStream_t st;
-    template <bool VEC, int E, int L, int NV>
-    void go() const {
-        constexpr int smem = VEC && NV == 1 ? kForwardAhead * 3 * 256 * E * (int)sizeof(T) : 0;   // 48 KB at most
-        norm_forward_kernel<T, VEC, E, L, NV><<<(unsigned)pl.ctas, 256, smem, st>>>(a, x, y, gate, h, u);
+    template <bool VEC, int E, int L>
+    slicegcn_status_t go() const {
+        constexpr int smem = kForwardAhead * 3 * 256 * kForwardSlot<T, VEC, E>;   // 48 KB at most
+        norm_forward_kernel<T, VEC, E, L><<<(unsigned)pl.ctas, 256, smem, st>>>(a, x, y, gate, h, u);
+        return SLICEGCN_OK;
+    }
+    template <bool VEC, int NV>
+    slicegcn_status_t staged() const {
+        SGCN_CUDA(cudaFuncSetAttribute(norm_forward_staged_kernel<T, VEC, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem));
+        norm_forward_staged_kernel<T, VEC, NV><<<(unsigned)pl.ctas, pl.warps * 32, pl.smem, st>>>(a, x, y, gate, h, u);
+        return SLICEGCN_OK;
     }
     template <bool VEC, int E>
-    void pick() const {
+    slicegcn_status_t pick() const {
         switch (pl.lanes) {
-            case 1: go<VEC, E, 1, 1>(); break;
-            case 2: go<VEC, E, 2, 1>(); break;
-            case 4: go<VEC, E, 4, 1>(); break;
-            case 8: go<VEC, E, 8, 1>(); break;
-            case 16: go<VEC, E, 16, 1>(); break;
-            default:
-                pl.chunks == 1 ? go<VEC, E, 32, 1>() : pl.chunks == 2 ? go<VEC, E, 32, 2>() : pl.chunks * E == 16 ? go<VEC, E, 32, 16 / E>()
-                                                                                                           : go<VEC, E, 32, 32 / E>();
+            case 0: return pl.chunks == 2 ? staged<VEC, 2>() : pl.chunks == 4 ? staged<VEC, 4>() : pl.chunks == 5 ? staged<VEC, 5>() : staged<VEC, 8>();
+            case 1: return go<VEC, E, 1>();
+            case 2: return go<VEC, E, 2>();
+            case 4: return go<VEC, E, 4>();
+            case 8: return go<VEC, E, 8>();
+            case 16: return go<VEC, E, 16>();
+            default: return go<VEC, E, 32>();
         }
     }
     template <bool VEC>
@@ -1143,20 +1314,20 @@ struct BackwardCall {
     cudaStream_t st;
     template <bool VEC, int L>
     slicegcn_status_t go() const {
-        constexpr int smem = VEC ? kBackwardAhead * BackwardRing<T>::kStage : 0;
+        constexpr int smem = kBackwardAhead * BackwardRing<T, VEC>::kStage;
         if (smem > 48 * 1024) SGCN_CUDA(cudaFuncSetAttribute(norm_backward_kernel<T, VEC, L>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         norm_backward_kernel<T, VEC, L><<<(unsigned)pl.ctas, 256, smem, st>>>(a, y, gate, h, dh, du, dx, dy, dgate);
         return SLICEGCN_OK;
     }
-    template <int NV, bool BIAS>
+    template <bool VEC, int NV, bool BIAS>
     slicegcn_status_t staged() const {
-        SGCN_CUDA(cudaFuncSetAttribute(norm_backward_staged_kernel<T, NV, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem));
-        norm_backward_staged_kernel<T, NV, BIAS><<<(unsigned)pl.ctas, pl.warps * 32, pl.smem, st>>>(a, y, gate, h, dh, du, dx, dy, dgate);
+        SGCN_CUDA(cudaFuncSetAttribute(norm_backward_staged_kernel<T, VEC, NV, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem));
+        norm_backward_staged_kernel<T, VEC, NV, BIAS><<<(unsigned)pl.ctas, pl.warps * 32, pl.smem, st>>>(a, y, gate, h, dh, du, dx, dy, dgate);
         return SLICEGCN_OK;
     }
-    template <bool BIAS>
+    template <bool VEC, bool BIAS>
     slicegcn_status_t staged_for() const {
-        return pl.chunks == 2 ? staged<2, BIAS>() : pl.chunks == 4 ? staged<4, BIAS>() : pl.chunks == 5 ? staged<5, BIAS>() : staged<8, BIAS>();
+        return pl.chunks == 2 ? staged<VEC, 2, BIAS>() : pl.chunks == 4 ? staged<VEC, 4, BIAS>() : pl.chunks == 5 ? staged<VEC, 5, BIAS>() : staged<VEC, 8, BIAS>();
     }
     template <bool VEC>
     slicegcn_status_t run(bool bias) const {
@@ -1170,7 +1341,7 @@ struct BackwardCall {
                 default: SGCN_TRY((go<VEC, 32>())); break;
             }
         } else if (pl.form == kStaged) {
-            SGCN_TRY(bias ? staged_for<true>() : staged_for<false>());
+            SGCN_TRY((bias ? staged_for<VEC, true>() : staged_for<VEC, false>()));
         } else {
             norm_stats_kernel<T, VEC><<<(unsigned)((a.n * a.p + 7) / 8), 256, 0, st>>>(a, y, gate, h, dh, du, stats);
             SGCN_LAUNCH_CHECK();
@@ -1231,14 +1402,14 @@ slicegcn_status_t slicegcn_residual_norm_forward(const slicegcn_residual_norm_de
         if (wide)
             vec4 ? call.template wide<true>() : call.template wide<false>();
         else
-            vec8 ? call.template pick<true, 8>() : vec4 ? call.template pick<true, 4>() : call.template pick<false, 4>();
+            SGCN_TRY((vec8 ? call.template pick<true, 8>() : vec4 ? call.template pick<true, 4>() : call.template pick<false, 4>()));
     } else {
         using T = float;
         const ForwardCall<T> call{pl, a, (const T*)x, (const T*)y, (const T*)gate, (T*)h, (T*)u, st};
         if (wide)
             vec4 ? call.template wide<true>() : call.template wide<false>();
         else
-            vec4 ? call.template pick<true, 4>() : call.template pick<false, 4>();
+            SGCN_TRY((vec4 ? call.template pick<true, 4>() : call.template pick<false, 4>()));
     }
     SGCN_LAUNCH_CHECK();
     count_launch();
@@ -1248,7 +1419,7 @@ slicegcn_status_t slicegcn_residual_norm_forward(const slicegcn_residual_norm_de
 slicegcn_status_t slicegcn_residual_norm_workspace_bytes(const slicegcn_residual_norm_desc* d, int64_t* bytes) {
     SGCN_TRY(check_desc(d, "residual_norm_workspace_bytes"));
     if (!bytes) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "residual_norm_workspace_bytes: NULL argument");
-    *bytes = std::max(backward_bytes(d, backward_plan(d, true)), backward_bytes(d, backward_plan(d, false)));
+    *bytes = backward_bytes(d, backward_plan(d));
     return SLICEGCN_OK;
 }
 
@@ -1282,9 +1453,9 @@ slicegcn_status_t slicegcn_residual_norm_backward(const slicegcn_residual_norm_d
     const bool sums = dw_post || db_post || dw_pre || db_pre;
     const bool fours = VecCheck(d, 4).with(y, d->y_ld, esz).with(gate, d->gate_ld, esz).with(h, d->h_ld, esz).with(dh, d->dh_ld, 4)
                          .with(du, d->du_ld, 4).with(dx, d->dx_ld, 4).with(dy, d->dy_ld, 4).with(dgate, d->dgate_ld, 4).ok;
-    const BackwardPlan pl = backward_plan(d, fours);
+    const BackwardPlan pl = backward_plan(d);
     const int cols = d->num_slices * d->h_s;
-    const int64_t need = std::max(backward_bytes(d, backward_plan(d, true)), backward_bytes(d, backward_plan(d, false)));
+    const int64_t need = backward_bytes(d, pl);
     if ((sums || pl.form == kTwoPasses) && (!workspace || workspace_bytes < need))
         SGCN_FAIL(SLICEGCN_ERR_ALLOC, "%s: workspace too small (%lld < %lld bytes)", who, (long long)workspace_bytes, (long long)need);
     if ((uintptr_t)workspace % 16) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: the workspace is not aligned to 16 bytes", who);
