@@ -247,17 +247,8 @@ slicegcn_status_t run_two(const ClipTable<N>& t, double max_norm, float* norm_ou
     const int ctas = (int)std::min<int64_t>(std::max<int64_t>(t.pieces, 1), kMaxCtas);
     clip_norm_kernel<N><<<ctas, kThreads, 0, st>>>(t, partial);
     SGCN_LAUNCH_CHECK();
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(kThreads);
-    cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    SGCN_CUDA(cudaLaunchKernelEx(&cfg, clip_scale_kernel<N>, t, (const double*)partial, ctas, max_norm, norm_out));
-    count_launch(2);
+    count_launch();
+    SGCN_TRY(launch_after(clip_scale_kernel<N>, dim3(ctas), kThreads, 0, st, t, (const double*)partial, ctas, max_norm, norm_out));
     return SLICEGCN_OK;
 }
 

@@ -46,6 +46,25 @@ void count_launch(int n = 1);
 long long launches();
 void reset_launches();
 
+// A launch that may start while the one before it on the stream ends: its kernel waits for the data on the device
+// (cudaGridDependencySynchronize) before it touches any.
+template <typename... P, typename... Q>
+slicegcn_status_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const Q&... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    SGCN_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+    count_launch();
+    return SLICEGCN_OK;
+}
+
 // ---- CSR view used by the SpMM ----------------------------------------------------------------
 // Rows with more than kLongRow stored entries are split into segments of kSegment entries; each
 // segment is reduced by one warp into a partial row, and the partial rows of a long row are summed

@@ -645,24 +645,6 @@ __global__ void __launch_bounds__(256) embed_finish_kernel(const SumArgs a) {
     }
 }
 
-// A launch that may start while the one before it ends: its kernel waits on the device for the data.
-template <typename... P, typename... Q>
-slicegcn_status_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const Q&... args) {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    SGCN_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
-    count_launch();
-    return SLICEGCN_OK;
-}
-
 slicegcn_status_t check_desc(const slicegcn_embed_desc* d, const char* who) {
     if (!d) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: NULL description", who);
     if (d->n < 0 || d->vocab < 1 || d->width < 1) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: bad sizes", who);

@@ -464,19 +464,35 @@ __global__ void __launch_bounds__(kForwardWarps * 32) norm_forward_staged_kernel
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// Slices of more than 1024 columns: a warp per slice row passes over it three times (four for the layer norm), and finds it
-// in L2 from the second time on.
+// sums over a CTA of kWideThreads, the same order every time; two buffers in turn, so that one barrier per sum is enough
+constexpr int kWideThreads = 256;
+template <int K>
+__device__ __forceinline__ void cta_sum(float (&v)[K], float (*buf)[kWideThreads / 32][K]) {
+    group_sum<32>(v);
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) (*buf)[threadIdx.x >> 5][k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        v[k] = 0.f;
+#pragma unroll
+        for (int o = 0; o < kWideThreads / 32; ++o) v[k] += (*buf)[o][k];
+    }
+}
+
+// Slices of more than 1024 columns: a CTA per slice row passes over it three times (five for the layer norm), and finds it
+// in the caches from the second time on.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) norm_forward_wide_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
+__global__ void __launch_bounds__(kWideThreads) norm_forward_wide_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
     constexpr int E = 4;
-    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (item >= a.n * a.p) return;
-    const int64_t row = item / a.p;
+    __shared__ float sums[4][kWideThreads / 32][1];   // one for each sum
+    const int64_t item = blockIdx.x, row = item / a.p;
     const int c0 = (int)(item - row * a.p) * a.w;
-    const Columns<VEC, E> cols(threadIdx.x & 31, 32, a.w, false);
+    const Columns<VEC, E> cols(threadIdx.x, kWideThreads, a.w, false);
     const bool ragged = a.w % E != 0;
     const float inv_w = 1.f / (float)a.w;
-    const int chunks = (a.w + 127) / 128;
+    const int chunks = (a.w + 4 * kWideThreads - 1) / (4 * kWideThreads);
     auto get = [&](const T* from, int i, float(&f)[E]) {
         Chunk<T, E> q;
         cols.load(q, from, i);
@@ -494,7 +510,7 @@ __global__ void __launch_bounds__(256) norm_forward_wide_kernel(const NormArgs a
 #pragma unroll
                 for (int j = 0; j < E; ++j) sum[0] += f[j];
             }
-            group_sum<32>(sum);
+            cta_sum(sum, sums + 0);
             my = sum[0] * inv_w;
         }
         sum[0] = 0.f;
@@ -508,7 +524,7 @@ __global__ void __launch_bounds__(256) norm_forward_wide_kernel(const NormArgs a
                 sum[0] = fmaf(t, t, sum[0]);
             }
         }
-        group_sum<32>(sum);
+        cta_sum(sum, sums + 1);
         ry = rsqrtf(fmaf(sum[0], inv_w, a.eps));
     }
     auto step = [&](int i, float(&v)[E]) {   // unrounded h, zero past the slice
@@ -539,7 +555,7 @@ __global__ void __launch_bounds__(256) norm_forward_wide_kernel(const NormArgs a
 #pragma unroll
                 for (int j = 0; j < E; ++j) sum[0] += v[j];
             }
-            group_sum<32>(sum);
+            cta_sum(sum, sums + 2);
             mh = sum[0] * inv_w;
         }
         sum[0] = 0.f;
@@ -553,7 +569,7 @@ __global__ void __launch_bounds__(256) norm_forward_wide_kernel(const NormArgs a
                 sum[0] = fmaf(t, t, sum[0]);
             }
         }
-        group_sum<32>(sum);
+        cta_sum(sum, sums + 3);
         rh = rsqrtf(fmaf(sum[0], inv_w, a.eps));
     }
 #pragma unroll 2
@@ -592,6 +608,7 @@ struct BackwardRing {
 template <typename T, bool VEC, int L>
 __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a, const T* y, const T* gate, const T* h, const float* dh,
                                                                const float* du, float* dx, float* dy, float* dgate) {
+    cudaTriggerProgrammaticLaunchCompletion();
     using R = BackwardRing<T, VEC>;
     constexpr int E = 4, S = kBackwardAhead;
     extern __shared__ __align__(16) unsigned char ring[];
@@ -772,6 +789,7 @@ template <typename T, bool VEC, int NV, bool BIAS>
 __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_kernel(const NormArgs a, const T* y, const T* gate, const T* h,
                                                                                        const float* dh, const float* du, float* dx,
                                                                                        float* dy, float* dgate) {
+    cudaTriggerProgrammaticLaunchCompletion();
     using S = Staged<T, NV>;
     constexpr int E = 4;
     constexpr int HF = 512, HT = 32 * E * (int)sizeof(T);   // bytes from one chunk of a lane to its next
@@ -964,23 +982,22 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
     }
 }
 
-// Wider slices.  First a warp per slice row takes
+// Wider slices.  First a CTA per slice row takes
 // the sums over the row, reading it twice (the second time from L2); then every thread applies them to columns of its own
 // for many rows, whose sums it keeps in registers.
 struct RowStats {
     float mh, rh, mg, mgh, my, ry, mt, mty;
 };
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) norm_stats_kernel(const NormArgs a, const T* y, const T* gate, const T* h, const float* dh,
+__global__ void __launch_bounds__(kWideThreads) norm_stats_kernel(const NormArgs a, const T* y, const T* gate, const T* h, const float* dh,
                                                          const float* du, RowStats* stats) {
     constexpr int E = 4;
-    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (item >= a.n * a.p) return;
-    const int64_t row = item / a.p;
-    const int c0 = (int)(item - row * a.p) * a.w, lane = threadIdx.x & 31;
-    const Columns<VEC, E> cols(lane, 32, a.w, false);
+    __shared__ float means[1][kWideThreads / 32][2], squares[1][kWideThreads / 32][4], products[1][kWideThreads / 32][2];
+    const int64_t item = blockIdx.x, row = item / a.p;
+    const int c0 = (int)(item - row * a.p) * a.w;
+    const Columns<VEC, E> cols(threadIdx.x, kWideThreads, a.w, false);
     const float inv_w = 1.f / (float)a.w;
-    const int chunks = (a.w + 127) / 128;
+    const int chunks = (a.w + 4 * kWideThreads - 1) / (4 * kWideThreads);
     auto get = [&](auto* from, int i, float(&f)[E]) {
         Chunk<typename std::remove_cv<typename std::remove_pointer<decltype(from)>::type>::type, E> q;
         cols.load(q, from, i);
@@ -1001,7 +1018,7 @@ __global__ void __launch_bounds__(256) norm_stats_kernel(const NormArgs a, const
                 for (int j = 0; j < E; ++j) m[1] += f[j];
             }
         }
-        group_sum<32>(m);
+        cta_sum(m, means);
         s.mh = m[0] * inv_w, s.my = m[1] * inv_w;
     }
     float q[4] = {0.f, 0.f, 0.f, 0.f};
@@ -1020,7 +1037,7 @@ __global__ void __launch_bounds__(256) norm_stats_kernel(const NormArgs a, const
             q[3] = fmaf(g, hc, q[3]);
         }
     }
-    group_sum<32>(q);
+    cta_sum(q, squares);
     s.rh = rsqrtf(fmaf(q[0], inv_w, a.eps)), s.ry = rsqrtf(fmaf(q[1], inv_w, a.eps));
     s.mg = a.layer ? q[2] * inv_w : 0.f, s.mgh = q[3] * inv_w * s.rh;
     if (y) {
@@ -1042,16 +1059,17 @@ __global__ void __launch_bounds__(256) norm_stats_kernel(const NormArgs a, const
                 z[1] = fmaf(t, yv[j] - s.my, z[1]);
             }
         }
-        group_sum<32>(z);
+        cta_sum(z, products);
         s.mt = a.layer ? z[0] * inv_w : 0.f, s.mty = z[1] * inv_w * s.ry;
     }
-    if (lane == 0) stats[item] = s;
+    if (threadIdx.x == 0) stats[item] = s;
 }
 
 // blockIdx.x: 128 columns of one slice per warp; blockIdx.y: every gridDim.y-th row
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) norm_apply_kernel(const NormArgs a, const T* y, const T* gate, const T* h, const float* dh,
                                                          const float* du, float* dx, float* dy, float* dgate, const RowStats* stats) {
+    cudaTriggerProgrammaticLaunchCompletion();
     constexpr int E = 4;
     const int per_slice = (a.w + 127) / 128;
     const int tile = blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -1119,6 +1137,7 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(int64_t rows, int cols,
     __shared__ float part[32][33];
     const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, k = blockIdx.y;
     float* out = k == 0 ? dw_post : k == 1 ? db_post : k == 2 ? dw_pre : db_pre;
+    cudaGridDependencySynchronize();
     if (!out) return;
     const int c = blockIdx.x * 32 + lane;
     float s = 0.f;
@@ -1299,7 +1318,7 @@ struct ForwardCall {
     }
     template <bool VEC>
     void wide() const {
-        norm_forward_wide_kernel<T, VEC><<<(unsigned)((a.n * a.p + 7) / 8), 256, 0, st>>>(a, x, y, gate, h, u);
+        norm_forward_wide_kernel<T, VEC><<<(unsigned)(a.n * a.p), kWideThreads, 0, st>>>(a, x, y, gate, h, u);
     }
 };
 
@@ -1343,7 +1362,7 @@ struct BackwardCall {
         } else if (pl.form == kStaged) {
             SGCN_TRY((bias ? staged_for<VEC, true>() : staged_for<VEC, false>()));
         } else {
-            norm_stats_kernel<T, VEC><<<(unsigned)((a.n * a.p + 7) / 8), 256, 0, st>>>(a, y, gate, h, dh, du, stats);
+            norm_stats_kernel<T, VEC><<<(unsigned)(a.n * a.p), kWideThreads, 0, st>>>(a, y, gate, h, dh, du, stats);
             SGCN_LAUNCH_CHECK();
             count_launch();
             const int tiles = (a.w + 127) / 128 * a.p;
@@ -1478,9 +1497,8 @@ slicegcn_status_t slicegcn_residual_norm_backward(const slicegcn_residual_norm_d
         }
     }
     if (sums) {
-        norm_join_kernel<<<dim3((cols + 31) / 32, 4), 1024, 0, st>>>(a.n > 0 ? pl.partial_rows : 0, cols, a.partial, dw_post, db_post, dw_pre, db_pre);
-        SGCN_LAUNCH_CHECK();
-        count_launch();
+        SGCN_TRY(launch_after(norm_join_kernel, dim3((cols + 31) / 32, 4), 1024, 0, st, a.n > 0 ? pl.partial_rows : (int64_t)0, cols,
+                              (const float*)a.partial, dw_post, db_post, dw_pre, db_pre));
     }
     return SLICEGCN_OK;
 }
