@@ -328,13 +328,13 @@ struct SumShared {
     float sums[U][2][4 * L];
     int4 unit_info[U];   // {head present, head ends here, tail's id or -1, unused}
 };
-// The sorted positions: in memory, or (small problems) in the CTA's own shared memory as 12 bits of position under the
+// The sorted positions: in memory, or (small problems) in the CTA's own shared memory as 13 bits of position under the
 // id's distance from the CTA's first one.
 struct PairsInMemory {
     const uint2* p;
     __device__ __forceinline__ uint2 operator()(int i) const { return p[i]; }
 };
-constexpr int kSmallBits = 12, kSmallN = 1 << kSmallBits;
+constexpr int kSmallBits = 13, kSmallN = 1 << kSmallBits;
 struct PairsInShared {
     const uint32_t* p;
     uint32_t first_id;
@@ -479,11 +479,11 @@ struct SmallShared {
     uint32_t before[kSmallN / kSumThreads][8];
     uint32_t present[kSmallRows / 32];
 };
-template <int L, bool VEC>
+// K: ids a thread looks at
+template <int L, bool VEC, int K>
 __global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs a, const int32_t* ids, int rows_per_cta, int32_t* status) {
     extern __shared__ __align__(16) unsigned char raw[];
     SmallShared<L>& sh = *reinterpret_cast<SmallShared<L>*>(raw);
-    constexpr int K = kSmallN / kSumThreads;
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t v0 = blockIdx.x * (uint32_t)rows_per_cta;
     const uint32_t rows = (uint32_t)min((int64_t)rows_per_cta, a.vocab - v0);
@@ -503,7 +503,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs 
         if (lane == 0) sh.before[k][w] = __popc(mine[k]);
     }
     __syncthreads();
-    if (w == 0) {   // K * 8 counts, four per lane, to exclusive sums
+    if (w == 0) {   // K * 8 counts to exclusive sums, an equal run of them per lane
         uint32_t* c = &sh.before[0][0];
         uint32_t v[K * 8 / 32], sum = 0;
 #pragma unroll
@@ -657,7 +657,11 @@ int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 
 // One launch while the picking (every CTA looks at all ids) and an id that holds all positions (one CTA sums them) are
 // cheaper than the sort's launches.
-bool is_small(const slicegcn_embed_desc* d) { return d->n > 0 && d->n <= kSmallN && d->vocab <= (int64_t)kSMs * kSmallRows; }
+// (4,096 ids: 15.5 us, or 36.9 us sorted by launches; with a table of 7 rows, whose CTAs sum many positions each, 33 against
+// 23 us.)
+bool is_small(const slicegcn_embed_desc* d) {
+    return d->n > 0 && d->n <= (d->vocab < 64 ? kSmallN / 8 : kSmallN) && d->vocab <= (int64_t)kSMs * kSmallRows;
+}
 
 // How the gradient is cut, and where its parts lie in the workspace.
 struct GradPlan {
@@ -717,26 +721,36 @@ slicegcn_status_t launch_sum(const SumArgs& a, int col_tiles, cudaStream_t st) {
     return SLICEGCN_OK;
 }
 
-template <int L, bool VEC>
+template <int L, bool VEC, int K>
 slicegcn_status_t launch_small(const SumArgs& a, const int32_t* ids, int32_t* status, int col_tiles, cudaStream_t st) {
-    const int rows = (int)((a.vocab + kSMs - 1) / kSMs);
+    // two CTAs per SM over the column tiles: every CTA looks at all ids
+    const int64_t ctas = std::min<int64_t>(kSMs, std::max(1, 2 * kSMs / col_tiles));
+    const int rows = (int)std::min<int64_t>((a.vocab + ctas - 1) / ctas, kSmallRows);
     constexpr int smem = (int)sizeof(SmallShared<L>);
-    SGCN_CUDA(cudaFuncSetAttribute(embed_small_kernel<L, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    embed_small_kernel<L, VEC><<<dim3((unsigned)((a.vocab + rows - 1) / rows), col_tiles), kSumThreads, smem, st>>>(a, ids, rows, status);
+    SGCN_CUDA(cudaFuncSetAttribute(embed_small_kernel<L, VEC, K>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    embed_small_kernel<L, VEC, K><<<dim3((unsigned)((a.vocab + rows - 1) / rows), col_tiles), kSumThreads, smem, st>>>(a, ids, rows, status);
     SGCN_LAUNCH_CHECK();
     count_launch();
     return SLICEGCN_OK;
 }
 
-template <bool VEC>
+template <bool VEC, int K>
 slicegcn_status_t launch_smalls(const SumArgs& a, const int32_t* ids, int32_t* status, int lanes, int col_tiles, cudaStream_t st) {
     switch (lanes) {
-        case 2: return launch_small<2, VEC>(a, ids, status, col_tiles, st);
-        case 4: return launch_small<4, VEC>(a, ids, status, col_tiles, st);
-        case 8: return launch_small<8, VEC>(a, ids, status, col_tiles, st);
-        case 16: return launch_small<16, VEC>(a, ids, status, col_tiles, st);
-        default: return launch_small<32, VEC>(a, ids, status, col_tiles, st);
+        case 2: return launch_small<2, VEC, K>(a, ids, status, col_tiles, st);
+        case 4: return launch_small<4, VEC, K>(a, ids, status, col_tiles, st);
+        case 8: return launch_small<8, VEC, K>(a, ids, status, col_tiles, st);
+        case 16: return launch_small<16, VEC, K>(a, ids, status, col_tiles, st);
+        default: return launch_small<32, VEC, K>(a, ids, status, col_tiles, st);
     }
+}
+
+// 4, 16 or 32 ids per thread (2,708 ids: 10.2 us with 16, 12.2 us with 32)
+template <bool VEC>
+slicegcn_status_t launch_small_for(const SumArgs& a, const int32_t* ids, int32_t* status, int lanes, int col_tiles, cudaStream_t st) {
+    if (a.n <= 4 * kSumThreads) return launch_smalls<VEC, 4>(a, ids, status, lanes, col_tiles, st);
+    if (a.n <= 16 * kSumThreads) return launch_smalls<VEC, 16>(a, ids, status, lanes, col_tiles, st);
+    return launch_smalls<VEC, 32>(a, ids, status, lanes, col_tiles, st);
 }
 
 template <bool VEC>
@@ -845,7 +859,7 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
     t.tail = reinterpret_cast<float*>(ws + p.tail);
     t.info = reinterpret_cast<int4*>(ws + p.info);
     const bool vec = d->width % 4 == 0 && d->dout_ld % 4 == 0 && d->dtable_ld % 4 == 0 && (uintptr_t)dout % 16 == 0 && (uintptr_t)dtable % 16 == 0;
-    if (is_small(d)) return vec ? launch_smalls<true>(t, ids, status, p.lanes, p.col_tiles, st) : launch_smalls<false>(t, ids, status, p.lanes, p.col_tiles, st);
+    if (is_small(d)) return vec ? launch_small_for<true>(t, ids, status, p.lanes, p.col_tiles, st) : launch_small_for<false>(t, ids, status, p.lanes, p.col_tiles, st);
     SortArgs a;
     a.n = (int32_t)d->n;
     a.vocab = d->vocab;

@@ -481,110 +481,105 @@ __device__ __forceinline__ void cta_sum(float (&v)[K], float (*buf)[kWideThreads
     }
 }
 
-// Slices of more than 1024 columns: a CTA per slice row passes over it three times (five for the layer norm), and finds it
-// in the caches from the second time on.
+// Slices of more than 1024 columns: a CTA per slice row, which it keeps in shared memory in fp32 between the passes (every
+// thread reads back its own columns), so that x, y and gate are read once here too.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kWideThreads) norm_forward_wide_kernel(const NormArgs a, const T* x, const T* y, const T* gate, T* h, T* u) {
     constexpr int E = 4;
+    extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float sums[4][kWideThreads / 32][1];   // one for each sum
+    float* const kept = reinterpret_cast<float*>(ring);
     const int64_t item = blockIdx.x, row = item / a.p;
     const int c0 = (int)(item - row * a.p) * a.w;
     const Columns<VEC, E> cols(threadIdx.x, kWideThreads, a.w, false);
     const bool ragged = a.w % E != 0;
     const float inv_w = 1.f / (float)a.w;
-    const int chunks = (a.w + 4 * kWideThreads - 1) / (4 * kWideThreads);
+    const int chunks = (a.w + E * kWideThreads - 1) / (E * kWideThreads);
     auto get = [&](const T* from, int i, float(&f)[E]) {
         Chunk<T, E> q;
         cols.load(q, from, i);
         q.get(f);
         cols.keep(f, i, false);
     };
-    float my = 0.f, ry = 0.f, sum[1];
-    if (y) {
-        if (a.layer) {
-            sum[0] = 0.f;
-#pragma unroll 4
-            for (int i = 0; i < chunks; ++i) {
-                float f[E];
-                get(y + row * a.y_ld + c0, i, f);
+    // slots [chunk][j][thread] of shared memory
+    auto keep = [&](int i, const float(&f)[E]) {
 #pragma unroll
-                for (int j = 0; j < E; ++j) sum[0] += f[j];
-            }
-            cta_sum(sum, sums + 0);
-            my = sum[0] * inv_w;
+        for (int j = 0; j < E; ++j) kept[(i * E + j) * kWideThreads + threadIdx.x] = f[j];
+    };
+    auto kept_at = [&](int i, float(&f)[E]) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) f[j] = kept[(i * E + j) * kWideThreads + threadIdx.x];
+    };
+    // sum of the squares about the mean (of the kept row) -> 1 / the root; the mean comes back in `mean`
+    auto scale_of = [&](float total, float& mean, float(*means)[kWideThreads / 32][1], float(*squares)[kWideThreads / 32][1]) {
+        float sum[1] = {total};
+        mean = 0.f;
+        if (a.layer) {
+            cta_sum(sum, means);
+            mean = sum[0] * inv_w;
         }
         sum[0] = 0.f;
+        for (int i = 0; i < chunks; ++i) {
+            float f[E];
+            kept_at(i, f);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float t = cols.inside(i, j) ? f[j] - mean : 0.f;
+                sum[0] = fmaf(t, t, sum[0]);
+            }
+        }
+        cta_sum(sum, squares);
+        return rsqrtf(fmaf(sum[0], inv_w, a.eps));
+    };
+    float my = 0.f, ry = 0.f;
+    if (y) {
+        float total = 0.f;
 #pragma unroll 4
         for (int i = 0; i < chunks; ++i) {
             float f[E];
             get(y + row * a.y_ld + c0, i, f);
+            keep(i, f);
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float t = cols.inside(i, j) ? f[j] - my : 0.f;
-                sum[0] = fmaf(t, t, sum[0]);
-            }
+            for (int j = 0; j < E; ++j) total += f[j];
         }
-        cta_sum(sum, sums + 1);
-        ry = rsqrtf(fmaf(sum[0], inv_w, a.eps));
+        ry = scale_of(total, my, sums + 0, sums + 1);
     }
-    auto step = [&](int i, float(&v)[E]) {   // unrounded h, zero past the slice
-        float t[E], g[E], wp[E], bp[E];
-#pragma unroll
-        for (int j = 0; j < E; ++j) v[j] = 0.f;
+    float total = 0.f;
+#pragma unroll 2
+    for (int i = 0; i < chunks; ++i) {   // h may be x: an element is read before it is written, and by the same thread
+        float v[E] = {0.f, 0.f, 0.f, 0.f};
         if (x) get(x + row * a.x_ld + c0, i, v);
-        if (!y) return;
-        get(y + row * a.y_ld + c0, i, t);
-        if (gate) get(gate + row * a.gate_ld + c0, i, g);
-        cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, wp);
-        cols.vector(a.b_post ? a.b_post + c0 : nullptr, i, 0.f, bp);
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            float b = fmaf((t[j] - my) * ry, wp[j], bp[j]);
-            if (gate) b *= sigmoid(g[j]);
-            v[j] = cols.inside(i, j) ? fmaf(a.s, b, v[j]) : 0.f;
-        }
-    };
-    float mh = 0.f, rh = 0.f;
-    if (u) {
-        if (a.layer) {
-            sum[0] = 0.f;
-#pragma unroll 2
-            for (int i = 0; i < chunks; ++i) {
-                float v[E];
-                step(i, v);
-#pragma unroll
-                for (int j = 0; j < E; ++j) sum[0] += v[j];
-            }
-            cta_sum(sum, sums + 2);
-            mh = sum[0] * inv_w;
-        }
-        sum[0] = 0.f;
-#pragma unroll 2
-        for (int i = 0; i < chunks; ++i) {
-            float v[E];
-            step(i, v);
+        if (y) {
+            float t[E], g[E], wp[E], bp[E];
+            kept_at(i, t);
+            if (gate) get(gate + row * a.gate_ld + c0, i, g);
+            cols.vector(a.w_post ? a.w_post + c0 : nullptr, i, 1.f, wp);
+            cols.vector(a.b_post ? a.b_post + c0 : nullptr, i, 0.f, bp);
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const float t = cols.inside(i, j) ? v[j] - mh : 0.f;
-                sum[0] = fmaf(t, t, sum[0]);
+                float b = fmaf((t[j] - my) * ry, wp[j], bp[j]);
+                if (gate) b *= sigmoid(g[j]);
+                v[j] = fmaf(a.s, b, v[j]);
             }
+            cols.keep(v, i, false);
         }
-        cta_sum(sum, sums + 3);
-        rh = rsqrtf(fmaf(sum[0], inv_w, a.eps));
-    }
-#pragma unroll 2
-    for (int i = 0; i < chunks; ++i) {   // h may be x: an element is read before it is written, and by the same lane
-        float v[E];
-        step(i, v);
-        if (h) cols.store(h + row * a.h_ld + c0, i, v, ragged);
-        if (u) {
-            float wq[E], bq[E];
-            cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, wq);
-            cols.vector(a.b_pre ? a.b_pre + c0 : nullptr, i, 0.f, bq);
+        keep(i, v);
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[j] = fmaf((v[j] - mh) * rh, wq[j], bq[j]);
-            cols.store(u + row * a.u_ld + c0, i, v, ragged);
-        }
+        for (int j = 0; j < E; ++j) total += v[j];
+        if (h) cols.store(h + row * a.h_ld + c0, i, v, ragged);
+    }
+    if (!u) return;
+    float mh;
+    const float rh = scale_of(total, mh, sums + 2, sums + 3);
+#pragma unroll 2
+    for (int i = 0; i < chunks; ++i) {
+        float v[E], wq[E], bq[E];
+        kept_at(i, v);
+        cols.vector(a.w_pre ? a.w_pre + c0 : nullptr, i, 1.f, wq);
+        cols.vector(a.b_pre ? a.b_pre + c0 : nullptr, i, 0.f, bq);
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = fmaf((v[j] - mh) * rh, wq[j], bq[j]);
+        cols.store(u + row * a.u_ld + c0, i, v, ragged);
     }
 }
 
@@ -1317,8 +1312,12 @@ struct ForwardCall {
         }
     }
     template <bool VEC>
-    void wide() const {
-        norm_forward_wide_kernel<T, VEC><<<(unsigned)(a.n * a.p), kWideThreads, 0, st>>>(a, x, y, gate, h, u);
+    slicegcn_status_t wide() const {
+        const int smem = (a.w + 4 * kWideThreads - 1) / (4 * kWideThreads) * 4 * kWideThreads * (int)sizeof(float);   // 64 KB at most
+        if (smem > 32 * 1024)
+            SGCN_CUDA(cudaFuncSetAttribute(norm_forward_wide_kernel<T, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        norm_forward_wide_kernel<T, VEC><<<(unsigned)(a.n * a.p), kWideThreads, smem, st>>>(a, x, y, gate, h, u);
+        return SLICEGCN_OK;
     }
 };
 
@@ -1419,14 +1418,14 @@ slicegcn_status_t slicegcn_residual_norm_forward(const slicegcn_residual_norm_de
         using T = __nv_bfloat16;
         const ForwardCall<T> call{pl, a, (const T*)x, (const T*)y, (const T*)gate, (T*)h, (T*)u, st};
         if (wide)
-            vec4 ? call.template wide<true>() : call.template wide<false>();
+            SGCN_TRY(vec4 ? call.template wide<true>() : call.template wide<false>());
         else
             SGCN_TRY((vec8 ? call.template pick<true, 8>() : vec4 ? call.template pick<true, 4>() : call.template pick<false, 4>()));
     } else {
         using T = float;
         const ForwardCall<T> call{pl, a, (const T*)x, (const T*)y, (const T*)gate, (T*)h, (T*)u, st};
         if (wide)
-            vec4 ? call.template wide<true>() : call.template wide<false>();
+            SGCN_TRY(vec4 ? call.template wide<true>() : call.template wide<false>());
         else
             SGCN_TRY((vec4 ? call.template pick<true, 4>() : call.template pick<false, 4>()));
     }
