@@ -74,3 +74,42 @@ def test_training_reduces_the_loss():
     losses = [float(m.step(0.5)) for _ in range(40)]
     assert np.isfinite(losses).all() and losses[-1] < 0.7 * losses[0]
     m.B.slicegcn_graph_destroy(m.g)
+
+
+def test_every_call_can_be_captured_in_a_graph():
+    """No call allocates, synchronises or reads back, so a step of all of them replays from a CUDA graph, small and large forms."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    torch.manual_seed(0)
+    for n, vocab, p, w, extra in [(900, 70, 4, 24, 10), (30_000, 500, 1, 300, 400_000), (50, 9, 1, 1500, 7)]:
+        cols = p * w
+        ids = torch.randint(0, vocab, (n,), dtype=torch.int32, device="cuda")
+        table, dtable = torch.randn((vocab, cols), device="cuda"), torch.empty((vocab, cols), device="cuda")
+        x, y, h, u, dx, dy = (torch.randn((n, cols), device="cuda") for _ in range(6))
+        dw, big, out = torch.empty(cols, device="cuda"), torch.randn(extra, device="cuda"), torch.empty(extra, device="cuda")
+        norm = torch.zeros(1, device="cuda")
+        e, r = B.make_embed_desc(n, vocab, cols), B.make_residual_norm_desc(n, p, w)
+        clipped = torch.empty_like(dtable)
+        t = B.make_tensor_list([dtable, big], [clipped, out])
+        wsb = max(B.slicegcn_embed_workspace_bytes(e), B.slicegcn_residual_norm_workspace_bytes(r), B.slicegcn_clip_workspace_bytes())
+        ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+
+        def step():
+            st = torch.cuda.current_stream().cuda_stream
+            B.slicegcn_embed_forward(e, ids, table, x, None, st)
+            B.slicegcn_residual_norm_forward(r, x, y, None, h, u, st)
+            B.slicegcn_residual_norm_backward(r, y, None, h, u, x, dx, dy, None, None, None, dw, None, ws, wsb, st)
+            B.slicegcn_embed_backward(e, ids, dx, dtable, None, ws, wsb, st)
+            B.slicegcn_clip_grads(t, 1.0, norm, ws, wsb, st)
+        step()
+        torch.cuda.synchronize()
+        want = [v.clone() for v in (x, h, u, dx, dy, dw, dtable, clipped, out, norm)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        for v in (x, h, u, dx, dy, dw, dtable, clipped, out, norm):
+            v.fill_(7.0)
+        graph.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((x, h, u, dx, dy, dw, dtable, clipped, out, norm), want))
