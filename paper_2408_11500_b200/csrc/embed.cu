@@ -4,6 +4,7 @@
 // The gradient sorts the ids (stable least-significant-digit radix sort), so the positions of one id lie next to each
 // other in their own order and every row of dtable is one sum in a fixed order: no floating-point atomics.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -319,6 +320,8 @@ __device__ __forceinline__ void store4(float* row, int col, int stride, int widt
     }
 }
 
+constexpr int kJoin = 4;   // units that one thread joins per column: all threads of the CTA share the first half of the joining
+
 // Shared memory of a CTA that sums.
 template <int L>
 struct SumShared {
@@ -326,7 +329,8 @@ struct SumShared {
     static constexpr int A = L < kAhead ? L : kAhead;   // rows on their way at any time, and positions per batch
     float4 ring[A][kSumThreads];
     float sums[U][2][4 * L];
-    int4 unit_info[U];   // {head present, head ends here, tail's id or -1, unused}
+    int4 unit_info[U];            // {head present, head ends here, tail's id or -1, unused}
+    int4 part_info[U / kJoin];    // the same for kJoin units each
 };
 // The sorted positions: in memory, or (small problems) in the CTA's own shared memory as 13 bits of position under the
 // id's distance from the CTA's first one.
@@ -427,36 +431,62 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
     if (s < e) finish(e < n && pairs(e).x == key);
     if (l == 0) sh.unit_info[unit] = make_int4(head, head_ends, tail_id, 0);
     __syncthreads();
-    // one thread per column joins the units' sums in order
-    if (tid >= 4 * L || c0 + tid >= a.width) return;
-    float sum = 0.f;
-    bool open = false, started = false, any_head = false, ended = false;
-    int id = -1;
-    auto write = [&](int to, float v) {
-        float* t = a.dtable + (int64_t)to * a.dtable_ld + c0 + tid;
+    // The units' sums are joined in order: first kJoin units per thread and column, then those results by one thread per column.
+    auto write = [&](int to, int c, float v) {
+        float* t = a.dtable + (int64_t)to * a.dtable_ld + c0 + c;
         *t = v + (a.accumulate ? *t : 0.f);
     };
-#pragma unroll 8
-    for (int k = 0; k < U; ++k) {
-        const int4 f = sh.unit_info[k];
-        if (f.x) {
-            if (!open) open = true, started = false, sum = 0.f, any_head = true;
-            sum += sh.sums[k][0][tid];
-            if (f.y) {
-                if (started)
-                    write(id, sum);
-                else if (!ONE)
-                    a.head[(int64_t)cta * a.width + c0 + tid] = sum, ended = true;
-                open = false;
+    struct Joined {
+        float head, tail;
+        bool any_head, ended;
+        int id;   // of the tail, or -1
+    };
+    auto join = [&](auto count, const int4* info, int first, int stride, int c) {
+        Joined r{0.f, 0.f, false, false, -1};
+        float sum = 0.f;
+        bool open = false, started = false;
+        int id = -1;
+        constexpr int N = decltype(count)::value;
+        int4 f[N];
+        float hs[N], ts[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] = info[k], hs[k] = sh.sums[first + k * stride][0][c], ts[k] = sh.sums[first + k * stride][1][c];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            if (f[k].x) {
+                if (!open) open = true, started = false, sum = 0.f, r.any_head = true;
+                sum += hs[k];
+                if (f[k].y) {
+                    if (started)
+                        write(id, c, sum);
+                    else
+                        r.head = sum, r.ended = true;
+                    open = false;
+                }
             }
+            if (f[k].z >= 0) open = true, started = true, sum = ts[k], id = f[k].z;
         }
-        if (f.z >= 0) open = true, started = true, sum = sh.sums[k][1][tid], id = f.z;
+        if (open && started) r.tail = sum, r.id = id;
+        if (open && !started) r.head = sum;
+        return r;
+    };
+    constexpr int W = 4 * L, P = U / kJoin;   // columns of the tile, first results
+    {
+        const int c = tid % W, g = tid / W;   // W * P threads: all of them
+        const bool inside = c0 + c < a.width;
+        Joined r{0.f, 0.f, false, false, -1};
+        if (inside) r = join(std::integral_constant<int, kJoin>{}, sh.unit_info + g * kJoin, g * kJoin, 1, c);
+        __syncthreads();
+        if (inside) sh.sums[g * kJoin][0][c] = r.head, sh.sums[g * kJoin][1][c] = r.tail;
+        if (c == 0) sh.part_info[g] = make_int4(r.any_head, r.ended, r.id, 0);
     }
+    __syncthreads();
+    if (tid >= W || c0 + tid >= a.width) return;
+    const Joined r = join(std::integral_constant<int, P>{}, sh.part_info, 0, kJoin, tid);
     if (ONE) return;
-    const bool tail = open && started;
-    if (tail) a.tail[(int64_t)cta * a.width + c0 + tid] = sum;
-    if (open && !started) a.head[(int64_t)cta * a.width + c0 + tid] = sum;
-    if (tid == 0 && blockIdx.y == 0) a.info[cta] = make_int4(any_head, ended, tail, id);
+    if (r.id >= 0) a.tail[(int64_t)cta * a.width + c0 + tid] = r.tail;
+    if (r.any_head) a.head[(int64_t)cta * a.width + c0 + tid] = r.head;
+    if (tid == 0 && blockIdx.y == 0) a.info[cta] = make_int4(r.any_head, r.ended, r.id >= 0, r.id);
 }
 
 template <int L, bool VEC>
