@@ -611,67 +611,97 @@ __global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs 
     sum_sorted<L, VEC, true>(a, PairsInShared{sh.list[cur], v0}, m, (m + U - 1) / U, 0, sh.sum);
 }
 
-// What is left after the sums.  CTAs 0 .. sum_ctas - 1: the id that starts in that CTA and reaches over its edge; eight
-// groups of 32 lanes each add a share of the CTAs in order, then the shares are added in order.  The others: rows of ids
-// that do not occur, by lane groups like those of the sums.
+// What is left after the sums.  The first join_ctas CTAs: ids that reach over the edges of the sums' CTAs, a warp for the one
+// that starts in each of them; one that reaches over more than kLongJoin is added by the whole CTA, in shares of consecutive
+// parts that are then added in order.  The other CTAs: rows of ids that do not occur, by lane groups like those of the sums.
+constexpr int kLongJoin = 16;
 template <int L, bool VEC>
-__global__ void __launch_bounds__(256) embed_finish_kernel(const SumArgs a) {
-    __shared__ float part[8][4 * L];
-    __shared__ int last;
+__global__ void __launch_bounds__(256) embed_finish_kernel(const SumArgs a, int join_ctas) {
+    constexpr int W = 4 * L, PER = (W + 31) / 32;   // columns of the tile, of a lane
+    __shared__ float part[8][W];
+    __shared__ int last_of[8], id_of[8];
     cudaGridDependencySynchronize();
-    const int c0 = blockIdx.y * 4 * L;
-    if ((int)blockIdx.x >= a.sum_ctas) {
+    const int c0 = blockIdx.y * W;
+    if ((int)blockIdx.x >= join_ctas) {
         const int l = threadIdx.x & (L - 1), col = c0 + (VEC ? 4 * l : l);
         const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-        if (col >= a.width) return;
-        const int64_t step = (int64_t)(gridDim.x - a.sum_ctas) * (256 / L);
-        for (int64_t v = ((int64_t)(blockIdx.x - a.sum_ctas) * 256 + threadIdx.x) / L; v < a.vocab; v += 4 * step) {
-            uint8_t there[4];   // four rows' flags at once
-#pragma unroll
-            for (int q = 0; q < 4; ++q) there[q] = a.present[min(v + q * step, a.vocab - 1)];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (!there[q] && v + q * step < a.vocab) store4<VEC>(a.dtable + (v + q * step) * a.dtable_ld, col, L, a.width, 0, zero);
+        // a lane group takes L rows: their flags with one load, then the rows that are absent
+        const unsigned group = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((threadIdx.x & 31) & ~(L - 1));
+        const int64_t step = (int64_t)(gridDim.x - join_ctas) * 256;
+        for (int64_t v = ((int64_t)(blockIdx.x - join_ctas) * 256 + threadIdx.x) / L * L; v < a.vocab; v += step) {
+            unsigned absent = __ballot_sync(group, v + l < a.vocab && !a.present[v + l]);
+            absent = (absent & group) >> ((threadIdx.x & 31) & ~(L - 1));
+            for (; absent; absent &= absent - 1) {
+                const int64_t r = v + __ffs(absent) - 1;
+                if (col < a.width) store4<VEC>(a.dtable + r * a.dtable_ld, col, L, a.width, 0, zero);
+            }
         }
         return;
     }
-    const int4 f = a.info[blockIdx.x];
-    if (!f.z) return;
-    const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
-    if (threadIdx.x < 32) {   // the CTA in which the id ends
-        int c = blockIdx.x + 1;
-        for (;; c += 32) {
-            const int k = c + lane;
-            const bool stop = k >= a.sum_ctas || !a.info[k].x || a.info[k].y;
-            const unsigned hit = __ballot_sync(0xffffffffu, stop);
-            if (hit) {
-                c += __ffs(hit) - 1;
-                break;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, start = blockIdx.x * 8 + w;
+    // the parts lo .. hi of an id's sum, in order: several on their way at a time
+    auto add = [&](int lo, int hi, float(&s)[PER]) {
+#pragma unroll 8
+        for (int k = lo; k <= hi; ++k)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) s[j] += a.head[(int64_t)k * a.width + min(c0 + lane + 32 * j, a.width - 1)];
+    };
+    auto finish = [&](int id, const float(&tail)[PER], const float(&s)[PER]) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int c = lane + 32 * j;
+            if (c < W && c0 + c < a.width) {
+                float* to = a.dtable + (int64_t)id * a.dtable_ld + c0 + c;
+                *to = tail[j] + s[j] + (a.accumulate ? *to : 0.f);
             }
         }
-        if (lane == 0) last = min(c, a.sum_ctas - 1);
-    }
-    __syncthreads();
-    const int lo = blockIdx.x + 1, count = last - lo + 1, share = (count + 7) / 8;
-    const int k1 = min(last + 1, lo + (g + 1) * share);
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int k = lo + g * share; k < k1; ++k)
+    };
+    const int4 none = make_int4(0, 1, 0, 0);
+    int4 f = start + lane < a.sum_ctas ? a.info[start + lane] : none;   // this one and those after it
+    const int has_tail = __shfl_sync(0xffffffffu, f.z, 0), id = __shfl_sync(0xffffffffu, f.w, 0);
+    int last = -1;
+    if (has_tail) {
+        float tail[PER];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = c0 + lane + 32 * j;
-            s[j] += a.head[(int64_t)k * a.width + min(c, a.width - 1)];
+        for (int j = 0; j < PER; ++j) tail[j] = a.tail[(int64_t)start * a.width + min(c0 + lane + 32 * j, a.width - 1)];
+        unsigned ends = __ballot_sync(0xffffffffu, lane > 0 && (!f.x || f.y));   // the CTA in which the id ends
+        int c = start;
+        while (!ends) {
+            c += 32;
+            f = c + lane < a.sum_ctas ? a.info[c + lane] : none;
+            ends = __ballot_sync(0xffffffffu, !f.x || f.y);
         }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (lane + 32 * j < 4 * L) part[g][lane + 32 * j] = s[j];
+        last = min(c + __ffs(ends) - 1, a.sum_ctas - 1);
+        if (last - start <= kLongJoin) {
+            float s[PER] = {};
+            add(start + 1, last, s);
+            finish(id, tail, s);
+            last = -1;
+        }
+    }
+    if (lane == 0) last_of[w] = last, id_of[w] = id;
     __syncthreads();
-    if (threadIdx.x < 4 * L && c0 + (int)threadIdx.x < a.width) {
-        const int c = threadIdx.x;
-        float t = a.tail[(int64_t)blockIdx.x * a.width + c0 + c];
-        for (int k = 0; k < 8; ++k) t += part[k][c];
-        float* to = a.dtable + (int64_t)f.w * a.dtable_ld + c0 + c;
-        *to = t + (a.accumulate ? *to : 0.f);
+    for (int q = 0; q < 8; ++q) {
+        if (last_of[q] < 0) continue;   // the same for the whole CTA
+        const int from = blockIdx.x * 8 + q, share = (last_of[q] - from + 7) / 8;
+        float s[PER] = {};
+        add(from + 1 + w * share, min(last_of[q], from + (w + 1) * share), s);
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (lane + 32 * j < W) part[w][lane + 32 * j] = s[j];
+        __syncthreads();
+        if (w == 0) {
+            float tail[PER];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                tail[j] = a.tail[(int64_t)from * a.width + min(c0 + lane + 32 * j, a.width - 1)];
+                s[j] = 0.f;
+                if (lane + 32 * j < W)
+                    for (int o = 0; o < 8; ++o) s[j] += part[o][lane + 32 * j];
+            }
+            finish(id_of[q], tail, s);
+        }
+        __syncthreads();
     }
 }
 
@@ -745,9 +775,10 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
 template <int L, bool VEC>
 slicegcn_status_t launch_sum(const SumArgs& a, int col_tiles, cudaStream_t st) {
     if (a.sum_ctas > 0) SGCN_TRY(launch_after(embed_sum_kernel<L, VEC>, dim3(a.sum_ctas, col_tiles), kSumThreads, 0, st, a));
-    const unsigned zero_ctas = a.accumulate ? 0 : (unsigned)std::min<int64_t>((a.vocab * L + 255) / 256, kSMs * 8);
-    if (a.sum_ctas > 1 || zero_ctas > 0)
-        SGCN_TRY(launch_after(embed_finish_kernel<L, VEC>, dim3(a.sum_ctas + zero_ctas, col_tiles), 256, 0, st, a));
+    const int join_ctas = a.sum_ctas > 1 ? (a.sum_ctas + 7) / 8 : 0;
+    const unsigned zero_ctas = a.accumulate ? 0 : (unsigned)std::min<int64_t>((a.vocab * L + 255) / 256, kSMs * 6);
+    if (join_ctas + zero_ctas > 0)
+        SGCN_TRY(launch_after(embed_finish_kernel<L, VEC>, dim3(join_ctas + zero_ctas, col_tiles), 256, 0, st, a, join_ctas));
     return SLICEGCN_OK;
 }
 
