@@ -780,7 +780,7 @@ struct Staged {
     static constexpr int kVectors = 3 * NV * 32 * 16;                             // w_post, b_post, w_pre
     static constexpr int smem(int warps) { return kVectors + warps * 2 * kRow; }
 };
-template <typename T, bool VEC, int NV, bool BIAS>
+template <typename T, bool VEC, int NV, bool BIAS, bool LAYER>
 __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_kernel(const NormArgs a, const T* y, const T* gate, const T* h,
                                                                                        const float* dh, const float* du, float* dx,
                                                                                        float* dy, float* dgate) {
@@ -841,9 +841,13 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    // zero what a ragged chunk holds past the slice, and what subtracting a mean leaves there
-    auto trim = [&](float(&f)[E], int i) {
-        if (a.w < 128 * (i + 1)) cols.keep(f, i, false);
+    // zero what a chunk holds past the slice, and what subtracting a mean leaves there; every chunk but the last ones is whole
+    auto whole = [&](int i) { return a.w >= 128 * (i + 1); };
+    auto store = [&](float* to, int i, const float(&f)[E]) {
+        if (VEC && whole(i))
+            Chunk<float, E>::store(to + cols.at(i), f);
+        else
+            cols.store(to, i, f, ragged);
     };
     float acc[BIAS ? 4 : 2][NV][E];   // dw_post, dw_pre, db_post, db_pre
 #pragma unroll
@@ -875,13 +879,13 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
                 words_get<float>(at + tensor, 0, cols, i, f);
         };
         float mh = 0.f, my = 0.f;
-        if (a.layer) {
+        if (LAYER) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 float hv[E], yv[E];
                 get_t(S::kH, odd_h, i, hv), get_t(S::kY, odd_y, i, yv);
-                trim(hv, i), trim(yv, i);
+                if (!whole(i)) cols.keep(hv, i, false), cols.keep(yv, i, false);
 #pragma unroll
                 for (int j = 0; j < E; ++j) m[0] += hv[j], m[1] += yv[j];
             }
@@ -897,20 +901,21 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
             get_t(S::kY, odd_y, i, yv);
             staged_get<float>(vectors + 2 * S::kF + i * HF, wq);
 #pragma unroll
-            for (int j = 0; j < E; ++j) hv[j] -= mh, yv[j] -= my;
-            trim(hv, i), trim(yv, i), trim(uv, i);
+            for (int j = 0; j < E; ++j)
+                if (LAYER) hv[j] -= mh, yv[j] -= my;
+            if (!whole(i)) cols.keep(hv, i, false), cols.keep(yv, i, false), cols.keep(uv, i, false);
 #pragma unroll
             for (int j = 0; j < E; ++j) {
                 const float g = uv[j] * wq[j];
                 q[0] = fmaf(hv[j], hv[j], q[0]);
                 q[1] = fmaf(yv[j], yv[j], q[1]);
-                q[2] += g;
+                if (LAYER) q[2] += g;
                 q[3] = fmaf(g, hv[j], q[3]);
             }
         }
         group_sum<32>(q);
         const float rh = rsqrtf(fmaf(q[0], inv_w, a.eps)), ry = rsqrtf(fmaf(q[1], inv_w, a.eps));
-        const float mg = a.layer ? q[2] * inv_w : 0.f, mgh = q[3] * inv_w * rh;
+        const float mg = LAYER ? q[2] * inv_w : 0.f, mgh = q[3] * inv_w * rh;
         float t[NV][E], z[2] = {0.f, 0.f};   // dt w_post; its sum, and that of its product with y
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -923,36 +928,39 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
             staged_get<float>(vectors + i * HF, wp);
             staged_get<float>(vectors + S::kF + i * HF, bp);
             staged_get<float>(vectors + 2 * S::kF + i * HF, wq);
-            trim(uv, i), trim(d, i), trim(yv, i), trim(gv, i), trim(hv, i);
+            if (!whole(i)) {
+                cols.keep(uv, i, false), cols.keep(d, i, false), cols.keep(yv, i, false);
+                cols.keep(gv, i, false), cols.keep(hv, i, false);
+            }
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const float hhat = (hv[j] - mh) * rh;
-                d[j] = fmaf(rh, fmaf(uv[j], wq[j], -mg) - hhat * mgh, d[j]);
+                const float hhat = (LAYER ? hv[j] - mh : hv[j]) * rh;
+                d[j] = fmaf(rh, (LAYER ? fmaf(uv[j], wq[j], -mg) : uv[j] * wq[j]) - hhat * mgh, d[j]);
                 acc[1][i][j] = fmaf(uv[j], hhat, acc[1][i][j]);
                 if (BIAS) acc[BIAS ? 3 : 1][i][j] += uv[j];
                 float open, slope;
                 gate_and_slope(gv[j], open, slope);
-                const float ds = d[j] * a.s, yc = yv[j] - my, yhat = yc * ry, dt = ds * open;
+                const float ds = d[j] * a.s, yc = LAYER ? yv[j] - my : yv[j], yhat = yc * ry, dt = ds * open;
                 gv[j] = ds * slope * fmaf(yhat, wp[j], bp[j]);
                 t[i][j] = dt * wp[j];              // w_post is zero past the slice
-                z[0] += t[i][j];
+                if (LAYER) z[0] += t[i][j];
                 z[1] = fmaf(t[i][j], yc, z[1]);
                 acc[0][i][j] = fmaf(dt, yhat, acc[0][i][j]);
                 if (BIAS) acc[BIAS ? 2 : 0][i][j] += dt;
             }
-            if (dx) cols.store(dx + row * a.dx_ld + c0, i, d, ragged);
-            if (dgate) cols.store(dgate + row * a.dgate_ld + c0, i, gv, ragged);
+            if (dx) store(dx + row * a.dx_ld + c0, i, d);
+            if (dgate) store(dgate + row * a.dgate_ld + c0, i, gv);
         }
         if (!dy) continue;
         group_sum<32>(z);
-        const float mt = a.layer ? z[0] * inv_w : 0.f, mty = z[1] * inv_w * ry;
+        const float mt = LAYER ? z[0] * inv_w : 0.f, mty = z[1] * inv_w * ry;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float yv[E];
             get_t(S::kY, odd_y, i, yv);
 #pragma unroll
-            for (int j = 0; j < E; ++j) yv[j] = ry * (t[i][j] - mt - (yv[j] - my) * ry * mty);
-            cols.store(dy + row * a.dy_ld + c0, i, yv, ragged);
+            for (int j = 0; j < E; ++j) yv[j] = LAYER ? ry * (t[i][j] - mt - (yv[j] - my) * ry * mty) : ry * (t[i][j] - yv[j] * ry * mty);
+            store(dy + row * a.dy_ld + c0, i, yv);
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -1337,15 +1345,18 @@ struct BackwardCall {
         norm_backward_kernel<T, VEC, L><<<(unsigned)pl.ctas, 256, smem, st>>>(a, y, gate, h, dh, du, dx, dy, dgate);
         return SLICEGCN_OK;
     }
-    template <bool VEC, int NV, bool BIAS>
+    template <bool VEC, int NV, bool BIAS, bool LAYER>
     slicegcn_status_t staged() const {
-        SGCN_CUDA(cudaFuncSetAttribute(norm_backward_staged_kernel<T, VEC, NV, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem));
-        norm_backward_staged_kernel<T, VEC, NV, BIAS><<<(unsigned)pl.ctas, pl.warps * 32, pl.smem, st>>>(a, y, gate, h, dh, du, dx, dy, dgate);
+        SGCN_CUDA(cudaFuncSetAttribute(norm_backward_staged_kernel<T, VEC, NV, BIAS, LAYER>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem));
+        norm_backward_staged_kernel<T, VEC, NV, BIAS, LAYER><<<(unsigned)pl.ctas, pl.warps * 32, pl.smem, st>>>(a, y, gate, h, dh, du, dx, dy, dgate);
         return SLICEGCN_OK;
     }
-    template <bool VEC, bool BIAS>
+    template <bool VEC, bool BIAS, bool LAYER>
     slicegcn_status_t staged_for() const {
-        return pl.chunks == 2 ? staged<VEC, 2, BIAS>() : pl.chunks == 4 ? staged<VEC, 4, BIAS>() : pl.chunks == 5 ? staged<VEC, 5, BIAS>() : staged<VEC, 8, BIAS>();
+        return pl.chunks == 2   ? staged<VEC, 2, BIAS, LAYER>()
+               : pl.chunks == 4 ? staged<VEC, 4, BIAS, LAYER>()
+               : pl.chunks == 5 ? staged<VEC, 5, BIAS, LAYER>()
+                                : staged<VEC, 8, BIAS, LAYER>();
     }
     template <bool VEC>
     slicegcn_status_t run(bool bias) const {
@@ -1359,7 +1370,10 @@ struct BackwardCall {
                 default: SGCN_TRY((go<VEC, 32>())); break;
             }
         } else if (pl.form == kStaged) {
-            SGCN_TRY((bias ? staged_for<VEC, true>() : staged_for<VEC, false>()));
+            if (a.layer)
+                SGCN_TRY((bias ? staged_for<VEC, true, true>() : staged_for<VEC, false, true>()));
+            else
+                SGCN_TRY((bias ? staged_for<VEC, true, false>() : staged_for<VEC, false, false>()));
         } else {
             norm_stats_kernel<T, VEC><<<(unsigned)(a.n * a.p), kWideThreads, 0, st>>>(a, y, gate, h, dh, du, stats);
             SGCN_LAUNCH_CHECK();
