@@ -414,10 +414,11 @@ slicegcn_status_t slicegcn_train_epochs_host(const slicegcn_model* m, const slic
  * first column, with the leading dimension of the whole matrix.
  */
 enum { SLICEGCN_DEVSTATUS_BAD_ID = 33 };
+#define SLICEGCN_MAX_EMBED_WIDTH (1 << 20)
 typedef struct slicegcn_embed_desc {
     int64_t n;             /* ids, >= 0 */
     int64_t vocab;         /* rows of the table, 1 .. 2^31 - 2 */
-    int32_t width;         /* columns, >= 1 */
+    int32_t width;         /* columns, 1 .. SLICEGCN_MAX_EMBED_WIDTH */
     int32_t table_dtype;   /* forward: storage type of the table ... */
     int32_t out_dtype;     /* ... and of out (fp32 arithmetic, one rounding) */
     int32_t accumulate;    /* backward: 0 overwrites the whole of dtable (rows of absent ids become zero), 1 adds to it */
@@ -425,13 +426,14 @@ typedef struct slicegcn_embed_desc {
     int64_t table_ld, out_ld;       /* leading dimensions; forward only */
     int64_t dout_ld, dtable_ld;     /* backward only */
 } slicegcn_embed_desc;
-/* ids [device, int32 n], table [device, vocab x width], out [device, n x width].  Errors: INVALID_ARG, OVERFLOW, CUDA. */
+/* ids [device, int32 n], table [device, vocab x width], out [device, n x width].
+ * Errors: INVALID_ARG, OVERFLOW, UNSUPPORTED (wider rows), CUDA. */
 slicegcn_status_t slicegcn_embed_forward(const slicegcn_embed_desc* d, const int32_t* ids, const void* table, void* out,
                                          int32_t* status, void* stream);
 /* dout [device, fp32 n x width], dtable [device, fp32 vocab x width].  Deterministic: the ids are sorted (stable) and every
  * row is summed in a fixed order; no floating-point atomics.  workspace [device, 16-byte aligned], at least
  * slicegcn_embed_workspace_bytes(d) bytes, contents undefined before and after.
- * Errors: INVALID_ARG, OVERFLOW, ALLOC (workspace too small), CUDA. */
+ * Errors: INVALID_ARG, OVERFLOW, UNSUPPORTED, ALLOC (workspace too small), CUDA. */
 slicegcn_status_t slicegcn_embed_workspace_bytes(const slicegcn_embed_desc* d, int64_t* bytes);
 slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const int32_t* ids, const float* dout, float* dtable,
                                           int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);

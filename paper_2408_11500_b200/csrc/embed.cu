@@ -710,6 +710,7 @@ slicegcn_status_t check_desc(const slicegcn_embed_desc* d, const char* who) {
     if (d->n < 0 || d->vocab < 1 || d->width < 1) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: bad sizes", who);
     if (d->n >= ((int64_t)1 << 31) || d->vocab >= ((int64_t)1 << 31) - 1)
         SGCN_FAIL(SLICEGCN_ERR_OVERFLOW, "%s: n or vocab does not fit int32", who);
+    if (d->width > SLICEGCN_MAX_EMBED_WIDTH) SGCN_FAIL(SLICEGCN_ERR_UNSUPPORTED, "%s: more than %d columns", who, SLICEGCN_MAX_EMBED_WIDTH);
     return SLICEGCN_OK;
 }
 

@@ -62,10 +62,7 @@ struct Chunk<__nv_bfloat16, E> {
     __device__ __forceinline__ void take(const uint2& v) { word[0] = v.x, word[1] = v.y; }
     __device__ __forceinline__ void take(const uint4& v) { word[0] = v.x, word[1] = v.y, word[E / 2 - 2] = v.z, word[E / 2 - 1] = v.w; }
     __device__ __forceinline__ void load(const __nv_bfloat16* p) {
-        if constexpr (E == 8)
-            take(__ldcs(reinterpret_cast<const uint4*>(p)));
-        else
-            take(__ldcs(reinterpret_cast<const uint2*>(p)));
+        take(__ldcs(reinterpret_cast<const uint2*>(p)));   // four columns; eight go through shared memory
     }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&f)[E]) {
         if constexpr (E == 8)
@@ -1193,7 +1190,7 @@ NormArgs make_args(const slicegcn_residual_norm_desc* d) {
 }
 
 constexpr int kSMs = 148;
-constexpr int kMaxWarpWidth = 1024;   // columns of a slice that one warp holds (forward: in registers, gradient: in shared memory)
+constexpr int kMaxWarpWidth = 1024;   // columns of a slice that one warp takes
 
 // Forward, up to 1024 columns.  By lanes (one chunk of E columns each), or staged with a warp per slice row.
 struct ForwardPlan {

@@ -255,6 +255,7 @@ def test_refusals():
     for bad in (dict(n=2 ** 31), dict(vocab=2 ** 31 - 1)):
         d = B.make_embed_desc(**{**ok, **bad})
         refused(B.ERR_OVERFLOW, lambda: B.slicegcn_embed_workspace_bytes(d))
+    refused(B.ERR_UNSUPPORTED, lambda: B.slicegcn_embed_workspace_bytes(B.make_embed_desc(4, 8, (1 << 20) + 1)))
     for bad in (dict(table_ld=3), dict(out_ld=3), dict(table_dtype=7), dict(out_dtype=-1)):
         d = B.make_embed_desc(**{**ok, **bad})
         refused(B.ERR_INVALID_ARG, lambda: B.slicegcn_embed_forward(d, buf, buf, buf))
