@@ -4,6 +4,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <utility>
 
 #include "common.cuh"
 
@@ -125,6 +126,7 @@ __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kClusterT
     __shared__ double smem[kClusterThreads / 32];
     __shared__ double sums[kClusterCtas];
     const cg::cluster_group cluster = cg::this_cluster();
+    auto started = cluster.barrier_arrive();
     const int rank = blockIdx.x, off = threadIdx.x * 16;
     Raw held[kHeld];
 #pragma unroll
@@ -135,6 +137,7 @@ __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kClusterT
     for (int q = 0; q < kHeld; ++q)
         if (rank + q * kClusterCtas < t.count) s += squares(t.p[rank + q * kClusterCtas], off, held[q]);
     s = cta_sum<kClusterThreads>(s, smem);
+    cluster.barrier_wait(std::move(started));   // another CTA's shared memory exists once that CTA runs; a CTA without a piece is here at once
     if (threadIdx.x < kClusterCtas) *cluster.map_shared_rank(&sums[rank], threadIdx.x) = s;
     cluster.sync();   // hardware barrier; no CTA reads another's memory after it
     double total = 0.0;
