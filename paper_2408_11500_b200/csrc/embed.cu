@@ -336,13 +336,13 @@ struct SumShared {
 // id's distance from the CTA's first one.
 struct PairsInMemory {
     const uint2* p;
-    __device__ __forceinline__ uint2 operator()(int i) const { return p[i]; }
+    __device__ __forceinline__ uint2 operator()(uint32_t i) const { return p[i]; }
 };
 constexpr int kSmallBits = 13, kSmallN = 1 << kSmallBits;
 struct PairsInShared {
     const uint32_t* p;
     uint32_t first_id;
-    __device__ __forceinline__ uint2 operator()(int i) const {
+    __device__ __forceinline__ uint2 operator()(uint32_t i) const {
         return make_uint2((p[i] >> kSmallBits) + first_id, p[i] & (kSmallN - 1));
     }
 };
@@ -357,7 +357,8 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
     const int col = c0 + (VEC ? 4 * l : l);
     const bool live_col = col < a.width;
     const int64_t s64 = ((int64_t)cta * U + unit) * per_unit;
-    const int s = (int)min((int64_t)n, s64), e = (int)min((int64_t)n, s64 + per_unit);
+    // unsigned: what is asked for ahead of the last of 2^31 - 1 positions lies past 31 bits
+    const uint32_t s = (uint32_t)min((int64_t)n, s64), e = (uint32_t)min((int64_t)n, s64 + per_unit);
     const unsigned group = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((tid & 31) & ~(L - 1));
     const uint32_t none = (uint32_t)a.vocab;
     const uint32_t before = s > 0 && s < e ? pairs(s - 1).x : 0xffffffffu;
@@ -386,7 +387,7 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
             store4<VEC>(a.dtable + (int64_t)key * a.dtable_ld, col, L, a.width, a.accumulate, acc);
         }
     };
-    auto batch = [&](int b) { return l < A && b + l < e ? pairs(b + l) : make_uint2(none, 0); };
+    auto batch = [&](uint32_t b) { return l < A && b + l < e ? pairs(b + l) : make_uint2(none, 0); };
     auto request = [&](int i, const uint2& p) {   // row i of a batch into slot i
         const uint32_t k = __shfl_sync(group, p.x, i, L), pos = __shfl_sync(group, p.y, i, L);
         if (live_col && k < none)
@@ -396,7 +397,7 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
     uint2 cur = batch(s), next = batch(s + A);
 #pragma unroll
     for (int i = 0; i < A - 1; ++i) request(i, cur);
-    for (int b = s; b < e; b += A) {
+    for (uint32_t b = s; b < e; b += A) {
         const uint2 later = batch(b + 2 * A);
 #pragma unroll
         for (int i = 0; i < A; ++i) {
@@ -428,7 +429,7 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
         next = later;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-    if (s < e) finish(e < n && pairs(e).x == key);
+    if (s < e) finish(e < (uint32_t)n && pairs(e).x == key);
     if (l == 0) sh.unit_info[unit] = make_int4(head, head_ends, tail_id, 0);
     __syncthreads();
     // The units' sums are joined in order: first kJoin units per thread and column, then those results by one thread per column.
