@@ -142,9 +142,11 @@ def _vp(x) -> c_void_p:
     return c_void_p(_ptr(x))
 
 
-def _with_address(d: ctypes.Structure) -> ctypes.Structure:
-    """The struct with its own address as an int beside it (its memory stays where it is)."""
-    d.address = ctypes.addressof(d)
+def _with_address(d: ctypes.Structure, *keep) -> ctypes.Structure:
+    """A struct that a call is given by its address, holding on to the arrays and tensors whose addresses stand in it.  Its own
+    address is taken at the call: a copy of the struct lies elsewhere."""
+    if keep:
+        d._keep = keep
     return d
 
 
@@ -444,7 +446,7 @@ def make_embed_desc(n: int, vocab: int, width: int, scale: float = 1.0, table_dt
 
 
 def slicegcn_embed_forward(d: EmbedDesc, ids, table, out, status=None, stream=None) -> None:
-    _check(_lib.slicegcn_embed_forward(d.address, _ptr(ids), _ptr(table), _ptr(out), _ptr(status), _ptr(stream)))
+    _check(_lib.slicegcn_embed_forward(byref(d), _ptr(ids), _ptr(table), _ptr(out), _ptr(status), _ptr(stream)))
 
 
 def slicegcn_embed_workspace_bytes(d: EmbedDesc) -> int:
@@ -454,7 +456,7 @@ def slicegcn_embed_workspace_bytes(d: EmbedDesc) -> int:
 
 
 def slicegcn_embed_backward(d: EmbedDesc, ids, dout, dtable, status, workspace, workspace_bytes: int, stream=None) -> None:
-    _check(_lib.slicegcn_embed_backward(d.address, _ptr(ids), _ptr(dout), _ptr(dtable), _ptr(status), _ptr(workspace),
+    _check(_lib.slicegcn_embed_backward(byref(d), _ptr(ids), _ptr(dout), _ptr(dtable), _ptr(status), _ptr(workspace),
                                         workspace_bytes, _ptr(stream)))
 
 
@@ -470,12 +472,11 @@ def make_residual_norm_desc(n: int, num_slices: int, h_s: int, kind: int = ROWNO
     if leading_dims:
         raise TypeError(f"unknown leading dimensions {sorted(leading_dims)}")
     d.w_post, d.b_post, d.w_pre, d.b_pre = _ptr(w_post), _ptr(b_post), _ptr(w_pre), _ptr(b_pre)
-    d._keep = (w_post, b_post, w_pre, b_pre)
-    return _with_address(d)
+    return _with_address(d, w_post, b_post, w_pre, b_pre)
 
 
 def slicegcn_residual_norm_forward(d: ResidualNormDesc, x, y, gate, h, u, stream=None) -> None:
-    _check(_lib.slicegcn_residual_norm_forward(d.address, _ptr(x), _ptr(y), _ptr(gate), _ptr(h), _ptr(u), _ptr(stream)))
+    _check(_lib.slicegcn_residual_norm_forward(byref(d), _ptr(x), _ptr(y), _ptr(gate), _ptr(h), _ptr(u), _ptr(stream)))
 
 
 def slicegcn_residual_norm_workspace_bytes(d: ResidualNormDesc) -> int:
@@ -486,7 +487,7 @@ def slicegcn_residual_norm_workspace_bytes(d: ResidualNormDesc) -> int:
 
 def slicegcn_residual_norm_backward(d: ResidualNormDesc, y, gate, h, dh, du, dx, dy, dgate, dw_post, db_post, dw_pre, db_pre,
                                     workspace, workspace_bytes: int, stream=None) -> None:
-    _check(_lib.slicegcn_residual_norm_backward(d.address, _ptr(y), _ptr(gate), _ptr(h), _ptr(dh), _ptr(du), _ptr(dx), _ptr(dy),
+    _check(_lib.slicegcn_residual_norm_backward(byref(d), _ptr(y), _ptr(gate), _ptr(h), _ptr(dh), _ptr(du), _ptr(dx), _ptr(dy),
                                                 _ptr(dgate), _ptr(dw_post), _ptr(db_post), _ptr(dw_pre), _ptr(db_pre),
                                                 _ptr(workspace), workspace_bytes, _ptr(stream)))
 
@@ -503,8 +504,7 @@ def make_tensor_list(src: Sequence, dst: Optional[Sequence] = None) -> TensorLis
               (c_int64 * max(n, 1))(*[t.numel() for t in src]), (c_int32 * max(n, 1))(*[codes[str(t.dtype)] for t in src]))
     d = TensorList(n, ctypes.cast(arrays[0], POINTER(c_void_p)), ctypes.cast(arrays[1], POINTER(c_void_p)) if dst is not None else None,
                    ctypes.cast(arrays[2], POINTER(c_int64)), ctypes.cast(arrays[3], POINTER(c_int32)))
-    d._keep = (arrays, list(src), list(dst) if dst is not None else None)      # pointer arrays and tensors live with the struct
-    return _with_address(d)
+    return _with_address(d, arrays, list(src), list(dst) if dst is not None else None)
 
 
 def slicegcn_clip_workspace_bytes() -> int:
@@ -514,7 +514,7 @@ def slicegcn_clip_workspace_bytes() -> int:
 
 
 def slicegcn_clip_grads(tensors: TensorList, max_norm: float, norm_out, workspace, workspace_bytes: int, stream=None) -> None:
-    _check(_lib.slicegcn_clip_grads(tensors.address, max_norm, _ptr(norm_out), _ptr(workspace), workspace_bytes, _ptr(stream)))
+    _check(_lib.slicegcn_clip_grads(byref(tensors), max_norm, _ptr(norm_out), _ptr(workspace), workspace_bytes, _ptr(stream)))
 
 
 # ------------------------------------------------------------------------------------------ parameter marshalling
