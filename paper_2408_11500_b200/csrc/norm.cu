@@ -1198,7 +1198,9 @@ struct ForwardPlan {
     int chunks, warps, smem;   // staged: chunks per lane, warps per CTA
     int64_t ctas, lanes_rows;
 };
-constexpr int kStagedSmem = 227 * 1024;
+// Shared memory of a CTA's staged rows at most.  Kernels whose size follows the call are allowed all of it, always: the limit
+// belongs to the kernel, and one that followed the call could be lowered by another host thread between here and the launch.
+constexpr int kStagedSmem = 226 * 1024, kWideSmem = SLICEGCN_MAX_NORM_WIDTH * (int)sizeof(float);
 int64_t rows_at_a_time(int64_t ctas, int groups, int p) { return ctas * groups / p; }
 int lanes_for(int need) {
     int lanes = 1;
@@ -1220,7 +1222,7 @@ int smem_for(int dtype, int chunks, int warps) {
 template <template <typename, int> class S>
 void staged_shape(const slicegcn_residual_norm_desc* d, int chunks, int most, int per_sm, int* warps, int* smem, int64_t* row_ctas) {
     *warps = most;
-    while (smem_for<S>(d->dtype, chunks, *warps) > kStagedSmem / per_sm - 1024) --*warps;
+    while (smem_for<S>(d->dtype, chunks, *warps) > kStagedSmem / per_sm) --*warps;
     const int64_t share = (d->n * d->num_slices + kSMs * per_sm - 1) / (kSMs * per_sm);
     *warps = (int)std::max<int64_t>(1, std::min<int64_t>(*warps, share));
     *smem = smem_for<S>(d->dtype, chunks, *warps);
@@ -1300,7 +1302,7 @@ struct ForwardCall {
     }
     template <bool VEC, int NV>
     slicegcn_status_t staged() const {
-        SGCN_CUDA(cudaFuncSetAttribute(norm_forward_staged_kernel<T, VEC, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem));
+        SGCN_CUDA(cudaFuncSetAttribute(norm_forward_staged_kernel<T, VEC, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStagedSmem));
         norm_forward_staged_kernel<T, VEC, NV><<<(unsigned)pl.ctas, pl.warps * 32, pl.smem, st>>>(a, x, y, gate, h, u);
         return SLICEGCN_OK;
     }
@@ -1319,8 +1321,7 @@ struct ForwardCall {
     template <bool VEC>
     slicegcn_status_t wide() const {
         const int smem = (a.w + 4 * kWideThreads - 1) / (4 * kWideThreads) * 4 * kWideThreads * (int)sizeof(float);   // 64 KB at most
-        if (smem > 32 * 1024)
-            SGCN_CUDA(cudaFuncSetAttribute(norm_forward_wide_kernel<T, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        SGCN_CUDA(cudaFuncSetAttribute(norm_forward_wide_kernel<T, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem));
         norm_forward_wide_kernel<T, VEC><<<(unsigned)(a.n * a.p), kWideThreads, smem, st>>>(a, x, y, gate, h, u);
         return SLICEGCN_OK;
     }
@@ -1344,7 +1345,7 @@ struct BackwardCall {
     }
     template <bool VEC, int NV, bool BIAS, bool LAYER>
     slicegcn_status_t staged() const {
-        SGCN_CUDA(cudaFuncSetAttribute(norm_backward_staged_kernel<T, VEC, NV, BIAS, LAYER>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem));
+        SGCN_CUDA(cudaFuncSetAttribute(norm_backward_staged_kernel<T, VEC, NV, BIAS, LAYER>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStagedSmem));
         norm_backward_staged_kernel<T, VEC, NV, BIAS, LAYER><<<(unsigned)pl.ctas, pl.warps * 32, pl.smem, st>>>(a, y, gate, h, dh, du, dx, dy, dgate);
         return SLICEGCN_OK;
     }
