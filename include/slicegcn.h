@@ -485,7 +485,9 @@ slicegcn_status_t slicegcn_residual_norm_backward(const slicegcn_residual_norm_d
  * Global gradient norm over a list of tensors, and clipping by it:
  *   norm = sqrt(sum of the squares of all elements of all tensors)  (squares and sums in 64 bits, fixed order)
  *   dst[i] = src[i] * max_norm / norm   if norm > max_norm and norm is finite, else src[i]
- * A norm that is infinite or NaN leaves the gradients as they are; *norm_out says so.  Nothing is read back to the host.
+ * The comparison and the quotient are those of the 64-bit norm; *norm_out is that norm rounded to fp32 (infinity if it lies past
+ * fp32's range, which alone does not keep the gradients from being clipped).  A 64-bit norm that is infinite or NaN (a gradient
+ * is) leaves the gradients as they are, and *norm_out is then infinite or NaN too.  Nothing is read back to the host.
  */
 #define SLICEGCN_MAX_TENSORS 512
 typedef struct slicegcn_tensor_list {

@@ -39,3 +39,21 @@ def test_clusters_with_ctas_that_own_nothing(pieces):
     for out in outs:
         for a, b in zip(src, out):
             assert bool(((b.double() - 0.5 * a.double()).abs() <= 4 * U32 * a.double().abs()).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count", [1017, 2_000_001])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("size,max_norm", [(3e38, 1e-3), (3e38, 1e-5), (1e37, 1e-6), (1e30, 1e-20), (2.0, 1e-37)])
+def test_factors_below_the_normal_numbers(size, max_norm, dt, count):
+    """One rounding of the product, which may itself lie below the normal numbers (2^-149 apart)."""
+    import torch
+    src = torch.full((count,), size, device="cuda", dtype=torch.float32 if dt == "f32" else torch.bfloat16)
+    src[1::2] *= -0.37
+    true = math.sqrt(float(src.double().pow(2).sum()))
+    (out,), norm = (v[0] for v in _call([src], max_norm))
+    want = src.double() * (max_norm / true)
+    u = U32 if dt == "f32" else 2.0 ** -9
+    assert bool(((out.double() - want).abs() <= 2 * u * want.abs() + (2.0 ** -149 if dt == "f32" else 2.0 ** -133)).all())
+    assert bool((out != 0).any())
+    assert math.isinf(float(norm)) if true > 3.41e38 else abs(float(norm) - true) <= 2 * U32 * true
