@@ -1512,6 +1512,9 @@ slicegcn_status_t slicegcn_residual_norm_backward(const slicegcn_residual_norm_d
         SGCN_FAIL(SLICEGCN_ERR_ALLOC, "%s: workspace too small (%lld < %lld bytes)", who, (long long)workspace_bytes, (long long)need);
     if ((uintptr_t)workspace % 16) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "%s: the workspace is not aligned to 16 bytes", who);
     NormArgs a = make_args(d);
+    // the kernels take what is not there as zeros; weights beside it, which the caller may have left as they were, are left out too
+    if (!du) a.w_pre = a.b_pre = nullptr;
+    if (!y) a.w_post = a.b_post = nullptr;
     a.lanes_rows = pl.lanes_rows;
     a.whole_rows = pl.whole_rows;
     RowStats* stats = static_cast<RowStats*>(workspace);
