@@ -1203,7 +1203,7 @@ NormArgs make_args(const slicegcn_residual_norm_desc* d) {
     a.p = d->num_slices;
     a.w = d->h_s;
     a.layer = d->kind == SLICEGCN_ROWNORM_LAYER;
-    a.eps = (float)d->eps;
+    a.eps = std::max((float)d->eps, 1.17549435e-38f);   // the least normal number: a row of zeros is divided by its root
     a.s = (float)d->residual_scale;
     a.x_ld = d->x_ld, a.y_ld = d->y_ld, a.gate_ld = d->gate_ld, a.h_ld = d->h_ld, a.u_ld = d->u_ld;
     a.dh_ld = d->dh_ld, a.du_ld = d->du_ld, a.dx_ld = d->dx_ld, a.dy_ld = d->dy_ld, a.dgate_ld = d->dgate_ld;

@@ -1,4 +1,4 @@
-"""What a call leaves out has no say in it."""
+"""What a call leaves out has no say in it, and an eps below fp32's range is not zero."""
 import pytest
 
 WIDTHS = [(50, 4, 32), (50, 2, 13), (50, 1, 300), (40, 1, 1000), (9, 1, 3000)]
@@ -36,3 +36,23 @@ def test_weights_of_a_norm_that_a_call_does_not_take(n, p, w, kind):
     want = _backward(_desc(n, p, w, kind=kind, w_pre=good), None, None, h, dh, y)[0]
     got = _backward(_desc(n, p, w, kind=kind, w_pre=good, w_post=bad, b_post=bad), None, None, h, dh, y)[0]
     assert bool(torch.isfinite(got).all()) and torch.equal(got, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,p,w", WIDTHS)
+@pytest.mark.parametrize("kind", [0, 1], ids=["rms", "layer"])
+def test_rows_of_zeros_with_the_least_eps(n, p, w, kind):
+    """0 / sqrt(0 + eps) is 0 however small eps is."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    x, y = torch.randn((n, p * w), device="cuda"), torch.randn((n, p * w), device="cuda")
+    y[3], x[3] = 0.0, 0.0
+    y[5], x[5] = 2.0, 0.0
+    h, u = torch.empty_like(x), torch.empty_like(x)
+    d = _desc(n, p, w, kind=kind, eps=1e-60)
+    B.slicegcn_residual_norm_forward(d, x, y, None, h, u, torch.cuda.current_stream().cuda_stream)
+    assert bool((h[3] == 0).all()) and bool((u[3] == 0).all())
+    assert bool(torch.isfinite(h).all()) and bool(torch.isfinite(u).all())
+    zero = torch.zeros_like(x)
+    dx, dy = _backward(d, y, None, h, zero, zero)
+    assert bool((dx == 0).all()) and bool((dy == 0).all())
