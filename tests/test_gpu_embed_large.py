@@ -34,3 +34,60 @@ def test_as_many_ids_as_31_bits_hold():
     count = (n - torch.arange(vocab, device="cuda") + vocab - 1) // vocab
     first = torch.tensor([0, -2, -3, -3, -2], device="cuda")     # of the first c mod 5 values; five in a row add up to nothing
     assert torch.equal(got[:, 0], 2.0 * first[count % 5])
+
+
+# many positions per unit and per CTA, runs of the sort that are read again, three digits, ids over 2 to 16 CTAs of the sums and over more
+CASES = [(2_449_029, 2_449_029, 4, "own"), (2_449_029, 2_449_029, 7, "own"), (1_500_000, 300_007, 8, "zipf"), (2_000_003, 262_144, 16, "uniform"),
+         (2_449_029, 200_003, 100, "zipf"), (1_300_000, 2_000_000, 7, "zipf"), (300_000, 1_500_000, 33, "zipf"), (1_600_000, 5, 12, "uniform"),
+         (1_500_000, 100, 3, "uniform"), (1_250_000, 3, 32, "hub"), (160_000, 70_001, 131, "zipf"), (2_400_000, 40, 20, "runs"), (700_000, 1_000, 300, "zipf"),
+         (20_000, 2_000_000, 20, "zipf"), (100_000, 400_000, 131, "zipf"), (9_000, 500_000, 5, "uniform"), (30_001, 120_004, 130, "uniform"),
+         (8_192, 900_001, 33, "zipf"), (5_000, 300_000, 262, "zipf"), (1_000, 60_000, 1_433, "uniform"), (8, 1_000_003, 6, "uniform"), (0, 100_003, 9, "uniform"),
+         (70_000, 280_000, 1, "uniform"), (8_000, 40_000, 2, "zipf"), (17, 90_000, 3, "uniform")]
+
+
+def _ids(n, vocab, kind):
+    import math
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + vocab)
+    if kind == "own":
+        ids = torch.randperm(vocab, generator=g, device="cuda")[:n]
+    elif kind == "runs":                                   # every id as often, in order: sums of many CTAs each
+        ids = torch.arange(n, device="cuda") * vocab // n
+    else:
+        ids = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+        if kind == "zipf":
+            ids = torch.exp(torch.rand(n, generator=g, device="cuda", dtype=torch.float64) * math.log(vocab + 1.0)).long().sub_(1).clamp_(0, vocab - 1)
+            ids = (ids * 1_000_003 + 7) % vocab
+        if kind == "hub":
+            ids[torch.rand(n, generator=g, device="cuda") < 0.7] = vocab - 1
+        ids[torch.rand(n, generator=g, device="cuda") < 0.02] = -1
+    return ids.to(torch.int32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,vocab,width,kind", CASES)
+@pytest.mark.parametrize("gap,start", [(0, 0), (4, 0), (3, 1)], ids=["dense", "rows apart", "odd start"])
+def test_sums_are_exact(n, vocab, width, kind, gap, start):
+    """Overwriting and adding, in tables whose rows follow one another or lie apart; nothing outside the rows changes."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    ids = _ids(n, vocab, kind)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(width)
+    dout = torch.randint(-3, 4, (n, width), generator=g, device="cuda").float()
+    known = (ids >= 0).nonzero()[:, 0]
+    want = torch.zeros((vocab, width), device="cuda", dtype=torch.float64).index_add_(0, ids[known].long(), dout[known].double()).mul_(2.0)
+    big = torch.full((vocab * (width + gap) + start + 8,), 9.0, device="cuda")
+    table = big[start:start + vocab * (width + gap)].view(vocab, width + gap)[:, :width]
+    for accumulate in (False, True):
+        table.fill_(3.0 if accumulate else float("nan"))
+        d = B.make_embed_desc(n, vocab, width, scale=2.0, accumulate=accumulate, dtable_ld=width + gap)
+        wsb = B.slicegcn_embed_workspace_bytes(d)
+        ws = torch.randint(0, 256, (wsb,), dtype=torch.uint8, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        B.slicegcn_embed_backward(d, ids, dout, table, status, ws, wsb, torch.cuda.current_stream().cuda_stream)
+        assert torch.equal(table.double(), want + (3.0 if accumulate else 0.0)) and status.item() == 0
+        assert bool((big[:start] == 9).all()) and bool((big[start + vocab * (width + gap):] == 9).all())
+        if gap:
+            assert bool((big[start:start + vocab * (width + gap)].view(vocab, width + gap)[:, width:] == 9).all())
