@@ -112,6 +112,92 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(int64_t n, int64_t v
     }
 }
 
+// ---- rows of ids that do not occur ------------------------------------------------------------
+// They are cleared 32 at a time by a warp.  Rows that follow one another without a gap go in aligned 16-byte pieces, whatever their
+// width (8 ids of 1,900,000 x 131: 426 us element by element, 156 us so); rows that lie apart one by one.
+struct RowClear {
+    float* table;
+    int64_t ld;
+    int width, lane;
+    bool pieces;                      // rows of four columns and more, without gaps: a piece lies in two of them at most
+    int lead;                         // elements before a block's first piece: the same for all blocks, which lie 128 width bytes apart
+    int row, col, row_step, col_step; // where the lane's first piece starts in a block, and how far its next one is
+    // blocks start `row0` and multiples of 32 rows from there on
+    __device__ __forceinline__ RowClear(float* t, int64_t ld_, int width_, int64_t row0)
+        : table(t), ld(ld_), width(width_), lane(threadIdx.x & 31), pieces(ld_ == width_ && width_ >= 4) {
+        lead = (int)(-(int64_t)((uintptr_t)(t + row0 * ld_) >> 2) & 3);
+        const int e = lead + 4 * lane;
+        row = e / width, col = e - row * width;
+        row_step = 128 / width, col_step = 128 - row_step * width;
+    }
+    // rows v .. v + rows - 1 (32 at most), those whose bit is set
+    __device__ __forceinline__ void block(int64_t v, int rows, uint32_t absent) const {
+        if (!absent) return;
+        float* const from = table + v * ld;
+        if (pieces) {
+            const int count = rows * width, whole = (count - lead) / 4, loose = count - 4 * whole;   // lead <= 3 < width
+            if (lane < loose) {
+                const int e = lane < lead ? lane : 4 * whole + lane;
+                if (absent >> (e < width ? 0 : rows - 1) & 1u) from[e] = 0.f;   // of the first row or the last
+            }
+            const bool all = absent == 0xffffffffu >> (32 - rows);
+            int r = row, c = col;
+            for (int k = lane; k < whole; k += 32) {
+                float* const to = from + lead + 4 * k;
+                const bool here = all || absent >> r & 1u, next = c + 4 > width ? all || absent >> (r + 1) & 1u : here;
+                if (here && next) {
+                    *reinterpret_cast<float4*>(to) = make_float4(0.f, 0.f, 0.f, 0.f);
+                } else if (here || next) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (c + j < width ? here : next) to[j] = 0.f;
+                }
+                r += row_step, c += col_step;
+                if (c >= width) c -= width, ++r;
+            }
+            return;
+        }
+        const bool fours = width % 4 == 0 && ld % 4 == 0 && (uintptr_t)table % 16 == 0;
+        const int per = fours ? 4 : 1;
+        int group = 1;
+        while (group < 32 && group * per < width) group *= 2;
+        for (int r = lane / group; r < rows; r += 32 / group) {
+            if (!(absent >> r & 1u)) continue;
+            for (int c = (lane & (group - 1)) * per; c < width; c += group * per) {
+                if (fours)
+                    *reinterpret_cast<float4*>(from + r * ld + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+                else
+                    from[r * ld + c] = 0.f;
+            }
+        }
+    }
+};
+// The whole table, by CTAs that stand beside those of the sort's launches (below): a share of the rows per launch.
+struct ClearShare {
+    float* table;
+    int64_t ld;
+    int width;
+    int64_t rows, row0, rows_per_cta;   // of the table; first of this launch; of a CTA (a multiple of 32)
+};
+__device__ __forceinline__ void clear_share(const ClearShare& c, int cta) {
+    const int64_t r0 = c.row0 + cta * c.rows_per_cta, r1 = min(c.rows, r0 + c.rows_per_cta);
+    if (r0 >= r1) return;
+    if (c.ld == c.width) {   // a span
+        float* const from = c.table + r0 * c.width;
+        const int64_t count = (r1 - r0) * c.width, lead = min(count, -(int64_t)((uintptr_t)from >> 2) & 3), whole = (count - lead) / 4;
+        for (int64_t k = threadIdx.x; k < whole; k += blockDim.x)
+            *reinterpret_cast<float4*>(from + lead + 4 * k) = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (threadIdx.x < lead) from[threadIdx.x] = 0.f;
+        if (lead + 4 * whole + threadIdx.x < count) from[lead + 4 * whole + threadIdx.x] = 0.f;
+        return;
+    }
+    const RowClear rows(c.table, c.ld, c.width, r0);
+    for (int64_t v = r0 + threadIdx.x / 32 * 32; v < r1; v += blockDim.x) {
+        const int n = (int)min((int64_t)32, r1 - v);
+        rows.block(v, n, 0xffffffffu >> (32 - n));
+    }
+}
+
 // ---- stable sort of the ids -------------------------------------------------------------------
 // Keys run from 0 to `vocab`: the id, or `vocab` (sorted last) for positions that take no part.  Per digit two launches:
 // sort_count_kernel counts every tile's digits, sort_scatter_kernel turns the counts into offsets (each CTA reads the whole
@@ -136,7 +222,8 @@ struct SortArgs {
     const uint2* in;         // (key, position), read by the others
     uint2* out;
     uint32_t* counts;        // [tiles][bins]
-    uint8_t* present;        // [vocab] cleared by the first count, see SumArgs
+    uint8_t* present;        // [vocab] cleared by the first count, see SumArgs; NULL: not wanted
+    ClearShare clear;        // for the CTAs past the tiles
     int32_t* status;
     int shift, bits, tiles;
     int32_t tile;            // positions per tile, a multiple of kSortWarps * 32
@@ -151,8 +238,14 @@ __device__ __forceinline__ uint2 sort_load(const SortArgs& a, int32_t i) {
 template <bool FIRST>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
     __shared__ uint32_t hist[1 << kMaxDigitBits];
-    if (FIRST)
-        for (int64_t i = (blockIdx.x * (int64_t)kSortThreads + threadIdx.x) * 16; i < a.vocab; i += (int64_t)gridDim.x * kSortThreads * 16)
+    if ((int)blockIdx.x >= a.tiles) {
+        cudaTriggerProgrammaticLaunchCompletion();
+        if (!FIRST) cudaGridDependencySynchronize();
+        clear_share(a.clear, blockIdx.x - a.tiles);
+        return;
+    }
+    if (FIRST && a.present)
+        for (int64_t i = (blockIdx.x * (int64_t)kSortThreads + threadIdx.x) * 16; i < a.vocab; i += (int64_t)a.tiles * kSortThreads * 16)
             *reinterpret_cast<uint4*>(a.present + i) = make_uint4(0, 0, 0, 0);   // (rounded up to 16 bytes)
     if (threadIdx.x < 1 << kMaxDigitBits) hist[threadIdx.x] = 0;
     __syncthreads();
@@ -178,6 +271,12 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     __shared__ uint4 part_before[kSortThreads], part_total[kSortThreads];   // [part][bins / 4]
     __shared__ uint32_t warp_total[kSortWarps];
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    if ((int)blockIdx.x >= a.tiles) {
+        cudaTriggerProgrammaticLaunchCompletion();
+        cudaGridDependencySynchronize();
+        clear_share(a.clear, blockIdx.x - a.tiles);
+        return;
+    }
     const int bins = 1 << a.bits;
     const uint32_t mask = (uint32_t)bins - 1u;
     uint32_t* mine = next + w * bins;
@@ -283,7 +382,7 @@ struct SumArgs {
     int64_t dtable_ld;
     float scale;
     uint8_t* present;        // [vocab] set where an id occurs: once per run and unit, as setting it per position would
-                             // queue the positions of a frequent id up on one byte (200 us for 2.4 M positions)
+                             // queue the positions of a frequent id up on one byte (200 us for 2.4 M positions); NULL: not wanted
     int32_t per_unit;        // R
     int sum_ctas;
     float* head;             // [sum_ctas][width] sum of the id that comes in from the CTA before
@@ -291,18 +390,17 @@ struct SumArgs {
     int4* info;              // [sum_ctas] {head present, head ends here, tail present, tail's id}
 };
 
-// Four columns of a row on their way to shared memory, asynchronously; then from there.  A thread reads back only what it
-// asked for itself, so its own count of finished copies is all the waiting there is.
-template <bool VEC>
-__device__ __forceinline__ void request4(uint32_t slot, const float* row, int col, int stride, int width) {
-    if (VEC) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot), "l"(row + col) : "memory");
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (col + j * stride < width)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(slot + 4 * j), "l"(row + col + j * stride) : "memory");
-    }
+// Asynchronous copies to shared memory.
+__device__ __forceinline__ void copy_async16(uint32_t to, const float* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async16_if(bool wanted, uint32_t to, const float* from) {
+    asm volatile("{.reg .pred p; setp.ne.u32 p, %2, 0; @p cp.async.cg.shared.global [%0], [%1], 16;}" ::"r"(to), "l"(from),
+                 "r"((uint32_t)wanted)
+                 : "memory");
+}
+__device__ __forceinline__ void copy_async4(uint32_t to, const float* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
 template <bool VEC>
 __device__ __forceinline__ void store4(float* row, int col, int stride, int width, int accumulate, const float (&v)[4]) {
@@ -322,12 +420,21 @@ __device__ __forceinline__ void store4(float* row, int col, int stride, int widt
 
 constexpr int kJoin = 4;   // units that one thread joins per column: all threads of the CTA share the first half of the joining
 
-// Shared memory of a CTA that sums.
+// The rows on their way: ROWS per unit, which are also the positions of a batch.  Every thread copies and reads back its own four
+// columns, so its own count of finished copies is all the waiting there is; but narrow rows that allow no accesses of 16 bytes
+// (SHARED) are copied as the aligned 16 bytes that hold them, one piece more than there are lanes, and read by all lanes of the
+// unit: element by element the copies alone paced the kernel (2,449,029 x 11, an id each: 281 and 226 us).  Wide ones go element
+// by element: a copy is then 64 to 128 bytes long, and finding the row in its pieces costs more (600,000 x 131: 169 and 237 us).
+template <int L, bool VEC>
+struct RowRing {
+    static constexpr bool SHARED = !VEC && L <= 8;
+    static constexpr int ROWS = !SHARED ? kAhead : L == 8 ? 7 : 4;
+    float4 at[ROWS][kSumThreads / L][SHARED ? L + 1 : L];   // 32 KB at most
+};
+// Shared memory of a CTA that sums, beside them.
 template <int L>
 struct SumShared {
     static constexpr int U = kSumThreads / L;
-    static constexpr int A = L < kAhead ? L : kAhead;   // rows on their way at any time, and positions per batch
-    float4 ring[A][kSumThreads];
     float sums[U][2][4 * L];
     int4 unit_info[U];            // {head present, head ends here, tail's id or -1, unused}
     int4 part_info[U / kJoin];    // the same for kJoin units each
@@ -341,17 +448,62 @@ struct PairsInMemory {
 constexpr int kSmallBits = 13, kSmallN = 1 << kSmallBits;
 struct PairsInShared {
     const uint32_t* p;
-    uint32_t first_id;
+    uint32_t first_id, step;   // the ids of a CTA
     __device__ __forceinline__ uint2 operator()(uint32_t i) const {
-        return make_uint2((p[i] >> kSmallBits) + first_id, p[i] & (kSmallN - 1));
+        return make_uint2((p[i] >> kSmallBits) * step + first_id, p[i] & (kSmallN - 1));
     }
 };
+
+// The sums of N units (the info and the sums of every stride-th) in one column, joined in order: ids that end inside go to the table.
+struct Joined {
+    float head, tail;
+    bool any_head, ended;
+    int id;   // of the tail, or -1
+};
+template <int N, int W>
+__device__ __forceinline__ Joined join_units(const SumArgs& a, const int4* info, const float (*sums)[2][W], int stride, int c, int table_col) {
+    auto write = [&](int to, float v) {
+        float* t = a.dtable + (int64_t)to * a.dtable_ld + table_col;
+        *t = v + (a.accumulate ? *t : 0.f);
+    };
+    Joined r{0.f, 0.f, false, false, -1};
+    float sum = 0.f;
+    bool open = false, started = false;
+    int id = -1;
+    constexpr int M = N < 4 ? N : 4;   // four on their way at a time
+#pragma unroll 1
+    for (int k0 = 0; k0 < N; k0 += M) {
+        int4 f[M];
+        float hs[M], ts[M];
+#pragma unroll
+        for (int k = 0; k < M; ++k) f[k] = info[k0 + k], hs[k] = sums[(k0 + k) * stride][0][c], ts[k] = sums[(k0 + k) * stride][1][c];
+#pragma unroll
+        for (int k = 0; k < M; ++k) {
+            if (f[k].x) {
+                if (!open) open = true, started = false, sum = 0.f, r.any_head = true;
+                sum += hs[k];
+                if (f[k].y) {
+                    if (started)
+                        write(id, sum);
+                    else
+                        r.head = sum, r.ended = true;
+                    open = false;
+                }
+            }
+            if (f[k].z >= 0) open = true, started = true, sum = ts[k], id = f[k].z;
+        }
+    }
+    if (open && started) r.tail = sum, r.id = id;
+    if (open && !started) r.head = sum;
+    return r;
+}
 
 // One CTA's share: positions cta * U * per_unit and on, of n.  ONE: the CTA holds all positions of its ids.
 // VEC: lane l holds columns 4 l .. 4 l + 3 of the tile (16-byte accesses); else columns l, l + L, l + 2 L, l + 3 L
 template <int L, bool VEC, bool ONE, typename Pairs>
-__device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, int n, int per_unit, int cta, SumShared<L>& sh) {
-    constexpr int U = SumShared<L>::U, A = SumShared<L>::A;
+__device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, int n, int per_unit, int cta, SumShared<L>& sh, RowRing<L, VEC>& ring) {
+    constexpr int U = SumShared<L>::U, A = RowRing<L, VEC>::ROWS;
+    constexpr bool SHARED = RowRing<L, VEC>::SHARED;
     const int tid = threadIdx.x, l = tid & (L - 1), unit = tid / L;
     const int c0 = blockIdx.y * 4 * L;
     const int col = c0 + (VEC ? 4 * l : l);
@@ -359,10 +511,11 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
     const int64_t s64 = ((int64_t)cta * U + unit) * per_unit;
     // unsigned: what is asked for ahead of the last of 2^31 - 1 positions lies past 31 bits
     const uint32_t s = (uint32_t)min((int64_t)n, s64), e = (uint32_t)min((int64_t)n, s64 + per_unit);
-    const unsigned group = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((tid & 31) & ~(L - 1));
     const uint32_t none = (uint32_t)a.vocab;
     const uint32_t before = s > 0 && s < e ? pairs(s - 1).x : 0xffffffffu;
-    const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(&sh.ring[0][tid]);
+    const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(&ring.at[0][unit][SHARED ? 0 : l]);
+    const int count = min(4 * L, a.width - c0);   // columns of the tile
+    uint32_t offs = 0;                            // where the rows on their way start in their first 16 bytes, two bits each
     uint32_t key = 0xffffffffu;
     bool first = true;             // still in the unit's first run
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
@@ -379,7 +532,7 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
             put(0);
             return;
         }
-        if (!ONE && l == 0 && blockIdx.y == 0) a.present[key] = 1;
+        if (!ONE && a.present && l == 0 && blockIdx.y == 0) a.present[key] = 1;
         if (goes_on) {
             tail_id = (int)key;
             put(1);
@@ -387,42 +540,101 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
             store4<VEC>(a.dtable + (int64_t)key * a.dtable_ld, col, L, a.width, a.accumulate, acc);
         }
     };
-    auto batch = [&](uint32_t b) { return l < A && b + l < e ? pairs(b + l) : make_uint2(none, 0); };
-    auto request = [&](int i, const uint2& p) {   // row i of a batch into slot i
-        const uint32_t k = __shfl_sync(group, p.x, i, L), pos = __shfl_sync(group, p.y, i, L);
-        if (live_col && k < none)
-            request4<VEC>(my_ring + i * (int)sizeof(sh.ring[0]), a.dout + (int64_t)pos * a.dout_ld, col, L, a.width);
+    constexpr int Q = L < A ? A / L : 1;   // positions of a batch that a lane holds
+    struct Batch {
+        uint2 p[Q];
+    };
+    auto batch = [&](uint32_t b) {
+        Batch t;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            t.p[q] = l < A && b + q * L + l < e ? pairs(b + q * L + l) : make_uint2(none, 0);
+            if (t.p[q].x >= none) t.p[q].y = 0xffffffffu;
+        }
+        return t;
+    };
+    auto request = [&](int i, const Batch& t) {   // row i of a batch into slot i
+        const uint32_t pos = __shfl_sync(0xffffffffu, t.p[i / L].y, i % L, L);
+        const uint32_t slot = my_ring + i * (int)sizeof(ring.at[0]);
+        const float* row = a.dout + (int64_t)pos * a.dout_ld + c0;
+        if constexpr (SHARED) {
+            const int off = (int)((uintptr_t)row >> 2 & 3), pieces = pos != 0xffffffffu ? (off + count + 3) / 4 : 0;
+            offs = offs & ~(3u << 2 * i) | (uint32_t)off << 2 * i;
+            if (pos - 3u < (uint32_t)a.n - 6u && a.n > 6 || pos == 0xffffffffu) {
+                copy_async16_if(l < pieces, slot + 16 * l, row - off + 4 * l);
+                copy_async16_if(l + L < pieces, slot + 16 * (l + L), row - off + 4 * (l + L));
+            } else {   // beside the first and the last rows there need not be anything
+                for (int q = l; q < count; q += L) copy_async4(slot + 4 * (off + q), row + q);
+            }
+        } else if (live_col && pos != 0xffffffffu) {
+            if constexpr (VEC) {
+                copy_async16(slot, row + 4 * l);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (l + j * L < count) copy_async4(slot + 4 * j, row + l + j * L);
+            }
+        }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    uint2 cur = batch(s), next = batch(s + A);
+    Batch cur = batch(s), next = batch(s + A);
+    // a shared slot is filled again two steps after it was read: a barrier of the warp lies between
+    constexpr int AHEAD = SHARED ? A - 2 : A - 1;
 #pragma unroll
-    for (int i = 0; i < A - 1; ++i) request(i, cur);
-    for (uint32_t b = s; b < e; b += A) {
-        const uint2 later = batch(b + 2 * A);
-#pragma unroll
-        for (int i = 0; i < A; ++i) {
-            // the slot read in the step before is free: the last row of this batch, then the next batch's rows
-            if (i == 0)
-                request(A - 1, cur);
+    for (int i = 0; i < AHEAD; ++i) request(i, cur);
+    // All units of a warp go as many rounds, whether or not theirs is a short one: shuffles of a part of the warp take an instruction
+    // each to keep its lanes in step, and its unit was three quarters busy with units of two lanes.
+    const int rounds = (per_unit + A - 1) / A;
+    uint32_t b = s;
+    for (int r = 0; r < rounds; ++r, b += A) {
+        const Batch later = batch(b + 2 * A);
+        // row i of the batch is waited for; the one AHEAD of it, of this batch or the next, is asked for
+        auto arrive = [&](int i) {
+            if (i + AHEAD < A)
+                request(i + AHEAD, cur);
             else
-                request(i - 1, next);
-            if (b + i >= e) continue;
-            asm volatile("cp.async.wait_group %0;" ::"n"(A - 1) : "memory");
-            const uint32_t k = __shfl_sync(group, cur.x, i, L);
-            if (k != key) {
-                if (key != 0xffffffffu) {
-                    finish(false);
-                    first = false;
-                }
-                key = k;
-                acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
-            }
-            if (live_col && k < none) {
-                const float4 v = sh.ring[i][tid];
+                request(i + AHEAD - A, next);
+            asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+            if (SHARED) __syncwarp();
+        };
+        auto add = [&](int i) {
+            if constexpr (SHARED) {
+                const float* row = reinterpret_cast<const float*>(ring.at[i][unit]) + (offs >> 2 * i & 3);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (l + j * L < count) acc[j] = fmaf(a.scale, row[l + j * L], acc[j]);
+            } else {
+                const float4 v = ring.at[i][unit][l];
                 acc[0] = fmaf(a.scale, v.x, acc[0]);
-                if (VEC || col + L < a.width) acc[1] = fmaf(a.scale, v.y, acc[1]);
-                if (VEC || col + 2 * L < a.width) acc[2] = fmaf(a.scale, v.z, acc[2]);
-                if (VEC || col + 3 * L < a.width) acc[3] = fmaf(a.scale, v.w, acc[3]);
+                if (VEC || l + L < count) acc[1] = fmaf(a.scale, v.y, acc[1]);
+                if (VEC || l + 2 * L < count) acc[2] = fmaf(a.scale, v.z, acc[2]);
+                if (VEC || l + 3 * L < count) acc[3] = fmaf(a.scale, v.w, acc[3]);
+            }
+        };
+        bool going_on = b + A <= e && key < none;   // the whole batch belongs to the run (frequent ids): no row needs a look at its id
+#pragma unroll
+        for (int q = 0; q < Q; ++q) going_on = going_on && (l >= A || cur.p[q].x == key);
+        if (__all_sync(0xffffffffu, going_on)) {
+#pragma unroll
+            for (int i = 0; i < A; ++i) {
+                arrive(i);
+                if (live_col) add(i);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < A; ++i) {
+                arrive(i);
+                const uint32_t k = __shfl_sync(0xffffffffu, cur.p[i / L].x, i % L, L);
+                if (b + i >= e) continue;
+                if (k != key) {
+                    if (key != 0xffffffffu) {
+                        finish(false);
+                        first = false;
+                    }
+                    key = k;
+                    acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+                }
+                if (live_col && k < none) add(i);
             }
         }
         cur = next;
@@ -433,57 +645,19 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
     if (l == 0) sh.unit_info[unit] = make_int4(head, head_ends, tail_id, 0);
     __syncthreads();
     // The units' sums are joined in order: first kJoin units per thread and column, then those results by one thread per column.
-    auto write = [&](int to, int c, float v) {
-        float* t = a.dtable + (int64_t)to * a.dtable_ld + c0 + c;
-        *t = v + (a.accumulate ? *t : 0.f);
-    };
-    struct Joined {
-        float head, tail;
-        bool any_head, ended;
-        int id;   // of the tail, or -1
-    };
-    auto join = [&](auto count, const int4* info, int first, int stride, int c) {
-        Joined r{0.f, 0.f, false, false, -1};
-        float sum = 0.f;
-        bool open = false, started = false;
-        int id = -1;
-        constexpr int N = decltype(count)::value;
-        int4 f[N];
-        float hs[N], ts[N];
-#pragma unroll
-        for (int k = 0; k < N; ++k) f[k] = info[k], hs[k] = sh.sums[first + k * stride][0][c], ts[k] = sh.sums[first + k * stride][1][c];
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            if (f[k].x) {
-                if (!open) open = true, started = false, sum = 0.f, r.any_head = true;
-                sum += hs[k];
-                if (f[k].y) {
-                    if (started)
-                        write(id, c, sum);
-                    else
-                        r.head = sum, r.ended = true;
-                    open = false;
-                }
-            }
-            if (f[k].z >= 0) open = true, started = true, sum = ts[k], id = f[k].z;
-        }
-        if (open && started) r.tail = sum, r.id = id;
-        if (open && !started) r.head = sum;
-        return r;
-    };
     constexpr int W = 4 * L, P = U / kJoin;   // columns of the tile, first results
     {
         const int c = tid % W, g = tid / W;   // W * P threads: all of them
         const bool inside = c0 + c < a.width;
         Joined r{0.f, 0.f, false, false, -1};
-        if (inside) r = join(std::integral_constant<int, kJoin>{}, sh.unit_info + g * kJoin, g * kJoin, 1, c);
+        if (inside) r = join_units<kJoin, W>(a, sh.unit_info + g * kJoin, sh.sums + g * kJoin, 1, c, c0 + c);
         __syncthreads();
         if (inside) sh.sums[g * kJoin][0][c] = r.head, sh.sums[g * kJoin][1][c] = r.tail;
         if (c == 0) sh.part_info[g] = make_int4(r.any_head, r.ended, r.id, 0);
     }
     __syncthreads();
     if (tid >= W || c0 + tid >= a.width) return;
-    const Joined r = join(std::integral_constant<int, P>{}, sh.part_info, 0, kJoin, tid);
+    const Joined r = join_units<P, W>(a, sh.part_info, sh.sums, kJoin, tid, c0 + tid);
     if (ONE) return;
     if (r.id >= 0) a.tail[(int64_t)cta * a.width + c0 + tid] = r.tail;
     if (r.any_head) a.head[(int64_t)cta * a.width + c0 + tid] = r.head;
@@ -493,31 +667,250 @@ __device__ __forceinline__ void sum_sorted(const SumArgs& a, const Pairs pairs, 
 template <int L, bool VEC>
 __global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_kernel(const SumArgs a) {
     __shared__ SumShared<L> sh;
+    __shared__ RowRing<L, VEC> ring;
     cudaTriggerProgrammaticLaunchCompletion();
     cudaGridDependencySynchronize();
-    sum_sorted<L, VEC, false>(a, PairsInMemory{a.pairs}, a.n, a.per_unit, blockIdx.x, sh);
+    sum_sorted<L, VEC, false>(a, PairsInMemory{a.pairs}, a.n, a.per_unit, blockIdx.x, sh, ring);
 }
 
-// Small problems (up to kSmallN positions): one launch.  Every CTA owns a stretch of the table, picks the positions of its ids
-// out of all of them, sorts those in shared memory and sums them as above; nothing passes between CTAs.
+// Rows of up to eight columns: a lane takes a whole row, a warp 32 sorted positions at a time, and the rows of one id are added by
+// shuffles.  Neighbouring ids are stored together, where a unit of two lanes stores one row of 32 bytes or less at a time (28
+// instead of 54 us for 2,449,029 x 4, an id each).  Rows that allow no wide accesses are read as the aligned 16 bytes that hold
+// them; the first and the last rows of dout, beside which there need not be anything, element by element.
+constexpr int kNarrow = 8, kNarrowUnits = kSumThreads / 32;
+template <int NW, bool VEC>
+struct NarrowRow {
+    static constexpr int C = VEC ? NW / 4 : NW / 4 + 1;
+    float4 part[C];
+    int off;   // where the row starts in the first part
+    __device__ __forceinline__ void load(const SumArgs& a, uint32_t pos, bool wanted) {
+        const float* row = a.dout + (int64_t)pos * a.dout_ld;
+        off = VEC ? 0 : (int)((uintptr_t)row >> 2 & 3);
+        const bool edge = !VEC && (pos < 3 || pos + 3 >= (uint32_t)a.n);
+        if (edge) off = 0;
+#pragma unroll
+        for (int q = 0; q < C; ++q) {
+            part[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (edge) {
+                if (wanted && 4 * q < a.width) part[q].x = row[4 * q];
+                if (wanted && 4 * q + 1 < a.width) part[q].y = row[4 * q + 1];
+                if (wanted && 4 * q + 2 < a.width) part[q].z = row[4 * q + 2];
+                if (wanted && 4 * q + 3 < a.width) part[q].w = row[4 * q + 3];
+            } else if (wanted && 4 * q < off + a.width) {
+                part[q] = __ldg(reinterpret_cast<const float4*>(row - off + 4 * q));
+            }
+        }
+    }
+    __device__ __forceinline__ void get(float scale, int width, float (&v)[NW]) const {
+        float w[4 * C];
+#pragma unroll
+        for (int q = 0; q < C; ++q) w[4 * q] = part[q].x, w[4 * q + 1] = part[q].y, w[4 * q + 2] = part[q].z, w[4 * q + 3] = part[q].w;
+        if (!VEC) {
+#pragma unroll
+            for (int j = 0; j + 1 < 4 * C; ++j) w[j] = off & 1 ? w[j + 1] : w[j];
+#pragma unroll
+            for (int j = 0; j + 2 < 4 * C; ++j) w[j] = off & 2 ? w[j + 2] : w[j];
+        }
+#pragma unroll
+        for (int j = 0; j < NW; ++j) v[j] = j < width ? scale * w[j] : 0.f;
+    }
+};
+template <int NW, bool VEC>
+__global__ void __launch_bounds__(kSumThreads, kSumPerSM) embed_sum_narrow_kernel(const SumArgs a) {
+    __shared__ float sums[kNarrowUnits][2][kNarrow];
+    __shared__ int4 unit_info[kNarrowUnits];
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
+    const int lane = threadIdx.x & 31, unit = threadIdx.x >> 5;
+    const int64_t s64 = ((int64_t)blockIdx.x * kNarrowUnits + unit) * a.per_unit;
+    const uint32_t s = (uint32_t)min((int64_t)a.n, s64), e = (uint32_t)min((int64_t)a.n, s64 + a.per_unit);
+    const uint32_t none = (uint32_t)a.vocab;
+    auto store_row = [&](uint32_t key, const float(&v)[NW]) {
+        float* row = a.dtable + (int64_t)key * a.dtable_ld;
+        if (a.present) a.present[key] = 1;
+        if (VEC) {
+#pragma unroll
+            for (int q = 0; q < NW / 4; ++q)
+                if (4 * q < a.width) {
+                    float4 t = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                    float4* to = reinterpret_cast<float4*>(row + 4 * q);
+                    if (a.accumulate) t.x += to->x, t.y += to->y, t.z += to->z, t.w += to->w;
+                    *to = t;
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NW; ++j)
+                if (j < a.width) row[j] = v[j] + (a.accumulate ? row[j] : 0.f);
+        }
+    };
+    auto pair = [&](uint32_t i) { return i < e ? a.pairs[i] : make_uint2(0xffffffffu, 0u); };
+    // The run that comes in from the 32 positions before, or from the unit before (then it is the unit's head, and empty so far).
+    uint32_t carry_key = s > 0 && s < e ? a.pairs[s - 1].x : 0xfffffffeu;
+    bool carry_head = true, carry_any = false;
+    float carry[NW];
+#pragma unroll
+    for (int j = 0; j < NW; ++j) carry[j] = 0.f;
+    bool head = false, head_ends = false;
+    int tail_id = -1;
+    auto finish_carry = [&](bool goes_on) {
+        if (!carry_any || carry_key >= none) return;
+        if (carry_head || goes_on) {
+            if (lane == 0)
+#pragma unroll
+                for (int j = 0; j < NW; ++j) sums[unit][carry_head ? 0 : 1][j] = carry[j];
+            if (carry_head) {
+                head = true, head_ends = !goes_on;
+            } else {
+                tail_id = (int)carry_key;
+                if (a.present && lane == 0) a.present[carry_key] = 1;
+            }
+        } else if (lane == 0) {
+            store_row(carry_key, carry);
+        }
+    };
+    uint2 p = pair(s + lane), next = pair(s + 32 + lane);
+    NarrowRow<NW, VEC> row, next_row;
+    row.load(a, p.y, p.x < none);
+    for (uint32_t b = s; b < e; b += 32) {
+        const uint2 later = pair(b + 64 + lane);
+        next_row.load(a, next.y, next.x < none);
+        float v[NW];
+        row.get(a.scale, a.width, v);
+        uint32_t before = __shfl_up_sync(0xffffffffu, p.x, 1);
+        if (lane == 0) before = carry_key;
+        const uint32_t starts = __ballot_sync(0xffffffffu, p.x != before);
+        if (starts & 1u) finish_carry(false);
+        const int from = 31 - __clz(starts & (0xffffffffu >> (31 - lane)));   // the run's first lane here, -1: it came in
+        if (starts != 0xffffffffu) {
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const bool same = lane - o >= max(from, 0);
+#pragma unroll
+                for (int j = 0; j < NW; ++j) {
+                    const float t = __shfl_up_sync(0xffffffffu, v[j], o);
+                    v[j] += same ? t : 0.f;
+                }
+            }
+            if (from < 0)
+#pragma unroll
+                for (int j = 0; j < NW; ++j) v[j] += carry[j];
+        }
+        const int last = (int)min(31u, e - 1 - b);   // the last lane's run stays open
+        const bool ends = lane < last && starts >> (lane + 1) & 1u && p.x < none;
+        const bool is_head = ends && from < 0 && carry_head;
+        if (__ballot_sync(0xffffffffu, is_head)) head = head_ends = true;
+        if (is_head) {
+#pragma unroll
+            for (int j = 0; j < NW; ++j) sums[unit][0][j] = v[j];
+        } else if (ends) {
+            store_row(p.x, v);
+        }
+        carry_head = carry_head && __shfl_sync(0xffffffffu, from, last) < 0;
+        carry_key = __shfl_sync(0xffffffffu, p.x, last);
+        carry_any = true;
+#pragma unroll
+        for (int j = 0; j < NW; ++j) carry[j] = __shfl_sync(0xffffffffu, v[j], last);
+        p = next;
+        next = later;
+        row = next_row;
+    }
+    if (s < e) finish_carry(e < (uint32_t)a.n && a.pairs[e].x == carry_key);
+    if (lane == 0) unit_info[unit] = make_int4(head, head_ends, tail_id, 0);
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c >= a.width) return;
+    const Joined r = join_units<kNarrowUnits, kNarrow>(a, unit_info, sums, 1, c, c);
+    if (r.id >= 0) a.tail[(int64_t)blockIdx.x * a.width + c] = r.tail;
+    if (r.any_head) a.head[(int64_t)blockIdx.x * a.width + c] = r.head;
+    if (c == 0) a.info[blockIdx.x] = make_int4(r.any_head, r.ended, r.id >= 0, r.id);
+}
+
+// Small problems (up to kSmallN positions): one launch that sums.  Every CTA owns every gridDim.x-th row of the table (frequent ids
+// often lie next to each other: with a stretch of the table each, one CTA had half of the positions), picks the positions of its
+// ids out of all of them, sorts those in shared memory and sums them as above; nothing passes between CTAs.
 constexpr int kSmallRows = 1 << 16;   // rows of the table per CTA at most
 template <int L>
 struct SmallShared {
     SumShared<L> sum;
-    uint32_t list[2][kSmallN];
+    alignas(16) uint32_t list[2][kSmallN];   // one of them holds the rows on their way later: two CTAs fit an SM
+    static_assert(sizeof(RowRing<L, true>) <= kSmallN * sizeof(uint32_t) && sizeof(RowRing<L, false>) <= kSmallN * sizeof(uint32_t));
     uint32_t next[8][256];
     uint32_t warp_total[8];
     uint32_t before[kSmallN / kSumThreads][8];
     uint32_t present[kSmallRows / 32];
 };
+// Tables of more rows, or bytes, than these take a launch of their own for it; smaller ones are cleared by the CTAs that sum, row by
+// row (2,000 ids x 7 of 286,000 / 1,143,000 rows: 14 / 35 us row by row, 17 / 20 us apart; x 128, 32 / 64 MB: 14 / 18 and 21 / 23 us;
+// x 100, 800 MB: 297 and 133 us).
+constexpr int64_t kApartRows = 1 << 19, kApartBytes = 64 << 20;
+// Rows without an id of a table that is large beside so few ids.  Every CTA marks which of its rows occur while the launch that sums
+// (and writes the rows that occur) is at work, and clears the others when that has ended: reads between so many stores would wait
+// long, and slow them (8,000 ids of 1,900,000 x 131: 203 us side by side, 186 one after the other).  The CTAs' rows are dealt out
+// in chunks, so that all write to one neighbourhood at a time, and eight CTAs per SM even out who started late (6.6 TB/s; 5.6 with a
+// stretch of the table for each of two per SM).  chunk: blocks of 32 rows, 1 .. kClearWarps.
+constexpr int kClearThreads = 512, kClearWarps = kClearThreads / 32, kClearCtas = 8 * kSMs;
+__global__ void __launch_bounds__(kClearThreads) embed_clear_kernel(const SumArgs a, const int32_t* ids, int chunk) {
+    extern __shared__ uint32_t occurs[];   // [chunks of this CTA][chunk]
+    const int first = (int)(4 * threadIdx.x + (-((uintptr_t)a.dtable >> 2) & 3));   // element of a chunk where the thread's first piece starts
+    const int first_row = first / a.width, first_col = first - first_row * a.width;
+    const int row_step = 4 * kClearThreads / a.width, col_step = 4 * kClearThreads - row_step * a.width;
+    const uint32_t blocks = (uint32_t)((a.vocab + 31) / 32), chunks = (blocks + chunk - 1) / chunk;
+    const int mine = (int)((chunks - blockIdx.x + gridDim.x - 1) / gridDim.x);
+    for (int k = threadIdx.x; k < mine * chunk; k += kClearThreads) occurs[k] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = threadIdx.x; i < a.n; i += kClearThreads) {
+        const uint32_t id = (uint32_t)ids[i], of = id / 32 / chunk, turn = of / gridDim.x;
+        if (id < (uint32_t)a.vocab && of - turn * gridDim.x == blockIdx.x) atomicOr(&occurs[turn * chunk + id / 32 % chunk], 1u << (id & 31));
+    }
+    __syncthreads();
+    cudaGridDependencySynchronize();
+    const RowClear clear(a.dtable, a.dtable_ld, a.width, 0);
+    for (int k = 0; k < mine; ++k) {
+        const int64_t v = (int64_t)(k * gridDim.x + blockIdx.x) * chunk * 32;
+        const int rows = (int)min((int64_t)chunk * 32, a.vocab - v);
+        const uint32_t* const marks = occurs + k * chunk;
+        if (!clear.pieces) {
+            for (int r = threadIdx.x / 32 * 32; r < rows; r += kClearThreads) {
+                const int count = min(32, rows - r);
+                clear.block(v + r, count, ~marks[r / 32] & 0xffffffffu >> (32 - count));
+            }
+            continue;
+        }
+        // the chunk as one span, by all threads
+        auto absent = [&](int r) { return !(marks[r >> 5] >> (r & 31) & 1u); };
+        float* const from = a.dtable + v * a.width;
+        const int count = rows * a.width, whole = (count - clear.lead) / 4, loose = count - 4 * whole;
+        if ((int)threadIdx.x < loose) {
+            const int e = (int)threadIdx.x < clear.lead ? threadIdx.x : 4 * whole + threadIdx.x;
+            if (absent(e < a.width ? 0 : rows - 1)) from[e] = 0.f;
+        }
+        int r = first_row, c = first_col;
+        for (int q = threadIdx.x; q < whole; q += kClearThreads) {
+            float* const to = from + clear.lead + 4 * q;
+            const bool here = absent(r), next = c + 4 > a.width ? absent(r + 1) : here;
+            if (here && next) {
+                *reinterpret_cast<float4*>(to) = make_float4(0.f, 0.f, 0.f, 0.f);
+            } else if (here || next) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + j < a.width ? here : next) to[j] = 0.f;
+            }
+            r += row_step, c += col_step;
+            if (c >= a.width) c -= a.width, ++r;
+        }
+    }
+}
+
 // K: ids a thread looks at
 template <int L, bool VEC, int K>
-__global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs a, const int32_t* ids, int rows_per_cta, int32_t* status) {
+__global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs a, const int32_t* ids, uint32_t magic, int apart, int32_t* status) {
     extern __shared__ __align__(16) unsigned char raw[];
     SmallShared<L>& sh = *reinterpret_cast<SmallShared<L>*>(raw);
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-    const uint32_t v0 = blockIdx.x * (uint32_t)rows_per_cta;
-    const uint32_t rows = (uint32_t)min((int64_t)rows_per_cta, a.vocab - v0);
+    cudaTriggerProgrammaticLaunchCompletion();   // the launch that clears the other rows may prepare
+    const uint32_t rows = (uint32_t)((a.vocab - blockIdx.x + gridDim.x - 1) / gridDim.x);   // blockIdx.x, + gridDim.x, ...
+    auto turn = [&](int32_t v) { return gridDim.x == 1 ? (uint32_t)v : __umulhi((uint32_t)v, magic); };   // v / gridDim.x
     int32_t id[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -530,7 +923,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs 
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         if (blockIdx.x == 0 && blockIdx.y == 0 && status && id[k] != -1 && (uint32_t)id[k] >= (uint32_t)a.vocab) atomicExch(status, SLICEGCN_DEVSTATUS_BAD_ID);
-        mine[k] = __ballot_sync(0xffffffffu, id[k] >= 0 && (uint32_t)id[k] - v0 < rows);
+        mine[k] = __ballot_sync(0xffffffffu, (uint32_t)id[k] < (uint32_t)a.vocab && (uint32_t)id[k] - turn(id[k]) * gridDim.x == blockIdx.x);
         if (lane == 0) sh.before[k][w] = __popc(mine[k]);
     }
     __syncthreads();
@@ -554,7 +947,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs 
 #pragma unroll
     for (int k = 0; k < K; ++k)
         if (mine[k] >> lane & 1u) {
-            const uint32_t local = (uint32_t)id[k] - v0;
+            const uint32_t local = turn(id[k]);
             sh.list[0][sh.before[k][w] + __popc(mine[k] & ((1u << lane) - 1u))] = local << kSmallBits | (uint32_t)(k * kSumThreads + tid);
             atomicOr(&sh.present[local >> 5], 1u << (local & 31));
         }
@@ -602,19 +995,21 @@ __global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs 
         __syncthreads();
     }
     constexpr int U = SumShared<L>::U;
-    if (!a.accumulate) {   // rows without an id
+    sum_sorted<L, VEC, true>(a, PairsInShared{sh.list[cur], blockIdx.x, gridDim.x}, m, (m + U - 1) / U, 0, sh.sum,
+                           *reinterpret_cast<RowRing<L, VEC>*>(sh.list[cur ^ 1]));   // the list that is not read any more
+    if (!a.accumulate && !apart) {   // rows without an id
         const int l = tid & (L - 1), col = blockIdx.y * 4 * L + (VEC ? 4 * l : l);
         const float zero[4] = {0.f, 0.f, 0.f, 0.f};
         if (col < a.width)
             for (uint32_t r = tid / L; r < rows; r += U)
-                if (!(sh.present[r >> 5] >> (r & 31) & 1u)) store4<VEC>(a.dtable + (int64_t)(v0 + r) * a.dtable_ld, col, L, a.width, 0, zero);
+                if (!(sh.present[r >> 5] >> (r & 31) & 1u))
+                    store4<VEC>(a.dtable + ((int64_t)r * gridDim.x + blockIdx.x) * a.dtable_ld, col, L, a.width, 0, zero);
     }
-    sum_sorted<L, VEC, true>(a, PairsInShared{sh.list[cur], v0}, m, (m + U - 1) / U, 0, sh.sum);
 }
 
 // What is left after the sums.  The first join_ctas CTAs: ids that reach over the edges of the sums' CTAs, a warp for the one
 // that starts in each of them; one that reaches over more than kLongJoin is added by the whole CTA, in shares of consecutive
-// parts that are then added in order.  The other CTAs: rows of ids that do not occur, by lane groups like those of the sums.
+// parts that are then added in order.  The other CTAs: rows of ids that do not occur, unless the table was cleared before.
 constexpr int kLongJoin = 16;
 template <int L, bool VEC>
 __global__ void __launch_bounds__(256) embed_finish_kernel(const SumArgs a, int join_ctas) {
@@ -624,17 +1019,24 @@ __global__ void __launch_bounds__(256) embed_finish_kernel(const SumArgs a, int 
     cudaGridDependencySynchronize();
     const int c0 = blockIdx.y * W;
     if ((int)blockIdx.x >= join_ctas) {
-        const int l = threadIdx.x & (L - 1), col = c0 + (VEC ? 4 * l : l);
-        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-        // a lane group takes L rows: their flags with one load, then the rows that are absent
-        const unsigned group = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((threadIdx.x & 31) & ~(L - 1));
-        const int64_t step = (int64_t)(gridDim.x - join_ctas) * 256;
-        for (int64_t v = ((int64_t)(blockIdx.x - join_ctas) * 256 + threadIdx.x) / L * L; v < a.vocab; v += step) {
-            unsigned absent = __ballot_sync(group, v + l < a.vocab && !a.present[v + l]);
-            absent = (absent & group) >> ((threadIdx.x & 31) & ~(L - 1));
-            for (; absent; absent &= absent - 1) {
-                const int64_t r = v + __ffs(absent) - 1;
-                if (col < a.width) store4<VEC>(a.dtable + r * a.dtable_ld, col, L, a.width, 0, zero);
+        // 32 rows per warp and step, or fewer (a multiple of four) where there are few rows for so many warps
+        const int64_t ctas = gridDim.x - join_ctas, warps = gridDim.y * ctas * 8;
+        const int64_t warp = (blockIdx.y * ctas + blockIdx.x - join_ctas) * 8 + threadIdx.x / 32;
+        const int rows = a.vocab >= 32 * warps ? 32 : a.vocab >= 16 * warps ? 16 : 8;
+        const RowClear clear(a.dtable, a.dtable_ld, a.width, 0);
+        const int64_t step = warps * rows;
+        for (int64_t v = warp * rows; v < a.vocab; v += 4 * step) {
+            bool absent[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t r = v + q * step + clear.lane;
+                absent[q] = !a.present[min(r, a.vocab - 1)] && r < a.vocab && clear.lane < rows;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t r = v + q * step;
+                const uint32_t bits = __ballot_sync(0xffffffffu, absent[q]);
+                if (r < a.vocab) clear.block(r, (int)min((int64_t)rows, a.vocab - r), bits);
             }
         }
         return;
@@ -725,6 +1127,11 @@ bool is_small(const slicegcn_embed_desc* d) {
     return d->n > 0 && d->n <= (d->vocab < 64 ? kSmallN / 8 : kSmallN) && d->vocab <= (int64_t)kSMs * kSmallRows;
 }
 
+// A table of many more rows than there are ids is cleared as a whole, beside the sort, which keeps few SMs busy: at most a quarter
+// of the rows is written a second time.  Otherwise the rows that do not occur are cleared at the end.
+bool clear_first(const slicegcn_embed_desc* d) { return !d->accumulate && d->vocab / 4 >= d->n; }
+constexpr int kClearBytes = 128 << 10;   // of a CTA that clears
+
 // How the gradient is cut, and where its parts lie in the workspace.
 struct GradPlan {
     int passes, bits, tiles;     // digit passes and bits per digit; CTAs of a pass
@@ -750,12 +1157,14 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
     p.lanes = 2;
     while (p.lanes < 32 && p.lanes < quads) p.lanes *= 2;
     p.col_tiles = (quads + p.lanes - 1) / p.lanes;
-    const int units = kSumThreads / p.lanes;
+    const bool narrow = d->width <= kNarrow;   // (two lanes: a warp is the unit)
+    const int units = narrow ? kNarrowUnits : kSumThreads / p.lanes;
     // One wave of CTAs, or two where the units are long enough to make up for their starts and ends (one / two waves:
     // 49 / 57 us at 18 positions per unit, 332 / 322 us at 259).
     const int64_t wave = std::max<int64_t>(1, kSMs * kSumPerSM / p.col_tiles) * units;
     const int64_t per_unit = (d->n + wave - 1) / wave;
     p.per_unit = (int32_t)std::max<int64_t>(8, per_unit >= 128 ? (per_unit + 1) / 2 : per_unit);
+    if (narrow) p.per_unit = (p.per_unit + 31) / 32 * 32;
     p.sum_ctas = (int)((d->n + (int64_t)p.per_unit * units - 1) / ((int64_t)p.per_unit * units));
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -776,9 +1185,14 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
 
 template <int L, bool VEC>
 slicegcn_status_t launch_sum(const SumArgs& a, int col_tiles, cudaStream_t st) {
-    if (a.sum_ctas > 0) SGCN_TRY(launch_after(embed_sum_kernel<L, VEC>, dim3(a.sum_ctas, col_tiles), kSumThreads, 0, st, a));
+    if (a.sum_ctas > 0) {
+        if constexpr (L == 2)
+            SGCN_TRY(launch_after(a.width <= 4 ? embed_sum_narrow_kernel<4, VEC> : embed_sum_narrow_kernel<8, VEC>, dim3(a.sum_ctas), kSumThreads, 0, st, a));
+        else
+            SGCN_TRY(launch_after(embed_sum_kernel<L, VEC>, dim3(a.sum_ctas, col_tiles), kSumThreads, 0, st, a));
+    }
     const int join_ctas = a.sum_ctas > 1 ? (a.sum_ctas + 7) / 8 : 0;
-    const unsigned zero_ctas = a.accumulate ? 0 : (unsigned)std::min<int64_t>((a.vocab * L + 255) / 256, kSMs * 6);
+    const unsigned zero_ctas = a.present ? (unsigned)std::min<int64_t>((a.vocab + 63) / 64, std::max(1, kSMs * 6 / col_tiles)) : 0;
     if (join_ctas + zero_ctas > 0)
         SGCN_TRY(launch_after(embed_finish_kernel<L, VEC>, dim3(join_ctas + zero_ctas, col_tiles), 256, 0, st, a, join_ctas));
     return SLICEGCN_OK;
@@ -786,15 +1200,26 @@ slicegcn_status_t launch_sum(const SumArgs& a, int col_tiles, cudaStream_t st) {
 
 template <int L, bool VEC, int K>
 slicegcn_status_t launch_small(const SumArgs& a, const int32_t* ids, int32_t* status, int col_tiles, cudaStream_t st) {
-    // two CTAs per SM over the column tiles: every CTA looks at all ids
-    const int64_t ctas = std::min<int64_t>(kSMs, std::max(1, 2 * kSMs / col_tiles));
-    const int rows = (int)std::min<int64_t>((a.vocab + ctas - 1) / ctas, kSmallRows);
+    // two CTAs per SM at most over the column tiles: every CTA looks at all ids
+    int64_t ctas = std::min<int64_t>(kSMs, std::max(1, 2 * kSMs / col_tiles));
+    ctas = std::min<int64_t>(a.vocab, std::max<int64_t>(ctas, (a.vocab + kSmallRows - 1) / kSmallRows));
+    // id / ctas by a product: exact for ids below 2^32 / ctas, which is more than kSMs * kSmallRows
+    const uint32_t magic = (uint32_t)(((uint64_t)1 << 32) / ctas + 1);
     constexpr int smem = (int)sizeof(SmallShared<L>);
     SGCN_CUDA(cudaFuncSetAttribute(embed_small_kernel<L, VEC, K>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    embed_small_kernel<L, VEC, K><<<dim3((unsigned)((a.vocab + rows - 1) / rows), col_tiles), kSumThreads, smem, st>>>(a, ids, rows, status);
+    const bool apart = !a.accumulate && (a.vocab > kApartRows || a.vocab * a.width * 4 > kApartBytes);
+    embed_small_kernel<L, VEC, K><<<dim3((unsigned)ctas, col_tiles), kSumThreads, smem, st>>>(a, ids, magic, apart, status);
     SGCN_LAUNCH_CHECK();
     count_launch();
-    return SLICEGCN_OK;
+    if (!apart) return SLICEGCN_OK;
+    const int64_t blocks = (a.vocab + 31) / 32;
+    int chunk = kClearWarps;   // as many blocks as make 128 KB, and no more than leave every CTA a chunk
+    while (chunk > 1 && ((int64_t)chunk * 128 * a.width > 128 << 10 || blocks < (int64_t)chunk * kClearCtas)) chunk /= 2;
+    const int64_t chunks = (blocks + chunk - 1) / chunk, clear_ctas = std::min<int64_t>(chunks, kClearCtas);
+    const size_t marks = (chunks + clear_ctas - 1) / clear_ctas * chunk * 4;   // 2 KB at most
+    // as much shared memory as there is: else an SM would have to be empty before it takes these CTAs beside the others
+    SGCN_CUDA(cudaFuncSetAttribute(embed_clear_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
+    return launch_after(embed_clear_kernel, dim3((unsigned)clear_ctas), kClearThreads, marks, st, a, ids, chunk);
 }
 
 template <bool VEC, int K>
@@ -915,7 +1340,7 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
     t.dtable = dtable;
     t.dtable_ld = d->dtable_ld;
     t.scale = (float)d->scale;
-    t.present = reinterpret_cast<uint8_t*>(ws + p.present);
+    t.present = d->accumulate || clear_first(d) ? nullptr : reinterpret_cast<uint8_t*>(ws + p.present);
     t.per_unit = p.per_unit;
     t.sum_ctas = p.sum_ctas;
     t.head = reinterpret_cast<float*>(ws + p.head);
@@ -933,6 +1358,11 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
     a.bits = p.bits;
     a.tiles = p.tiles;
     a.tile = p.tile;
+    a.clear = ClearShare{dtable, d->dtable_ld, d->width, d->vocab, 0, (kClearBytes / 4 / d->width + 32) / 32 * 32};
+    unsigned clear_ctas = 0;   // per launch
+    const int64_t of_a_cta_each = a.clear.rows_per_cta * 2 * p.passes;   // rows that one CTA in every launch clears
+    if (clear_first(d)) clear_ctas = (unsigned)((d->vocab + of_a_cta_each - 1) / of_a_cta_each);
+    const int64_t clear_rows = clear_ctas * a.clear.rows_per_cta;
     constexpr int kMaxSmem = kSortWarps * 4 << kMaxDigitBits;
     SGCN_CUDA(cudaFuncSetAttribute(sort_scatter_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem));
     SGCN_CUDA(cudaFuncSetAttribute(sort_scatter_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem));
@@ -942,14 +1372,17 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
         a.in = buf[(k + 1) & 1];
         a.out = buf[k & 1];
         const size_t smem = (size_t)kSortWarps * 4 << p.bits;
+        const dim3 grid(p.tiles + clear_ctas);
         if (k == 0) {
-            sort_count_kernel<true><<<p.tiles, kSortThreads, 0, st>>>(a);   // after whatever the stream holds
+            sort_count_kernel<true><<<grid, kSortThreads, 0, st>>>(a);   // after whatever the stream holds
             SGCN_LAUNCH_CHECK();
             count_launch();
         } else {
-            SGCN_TRY(launch_after(sort_count_kernel<false>, dim3(p.tiles), kSortThreads, 0, st, a));
+            SGCN_TRY(launch_after(sort_count_kernel<false>, grid, kSortThreads, 0, st, a));
         }
-        SGCN_TRY(launch_after(k == 0 ? sort_scatter_kernel<true> : sort_scatter_kernel<false>, dim3(p.tiles), kSortThreads, smem, st, a));
+        a.clear.row0 += clear_rows;
+        SGCN_TRY(launch_after(k == 0 ? sort_scatter_kernel<true> : sort_scatter_kernel<false>, grid, kSortThreads, smem, st, a));
+        a.clear.row0 += clear_rows;
     }
     t.pairs = buf[(p.passes + 1) & 1];
     SGCN_TRY(vec ? launch_sums<true>(t, p.lanes, p.col_tiles, st) : launch_sums<false>(t, p.lanes, p.col_tiles, st));

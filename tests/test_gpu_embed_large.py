@@ -42,7 +42,7 @@ CASES = [(2_449_029, 2_449_029, 4, "own"), (2_449_029, 2_449_029, 7, "own"), (1_
          (1_500_000, 100, 3, "uniform"), (1_250_000, 3, 32, "hub"), (160_000, 70_001, 131, "zipf"), (2_400_000, 40, 20, "runs"), (700_000, 1_000, 300, "zipf"),
          (20_000, 2_000_000, 20, "zipf"), (100_000, 400_000, 131, "zipf"), (9_000, 500_000, 5, "uniform"), (30_001, 120_004, 130, "uniform"),
          (8_192, 900_001, 33, "zipf"), (5_000, 300_000, 262, "zipf"), (1_000, 60_000, 1_433, "uniform"), (8, 1_000_003, 6, "uniform"), (0, 100_003, 9, "uniform"),
-         (70_000, 280_000, 1, "uniform"), (8_000, 40_000, 2, "zipf"), (17, 90_000, 3, "uniform")]
+         (70_000, 280_000, 1, "uniform"), (50_000, 3_000, 2, "zipf"), (60_000, 60_000, 6, "own"), (400_000, 20, 6, "hub"), (90_000, 2, 8, "uniform"), (5, 1, 3, "uniform"), (300, 400, 40_000, "uniform"), (8_192, 9_699_000, 2, "uniform"), (8_000, 40_000, 2, "zipf"), (17, 90_000, 3, "uniform")]
 
 
 def _ids(n, vocab, kind):
@@ -91,3 +91,27 @@ def test_sums_are_exact(n, vocab, width, kind, gap, start):
         assert bool((big[:start] == 9).all()) and bool((big[start + vocab * (width + gap):] == 9).all())
         if gap:
             assert bool((big[start:start + vocab * (width + gap)].view(vocab, width + gap)[:, width:] == 9).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("width", [1, 2, 3, 5, 6, 7, 8, 11, 33, 130])
+@pytest.mark.parametrize("n,vocab,kind", [(20_000, 700, "zipf"), (30_000, 30_000, "own"), (2_000, 90, "zipf")])
+@pytest.mark.parametrize("ld,start", [(0, 1), (0, 3), (3, 2), (4, 0)])
+def test_rows_of_dout_at_every_start(n, vocab, kind, width, ld, start):
+    """What lies between the rows, before the first and behind the last is never taken (NaN)."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    ids = _ids(n, vocab, kind)
+    big = torch.full((n * (width + ld) + start + 3,), float("nan"), device="cuda")
+    dout = big[start:start + n * (width + ld)].view(n, width + ld)[:, :width]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(width)
+    dout.copy_(torch.randint(-3, 4, (n, width), generator=g, device="cuda").float())
+    known = (ids >= 0).nonzero()[:, 0]
+    want = torch.zeros((vocab, width), device="cuda", dtype=torch.float64).index_add_(0, ids[known].long(), dout[known].double())
+    d = B.make_embed_desc(n, vocab, width, dout_ld=width + ld)
+    wsb = B.slicegcn_embed_workspace_bytes(d)
+    ws = torch.randint(0, 256, (wsb,), dtype=torch.uint8, device="cuda")
+    out = torch.full((vocab, width), float("nan"), device="cuda")
+    B.slicegcn_embed_backward(d, ids, dout, out, None, ws, wsb, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(out.double(), want)
