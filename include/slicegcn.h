@@ -446,7 +446,10 @@ slicegcn_status_t slicegcn_embed_backward(const slicegcn_embed_desc* d, const in
  *   u = N(h) * w_pre + b_pre
  *   N(t) = t / sqrt(mean(t^2) + eps)  (ROWNORM_RMS)    or    (t - mean(t)) / sqrt(var(t) + eps)  (ROWNORM_LAYER)
  * x is the residual stream, y the block's output (slicegcn_layer_forward), h the new residual stream and u the next
- * block's input.  u is computed from h before h is rounded to its storage type.  What is NULL is left out: gate = NULL
+ * block's input.  u is computed from h before h is rounded to its storage type.  An eps below the least normal fp32 number
+ * counts as that number.  The gate's exponential has fp32's accuracy, except where h and u are stored as bf16.
+ * Reads may take in (and ignore) what lies beside a row in the aligned 16 bytes of its first and last element, so those have to be
+ * readable; any allocation of this device's memory is.  What is NULL is left out: gate = NULL
  * no gate; x = NULL no residual; y = NULL a norm before a block alone (h = x, u = N(x) ...); u = NULL after the last block
  * (h alone); h = NULL when only u is wanted; a NULL weight is a vector of ones, a NULL bias of zeros.
  */
@@ -488,6 +491,7 @@ slicegcn_status_t slicegcn_residual_norm_backward(const slicegcn_residual_norm_d
  * The comparison and the quotient are those of the 64-bit norm; *norm_out is that norm rounded to fp32 (infinity if it lies past
  * fp32's range, which alone does not keep the gradients from being clipped).  A 64-bit norm that is infinite or NaN (a gradient
  * is) leaves the gradients as they are, and *norm_out is then infinite or NaN too.  Nothing is read back to the host.
+ * Reads may take in (and ignore) the rest of the aligned 16 bytes that hold a tensor's last element.
  */
 #define SLICEGCN_MAX_TENSORS 512
 typedef struct slicegcn_tensor_list {

@@ -787,8 +787,10 @@ __global__ void __launch_bounds__(256, 2) norm_backward_kernel(const NormArgs a,
 // CTA stands in the loop.  The row is read from shared memory in each of the passes over it, which leaves the registers to the
 // columns' sums (BIAS: those of the biases too).  A CTA works on one slice: its warps' sums are added in order at the end.
 // What is not given is left in shared memory as values that change nothing (zeros; an infinite gate is an open one).
-// Shared memory (two rows per warp) and registers (the sums) bound the warps per SM, so what counts here is instructions
-// per element: twelve warps of them keep up with HBM at 602 columns.
+// Shared memory (two rows per warp) and registers (the sums) bound the warps per SM, so what counts here is instructions per element
+// and latency: 232,965 x 602 bf16, gated, plain norm without biases, moves 5.0-5.4 TB/s (680-730 us where the bytes take 557).
+// With biases the sums take twice the registers and part of them spills (up to 500 bytes a thread with accesses of four
+// elements, 850 without): 1.5 times the time at 602 columns, 1.9 at 1,024.
 template <int NV>
 constexpr int staged_warps() { return NV <= 5 ? 12 : 8; }
 // bytes of one row of a warp: dh, du in fp32 and y, gate, h in T, 32 lanes x NV chunks each
@@ -1004,9 +1006,9 @@ __global__ void __launch_bounds__(staged_warps<NV>() * 32) norm_backward_staged_
     }
 }
 
-// Wider slices.  First a CTA per slice row takes
-// the sums over the row, reading it twice (the second time from L2); then every thread applies them to columns of its own
-// for many rows, whose sums it keeps in registers.
+// Wider slices.  First a CTA per slice row takes the sums over the row, reading it twice, or three times for the layer norm (from L2
+// but for the first time); then every thread applies them to columns of its own for many rows, whose sums it keeps in
+// registers.  The second kernel reads everything from HBM again: 20,000 x 4,096 fp32 takes 1.07 ms where the bytes take 400 us.
 struct RowStats {
     float mh, rh, mg, mgh, my, ry, mt, mty;
 };
