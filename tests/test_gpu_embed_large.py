@@ -115,3 +115,32 @@ def test_rows_of_dout_at_every_start(n, vocab, kind, width, ld, start):
     out = torch.full((vocab, width), float("nan"), device="cuda")
     B.slicegcn_embed_backward(d, ids, dout, out, None, ws, wsb, torch.cuda.current_stream().cuda_stream)
     assert torch.equal(out.double(), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,vocab,width", [(3_000, 700_001, 33), (3_000, 700_001, 64), (20_000, 300_000, 7), (20_000, 300_000, 131), (300_000, 270_000, 5), (60_000, 60_000, 40)])
+def test_replayed_and_on_another_stream(n, vocab, width):
+    """Launches that overlap do so in a graph and on a side stream as well; every replay starts from other contents."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    ids = _ids(n, vocab, "zipf")
+    dout = torch.randint(-3, 4, (n, width), device="cuda").float()
+    want = _gradient(ids, dout, vocab, 2.0)
+    out = torch.empty_like(want)
+    d = B.make_embed_desc(n, vocab, width, scale=2.0)
+    wsb = B.slicegcn_embed_workspace_bytes(d)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out.fill_(5.0)
+        B.slicegcn_embed_backward(d, ids, dout, out, None, ws, wsb, torch.cuda.current_stream().cuda_stream)
+        doubled = out * 2.0
+    for _ in range(20):
+        graph.replay()
+        assert torch.equal(out, want) and torch.equal(doubled, 2.0 * want)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            out.fill_(float("nan"))
+            B.slicegcn_embed_backward(d, ids, dout, out, None, ws, wsb, side.cuda_stream)
+            assert torch.equal(out, want)
