@@ -1121,12 +1121,11 @@ slicegcn_status_t check_desc(const slicegcn_embed_desc* d, const char* who) {
 
 int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 
-// One launch while the picking (every CTA looks at all ids) and an id that holds all positions (one CTA sums them) are
-// cheaper than the sort's launches.
-// (4,096 ids: 15.5 us, or 36.9 us sorted by launches; with a table of 7 rows, whose CTAs sum many positions each, 33 against
-// 23 us.)
+// One launch that sums while the picking (every CTA looks at all ids) and the most frequent rows (a row is one CTA's) are cheaper
+// than the sort's launches: up to 8,192 ids and 1,024 of them per row on average.  (8,192 x 128 of 4,096 rows: 8.5 us, or 19.0 sorted
+// by launches; 8,192 x 131 of 20 rows: 14.4 and 16.2; of 3 rows: 50 and 23.)
 bool is_small(const slicegcn_embed_desc* d) {
-    return d->n > 0 && d->n <= (d->vocab < 64 ? kSmallN / 8 : kSmallN) && d->vocab <= (int64_t)kSMs * kSmallRows;
+    return d->n > 0 && d->n <= kSmallN && (d->n + 1023) / 1024 <= d->vocab && d->vocab <= (int64_t)kSMs * kSmallRows;
 }
 
 // A table of many more rows than there are ids is cleared as a whole, beside the sort, which keeps few SMs busy: at most a quarter
@@ -1162,7 +1161,7 @@ GradPlan grad_plan(const slicegcn_embed_desc* d) {
     const bool narrow = d->width <= kNarrow;   // (two lanes: a warp is the unit)
     const int units = narrow ? kNarrowUnits : kSumThreads / p.lanes;
     // One wave of CTAs, or two where the units are long enough to make up for their starts and ends (one / two waves:
-    // 49 / 57 us at 18 positions per unit, 332 / 322 us at 259).
+    // 42 / 45 us at 36 positions per unit, 319 / 311 us at 518).
     const int64_t wave = std::max<int64_t>(1, kSMs * kSumPerSM / p.col_tiles) * units;
     const int64_t per_unit = (d->n + wave - 1) / wave;
     p.per_unit = (int32_t)std::max<int64_t>(8, per_unit >= 128 ? (per_unit + 1) / 2 : per_unit);
@@ -1235,7 +1234,7 @@ slicegcn_status_t launch_smalls(const SumArgs& a, const int32_t* ids, int32_t* s
     }
 }
 
-// 4, 16 or 32 ids per thread (2,708 ids: 10.2 us with 16, 12.2 us with 32)
+// 4, 16 or 32 ids per thread (2,708 ids: 6.5 us with 16, 7.8 us with 32)
 template <bool VEC>
 slicegcn_status_t launch_small_for(const SumArgs& a, const int32_t* ids, int32_t* status, int lanes, int col_tiles, cudaStream_t st) {
     if (a.n <= 4 * kSumThreads) return launch_smalls<VEC, 4>(a, ids, status, lanes, col_tiles, st);

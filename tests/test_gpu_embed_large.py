@@ -42,7 +42,7 @@ CASES = [(2_449_029, 2_449_029, 4, "own"), (2_449_029, 2_449_029, 7, "own"), (1_
          (1_500_000, 100, 3, "uniform"), (1_250_000, 3, 32, "hub"), (160_000, 70_001, 131, "zipf"), (2_400_000, 40, 20, "runs"), (700_000, 1_000, 300, "zipf"),
          (20_000, 2_000_000, 20, "zipf"), (100_000, 400_000, 131, "zipf"), (9_000, 500_000, 5, "uniform"), (30_001, 120_004, 130, "uniform"),
          (8_192, 900_001, 33, "zipf"), (5_000, 300_000, 262, "zipf"), (1_000, 60_000, 1_433, "uniform"), (8, 1_000_003, 6, "uniform"), (0, 100_003, 9, "uniform"),
-         (70_000, 280_000, 1, "uniform"), (50_000, 3_000, 2, "zipf"), (60_000, 60_000, 6, "own"), (400_000, 20, 6, "hub"), (90_000, 2, 8, "uniform"), (5, 1, 3, "uniform"), (300, 400, 40_000, "uniform"), (8_192, 9_699_000, 2, "uniform"), (8_000, 40_000, 2, "zipf"), (17, 90_000, 3, "uniform")]
+         (70_000, 280_000, 1, "uniform"), (50_000, 3_000, 2, "zipf"), (60_000, 60_000, 6, "own"), (400_000, 20, 6, "hub"), (90_000, 2, 8, "uniform"), (5, 1, 3, "uniform"), (1_024, 1, 5, "uniform"), (1_025, 1, 5, "uniform"), (4_096, 4, 33, "uniform"), (8_192, 8, 131, "hub"), (8_192, 7, 131, "hub"), (8_000, 20, 12, "zipf"), (300, 400, 40_000, "uniform"), (8_192, 9_699_000, 2, "uniform"), (8_000, 40_000, 2, "zipf"), (17, 90_000, 3, "uniform")]
 
 
 def _ids(n, vocab, kind):
