@@ -509,6 +509,94 @@ slicegcn_status_t slicegcn_clip_grads(const slicegcn_tensor_list* list, double m
                                       int64_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Feed-forward projections per slice -- the matrix products of a block between sliced layers, with bias, activation, gate and
+ * residual in one kernel.  Slice s reads its in_s columns of x and writes its out_s columns of out:
+ *   a = x_s W_s + b_s,  c = x_s W2_s + b2_s
+ *   out_s = r_s + scale * act(a)          (W2 = NULL)
+ *   out_s = r_s + scale * act(a) * c      (gated)
+ * num_slices = 1 is the ordinary matrix product.  act: NONE a;  RELU max(a, 0);  SILU a / (1 + exp(-a));
+ * GELU a/2 * (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))).  ReLU'(0) = 0.
+ * x, W, W2, r and out are stored as `dtype` (bf16 weights: the copies that slicegcn_adamw_step keeps), biases are fp32.  All
+ * arithmetic is fp32-accurate from the stored values, with one rounding of out; sums over long axes are added in pieces.
+ */
+enum { SLICEGCN_ACT_NONE = 0, SLICEGCN_ACT_RELU = 1, SLICEGCN_ACT_SILU = 2, SLICEGCN_ACT_GELU = 3 };
+#define SLICEGCN_MAX_FFN_WIDTH 65536
+/* Bit of the status word that a bounded wait inside a kernel sets when it runs out (the outputs are then undefined). */
+enum { SLICEGCN_DEVSTATUS_WAIT = 64 };
+typedef struct slicegcn_ffn_desc {
+    int64_t n;                   /* rows, 0 .. 2^31 - 16385 */
+    int32_t num_slices;          /* 1 .. SLICEGCN_MAX_SLICES */
+    int32_t in_s, out_s;         /* columns per slice of x and of out, 1 .. SLICEGCN_MAX_FFN_WIDTH */
+    int32_t act;                 /* SLICEGCN_ACT_* */
+    int32_t dtype;               /* storage type of x, W, W2, r and out */
+    int32_t grad_dtype;          /* storage type of dout, dx, dW and dW2: SLICEGCN_F32, or SLICEGCN_BF16 with dtype BF16 */
+    double scale;
+    int64_t x_ld, r_ld, out_ld;  /* leading dimensions of the matrices a call is given */
+    int64_t dout_ld, dx_ld;      /* (>= num_slices * in_s or out_s; those of others are ignored) */
+    const void *W, *W2;          /* [device, num_slices x in_s x out_s, dense, slice-major]; W2 NULL: no gate */
+    const float *b, *b2;         /* [device, num_slices x out_s] or NULL */
+} slicegcn_ffn_desc;
+/* Scratch bytes of a forward call (dout = NULL) or of a backward call with these matrices; of x and dout only the alignment is
+ * looked at.  Matrices of bf16 whose rows start on 16 bytes (slices of them too) are read as they are; others, and fp32, are
+ * laid out in the workspace first. */
+slicegcn_status_t slicegcn_ffn_workspace_bytes(const slicegcn_ffn_desc* d, const void* x, const void* dout, int64_t* bytes);
+/* x [device, n x num_slices*in_s], r [device, n x num_slices*out_s] or NULL, out like r; out may be r (same pointer and leading
+ * dimension), no other overlap.  status [device, one int32, caller-owned, may be NULL]: SLICEGCN_DEVSTATUS_WAIT or nothing.
+ * workspace [device, 128-byte aligned], contents undefined before and after.
+ * Errors: INVALID_ARG, OVERFLOW, UNSUPPORTED, ALLOC (workspace too small), CUDA. */
+slicegcn_status_t slicegcn_ffn_forward(const slicegcn_ffn_desc* d, const void* x, const void* r, void* out, int32_t* status,
+                                       void* workspace, int64_t workspace_bytes, void* stream);
+/* Gradient of the same call from x alone (a and c are computed again); the gradient w.r.t. r is dout.
+ *   dout [device, n x num_slices*out_s, grad_dtype]: gradient of the loss w.r.t. out
+ * Outputs (OVERWRITTEN, each may be NULL to skip): dx [n x num_slices*in_s], dW, dW2 [num_slices x in_s x out_s] of
+ * grad_dtype; db, db2 [num_slices x out_s] fp32.  dW2 and db2 only with W2.  No overlap.  Deterministic: sums over rows are
+ * taken in a fixed order.  With grad_dtype BF16 the gradients w.r.t. a and c are rounded to bf16 once, as operands of the
+ * products that give dx, dW and dW2 (db and db2 are summed before that); with F32 they keep fp32's digits.
+ * Errors: as slicegcn_ffn_forward. */
+slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* x, const void* dout, void* dx, void* dW,
+                                        void* dW2, float* db, float* db2, int32_t* status, void* workspace,
+                                        int64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * AdamW over a list of tensors in one launch:
+ *   g = grad * c      c = max_norm / *grad_norm if *grad_norm > max_norm and finite, else 1   (grad_norm = NULL: 1)
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,   t = step[0] + 1
+ *   param = param (1 - rate * weight_decay) - rate * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * with rate = lr * *lr_scale (lr_scale = NULL: lr), and afterwards step[0] = t.  The step count, the norm (the one that
+ * slicegcn_clip_grads leaves, which then need not write clipped gradients) and lr_scale are read on the device, so that a
+ * captured call can be replayed.
+ * States: SLICEGCN_F32, or SLICEGCN_Q8 -- m as int8 and sqrt(v) as uint8 with one fp32 scale each for every 256 consecutive
+ * elements of a tensor (the block's largest magnitude / 127, / 255; 0 when that is below the least normal number).  What a code
+ * stands for is code * scale.  A code is rounded up where its fraction reaches a threshold that a hash of the element's index and t gives:
+ * a state that moves by less than a code a step moves on average as it should, where rounding to nearest would leave it.  sqrt(v) > 0 never
+ * becomes code 0.  The update uses m and v before they are rounded.  An eps below the least normal fp32 number counts as that number.  A gradient that is infinite or NaN makes the whole block's
+ * states NaN.
+ */
+enum { SLICEGCN_Q8 = 2 };
+#define SLICEGCN_ADAMW_BLOCK 256
+typedef struct slicegcn_adamw_desc {
+    int32_t count;                  /* 0 .. SLICEGCN_MAX_TENSORS */
+    int32_t state_dtype;            /* SLICEGCN_F32 or SLICEGCN_Q8 */
+    float* const* params;           /* [host, count] device pointers, each tensor dense; updated in place */
+    const void* const* grads;       /* [host, count] */
+    void* const* m;                 /* [host, count] fp32 or int8 */
+    void* const* v;                 /* [host, count] fp32 or uint8 */
+    float* const* m_scale;          /* [host, count] fp32, ceil(elems / 256) each; Q8 only */
+    float* const* v_scale;
+    void* const* copies;            /* [host, count] or NULL: the new parameters rounded to bf16; an entry may be NULL */
+    const int64_t* elems;           /* [host, count], 0 allowed */
+    const int32_t* grad_dtypes;     /* [host, count] SLICEGCN_F32 / SLICEGCN_BF16, or NULL = all fp32 */
+    const int32_t* decayed;         /* [host, count] 0: no weight decay for that tensor; NULL = all decay */
+    double lr, beta1, beta2, eps, weight_decay;   /* lr >= 0, 0 <= beta < 1, eps > 0, weight_decay >= 0 */
+    double max_norm;                /* > 0 (infinity: no clipping) */
+    const float* lr_scale;          /* [device, one float] or NULL */
+} slicegcn_adamw_desc;
+/* step [device, two int64, 8-byte aligned]: steps done so far, and a counter that is zero between calls (zero both before the
+ * first).  Calls that share tensors or `step` must not overlap.  Tensors must not overlap.
+ * Errors: INVALID_ARG, UNSUPPORTED (too many tensors), CUDA. */
+slicegcn_status_t slicegcn_adamw_step(const slicegcn_adamw_desc* d, int64_t* step, const float* grad_norm, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Instrumentation for benchmarks (the paper reports only end-to-end epochs per second, Table IV;
  * this splits out the aggregation kernel).  Between profile_begin and profile_end every SpMM call
  * is bracketed by CUDA events on its stream and kernel launches are counted.  profile_end

@@ -19,14 +19,15 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libslicegcn.so")
 
 OK, ERR_INVALID_ARG, ERR_OUT_OF_RANGE, ERR_OVERFLOW, ERR_ALLOC, ERR_CUDA, ERR_UNSUPPORTED = range(7)
-F32, BF16 = 0, 1
+F32, BF16, Q8 = 0, 1, 2
 ORDER_AUTO, AGG_FIRST, XFORM_FIRST = 0, 1, 2
 RULE_CEIL, RULE_FLOOR_PLUS_1 = 0, 1
 SYMMETRIZE, ADD_SELF_LOOPS, INPUT_ON_DEVICE, NORM_MEAN, NORM_SUM = 1, 2, 4, 8, 16
 MAX_SLICES = 64
-DEVSTATUS_BAD_LABEL, DEVSTATUS_BAD_ID = 32, 33
+DEVSTATUS_BAD_LABEL, DEVSTATUS_BAD_ID, DEVSTATUS_WAIT = 32, 33, 64
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 ROWNORM_RMS, ROWNORM_LAYER = 0, 1
-MAX_NORM_WIDTH, MAX_TENSORS = 16384, 512
+MAX_NORM_WIDTH, MAX_TENSORS, MAX_FFN_WIDTH, ADAMW_BLOCK = 16384, 512, 65536, 256
 
 EXPORTS = [
     "slicegcn_last_error", "slicegcn_slice_strategy", "slicegcn_graph_create", "slicegcn_graph_create_from_csr",
@@ -37,7 +38,8 @@ EXPORTS = [
     "slicegcn_model_layer_order", "slicegcn_train_workspace_bytes", "slicegcn_train_epoch", "slicegcn_train_epoch_dropout", "slicegcn_train_epoch_sliced", "slicegcn_forward_logits", "slicegcn_train_epoch_host", "slicegcn_train_epochs_host", "slicegcn_profile_begin", "slicegcn_profile_begin_sampled",
     "slicegcn_profile_end", "slicegcn_embed_forward", "slicegcn_embed_workspace_bytes", "slicegcn_embed_backward",
     "slicegcn_residual_norm_forward", "slicegcn_residual_norm_workspace_bytes", "slicegcn_residual_norm_backward",
-    "slicegcn_clip_workspace_bytes", "slicegcn_clip_grads",
+    "slicegcn_clip_workspace_bytes", "slicegcn_clip_grads", "slicegcn_ffn_workspace_bytes", "slicegcn_ffn_forward",
+    "slicegcn_ffn_backward", "slicegcn_adamw_step",
 ]
 
 
@@ -49,6 +51,10 @@ ARGTYPES = {
     "slicegcn_residual_norm_forward": [_P] * 7,
     "slicegcn_residual_norm_backward": [_P] * 14 + [c_int64, _P],
     "slicegcn_clip_grads": [_P, c_double, _P, _P, c_int64, _P],
+    "slicegcn_ffn_workspace_bytes": [_P] * 4,
+    "slicegcn_ffn_forward": [_P] * 6 + [c_int64, _P],
+    "slicegcn_ffn_backward": [_P] * 10 + [c_int64, _P],
+    "slicegcn_adamw_step": [_P] * 4,
 }
 
 
@@ -96,6 +102,19 @@ class ResidualNormDesc(ctypes.Structure):
 class TensorList(ctypes.Structure):
     _fields_ = [("count", c_int32), ("src", POINTER(c_void_p)), ("dst", POINTER(c_void_p)), ("elems", POINTER(c_int64)),
                 ("dtypes", POINTER(c_int32))]
+
+
+class FfnDesc(ctypes.Structure):
+    _fields_ = [("n", c_int64), ("num_slices", c_int32), ("in_s", c_int32), ("out_s", c_int32), ("act", c_int32), ("dtype", c_int32),
+                ("grad_dtype", c_int32), ("scale", c_double)] + [(k + "_ld", c_int64) for k in ("x", "r", "out", "dout", "dx")] + \
+               [(k, c_void_p) for k in ("W", "W2", "b", "b2")]
+
+
+class AdamwDesc(ctypes.Structure):
+    _fields_ = [("count", c_int32), ("state_dtype", c_int32)] + \
+               [(k, POINTER(c_void_p)) for k in ("params", "grads", "m", "v", "m_scale", "v_scale", "copies")] + \
+               [("elems", POINTER(c_int64)), ("grad_dtypes", POINTER(c_int32)), ("decayed", POINTER(c_int32))] + \
+               [(k, c_double) for k in ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm")] + [("lr_scale", c_void_p)]
 
 
 def make_dropout_desc(rate: float, masks: Sequence, mask_ld: int) -> DropoutDesc:
@@ -515,6 +534,75 @@ def slicegcn_clip_workspace_bytes() -> int:
 
 def slicegcn_clip_grads(tensors: TensorList, max_norm: float, norm_out, workspace, workspace_bytes: int, stream=None) -> None:
     _check(_lib.slicegcn_clip_grads(byref(tensors), max_norm, _ptr(norm_out), _ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+# ------------------------------------------------------------------------------------------ feed-forward projections, AdamW
+
+def make_ffn_desc(n: int, num_slices: int, in_s: int, out_s: int, W, W2=None, b=None, b2=None, act: int = ACT_NONE, dtype: int = F32,
+                  grad_dtype: Optional[int] = None, scale: float = 1.0, **leading_dims: int) -> FfnDesc:
+    """leading_dims: x_ld, r_ld, out_ld, dout_ld, dx_ld; left out = dense rows.  grad_dtype=None: as dtype."""
+    d = FfnDesc(n, num_slices, in_s, out_s, act, dtype, dtype if grad_dtype is None else grad_dtype, scale)
+    for k, width in (("x", in_s), ("r", out_s), ("out", out_s), ("dout", out_s), ("dx", in_s)):
+        setattr(d, k + "_ld", leading_dims.pop(k + "_ld", 0) or num_slices * width)
+    if leading_dims:
+        raise TypeError(f"unknown leading dimensions {sorted(leading_dims)}")
+    d.W, d.W2, d.b, d.b2 = _ptr(W), _ptr(W2), _ptr(b), _ptr(b2)
+    return _with_address(d, W, W2, b, b2)
+
+
+def slicegcn_ffn_workspace_bytes(d: FfnDesc, x, dout=None) -> int:
+    """Of a forward call, or (dout given) of a backward call."""
+    b = c_int64()
+    _check(_lib.slicegcn_ffn_workspace_bytes(byref(d), _ptr(x), _ptr(dout), byref(b)))
+    return b.value
+
+
+def slicegcn_ffn_forward(d: FfnDesc, x, r, out, status, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(_lib.slicegcn_ffn_forward(byref(d), _ptr(x), _ptr(r), _ptr(out), _ptr(status), _ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+def slicegcn_ffn_backward(d: FfnDesc, x, dout, dx, dW, dW2, db, db2, status, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(_lib.slicegcn_ffn_backward(byref(d), _ptr(x), _ptr(dout), _ptr(dx), _ptr(dW), _ptr(dW2), _ptr(db), _ptr(db2), _ptr(status),
+                                      _ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+def make_adamw_desc(params: Sequence, grads: Sequence, m: Sequence, v: Sequence, m_scale: Optional[Sequence] = None,
+                    v_scale: Optional[Sequence] = None, copies: Optional[Sequence] = None, lr: float = 1e-3, beta1: float = 0.9,
+                    beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0, decayed: Optional[Sequence[bool]] = None,
+                    max_norm: float = float("inf"), lr_scale=None) -> AdamwDesc:
+    """Dense device tensors: params fp32, grads fp32 or bf16, m and v fp32, or int8 and uint8 with one fp32 scale for every
+    ADAMW_BLOCK elements in m_scale and v_scale; copies (bf16) may hold None."""
+    n = len(params)
+    q8 = m_scale is not None or v_scale is not None
+    lists = [list(params), list(grads), list(m), list(v)] + ([list(m_scale or []), list(v_scale or [])] if q8 else []) + \
+            ([list(copies)] if copies is not None else [])
+    if any(len(t) != n for t in lists) or (decayed is not None and len(decayed) != n):
+        raise ValueError("the lists must have one entry for each parameter tensor")
+    wants = ["float32", None, "int8" if q8 else "float32", "uint8" if q8 else "float32"] + (["float32"] * 2 if q8 else []) + ["bfloat16"]
+    for k, (tensors, want) in enumerate(zip(lists, wants)):
+        for t, p in zip(tensors, lists[0]):
+            if t is None and copies is not None and k == len(lists) - 1:
+                continue
+            size = -(-p.numel() // ADAMW_BLOCK) if q8 and k in (4, 5) else p.numel()
+            if t.numel() != size or not t.is_contiguous() or (want and str(t.dtype) != "torch." + want):
+                raise ValueError("the tensors of a list must be dense, of the list's type and of the parameter's size")
+    codes = {"torch.float32": F32, "torch.bfloat16": BF16}
+    pointers = [(c_void_p * max(n, 1))(*[_ptr(t) for t in tensors]) for tensors in lists]
+    elems, types = (c_int64 * max(n, 1))(*[t.numel() for t in params]), (c_int32 * max(n, 1))(*[codes[str(t.dtype)] for t in grads])
+    mask = (c_int32 * max(n, 1))(*[int(x) for x in decayed]) if decayed is not None else None
+    d = AdamwDesc(count=n, state_dtype=Q8 if q8 else F32, lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay,
+                  max_norm=max_norm, lr_scale=_ptr(lr_scale))
+    names = ["params", "grads", "m", "v"] + (["m_scale", "v_scale"] if q8 else []) + (["copies"] if copies is not None else [])
+    for name, array in zip(names, pointers):
+        setattr(d, name, ctypes.cast(array, POINTER(c_void_p)))
+    d.elems, d.grad_dtypes = ctypes.cast(elems, POINTER(c_int64)), ctypes.cast(types, POINTER(c_int32))
+    if mask is not None:
+        d.decayed = ctypes.cast(mask, POINTER(c_int32))
+    return _with_address(d, pointers, elems, types, mask, lists, lr_scale)
+
+
+def slicegcn_adamw_step(d: AdamwDesc, step, grad_norm=None, stream=None) -> None:
+    _check(_lib.slicegcn_adamw_step(byref(d), _ptr(step), _ptr(grad_norm), _ptr(stream)))
 
 
 # ------------------------------------------------------------------------------------------ parameter marshalling
