@@ -211,7 +211,7 @@ __device__ __forceinline__ void update_block(const Entry& e, int64_t block, int 
         return;
     }
     // elements past the tensor's end were loaded as zeros and stay zeros
-    float ms = __fdiv_rn(block_max(m), 127.f), vs = __fdiv_rn(block_max(v), 255.f);
+    float ms = __fmul_rn(block_max(m), 1.f / 127.f), vs = __fmul_rn(block_max(v), 1.f / 255.f);
     if (ms < kLeastNormal) ms = 0.f;
     if (vs < kLeastNormal) vs = 0.f;
     const float mi = ms > 0.f ? __fdiv_rn(1.f, ms) : 0.f, vi = vs > 0.f ? __fdiv_rn(1.f, vs) : 0.f;

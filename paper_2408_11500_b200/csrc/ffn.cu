@@ -30,17 +30,33 @@ namespace {
 constexpr int kPairs = 74;                       // pairs of SMs
 constexpr int kStages = 5, kStageBytes = 32768;  // A: 128 x 64 bf16, B: up to 128 x 64
 constexpr int kEpiWarps = 16, kThreads = (kEpiWarps + 2) * 32;
-constexpr int kSlabBytes = 4096;                 // of an epilogue warp: 32 rows x 128 bytes
-constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kSlabBytes + 1024 + 256;
+constexpr int kSlabBytes = 2048;                 // of an epilogue warp: 32 rows x 64 bytes
+constexpr int kBiasBytes = 256;                  // and 32 columns of both biases
+constexpr int kSmem = kStages * kStageBytes + kEpiWarps * (kSlabBytes + kBiasBytes) + 1024 + 256;
 constexpr long long kWaitClocks = 2000000000LL;  // about a second
 
 enum Mode { kFwd, kFwdGated, kDz, kDzGated, kDx, kDw };
+
+// n / d for 0 <= n < 2^31 by a multiplication
+struct Divide {
+    uint32_t mul, shift;
+    int d;
+    __device__ __forceinline__ int operator()(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+};
+Divide divide_by(int d) {
+    Divide r;
+    r.d = d;
+    for (r.shift = 0; (1ll << r.shift) < d; ++r.shift) {}
+    r.mul = (uint32_t)(((1ull << 32) * ((1ull << r.shift) - (uint64_t)d)) / (uint64_t)d + 1);
+    return r;
+}
 
 struct Params {
     CUtensorMap a, b0, b1;
     int n;                         // rows of x
     int p, slices;                 // slices; slices times parts of the output (kDw), else the same
     int tiles_m, tiles_n, group;   // per slice; m tiles that follow one another before the next n tile
+    Divide by_first, by_n, by_m, by_last;   // what item_of divides by
     int items;
     int nt;                        // columns of B per CTA: 64 or 128
     int kb_total, kb_part, k_part; // 64-wide steps of an item, of one part of k, and that part's extent
@@ -48,6 +64,7 @@ struct Params {
     int pairs;                     // products of operand parts
     int8_t ia[6], ib[6];
     int splits;                    // kDw: pieces of the rows, kb_total steps each
+    int splits_rows;               // kDw
     // epilogue
     int act, cols;                 // columns of D per slice
     float scale;
@@ -87,7 +104,7 @@ __device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok)
         : "r"(smem_u32(bar)), "r"(parity)
@@ -107,12 +124,13 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
 __device__ __forceinline__ void mbar_expect(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
-// Arrives at the same barrier of the pair's first CTA.
+// Arrives at the same barrier of the pair's first CTA.  Relaxed: what it hands over are accumulators that have been read (the wait for
+// those reads is behind this thread); a release would first wait for all results the warp has stored (17 % of all warp stalls).
 __device__ __forceinline__ void mbar_arrive_first(uint64_t* bar) {
     asm volatile(
         "{\n\t.reg .b32 a;\n\t"
         "mapa.shared::cluster.u32 a, %0, 0;\n\t"
-        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(smem_u32(bar))
+        "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(smem_u32(bar))
         : "memory");
 }
 // One box of a tensor map into this CTA's memory; the bytes are counted at the barrier of the pair's first CTA.
@@ -307,17 +325,28 @@ __device__ __forceinline__ void store_lines(const uint32_t* w, char* at, int64_t
 }
 
 // 1 / (1 + exp(-w)).  Where results are rounded to bf16 the hardware's exponential and reciprocal (2^-22 each, and 2^-24 |w| of the
-// argument) are exact enough.
+// argument) are exact enough; `t` is -w log2(e).
+__device__ __forceinline__ float sigmoid_of(float t) {
+    float e, q;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(1.f + e));
+    return q;
+}
+constexpr float kLog2e = 1.4426950408889634f, kGeluA = 0.7978845608028654f, kGeluB = 0.044715f;
 template <bool ACCURATE>
 __device__ __forceinline__ float sigmoid(float w) {
-    return ACCURATE ? 1.f / (1.f + expf(-w)) : __fdividef(1.f, 1.f + __expf(-w));
+    return ACCURATE ? 1.f / (1.f + expf(-w)) : sigmoid_of(-kLog2e * w);
 }
-constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f;
-// act(a); gelu through (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u))
+template <bool ACCURATE>
+__device__ __forceinline__ float gelu_gate(float a) {   // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u))
+    const float s = a * a;
+    return ACCURATE ? sigmoid<true>(2.f * kGeluA * a * fmaf(kGeluB, s, 1.f)) : sigmoid_of(a * fmaf(-2.f * kLog2e * kGeluA * kGeluB, s, -2.f * kLog2e * kGeluA));
+}
+// act(a)
 template <bool ACCURATE>
 __device__ __forceinline__ float act_of(int act, float a) {
     if (act == SLICEGCN_ACT_SILU) return a * sigmoid<ACCURATE>(a);
-    if (act == SLICEGCN_ACT_GELU) return a * sigmoid<ACCURATE>(2.f * kGeluA * a * fmaf(kGeluB, a * a, 1.f));
+    if (act == SLICEGCN_ACT_GELU) return a * gelu_gate<ACCURATE>(a);
     if (act == SLICEGCN_ACT_RELU) return a > 0.f || isnan(a) ? a : 0.f;
     return a;
 }
@@ -329,7 +358,7 @@ __device__ __forceinline__ void act_both(int act, float a, float& y, float& dy) 
         y = a * q;
         dy = fmaf(y, 1.f - q, q);
     } else if (act == SLICEGCN_ACT_GELU) {
-        const float q = sigmoid<ACCURATE>(2.f * kGeluA * a * fmaf(kGeluB, a * a, 1.f));
+        const float q = gelu_gate<ACCURATE>(a);
         y = a * q;
         dy = fmaf(y * (1.f - q), 2.f * kGeluA * fmaf(3.f * kGeluB, a * a, 1.f), q);
     } else if (act == SLICEGCN_ACT_RELU) {
@@ -505,6 +534,170 @@ __device__ __forceinline__ void finish_dz(const Params& P, const Where& w, int c
     if (GATED) put_dz(P, w, 1, col, c, slab, lane);
 }
 
+// ---- bf16: 32 columns at a time
+
+__device__ __forceinline__ void sts4(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory"); }
+// Sixteen numbers that every lane reads alike, added.
+__device__ __forceinline__ void add16(float (&v)[16], uint32_t at) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint4 t = lds16(at + k * 16);
+        v[4 * k] += __uint_as_float(t.x), v[4 * k + 1] += __uint_as_float(t.y);
+        v[4 * k + 2] += __uint_as_float(t.z), v[4 * k + 3] += __uint_as_float(t.w);
+    }
+}
+// Where a lane finds its row's chunk c of eight columns, and its line i of eight (row i * 8 + lane / 4, chunk lane % 4).
+__device__ __forceinline__ uint32_t own_chunk(uint32_t slab, int lane, int c) { return (slab + lane * 64 + (((lane >> 1) & 3) << 4)) ^ (c << 4); }
+__device__ __forceinline__ uint32_t own_line(uint32_t slab, int lane, int i) {
+    return slab + i * 512 + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4);
+}
+__device__ __forceinline__ void put_rows(const uint32_t* w, uint32_t slab, int lane) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) sts16(own_chunk(slab, lane, c), make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
+}
+// The slab's 32 rows x 32 columns to memory, `rows` and `cols` of them.
+__device__ __forceinline__ void slab_out(char* at, int64_t ld_bytes, int rows, int cols, bool vec, uint32_t slab, int lane) {
+    if (vec && cols >= 8) {
+        const int left = cols - (lane & 3) * 8;
+        char* to = at + (int64_t)(lane >> 2) * ld_bytes + (lane & 3) * 16;
+        if (rows == 32 && cols >= 32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(to + i * 8 * ld_bytes) = lds16(own_line(slab, lane, i));
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i * 8 + (lane >> 2) < rows && left >= 8) *reinterpret_cast<uint4*>(to + i * 8 * ld_bytes) = lds16(own_line(slab, lane, i));
+        if (cols >= 32 || cols % 8 == 0) return;
+    }
+    // element by element: all columns, or those behind the last eight
+    const int c = lane, from = vec ? min(cols, 32) & ~7 : 0;
+    if (c >= from && c < cols)
+#pragma unroll 4
+        for (int i = 0; i < rows; ++i) {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(slab + slab_at<64>(i, c >> 3) + (c & 7) * 2) : "memory");
+            *reinterpret_cast<uint16_t*>(at + (int64_t)i * ld_bytes + c * 2) = v;
+        }
+}
+// 32 rows x 32 columns of r or dout: asked for here (whole chunks where they are aligned) ...
+__device__ __forceinline__ void load_in(const Params& P, const Where& w, int col, uint4 (&raw)[4], int lane) {
+    const int left = P.cols - col - (lane & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
+    if (!P.in_vec || w.rows <= 0 || left < 8) return;
+    const char* at = static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col + (lane & 3) * 8) * 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 8 + (lane >> 2);
+        const uint4 t = *reinterpret_cast<const uint4*>(at + (int64_t)min(row, w.rows - 1) * P.in_ld * 2);
+        if (row < w.rows) raw[i] = t;
+    }
+}
+// ... and laid into the slab here, with what no whole chunk holds.
+__device__ __forceinline__ void put_in(const Params& P, const Where& w, int col, const uint4 (&raw)[4], uint32_t slab, int lane) {
+    const int cols = min(32, P.cols - col), from = P.in_vec ? max(cols, 0) & ~7 : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sts16(own_line(slab, lane, i), raw[i]);
+    if (from >= cols || w.rows <= 0) return;
+    __syncwarp();
+    const int c = lane;
+    const char* at = static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col + c) * 2;
+    if (c >= from && c < cols)
+#pragma unroll 8
+        for (int i = 0; i < w.rows; ++i) {
+            const uint16_t v = *reinterpret_cast<const uint16_t*>(at + (int64_t)i * P.in_ld * 2);
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(slab + slab_at<64>(i, c >> 3) + (c & 7) * 2), "h"(v) : "memory");
+        }
+}
+// Sixteen columns of the lane's row in the slab.
+__device__ __forceinline__ void own_row16(float (&v)[16], uint32_t slab, int lane, int h) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const uint4 t = lds16(own_chunk(slab, lane, 2 * h + q));
+        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[q * 8 + 2 * k] = __uint_as_float(w[k] << 16);
+            v[q * 8 + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+        }
+    }
+}
+
+// Half of 32 columns of a forward product (of dx: PLAIN), packed.
+template <bool GATED, bool PLAIN>
+__device__ __forceinline__ void forward_half(const Params& P, int h, float (&a)[16], const float (&c)[16], uint32_t* words, uint32_t slab, int lane) {
+    if (!PLAIN) {
+#define SGCN_ACT(A) _Pragma("unroll") for (int j = 0; j < 16; ++j) a[j] = act_of<false>(A, a[j])
+        if (P.act == SLICEGCN_ACT_SILU)
+            SGCN_ACT(SLICEGCN_ACT_SILU);
+        else if (P.act == SLICEGCN_ACT_GELU)
+            SGCN_ACT(SLICEGCN_ACT_GELU);
+        else if (P.act == SLICEGCN_ACT_RELU)
+            SGCN_ACT(SLICEGCN_ACT_RELU);
+#undef SGCN_ACT
+        if (GATED) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) a[j] *= c[j];
+        }
+    }
+    if (P.scale != 1.f) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) a[j] *= P.scale;
+    }
+    if (!PLAIN && P.in) {
+        float r[16];
+        own_row16(r, slab, lane, h);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) a[j] += r[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) words[j] = pack2(a[2 * j], a[2 * j + 1]);
+}
+// Half of 32 columns of da, which takes dout's place in the slab, and of dc, packed; their sums over the warp's rows.
+template <bool GATED>
+__device__ __forceinline__ void dz_half(const Params& P, const Where& w, int col, int h, float (&a)[16], float (&c)[16], uint32_t* words, uint32_t slab, int lane) {
+    float g[16];
+    own_row16(g, slab, lane, h);
+#define SGCN_ACT(A)                                                       \
+    _Pragma("unroll") for (int j = 0; j < 16; ++j) {                      \
+        float y, dy;                                                      \
+        act_both<false>(A, a[j], y, dy);                                  \
+        const float gj = g[j] * P.scale;                                  \
+        a[j] = GATED ? gj * c[j] * dy : gj * dy;                          \
+        if (GATED) c[j] = gj * y;                                         \
+    }
+    if (P.act == SLICEGCN_ACT_SILU) {
+        SGCN_ACT(SLICEGCN_ACT_SILU)
+    } else if (P.act == SLICEGCN_ACT_GELU) {
+        SGCN_ACT(SLICEGCN_ACT_GELU)
+    } else if (P.act == SLICEGCN_ACT_RELU) {
+        SGCN_ACT(SLICEGCN_ACT_RELU)
+    } else {
+        SGCN_ACT(SLICEGCN_ACT_NONE)
+    }
+#undef SGCN_ACT
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+        sts16(own_chunk(slab, lane, 2 * h + q), make_uint4(pack2(a[8 * q], a[8 * q + 1]), pack2(a[8 * q + 2], a[8 * q + 3]), pack2(a[8 * q + 4], a[8 * q + 5]),
+                                                           pack2(a[8 * q + 6], a[8 * q + 7])));
+    if (GATED) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) words[j] = pack2(c[2 * j], c[2 * j + 1]);
+    }
+    if (P.sums) {
+        const int at = col + (lane >> 1);
+        const bool mine = !(lane & 1) && at < P.cols && w.rows > 0;
+        float* to = P.sums + ((int64_t)(w.row >> 5) * P.slices + w.slice) * P.cols + at;
+        const float s = column_sums16(a, lane);
+        if (mine) *to = s;
+        if (GATED) {
+            const float s2 = column_sums16(c, lane);
+            if (mine) to[(int64_t)P.p * P.cols] = s2;
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------ the product
 
 struct Item {
@@ -516,19 +709,17 @@ __device__ __forceinline__ Item item_of(const Params& P, int i) {
     const int cols = 2 * P.nt;
     const int per_tile = MODE == kFwdGated || MODE == kDzGated ? P.nt : cols;   // columns of D that a tile makes
     if (MODE == kDw) {
-        const int tiles = P.slices * P.tiles_m * P.tiles_n;
-        t.split = i / tiles;
-        i -= t.split * tiles;
-        t.n = i % P.tiles_n * per_tile;
-        i /= P.tiles_n;
-        t.m = i % P.tiles_m * 256;
-        t.slice = i / P.tiles_m;
+        t.split = P.by_first(i);
+        i -= t.split * P.by_first.d;
+        const int above = P.by_n(i);
+        t.n = (i - above * P.tiles_n) * per_tile;
+        t.slice = P.by_m(above);
+        t.m = (above - t.slice * P.tiles_m) * 256;
     } else {   // `group` row tiles side by side, then the next column tile: operands come from L2 in between
-        const int sn = P.p * P.tiles_n, per = P.group * sn;
-        const int g = i / per, rest = i - g * per, size = min(P.group, P.tiles_m - g * P.group);
-        const int c = rest / size;
+        const int g = P.by_first(i), rest = i - g * P.by_first.d, size = min(P.group, P.tiles_m - g * P.group);
+        const int c = size == P.group ? P.by_m(rest) : P.by_last(rest);
         t.m = (g * P.group + rest - c * size) * 256;
-        t.slice = c / P.tiles_n;
+        t.slice = P.by_n(c);
         t.n = (c - t.slice * P.tiles_n) * per_tile;
         t.split = 0;
     }
@@ -539,11 +730,12 @@ __device__ __forceinline__ Item item_of(const Params& P, int i) {
 template <int MODE, bool PROMO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_kernel(const __grid_constant__ Params P) {
     constexpr bool kGated = MODE == kFwdGated || MODE == kDzGated;
+    constexpr bool kIsDz = MODE == kDz || MODE == kDzGated;
     constexpr bool kAK = MODE != kDw;    // A's k is contiguous
     constexpr bool kBK = MODE == kDx;    // B's
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    unsigned char* tail = smem_raw + (base - smem_u32(smem_raw)) + kStages * kStageBytes + kEpiWarps * kSlabBytes;
+    unsigned char* tail = smem_raw + (base - smem_u32(smem_raw)) + kStages * kStageBytes + kEpiWarps * (kSlabBytes + kBiasBytes);
     uint64_t* full = reinterpret_cast<uint64_t*>(tail);
     uint64_t* empty = full + kStages;
     uint64_t* tfull = empty + kStages;    // [2]
@@ -574,7 +766,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
     if (warp == kEpiWarps) {
         if (lane == 0) {
             bool ok = true;
-            int fill = 0;
+            int fill = 0, st = 0;
+            uint32_t phase = 1;
             const uint32_t bytes = 2u * (16384u + (uint32_t)P.nt * 128u);
             for (int i = first; ok && i < P.items; i += stride) {
                 const Item t = item_of<MODE>(P, i);
@@ -585,14 +778,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     const int kb0 = c * P.chunk, kb1 = min(kb0 + P.chunk, P.kb_total);
                     for (int q = 0; ok && q < P.pairs; ++q)
                         for (int kb = kb0; kb < kb1; ++kb, ++fill) {
-                            const int st = fill % kStages;
-                            if (!mbar_wait(empty + st, ((fill / kStages) & 1) ^ 1)) {
+                            if (!mbar_wait(empty + st, phase)) {
                                 ok = false;
                                 break;
                             }
                             if (rank == 0) mbar_expect(full + st, bytes);
                             const uint32_t a = base + st * kStageBytes, b = a + 16384u;
-                            const int part = MODE == kDx ? kb / P.kb_part : 0;
+                            const int part = MODE == kDx && kb >= P.kb_part;
                             const int k = MODE == kDw ? (t.split * P.kb_total + kb) * 64 : (kb - part * P.kb_part) * 64;
                             if (kAK)
                                 tma_load(a, &P.a, k, row0, part * P.p + slice, P.ia[q], full + st);
@@ -603,6 +795,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                                 tma_load(b, bm, k, bcol, slice, P.ib[q], full + st);
                             else
                                 for (int j = 0; j < P.nt / 64; ++j) tma_load(b + j * 8192, bm, bcol + 64 * j, k, slice, P.ib[q], full + st);
+                            if (++st == kStages) st = 0, phase ^= 1;
                         }
                 }
             }
@@ -613,7 +806,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
     } else if (warp == kEpiWarps + 1) {
         if (lane == 0 && rank == 0) {
             bool ok = true;
-            int fill = 0, use = 0;
+            int use = 0, st = 0;
+            uint32_t phase = 0;
             const uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | (kAK ? 0u : 1u << 15) | (kBK ? 0u : 1u << 16) | (uint32_t)(2 * P.nt >> 3) << 17 | 16u << 24;
             for (int i = first; ok && i < P.items; i += stride) {
                 for (int c = 0; ok && c < chunks; ++c, ++use) {
@@ -626,31 +820,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     fence_after();
                     bool more = false;
                     for (int q = 0; ok && q < P.pairs; ++q)
-                        for (int kb = kb0; kb < kb1; ++kb, ++fill) {
-                            const int st = fill % kStages;
-                            if (!mbar_wait(full + st, (fill / kStages) & 1)) {
+                        for (int kb = kb0; kb < kb1; ++kb) {
+                            if (!mbar_wait(full + st, phase)) {
                                 ok = false;
                                 break;
                             }
                             fence_after();
                             const uint32_t at = base + st * kStageBytes;
                             const uint64_t ad = tile_desc(at, kAK), bd = tile_desc(at + 16384u, kBK);
-                            const int k = (kb % P.kb_part) * 64;
+                            const int k = (kb >= P.kb_part ? kb - P.kb_part : kb) * 64;
                             const int steps = MODE == kDw ? 4 : min(4, (P.k_part - k + 15) / 16);   // past the end there are only zeros
                             for (int s = 0; s < steps; ++s, more = true)
                                 umma(d, ad + (uint64_t)(s * (kAK ? 2 : 128)), bd + (uint64_t)(s * (kBK ? 2 : 128)), idesc, more);
                             umma_commit(empty + st);
+                            if (++st == kStages) st = 0, phase ^= 1;
                         }
                     umma_commit(tfull + (use & 1));
                 }
             }
             if (!ok) {   // the copies on their way, before this memory is given up
-                for (int s = 0; s < kStages; ++s, ++fill) mbar_wait(full + fill % kStages, (fill / kStages) & 1);
+                for (int s = 0; s < kStages; ++s) {
+                    mbar_wait(full + st, phase);
+                    if (++st == kStages) st = 0, phase ^= 1;
+                }
                 if (P.status) atomicExch(P.status, SLICEGCN_DEVSTATUS_WAIT);
             }
         }
     } else {
         const uint32_t slab = base + kStages * kStageBytes + warp * kSlabBytes;
+        const uint32_t biases = base + kStages * kStageBytes + kEpiWarps * kSlabBytes + warp * kBiasBytes;
         const int quarter = warp & 3, part = warp >> 2;   // 32 rows of the tile, and a share of its columns
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         // columns of D per warp, and where they start in the accumulator; gated: c's lie nt further on
@@ -733,41 +931,95 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     }
                 }
             } else {
+                // what the columns need besides the product is on its way while the product is waited for
+                const int units = busy ? share / 32 : 0;
+                float bias[2] = {0.f, 0.f}, bias2 = 0.f;
+                uint4 raw[4];
+                const bool with_in = kIsDz || (MODE != kDx && P.in);
+                if (units > 0) {
+                    const int64_t bat = (int64_t)t.slice * P.cols;
+                    if (MODE != kDx) {
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int c = w.col + u * 32 + lane;
+                            if (u < units && P.b && c < P.cols) bias[u] = __ldg(P.b + bat + c);
+                        }
+                        if (kGated && P.b2 && w.col + lane < P.cols) bias2 = __ldg(P.b2 + bat + w.col + lane);
+                    }
+                    if (with_in) load_in(P, w, w.col, raw, lane);
+                }
                 if (!mbar_wait(tfull + (use & 1), (use >> 1) & 1)) {
                     ok = false;
                     break;
                 }
                 fence_after();
                 const uint32_t d = tmem + (use & 1) * 256 + lanes + part * share;
-                constexpr int U = MODE == kDz || MODE == kDzGated ? 16 : 32;
-                const int units = busy ? share / U : 0;
                 for (int u = 0; u < units; ++u) {
-                    const int col = w.col + u * U;
-                    uint32_t ra[U], rc[U];
-#pragma unroll
-                    for (int h = 0; h < U / 16; ++h) {
-                        tmem_ld16(d + u * U + h * 16, ra + h * 16);
-                        if (kGated) tmem_ld16(d + u * U + h * 16 + P.nt, rc + h * 16);
-                    }
-                    tmem_wait(ra);
-#pragma unroll
-                    for (int h = 0; h < U / 16; ++h) {
-                        if (h) after_wait(ra + h * 16);
-                        if (kGated) after_wait(rc + h * 16);
-                    }
-                    float a[U], cc[U];
-#pragma unroll
-                    for (int j = 0; j < U; ++j) a[j] = __uint_as_float(ra[j]), cc[j] = kGated ? __uint_as_float(rc[j]) : 0.f;
-                    if (u == units - 1) {
-                        fence_before();
+                    const int col = w.col + u * 32;
+                    const bool last = u == units - 1, there = col < P.cols && w.rows > 0;
+                    uint32_t ra[16], rc[16];
+                    tmem_ld16(d + u * 32, ra);
+                    if (kGated) tmem_ld16(d + u * 32 + P.nt, rc);
+                    if (MODE != kDx) {
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_first(tempty + (use & 1));
+                        sts4(biases + lane * 4, u ? bias[1] : bias[0]);
+                        if (kGated) sts4(biases + 128 + lane * 4, bias2);
                     }
-                    if (col >= P.cols || w.rows <= 0) continue;
-                    if constexpr (MODE == kDz || MODE == kDzGated)
-                        finish_dz<kGated, false>(P, w, col, a, cc, slab, lane);
-                    else
-                        finish_forward<32, kGated, false>(P, w, col, a, cc, slab, lane);
+                    if (with_in) put_in(P, w, col, raw, slab, lane);
+                    __syncwarp();
+                    tmem_wait(ra);
+                    if (kGated) after_wait(rc);
+                    uint32_t words[16], words2[16];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t na[16], nc[16];
+                        if (h == 0) {   // the second half's numbers come while the first half's are worked on
+                            tmem_ld16(d + u * 32 + 16, na);
+                            if (kGated) tmem_ld16(d + u * 32 + 16 + P.nt, nc);
+                        }
+                        float a[16], c[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) a[j] = __uint_as_float(ra[j]), c[j] = kGated ? __uint_as_float(rc[j]) : 0.f;
+                        if (MODE != kDx) {
+                            add16(a, biases + h * 64);
+                            if (kGated) add16(c, biases + 128 + h * 64);
+                        }
+                        if constexpr (kIsDz)
+                            dz_half<kGated>(P, w, col + 16 * h, h, a, c, words2 + 8 * h, slab, lane);
+                        else
+                            forward_half<kGated, MODE == kDx>(P, h, a, c, words + 8 * h, slab, lane);
+                        if (h == 0) {
+                            tmem_wait(na);
+                            if (kGated) after_wait(nc);
+                            if (last) {
+                                fence_before();
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive_first(tempty + (use & 1));
+                            }
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) ra[j] = na[j], rc[j] = kGated ? nc[j] : 0u;
+                        }
+                    }
+                    if (with_in && !last) load_in(P, w, col + 32, raw, lane);
+                    if constexpr (kIsDz) {
+                        if (there) {
+                            __nv_bfloat16* at = P.dz + (int64_t)w.row * P.dz_row + (int64_t)w.slice * P.dz_pad + col;
+                            __syncwarp();
+                            slab_out(reinterpret_cast<char*>(at), P.dz_row * 2, w.rows, P.dz_pad - col, true, slab, lane);
+                            if (kGated) {
+                                __syncwarp();
+                                put_rows(words2, slab, lane);
+                                __syncwarp();
+                                slab_out(reinterpret_cast<char*>(at + (int64_t)P.p * P.dz_pad), P.dz_row * 2, w.rows, P.dz_pad - col, true, slab, lane);
+                            }
+                        }
+                    } else if (there) {
+                        __syncwarp();
+                        put_rows(words, slab, lane);
+                        __syncwarp();
+                        slab_out(static_cast<char*>(P.out) + ((int64_t)w.row * P.out_ld + (int64_t)w.slice * P.cols + col) * 2, P.out_ld * 2, w.rows, P.cols - col,
+                                 P.out_vec, slab, lane);
+                    }
                 }
                 if (units == 0 && lane == 0) mbar_arrive_first(tempty + (use & 1));
                 ++use;
@@ -1073,6 +1325,15 @@ slicegcn_status_t item_count(Params& P) {
     const int64_t items = (int64_t)P.slices * P.tiles_m * P.tiles_n * P.splits;
     if (items > (1 << 30)) SGCN_FAIL(SLICEGCN_ERR_OVERFLOW, "ffn: too many tiles");
     P.items = (int)items;
+    P.by_n = divide_by(P.tiles_n);
+    if (P.splits_rows) {
+        P.by_first = divide_by(P.slices * P.tiles_m * P.tiles_n);
+        P.by_m = P.by_last = divide_by(P.tiles_m);
+    } else {
+        P.by_first = divide_by(P.group * P.slices * P.tiles_n);
+        P.by_m = divide_by(P.group);
+        P.by_last = divide_by(std::max(1, P.tiles_m % P.group));
+    }
     return SLICEGCN_OK;
 }
 
@@ -1101,7 +1362,7 @@ slicegcn_status_t operands(const slicegcn_ffn_desc* d, const Plan& q, const void
 // The product a = x W (and c = x W2) and its epilogue.
 slicegcn_status_t forward_product(Params& P, const slicegcn_ffn_desc* d, const Plan& q, const Operand& ox, const Operand& ow, const Operand& ow2, bool back,
                                   cudaStream_t st) {
-    const bool gated = d->W2 != nullptr, promo = d->dtype == SLICEGCN_F32;
+    const bool gated = d->W2 != nullptr, promo = d->dtype == SLICEGCN_F32 || (back && d->grad_dtype == SLICEGCN_F32);
     set_tiles(P, d->n, d->num_slices, d->out_s, gated);
     SGCN_TRY(item_count(P));
     SGCN_TRY(make_map(&P.a, ox, 128));
@@ -1110,7 +1371,7 @@ slicegcn_status_t forward_product(Params& P, const slicegcn_ffn_desc* d, const P
     P.kb_total = P.kb_part = ceil_div(d->in_s, 64);
     P.k_part = d->in_s;
     set_pairs(P, q.x_planes, q.w_planes);
-    P.chunk = promo ? kChunkF32 : P.kb_total;
+    P.chunk = P.pairs > 1 ? kChunkF32 : P.kb_total;
     P.act = d->act, P.scale = (float)d->scale, P.b = d->b, P.b2 = d->b2;
     if (back) {
         P.slices = q.parts * d->num_slices;   // of the sums
@@ -1233,7 +1494,7 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         P.n = d->out_s, P.p = p, P.slices = q.parts * p, P.cols = d->out_s, P.k_part = d->in_s;
         P.nt = q.dw_nt, P.tiles_m = ceil_div(d->out_s, 256), P.tiles_n = ceil_div(d->in_s, 2 * P.nt), P.group = 1;
         P.kb_total = P.kb_part = ceil_div(ceil_div(n, 64), q.splits);
-        P.splits = q.splits;
+        P.splits = q.splits, P.splits_rows = 1;
         SGCN_TRY(item_count(P));
         SGCN_TRY(make_map(&P.a, oz, 64));
         SGCN_TRY(make_map(&P.b0, ox, 64));
