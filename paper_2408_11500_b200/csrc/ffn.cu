@@ -97,6 +97,11 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ void mbar_init(uint64_t* bar, int count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
 }
@@ -741,7 +746,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
     uint64_t* tfull = empty + kStages;    // [2]
     uint64_t* tempty = tfull + 2;         // [2]
     uint32_t* tmem_at = reinterpret_cast<uint32_t*>(tempty + 2);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int first = blockIdx.x >> 1, stride = gridDim.x >> 1;
 
@@ -763,48 +768,56 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
     cudaTriggerProgrammaticLaunchCompletion();
 
     const int chunks = (P.kb_total + P.chunk - 1) / P.chunk;
+    // The two issuing warps walk their loops as whole warps, and one lane issues: what copies and MMAs are given then stays in
+    // uniform registers.  (One lane in a loop of its own: 880 cycles per 64-wide step where the MMAs take 512.)
     if (warp == kEpiWarps) {
-        if (lane == 0) {
-            bool ok = true;
-            int fill = 0, st = 0;
-            uint32_t phase = 1;
-            const uint32_t bytes = 2u * (16384u + (uint32_t)P.nt * 128u);
-            for (int i = first; ok && i < P.items; i += stride) {
-                const Item t = item_of<MODE>(P, i);
-                const int row0 = t.m + (int)rank * 128;
-                const int slice = MODE == kDw ? t.slice % P.p : t.slice;
-                const int bcol = kGated ? t.n : t.n + (int)rank * P.nt;
-                for (int c = 0; ok && c < chunks; ++c) {
-                    const int kb0 = c * P.chunk, kb1 = min(kb0 + P.chunk, P.kb_total);
-                    for (int q = 0; ok && q < P.pairs; ++q)
-                        for (int kb = kb0; kb < kb1; ++kb, ++fill) {
-                            if (!mbar_wait(empty + st, phase)) {
-                                ok = false;
-                                break;
-                            }
+        const bool one = elect_one();
+        bool ok = true;
+        int fill = 0, st = 0;
+        uint32_t phase = 1;
+        const uint32_t bytes = 2u * (16384u + (uint32_t)P.nt * 128u);
+        const CUtensorMap* other = kGated && rank ? &P.b1 : &P.b0;
+        for (int i = first; ok && i < P.items; i += stride) {
+            const Item t = item_of<MODE>(P, i);
+            const int row0 = t.m + (int)rank * 128;
+            const int slice = MODE == kDw && t.slice >= P.p ? t.slice - P.p : t.slice;
+            const int bcol = kGated ? t.n : t.n + (int)rank * P.nt;
+            const int k0 = MODE == kDw ? t.split * P.kb_total * 64 : 0;
+            for (int c = 0; ok && c < chunks; ++c) {
+                const int kb0 = c * P.chunk, kb1 = min(kb0 + P.chunk, P.kb_total);
+                for (int q = 0; ok && q < P.pairs; ++q)
+                    for (int kb = kb0; kb < kb1; ++kb, ++fill) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(empty + st, phase));
+                        if (!ok) break;
+                        const uint32_t a = base + st * kStageBytes, b = a + 16384u;
+                        const bool second = MODE == kDx && kb >= P.kb_part;
+                        const int k = k0 + (second ? kb - P.kb_part : kb) * 64;
+                        if (one) {
                             if (rank == 0) mbar_expect(full + st, bytes);
-                            const uint32_t a = base + st * kStageBytes, b = a + 16384u;
-                            const int part = MODE == kDx && kb >= P.kb_part;
-                            const int k = MODE == kDw ? (t.split * P.kb_total + kb) * 64 : (kb - part * P.kb_part) * 64;
-                            if (kAK)
-                                tma_load(a, &P.a, k, row0, part * P.p + slice, P.ia[q], full + st);
-                            else
-                                for (int j = 0; j < 2; ++j) tma_load(a + j * 8192, &P.a, row0 + 64 * j, k, t.slice, P.ia[q], full + st);
-                            const CUtensorMap* bm = (kGated && rank) || part ? &P.b1 : &P.b0;
-                            if (kBK)
-                                tma_load(b, bm, k, bcol, slice, P.ib[q], full + st);
-                            else
-                                for (int j = 0; j < P.nt / 64; ++j) tma_load(b + j * 8192, bm, bcol + 64 * j, k, slice, P.ib[q], full + st);
-                            if (++st == kStages) st = 0, phase ^= 1;
+                            if (kAK) {
+                                tma_load(a, &P.a, k, row0, second ? P.p + slice : slice, P.ia[q], full + st);
+                            } else {
+                                tma_load(a, &P.a, row0, k, t.slice, P.ia[q], full + st);
+                                tma_load(a + 8192, &P.a, row0 + 64, k, t.slice, P.ia[q], full + st);
+                            }
+                            if (kBK) {
+                                tma_load(b, second ? &P.b1 : &P.b0, k, bcol, slice, P.ib[q], full + st);
+                            } else {
+                                tma_load(b, other, bcol, k, slice, P.ib[q], full + st);
+                                if (P.nt > 64) tma_load(b + 8192, other, bcol + 64, k, slice, P.ib[q], full + st);
+                            }
                         }
-                }
+                        __syncwarp();
+                        if (++st == kStages) st = 0, phase ^= 1;
+                    }
             }
-            // the pair's last arrivals at this CTA's barriers, before its memory is given up
-            for (int s = max(0, fill - kStages); ok && s < fill; ++s) ok = mbar_wait(empty + s % kStages, (s / kStages) & 1);
-            if (!ok && P.status) atomicExch(P.status, SLICEGCN_DEVSTATUS_WAIT);
         }
+        // the pair's last arrivals at this CTA's barriers, before its memory is given up
+        for (int s = max(0, fill - kStages); ok && s < fill; ++s) ok = mbar_wait(empty + s % kStages, (s / kStages) & 1);
+        if (!ok && P.status) atomicExch(P.status, SLICEGCN_DEVSTATUS_WAIT);
     } else if (warp == kEpiWarps + 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
+            const bool one = elect_one();
             bool ok = true;
             int use = 0, st = 0;
             uint32_t phase = 0;
@@ -813,29 +826,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                 for (int c = 0; ok && c < chunks; ++c, ++use) {
                     const int kb0 = c * P.chunk, kb1 = min(kb0 + P.chunk, P.kb_total);
                     const uint32_t d = tmem + (use & 1) * 256;
-                    if (!mbar_wait(tempty + (use & 1), ((use >> 1) & 1) ^ 1)) {
-                        ok = false;
-                        break;
-                    }
+                    ok = __all_sync(0xffffffffu, mbar_wait(tempty + (use & 1), ((use >> 1) & 1) ^ 1));
+                    if (!ok) break;
                     fence_after();
                     bool more = false;
                     for (int q = 0; ok && q < P.pairs; ++q)
                         for (int kb = kb0; kb < kb1; ++kb) {
-                            if (!mbar_wait(full + st, phase)) {
-                                ok = false;
-                                break;
-                            }
+                            ok = __all_sync(0xffffffffu, mbar_wait(full + st, phase));
+                            if (!ok) break;
                             fence_after();
                             const uint32_t at = base + st * kStageBytes;
                             const uint64_t ad = tile_desc(at, kAK), bd = tile_desc(at + 16384u, kBK);
-                            const int k = (kb >= P.kb_part ? kb - P.kb_part : kb) * 64;
-                            const int steps = MODE == kDw ? 4 : min(4, (P.k_part - k + 15) / 16);   // past the end there are only zeros
-                            for (int s = 0; s < steps; ++s, more = true)
-                                umma(d, ad + (uint64_t)(s * (kAK ? 2 : 128)), bd + (uint64_t)(s * (kBK ? 2 : 128)), idesc, more);
-                            umma_commit(empty + st);
+                            const int left = MODE == kDw ? 64 : P.k_part - (kb >= P.kb_part ? kb - P.kb_part : kb) * 64;   // past the end there are only zeros
+                            if (one) {
+#pragma unroll
+                                for (int s = 0; s < 4; ++s)
+                                    if (s * 16 < left) umma(d, ad + (uint64_t)(s * (kAK ? 2 : 128)), bd + (uint64_t)(s * (kBK ? 2 : 128)), idesc, s > 0 || more);
+                                umma_commit(empty + st);
+                            }
+                            __syncwarp();
+                            more = true;
                             if (++st == kStages) st = 0, phase ^= 1;
                         }
-                    umma_commit(tfull + (use & 1));
+                    if (one) umma_commit(tfull + (use & 1));
+                    __syncwarp();
                 }
             }
             if (!ok) {   // the copies on their way, before this memory is given up
