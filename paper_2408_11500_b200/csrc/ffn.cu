@@ -30,9 +30,8 @@ namespace {
 constexpr int kPairs = 74;                       // pairs of SMs
 constexpr int kStages = 5, kStageBytes = 32768;  // A: 128 x 64 bf16, B: up to 128 x 64
 constexpr int kEpiWarps = 16, kThreads = (kEpiWarps + 2) * 32;
-constexpr int kSlabBytes = 2048;                 // of an epilogue warp: 32 rows x 64 bytes
-constexpr int kBiasBytes = 256;                  // and 32 columns of both biases
-constexpr int kSmem = kStages * kStageBytes + kEpiWarps * (kSlabBytes + kBiasBytes) + 1024 + 256;
+constexpr int kSlabBytes = 4096;                 // of an epilogue warp: twice 32 rows x 64 bytes
+constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kSlabBytes + 1024 + 256;
 constexpr long long kWaitClocks = 2000000000LL;  // about a second
 
 enum Mode { kFwd, kFwdGated, kDz, kDzGated, kDx, kDw };
@@ -69,16 +68,17 @@ struct Params {
     int act, cols;                 // columns of D per slice
     float scale;
     const float *b, *b2;           // [slices][cols]
+    int bias_vec;                  // two of them at a time are aligned
     const void* in;                // r or dout
     int64_t in_ld;
-    int in_bf16, in_vec;
+    int in_vec;
     void* out;
     int64_t out_ld;
     int out_bf16, out_vec;
     // kDz: planes of da (and dc after it) in the workspace, and sums over 32 rows each
     __nv_bfloat16* dz;
     int64_t dz_plane, dz_row;      // elements between planes and between rows
-    int dz_planes, dz_pad;         // columns of one (part, slice)
+    int dz_pad;                    // columns of one (part, slice)
     float* sums;                   // [ceil(n/32)][parts * p][cols], or NULL
     // kDw
     float* partial;                // [splits][slices][k][cols of A]
@@ -169,6 +169,15 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* r) {
         : "r"(addr)
         : "memory");
 }
+// 16 lanes x 32 columns as fragments of 8x8 matrices
+__device__ __forceinline__ void tmem_fragments(uint32_t addr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+}
 // The wait takes part in the registers' dataflow, so that no use of them moves in front of it.
 #define SGCN_R16(r)                                                                                                                              \
     "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), \
@@ -185,14 +194,19 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, bool k_contiguous) 
 }
 
 // ------------------------------------------------------------------------------------------ pieces of the epilogue
+//
+// A warp works on units of 32 rows x 32 columns, in halves of 16 rows.  Its registers hold them as tensor memory's 16x256b form, the
+// form of 8x8 matrix fragments, gives them: v[4 j + 2 q + e] is row 8 q + lane / 4, column 8 j + 2 (lane % 4) + e.  A lane then
+// needs the biases of eight columns only and adds up columns mostly within itself (a row per lane took 64 broadcast reads of biases
+// and 136 instructions per 32 columns' sums; the gated forward's epilogue fell from 552 instructions a unit to under 400), and 8x8
+// matrix loads and stores bring bf16 fragments to shared memory, from where they leave in whole lines.
 
-// A warp's 32 rows x UB bytes pass through its slab, so that lanes that hold a row each meet global memory in whole lines.
-template <int UB>
-__device__ __forceinline__ uint32_t slab_at(int row, int chunk) {   // bank-conflict free both by rows and by lines
-    constexpr int per = UB / 16;
-    const int swz = per == 8 ? row & 7 : per == 4 ? (row >> 1) & 3 : (row >> 2) & 1;
-    return (uint32_t)(row * UB + ((chunk ^ swz) << 4));
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&t);
 }
+// A slab: 32 rows of 64 bytes, 16-byte chunks exchanged so that neither matrices nor lines meet bank conflicts.
+__device__ __forceinline__ uint32_t slab_at(int row, int chunk) { return (uint32_t)(row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4)); }
 __device__ __forceinline__ void sts16(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -201,132 +215,173 @@ __device__ __forceinline__ uint4 lds16(uint32_t a) {
     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
 }
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&t);
+// Line i of eight rows: row 8 i + lane / 4, chunk lane % 4.
+__device__ __forceinline__ uint32_t line_at(uint32_t slab, int lane, int i) { return slab + i * 512 + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4); }
+// Where this lane points for the four 8x8 matrices of half h and columns 16 q .. 16 q + 15.
+__device__ __forceinline__ uint32_t matrix_at(uint32_t slab, int lane, int h, int q) {
+    return slab + h * 1024 + ((lane >> 3) & 1) * 512 + (lane & 7) * 64 + (((2 * q + (lane >> 4)) ^ ((lane >> 1) & 3)) << 4);
+}
+__device__ __forceinline__ void half_to_slab(const uint32_t (&w)[8], uint32_t slab, int lane, int h) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+        asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(matrix_at(slab, lane, h, q)), "r"(w[4 * q]), "r"(w[4 * q + 1]),
+                     "r"(w[4 * q + 2]), "r"(w[4 * q + 3])
+                     : "memory");
+}
+__device__ __forceinline__ void half_from_slab(float (&v)[16], uint32_t slab, int lane, int h) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        uint32_t w[4];
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                     : "r"(matrix_at(slab, lane, h, q))
+                     : "memory");
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[8 * q + 2 * k] = __uint_as_float(w[k] << 16), v[8 * q + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void pack_half(const float (&v)[16], uint32_t (&w)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = pack2(v[2 * k], v[2 * k + 1]);
 }
 
-// U columns x 32 rows of a matrix as the lines a warp reads them; `rows` and `cols` are what exists of them.
-template <int U, bool BF16>
-struct Lines {
-    static constexpr int UB = U * (BF16 ? 2 : 4), per = UB / 16;
-    uint4 raw[per];
-    __device__ __forceinline__ void load(const char* at, int64_t ld_bytes, int rows, int cols, bool vec, uint32_t slab, int lane) {
-        constexpr int E = BF16 ? 2 : 4;
-        if (vec) {
-#pragma unroll
-            for (int i = 0; i < per; ++i) {
-                const int row = i * (32 / per) + lane / per, c = lane % per;
-                const int left = cols * E - c * 16;
-                const char* src = at + (int64_t)(row < rows ? row : 0) * ld_bytes + c * 16;
-                raw[i] = make_uint4(0, 0, 0, 0);
-                if (row < rows && left > 0) {
-                    if (left >= 16)
-                        raw[i] = *reinterpret_cast<const uint4*>(src);
-                    else {
-                        uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-                        for (int k = 0; k < 16 / E; ++k)
-                            if (k * E < left) {
-                                if (BF16)
-                                    w[k / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(src)[k] << (16 * (k & 1));
-                                else
-                                    w[k & 3] = reinterpret_cast<const uint32_t*>(src)[k];
-                            }
-                        raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                }
-            }
-        } else {   // element by element, a row (U = 16: two rows) at a time; they go to the slab at once
-            __syncwarp();
-#pragma unroll 8
-            for (int i = 0; i < U; ++i) {
-                const int row = i * (32 / U) + lane / U, c = lane % U;
-                const bool there = row < rows && c < cols;
-                const uint32_t to = slab + slab_at<UB>(row, c * E / 16) + (uint32_t)(c * E % 16);
-                if (BF16) {
-                    const uint16_t v = there ? *reinterpret_cast<const uint16_t*>(at + (int64_t)row * ld_bytes + c * 2) : (uint16_t)0;
-                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"(v) : "memory");
-                } else {
-                    const uint32_t v = there ? *reinterpret_cast<const uint32_t*>(at + (int64_t)row * ld_bytes + c * 4) : 0u;
-                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(v) : "memory");
-                }
-            }
-        }
-    }
-    // The lane's own row.
-    __device__ __forceinline__ void row(float* v, bool vec, uint32_t slab, int lane) {
-        if (vec) {
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < per; ++i) sts16(slab + slab_at<UB>(i * (32 / per) + lane / per, lane % per), raw[i]);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int c = 0; c < per; ++c) {
-            const uint4 t = lds16(slab + slab_at<UB>(lane, c));
-            const uint32_t w[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (BF16) {
-                    v[c * 8 + 2 * k] = __uint_as_float(w[k] << 16);
-                    v[c * 8 + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-                } else {
-                    v[c * 4 + k] = __uint_as_float(w[k]);
-                }
-            }
-        }
-    }
+struct Where {
+    int slice, row;        // first of the warp's 32 rows in D
+    int rows;              // how many of them exist
 };
 
-// The lanes' rows of U words or halves to memory.
-template <int U, bool BF16>
-__device__ __forceinline__ void store_lines(const uint32_t* w, char* at, int64_t ld_bytes, int rows, int cols, bool vec, uint32_t slab, int lane) {
-    constexpr int E = BF16 ? 2 : 4, UB = U * E, per = UB / 16;
-    __syncwarp();
+// Lines [from, to) of the slab to memory; of its 32 rows x 32 columns `rows` and `cols` exist.
+__device__ __forceinline__ void slab_out(__nv_bfloat16* at, int64_t ld, int rows, int cols, bool vec, uint32_t slab, int lane, int from, int to) {
+    if (vec && cols >= 8) {
+        __nv_bfloat16* p = at + (int64_t)(8 * from + (lane >> 2)) * ld + (lane & 3) * 8;
+        const bool mine = cols >= 32 || cols - (lane & 3) * 8 >= 8;
 #pragma unroll
-    for (int c = 0; c < per; ++c) sts16(slab + slab_at<UB>(lane, c), make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
-    __syncwarp();
-    if (vec) {
-#pragma unroll
-        for (int i = 0; i < per; ++i) {
-            const int row = i * (32 / per) + lane / per, c = lane % per;
-            const int left = cols * E - c * 16;
-            if (row >= rows || left <= 0) continue;
-            const uint4 t = lds16(slab + slab_at<UB>(row, c));
-            char* dst = at + (int64_t)row * ld_bytes + c * 16;
-            if (left >= 16)
-                *reinterpret_cast<uint4*>(dst) = t;
-            else {
-                const uint32_t v[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-                for (int k = 0; k < 16 / E; ++k)
-                    if (k * E < left) {
-                        if (BF16)
-                            reinterpret_cast<uint16_t*>(dst)[k] = (uint16_t)(v[k / 2] >> (16 * (k & 1)));
-                        else
-                            reinterpret_cast<uint32_t*>(dst)[k] = v[k & 3];
-                    }
-            }
+        for (int i = 0; i < 4; ++i) {
+            if (i < from || i >= to) continue;
+            if (mine && (rows == 32 || i * 8 + (lane >> 2) < rows)) *reinterpret_cast<uint4*>(p) = lds16(line_at(slab, lane, i));
+            p += 8 * ld;
         }
-    } else {
+        if (cols >= 32 || cols % 8 == 0) return;
+    }
+    // element by element: all columns, or those behind the last eight
+    const int first = vec ? min(cols, 32) & ~7 : 0;
+    if (lane >= first && lane < cols)
+#pragma unroll 4
+        for (int i = 8 * from; i < min(rows, 8 * to); ++i) {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(slab + slab_at(i, lane >> 3) + (lane & 7) * 2) : "memory");
+            reinterpret_cast<uint16_t*>(at)[(int64_t)i * ld + lane] = v;
+        }
+}
+// 32 rows x 32 columns of r or dout in bf16: asked for here (whole chunks, where they are aligned) ...
+__device__ __forceinline__ void load_in(const Params& P, const Where& w, int col, uint4 (&raw)[4], int lane) {
+    const int left = P.cols - col - (lane & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
+    if (!P.in_vec || w.rows <= 0 || left < 8) return;
+    const char* at = static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col + (lane & 3) * 8) * 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 8 + (lane >> 2);
+        const uint4 t = *reinterpret_cast<const uint4*>(at + (int64_t)min(row, w.rows - 1) * P.in_ld * 2);
+        if (row < w.rows) raw[i] = t;
+    }
+}
+// ... and laid into the slab here, with what no whole chunk holds.
+__device__ __forceinline__ void put_in(const Params& P, const Where& w, int col, const uint4 (&raw)[4], uint32_t slab, int lane) {
+    const int cols = min(32, P.cols - col), from = P.in_vec ? max(cols, 0) & ~7 : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sts16(line_at(slab, lane, i), raw[i]);
+    if (from >= cols || w.rows <= 0) return;
+    __syncwarp();
+    if (lane >= from && lane < cols) {
+        const uint16_t* at = static_cast<const uint16_t*>(P.in) + (int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col + lane;
 #pragma unroll 8
-        for (int i = 0; i < U; ++i) {
-            const int row = i * (32 / U) + lane / U, c = lane % U;
-            const uint32_t from = slab + slab_at<UB>(row, c * E / 16) + (uint32_t)(c * E % 16);
-            if (row < rows && c < cols) {
-                if (BF16) {
-                    uint16_t v;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(from) : "memory");
-                    *reinterpret_cast<uint16_t*>(at + (int64_t)row * ld_bytes + c * 2) = v;
-                } else {
-                    uint32_t v;
-                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(from) : "memory");
-                    *reinterpret_cast<uint32_t*>(at + (int64_t)row * ld_bytes + c * 4) = v;
-                }
+        for (int i = 0; i < w.rows; ++i) {
+            const uint16_t v = at[(int64_t)i * P.in_ld];
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(slab + slab_at(i, lane >> 3) + (lane & 7) * 2), "h"(v) : "memory");
+        }
+    }
+}
+// fp32 fragments and memory: four lanes share an aligned 32 bytes, so that no detour pays.
+__device__ __forceinline__ void load_half_f32(const Params& P, const Where& w, int col, int h, float (&v)[16], int lane) {
+    const float* at = static_cast<const float*>(P.in) + (int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int c = col + 8 * (k >> 1) + 2 * (lane & 3), row = 16 * h + 8 * (k & 1) + (lane >> 2);
+        const float* p = at + (int64_t)row * P.in_ld + c;
+        v[2 * k] = v[2 * k + 1] = 0.f;
+        if (row < w.rows) {
+            if (P.in_vec && c + 1 < P.cols) {
+                const float2 t = *reinterpret_cast<const float2*>(p);
+                v[2 * k] = t.x, v[2 * k + 1] = t.y;
+            } else {
+                if (c < P.cols) v[2 * k] = p[0];
+                if (c + 1 < P.cols) v[2 * k + 1] = p[1];
             }
         }
     }
+}
+__device__ __forceinline__ void store_half_f32(const Params& P, const Where& w, int col, int h, const float (&v)[16], int lane) {
+    float* at = static_cast<float*>(P.out) + (int64_t)w.row * P.out_ld + (int64_t)w.slice * P.cols;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int c = col + 8 * (k >> 1) + 2 * (lane & 3), row = 16 * h + 8 * (k & 1) + (lane >> 2);
+        float* p = at + (int64_t)row * P.out_ld + c;
+        if (row < w.rows) {
+            if (P.out_vec && c + 1 < P.cols) {
+                *reinterpret_cast<float2*>(p) = make_float2(v[2 * k], v[2 * k + 1]);
+            } else {
+                if (c < P.cols) p[0] = v[2 * k];
+                if (c + 1 < P.cols) p[1] = v[2 * k + 1];
+            }
+        }
+    }
+}
+// The biases of this lane's eight columns of a unit.
+__device__ __forceinline__ void load_bias(const Params& P, const float* b, int slice, int col, float (&v)[8], int lane) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    if (!b) return;
+    const float* at = b + (int64_t)slice * P.cols;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int c = col + 8 * j + 2 * (lane & 3);
+        if (P.bias_vec) {
+            if (c < P.cols) {
+                const float2 t = __ldg(reinterpret_cast<const float2*>(at + c));
+                v[2 * j] = t.x, v[2 * j + 1] = t.y;
+            }
+        } else {
+            if (c < P.cols) v[2 * j] = __ldg(at + c);
+            if (c + 1 < P.cols) v[2 * j + 1] = __ldg(at + c + 1);
+        }
+    }
+}
+__device__ __forceinline__ void add_bias(float (&v)[16], const float (&b)[8]) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] += b[(k >> 2) * 2 + (k & 1)];
+}
+// Column sums of a unit: each lane's over its rows, then over the eight lanes that hold the same columns, each of which ends with one.
+__device__ __forceinline__ void sum_half(const float (&v)[16], float (&s)[8]) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s[(k >> 2) * 2 + (k & 1)] += v[k];
+}
+__device__ __forceinline__ float sum_lanes(float (&s)[8], int lane) {   // of column 8 (k >> 1) + 2 (lane % 4) + (k & 1), k = sum_column(lane)
+#pragma unroll
+    for (int half = 4, mask = 16; half >= 1; half >>= 1, mask >>= 1) {
+        const bool upper = lane & mask;
+#pragma unroll
+        for (int j = 0; j < half; ++j) {
+            const float keep = upper ? s[j + half] : s[j], give = upper ? s[j] : s[j + half];
+            s[j] = keep + __shfl_xor_sync(0xffffffffu, give, mask);
+        }
+    }
+    return s[0];
+}
+__device__ __forceinline__ int sum_column(int lane) {
+    const int k = lane >> 2;
+    return 8 * (k >> 1) + 2 * (lane & 3) + (k & 1);
 }
 
 // 1 / (1 + exp(-w)).  Where results are rounded to bf16 the hardware's exponential and reciprocal (2^-22 each, and 2^-24 |w| of the
@@ -348,25 +403,25 @@ __device__ __forceinline__ float gelu_gate(float a) {   // (1 + tanh(u)) / 2 = 1
     return ACCURATE ? sigmoid<true>(2.f * kGeluA * a * fmaf(kGeluB, s, 1.f)) : sigmoid_of(a * fmaf(-2.f * kLog2e * kGeluA * kGeluB, s, -2.f * kLog2e * kGeluA));
 }
 // act(a)
-template <bool ACCURATE>
-__device__ __forceinline__ float act_of(int act, float a) {
-    if (act == SLICEGCN_ACT_SILU) return a * sigmoid<ACCURATE>(a);
-    if (act == SLICEGCN_ACT_GELU) return a * gelu_gate<ACCURATE>(a);
-    if (act == SLICEGCN_ACT_RELU) return a > 0.f || isnan(a) ? a : 0.f;
+template <int ACT, bool ACCURATE>
+__device__ __forceinline__ float act_of(float a) {
+    if (ACT == SLICEGCN_ACT_SILU) return a * sigmoid<ACCURATE>(a);
+    if (ACT == SLICEGCN_ACT_GELU) return a * gelu_gate<ACCURATE>(a);
+    if (ACT == SLICEGCN_ACT_RELU) return a > 0.f || isnan(a) ? a : 0.f;
     return a;
 }
 // act(a) and act'(a)
-template <bool ACCURATE>
-__device__ __forceinline__ void act_both(int act, float a, float& y, float& dy) {
-    if (act == SLICEGCN_ACT_SILU) {
+template <int ACT, bool ACCURATE>
+__device__ __forceinline__ void act_both(float a, float& y, float& dy) {
+    if (ACT == SLICEGCN_ACT_SILU) {
         const float q = sigmoid<ACCURATE>(a);
         y = a * q;
         dy = fmaf(y, 1.f - q, q);
-    } else if (act == SLICEGCN_ACT_GELU) {
+    } else if (ACT == SLICEGCN_ACT_GELU) {
         const float q = gelu_gate<ACCURATE>(a);
         y = a * q;
         dy = fmaf(y * (1.f - q), 2.f * kGeluA * fmaf(3.f * kGeluB, a * a, 1.f), q);
-    } else if (act == SLICEGCN_ACT_RELU) {
+    } else if (ACT == SLICEGCN_ACT_RELU) {
         y = a > 0.f || isnan(a) ? a : 0.f;
         dy = a > 0.f ? 1.f : 0.f;
     } else {
@@ -374,333 +429,77 @@ __device__ __forceinline__ void act_both(int act, float a, float& y, float& dy) 
         dy = 1.f;
     }
 }
-
-// Sums of 16 columns over the warp's rows: lane l gets column l / 2.
-__device__ __forceinline__ float column_sums16(float (&v)[16], int lane) {
+template <int ACT, bool GATED, bool ACCURATE>
+__device__ __forceinline__ void forward_as(float (&a)[16], const float (&c)[16]) {
 #pragma unroll
-    for (int half = 8, mask = 16; half >= 1; half >>= 1, mask >>= 1) {
-        const bool up = lane & mask;
-#pragma unroll
-        for (int j = 0; j < half; ++j) {
-            const float keep = up ? v[j + half] : v[j], give = up ? v[j] : v[j + half];
-            v[j] = keep + __shfl_xor_sync(0xffffffffu, give, mask);
-        }
-    }
-    return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
-}
-
-// Parts of an fp32 number whose sum it is: 8 bits each.  Cut, not rounded: no part leaves the range, and each is exact.
-__device__ __forceinline__ void split3(float x, float (&part)[3]) {
-    if (isnan(x)) x = __int_as_float(0x7fc00000);   // one whose upper half alone is a NaN too
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        part[k] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-        x = isfinite(x) ? x - part[k] : 0.f;
+    for (int k = 0; k < 16; ++k) {
+        a[k] = act_of<ACT, ACCURATE>(a[k]);
+        if (GATED) a[k] *= c[k];
     }
 }
-
-struct Where {
-    int slice, row, col;   // of the warp's rows in D and of its first column there
-    int rows;              // how many of its 32 rows exist
-};
-
-template <int U>
-__device__ __forceinline__ void add_bias(float (&v)[U], const float* b, int slice, int cols, int col) {
-    if (!b) return;
-    const float* at = b + (int64_t)slice * cols;
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-        const float t = __ldg(at + min(col + j, cols - 1));   // the same address in every lane
-        v[j] += col + j < cols ? t : 0.f;
-    }
-}
-
-// U columns of a forward product (or of dx): bias, activation, gate, scale, residual.
-template <int U, bool GATED, bool ACCURATE, bool IN_BF16, bool OUT_BF16>
-__device__ __forceinline__ void finish_forward_as(const Params& P, const Where& w, int col, float (&a)[U], float (&c)[U], Lines<U, IN_BF16>& lines, uint32_t slab, int lane) {
-    add_bias<U>(a, P.b, w.slice, P.cols, col);
-    if (GATED) add_bias<U>(c, P.b2, w.slice, P.cols, col);
-#define SGCN_ACT(A)                                                       \
-    _Pragma("unroll") for (int j = 0; j < U; ++j) {                       \
-        float y = act_of<ACCURATE>(A, a[j]);                              \
-        if (GATED) y *= c[j];                                             \
-        a[j] = y * P.scale;                                               \
-    }
-    if (P.act == SLICEGCN_ACT_SILU) {
-        SGCN_ACT(SLICEGCN_ACT_SILU)
-    } else if (P.act == SLICEGCN_ACT_GELU) {
-        SGCN_ACT(SLICEGCN_ACT_GELU)
-    } else if (P.act == SLICEGCN_ACT_RELU) {
-        SGCN_ACT(SLICEGCN_ACT_RELU)
-    } else {
-        SGCN_ACT(SLICEGCN_ACT_NONE)
-    }
-#undef SGCN_ACT
-    if (P.in) {
-        float r[U];
-        lines.row(r, P.in_vec, slab, lane);
-#pragma unroll
-        for (int j = 0; j < U; ++j) a[j] += r[j];
-    }
-    constexpr int E = OUT_BF16 ? 2 : 4, W = U * E / 4;
-    uint32_t words[W];
-#pragma unroll
-    for (int j = 0; j < W; ++j) words[j] = OUT_BF16 ? pack2(a[(2 * j) % U], a[(2 * j + 1) % U]) : __float_as_uint(a[j % U]);
-    char* at = static_cast<char*>(P.out) + ((int64_t)w.row * P.out_ld + (int64_t)w.slice * P.cols + col) * E;
-    store_lines<U, OUT_BF16>(words, at, P.out_ld * E, w.rows, P.cols - col, P.out_vec, slab, lane);
-}
-
-template <int U, bool GATED, bool ACCURATE>
-__device__ __forceinline__ void finish_forward(const Params& P, const Where& w, int col, float (&a)[U], float (&c)[U], uint32_t slab, int lane) {
-    // residual and output have one type
-    if (P.out_bf16) {
-        Lines<U, true> lines;
-        if (P.in)
-            lines.load(static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col) * 2, P.in_ld * 2, w.rows, P.cols - col,
-                       P.in_vec, slab, lane);
-        finish_forward_as<U, GATED, ACCURATE, true, true>(P, w, col, a, c, lines, slab, lane);
-    } else {
-        Lines<U, false> lines;
-        if (P.in)
-            lines.load(static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col) * 4, P.in_ld * 4, w.rows, P.cols - col,
-                       P.in_vec, slab, lane);
-        finish_forward_as<U, GATED, ACCURATE, false, false>(P, w, col, a, c, lines, slab, lane);
-    }
-}
-
-// Sixteen columns of one of da and dc: planes to the workspace, and the sums over the warp's rows.
-__device__ __forceinline__ void put_dz(const Params& P, const Where& w, int part, int col, float (&v)[16], uint32_t slab, int lane) {
-    const int ps = part * P.p + w.slice;
-    __nv_bfloat16* at = P.dz + (int64_t)w.row * P.dz_row + (int64_t)ps * P.dz_pad + col;
-    uint32_t words[8];
-    if (P.dz_planes == 1) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) words[j] = pack2(v[2 * j], v[2 * j + 1]);
-        store_lines<16, true>(words, reinterpret_cast<char*>(at), P.dz_row * 2, w.rows, P.dz_pad - col, true, slab, lane);
-    } else {
-        float rest[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) rest[j] = v[j];
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t lo = __float_as_uint(rest[2 * j]) & 0xffff0000u, hi = __float_as_uint(rest[2 * j + 1]) & 0xffff0000u;
-                words[j] = lo >> 16 | hi;
-                rest[2 * j] = isfinite(rest[2 * j]) ? rest[2 * j] - __uint_as_float(lo) : 0.f;
-                rest[2 * j + 1] = isfinite(rest[2 * j + 1]) ? rest[2 * j + 1] - __uint_as_float(hi) : 0.f;
-            }
-            store_lines<16, true>(words, reinterpret_cast<char*>(at + k * P.dz_plane), P.dz_row * 2, w.rows, P.dz_pad - col, true, slab, lane);
-        }
-    }
-    if (P.sums) {
-        const float s = column_sums16(v, lane);
-        const int c = col + (lane >> 1);
-        if (!(lane & 1) && c < P.cols && w.rows > 0) P.sums[((int64_t)(w.row >> 5) * (P.slices) + ps) * P.cols + c] = s;
-    }
-}
-
-// Sixteen columns of da (and dc).
 template <bool GATED, bool ACCURATE>
-__device__ __forceinline__ void finish_dz(const Params& P, const Where& w, int col, float (&a)[16], float (&c)[16], uint32_t slab, int lane) {
-    float g[16];
-    if (P.in_bf16) {
-        Lines<16, true> lines;
-        lines.load(static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col) * 2, P.in_ld * 2, w.rows, P.cols - col, P.in_vec,
-                   slab, lane);
-        lines.row(g, P.in_vec, slab, lane);
-    } else {
-        Lines<16, false> lines;
-        lines.load(static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col) * 4, P.in_ld * 4, w.rows, P.cols - col, P.in_vec,
-                   slab, lane);
-        lines.row(g, P.in_vec, slab, lane);
+__device__ __forceinline__ void forward_math(const Params& P, float (&a)[16], const float (&c)[16]) {
+    if (P.act == SLICEGCN_ACT_SILU)
+        forward_as<SLICEGCN_ACT_SILU, GATED, ACCURATE>(a, c);
+    else if (P.act == SLICEGCN_ACT_GELU)
+        forward_as<SLICEGCN_ACT_GELU, GATED, ACCURATE>(a, c);
+    else if (P.act == SLICEGCN_ACT_RELU)
+        forward_as<SLICEGCN_ACT_RELU, GATED, ACCURATE>(a, c);
+    else
+        forward_as<SLICEGCN_ACT_NONE, GATED, ACCURATE>(a, c);
+}
+// a, c -> da, dc
+template <int ACT, bool GATED, bool ACCURATE>
+__device__ __forceinline__ void backward_as(float scale, const float (&g)[16], float (&a)[16], float (&c)[16]) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        float y, dy;
+        act_both<ACT, ACCURATE>(a[k], y, dy);
+        const float gk = g[k] * scale;
+        a[k] = GATED ? gk * c[k] * dy : gk * dy;
+        if (GATED) c[k] = gk * y;
     }
-    add_bias<16>(a, P.b, w.slice, P.cols, col);
-    if (GATED) add_bias<16>(c, P.b2, w.slice, P.cols, col);
-#define SGCN_ACT(A)                                                       \
-    _Pragma("unroll") for (int j = 0; j < 16; ++j) {                      \
-        float y, dy;                                                      \
-        act_both<ACCURATE>(A, a[j], y, dy);                               \
-        const float gj = g[j] * P.scale;                                  \
-        a[j] = GATED ? gj * c[j] * dy : gj * dy;                          \
-        if (GATED) c[j] = gj * y;                                         \
-    }
-    if (P.act == SLICEGCN_ACT_SILU) {
-        SGCN_ACT(SLICEGCN_ACT_SILU)
-    } else if (P.act == SLICEGCN_ACT_GELU) {
-        SGCN_ACT(SLICEGCN_ACT_GELU)
-    } else if (P.act == SLICEGCN_ACT_RELU) {
-        SGCN_ACT(SLICEGCN_ACT_RELU)
-    } else {
-        SGCN_ACT(SLICEGCN_ACT_NONE)
-    }
-#undef SGCN_ACT
-    put_dz(P, w, 0, col, a, slab, lane);
-    if (GATED) put_dz(P, w, 1, col, c, slab, lane);
+}
+template <bool GATED, bool ACCURATE>
+__device__ __forceinline__ void backward_math(const Params& P, const float (&g)[16], float (&a)[16], float (&c)[16]) {
+    if (P.act == SLICEGCN_ACT_SILU)
+        backward_as<SLICEGCN_ACT_SILU, GATED, ACCURATE>(P.scale, g, a, c);
+    else if (P.act == SLICEGCN_ACT_GELU)
+        backward_as<SLICEGCN_ACT_GELU, GATED, ACCURATE>(P.scale, g, a, c);
+    else if (P.act == SLICEGCN_ACT_RELU)
+        backward_as<SLICEGCN_ACT_RELU, GATED, ACCURATE>(P.scale, g, a, c);
+    else
+        backward_as<SLICEGCN_ACT_NONE, GATED, ACCURATE>(P.scale, g, a, c);
 }
 
-// ---- bf16: 32 columns at a time
-
-__device__ __forceinline__ void sts4(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory"); }
-// Sixteen numbers that every lane reads alike, added.
-__device__ __forceinline__ void add16(float (&v)[16], uint32_t at) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const uint4 t = lds16(at + k * 16);
-        v[4 * k] += __uint_as_float(t.x), v[4 * k + 1] += __uint_as_float(t.y);
-        v[4 * k + 2] += __uint_as_float(t.z), v[4 * k + 3] += __uint_as_float(t.w);
-    }
+// Parts of an fp32 number whose sum it is: 8 bits each.  Cut, not rounded: no part leaves the range, and each is exact.  Takes the
+// next part off x.
+__device__ __forceinline__ uint32_t next_part(float& x) {
+    const uint32_t part = __float_as_uint(x) & 0xffff0000u;
+    x = isfinite(x) ? x - __uint_as_float(part) : 0.f;
+    return part;
 }
-// Where a lane finds its row's chunk c of eight columns, and its line i of eight (row i * 8 + lane / 4, chunk lane % 4).
-__device__ __forceinline__ uint32_t own_chunk(uint32_t slab, int lane, int c) { return (slab + lane * 64 + (((lane >> 1) & 3) << 4)) ^ (c << 4); }
-__device__ __forceinline__ uint32_t own_line(uint32_t slab, int lane, int i) {
-    return slab + i * 512 + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4);
-}
-__device__ __forceinline__ void put_rows(const uint32_t* w, uint32_t slab, int lane) {
+// Half h of da or dc as three planes, by way of the slab.
+__device__ __forceinline__ void planes_out(const Params& P, const Where& w, int part, int col, int h, float (&v)[16], uint32_t slab, int lane) {
+    __nv_bfloat16* at = P.dz + (int64_t)w.row * P.dz_row + (int64_t)(part * P.p + w.slice) * P.dz_pad + col;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) sts16(own_chunk(slab, lane, c), make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
-}
-// The slab's 32 rows x 32 columns to memory, `rows` and `cols` of them.
-__device__ __forceinline__ void slab_out(char* at, int64_t ld_bytes, int rows, int cols, bool vec, uint32_t slab, int lane) {
-    if (vec && cols >= 8) {
-        const int left = cols - (lane & 3) * 8;
-        char* to = at + (int64_t)(lane >> 2) * ld_bytes + (lane & 3) * 16;
-        if (rows == 32 && cols >= 32) {
+    for (int q = 0; q < 3; ++q) {
+        uint32_t words[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(to + i * 8 * ld_bytes) = lds16(own_line(slab, lane, i));
-            return;
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t lo = next_part(v[2 * k]), hi = next_part(v[2 * k + 1]);
+            words[k] = lo >> 16 | hi;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i * 8 + (lane >> 2) < rows && left >= 8) *reinterpret_cast<uint4*>(to + i * 8 * ld_bytes) = lds16(own_line(slab, lane, i));
-        if (cols >= 32 || cols % 8 == 0) return;
-    }
-    // element by element: all columns, or those behind the last eight
-    const int c = lane, from = vec ? min(cols, 32) & ~7 : 0;
-    if (c >= from && c < cols)
-#pragma unroll 4
-        for (int i = 0; i < rows; ++i) {
-            uint16_t v;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(slab + slab_at<64>(i, c >> 3) + (c & 7) * 2) : "memory");
-            *reinterpret_cast<uint16_t*>(at + (int64_t)i * ld_bytes + c * 2) = v;
-        }
-}
-// 32 rows x 32 columns of r or dout: asked for here (whole chunks where they are aligned) ...
-__device__ __forceinline__ void load_in(const Params& P, const Where& w, int col, uint4 (&raw)[4], int lane) {
-    const int left = P.cols - col - (lane & 3) * 8;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
-    if (!P.in_vec || w.rows <= 0 || left < 8) return;
-    const char* at = static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col + (lane & 3) * 8) * 2;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = i * 8 + (lane >> 2);
-        const uint4 t = *reinterpret_cast<const uint4*>(at + (int64_t)min(row, w.rows - 1) * P.in_ld * 2);
-        if (row < w.rows) raw[i] = t;
+        __syncwarp();
+        half_to_slab(words, slab, lane, h);
+        __syncwarp();
+        slab_out(at + q * P.dz_plane, P.dz_row, w.rows, P.dz_pad - col, true, slab, lane, 2 * h, 2 * h + 2);
     }
 }
-// ... and laid into the slab here, with what no whole chunk holds.
-__device__ __forceinline__ void put_in(const Params& P, const Where& w, int col, const uint4 (&raw)[4], uint32_t slab, int lane) {
-    const int cols = min(32, P.cols - col), from = P.in_vec ? max(cols, 0) & ~7 : 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sts16(own_line(slab, lane, i), raw[i]);
-    if (from >= cols || w.rows <= 0) return;
-    __syncwarp();
-    const int c = lane;
-    const char* at = static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col + c) * 2;
-    if (c >= from && c < cols)
-#pragma unroll 8
-        for (int i = 0; i < w.rows; ++i) {
-            const uint16_t v = *reinterpret_cast<const uint16_t*>(at + (int64_t)i * P.in_ld * 2);
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(slab + slab_at<64>(i, c >> 3) + (c & 7) * 2), "h"(v) : "memory");
-        }
-}
-// Sixteen columns of the lane's row in the slab.
-__device__ __forceinline__ void own_row16(float (&v)[16], uint32_t slab, int lane, int h) {
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        const uint4 t = lds16(own_chunk(slab, lane, 2 * h + q));
-        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[q * 8 + 2 * k] = __uint_as_float(w[k] << 16);
-            v[q * 8 + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-        }
-    }
-}
-
-// Half of 32 columns of a forward product (of dx: PLAIN), packed.
-template <bool GATED, bool PLAIN>
-__device__ __forceinline__ void forward_half(const Params& P, int h, float (&a)[16], const float (&c)[16], uint32_t* words, uint32_t slab, int lane) {
-    if (!PLAIN) {
-#define SGCN_ACT(A) _Pragma("unroll") for (int j = 0; j < 16; ++j) a[j] = act_of<false>(A, a[j])
-        if (P.act == SLICEGCN_ACT_SILU)
-            SGCN_ACT(SLICEGCN_ACT_SILU);
-        else if (P.act == SLICEGCN_ACT_GELU)
-            SGCN_ACT(SLICEGCN_ACT_GELU);
-        else if (P.act == SLICEGCN_ACT_RELU)
-            SGCN_ACT(SLICEGCN_ACT_RELU);
-#undef SGCN_ACT
-        if (GATED) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) a[j] *= c[j];
-        }
-    }
-    if (P.scale != 1.f) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) a[j] *= P.scale;
-    }
-    if (!PLAIN && P.in) {
-        float r[16];
-        own_row16(r, slab, lane, h);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) a[j] += r[j];
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) words[j] = pack2(a[2 * j], a[2 * j + 1]);
-}
-// Half of 32 columns of da, which takes dout's place in the slab, and of dc, packed; their sums over the warp's rows.
-template <bool GATED>
-__device__ __forceinline__ void dz_half(const Params& P, const Where& w, int col, int h, float (&a)[16], float (&c)[16], uint32_t* words, uint32_t slab, int lane) {
-    float g[16];
-    own_row16(g, slab, lane, h);
-#define SGCN_ACT(A)                                                       \
-    _Pragma("unroll") for (int j = 0; j < 16; ++j) {                      \
-        float y, dy;                                                      \
-        act_both<false>(A, a[j], y, dy);                                  \
-        const float gj = g[j] * P.scale;                                  \
-        a[j] = GATED ? gj * c[j] * dy : gj * dy;                          \
-        if (GATED) c[j] = gj * y;                                         \
-    }
-    if (P.act == SLICEGCN_ACT_SILU) {
-        SGCN_ACT(SLICEGCN_ACT_SILU)
-    } else if (P.act == SLICEGCN_ACT_GELU) {
-        SGCN_ACT(SLICEGCN_ACT_GELU)
-    } else if (P.act == SLICEGCN_ACT_RELU) {
-        SGCN_ACT(SLICEGCN_ACT_RELU)
-    } else {
-        SGCN_ACT(SLICEGCN_ACT_NONE)
-    }
-#undef SGCN_ACT
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-        sts16(own_chunk(slab, lane, 2 * h + q), make_uint4(pack2(a[8 * q], a[8 * q + 1]), pack2(a[8 * q + 2], a[8 * q + 3]), pack2(a[8 * q + 4], a[8 * q + 5]),
-                                                           pack2(a[8 * q + 6], a[8 * q + 7])));
-    if (GATED) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) words[j] = pack2(c[2 * j], c[2 * j + 1]);
-    }
-    if (P.sums) {
-        const int at = col + (lane >> 1);
-        const bool mine = !(lane & 1) && at < P.cols && w.rows > 0;
-        float* to = P.sums + ((int64_t)(w.row >> 5) * P.slices + w.slice) * P.cols + at;
-        const float s = column_sums16(a, lane);
-        if (mine) *to = s;
-        if (GATED) {
-            const float s2 = column_sums16(c, lane);
-            if (mine) to[(int64_t)P.p * P.cols] = s2;
-        }
-    }
+__device__ __forceinline__ void sums_out(const Params& P, const Where& w, int part, int col, float (&s)[8], int lane) {
+    const float t = sum_lanes(s, lane);
+    const int c = col + sum_column(lane);
+    if (c < P.cols && w.rows > 0) P.sums[((int64_t)(w.row >> 5) * P.slices + part * P.p + w.slice) * P.cols + c] = t;
 }
 
 // ------------------------------------------------------------------------------------------ the product
@@ -740,19 +539,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
     constexpr bool kBK = MODE == kDx;    // B's
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    unsigned char* tail = smem_raw + (base - smem_u32(smem_raw)) + kStages * kStageBytes + kEpiWarps * (kSlabBytes + kBiasBytes);
+    unsigned char* tail = smem_raw + (base - smem_u32(smem_raw)) + kStages * kStageBytes + kEpiWarps * kSlabBytes;
     uint64_t* full = reinterpret_cast<uint64_t*>(tail);
     uint64_t* empty = full + kStages;
-    uint64_t* tfull = empty + kStages;    // [2]
-    uint64_t* tempty = tfull + 2;         // [2]
-    uint32_t* tmem_at = reinterpret_cast<uint32_t*>(tempty + 2);
+    uint64_t* tfull = empty + kStages;    // [2 groups]
+    uint64_t* tempty = tfull + 4;         // [2 groups]
+    uint32_t* tmem_at = reinterpret_cast<uint32_t*>(tempty + 4);
+    // Tiles of half width: two groups of eight epilogue warps take turns at the tiles, each with two accumulators of its own (a
+    // group waits for its own ones in order, whatever the other does).  Else all sixteen warps work on each tile.
+    const int groups_log = P.nt == 64, groups = 1 << groups_log;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int first = blockIdx.x >> 1, stride = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) mbar_init(full + s, 1), mbar_init(empty + s, 1);
-        for (int s = 0; s < 2; ++s) mbar_init(tfull + s, 1), mbar_init(tempty + s, 2 * kEpiWarps);
+        for (int s = 0; s < 2 * groups; ++s) mbar_init(tfull + s, 1), mbar_init(tempty + s, 2 * kEpiWarps >> groups_log);   // of both CTAs
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
@@ -819,14 +621,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
         if (rank == 0) {
             const bool one = elect_one();
             bool ok = true;
-            int use = 0, st = 0;
+            int turn = 0, st = 0;
             uint32_t phase = 0;
             const uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | (kAK ? 0u : 1u << 15) | (kBK ? 0u : 1u << 16) | (uint32_t)(2 * P.nt >> 3) << 17 | 16u << 24;
-            for (int i = first; ok && i < P.items; i += stride) {
+            for (int i = first; ok && i < P.items; i += stride, ++turn) {
+                int use = (turn >> groups_log) * chunks;
                 for (int c = 0; ok && c < chunks; ++c, ++use) {
                     const int kb0 = c * P.chunk, kb1 = min(kb0 + P.chunk, P.kb_total);
-                    const uint32_t d = tmem + (use & 1) * 256;
-                    ok = __all_sync(0xffffffffu, mbar_wait(tempty + (use & 1), ((use >> 1) & 1) ^ 1));
+                    const int acc = (turn & (groups - 1)) * 2 + (use & 1);
+                    const uint32_t d = tmem + acc * (2 * P.nt);
+                    ok = __all_sync(0xffffffffu, mbar_wait(tempty + acc, ((use >> 1) & 1) ^ 1));
                     if (!ok) break;
                     fence_after();
                     bool more = false;
@@ -848,7 +652,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                             more = true;
                             if (++st == kStages) st = 0, phase ^= 1;
                         }
-                    if (one) umma_commit(tfull + (use & 1));
+                    if (one) umma_commit(tfull + acc);
                     __syncwarp();
                 }
             }
@@ -861,182 +665,218 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
             }
         }
     } else {
-        const uint32_t slab = base + kStages * kStageBytes + warp * kSlabBytes;
-        const uint32_t biases = base + kStages * kStageBytes + kEpiWarps * kSlabBytes + warp * kBiasBytes;
-        const int quarter = warp & 3, part = warp >> 2;   // 32 rows of the tile, and a share of its columns
-        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        // columns of D per warp, and where they start in the accumulator; gated: c's lie nt further on
-        const int share = kGated ? (PROMO ? P.nt / 4 : 32) : P.nt / 2;
-        const bool busy = part * share < (kGated ? P.nt : 2 * P.nt);
-        int use = 0;
+        const uint32_t slab = base + kStages * kStageBytes + warp * kSlabBytes, slab2 = slab + 2048;
+        // a warp has 32 rows and 64 columns of the accumulator, gated: 32 of a and the same 32 of c
+        const int group = (warp >> 2) & (groups - 1), part = (warp >> 2) >> groups_log;
+        const int quarter = warp & 3, share = kGated ? 32 : 64;
+        const uint32_t mine = tmem + ((uint32_t)(quarter * 32) << 16) + part * share;
+        const int second = kGated ? P.nt : 32;   // columns from the first 32 to the other 32
         bool ok = true;
-        for (int i = first; ok && i < P.items; i += stride) {
+        int turn = 0;
+        for (int i = first; ok && i < P.items; i += stride, ++turn) {
+            if ((turn & (groups - 1)) != group) continue;
             const Item t = item_of<MODE>(P, i);
             Where w;
             w.slice = t.slice;
             w.row = t.m + (int)rank * 128 + quarter * 32;
             w.rows = min(32, max(0, P.n - w.row));
-            w.col = t.n + part * share;
-            if (PROMO) {
+            const int col0 = t.n + part * share;
+            int use = (turn >> groups_log) * chunks;
+            if constexpr (MODE == kDw) {
                 float acc[64];
 #pragma unroll
                 for (int j = 0; j < 64; ++j) acc[j] = 0.f;
-                for (int c = 0; ok && c < chunks; ++c, ++use) {
-                    if (!mbar_wait(tfull + (use & 1), (use >> 1) & 1)) {
-                        ok = false;
-                        break;
-                    }
+                for (int c = 0; c < chunks; ++c, ++use) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(tfull + group * 2 + (use & 1), (use >> 1) & 1));
+                    if (!ok) break;
                     fence_after();
-                    const uint32_t d = tmem + (use & 1) * 256 + lanes + part * share;
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        // gated: 16 or 32 columns of a in the first half of the registers, c's in the second
-                        const int off = kGated ? (u & 1) * 16 : u * 16;
-                        if (off >= share) continue;
                         uint32_t r[16];
-                        tmem_ld16(d + off + (kGated && u >= 2 ? P.nt : 0), r);
+                        tmem_ld16(mine + (group * 2 + (use & 1)) * (2 * P.nt) + u * 16, r);
                         tmem_wait(r);
 #pragma unroll
                         for (int j = 0; j < 16; ++j) acc[u * 16 + j] += __uint_as_float(r[j]);
                     }
                     fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_first(tempty + (use & 1));
+                    if (lane == 0) mbar_arrive_first(tempty + group * 2 + (use & 1));
                 }
                 if (!ok) break;
-                if (MODE == kDw) {
-                    const int f = w.row + lane, fs = P.cols;   // this lane's column of dW; its rows are this tile's columns
-                    const int ks = P.k_part;
-                    if (f < fs) {
-                        if (P.splits > 1) {
-                            float* to = P.partial + (((int64_t)t.split * P.slices + t.slice) * ks + w.col) * fs + f;
+                const int f = w.row + lane, fs = P.cols, ks = P.k_part;   // this lane's column of dW; its rows are this tile's columns
+                if (f < fs) {
+                    if (P.splits > 1) {
+                        float* to = P.partial + (((int64_t)t.split * P.slices + t.slice) * ks + col0) * fs + f;
 #pragma unroll
-                            for (int j = 0; j < 64; ++j)
-                                if (j < share && w.col + j < ks) to[(int64_t)j * fs] = acc[j];
-                        } else {
-                            const int64_t at = ((int64_t)(t.slice % P.p) * ks + w.col) * fs + f;
-                            void* dw = t.slice < P.p ? P.dw : P.dw2;
-                            if (dw) {
+                        for (int j = 0; j < 64; ++j)
+                            if (col0 + j < ks) to[(int64_t)j * fs] = acc[j];
+                    } else if (void* dw = t.slice < P.p ? P.dw : P.dw2) {
+                        const int64_t at = ((int64_t)(t.slice < P.p ? t.slice : t.slice - P.p) * ks + col0) * fs + f;
 #pragma unroll
-                                for (int j = 0; j < 64; ++j)
-                                    if (j < share && w.col + j < ks) {
-                                        const float v = acc[j] * P.scale;
-                                        if (P.out_bf16)
-                                            static_cast<__nv_bfloat16*>(dw)[at + (int64_t)j * fs] = __float2bfloat16_rn(v);
-                                        else
-                                            static_cast<float*>(dw)[at + (int64_t)j * fs] = v;
-                                    }
+                        for (int j = 0; j < 64; ++j)
+                            if (col0 + j < ks) {
+                                if (P.out_bf16)
+                                    static_cast<__nv_bfloat16*>(dw)[at + (int64_t)j * fs] = __float2bfloat16_rn(acc[j] * P.scale);
+                                else
+                                    static_cast<float*>(dw)[at + (int64_t)j * fs] = acc[j] * P.scale;
                             }
+                    }
+                }
+            } else if constexpr (PROMO) {
+                float acc[64];   // half h of the first 32 columns at 16 h, of the other 32 at 32 + 16 h
+#pragma unroll
+                for (int j = 0; j < 64; ++j) acc[j] = 0.f;
+                for (int c = 0; c < chunks; ++c, ++use) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(tfull + group * 2 + (use & 1), (use >> 1) & 1));
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t d = mine + (group * 2 + (use & 1)) * (2 * P.nt);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        uint32_t r[16];
+                        tmem_fragments(d + (u & 2 ? second : 0) + ((uint32_t)((u & 1) * 16) << 16), r);
+                        tmem_wait(r);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) acc[u * 16 + j] += __uint_as_float(r[j]);
+                    }
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_first(tempty + group * 2 + (use & 1));
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int u = 0; u < (kGated ? 1 : 2); ++u) {
+                    const int col = col0 + u * 32;
+                    if (col >= P.cols || w.rows <= 0) continue;
+                    float bias[8], bias2[8], s[8], s2[8];
+                    load_bias(P, MODE == kDx ? nullptr : P.b, w.slice, col, bias, lane);
+                    if (kGated) load_bias(P, P.b2, w.slice, col, bias2, lane);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s[j] = s2[j] = 0.f;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float a[16], c[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) a[j] = acc[u * 32 + h * 16 + j], c[j] = kGated ? acc[(32 + h * 16 + j) & 63] : 0.f;
+                        if (MODE != kDx) add_bias(a, bias);
+                        if (kGated) add_bias(c, bias2);
+                        float in[16];
+                        if (kIsDz || (MODE != kDx && P.in)) load_half_f32(P, w, col, h, in, lane);
+                        if constexpr (kIsDz) {
+                            backward_math<kGated, true>(P, in, a, c);
+                            sum_half(a, s);
+                            if (kGated) sum_half(c, s2);
+                            planes_out(P, w, 0, col, h, a, slab, lane);
+                            if (kGated) planes_out(P, w, 1, col, h, c, slab2, lane);
+                        } else {
+                            if (MODE != kDx) forward_math<kGated, true>(P, a, c);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) a[j] = MODE != kDx && P.in ? fmaf(a[j], P.scale, in[j]) : a[j] * P.scale;
+                            store_half_f32(P, w, col, h, a, lane);
                         }
                     }
-                } else {
-#pragma unroll
-                    for (int u = 0; u < (kGated ? 2 : 4); ++u) {
-                        if (u * 16 >= share) continue;
-                        const int col = w.col + u * 16;
-                        if (col >= P.cols || w.rows <= 0) continue;
-                        float a[16], cc[16];
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) a[j] = acc[u * 16 + j], cc[j] = kGated ? acc[(32 + u * 16 + j) & 63] : 0.f;
-                        if (MODE == kDz || MODE == kDzGated)
-                            finish_dz<kGated, true>(P, w, col, a, cc, slab, lane);
-                        else
-                            finish_forward<16, kGated, true>(P, w, col, a, cc, slab, lane);
+                    if (kIsDz && P.sums) {
+                        sums_out(P, w, 0, col, s, lane);
+                        if (kGated) sums_out(P, w, 1, col, s2, lane);
                     }
                 }
             } else {
-                // what the columns need besides the product is on its way while the product is waited for
-                const int units = busy ? share / 32 : 0;
-                float bias[2] = {0.f, 0.f}, bias2 = 0.f;
-                uint4 raw[4];
+                // what a unit needs besides the product is on its way while the product is waited for
                 const bool with_in = kIsDz || (MODE != kDx && P.in);
-                if (units > 0) {
-                    const int64_t bat = (int64_t)t.slice * P.cols;
-                    if (MODE != kDx) {
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const int c = w.col + u * 32 + lane;
-                            if (u < units && P.b && c < P.cols) bias[u] = __ldg(P.b + bat + c);
-                        }
-                        if (kGated && P.b2 && w.col + lane < P.cols) bias2 = __ldg(P.b2 + bat + w.col + lane);
-                    }
-                    if (with_in) load_in(P, w, w.col, raw, lane);
-                }
-                if (!mbar_wait(tfull + (use & 1), (use >> 1) & 1)) {
-                    ok = false;
-                    break;
-                }
+                float bias[8], bias2[8];
+                uint4 raw[4];
+                load_bias(P, MODE == kDx ? nullptr : P.b, w.slice, col0, bias, lane);
+                if (kGated) load_bias(P, P.b2, w.slice, col0, bias2, lane);
+                if (with_in) load_in(P, w, col0, raw, lane);
+                ok = __all_sync(0xffffffffu, mbar_wait(tfull + group * 2 + (use & 1), (use >> 1) & 1));
+                if (!ok) break;
                 fence_after();
-                const uint32_t d = tmem + (use & 1) * 256 + lanes + part * share;
-                for (int u = 0; u < units; ++u) {
-                    const int col = w.col + u * 32;
-                    const bool last = u == units - 1, there = col < P.cols && w.rows > 0;
+                const uint32_t d = mine + (group * 2 + (use & 1)) * (2 * P.nt);
+#pragma unroll 1
+                for (int u = 0; u < (kGated ? 1 : 2); ++u) {
+                    const int col = col0 + u * 32;
+                    const bool last = kGated || u == 1;
                     uint32_t ra[16], rc[16];
-                    tmem_ld16(d + u * 32, ra);
-                    if (kGated) tmem_ld16(d + u * 32 + P.nt, rc);
-                    if (MODE != kDx) {
+                    tmem_fragments(d + u * 32, ra);
+                    if (kGated) tmem_fragments(d + second, rc);
+                    if (with_in) {
                         __syncwarp();
-                        sts4(biases + lane * 4, u ? bias[1] : bias[0]);
-                        if (kGated) sts4(biases + 128 + lane * 4, bias2);
+                        put_in(P, w, col, raw, slab, lane);
+                        __syncwarp();
                     }
-                    if (with_in) put_in(P, w, col, raw, slab, lane);
-                    __syncwarp();
                     tmem_wait(ra);
                     if (kGated) after_wait(rc);
-                    uint32_t words[16], words2[16];
+                    float s[8], s2[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s[j] = s2[j] = 0.f;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t na[16], nc[16];
-                        if (h == 0) {   // the second half's numbers come while the first half's are worked on
-                            tmem_ld16(d + u * 32 + 16, na);
-                            if (kGated) tmem_ld16(d + u * 32 + 16 + P.nt, nc);
-                        }
+                        if (h == 0 && !kGated) tmem_fragments(d + u * 32 + (16u << 16), na);   // comes while the first half is worked on (gated: no registers for that)
                         float a[16], c[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) a[j] = __uint_as_float(ra[j]), c[j] = kGated ? __uint_as_float(rc[j]) : 0.f;
-                        if (MODE != kDx) {
-                            add16(a, biases + h * 64);
-                            if (kGated) add16(c, biases + 128 + h * 64);
+                        if (MODE != kDx) add_bias(a, bias);
+                        if (kGated) add_bias(c, bias2);
+                        float in[16];
+                        if (with_in) half_from_slab(in, slab, lane, h);
+                        uint32_t words[8];
+                        if constexpr (kIsDz) {
+                            backward_math<kGated, false>(P, in, a, c);
+                            if (P.sums) {
+                                sum_half(a, s);
+                                if (kGated) sum_half(c, s2);
+                            }
+                            if (kGated) {
+                                pack_half(c, words);
+                                half_to_slab(words, slab2, lane, h);
+                            }
+                        } else {
+                            if (MODE != kDx) forward_math<kGated, false>(P, a, c);
+                            if (with_in) {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) a[j] = fmaf(a[j], P.scale, in[j]);
+                            } else if (P.scale != 1.f) {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) a[j] *= P.scale;
+                            }
                         }
-                        if constexpr (kIsDz)
-                            dz_half<kGated>(P, w, col + 16 * h, h, a, c, words2 + 8 * h, slab, lane);
-                        else
-                            forward_half<kGated, MODE == kDx>(P, h, a, c, words + 8 * h, slab, lane);
+                        pack_half(a, words);
+                        half_to_slab(words, slab, lane, h);   // in the place of what came in
                         if (h == 0) {
+                            if (kGated) tmem_fragments(d + u * 32 + (16u << 16), na), tmem_fragments(d + second + (16u << 16), nc);
                             tmem_wait(na);
                             if (kGated) after_wait(nc);
                             if (last) {
                                 fence_before();
                                 __syncwarp();
-                                if (lane == 0) mbar_arrive_first(tempty + (use & 1));
+                                if (lane == 0) mbar_arrive_first(tempty + group * 2 + (use & 1));
                             }
 #pragma unroll
                             for (int j = 0; j < 16; ++j) ra[j] = na[j], rc[j] = kGated ? nc[j] : 0u;
                         }
                     }
-                    if (with_in && !last) load_in(P, w, col + 32, raw, lane);
-                    if constexpr (kIsDz) {
-                        if (there) {
-                            __nv_bfloat16* at = P.dz + (int64_t)w.row * P.dz_row + (int64_t)w.slice * P.dz_pad + col;
-                            __syncwarp();
-                            slab_out(reinterpret_cast<char*>(at), P.dz_row * 2, w.rows, P.dz_pad - col, true, slab, lane);
-                            if (kGated) {
-                                __syncwarp();
-                                put_rows(words2, slab, lane);
-                                __syncwarp();
-                                slab_out(reinterpret_cast<char*>(at + (int64_t)P.p * P.dz_pad), P.dz_row * 2, w.rows, P.dz_pad - col, true, slab, lane);
-                            }
-                        }
-                    } else if (there) {
-                        __syncwarp();
-                        put_rows(words, slab, lane);
-                        __syncwarp();
-                        slab_out(static_cast<char*>(P.out) + ((int64_t)w.row * P.out_ld + (int64_t)w.slice * P.cols + col) * 2, P.out_ld * 2, w.rows, P.cols - col,
-                                 P.out_vec, slab, lane);
+                    __syncwarp();
+                    if (!last) {
+                        load_bias(P, MODE == kDx ? nullptr : P.b, w.slice, col + 32, bias, lane);
+                        if (with_in) load_in(P, w, col + 32, raw, lane);
                     }
+                    if (col < P.cols && w.rows > 0) {
+                        if constexpr (kIsDz) {
+                            __nv_bfloat16* at = P.dz + (int64_t)w.row * P.dz_row + (int64_t)w.slice * P.dz_pad + col;
+                            slab_out(at, P.dz_row, w.rows, P.dz_pad - col, true, slab, lane, 0, 4);
+                            if (kGated) slab_out(at + (int64_t)P.p * P.dz_pad, P.dz_row, w.rows, P.dz_pad - col, true, slab2, lane, 0, 4);
+                            if (P.sums) {
+                                sums_out(P, w, 0, col, s, lane);
+                                if (kGated) sums_out(P, w, 1, col, s2, lane);
+                            }
+                        } else {
+                            slab_out(static_cast<__nv_bfloat16*>(P.out) + (int64_t)w.row * P.out_ld + (int64_t)w.slice * P.cols + col, P.out_ld, w.rows,
+                                     P.cols - col, P.out_vec, slab, lane, 0, 4);
+                        }
+                    }
+                    __syncwarp();   // the slab is free again
                 }
-                if (units == 0 && lane == 0) mbar_arrive_first(tempty + (use & 1));
-                ++use;
             }
         }
         if (!ok && lane == 0 && P.status) atomicExch(P.status, SLICEGCN_DEVSTATUS_WAIT);
@@ -1084,11 +924,14 @@ __global__ void __launch_bounds__(256) ffn_pack_kernel(const __grid_constant__ P
             uint32_t w[3][4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                float lo[3], hi[3];
-                split3(2 * k < left ? s[2 * k] : 0.f, lo);
-                split3(2 * k + 1 < left ? s[2 * k + 1] : 0.f, hi);
+                float lo = 2 * k < left ? s[2 * k] : 0.f, hi = 2 * k + 1 < left ? s[2 * k + 1] : 0.f;
+                if (isnan(lo)) lo = __int_as_float(0x7fc00000);   // one whose upper half alone is a NaN too
+                if (isnan(hi)) hi = __int_as_float(0x7fc00000);
 #pragma unroll
-                for (int q = 0; q < 3; ++q) w[q][k] = __float_as_uint(lo[q]) >> 16 | (__float_as_uint(hi[q]) & 0xffff0000u);
+                for (int q = 0; q < 3; ++q) {
+                    const uint32_t l = next_part(lo);
+                    w[q][k] = l >> 16 | next_part(hi);
+                }
             }
 #pragma unroll
             for (int q = 0; q < 3; ++q) out[q] = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
@@ -1387,6 +1230,7 @@ slicegcn_status_t forward_product(Params& P, const slicegcn_ffn_desc* d, const P
     set_pairs(P, q.x_planes, q.w_planes);
     P.chunk = P.pairs > 1 ? kChunkF32 : P.kb_total;
     P.act = d->act, P.scale = (float)d->scale, P.b = d->b, P.b2 = d->b2;
+    P.bias_vec = d->out_s % 2 == 0 && (uintptr_t)d->b % 8 == 0 && (uintptr_t)d->b2 % 8 == 0;
     if (back) {
         P.slices = q.parts * d->num_slices;   // of the sums
         if (gated) return promo ? launch<kDzGated, true>(P, st) : launch<kDzGated, false>(P, st);
@@ -1396,8 +1240,10 @@ slicegcn_status_t forward_product(Params& P, const slicegcn_ffn_desc* d, const P
     return promo ? launch<kFwd, true>(P, st) : launch<kFwd, false>(P, st);
 }
 
+// 16 bytes at a time of bf16, 8 of fp32 (as the epilogue reads and writes them)
 bool wide_access(const void* p, int64_t ld, int elem, int groups, int width) {
-    return (uintptr_t)p % 16 == 0 && ld * elem % 16 == 0 && (groups == 1 || width * elem % 16 == 0);
+    const int unit = elem == 2 ? 16 : 8;
+    return (uintptr_t)p % unit == 0 && ld * elem % unit == 0 && (groups == 1 || width * elem % unit == 0);
 }
 
 }  // namespace
@@ -1438,7 +1284,7 @@ slicegcn_status_t slicegcn_ffn_forward(const slicegcn_ffn_desc* d, const void* x
     SGCN_TRY(operands(d, q, x, static_cast<char*>(workspace), ox, ow, ow2, st));
     Params P = {};
     P.status = status;
-    P.in = r, P.in_ld = d->r_ld, P.in_bf16 = e == 2, P.in_vec = r && wide_access(r, d->r_ld, e, p, d->out_s);
+    P.in = r, P.in_ld = d->r_ld, P.in_vec = r && wide_access(r, d->r_ld, e, p, d->out_s);
     P.out = out, P.out_ld = d->out_ld, P.out_bf16 = e == 2, P.out_vec = wide_access(out, d->out_ld, e, p, d->out_s);
     return forward_product(P, d, q, ox, ow, ow2, false, st);
 }
@@ -1474,9 +1320,9 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
     if (q.dz) {
         Params P = {};
         P.status = status;
-        P.in = dout, P.in_ld = d->dout_ld, P.in_bf16 = ge == 2, P.in_vec = wide_access(dout, d->dout_ld, ge, p, d->out_s);
+        P.in = dout, P.in_ld = d->dout_ld, P.in_vec = wide_access(dout, d->dout_ld, ge, p, d->out_s);
         P.dz = reinterpret_cast<__nv_bfloat16*>(ws + q.z_at);
-        P.dz_row = (int64_t)q.parts * p * q.out_pad, P.dz_plane = n * P.dz_row, P.dz_planes = q.z_planes, P.dz_pad = q.out_pad;
+        P.dz_row = (int64_t)q.parts * p * q.out_pad, P.dz_plane = n * P.dz_row, P.dz_pad = q.out_pad;
         P.sums = sums ? reinterpret_cast<float*>(ws + q.sums_at) : nullptr;
         SGCN_TRY(forward_product(P, d, q, ox, ow, ow2, true, st));
         oz.base = P.dz, oz.rows = n, oz.ld = P.dz_row, oz.group_stride = q.out_pad, oz.plane_stride = P.dz_plane;

@@ -183,3 +183,17 @@ def test_backward(shape, gated, types):
     for act, pad in (("silu", 0), ("gelu", 8), ("none", 3)):
         q = Problem(*shape, gated, act, dtype, grad, pad=pad, seed=len(act))
         q.check_backward(q.backward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("types", ["bf16", "fp32", "bf16/fp32"])
+@pytest.mark.parametrize("shape", [(30_000, 8, 48, 40), (50_001, 1, 300, 72), (40_000, 2, 72, 300), (20_000, 1, 700, 700)], ids=str)
+def test_many_tiles_per_pair_of_sms(shape, types):
+    """Several tiles one after another on every pair of SMs, of half and of whole width, with one and with many chunks of k."""
+    dtype, grad = types.split("/") if "/" in types else (types, "same")
+    for gated in (False, True):
+        q = Problem(*shape, gated, "silu", dtype, grad)
+        q.check_forward(q.forward())
+        q.check_backward(q.backward())
+        q = Problem(*shape, gated, "none", dtype, grad)
+        q.check_backward(q.backward())
