@@ -51,7 +51,7 @@ Divide divide_by(int d) {
 }
 
 struct Params {
-    CUtensorMap a, b0, b1;
+    CUtensorMap a, b0, b1, o;      // o: bf16 results, da and dc
     int n;                         // rows of x
     int p, slices;                 // slices; slices times parts of the output (kDw), else the same
     int tiles_m, tiles_n, group;   // per slice; m tiles that follow one another before the next n tile
@@ -65,20 +65,17 @@ struct Params {
     int splits;                    // kDw: pieces of the rows, kb_total steps each
     int splits_rows;               // kDw
     // epilogue
-    int act, cols;                 // columns of D per slice
+    int cols;                      // columns of D per slice
     float scale;
     const float *b, *b2;           // [slices][cols]
     int bias_vec;                  // two of them at a time are aligned
     const void* in;                // r or dout
-    int64_t in_ld;
+    int in_ld;
     int in_vec;
     void* out;
-    int64_t out_ld;
+    int out_ld;
     int out_bf16, out_vec;
-    // kDz: planes of da (and dc after it) in the workspace, and sums over 32 rows each
-    __nv_bfloat16* dz;
-    int64_t dz_plane, dz_row;      // elements between planes and between rows
-    int dz_pad;                    // columns of one (part, slice)
+    // kDz: sums over 32 rows each
     float* sums;                   // [ceil(n/32)][parts * p][cols], or NULL
     // kDw
     float* partial;                // [splits][slices][k][cols of A]
@@ -145,6 +142,16 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar) & 0xFEFFFFFFu)
         : "memory");
 }
+// One box of shared memory to a tensor map; what lies outside the tensor is left out.  Groups of them are waited for by the lane that issued them.
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int x, int y, int z, int w) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];\n\tcp.async.bulk.commit_group;" ::"l"(map), "r"(src),
+                 "r"(x), "r"(y), "r"(z), "r"(w)
+                 : "memory");
+}
+template <int PENDING>
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -161,29 +168,29 @@ __device__ __forceinline__ void umma_commit(uint64_t* bar) {
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // 32 lanes x 16 columns: a lane gets its row
-__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* r) {
+__device__ __forceinline__ void tmem_rows(uint32_t addr, float (&r)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+          "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
         : "r"(addr)
         : "memory");
 }
 // 16 lanes x 32 columns as fragments of 8x8 matrices
-__device__ __forceinline__ void tmem_fragments(uint32_t addr, uint32_t* r) {
+__device__ __forceinline__ void tmem_fragments(uint32_t addr, float (&r)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+          "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
         : "r"(addr)
         : "memory");
 }
 // The wait takes part in the registers' dataflow, so that no use of them moves in front of it.
 #define SGCN_R16(r)                                                                                                                              \
-    "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), \
-        "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-__device__ __forceinline__ void tmem_wait(uint32_t* r) { asm volatile("tcgen05.wait::ld.sync.aligned;" : SGCN_R16(r)::"memory"); }
-__device__ __forceinline__ void after_wait(uint32_t* r) { asm volatile("" : SGCN_R16(r)::"memory"); }
+    "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), \
+        "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15])
+__device__ __forceinline__ void tmem_wait(float (&r)[16]) { asm volatile("tcgen05.wait::ld.sync.aligned;" : SGCN_R16(r)::"memory"); }
+__device__ __forceinline__ void after_wait(float (&r)[16]) { asm volatile("" : SGCN_R16(r)::"memory"); }
 #undef SGCN_R16
 
 // Operand tiles, 128-byte swizzle.  k contiguous: rows of 64 k, 8-row groups 1 KB apart.  Rows (or columns) contiguous: blocks of
@@ -205,15 +212,11 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&t);
 }
-// A slab: 32 rows of 64 bytes, 16-byte chunks exchanged so that neither matrices nor lines meet bank conflicts.
+// A slab: 32 rows of 64 bytes, 16-byte chunks exchanged as tensor copies with the 64-byte swizzle do; neither matrices nor lines meet
+// bank conflicts.
 __device__ __forceinline__ uint32_t slab_at(int row, int chunk) { return (uint32_t)(row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4)); }
 __device__ __forceinline__ void sts16(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-__device__ __forceinline__ uint4 lds16(uint32_t a) {
-    uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-    return v;
 }
 // Line i of eight rows: row 8 i + lane / 4, chunk lane % 4.
 __device__ __forceinline__ uint32_t line_at(uint32_t slab, int lane, int i) { return slab + i * 512 + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4); }
@@ -250,28 +253,16 @@ struct Where {
     int rows;              // how many of them exist
 };
 
-// Lines [from, to) of the slab to memory; of its 32 rows x 32 columns `rows` and `cols` exist.
-__device__ __forceinline__ void slab_out(__nv_bfloat16* at, int64_t ld, int rows, int cols, bool vec, uint32_t slab, int lane, int from, int to) {
-    if (vec && cols >= 8) {
-        __nv_bfloat16* p = at + (int64_t)(8 * from + (lane >> 2)) * ld + (lane & 3) * 8;
-        const bool mine = cols >= 32 || cols - (lane & 3) * 8 >= 8;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < from || i >= to) continue;
-            if (mine && (rows == 32 || i * 8 + (lane >> 2) < rows)) *reinterpret_cast<uint4*>(p) = lds16(line_at(slab, lane, i));
-            p += 8 * ld;
-        }
-        if (cols >= 32 || cols % 8 == 0) return;
-    }
-    // element by element: all columns, or those behind the last eight
-    const int first = vec ? min(cols, 32) & ~7 : 0;
-    if (lane >= first && lane < cols)
+// The slab to memory whose rows no tensor copy can reach, element by element.
+__device__ __forceinline__ void slab_out(__nv_bfloat16* at, int ld, int rows, int cols, uint32_t slab, int lane) {
+    if (lane < cols)
 #pragma unroll 4
-        for (int i = 8 * from; i < min(rows, 8 * to); ++i) {
+        for (int i = 0; i < rows; ++i) {
             uint16_t v;
             asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(slab + slab_at(i, lane >> 3) + (lane & 7) * 2) : "memory");
             reinterpret_cast<uint16_t*>(at)[(int64_t)i * ld + lane] = v;
         }
+    __syncwarp();
 }
 // 32 rows x 32 columns of r or dout in bf16: asked for here (whole chunks, where they are aligned) ...
 __device__ __forceinline__ void load_in(const Params& P, const Where& w, int col, uint4 (&raw)[4], int lane) {
@@ -279,12 +270,17 @@ __device__ __forceinline__ void load_in(const Params& P, const Where& w, int col
 #pragma unroll
     for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
     if (!P.in_vec || w.rows <= 0 || left < 8) return;
-    const char* at = static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col + (lane & 3) * 8) * 2;
+    const __nv_bfloat16* at = static_cast<const __nv_bfloat16*>(P.in) + ((int64_t)w.row * P.in_ld + (w.slice * P.cols + col + (lane & 3) * 8));
+    if (w.rows == 32) {
+        at += (int64_t)(lane >> 2) * P.in_ld;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const uint4*>(at + (int64_t)i * 8 * P.in_ld);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int row = i * 8 + (lane >> 2);
-        const uint4 t = *reinterpret_cast<const uint4*>(at + (int64_t)min(row, w.rows - 1) * P.in_ld * 2);
-        if (row < w.rows) raw[i] = t;
+        if (row < w.rows) raw[i] = *reinterpret_cast<const uint4*>(at + (int64_t)row * P.in_ld);
     }
 }
 // ... and laid into the slab here, with what no whole chunk holds.
@@ -295,7 +291,7 @@ __device__ __forceinline__ void put_in(const Params& P, const Where& w, int col,
     if (from >= cols || w.rows <= 0) return;
     __syncwarp();
     if (lane >= from && lane < cols) {
-        const uint16_t* at = static_cast<const uint16_t*>(P.in) + (int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols + col + lane;
+        const uint16_t* at = static_cast<const uint16_t*>(P.in) + (int64_t)w.row * P.in_ld + (w.slice * P.cols + col + lane);
 #pragma unroll 8
         for (int i = 0; i < w.rows; ++i) {
             const uint16_t v = at[(int64_t)i * P.in_ld];
@@ -343,20 +339,19 @@ __device__ __forceinline__ void load_bias(const Params& P, const float* b, int s
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = 0.f;
     if (!b) return;
-    const float* at = b + (int64_t)slice * P.cols;
+    const int c0 = col + 2 * (lane & 3);
+    const float* at = b + (slice * P.cols + c0);
+    if (P.bias_vec && col + 32 <= P.cols) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int c = col + 8 * j + 2 * (lane & 3);
-        if (P.bias_vec) {
-            if (c < P.cols) {
-                const float2 t = __ldg(reinterpret_cast<const float2*>(at + c));
-                v[2 * j] = t.x, v[2 * j + 1] = t.y;
-            }
-        } else {
-            if (c < P.cols) v[2 * j] = __ldg(at + c);
-            if (c + 1 < P.cols) v[2 * j + 1] = __ldg(at + c + 1);
+        for (int j = 0; j < 4; ++j) {
+            const float2 t = __ldg(reinterpret_cast<const float2*>(at) + 4 * j);
+            v[2 * j] = t.x, v[2 * j + 1] = t.y;
         }
+        return;
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (c0 + 8 * (j >> 1) + (j & 1) < P.cols) v[j] = __ldg(at + 8 * (j >> 1) + (j & 1));
 }
 __device__ __forceinline__ void add_bias(float (&v)[16], const float (&b)[8]) {
 #pragma unroll
@@ -437,17 +432,6 @@ __device__ __forceinline__ void forward_as(float (&a)[16], const float (&c)[16])
         if (GATED) a[k] *= c[k];
     }
 }
-template <bool GATED, bool ACCURATE>
-__device__ __forceinline__ void forward_math(const Params& P, float (&a)[16], const float (&c)[16]) {
-    if (P.act == SLICEGCN_ACT_SILU)
-        forward_as<SLICEGCN_ACT_SILU, GATED, ACCURATE>(a, c);
-    else if (P.act == SLICEGCN_ACT_GELU)
-        forward_as<SLICEGCN_ACT_GELU, GATED, ACCURATE>(a, c);
-    else if (P.act == SLICEGCN_ACT_RELU)
-        forward_as<SLICEGCN_ACT_RELU, GATED, ACCURATE>(a, c);
-    else
-        forward_as<SLICEGCN_ACT_NONE, GATED, ACCURATE>(a, c);
-}
 // a, c -> da, dc
 template <int ACT, bool GATED, bool ACCURATE>
 __device__ __forceinline__ void backward_as(float scale, const float (&g)[16], float (&a)[16], float (&c)[16]) {
@@ -460,18 +444,6 @@ __device__ __forceinline__ void backward_as(float scale, const float (&g)[16], f
         if (GATED) c[k] = gk * y;
     }
 }
-template <bool GATED, bool ACCURATE>
-__device__ __forceinline__ void backward_math(const Params& P, const float (&g)[16], float (&a)[16], float (&c)[16]) {
-    if (P.act == SLICEGCN_ACT_SILU)
-        backward_as<SLICEGCN_ACT_SILU, GATED, ACCURATE>(P.scale, g, a, c);
-    else if (P.act == SLICEGCN_ACT_GELU)
-        backward_as<SLICEGCN_ACT_GELU, GATED, ACCURATE>(P.scale, g, a, c);
-    else if (P.act == SLICEGCN_ACT_RELU)
-        backward_as<SLICEGCN_ACT_RELU, GATED, ACCURATE>(P.scale, g, a, c);
-    else
-        backward_as<SLICEGCN_ACT_NONE, GATED, ACCURATE>(P.scale, g, a, c);
-}
-
 // Parts of an fp32 number whose sum it is: 8 bits each.  Cut, not rounded: no part leaves the range, and each is exact.  Takes the
 // next part off x.
 __device__ __forceinline__ uint32_t next_part(float& x) {
@@ -479,9 +451,8 @@ __device__ __forceinline__ uint32_t next_part(float& x) {
     x = isfinite(x) ? x - __uint_as_float(part) : 0.f;
     return part;
 }
-// Half h of da or dc as three planes, by way of the slab.
-__device__ __forceinline__ void planes_out(const Params& P, const Where& w, int part, int col, int h, float (&v)[16], uint32_t slab, int lane) {
-    __nv_bfloat16* at = P.dz + (int64_t)w.row * P.dz_row + (int64_t)(part * P.p + w.slice) * P.dz_pad + col;
+// Half h of da or dc as three planes, by way of the slabs' four halves in turn.
+__device__ __forceinline__ void planes_out(const Params& P, const Where& w, int part, int col, int h, float (&v)[16], uint32_t slab, int& halves, int lane) {
 #pragma unroll
     for (int q = 0; q < 3; ++q) {
         uint32_t words[8];
@@ -490,10 +461,14 @@ __device__ __forceinline__ void planes_out(const Params& P, const Where& w, int 
             const uint32_t lo = next_part(v[2 * k]), hi = next_part(v[2 * k + 1]);
             words[k] = lo >> 16 | hi;
         }
+        if (lane == 0) stores_read<3>();
         __syncwarp();
-        half_to_slab(words, slab, lane, h);
+        const uint32_t at = slab + (halves & 3) * 1024;
+        ++halves;
+        half_to_slab(words, at, lane, 0);
+        proxy_fence();
         __syncwarp();
-        slab_out(at + q * P.dz_plane, P.dz_row, w.rows, P.dz_pad - col, true, slab, lane, 2 * h, 2 * h + 2);
+        if (lane == 0 && w.rows > 16 * h) tma_store(&P.o, at, col, w.row + 16 * h, part * P.p + w.slice, q);
     }
 }
 __device__ __forceinline__ void sums_out(const Params& P, const Where& w, int part, int col, float (&s)[8], int lane) {
@@ -531,7 +506,7 @@ __device__ __forceinline__ Item item_of(const Params& P, int i) {
 }
 
 // PROMO: the accumulator is emptied into registers every P.chunk steps (fp32 digits, or long sums).
-template <int MODE, bool PROMO>
+template <int MODE, bool PROMO, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_kernel(const __grid_constant__ Params P) {
     constexpr bool kGated = MODE == kFwdGated || MODE == kDzGated;
     constexpr bool kIsDz = MODE == kDz || MODE == kDzGated;
@@ -672,10 +647,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
         const uint32_t mine = tmem + ((uint32_t)(quarter * 32) << 16) + part * share;
         const int second = kGated ? P.nt : 32;   // columns from the first 32 to the other 32
         bool ok = true;
-        int turn = 0;
+        int turn = 0, halves = 0;
+        Item ahead;   // of turn / 32 * 32 + lane: 32 tiles are worked out at once, each lane one, and passed around when their turn comes
         for (int i = first; ok && i < P.items; i += stride, ++turn) {
+            if ((turn & 31) == 0) ahead = item_of<MODE>(P, min(i + lane * stride, P.items - 1));
             if ((turn & (groups - 1)) != group) continue;
-            const Item t = item_of<MODE>(P, i);
+            Item t;
+            t.m = __shfl_sync(0xffffffffu, ahead.m, turn & 31);
+            t.n = __shfl_sync(0xffffffffu, ahead.n, turn & 31);
+            t.slice = __shfl_sync(0xffffffffu, ahead.slice, turn & 31);
+            t.split = MODE == kDw ? __shfl_sync(0xffffffffu, ahead.split, turn & 31) : 0;
             Where w;
             w.slice = t.slice;
             w.row = t.m + (int)rank * 128 + quarter * 32;
@@ -692,11 +673,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     fence_after();
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        uint32_t r[16];
-                        tmem_ld16(mine + (group * 2 + (use & 1)) * (2 * P.nt) + u * 16, r);
+                        float r[16];
+                        tmem_rows(mine + (group * 2 + (use & 1)) * (2 * P.nt) + u * 16, r);
                         tmem_wait(r);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) acc[u * 16 + j] += __uint_as_float(r[j]);
+                        for (int j = 0; j < 16; ++j) acc[u * 16 + j] += r[j];
                     }
                     fence_before();
                     __syncwarp();
@@ -733,11 +714,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     const uint32_t d = mine + (group * 2 + (use & 1)) * (2 * P.nt);
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        uint32_t r[16];
+                        float r[16];
                         tmem_fragments(d + (u & 2 ? second : 0) + ((uint32_t)((u & 1) * 16) << 16), r);
                         tmem_wait(r);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) acc[u * 16 + j] += __uint_as_float(r[j]);
+                        for (int j = 0; j < 16; ++j) acc[u * 16 + j] += r[j];
                     }
                     fence_before();
                     __syncwarp();
@@ -763,13 +744,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                         float in[16];
                         if (kIsDz || (MODE != kDx && P.in)) load_half_f32(P, w, col, h, in, lane);
                         if constexpr (kIsDz) {
-                            backward_math<kGated, true>(P, in, a, c);
+                            backward_as<ACT, kGated, true>(P.scale, in, a, c);
                             sum_half(a, s);
                             if (kGated) sum_half(c, s2);
-                            planes_out(P, w, 0, col, h, a, slab, lane);
-                            if (kGated) planes_out(P, w, 1, col, h, c, slab2, lane);
+                            planes_out(P, w, 0, col, h, a, slab, halves, lane);
+                            if (kGated) planes_out(P, w, 1, col, h, c, slab, halves, lane);
                         } else {
-                            if (MODE != kDx) forward_math<kGated, true>(P, a, c);
+                            if (MODE != kDx) forward_as<ACT, kGated, true>(a, c);
 #pragma unroll
                             for (int j = 0; j < 16; ++j) a[j] = MODE != kDx && P.in ? fmaf(a[j], P.scale, in[j]) : a[j] * P.scale;
                             store_half_f32(P, w, col, h, a, lane);
@@ -796,33 +777,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                 for (int u = 0; u < (kGated ? 1 : 2); ++u) {
                     const int col = col0 + u * 32;
                     const bool last = kGated || u == 1;
-                    uint32_t ra[16], rc[16];
-                    tmem_fragments(d + u * 32, ra);
-                    if (kGated) tmem_fragments(d + second, rc);
+                    float a[16], c[16], s[8], s2[8];
+                    // da and dc need both slabs, else the two take turns, so that one leaves while the other is filled
+                    const uint32_t to = kIsDz && kGated ? slab : slab + (halves++ & 1) * 2048;
+                    tmem_fragments(d + u * 32, a);
+                    if (kGated) tmem_fragments(d + second, c);
+                    if (lane == 0) stores_read<kIsDz && kGated ? 0 : 1>();
+                    __syncwarp();
                     if (with_in) {
-                        __syncwarp();
-                        put_in(P, w, col, raw, slab, lane);
+                        put_in(P, w, col, raw, to, lane);
                         __syncwarp();
                     }
-                    tmem_wait(ra);
-                    if (kGated) after_wait(rc);
-                    float s[8], s2[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) s[j] = s2[j] = 0.f;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        uint32_t na[16], nc[16];
-                        if (h == 0 && !kGated) tmem_fragments(d + u * 32 + (16u << 16), na);   // comes while the first half is worked on (gated: no registers for that)
-                        float a[16], c[16];
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) a[j] = __uint_as_float(ra[j]), c[j] = kGated ? __uint_as_float(rc[j]) : 0.f;
+                        if (h) {
+                            tmem_fragments(d + u * 32 + (16u << 16), a);
+                            if (kGated) tmem_fragments(d + second + (16u << 16), c);
+                        }
+                        tmem_wait(a);
+                        if (kGated) after_wait(c);
+                        if (h && last) {
+                            fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_first(tempty + group * 2 + (use & 1));
+                        }
                         if (MODE != kDx) add_bias(a, bias);
                         if (kGated) add_bias(c, bias2);
                         float in[16];
-                        if (with_in) half_from_slab(in, slab, lane, h);
+                        if (with_in) half_from_slab(in, to, lane, h);
                         uint32_t words[8];
                         if constexpr (kIsDz) {
-                            backward_math<kGated, false>(P, in, a, c);
+                            backward_as<ACT, kGated, false>(P.scale, in, a, c);
                             if (P.sums) {
                                 sum_half(a, s);
                                 if (kGated) sum_half(c, s2);
@@ -832,7 +819,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                                 half_to_slab(words, slab2, lane, h);
                             }
                         } else {
-                            if (MODE != kDx) forward_math<kGated, false>(P, a, c);
+                            if (MODE != kDx) forward_as<ACT, kGated, false>(a, c);
                             if (with_in) {
 #pragma unroll
                                 for (int j = 0; j < 16; ++j) a[j] = fmaf(a[j], P.scale, in[j]);
@@ -842,43 +829,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                             }
                         }
                         pack_half(a, words);
-                        half_to_slab(words, slab, lane, h);   // in the place of what came in
-                        if (h == 0) {
-                            if (kGated) tmem_fragments(d + u * 32 + (16u << 16), na), tmem_fragments(d + second + (16u << 16), nc);
-                            tmem_wait(na);
-                            if (kGated) after_wait(nc);
-                            if (last) {
-                                fence_before();
-                                __syncwarp();
-                                if (lane == 0) mbar_arrive_first(tempty + group * 2 + (use & 1));
-                            }
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) ra[j] = na[j], rc[j] = kGated ? nc[j] : 0u;
-                        }
+                        half_to_slab(words, to, lane, h);   // in the place of what came in
                     }
+                    proxy_fence();
                     __syncwarp();
+                    const bool there = col < P.cols && w.rows > 0;
+                    if (kIsDz || P.out_vec) {
+                        if (lane == 0 && there) {
+                            tma_store(&P.o, to, col, w.row, w.slice, 0);
+                            if (kIsDz && kGated) tma_store(&P.o, slab2, col, w.row, P.p + w.slice, 0);
+                        }
+                    } else if (there) {
+                        slab_out(static_cast<__nv_bfloat16*>(P.out) + (int64_t)w.row * P.out_ld + (w.slice * P.cols + col), P.out_ld, w.rows, P.cols - col, to, lane);
+                    }
+                    if (kIsDz && P.sums && there) {
+                        sums_out(P, w, 0, col, s, lane);
+                        if (kGated) sums_out(P, w, 1, col, s2, lane);
+                    }
                     if (!last) {
                         load_bias(P, MODE == kDx ? nullptr : P.b, w.slice, col + 32, bias, lane);
                         if (with_in) load_in(P, w, col + 32, raw, lane);
                     }
-                    if (col < P.cols && w.rows > 0) {
-                        if constexpr (kIsDz) {
-                            __nv_bfloat16* at = P.dz + (int64_t)w.row * P.dz_row + (int64_t)w.slice * P.dz_pad + col;
-                            slab_out(at, P.dz_row, w.rows, P.dz_pad - col, true, slab, lane, 0, 4);
-                            if (kGated) slab_out(at + (int64_t)P.p * P.dz_pad, P.dz_row, w.rows, P.dz_pad - col, true, slab2, lane, 0, 4);
-                            if (P.sums) {
-                                sums_out(P, w, 0, col, s, lane);
-                                if (kGated) sums_out(P, w, 1, col, s2, lane);
-                            }
-                        } else {
-                            slab_out(static_cast<__nv_bfloat16*>(P.out) + (int64_t)w.row * P.out_ld + (int64_t)w.slice * P.cols + col, P.out_ld, w.rows,
-                                     P.cols - col, P.out_vec, slab, lane, 0, 4);
-                        }
-                    }
-                    __syncwarp();   // the slab is free again
                 }
             }
         }
+        if (lane == 0) stores_done();
         if (!ok && lane == 0 && P.status) atomicExch(P.status, SLICEGCN_DEVSTATUS_WAIT);
     }
     __syncwarp();
@@ -1023,7 +998,7 @@ struct Operand {
     int64_t rows = 0, ld = 0, group_stride = 0, plane_stride = 0;
     int width = 0, groups = 1, planes = 1;
 };
-slicegcn_status_t make_map(CUtensorMap* map, const Operand& o, int box_rows) {
+slicegcn_status_t make_map(CUtensorMap* map, const Operand& o, int box_rows, bool result = false) {
     static EncodeFn encode = [] {
         void* fn = nullptr;
         cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
@@ -1035,9 +1010,9 @@ slicegcn_status_t make_map(CUtensorMap* map, const Operand& o, int box_rows) {
     const cuuint64_t dims[4] = {(cuuint64_t)o.width, (cuuint64_t)o.rows, (cuuint64_t)o.groups, (cuuint64_t)o.planes};
     const cuuint64_t strides[3] = {(cuuint64_t)(o.rows > 1 ? o.ld : 8) * 2, (cuuint64_t)(o.groups > 1 ? o.group_stride : 8) * 2,
                                    (cuuint64_t)(o.planes > 1 ? o.plane_stride : 8) * 2};
-    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {result ? 32u : 64u, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
     const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(o.base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                              result ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) SGCN_FAIL(SLICEGCN_ERR_CUDA, "ffn: tensor map refused (%d)", (int)r);
     return SLICEGCN_OK;
 }
@@ -1127,7 +1102,7 @@ slicegcn_status_t check_matrix(const char* name, const void* p, int64_t ld, int6
     if (!p && needed) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "ffn: %s is NULL", name);
     if (!p) return SLICEGCN_OK;
     if (ld < cols) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "ffn: leading dimension of %s too small", name);
-    if (ld > ((int64_t)1 << 38)) SGCN_FAIL(SLICEGCN_ERR_OVERFLOW, "ffn: leading dimension of %s too large", name);
+    if (ld > INT32_MAX) SGCN_FAIL(SLICEGCN_ERR_OVERFLOW, "ffn: leading dimension of %s too large", name);
     if ((uintptr_t)p % (dtype == SLICEGCN_F32 ? 4 : 2)) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "ffn: %s is not aligned to its type", name);
     return SLICEGCN_OK;
 }
@@ -1157,10 +1132,19 @@ void set_pairs(Params& P, int pa, int pb) {
             if (order - i < pb) P.ia[P.pairs] = (int8_t)i, P.ib[P.pairs] = (int8_t)(order - i), ++P.pairs;
 }
 
+template <int MODE, bool PROMO, int ACT>
+slicegcn_status_t launch_as(const Params& P, cudaStream_t st) {
+    SGCN_CUDA(cudaFuncSetAttribute(ffn_kernel<MODE, PROMO, ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    return launch_after(ffn_kernel<MODE, PROMO, ACT>, dim3(2 * std::min(P.items, kPairs)), kThreads, kSmem, st, P);
+}
 template <int MODE, bool PROMO>
-slicegcn_status_t launch(const Params& P, cudaStream_t st) {
-    SGCN_CUDA(cudaFuncSetAttribute(ffn_kernel<MODE, PROMO>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-    return launch_after(ffn_kernel<MODE, PROMO>, dim3(2 * std::min(P.items, kPairs)), kThreads, kSmem, st, P);
+slicegcn_status_t launch(const Params& P, int act, cudaStream_t st) {
+    switch (act) {
+        case SLICEGCN_ACT_RELU: return launch_as<MODE, PROMO, SLICEGCN_ACT_RELU>(P, st);
+        case SLICEGCN_ACT_SILU: return launch_as<MODE, PROMO, SLICEGCN_ACT_SILU>(P, st);
+        case SLICEGCN_ACT_GELU: return launch_as<MODE, PROMO, SLICEGCN_ACT_GELU>(P, st);
+        default: return launch_as<MODE, PROMO, SLICEGCN_ACT_NONE>(P, st);
+    }
 }
 
 // Steps between emptyings: fp32's digits allow 256 k (16 additions in tensor memory); bf16 results only need it for long sums.
@@ -1229,21 +1213,30 @@ slicegcn_status_t forward_product(Params& P, const slicegcn_ffn_desc* d, const P
     P.k_part = d->in_s;
     set_pairs(P, q.x_planes, q.w_planes);
     P.chunk = P.pairs > 1 ? kChunkF32 : P.kb_total;
-    P.act = d->act, P.scale = (float)d->scale, P.b = d->b, P.b2 = d->b2;
+    P.scale = (float)d->scale, P.b = d->b, P.b2 = d->b2;
     P.bias_vec = d->out_s % 2 == 0 && (uintptr_t)d->b % 8 == 0 && (uintptr_t)d->b2 % 8 == 0;
     if (back) {
         P.slices = q.parts * d->num_slices;   // of the sums
-        if (gated) return promo ? launch<kDzGated, true>(P, st) : launch<kDzGated, false>(P, st);
-        return promo ? launch<kDz, true>(P, st) : launch<kDz, false>(P, st);
+        if (gated) return promo ? launch<kDzGated, true>(P, d->act, st) : launch<kDzGated, false>(P, d->act, st);
+        return promo ? launch<kDz, true>(P, d->act, st) : launch<kDz, false>(P, d->act, st);
     }
-    if (gated) return promo ? launch<kFwdGated, true>(P, st) : launch<kFwdGated, false>(P, st);
-    return promo ? launch<kFwd, true>(P, st) : launch<kFwd, false>(P, st);
+    if (gated) return promo ? launch<kFwdGated, true>(P, d->act, st) : launch<kFwdGated, false>(P, d->act, st);
+    return promo ? launch<kFwd, true>(P, d->act, st) : launch<kFwd, false>(P, d->act, st);
 }
 
 // 16 bytes at a time of bf16, 8 of fp32 (as the epilogue reads and writes them)
 bool wide_access(const void* p, int64_t ld, int elem, int groups, int width) {
     const int unit = elem == 2 ? 16 : 8;
     return (uintptr_t)p % unit == 0 && ld * elem % unit == 0 && (groups == 1 || width * elem % unit == 0);
+}
+
+// Where a product's result goes: bf16 by tensor copies, where they can reach it.
+slicegcn_status_t set_result(Params& P, void* out, int64_t ld, int elem, int groups, int width, int64_t rows) {
+    P.out = out, P.out_ld = (int)ld, P.out_bf16 = elem == 2, P.out_vec = wide_access(out, ld, elem, groups, width);
+    if (elem != 2 || !P.out_vec) return SLICEGCN_OK;
+    Operand o;
+    o.base = out, o.rows = rows, o.ld = ld, o.group_stride = width, o.width = width, o.groups = groups;
+    return make_map(&P.o, o, 32, true);
 }
 
 }  // namespace
@@ -1284,8 +1277,8 @@ slicegcn_status_t slicegcn_ffn_forward(const slicegcn_ffn_desc* d, const void* x
     SGCN_TRY(operands(d, q, x, static_cast<char*>(workspace), ox, ow, ow2, st));
     Params P = {};
     P.status = status;
-    P.in = r, P.in_ld = d->r_ld, P.in_vec = r && wide_access(r, d->r_ld, e, p, d->out_s);
-    P.out = out, P.out_ld = d->out_ld, P.out_bf16 = e == 2, P.out_vec = wide_access(out, d->out_ld, e, p, d->out_s);
+    P.in = r, P.in_ld = (int)d->r_ld, P.in_vec = r && wide_access(r, d->r_ld, e, p, d->out_s);
+    SGCN_TRY(set_result(P, out, d->out_ld, e, p, d->out_s, d->n));
     return forward_product(P, d, q, ox, ow, ow2, false, st);
 }
 
@@ -1320,13 +1313,12 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
     if (q.dz) {
         Params P = {};
         P.status = status;
-        P.in = dout, P.in_ld = d->dout_ld, P.in_vec = wide_access(dout, d->dout_ld, ge, p, d->out_s);
-        P.dz = reinterpret_cast<__nv_bfloat16*>(ws + q.z_at);
-        P.dz_row = (int64_t)q.parts * p * q.out_pad, P.dz_plane = n * P.dz_row, P.dz_pad = q.out_pad;
+        P.in = dout, P.in_ld = (int)d->dout_ld, P.in_vec = wide_access(dout, d->dout_ld, ge, p, d->out_s);
         P.sums = sums ? reinterpret_cast<float*>(ws + q.sums_at) : nullptr;
-        SGCN_TRY(forward_product(P, d, q, ox, ow, ow2, true, st));
-        oz.base = P.dz, oz.rows = n, oz.ld = P.dz_row, oz.group_stride = q.out_pad, oz.plane_stride = P.dz_plane;
+        oz.base = ws + q.z_at, oz.rows = n, oz.ld = (int64_t)q.parts * p * q.out_pad, oz.group_stride = q.out_pad, oz.plane_stride = n * oz.ld;
         oz.width = d->out_s, oz.groups = q.parts * p, oz.planes = q.z_planes;
+        SGCN_TRY(make_map(&P.o, oz, q.z_planes == 1 ? 32 : 16, true));
+        SGCN_TRY(forward_product(P, d, q, ox, ow, ow2, true, st));
     } else if (q.pack_g) {
         SGCN_TRY(pack(dout, d->dout_ld, n, p, d->out_s, ge == 2, ws + q.z_at, oz, st));
     } else {
@@ -1344,9 +1336,9 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         set_pairs(P, q.z_planes, q.w_planes);
         const bool promo = P.pairs > 1;
         P.chunk = promo ? kChunkF32 : P.kb_total;
-        P.act = SLICEGCN_ACT_NONE, P.scale = scale;
-        P.out = dx, P.out_ld = d->dx_ld, P.out_bf16 = ge == 2, P.out_vec = wide_access(dx, d->dx_ld, ge, p, d->in_s);
-        SGCN_TRY((promo ? launch<kDx, true>(P, st) : launch<kDx, false>(P, st)));
+        P.scale = scale;
+        SGCN_TRY(set_result(P, dx, d->dx_ld, ge, p, d->in_s, n));
+        SGCN_TRY((promo ? launch_as<kDx, true, SLICEGCN_ACT_NONE>(P, st) : launch_as<kDx, false, SLICEGCN_ACT_NONE>(P, st)));
     }
     if (dW || dW2) {
         Params P = {};
@@ -1364,7 +1356,7 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         P.scale = scale, P.out_bf16 = ge == 2;
         P.partial = reinterpret_cast<float*>(ws + q.partial_at);
         P.dw = dW, P.dw2 = dW2;
-        SGCN_TRY((launch<kDw, true>(P, st)));
+        SGCN_TRY((launch_as<kDw, true, SLICEGCN_ACT_NONE>(P, st)));
         if (q.splits > 1) {
             JoinArgs J = {P.partial, q.splits, ge == 2, (int64_t)q.parts * d->in_s * outs, d->in_s * outs, scale, {dW, dW2}};
             SGCN_TRY(launch_after(ffn_join_kernel, dim3((unsigned)std::min<int64_t>((J.total + 255) / 256, 148 * 8)), 256, 0, st, J));
