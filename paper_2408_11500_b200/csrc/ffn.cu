@@ -142,12 +142,14 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar) & 0xFEFFFFFFu)
         : "memory");
 }
-// One box of shared memory to a tensor map; what lies outside the tensor is left out.  Groups of them are waited for by the lane that issued them.
+// One box of shared memory to a tensor map; what lies outside the tensor is left out.  Groups of them are waited for by the lane that
+// issued them; a turn without a box commits its (empty) group too, since the waits count groups.
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int x, int y, int z, int w) {
-    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];\n\tcp.async.bulk.commit_group;" ::"l"(map), "r"(src),
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map), "r"(src),
                  "r"(x), "r"(y), "r"(z), "r"(w)
                  : "memory");
 }
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int PENDING>
 __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory"); }
 __device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
@@ -380,7 +382,7 @@ __device__ __forceinline__ int sum_column(int lane) {
 }
 
 // 1 / (1 + exp(-w)).  Where results are rounded to bf16 the hardware's exponential and reciprocal (2^-22 each, and 2^-24 |w| of the
-// argument) are exact enough; `t` is -w log2(e).
+// argument) are exact enough (one reciprocal for two numbers, 1/x = y/(xy), gained nothing); `t` is -w log2(e).
 __device__ __forceinline__ float sigmoid_of(float t) {
     float e, q;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
@@ -468,7 +470,10 @@ __device__ __forceinline__ void planes_out(const Params& P, const Where& w, int 
         half_to_slab(words, at, lane, 0);
         proxy_fence();
         __syncwarp();
-        if (lane == 0 && w.rows > 16 * h) tma_store(&P.o, at, col, w.row + 16 * h, part * P.p + w.slice, q);
+        if (lane == 0) {
+            if (w.rows > 16 * h) tma_store(&P.o, at, col, w.row + 16 * h, part * P.p + w.slice, q);
+            stores_commit();
+        }
     }
 }
 __device__ __forceinline__ void sums_out(const Params& P, const Where& w, int part, int col, float (&s)[8], int lane) {
@@ -835,9 +840,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     __syncwarp();
                     const bool there = col < P.cols && w.rows > 0;
                     if (kIsDz || P.out_vec) {
-                        if (lane == 0 && there) {
-                            tma_store(&P.o, to, col, w.row, w.slice, 0);
-                            if (kIsDz && kGated) tma_store(&P.o, slab2, col, w.row, P.p + w.slice, 0);
+                        if (lane == 0) {
+                            if (there) {
+                                tma_store(&P.o, to, col, w.row, w.slice, 0);
+                                if (kIsDz && kGated) tma_store(&P.o, slab2, col, w.row, P.p + w.slice, 0);
+                            }
+                            stores_commit();
                         }
                     } else if (there) {
                         slab_out(static_cast<__nv_bfloat16*>(P.out) + (int64_t)w.row * P.out_ld + (w.slice * P.cols + col), P.out_ld, w.rows, P.cols - col, to, lane);
