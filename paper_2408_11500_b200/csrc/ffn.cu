@@ -55,15 +55,15 @@ struct Params {
     int n;                         // rows of x
     int p, slices;                 // slices; slices times parts of the output (kDw), else the same
     int tiles_m, tiles_n, group;   // per slice; m tiles that follow one another before the next n tile
-    Divide by_first, by_n, by_m, by_last;   // what item_of divides by
+    Divide by_split, by_group, by_n, by_m, by_last;   // what item_of divides by
     int items;
     int nt;                        // columns of B per CTA: 64 or 128
     int kb_total, kb_part, k_part; // 64-wide steps of an item, of one part of k, and that part's extent
     int chunk;                     // steps between emptyings of the accumulator
     int pairs;                     // products of operand parts
     int8_t ia[6], ib[6];
-    int splits;                    // kDw: pieces of the rows, kb_total steps each
-    int splits_rows;               // kDw
+    int splits;                    // pieces of k (kDw: of the rows), kb_total steps each
+    int swapped, pair;             // kDw: a tile's rows are dW's; and its column halves are dW's and dW2's
     // epilogue
     int cols;                      // columns of D per slice
     float scale;
@@ -77,9 +77,9 @@ struct Params {
     int out_bf16, out_vec;
     // kDz: sums over 32 rows each
     float* sums;                   // [ceil(n/32)][parts * p][cols], or NULL
-    // kDw
-    float* partial;                // [splits][slices][k][cols of A]
-    void *dw, *dw2;                // splits == 1
+    float* partial;                // splits > 1: the pieces' products; kDw: [splits][slices][in_s][out_s], else [splits][slices][n][cols]
+    int matrices;                  // kDw: slices times parts
+    void *dw, *dw2;                // kDw, splits == 1
     int32_t* status;
 };
 
@@ -426,19 +426,19 @@ __device__ __forceinline__ void act_both(float a, float& y, float& dy) {
         dy = 1.f;
     }
 }
-template <int ACT, bool GATED, bool ACCURATE>
-__device__ __forceinline__ void forward_as(float (&a)[16], const float (&c)[16]) {
+template <int ACT, bool GATED, bool ACCURATE, int N>
+__device__ __forceinline__ void forward_as(float (&a)[N], const float (&c)[N]) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
+    for (int k = 0; k < N; ++k) {
         a[k] = act_of<ACT, ACCURATE>(a[k]);
         if (GATED) a[k] *= c[k];
     }
 }
 // a, c -> da, dc
-template <int ACT, bool GATED, bool ACCURATE>
-__device__ __forceinline__ void backward_as(float scale, const float (&g)[16], float (&a)[16], float (&c)[16]) {
+template <int ACT, bool GATED, bool ACCURATE, int N>
+__device__ __forceinline__ void backward_as(float scale, const float (&g)[N], float (&a)[N], float (&c)[N]) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
+    for (int k = 0; k < N; ++k) {
         float y, dy;
         act_both<ACT, ACCURATE>(a[k], y, dy);
         const float gk = g[k] * scale;
@@ -491,21 +491,20 @@ template <int MODE>
 __device__ __forceinline__ Item item_of(const Params& P, int i) {
     Item t;
     const int cols = 2 * P.nt;
-    const int per_tile = MODE == kFwdGated || MODE == kDzGated ? P.nt : cols;   // columns of D that a tile makes
+    const int per_tile = MODE == kFwdGated || MODE == kDzGated || (MODE == kDw && P.pair) ? P.nt : cols;   // columns of D that a tile makes
+    t.split = P.splits > 1 ? P.by_split(i) : 0;
+    i -= t.split * P.by_split.d;
     if (MODE == kDw) {
-        t.split = P.by_first(i);
-        i -= t.split * P.by_first.d;
         const int above = P.by_n(i);
         t.n = (i - above * P.tiles_n) * per_tile;
         t.slice = P.by_m(above);
         t.m = (above - t.slice * P.tiles_m) * 256;
     } else {   // `group` row tiles side by side, then the next column tile: operands come from L2 in between
-        const int g = P.by_first(i), rest = i - g * P.by_first.d, size = min(P.group, P.tiles_m - g * P.group);
+        const int g = P.by_group(i), rest = i - g * P.by_group.d, size = min(P.group, P.tiles_m - g * P.group);
         const int c = size == P.group ? P.by_m(rest) : P.by_last(rest);
         t.m = (g * P.group + rest - c * size) * 256;
         t.slice = P.by_n(c);
         t.n = (c - t.slice * P.tiles_n) * per_tile;
-        t.split = 0;
     }
     return t;
 }
@@ -558,13 +557,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
         int fill = 0, st = 0;
         uint32_t phase = 1;
         const uint32_t bytes = 2u * (16384u + (uint32_t)P.nt * 128u);
-        const CUtensorMap* other = kGated && rank ? &P.b1 : &P.b0;
         for (int i = first; ok && i < P.items; i += stride) {
             const Item t = item_of<MODE>(P, i);
             const int row0 = t.m + (int)rank * 128;
-            const int slice = MODE == kDw && t.slice >= P.p ? t.slice - P.p : t.slice;
-            const int bcol = kGated ? t.n : t.n + (int)rank * P.nt;
-            const int k0 = MODE == kDw ? t.split * P.kb_total * 64 : 0;
+            const bool upper = !kGated && t.slice >= P.p;            // the second projection's
+            const int slice = upper ? t.slice - P.p : t.slice;
+            const int aslice = MODE == kDw && !P.swapped ? t.slice : slice;
+            const int bslice = MODE == kDw && P.swapped ? t.slice + (P.pair ? (int)rank * P.p : 0) : slice;
+            const CUtensorMap* bmap = (kGated && rank) || (MODE == kFwd && upper) ? &P.b1 : &P.b0;
+            const int bcol = kGated || (MODE == kDw && P.pair) ? t.n : t.n + (int)rank * P.nt;
+            const int first_kb = t.split * P.kb_total;
             for (int c = 0; ok && c < chunks; ++c) {
                 const int kb0 = c * P.chunk, kb1 = min(kb0 + P.chunk, P.kb_total);
                 for (int q = 0; ok && q < P.pairs; ++q)
@@ -572,21 +574,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                         ok = __all_sync(0xffffffffu, mbar_wait(empty + st, phase));
                         if (!ok) break;
                         const uint32_t a = base + st * kStageBytes, b = a + 16384u;
-                        const bool second = MODE == kDx && kb >= P.kb_part;
-                        const int k = k0 + (second ? kb - P.kb_part : kb) * 64;
+                        const bool second = MODE == kDx && first_kb + kb >= P.kb_part;
+                        const int k = (first_kb + kb - (second ? P.kb_part : 0)) * 64;   // past the end there are only zeros
                         if (one) {
                             if (rank == 0) mbar_expect(full + st, bytes);
                             if (kAK) {
                                 tma_load(a, &P.a, k, row0, second ? P.p + slice : slice, P.ia[q], full + st);
                             } else {
-                                tma_load(a, &P.a, row0, k, t.slice, P.ia[q], full + st);
-                                tma_load(a + 8192, &P.a, row0 + 64, k, t.slice, P.ia[q], full + st);
+                                tma_load(a, &P.a, row0, k, aslice, P.ia[q], full + st);
+                                tma_load(a + 8192, &P.a, row0 + 64, k, aslice, P.ia[q], full + st);
                             }
                             if (kBK) {
                                 tma_load(b, second ? &P.b1 : &P.b0, k, bcol, slice, P.ib[q], full + st);
                             } else {
-                                tma_load(b, other, bcol, k, slice, P.ib[q], full + st);
-                                if (P.nt > 64) tma_load(b + 8192, other, bcol + 64, k, slice, P.ib[q], full + st);
+                                tma_load(b, bmap, bcol, k, bslice, P.ib[q], full + st);
+                                if (P.nt > 64) tma_load(b + 8192, bmap, bcol + 64, k, bslice, P.ib[q], full + st);
                             }
                         }
                         __syncwarp();
@@ -606,6 +608,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
             const uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | (kAK ? 0u : 1u << 15) | (kBK ? 0u : 1u << 16) | (uint32_t)(2 * P.nt >> 3) << 17 | 16u << 24;
             for (int i = first; ok && i < P.items; i += stride, ++turn) {
                 int use = (turn >> groups_log) * chunks;
+                const int first_kb = P.splits > 1 ? P.by_split(i) * P.kb_total : 0;
                 for (int c = 0; ok && c < chunks; ++c, ++use) {
                     const int kb0 = c * P.chunk, kb1 = min(kb0 + P.chunk, P.kb_total);
                     const int acc = (turn & (groups - 1)) * 2 + (use & 1);
@@ -621,11 +624,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                             fence_after();
                             const uint32_t at = base + st * kStageBytes;
                             const uint64_t ad = tile_desc(at, kAK), bd = tile_desc(at + 16384u, kBK);
-                            const int left = MODE == kDw ? 64 : P.k_part - (kb >= P.kb_part ? kb - P.kb_part : kb) * 64;   // past the end there are only zeros
+                            const int at_kb = first_kb + kb;
+                            const int left = MODE == kDw ? 64 : P.k_part - (at_kb >= P.kb_part ? at_kb - P.kb_part : at_kb) * 64;   // past the end there are only zeros
                             if (one) {
 #pragma unroll
                                 for (int s = 0; s < 4; ++s)
-                                    if (s * 16 < left) umma(d, ad + (uint64_t)(s * (kAK ? 2 : 128)), bd + (uint64_t)(s * (kBK ? 2 : 128)), idesc, s > 0 || more);
+                                    if (s == 0 || s * 16 < left) umma(d, ad + (uint64_t)(s * (kAK ? 2 : 128)), bd + (uint64_t)(s * (kBK ? 2 : 128)), idesc, s > 0 || more);
                                 umma_commit(empty + st);
                             }
                             __syncwarp();
@@ -661,7 +665,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
             t.m = __shfl_sync(0xffffffffu, ahead.m, turn & 31);
             t.n = __shfl_sync(0xffffffffu, ahead.n, turn & 31);
             t.slice = __shfl_sync(0xffffffffu, ahead.slice, turn & 31);
-            t.split = MODE == kDw ? __shfl_sync(0xffffffffu, ahead.split, turn & 31) : 0;
+            t.split = PROMO ? __shfl_sync(0xffffffffu, ahead.split, turn & 31) : 0;
             Where w;
             w.slice = t.slice;
             w.row = t.m + (int)rank * 128 + quarter * 32;
@@ -689,22 +693,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     if (lane == 0) mbar_arrive_first(tempty + group * 2 + (use & 1));
                 }
                 if (!ok) break;
-                const int f = w.row + lane, fs = P.cols, ks = P.k_part;   // this lane's column of dW; its rows are this tile's columns
-                if (f < fs) {
+                // this lane's row of the tile, dW's column (swapped: its row); the tile's columns are dW's rows (columns)
+                const int m = w.row + lane, fs = P.cols, ks = P.k_part;
+                const int m_end = P.swapped ? ks : fs, n_end = P.swapped ? fs : ks;
+                const int64_t m_step = P.swapped ? fs : 1, n_step = P.swapped ? 1 : fs, matrix = (int64_t)ks * fs;
+                const bool upper = P.pair ? part * share >= P.nt : t.slice >= P.p;   // dW2's
+                const int slice = P.pair || !upper ? t.slice : t.slice - P.p, n0 = P.pair && upper ? col0 - P.nt : col0;
+                if (m < m_end) {
+                    const int64_t from = m * m_step + n0 * n_step;
                     if (P.splits > 1) {
-                        float* to = P.partial + (((int64_t)t.split * P.slices + t.slice) * ks + col0) * fs + f;
+                        float* to = P.partial + ((int64_t)t.split * P.matrices + (upper ? P.p : 0) + slice) * matrix + from;
 #pragma unroll
                         for (int j = 0; j < 64; ++j)
-                            if (col0 + j < ks) to[(int64_t)j * fs] = acc[j];
-                    } else if (void* dw = t.slice < P.p ? P.dw : P.dw2) {
-                        const int64_t at = ((int64_t)(t.slice < P.p ? t.slice : t.slice - P.p) * ks + col0) * fs + f;
+                            if (n0 + j < n_end) to[j * n_step] = acc[j];
+                    } else if (void* dw = upper ? P.dw2 : P.dw) {
+                        const int64_t at = slice * matrix + from;
 #pragma unroll
                         for (int j = 0; j < 64; ++j)
-                            if (col0 + j < ks) {
+                            if (n0 + j < n_end) {
                                 if (P.out_bf16)
-                                    static_cast<__nv_bfloat16*>(dw)[at + (int64_t)j * fs] = __float2bfloat16_rn(acc[j] * P.scale);
+                                    static_cast<__nv_bfloat16*>(dw)[at + j * n_step] = __float2bfloat16_rn(acc[j] * P.scale);
                                 else
-                                    static_cast<float*>(dw)[at + (int64_t)j * fs] = acc[j] * P.scale;
+                                    static_cast<float*>(dw)[at + j * n_step] = acc[j] * P.scale;
                             }
                     }
                 }
@@ -734,6 +744,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                 for (int u = 0; u < (kGated ? 1 : 2); ++u) {
                     const int col = col0 + u * 32;
                     if (col >= P.cols || w.rows <= 0) continue;
+                    if ((MODE == kFwd || MODE == kDx) && P.splits > 1) {   // a piece's product, as it is
+                        float* at = P.partial + ((int64_t)t.split * P.slices + w.slice) * P.n * P.cols;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            const int row = w.row + 8 * ((k >> 1) & 1) + 16 * (k >> 4) + (lane >> 2), c = col + 8 * ((k >> 2) & 3) + 2 * (lane & 3) + (k & 1);
+                            if (row < P.n && c < P.cols) at[(int64_t)row * P.cols + c] = acc[u * 32 + k];
+                        }
+                        continue;
+                    }
                     float bias[8], bias2[8], s[8], s2[8];
                     load_bias(P, MODE == kDx ? nullptr : P.b, w.slice, col, bias, lane);
                     if (kGated) load_bias(P, P.b2, w.slice, col, bias2, lane);
@@ -877,20 +896,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
 // ------------------------------------------------------------------------------------------ small kernels
 
 // A matrix of rows x groups x width (row stride ld) as bf16 planes [plane][row][group][pad], pad the next multiple of 8 (filled with
-// zeros): fp32 as three planes, bf16 as one.  A thread makes 16 bytes of each plane.
-struct PackArgs {
+// zeros): fp32 as three planes, bf16 as one.  A thread makes 16 bytes of each plane.  Up to four matrices in a launch.
+struct PackJob {
     const void* src;
     int64_t ld, rows, plane;
-    int groups, width, pad, bf16;
+    int groups, width, pad, bf16, vec;
+    int ctas;
     __nv_bfloat16* dst;
 };
-__global__ void __launch_bounds__(256) ffn_pack_kernel(const __grid_constant__ PackArgs A) {
+struct PackArgs {
+    int count;
+    PackJob job[4];
+};
+__global__ void __launch_bounds__(256) ffn_pack_kernel(const __grid_constant__ PackArgs args) {
     cudaGridDependencySynchronize();
     cudaTriggerProgrammaticLaunchCompletion();
+    int cta = blockIdx.x, k = 0;
+    while (cta >= args.job[k].ctas) cta -= args.job[k++].ctas;
+    const PackJob& A = args.job[k];
     const int per_group = A.pad / 8, per_row = per_group * A.groups;
     const int64_t total = A.rows * per_row;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / per_row;
+    for (int64_t i = (int64_t)cta * 256 + threadIdx.x; i < total; i += (int64_t)A.ctas * 256) {
+        const int64_t row = total < (1ll << 32) ? (int64_t)((uint32_t)i / (uint32_t)per_row) : i / per_row;
         const int in_row = (int)(i - row * per_row), g = in_row / per_group, c = (in_row - g * per_group) * 8;
         const int64_t at = row * A.ld + (int64_t)g * A.width + c;
         const int left = A.width - c;
@@ -899,25 +926,32 @@ __global__ void __launch_bounds__(256) ffn_pack_kernel(const __grid_constant__ P
             const uint16_t* s = static_cast<const uint16_t*>(A.src) + at;
             uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                w[k] = (2 * k < left ? (uint32_t)s[2 * k] : 0u) | (2 * k + 1 < left ? (uint32_t)s[2 * k + 1] << 16 : 0u);
+            for (int q = 0; q < 4; ++q)
+                w[q] = (2 * q < left ? (uint32_t)s[2 * q] : 0u) | (2 * q + 1 < left ? (uint32_t)s[2 * q + 1] << 16 : 0u);
             out[0] = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
             const float* s = static_cast<const float*>(A.src) + at;
+            float v[8];
+            if (A.vec && left >= 8) {
+                const float4 a = *reinterpret_cast<const float4*>(s), b = *reinterpret_cast<const float4*>(s + 4);
+                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] = q < left ? s[q] : 0.f;
+            }
             uint32_t w[3][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float lo = 2 * k < left ? s[2 * k] : 0.f, hi = 2 * k + 1 < left ? s[2 * k + 1] : 0.f;
-                if (isnan(lo)) lo = __int_as_float(0x7fc00000);   // one whose upper half alone is a NaN too
-                if (isnan(hi)) hi = __int_as_float(0x7fc00000);
+            for (int q = 0; q < 8; ++q)
+                if (isnan(v[q])) v[q] = __int_as_float(0x7fc00000);   // one whose upper half alone is a NaN too
 #pragma unroll
-                for (int q = 0; q < 3; ++q) {
-                    const uint32_t l = next_part(lo);
-                    w[q][k] = l >> 16 | next_part(hi);
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                    const uint32_t lo = next_part(v[2 * q]);
+                    w[part][q] = lo >> 16 | next_part(v[2 * q + 1]);
                 }
-            }
 #pragma unroll
-            for (int q = 0; q < 3; ++q) out[q] = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+            for (int part = 0; part < 3; ++part) out[part] = make_uint4(w[part][0], w[part][1], w[part][2], w[part][3]);
         }
         __nv_bfloat16* d = A.dst + i * 8;
         *reinterpret_cast<uint4*>(d) = out[0];
@@ -928,63 +962,101 @@ __global__ void __launch_bounds__(256) ffn_pack_kernel(const __grid_constant__ P
     }
 }
 
-// Sums of columns, in a fixed order: chunks of rows by the first kernel, the chunks by the second.
-constexpr int kSumChunks = 128;
+// Sums of columns, in a fixed order: chunks of rows by the first kernel, the chunks by the second.  A warp reads whole lines, 16 bytes
+// a lane where they are aligned, and eight rows are on their way together.
+constexpr int kSumChunks = 512;
 struct SumArgs {
     const void* src;
     int64_t rows, ld, per;    // rows of a chunk
-    int cols, bf16;
+    int cols, bf16, vec;
     float* partial;           // [chunks][cols]
 };
+template <bool BF16, bool VEC>
 __global__ void __launch_bounds__(256) ffn_colsum_kernel(const __grid_constant__ SumArgs A) {
-    __shared__ float sh[8][33];
+    constexpr int W = VEC ? (BF16 ? 8 : 4) : 1;
+    __shared__ float sh[8][32 * W + 1];
     cudaGridDependencySynchronize();
     cudaTriggerProgrammaticLaunchCompletion();
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = (blockIdx.x * 32 + x) * W;
     const int64_t r0 = blockIdx.y * A.per, r1 = min(r0 + A.per, A.rows);
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    if (c < A.cols) {
-        int64_t r = r0 + y;
-        for (; r + 24 < r1; r += 32) {
+    float s[W];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int64_t at = (r + 8 * k) * A.ld + c;
-                s[k] += A.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(A.src)[at]) : static_cast<const float*>(A.src)[at];
+    for (int k = 0; k < W; ++k) s[k] = 0.f;
+    if (c < A.cols) {
+        auto add = [&](const uint4& t) {
+            const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+            for (int k = 0; k < (VEC ? 4 : 0); ++k) {
+                if (BF16)
+                    s[(2 * k) % W] += __uint_as_float(w[k] << 16), s[(2 * k + 1) % W] += __uint_as_float(w[k] & 0xffff0000u);
+                else
+                    s[k % W] += __uint_as_float(w[k]);
             }
-        }
-        for (; r < r1; r += 8) {
+        };
+        auto get = [&](int64_t r) {
             const int64_t at = r * A.ld + c;
-            s[0] += A.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(A.src)[at]) : static_cast<const float*>(A.src)[at];
+            if (VEC) return BF16 ? *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(A.src) + at)
+                                 : *reinterpret_cast<const uint4*>(static_cast<const float*>(A.src) + at);
+            const float v = BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(A.src)[at]) : static_cast<const float*>(A.src)[at];
+            return make_uint4(__float_as_uint(v), 0, 0, 0);
+        };
+        auto put = [&](const uint4& t) {
+            if (VEC)
+                add(t);
+            else
+                s[0] += __uint_as_float(t.x);
+        };
+        int64_t r = r0 + y;
+        for (; r + 56 < r1; r += 64) {
+            uint4 t[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t[k] = get(r + 8 * k);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) put(t[k]);
         }
+        for (; r < r1; r += 8) put(get(r));
     }
-    sh[y][x] = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+    for (int k = 0; k < W; ++k) sh[y][x * W + k] = s[k];
     __syncthreads();
-    if (y == 0 && c < A.cols) {
+    for (int k = threadIdx.x; k < 32 * W; k += 256) {
+        const int col = blockIdx.x * 32 * W + k;
+        if (col >= A.cols) break;
         float t = 0.f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t += sh[k][x];
-        A.partial[(int64_t)blockIdx.y * A.cols + c] = t;
+        for (int q = 0; q < 8; ++q) t += sh[q][k];
+        A.partial[(int64_t)blockIdx.y * A.cols + col] = t;
     }
 }
-// out[0][i] (i < each) and out[1][i - each] = scale * the sum over `count` pieces of `total` numbers each
-struct JoinArgs {
+// out[0][i] (i < each) and out[1][i - each] = scale * the sum over `count` pieces of `total` numbers each.  Up to two such jobs in a launch.
+struct JoinJob {
     const float* partial;
     int count, bf16;
     int64_t total, each;
     float scale;
     void* out[2];
+    int ctas;
 };
-__global__ void __launch_bounds__(256) ffn_join_kernel(const __grid_constant__ JoinArgs A) {
+struct JoinArgs {
+    JoinJob job[2];
+};
+__global__ void __launch_bounds__(256) ffn_join_kernel(const __grid_constant__ JoinArgs args) {
     cudaGridDependencySynchronize();
     cudaTriggerProgrammaticLaunchCompletion();
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < A.total; i += (int64_t)gridDim.x * 256) {
+    const int second_job = blockIdx.x >= args.job[0].ctas, cta = blockIdx.x - (second_job ? args.job[0].ctas : 0);
+    const JoinJob& A = args.job[second_job];
+    for (int64_t i = (int64_t)cta * 256 + threadIdx.x; i < A.total; i += (int64_t)A.ctas * 256) {
         const int second = i >= A.each;
         if (!A.out[second]) continue;
         float s[4] = {0.f, 0.f, 0.f, 0.f};
         int k = 0;
-        for (; k + 4 <= A.count; k += 4)
+        for (; k + 8 <= A.count; k += 8) {
+            float t[8];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s[q] += A.partial[(k + q) * A.total + i];
+            for (int q = 0; q < 8; ++q) t[q] = A.partial[(k + q) * A.total + i];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s[q & 3] += t[q];
+        }
         for (; k < A.count; ++k) s[0] += A.partial[k * A.total + i];
         const float v = ((s[0] + s[1]) + (s[2] + s[3])) * A.scale;
         const int64_t at = second ? i - A.each : i;
@@ -993,6 +1065,271 @@ __global__ void __launch_bounds__(256) ffn_join_kernel(const __grid_constant__ J
         else
             static_cast<float*>(A.out[second])[at] = v;
     }
+}
+
+// Where few tiles have a long k, pieces of k are different items, and this kernel adds their products up and does what the
+// product's epilogue does otherwise.  A CTA has 32 rows x 32 columns, a thread four rows of a column.
+struct FinishArgs {
+    const float* partial;     // [splits][parts * p][n][cols]
+    int splits, n, p, cols, gated, act, back;
+    float scale;
+    const float *b, *b2;
+    const void* in;           // r or dout
+    int64_t in_ld;
+    void* out;                // out or dx
+    int64_t out_ld;
+    int in_bf16, out_bf16;
+    __nv_bfloat16* dz;        // back: planes of da and dc
+    int64_t dz_plane;
+    int dz_row, dz_pad, dz_planes;
+    float* sums;
+};
+template <int ACT>
+__device__ __forceinline__ void finish_as(const FinishArgs& A, const float (&in)[4], float (&a)[4], float (&c)[4]) {
+    if (A.back) {
+        if (A.gated)
+            backward_as<ACT, true, true>(A.scale, in, a, c);
+        else
+            backward_as<ACT, false, true>(A.scale, in, a, c);
+    } else {
+        if (A.gated)
+            forward_as<ACT, true, true>(a, c);
+        else
+            forward_as<ACT, false, true>(a, c);
+    }
+}
+__global__ void __launch_bounds__(256) ffn_finish_kernel(const __grid_constant__ FinishArgs A) {
+    __shared__ float sh[2][8][33];
+    cudaGridDependencySynchronize();
+    cudaTriggerProgrammaticLaunchCompletion();
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int blocks = (A.cols + 31) / 32, slice = blockIdx.x / blocks, col = (blockIdx.x - slice * blocks) * 32 + x;
+    const int row0 = blockIdx.y * 32 + y;
+    const bool there = col < A.cols;
+    const int64_t slot = (int64_t)A.n * A.cols, piece = slot * A.p * (1 + A.gated);
+    float a[4], c[4], in[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int row = row0 + 8 * k;
+        a[k] = c[k] = in[k] = 0.f;
+        if (!there || row >= A.n) continue;
+        const float* at = A.partial + slice * slot + (int64_t)row * A.cols + col;
+        for (int s = 0; s < A.splits; ++s) {
+            a[k] += at[s * piece];
+            if (A.gated) c[k] += at[s * piece + A.p * slot];
+        }
+        if (A.b) a[k] += A.b[slice * A.cols + col];
+        if (A.b2) c[k] += A.b2[slice * A.cols + col];
+        if (A.in) {
+            const int64_t i = (int64_t)row * A.in_ld + slice * A.cols + col;
+            in[k] = A.in_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(A.in)[i]) : static_cast<const float*>(A.in)[i];
+        }
+    }
+    if (A.act == SLICEGCN_ACT_SILU)
+        finish_as<SLICEGCN_ACT_SILU>(A, in, a, c);
+    else if (A.act == SLICEGCN_ACT_GELU)
+        finish_as<SLICEGCN_ACT_GELU>(A, in, a, c);
+    else if (A.act == SLICEGCN_ACT_RELU)
+        finish_as<SLICEGCN_ACT_RELU>(A, in, a, c);
+    else
+        finish_as<SLICEGCN_ACT_NONE>(A, in, a, c);
+    if (!A.back) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = row0 + 8 * k;
+            if (!there || row >= A.n) continue;
+            const int64_t i = (int64_t)row * A.out_ld + slice * A.cols + col;
+            const float v = fmaf(a[k], A.scale, in[k]);
+            if (A.out_bf16)
+                static_cast<__nv_bfloat16*>(A.out)[i] = __float2bfloat16_rn(v);
+            else
+                static_cast<float*>(A.out)[i] = v;
+        }
+        return;
+    }
+    if (A.sums) {
+        sh[0][y][x] = (a[0] + a[1]) + (a[2] + a[3]);   // rows past the end have no dout and add nothing
+        sh[1][y][x] = (c[0] + c[1]) + (c[2] + c[3]);
+    }
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+        if (part && !A.gated) break;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = row0 + 8 * k;
+            if (!there || row >= A.n) continue;
+            __nv_bfloat16* to = A.dz + (int64_t)row * A.dz_row + (part * A.p + slice) * A.dz_pad + col;
+            float v = part ? c[k] : a[k];
+            if (A.dz_planes == 1) {
+                *to = __float2bfloat16_rn(v);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint16_t*>(to + q * A.dz_plane) = (uint16_t)(next_part(v) >> 16);
+            }
+        }
+    }
+    if (A.sums) {
+        __syncthreads();
+        if (y < 1 + A.gated && there) {
+            float t = 0.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) t += sh[y][q][x];
+            A.sums[((int64_t)blockIdx.y * (A.p * (1 + A.gated)) + y * A.p + slice) * A.cols + col] = t;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ a few rows
+//
+// Up to eight rows (serving): bound by reading the weights once, which tiles of 256 rows would do with few SMs and, in fp32, three
+// times over.  A cluster has 128 columns; its CTAs and their warps split k.  Plain fp32 multiply-adds; the warps' sums meet in shared memory, the
+// CTAs' in distributed shared memory.  One launch, no workspace.
+constexpr int kRowsThreads = 256, kRowsCols = 128;
+struct RowsArgs {
+    const void* x;
+    int64_t x_ld;
+    const void *W, *W2;
+    const float *b, *b2;
+    const void* r;
+    int64_t r_ld;
+    void* out;
+    int64_t out_ld;
+    int n, in_s, out_s, act, per;   // per: k of a CTA, a multiple of 8
+    float scale;
+};
+template <bool BF16>
+__device__ __forceinline__ float load_one(const void* p, int64_t i) {
+    return BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+// Four of a lane's columns of one row of weights, as they lie in memory: neighbours (VEC), else every 32nd.
+template <bool BF16, bool VEC>
+struct Quad {
+    float v[4];
+    __device__ __forceinline__ void load(const void* W, int64_t at, int col, int out_s, int lane) {
+        if (VEC) {
+            const int64_t i = at + min(col + lane * 4, out_s - 4);
+            if (BF16) {
+                const uint2 t = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(W) + i));
+                v[0] = __uint_as_float(t.x), v[1] = __uint_as_float(t.y);
+            } else {
+                const float4 t = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(W) + i));
+                v[0] = t.x, v[1] = t.y, v[2] = t.z, v[3] = t.w;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = load_one<BF16>(W, at + min(col + lane + 32 * j, out_s - 1));
+        }
+    }
+    __device__ __forceinline__ float get(int j) const {
+        if (VEC && BF16) {
+            const uint32_t t = __float_as_uint(v[j >> 1]);
+            return __uint_as_float(j & 1 ? t & 0xffff0000u : t << 16);
+        }
+        return v[j];
+    }
+};
+template <int R, bool GATED, bool BF16, bool VEC>
+__global__ void __launch_bounds__(kRowsThreads) ffn_rows_kernel(const __grid_constant__ RowsArgs A) {
+    constexpr int V = R * (1 + GATED);
+    extern __shared__ __align__(16) float rows_smem[];
+    float* xs = rows_smem;                        // [R][per]
+    float* red = rows_smem + R * A.per;           // [8][V][128], then [V][128] in its first part
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t parts;
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(parts));
+    const uint32_t rank = cluster_rank();
+    const int slice = blockIdx.y, col0 = (int)(blockIdx.x / parts) * kRowsCols, k0 = (int)rank * A.per;
+    const int kc = max(0, min(A.per, A.in_s - k0));
+    cudaGridDependencySynchronize();
+    cudaTriggerProgrammaticLaunchCompletion();
+    for (int i = threadIdx.x; i < R * A.per; i += kRowsThreads) {
+        const int r = i / A.per, k = i - r * A.per;
+        xs[i] = r < A.n && k < kc ? load_one<BF16>(A.x, r * A.x_ld + (int64_t)slice * A.in_s + k0 + k) : 0.f;
+    }
+    __syncthreads();
+    float acc[V][4];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[v][j] = 0.f;
+    const int64_t base = ((int64_t)slice * A.in_s + k0) * A.out_s;
+    constexpr int D = R == 1 && !GATED ? 16 : 8;  // rows of weights on their way together
+    for (int k = warp * D; k < kc; k += 8 * D) {
+        Quad<BF16, VEC> w[D], w2[D];
+#pragma unroll
+        for (int q = 0; q < D; ++q) {             // rows past the end repeat the last one; x is zero there
+            const int64_t at = base + (int64_t)min(k + q, kc - 1) * A.out_s;
+            w[q].load(A.W, at, col0, A.out_s, lane);
+            if (GATED) w2[q].load(A.W2, at, col0, A.out_s, lane);
+        }
+#pragma unroll
+        for (int q0 = 0; q0 < D; q0 += 4) {
+            if (q0 >= 8 && k + q0 >= A.per) break;   // per is a multiple of 8, D may be 16
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float4 x4 = *reinterpret_cast<const float4*>(xs + r * A.per + k + q0);
+                const float xv[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        acc[r][j] = fmaf(xv[q], w[q0 + q].get(j), acc[r][j]);
+                        if (GATED) acc[(R + r) % V][j] = fmaf(xv[q], w2[q0 + q].get(j), acc[(R + r) % V][j]);
+                    }
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float* to = red + (warp * V + v) * kRowsCols;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[VEC ? lane * 4 + j : lane + 32 * j] = acc[v][j];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < V * kRowsCols; i += kRowsThreads) {
+        float t = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) t += red[q * V * kRowsCols + i];
+        red[i] = t;                               // read by this thread alone so far
+    }
+    if (parts > 1)
+        cluster_sync();
+    else
+        __syncthreads();
+    const int share = kRowsCols / (int)parts;     // columns that this CTA finishes
+    for (int i = threadIdx.x; i < R * share; i += kRowsThreads) {
+        const int r = i / share, c = (int)rank * share + (i - r * share), col = col0 + c;
+        float a[1] = {0.f}, g[1] = {0.f};
+        for (uint32_t q = 0; q < parts; ++q) {
+            uint32_t at = smem_u32(red + r * kRowsCols + c);
+            asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(at) : "r"(q));
+            float t;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(t) : "r"(at) : "memory");
+            a[0] += t;
+            if (GATED) {
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(t) : "r"(at + R * kRowsCols * 4) : "memory");
+                g[0] += t;
+            }
+        }
+        if (r >= A.n || col >= A.out_s) continue;
+        const int at = slice * A.out_s + col;
+        if (A.b) a[0] += A.b[at];
+        if (GATED && A.b2) g[0] += A.b2[at];
+        if (A.act == SLICEGCN_ACT_SILU)
+            forward_as<SLICEGCN_ACT_SILU, GATED, true>(a, g);
+        else if (A.act == SLICEGCN_ACT_GELU)
+            forward_as<SLICEGCN_ACT_GELU, GATED, true>(a, g);
+        else if (A.act == SLICEGCN_ACT_RELU)
+            forward_as<SLICEGCN_ACT_RELU, GATED, true>(a, g);
+        else
+            forward_as<SLICEGCN_ACT_NONE, GATED, true>(a, g);
+        const float v = A.r ? fmaf(a[0], A.scale, load_one<BF16>(A.r, r * A.r_ld + at)) : a[0] * A.scale;
+        if (BF16)
+            static_cast<__nv_bfloat16*>(A.out)[r * A.out_ld + at] = __float2bfloat16_rn(v);
+        else
+            static_cast<float*>(A.out)[r * A.out_ld + at] = v;
+    }
+    if (parts > 1) cluster_sync();                // no CTA's memory goes while another reads it
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -1020,37 +1357,100 @@ slicegcn_status_t make_map(CUtensorMap* map, const Operand& o, int box_rows, boo
                                    (cuuint64_t)(o.planes > 1 ? o.plane_stride : 8) * 2};
     const cuuint32_t box[4] = {result ? 32u : 64u, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
     const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(o.base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              result ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                              result ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) SGCN_FAIL(SLICEGCN_ERR_CUDA, "ffn: tensor map refused (%d)", (int)r);
     return SLICEGCN_OK;
 }
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
-int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Steps between emptyings: fp32's digits allow 256 k (16 additions in tensor memory); bf16 results only need it for long sums.
+constexpr int kChunkF32 = 4, kChunkLong = 64;
+
+// How a product is cut up.
+struct Cut {
+    int nt = 128, tiles_m = 1, tiles_n = 1, splits = 1, kb = 1, chunk = 1;   // kb: steps of a piece of k, the same for each
+    bool swapped = false, pair = false;
+    double cost = 1e300;
+};
+// SM cycles of `items` tiles: a 64-wide step takes its MMAs' time, or with half-width tiles rather what its copies take; a tile's start
+// and end about 4,500.  Splitting k adds 12,000 (a launch, a kernel that keeps the sums in registers) and each piece's way to memory and back (3,400 bytes a cycle over all SMs).
+double cost_of(int64_t tiles, int splits, int64_t kb, int pairs, int nt, double piece_bytes) {
+    const double step = nt == 128 ? 512 : 430;
+    return (double)ceil_div(tiles * splits, kPairs) * ((double)kb * pairs * step + 4500.0) +
+           (splits > 1 ? 12000.0 + 2.0 * splits * piece_bytes / 3400.0 : 0.0);
+}
+int pairs_of(int pa, int pb) {
+    int n = 0;
+    for (int i = 0; i < pa; ++i)
+        for (int j = 0; j < pb; ++j) n += i + j < 3;
+    return n;
+}
+// Tiles of a product over the rows of x (gated: of two at once); half-width ones where they cover the columns, or where whole ones
+// would leave pairs of SMs idle; pieces of k where there are few tiles (as two separate products then, if gated).
+Cut cut_rows(int64_t n, int p, int cols, bool gated, int64_t kb, int pairs) {
+    Cut best;
+    for (int s = 1; s <= 32; ++s) {
+        Cut c;
+        const int chunk = pairs > 1 ? kChunkF32 : 1, per = s > 1 ? (int)up(ceil_div(kb, s), chunk) : (int)kb;
+        if (s > 1 && ceil_div(kb, per) != s) continue;
+        const bool two = gated && s == 1;
+        const int one = two ? 64 : 128, slices = p * (gated && !two ? 2 : 1);
+        c.tiles_m = (int)ceil_div(n, 256);
+        c.nt = cols <= one || (int64_t)c.tiles_m * slices * ceil_div(cols, 2 * one) * s * 2 <= kPairs ? 64 : 128;
+        c.tiles_n = (int)ceil_div(cols, two ? c.nt : 2 * c.nt);
+        c.splits = s, c.kb = per, c.chunk = pairs > 1 ? kChunkF32 : per;
+        c.cost = cost_of((int64_t)slices * c.tiles_m * c.tiles_n, s, per, pairs, c.nt, 4.0 * n * slices * cols);
+        if (c.cost < best.cost) best = c;
+        if (n > 74 * 256) break;   // the SMs have work anyway
+    }
+    return best;
+}
+// Pieces of the rows for dW; which of the two operands gives the tile's 256 rows.
+Cut cut_dw(int64_t n, int p, int parts, int in_s, int out_s, int pairs) {
+    Cut best;
+    for (int swapped = 0; swapped < 2; ++swapped) {
+        const int m = swapped ? in_s : out_s, k = swapped ? out_s : in_s;
+        const int64_t all = ceil_div(n, 64);
+        for (int s = 1; s <= 2 * kPairs; ++s) {
+            Cut c;
+            c.swapped = swapped, c.splits = s;
+            c.kb = (int)ceil_div(all, s);
+            if (ceil_div(all, c.kb) != s) continue;
+            c.pair = swapped && parts == 2;
+            const int one = c.pair ? 64 : 128, slices = c.pair ? p : parts * p;
+            c.nt = k <= one ? 64 : 128;
+            c.tiles_m = (int)ceil_div(m, 256), c.tiles_n = (int)ceil_div(k, c.pair ? c.nt : 2 * c.nt);
+            c.chunk = pairs > 1 ? kChunkF32 : kChunkLong;
+            c.cost = cost_of((int64_t)slices * c.tiles_m * c.tiles_n, s, c.kb, pairs, c.nt, 4.0 * parts * p * in_s * out_s);
+            if (c.cost < best.cost) best = c;
+        }
+    }
+    return best;
+}
 
 // What a call needs in the workspace, and where.
 struct Plan {
-    bool pack_x = false, pack_w = false, pack_g = false, dz = false;
+    bool rows = false, pack_x = false, pack_w = false, pack_g = false, dz = false;
     int x_planes = 1, w_planes = 1, z_planes = 1;
-    int in_pad = 0, out_pad = 0, parts = 1, splits = 1, dw_nt = 128;
+    int in_pad = 0, out_pad = 0, parts = 1, sum_chunks = 1;
+    Cut product, dx, dw;
     int64_t x_at = 0, w_at = 0, w2_at = 0, z_at = 0, sums_at = 0, chunks_at = 0, partial_at = 0, bytes = 0;
 };
 
 bool unaligned(const void* p, int64_t ld, int groups, int width) {
     return (uintptr_t)p % 16 || ld % 8 || (groups > 1 && width % 8);
 }
-
-// Pieces of the rows for dW: as many as fill the pairs of SMs evenly, if each still is 1,024 rows or more and their sums stay a
-// fraction of what is read.
-int splits_of(int64_t tiles, int64_t n) {
-    int best = 1;
-    double cost = 1e300;
-    for (int s = 1; s <= 148; ++s) {
-        if (s > 1 && n / s < 1024) break;
-        const double c = (double)((tiles * s + kPairs - 1) / kPairs) / s * (1.0 + 0.004 * s);
-        if (c < cost) cost = c, best = s;
-    }
-    return best;
+// CTAs of a cluster that split k for a few rows, and k of each.
+int rows_parts(const slicegcn_ffn_desc* d, int* per) {
+    const int64_t blocks = ceil_div(d->out_s, kRowsCols) * d->num_slices;
+    int parts = 1;
+    while (parts < 8 && blocks * parts < 2 * 148 && d->in_s / (2 * parts) >= 64) parts *= 2;
+    while (parts < 8 && ceil_div(d->in_s, parts) > 2048) parts *= 2;
+    *per = (int)up(ceil_div(d->in_s, parts), 8);
+    return parts;
 }
 
 void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) {
@@ -1062,11 +1462,15 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
     q.out_pad = (int)up(d->out_s, 8);
     q.x_planes = q.w_planes = f32 ? 3 : 1;
     q.z_planes = d->grad_dtype == SLICEGCN_F32 ? 3 : 1;
+    if (!back && n <= 8 && d->in_s <= 16384) {
+        q.rows = true;
+        return;
+    }
     q.pack_x = f32 || unaligned(x, d->x_ld, p, d->in_s);
     q.pack_w = f32 || unaligned(d->W, d->out_s, 1, 8) || unaligned(d->W2, d->out_s, 1, 8);
     q.dz = back && (d->act != SLICEGCN_ACT_NONE || d->W2);
     q.pack_g = back && !q.dz && (q.z_planes == 3 || unaligned(dout, d->dout_ld, p, d->out_s));
-    int64_t at = 0;
+    int64_t at = 0, partial = 0;
     auto take = [&](int64_t bytes) {
         const int64_t here = at;
         at += up(bytes, 256);
@@ -1077,15 +1481,23 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
         q.w_at = take(2LL * q.w_planes * p * d->in_s * q.out_pad);
         if (d->W2) q.w2_at = take(2LL * q.w_planes * p * d->in_s * q.out_pad);
     }
-    if (back) {
-        const int64_t cols = (int64_t)q.parts * p * d->out_s;
-        if (q.dz || q.pack_g) q.z_at = take(2 * q.z_planes * n * q.parts * p * q.out_pad);
-        if (q.dz) q.sums_at = take(4 * ((n + 31) / 32) * cols);
-        q.chunks_at = take(4 * kSumChunks * cols);
-        q.dw_nt = d->in_s <= 128 ? 64 : 128;
-        q.splits = splits_of((int64_t)q.parts * p * ceil_div(d->out_s, 256) * ceil_div(d->in_s, 2 * q.dw_nt), n);
-        if (q.splits > 1) q.partial_at = take(4LL * q.splits * d->in_s * cols);
+    const int64_t cols = (int64_t)q.parts * p * d->out_s;
+    if (!back || q.dz) {
+        q.product = cut_rows(n, p, d->out_s, d->W2 != nullptr, ceil_div(d->in_s, 64), pairs_of(q.x_planes, q.w_planes));
+        if (q.product.splits > 1) partial = 4LL * q.product.splits * n * cols;
     }
+    if (back) {
+        if (q.dz || q.pack_g) q.z_at = take(2 * q.z_planes * n * q.parts * p * q.out_pad);
+        if (q.dz) q.sums_at = take(4 * ceil_div(n, 32) * cols);
+        const int64_t rows = q.dz ? ceil_div(n, 32) : n;
+        q.sum_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({kSumChunks, ceil_div(148 * 6, ceil_div(cols, 128)), rows / 64}));
+        q.chunks_at = take(4 * q.sum_chunks * cols);
+        q.dx = cut_rows(n, p, d->in_s, false, q.parts * ceil_div(d->out_s, 64), pairs_of(q.z_planes, q.w_planes));
+        if (q.dx.splits > 1) partial = std::max<int64_t>(partial, 4LL * q.dx.splits * n * p * d->in_s);
+        q.dw = cut_dw(n, p, q.parts, d->in_s, d->out_s, pairs_of(q.z_planes, q.x_planes));
+        if (q.dw.splits > 1) partial = std::max<int64_t>(partial, 4LL * q.dw.splits * d->in_s * cols);
+    }
+    if (partial) q.partial_at = take(partial);
     q.bytes = at;
 }
 
@@ -1120,16 +1532,20 @@ slicegcn_status_t check_workspace(const void* ws, int64_t have, int64_t need, co
     return SLICEGCN_OK;
 }
 
-slicegcn_status_t pack(const void* src, int64_t ld, int64_t rows, int groups, int width, bool bf16, void* dst, Operand& o, cudaStream_t st) {
-    PackArgs A;
+void add_pack(PackArgs& args, const void* src, int64_t ld, int64_t rows, int groups, int width, bool bf16, void* dst, Operand& o) {
+    PackJob& A = args.job[args.count++];
     A.src = src, A.ld = ld, A.rows = rows, A.groups = groups, A.width = width, A.pad = (int)up(width, 8), A.bf16 = bf16;
+    A.vec = !bf16 && (uintptr_t)src % 16 == 0 && ld % 4 == 0 && (groups == 1 || width % 4 == 0);
     A.plane = rows * groups * A.pad;
     A.dst = static_cast<__nv_bfloat16*>(dst);
+    A.ctas = (int)std::min<int64_t>(ceil_div(A.plane / 8, 256), 148 * 16);
     o.base = dst, o.rows = rows, o.ld = (int64_t)groups * A.pad, o.group_stride = A.pad, o.plane_stride = A.plane;
     o.width = width, o.groups = groups, o.planes = bf16 ? 1 : 3;
-    const int64_t chunks = A.plane / 8;
-    const int ctas = (int)std::min<int64_t>((chunks + 255) / 256, 148 * 16);
-    return launch_after(ffn_pack_kernel, dim3(ctas), 256, 0, st, A);
+}
+slicegcn_status_t run_packs(const PackArgs& args, cudaStream_t st) {
+    int ctas = 0;
+    for (int k = 0; k < args.count; ++k) ctas += args.job[k].ctas;
+    return ctas ? launch_after(ffn_pack_kernel, dim3(ctas), 256, 0, st, args) : SLICEGCN_OK;
 }
 
 // Products of operand parts, the smallest first.
@@ -1155,74 +1571,61 @@ slicegcn_status_t launch(const Params& P, int act, cudaStream_t st) {
     }
 }
 
-// Steps between emptyings: fp32's digits allow 256 k (16 additions in tensor memory); bf16 results only need it for long sums.
-constexpr int kChunkF32 = 4, kChunkLong = 64;
-
-// Tiles of a product over the rows of x; columns of B per CTA by what wastes least: half-width tiles where they cover the columns,
-// or where whole ones would leave pairs of SMs idle.
-void set_tiles(Params& P, int64_t n, int p, int cols, bool gated) {
-    const int one = gated ? 64 : 128;
-    P.n = (int)n, P.p = P.slices = p, P.cols = cols;
-    P.tiles_m = ceil_div(n, 256);
-    P.nt = cols <= one || (int64_t)P.tiles_m * p * ceil_div(cols, 2 * one) * 2 <= kPairs ? 64 : 128;
-    P.tiles_n = ceil_div(cols, gated ? P.nt : 2 * P.nt);
-    P.group = std::min(P.tiles_m, 8);
-    P.splits = 1;
-}
-
-slicegcn_status_t item_count(Params& P) {
-    const int64_t items = (int64_t)P.slices * P.tiles_m * P.tiles_n * P.splits;
-    if (items > (1 << 30)) SGCN_FAIL(SLICEGCN_ERR_OVERFLOW, "ffn: too many tiles");
-    P.items = (int)items;
+slicegcn_status_t set_cut(Params& P, const Cut& c, bool dw) {
+    P.nt = c.nt, P.tiles_m = c.tiles_m, P.tiles_n = c.tiles_n, P.splits = c.splits, P.kb_total = c.kb, P.chunk = c.chunk;
+    P.group = dw ? 1 : std::min(c.tiles_m, 8);
+    const int64_t tiles = (int64_t)P.slices * P.tiles_m * P.tiles_n;
+    if (tiles * P.splits > (1 << 30)) SGCN_FAIL(SLICEGCN_ERR_OVERFLOW, "ffn: too many tiles");
+    P.items = (int)tiles * P.splits;
+    P.by_split = divide_by((int)tiles);
     P.by_n = divide_by(P.tiles_n);
-    if (P.splits_rows) {
-        P.by_first = divide_by(P.slices * P.tiles_m * P.tiles_n);
-        P.by_m = P.by_last = divide_by(P.tiles_m);
-    } else {
-        P.by_first = divide_by(P.group * P.slices * P.tiles_n);
-        P.by_m = divide_by(P.group);
-        P.by_last = divide_by(std::max(1, P.tiles_m % P.group));
-    }
+    P.by_group = divide_by(P.group * P.slices * P.tiles_n);
+    P.by_m = divide_by(dw ? P.tiles_m : P.group);
+    P.by_last = divide_by(std::max(1, P.tiles_m % P.group));
     return SLICEGCN_OK;
 }
 
-// x, W and W2 as operands, laid out anew where they have to be.
-slicegcn_status_t operands(const slicegcn_ffn_desc* d, const Plan& q, const void* x, char* ws, Operand& ox, Operand& ow, Operand& ow2, cudaStream_t st) {
+// x, W and W2 as operands; what has to be laid out anew is added to the packs.
+void operands(const slicegcn_ffn_desc* d, const Plan& q, const void* x, char* ws, Operand& ox, Operand (&ow)[2], PackArgs& packs) {
     const bool bf16 = d->dtype == SLICEGCN_BF16;
     const int p = d->num_slices;
-    if (q.pack_x) {
-        SGCN_TRY(pack(x, d->x_ld, d->n, p, d->in_s, bf16, ws + q.x_at, ox, st));
-    } else {
+    if (q.pack_x)
+        add_pack(packs, x, d->x_ld, d->n, p, d->in_s, bf16, ws + q.x_at, ox);
+    else
         ox.base = x, ox.rows = d->n, ox.ld = d->x_ld, ox.group_stride = d->in_s, ox.width = d->in_s, ox.groups = p;
-    }
     for (int k = 0; k < q.parts; ++k) {
-        Operand& o = k ? ow2 : ow;
         const void* w = k ? d->W2 : d->W;
         if (q.pack_w) {
-            SGCN_TRY(pack(w, d->out_s, (int64_t)p * d->in_s, 1, d->out_s, bf16, ws + (k ? q.w2_at : q.w_at), o, st));
-            o.groups = p, o.rows = d->in_s, o.group_stride = (int64_t)d->in_s * q.out_pad;
+            add_pack(packs, w, d->out_s, (int64_t)p * d->in_s, 1, d->out_s, bf16, ws + (k ? q.w2_at : q.w_at), ow[k]);
+            ow[k].groups = p, ow[k].rows = d->in_s, ow[k].group_stride = (int64_t)d->in_s * q.out_pad;
         } else {
-            o.base = w, o.rows = d->in_s, o.ld = d->out_s, o.group_stride = (int64_t)d->in_s * d->out_s, o.width = d->out_s, o.groups = p;
+            ow[k].base = w, ow[k].rows = d->in_s, ow[k].ld = d->out_s, ow[k].group_stride = (int64_t)d->in_s * d->out_s, ow[k].width = d->out_s, ow[k].groups = p;
         }
     }
-    return SLICEGCN_OK;
+    if (q.parts == 1) ow[1] = ow[0];
 }
 
-// The product a = x W (and c = x W2) and its epilogue.
-slicegcn_status_t forward_product(Params& P, const slicegcn_ffn_desc* d, const Plan& q, const Operand& ox, const Operand& ow, const Operand& ow2, bool back,
+// The product a = x W (and c = x W2) and its epilogue, which `F` repeats for a product in pieces.
+slicegcn_status_t forward_product(Params& P, FinishArgs& F, const slicegcn_ffn_desc* d, const Plan& q, const Operand& ox, const Operand (&ow)[2], char* ws, bool back,
                                   cudaStream_t st) {
-    const bool gated = d->W2 != nullptr, promo = d->dtype == SLICEGCN_F32 || (back && d->grad_dtype == SLICEGCN_F32);
-    set_tiles(P, d->n, d->num_slices, d->out_s, gated);
-    SGCN_TRY(item_count(P));
+    const bool gated = d->W2 != nullptr, split = q.product.splits > 1;
+    const bool promo = d->dtype == SLICEGCN_F32 || (back && d->grad_dtype == SLICEGCN_F32) || split;
+    P.n = (int)d->n, P.p = d->num_slices, P.slices = split ? q.parts * d->num_slices : d->num_slices, P.cols = d->out_s;
+    SGCN_TRY(set_cut(P, q.product, false));
     SGCN_TRY(make_map(&P.a, ox, 128));
-    SGCN_TRY(make_map(&P.b0, ow, 64));
-    SGCN_TRY(make_map(&P.b1, gated ? ow2 : ow, 64));
-    P.kb_total = P.kb_part = ceil_div(d->in_s, 64);
-    P.k_part = d->in_s;
+    SGCN_TRY(make_map(&P.b0, ow[0], 64));
+    SGCN_TRY(make_map(&P.b1, ow[1], 64));
+    P.kb_part = (int)ceil_div(d->in_s, 64), P.k_part = d->in_s;
     set_pairs(P, q.x_planes, q.w_planes);
-    P.chunk = P.pairs > 1 ? kChunkF32 : P.kb_total;
     P.scale = (float)d->scale, P.b = d->b, P.b2 = d->b2;
     P.bias_vec = d->out_s % 2 == 0 && (uintptr_t)d->b % 8 == 0 && (uintptr_t)d->b2 % 8 == 0;
+    if (split) {
+        P.partial = reinterpret_cast<float*>(ws + q.partial_at);
+        SGCN_TRY((launch_as<kFwd, true, SLICEGCN_ACT_NONE>(P, st)));
+        F.partial = P.partial, F.splits = q.product.splits, F.n = P.n, F.p = P.p, F.cols = P.cols, F.gated = gated, F.act = d->act, F.back = back;
+        F.scale = P.scale, F.b = d->b, F.b2 = d->b2;
+        return launch_after(ffn_finish_kernel, dim3((unsigned)(ceil_div(P.cols, 32) * P.p), (unsigned)ceil_div(P.n, 32)), 256, 0, st, F);
+    }
     if (back) {
         P.slices = q.parts * d->num_slices;   // of the sums
         if (gated) return promo ? launch<kDzGated, true>(P, d->act, st) : launch<kDzGated, false>(P, d->act, st);
@@ -1237,14 +1640,55 @@ bool wide_access(const void* p, int64_t ld, int elem, int groups, int width) {
     const int unit = elem == 2 ? 16 : 8;
     return (uintptr_t)p % unit == 0 && ld * elem % unit == 0 && (groups == 1 || width * elem % unit == 0);
 }
-
 // Where a product's result goes: bf16 by tensor copies, where they can reach it.
-slicegcn_status_t set_result(Params& P, void* out, int64_t ld, int elem, int groups, int width, int64_t rows) {
-    P.out = out, P.out_ld = (int)ld, P.out_bf16 = elem == 2, P.out_vec = wide_access(out, ld, elem, groups, width);
+slicegcn_status_t set_result(Params& P, FinishArgs& F, void* out, int64_t ld, int elem, int groups, int width, int64_t rows) {
+    P.out = F.out = out, P.out_ld = (int)ld, F.out_ld = ld, P.out_bf16 = F.out_bf16 = elem == 2, P.out_vec = wide_access(out, ld, elem, groups, width);
     if (elem != 2 || !P.out_vec) return SLICEGCN_OK;
     Operand o;
     o.base = out, o.rows = rows, o.ld = ld, o.group_stride = width, o.width = width, o.groups = groups;
     return make_map(&P.o, o, 32, true);
+}
+void set_input(Params& P, FinishArgs& F, const void* in, int64_t ld, int elem, int groups, int width) {
+    P.in = F.in = in, P.in_ld = (int)ld, F.in_ld = ld, F.in_bf16 = elem == 2, P.in_vec = in && wide_access(in, ld, elem, groups, width);
+}
+
+template <int R, bool GATED, bool BF16, bool VEC>
+slicegcn_status_t launch_rows(const RowsArgs& A, int parts, int slices, cudaStream_t st) {
+    const size_t smem = sizeof(float) * ((size_t)R * A.per + 8 * R * (1 + GATED) * kRowsCols);
+    SGCN_CUDA(cudaFuncSetAttribute(ffn_rows_kernel<R, GATED, BF16, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * (R * 16384 / 8 + 8 * R * (1 + GATED) * kRowsCols)));
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)parts, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(ceil_div(A.out_s, kRowsCols) * parts), (unsigned)slices);
+    cfg.blockDim = dim3(kRowsThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    SGCN_CUDA(cudaLaunchKernelEx(&cfg, ffn_rows_kernel<R, GATED, BF16, VEC>, A));
+    count_launch();
+    return SLICEGCN_OK;
+}
+template <int R, bool GATED, bool BF16>
+slicegcn_status_t launch_rows(const RowsArgs& A, bool vec, int parts, int slices, cudaStream_t st) {
+    return vec ? launch_rows<R, GATED, BF16, true>(A, parts, slices, st) : launch_rows<R, GATED, BF16, false>(A, parts, slices, st);
+}
+template <int R>
+slicegcn_status_t launch_rows(const RowsArgs& A, bool bf16, bool vec, int parts, int slices, cudaStream_t st) {
+    if (A.W2) return bf16 ? launch_rows<R, true, true>(A, vec, parts, slices, st) : launch_rows<R, true, false>(A, vec, parts, slices, st);
+    return bf16 ? launch_rows<R, false, true>(A, vec, parts, slices, st) : launch_rows<R, false, false>(A, vec, parts, slices, st);
+}
+slicegcn_status_t rows_forward(const slicegcn_ffn_desc* d, const void* x, const void* r, void* out, cudaStream_t st) {
+    RowsArgs A = {x, d->x_ld, d->W, d->W2, d->b, d->b2, r, d->r_ld, out, d->out_ld, (int)d->n, d->in_s, d->out_s, d->act, 0, (float)d->scale};
+    const int parts = rows_parts(d, &A.per);
+    const bool bf16 = d->dtype == SLICEGCN_BF16;
+    const bool vec = d->out_s % 4 == 0 && (uintptr_t)d->W % (bf16 ? 8 : 16) == 0 && (uintptr_t)d->W2 % (bf16 ? 8 : 16) == 0;
+    if (d->n == 1) return launch_rows<1>(A, bf16, vec, parts, d->num_slices, st);
+    if (d->n <= 4) return launch_rows<4>(A, bf16, vec, parts, d->num_slices, st);
+    return launch_rows<8>(A, bf16, vec, parts, d->num_slices, st);
 }
 
 }  // namespace
@@ -1281,13 +1725,18 @@ slicegcn_status_t slicegcn_ffn_forward(const slicegcn_ffn_desc* d, const void* x
     SGCN_TRY(check_workspace(workspace, workspace_bytes, q.bytes, status));
     if (!some) return SLICEGCN_OK;
     cudaStream_t st = (cudaStream_t)stream;
-    Operand ox, ow, ow2;
-    SGCN_TRY(operands(d, q, x, static_cast<char*>(workspace), ox, ow, ow2, st));
+    if (q.rows) return rows_forward(d, x, r, out, st);
+    char* ws = static_cast<char*>(workspace);
+    Operand ox, ow[2];
+    PackArgs packs = {};
+    operands(d, q, x, ws, ox, ow, packs);
+    SGCN_TRY(run_packs(packs, st));
     Params P = {};
+    FinishArgs F = {};
     P.status = status;
-    P.in = r, P.in_ld = (int)d->r_ld, P.in_vec = r && wide_access(r, d->r_ld, e, p, d->out_s);
-    SGCN_TRY(set_result(P, out, d->out_ld, e, p, d->out_s, d->n));
-    return forward_product(P, d, q, ox, ow, ow2, false, st);
+    set_input(P, F, r, d->r_ld, e, p, d->out_s);
+    SGCN_TRY(set_result(P, F, out, d->out_ld, e, p, d->out_s, d->n));
+    return forward_product(P, F, d, q, ox, ow, ws, false, st);
 }
 
 slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* x, const void* dout, void* dx, void* dW, void* dW2, float* db,
@@ -1314,76 +1763,90 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         return SLICEGCN_OK;
     }
     char* ws = static_cast<char*>(workspace);
-    Operand ox, ow, ow2, oz;
-    SGCN_TRY(operands(d, q, x, ws, ox, ow, ow2, st));
+    Operand ox, ow[2], oz;
+    PackArgs packs = {};
+    operands(d, q, x, ws, ox, ow, packs);
+    if (q.pack_g)
+        add_pack(packs, dout, d->dout_ld, n, p, d->out_s, ge == 2, ws + q.z_at, oz);
+    else if (!q.dz)
+        oz.base = dout, oz.rows = n, oz.ld = d->dout_ld, oz.group_stride = d->out_s, oz.width = d->out_s, oz.groups = p;
+    SGCN_TRY(run_packs(packs, st));
     const bool sums = db || db2;
     const float scale = q.dz ? 1.f : (float)d->scale;   // what the products still have to be multiplied by
     if (q.dz) {
         Params P = {};
+        FinishArgs F = {};
         P.status = status;
-        P.in = dout, P.in_ld = (int)d->dout_ld, P.in_vec = wide_access(dout, d->dout_ld, ge, p, d->out_s);
-        P.sums = sums ? reinterpret_cast<float*>(ws + q.sums_at) : nullptr;
+        set_input(P, F, dout, d->dout_ld, ge, p, d->out_s);
+        P.sums = F.sums = sums ? reinterpret_cast<float*>(ws + q.sums_at) : nullptr;
         oz.base = ws + q.z_at, oz.rows = n, oz.ld = (int64_t)q.parts * p * q.out_pad, oz.group_stride = q.out_pad, oz.plane_stride = n * oz.ld;
         oz.width = d->out_s, oz.groups = q.parts * p, oz.planes = q.z_planes;
+        F.dz = reinterpret_cast<__nv_bfloat16*>(ws + q.z_at);
+        F.dz_plane = oz.plane_stride, F.dz_row = (int)oz.ld, F.dz_pad = q.out_pad, F.dz_planes = q.z_planes;
         SGCN_TRY(make_map(&P.o, oz, q.z_planes == 1 ? 32 : 16, true));
-        SGCN_TRY(forward_product(P, d, q, ox, ow, ow2, true, st));
-    } else if (q.pack_g) {
-        SGCN_TRY(pack(dout, d->dout_ld, n, p, d->out_s, ge == 2, ws + q.z_at, oz, st));
-    } else {
-        oz.base = dout, oz.rows = n, oz.ld = d->dout_ld, oz.group_stride = d->out_s, oz.width = d->out_s, oz.groups = p;
+        SGCN_TRY(forward_product(P, F, d, q, ox, ow, ws, true, st));
     }
     if (dx) {
         Params P = {};
+        FinishArgs F = {};
         P.status = status;
-        set_tiles(P, n, p, d->in_s, false);
-        SGCN_TRY(item_count(P));
+        P.n = (int)n, P.p = P.slices = p, P.cols = d->in_s;
+        SGCN_TRY(set_cut(P, q.dx, false));
         SGCN_TRY(make_map(&P.a, oz, 128));
-        SGCN_TRY(make_map(&P.b0, ow, P.nt));
-        SGCN_TRY(make_map(&P.b1, q.parts == 2 ? ow2 : ow, P.nt));
-        P.kb_part = ceil_div(d->out_s, 64), P.kb_total = P.kb_part * q.parts, P.k_part = d->out_s;
+        SGCN_TRY(make_map(&P.b0, ow[0], P.nt));
+        SGCN_TRY(make_map(&P.b1, ow[1], P.nt));
+        P.kb_part = (int)ceil_div(d->out_s, 64), P.k_part = d->out_s;
         set_pairs(P, q.z_planes, q.w_planes);
-        const bool promo = P.pairs > 1;
-        P.chunk = promo ? kChunkF32 : P.kb_total;
         P.scale = scale;
-        SGCN_TRY(set_result(P, dx, d->dx_ld, ge, p, d->in_s, n));
-        SGCN_TRY((promo ? launch_as<kDx, true, SLICEGCN_ACT_NONE>(P, st) : launch_as<kDx, false, SLICEGCN_ACT_NONE>(P, st)));
+        SGCN_TRY(set_result(P, F, dx, d->dx_ld, ge, p, d->in_s, n));
+        const bool split = P.splits > 1;
+        if (split) P.partial = reinterpret_cast<float*>(ws + q.partial_at);
+        SGCN_TRY((P.pairs > 1 || split ? launch_as<kDx, true, SLICEGCN_ACT_NONE>(P, st) : launch_as<kDx, false, SLICEGCN_ACT_NONE>(P, st)));
+        if (split) {
+            F.partial = P.partial, F.splits = P.splits, F.n = P.n, F.p = p, F.cols = P.cols, F.act = SLICEGCN_ACT_NONE, F.scale = scale;
+            SGCN_TRY(launch_after(ffn_finish_kernel, dim3((unsigned)(ceil_div(P.cols, 32) * p), (unsigned)ceil_div(n, 32)), 256, 0, st, F));
+        }
     }
+    JoinArgs J = {};
     if (dW || dW2) {
         Params P = {};
         P.status = status;
-        P.n = d->out_s, P.p = p, P.slices = q.parts * p, P.cols = d->out_s, P.k_part = d->in_s;
-        P.nt = q.dw_nt, P.tiles_m = ceil_div(d->out_s, 256), P.tiles_n = ceil_div(d->in_s, 2 * P.nt), P.group = 1;
-        P.kb_total = P.kb_part = ceil_div(ceil_div(n, 64), q.splits);
-        P.splits = q.splits, P.splits_rows = 1;
-        SGCN_TRY(item_count(P));
-        SGCN_TRY(make_map(&P.a, oz, 64));
-        SGCN_TRY(make_map(&P.b0, ox, 64));
+        P.swapped = q.dw.swapped, P.pair = q.dw.pair, P.matrices = q.parts * p;
+        P.n = P.swapped ? d->in_s : d->out_s, P.p = p, P.slices = P.pair ? p : q.parts * p, P.cols = d->out_s, P.k_part = d->in_s;
+        SGCN_TRY(set_cut(P, q.dw, true));
+        P.kb_part = P.kb_total;
+        SGCN_TRY(make_map(&P.a, P.swapped ? ox : oz, 64));
+        SGCN_TRY(make_map(&P.b0, P.swapped ? oz : ox, 64));
         P.b1 = P.b0;
-        set_pairs(P, q.z_planes, q.x_planes);
-        P.chunk = P.pairs > 1 ? kChunkF32 : kChunkLong;
+        set_pairs(P, P.swapped ? q.x_planes : q.z_planes, P.swapped ? q.z_planes : q.x_planes);
         P.scale = scale, P.out_bf16 = ge == 2;
         P.partial = reinterpret_cast<float*>(ws + q.partial_at);
         P.dw = dW, P.dw2 = dW2;
         SGCN_TRY((launch_as<kDw, true, SLICEGCN_ACT_NONE>(P, st)));
-        if (q.splits > 1) {
-            JoinArgs J = {P.partial, q.splits, ge == 2, (int64_t)q.parts * d->in_s * outs, d->in_s * outs, scale, {dW, dW2}};
-            SGCN_TRY(launch_after(ffn_join_kernel, dim3((unsigned)std::min<int64_t>((J.total + 255) / 256, 148 * 8)), 256, 0, st, J));
+        if (P.splits > 1) {
+            const int64_t total = (int64_t)q.parts * d->in_s * outs;
+            J.job[0] = {P.partial, P.splits, ge == 2, total, d->in_s * outs, scale, {dW, dW2}, (int)std::min<int64_t>(ceil_div(total, 256), 148 * 8)};
         }
     }
     if (sums) {
         SumArgs A;
         A.src = q.dz ? (const void*)(ws + q.sums_at) : dout;
-        A.rows = q.dz ? (n + 31) / 32 : n;
+        A.rows = q.dz ? ceil_div(n, 32) : n;
         A.cols = (int)(q.parts * outs);
         A.ld = q.dz ? A.cols : d->dout_ld;
         A.bf16 = !q.dz && ge == 2;
-        const int chunks = (int)std::min<int64_t>(kSumChunks, std::max<int64_t>(1, A.rows / 32));
-        A.per = (A.rows + chunks - 1) / chunks;
+        const int width = A.bf16 ? 8 : 4;
+        A.vec = (uintptr_t)A.src % 16 == 0 && A.ld % width == 0 && A.cols % width == 0;
+        A.per = ceil_div(A.rows, q.sum_chunks);
         A.partial = reinterpret_cast<float*>(ws + q.chunks_at);
-        SGCN_TRY(launch_after(ffn_colsum_kernel, dim3(ceil_div(A.cols, 32), chunks), 256, 0, st, A));
-        JoinArgs J = {A.partial, chunks, 0, A.cols, outs, scale, {db, db2}};
-        SGCN_TRY(launch_after(ffn_join_kernel, dim3(ceil_div(J.total, 256)), 256, 0, st, J));
+        const dim3 grid((unsigned)ceil_div(A.cols, 32 * (A.vec ? width : 1)), (unsigned)q.sum_chunks);
+        if (A.bf16)
+            SGCN_TRY((A.vec ? launch_after(ffn_colsum_kernel<true, true>, grid, 256, 0, st, A) : launch_after(ffn_colsum_kernel<true, false>, grid, 256, 0, st, A)));
+        else
+            SGCN_TRY((A.vec ? launch_after(ffn_colsum_kernel<false, true>, grid, 256, 0, st, A) : launch_after(ffn_colsum_kernel<false, false>, grid, 256, 0, st, A)));
+        J.job[1] = {A.partial, q.sum_chunks, 0, A.cols, outs, scale, {db, db2}, (int)ceil_div(A.cols, 256)};
     }
+    if (J.job[0].ctas + J.job[1].ctas > 0) SGCN_TRY(launch_after(ffn_join_kernel, dim3(J.job[0].ctas + J.job[1].ctas), 256, 0, st, J));
     return SLICEGCN_OK;
 }
 

@@ -197,3 +197,26 @@ def test_many_tiles_per_pair_of_sms(shape, types):
         q.check_backward(q.backward())
         q = Problem(*shape, gated, "none", dtype, grad)
         q.check_backward(q.backward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [1, 2, 4, 5, 8, 9])
+def test_a_few_rows(n, dtype):
+    """Serving: up to eight rows go another way than more do."""
+    for p, ins, outs, pad in ((1, 256, 1024, 0), (1, 4096, 260, 3), (4, 33, 129, 1), (1, 1433, 6, 0), (2, 3, 1, 5), (8, 700, 128, 8), (1, 16384, 40, 0), (1, 20000, 12, 0)):
+        for gated, act, residual in ((False, "gelu", True), (True, "silu", False), (False, "none", False)):
+            q = Problem(n, p, ins, outs, gated, act, dtype, pad=pad, residual=residual, bias=act != "none", seed=n)
+            q.check_forward(q.forward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("types", ["bf16", "fp32", "bf16/fp32"])
+@pytest.mark.parametrize("shape", [(100, 1, 4096, 64), (2708, 1, 1433, 16), (16, 1, 64, 2500), (700, 1, 2000, 130), (40, 2, 900, 300), (5, 1, 513, 2100), (5000, 1, 800, 72)], ids=str)
+def test_products_in_pieces(shape, types):
+    """Few tiles with a long sum: pieces of it are added up by a second kernel."""
+    dtype, grad = types.split("/") if "/" in types else (types, "same")
+    for gated, act, pad, residual in ((False, "silu", 1, True), (True, "gelu", 0, True), (False, "none", 0, False)):
+        q = Problem(*shape, gated, act, dtype, grad, pad=pad, residual=residual)
+        q.check_forward(q.forward())
+        q.check_backward(q.backward())
