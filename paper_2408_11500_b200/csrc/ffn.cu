@@ -20,6 +20,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "common.cuh"
@@ -1376,11 +1377,11 @@ struct Cut {
     double cost = 1e300;
 };
 // SM cycles of `items` tiles: a 64-wide step takes its MMAs' time, or with half-width tiles rather what its copies take; a tile's start
-// and end about 4,500.  Splitting k adds 12,000 (a launch, a kernel that keeps the sums in registers) and each piece's way to memory and back (3,400 bytes a cycle over all SMs).
+// and end about 4,500.  Splitting k adds 16,000 (a launch, a kernel that keeps the sums in registers) and each piece's way to memory and back (3,400 bytes a cycle over all SMs).
 double cost_of(int64_t tiles, int splits, int64_t kb, int pairs, int nt, double piece_bytes) {
     const double step = nt == 128 ? 512 : 430;
     return (double)ceil_div(tiles * splits, kPairs) * ((double)kb * pairs * step + 4500.0) +
-           (splits > 1 ? 12000.0 + 2.0 * splits * piece_bytes / 3400.0 : 0.0);
+           (splits > 1 ? 16000.0 + 2.0 * splits * piece_bytes / 3400.0 : 0.0);
 }
 int pairs_of(int pa, int pb) {
     int n = 0;
@@ -1556,9 +1557,24 @@ void set_pairs(Params& P, int pa, int pb) {
             if (order - i < pb) P.ia[P.pairs] = (int8_t)i, P.ib[P.pairs] = (int8_t)(order - i), ++P.pairs;
 }
 
+// A kernel's limit of dynamic shared memory, a constant of the kernel, set at its first launch on each device (a call costs a
+// microsecond).  Threads that come at the same time all set it.
+struct SmemLimit {
+    std::atomic<uint64_t> devices{0};
+    slicegcn_status_t set(const void* kernel, int bytes) {
+        int dev = 0;
+        SGCN_CUDA(cudaGetDevice(&dev));
+        const uint64_t bit = 1ull << (dev & 63);
+        if (dev < 64 && (devices.load(std::memory_order_relaxed) & bit)) return SLICEGCN_OK;
+        SGCN_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        devices.fetch_or(bit, std::memory_order_relaxed);
+        return SLICEGCN_OK;
+    }
+};
 template <int MODE, bool PROMO, int ACT>
 slicegcn_status_t launch_as(const Params& P, cudaStream_t st) {
-    SGCN_CUDA(cudaFuncSetAttribute(ffn_kernel<MODE, PROMO, ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    static SmemLimit limit;
+    SGCN_TRY(limit.set((const void*)ffn_kernel<MODE, PROMO, ACT>, kSmem));
     return launch_after(ffn_kernel<MODE, PROMO, ACT>, dim3(2 * std::min(P.items, kPairs)), kThreads, kSmem, st, P);
 }
 template <int MODE, bool PROMO>
@@ -1655,7 +1671,8 @@ void set_input(Params& P, FinishArgs& F, const void* in, int64_t ld, int elem, i
 template <int R, bool GATED, bool BF16, bool VEC>
 slicegcn_status_t launch_rows(const RowsArgs& A, int parts, int slices, cudaStream_t st) {
     const size_t smem = sizeof(float) * ((size_t)R * A.per + 8 * R * (1 + GATED) * kRowsCols);
-    SGCN_CUDA(cudaFuncSetAttribute(ffn_rows_kernel<R, GATED, BF16, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * (R * 16384 / 8 + 8 * R * (1 + GATED) * kRowsCols)));
+    static SmemLimit limit;
+    SGCN_TRY(limit.set((const void*)ffn_rows_kernel<R, GATED, BF16, VEC>, 4 * (R * 16384 / 8 + 8 * R * (1 + GATED) * kRowsCols)));
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
