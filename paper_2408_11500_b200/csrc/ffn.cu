@@ -78,7 +78,7 @@ struct Params {
     int out_bf16, out_vec;
     // kDz: sums over 32 rows each
     float* sums;                   // [ceil(n/32)][parts * p][cols], or NULL
-    float* partial;                // splits > 1: the pieces' products; kDw: [splits][slices][in_s][out_s], else [splits][slices][n][cols]
+    float* partial;                // pieces' products, where they are joined by another kernel; kDw: [splits][slices][in_s][out_s], else [splits][slices][n][cols]
     int matrices;                  // kDw: slices times parts
     void *dw, *dw2;                // kDw, splits == 1
     int32_t* status;
@@ -702,7 +702,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                 const int slice = P.pair || !upper ? t.slice : t.slice - P.p, n0 = P.pair && upper ? col0 - P.nt : col0;
                 if (m < m_end) {
                     const int64_t from = m * m_step + n0 * n_step;
-                    if (P.splits > 1) {
+                    if (P.partial) {
                         float* to = P.partial + ((int64_t)t.split * P.matrices + (upper ? P.p : 0) + slice) * matrix + from;
 #pragma unroll
                         for (int j = 0; j < 64; ++j)
@@ -902,6 +902,7 @@ struct PackJob {
     const void* src;
     int64_t ld, rows, plane;
     int groups, width, pad, bf16, vec;
+    int merge, block_rows, block_cols;   // weights of `merge` slices as one block-diagonal matrix: a slice's block, else merge = 1
     int ctas;
     __nv_bfloat16* dst;
 };
@@ -920,25 +921,28 @@ __global__ void __launch_bounds__(256) ffn_pack_kernel(const __grid_constant__ P
     for (int64_t i = (int64_t)cta * 256 + threadIdx.x; i < total; i += (int64_t)A.ctas * 256) {
         const int64_t row = total < (1ll << 32) ? (int64_t)((uint32_t)i / (uint32_t)per_row) : i / per_row;
         const int in_row = (int)(i - row * per_row), g = in_row / per_group, c = (in_row - g * per_group) * 8;
-        const int64_t at = row * A.ld + (int64_t)g * A.width + c;
-        const int left = A.width - c;
+        // columns [first, left) of the eight have a source
+        const int shift = A.merge > 1 ? (int)(row / A.block_rows % A.merge) * A.block_cols : 0;
+        const int64_t at = row * A.ld + (int64_t)g * A.width + c - shift;
+        const int first = shift - c, left = A.merge > 1 ? first + A.block_cols : A.width - c;
         uint4 out[3];
         if (A.bf16) {
             const uint16_t* s = static_cast<const uint16_t*>(A.src) + at;
             uint32_t w[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                w[q] = (2 * q < left ? (uint32_t)s[2 * q] : 0u) | (2 * q + 1 < left ? (uint32_t)s[2 * q + 1] << 16 : 0u);
+                w[q] = (2 * q >= first && 2 * q < left ? (uint32_t)s[2 * q] : 0u) |
+                       (2 * q + 1 >= first && 2 * q + 1 < left ? (uint32_t)s[2 * q + 1] << 16 : 0u);
             out[0] = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
             const float* s = static_cast<const float*>(A.src) + at;
             float v[8];
-            if (A.vec && left >= 8) {
+            if (A.vec && first <= 0 && left >= 8) {
                 const float4 a = *reinterpret_cast<const float4*>(s), b = *reinterpret_cast<const float4*>(s + 4);
                 v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
             } else {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] = q < left ? s[q] : 0.f;
+                for (int q = 0; q < 8; ++q) v[q] = q >= first && q < left ? s[q] : 0.f;
             }
             uint32_t w[3][4];
 #pragma unroll
@@ -1033,9 +1037,10 @@ __global__ void __launch_bounds__(256) ffn_colsum_kernel(const __grid_constant__
 struct JoinJob {
     const float* partial;
     int count, bf16;
-    int64_t total, each;
+    int64_t total, each, piece;   // piece: numbers of a piece, more than `total` where slices were merged
     float scale;
     void* out[2];
+    int merge, rows, cols;        // merge > 1: of a slice's block, which lies on the diagonal of a piece's matrix of `merge` slices
     int ctas;
 };
 struct JoinArgs {
@@ -1049,16 +1054,22 @@ __global__ void __launch_bounds__(256) ffn_join_kernel(const __grid_constant__ J
     for (int64_t i = (int64_t)cta * 256 + threadIdx.x; i < A.total; i += (int64_t)A.ctas * 256) {
         const int second = i >= A.each;
         if (!A.out[second]) continue;
+        const float* from = A.partial + i;
+        if (A.merge > 1) {
+            const int64_t row = i / A.cols, slice = row / A.rows;
+            const int b = (int)(slice % A.merge);
+            from = A.partial + row * A.cols * A.merge + b * A.cols + (i - row * A.cols);
+        }
         float s[4] = {0.f, 0.f, 0.f, 0.f};
         int k = 0;
         for (; k + 8 <= A.count; k += 8) {
             float t[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) t[q] = A.partial[(k + q) * A.total + i];
+            for (int q = 0; q < 8; ++q) t[q] = from[(k + q) * A.piece];
 #pragma unroll
             for (int q = 0; q < 8; ++q) s[q & 3] += t[q];
         }
-        for (; k < A.count; ++k) s[0] += A.partial[k * A.total + i];
+        for (; k < A.count; ++k) s[0] += from[k * A.piece];
         const float v = ((s[0] + s[1]) + (s[2] + s[3])) * A.scale;
         const int64_t at = second ? i - A.each : i;
         if (A.bf16)
@@ -1433,7 +1444,11 @@ Cut cut_dw(int64_t n, int p, int parts, int in_s, int out_s, int pairs) {
 }
 
 // What a call needs in the workspace, and where.
+//
+// Slices of few columns are taken together, as long as their columns of x stay within one 64-wide step of k: their weights as one
+// block-diagonal matrix cost no MMA more, and there are fewer and wider tiles (8 slices of 14 -> 23 columns: half the time).
 struct Plan {
+    int p = 1, in_s = 1, out_s = 1, merge = 1;   // slices and their columns as the products see them
     bool rows = false, pack_x = false, pack_w = false, pack_g = false, dz = false;
     int x_planes = 1, w_planes = 1, z_planes = 1;
     int in_pad = 0, out_pad = 0, parts = 1, sum_chunks = 1;
@@ -1456,21 +1471,27 @@ int rows_parts(const slicegcn_ffn_desc* d, int* per) {
 
 void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) {
     const int64_t n = d->n;
-    const int p = d->num_slices;
     const bool f32 = d->dtype == SLICEGCN_F32, back = dout != nullptr;
     q.parts = d->W2 ? 2 : 1;
-    q.in_pad = (int)up(d->in_s, 8);
-    q.out_pad = (int)up(d->out_s, 8);
     q.x_planes = q.w_planes = f32 ? 3 : 1;
     q.z_planes = d->grad_dtype == SLICEGCN_F32 ? 3 : 1;
     if (!back && n <= 8 && d->in_s <= 16384) {
         q.rows = true;
         return;
     }
-    q.pack_x = f32 || unaligned(x, d->x_ld, p, d->in_s);
-    q.pack_w = f32 || unaligned(d->W, d->out_s, 1, 8) || unaligned(d->W2, d->out_s, 1, 8);
+    for (int m = d->num_slices; m > 1; --m)
+        if (d->num_slices % m == 0 && m * d->in_s <= 64 && (int64_t)m * d->out_s <= SLICEGCN_MAX_FFN_WIDTH) {
+            q.merge = m;
+            break;
+        }
+    q.p = d->num_slices / q.merge, q.in_s = d->in_s * q.merge, q.out_s = d->out_s * q.merge;
+    q.in_pad = (int)up(q.in_s, 8);
+    q.out_pad = (int)up(q.out_s, 8);
+    const int p = q.p;
+    q.pack_x = f32 || unaligned(x, d->x_ld, p, q.in_s);
+    q.pack_w = f32 || q.merge > 1 || unaligned(d->W, d->out_s, 1, 8) || unaligned(d->W2, d->out_s, 1, 8);
     q.dz = back && (d->act != SLICEGCN_ACT_NONE || d->W2);
-    q.pack_g = back && !q.dz && (q.z_planes == 3 || unaligned(dout, d->dout_ld, p, d->out_s));
+    q.pack_g = back && !q.dz && (q.z_planes == 3 || unaligned(dout, d->dout_ld, p, q.out_s));
     int64_t at = 0, partial = 0;
     auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -1479,12 +1500,12 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
     };
     if (q.pack_x) q.x_at = take(2 * q.x_planes * n * p * q.in_pad);
     if (q.pack_w) {
-        q.w_at = take(2LL * q.w_planes * p * d->in_s * q.out_pad);
-        if (d->W2) q.w2_at = take(2LL * q.w_planes * p * d->in_s * q.out_pad);
+        q.w_at = take(2LL * q.w_planes * p * q.in_s * q.out_pad);
+        if (d->W2) q.w2_at = take(2LL * q.w_planes * p * q.in_s * q.out_pad);
     }
-    const int64_t cols = (int64_t)q.parts * p * d->out_s;
+    const int64_t cols = (int64_t)q.parts * p * q.out_s;
     if (!back || q.dz) {
-        q.product = cut_rows(n, p, d->out_s, d->W2 != nullptr, ceil_div(d->in_s, 64), pairs_of(q.x_planes, q.w_planes));
+        q.product = cut_rows(n, p, q.out_s, d->W2 != nullptr, ceil_div(q.in_s, 64), pairs_of(q.x_planes, q.w_planes));
         if (q.product.splits > 1) partial = 4LL * q.product.splits * n * cols;
     }
     if (back) {
@@ -1493,10 +1514,10 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
         const int64_t rows = q.dz ? ceil_div(n, 32) : n;
         q.sum_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({kSumChunks, ceil_div(148 * 6, ceil_div(cols, 128)), rows / 64}));
         q.chunks_at = take(4 * q.sum_chunks * cols);
-        q.dx = cut_rows(n, p, d->in_s, false, q.parts * ceil_div(d->out_s, 64), pairs_of(q.z_planes, q.w_planes));
-        if (q.dx.splits > 1) partial = std::max<int64_t>(partial, 4LL * q.dx.splits * n * p * d->in_s);
-        q.dw = cut_dw(n, p, q.parts, d->in_s, d->out_s, pairs_of(q.z_planes, q.x_planes));
-        if (q.dw.splits > 1) partial = std::max<int64_t>(partial, 4LL * q.dw.splits * d->in_s * cols);
+        q.dx = cut_rows(n, p, q.in_s, false, q.parts * ceil_div(q.out_s, 64), pairs_of(q.z_planes, q.w_planes));
+        if (q.dx.splits > 1) partial = std::max<int64_t>(partial, 4LL * q.dx.splits * n * p * q.in_s);
+        q.dw = cut_dw(n, p, q.parts, q.in_s, q.out_s, pairs_of(q.z_planes, q.x_planes));
+        if (q.dw.splits > 1 || q.merge > 1) partial = std::max<int64_t>(partial, 4LL * q.dw.splits * q.in_s * cols);
     }
     if (partial) q.partial_at = take(partial);
     q.bytes = at;
@@ -1537,6 +1558,7 @@ void add_pack(PackArgs& args, const void* src, int64_t ld, int64_t rows, int gro
     PackJob& A = args.job[args.count++];
     A.src = src, A.ld = ld, A.rows = rows, A.groups = groups, A.width = width, A.pad = (int)up(width, 8), A.bf16 = bf16;
     A.vec = !bf16 && (uintptr_t)src % 16 == 0 && ld % 4 == 0 && (groups == 1 || width % 4 == 0);
+    A.merge = 1, A.block_rows = 1, A.block_cols = width;
     A.plane = rows * groups * A.pad;
     A.dst = static_cast<__nv_bfloat16*>(dst);
     A.ctas = (int)std::min<int64_t>(ceil_div(A.plane / 8, 256), 148 * 16);
@@ -1604,18 +1626,21 @@ slicegcn_status_t set_cut(Params& P, const Cut& c, bool dw) {
 // x, W and W2 as operands; what has to be laid out anew is added to the packs.
 void operands(const slicegcn_ffn_desc* d, const Plan& q, const void* x, char* ws, Operand& ox, Operand (&ow)[2], PackArgs& packs) {
     const bool bf16 = d->dtype == SLICEGCN_BF16;
-    const int p = d->num_slices;
+    const int p = q.p;
     if (q.pack_x)
-        add_pack(packs, x, d->x_ld, d->n, p, d->in_s, bf16, ws + q.x_at, ox);
+        add_pack(packs, x, d->x_ld, d->n, p, q.in_s, bf16, ws + q.x_at, ox);
     else
-        ox.base = x, ox.rows = d->n, ox.ld = d->x_ld, ox.group_stride = d->in_s, ox.width = d->in_s, ox.groups = p;
+        ox.base = x, ox.rows = d->n, ox.ld = d->x_ld, ox.group_stride = q.in_s, ox.width = q.in_s, ox.groups = p;
     for (int k = 0; k < q.parts; ++k) {
         const void* w = k ? d->W2 : d->W;
         if (q.pack_w) {
-            add_pack(packs, w, d->out_s, (int64_t)p * d->in_s, 1, d->out_s, bf16, ws + (k ? q.w2_at : q.w_at), ow[k]);
-            ow[k].groups = p, ow[k].rows = d->in_s, ow[k].group_stride = (int64_t)d->in_s * q.out_pad;
+            add_pack(packs, w, d->out_s, (int64_t)p * q.in_s, 1, q.out_s, bf16, ws + (k ? q.w2_at : q.w_at), ow[k]);
+            PackJob& job = packs.job[packs.count - 1];
+            job.merge = q.merge, job.block_rows = d->in_s, job.block_cols = d->out_s;
+            job.vec = job.vec && q.merge == 1;
+            ow[k].groups = p, ow[k].rows = q.in_s, ow[k].group_stride = (int64_t)q.in_s * q.out_pad;
         } else {
-            ow[k].base = w, ow[k].rows = d->in_s, ow[k].ld = d->out_s, ow[k].group_stride = (int64_t)d->in_s * d->out_s, ow[k].width = d->out_s, ow[k].groups = p;
+            ow[k].base = w, ow[k].rows = q.in_s, ow[k].ld = q.out_s, ow[k].group_stride = (int64_t)q.in_s * q.out_s, ow[k].width = q.out_s, ow[k].groups = p;
         }
     }
     if (q.parts == 1) ow[1] = ow[0];
@@ -1626,15 +1651,15 @@ slicegcn_status_t forward_product(Params& P, FinishArgs& F, const slicegcn_ffn_d
                                   cudaStream_t st) {
     const bool gated = d->W2 != nullptr, split = q.product.splits > 1;
     const bool promo = d->dtype == SLICEGCN_F32 || (back && d->grad_dtype == SLICEGCN_F32) || split;
-    P.n = (int)d->n, P.p = d->num_slices, P.slices = split ? q.parts * d->num_slices : d->num_slices, P.cols = d->out_s;
+    P.n = (int)d->n, P.p = q.p, P.slices = split ? q.parts * q.p : q.p, P.cols = q.out_s;
     SGCN_TRY(set_cut(P, q.product, false));
     SGCN_TRY(make_map(&P.a, ox, 128));
     SGCN_TRY(make_map(&P.b0, ow[0], 64));
     SGCN_TRY(make_map(&P.b1, ow[1], 64));
-    P.kb_part = (int)ceil_div(d->in_s, 64), P.k_part = d->in_s;
+    P.kb_part = (int)ceil_div(q.in_s, 64), P.k_part = q.in_s;
     set_pairs(P, q.x_planes, q.w_planes);
     P.scale = (float)d->scale, P.b = d->b, P.b2 = d->b2;
-    P.bias_vec = d->out_s % 2 == 0 && (uintptr_t)d->b % 8 == 0 && (uintptr_t)d->b2 % 8 == 0;
+    P.bias_vec = q.out_s % 2 == 0 && (uintptr_t)d->b % 8 == 0 && (uintptr_t)d->b2 % 8 == 0;
     if (split) {
         P.partial = reinterpret_cast<float*>(ws + q.partial_at);
         SGCN_TRY((launch_as<kFwd, true, SLICEGCN_ACT_NONE>(P, st)));
@@ -1643,7 +1668,7 @@ slicegcn_status_t forward_product(Params& P, FinishArgs& F, const slicegcn_ffn_d
         return launch_after(ffn_finish_kernel, dim3((unsigned)(ceil_div(P.cols, 32) * P.p), (unsigned)ceil_div(P.n, 32)), 256, 0, st, F);
     }
     if (back) {
-        P.slices = q.parts * d->num_slices;   // of the sums
+        P.slices = q.parts * q.p;   // of the sums
         if (gated) return promo ? launch<kDzGated, true>(P, d->act, st) : launch<kDzGated, false>(P, d->act, st);
         return promo ? launch<kDz, true>(P, d->act, st) : launch<kDz, false>(P, d->act, st);
     }
@@ -1751,16 +1776,16 @@ slicegcn_status_t slicegcn_ffn_forward(const slicegcn_ffn_desc* d, const void* x
     Params P = {};
     FinishArgs F = {};
     P.status = status;
-    set_input(P, F, r, d->r_ld, e, p, d->out_s);
-    SGCN_TRY(set_result(P, F, out, d->out_ld, e, p, d->out_s, d->n));
+    set_input(P, F, r, d->r_ld, e, q.p, q.out_s);
+    SGCN_TRY(set_result(P, F, out, d->out_ld, e, q.p, q.out_s, d->n));
     return forward_product(P, F, d, q, ox, ow, ws, false, st);
 }
 
 slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* x, const void* dout, void* dx, void* dW, void* dW2, float* db,
                                         float* db2, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream) {
     SGCN_TRY(check(d));
-    const int p = d->num_slices, ge = d->grad_dtype == SLICEGCN_F32 ? 4 : 2;
-    const int64_t n = d->n, ins = (int64_t)p * d->in_s, outs = (int64_t)p * d->out_s;
+    const int ge = d->grad_dtype == SLICEGCN_F32 ? 4 : 2;
+    const int64_t n = d->n, ins = (int64_t)d->num_slices * d->in_s, outs = (int64_t)d->num_slices * d->out_s;
     const bool some = n > 0;
     SGCN_TRY(check_matrix("x", x, d->x_ld, ins, d->dtype, some));
     SGCN_TRY(check_matrix("dout", dout, d->dout_ld, outs, d->grad_dtype, some));
@@ -1779,14 +1804,15 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         if (db2) SGCN_CUDA(cudaMemsetAsync(db2, 0, (size_t)(outs * 4), st));
         return SLICEGCN_OK;
     }
+    const int p = q.p;
     char* ws = static_cast<char*>(workspace);
     Operand ox, ow[2], oz;
     PackArgs packs = {};
     operands(d, q, x, ws, ox, ow, packs);
     if (q.pack_g)
-        add_pack(packs, dout, d->dout_ld, n, p, d->out_s, ge == 2, ws + q.z_at, oz);
+        add_pack(packs, dout, d->dout_ld, n, p, q.out_s, ge == 2, ws + q.z_at, oz);
     else if (!q.dz)
-        oz.base = dout, oz.rows = n, oz.ld = d->dout_ld, oz.group_stride = d->out_s, oz.width = d->out_s, oz.groups = p;
+        oz.base = dout, oz.rows = n, oz.ld = d->dout_ld, oz.group_stride = q.out_s, oz.width = q.out_s, oz.groups = p;
     SGCN_TRY(run_packs(packs, st));
     const bool sums = db || db2;
     const float scale = q.dz ? 1.f : (float)d->scale;   // what the products still have to be multiplied by
@@ -1794,10 +1820,10 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         Params P = {};
         FinishArgs F = {};
         P.status = status;
-        set_input(P, F, dout, d->dout_ld, ge, p, d->out_s);
+        set_input(P, F, dout, d->dout_ld, ge, p, q.out_s);
         P.sums = F.sums = sums ? reinterpret_cast<float*>(ws + q.sums_at) : nullptr;
         oz.base = ws + q.z_at, oz.rows = n, oz.ld = (int64_t)q.parts * p * q.out_pad, oz.group_stride = q.out_pad, oz.plane_stride = n * oz.ld;
-        oz.width = d->out_s, oz.groups = q.parts * p, oz.planes = q.z_planes;
+        oz.width = q.out_s, oz.groups = q.parts * p, oz.planes = q.z_planes;
         F.dz = reinterpret_cast<__nv_bfloat16*>(ws + q.z_at);
         F.dz_plane = oz.plane_stride, F.dz_row = (int)oz.ld, F.dz_pad = q.out_pad, F.dz_planes = q.z_planes;
         SGCN_TRY(make_map(&P.o, oz, q.z_planes == 1 ? 32 : 16, true));
@@ -1807,15 +1833,15 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         Params P = {};
         FinishArgs F = {};
         P.status = status;
-        P.n = (int)n, P.p = P.slices = p, P.cols = d->in_s;
+        P.n = (int)n, P.p = P.slices = p, P.cols = q.in_s;
         SGCN_TRY(set_cut(P, q.dx, false));
         SGCN_TRY(make_map(&P.a, oz, 128));
         SGCN_TRY(make_map(&P.b0, ow[0], P.nt));
         SGCN_TRY(make_map(&P.b1, ow[1], P.nt));
-        P.kb_part = (int)ceil_div(d->out_s, 64), P.k_part = d->out_s;
+        P.kb_part = (int)ceil_div(q.out_s, 64), P.k_part = q.out_s;
         set_pairs(P, q.z_planes, q.w_planes);
         P.scale = scale;
-        SGCN_TRY(set_result(P, F, dx, d->dx_ld, ge, p, d->in_s, n));
+        SGCN_TRY(set_result(P, F, dx, d->dx_ld, ge, p, q.in_s, n));
         const bool split = P.splits > 1;
         if (split) P.partial = reinterpret_cast<float*>(ws + q.partial_at);
         SGCN_TRY((P.pairs > 1 || split ? launch_as<kDx, true, SLICEGCN_ACT_NONE>(P, st) : launch_as<kDx, false, SLICEGCN_ACT_NONE>(P, st)));
@@ -1829,7 +1855,7 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         Params P = {};
         P.status = status;
         P.swapped = q.dw.swapped, P.pair = q.dw.pair, P.matrices = q.parts * p;
-        P.n = P.swapped ? d->in_s : d->out_s, P.p = p, P.slices = P.pair ? p : q.parts * p, P.cols = d->out_s, P.k_part = d->in_s;
+        P.n = P.swapped ? q.in_s : q.out_s, P.p = p, P.slices = P.pair ? p : q.parts * p, P.cols = q.out_s, P.k_part = q.in_s;
         SGCN_TRY(set_cut(P, q.dw, true));
         P.kb_part = P.kb_total;
         SGCN_TRY(make_map(&P.a, P.swapped ? ox : oz, 64));
@@ -1837,12 +1863,14 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         P.b1 = P.b0;
         set_pairs(P, P.swapped ? q.x_planes : q.z_planes, P.swapped ? q.z_planes : q.x_planes);
         P.scale = scale, P.out_bf16 = ge == 2;
-        P.partial = reinterpret_cast<float*>(ws + q.partial_at);
+        const bool join = P.splits > 1 || q.merge > 1;
+        if (join) P.partial = reinterpret_cast<float*>(ws + q.partial_at);
         P.dw = dW, P.dw2 = dW2;
         SGCN_TRY((launch_as<kDw, true, SLICEGCN_ACT_NONE>(P, st)));
-        if (P.splits > 1) {
-            const int64_t total = (int64_t)q.parts * d->in_s * outs;
-            J.job[0] = {P.partial, P.splits, ge == 2, total, d->in_s * outs, scale, {dW, dW2}, (int)std::min<int64_t>(ceil_div(total, 256), 148 * 8)};
+        if (join) {
+            const int64_t each = d->in_s * outs, total = q.parts * each;
+            J.job[0] = {P.partial, P.splits, ge == 2, total, each, total * q.merge, scale, {dW, dW2}, q.merge, d->in_s, d->out_s,
+                        (int)std::min<int64_t>(ceil_div(total, 256), 148 * 8)};
         }
     }
     if (sums) {
@@ -1861,7 +1889,7 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
             SGCN_TRY((A.vec ? launch_after(ffn_colsum_kernel<true, true>, grid, 256, 0, st, A) : launch_after(ffn_colsum_kernel<true, false>, grid, 256, 0, st, A)));
         else
             SGCN_TRY((A.vec ? launch_after(ffn_colsum_kernel<false, true>, grid, 256, 0, st, A) : launch_after(ffn_colsum_kernel<false, false>, grid, 256, 0, st, A)));
-        J.job[1] = {A.partial, q.sum_chunks, 0, A.cols, outs, scale, {db, db2}, (int)ceil_div(A.cols, 256)};
+        J.job[1] = {A.partial, q.sum_chunks, 0, A.cols, outs, A.cols, scale, {db, db2}, 1, 1, 1, (int)ceil_div(A.cols, 256)};
     }
     if (J.job[0].ctas + J.job[1].ctas > 0) SGCN_TRY(launch_after(ffn_join_kernel, dim3(J.job[0].ctas + J.job[1].ctas), 256, 0, st, J));
     return SLICEGCN_OK;

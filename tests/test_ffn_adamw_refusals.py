@@ -18,7 +18,7 @@ AT = BUF.ctypes.data + (-BUF.ctypes.data) % 256       # an address on 256 bytes
 
 def _ffn(**kw):
     from paper_2408_11500_b200 import binding as B
-    args = dict(n=40, num_slices=2, in_s=8, out_s=16, W=AT, act=B.ACT_SILU, dtype=B.BF16)
+    args = dict(n=40, num_slices=2, in_s=40, out_s=16, W=AT, act=B.ACT_SILU, dtype=B.BF16)
     args.update(kw)
     return B.make_ffn_desc(**args)
 
@@ -30,7 +30,7 @@ def test_ffn_descriptions():
            (dict(act=4), B.ERR_INVALID_ARG), (dict(act=-1), B.ERR_INVALID_ARG), (dict(dtype=2), B.ERR_INVALID_ARG), (dict(grad_dtype=7), B.ERR_INVALID_ARG),
            (dict(dtype=B.F32, grad_dtype=B.BF16), B.ERR_UNSUPPORTED), (dict(scale=float("nan")), B.ERR_INVALID_ARG), (dict(scale=float("inf")), B.ERR_INVALID_ARG),
            (dict(W=None), B.ERR_INVALID_ARG), (dict(W=AT + 1), B.ERR_INVALID_ARG), (dict(W2=AT + 1), B.ERR_INVALID_ARG), (dict(b=AT + 2), B.ERR_INVALID_ARG),
-           (dict(b2=AT), B.ERR_INVALID_ARG), (dict(x_ld=15), B.ERR_INVALID_ARG), (dict(dtype=B.F32, W=AT + 2), B.ERR_INVALID_ARG)]
+           (dict(b2=AT), B.ERR_INVALID_ARG), (dict(x_ld=79), B.ERR_INVALID_ARG), (dict(dtype=B.F32, W=AT + 2), B.ERR_INVALID_ARG)]
     for kw, want in bad:
         d = _ffn(**kw)
         calls = [lambda: B.slicegcn_ffn_workspace_bytes(d, AT, AT), lambda: B.slicegcn_ffn_forward(d, AT, None, AT, None, AT, 1 << 20),
@@ -55,9 +55,9 @@ def test_ffn_matrices():
     assert _status(bwd) == B.ERR_INVALID_ARG
     d.dout_ld, d.out_ld = 32, 31
     assert _status(fwd) == B.ERR_INVALID_ARG
-    d.out_ld, d.x_ld = 32, 17                            # rows off 16 bytes are laid out anew and need room for it
+    d.out_ld, d.x_ld = 32, 81                            # rows off 16 bytes are laid out anew and need room for it
     assert _status(lambda: fwd(n=0)) == B.ERR_ALLOC
-    assert B.slicegcn_ffn_workspace_bytes(d, AT) >= 2 * 40 * 16
+    assert B.slicegcn_ffn_workspace_bytes(d, AT) >= 2 * 40 * 80
     with pytest.raises(B.SliceGCNError):
         B.slicegcn_ffn_workspace_bytes(d, None)
 
@@ -66,8 +66,8 @@ def test_ffn_workspace_follows_what_is_laid_out():
     from paper_2408_11500_b200 import binding as B
     size = B.slicegcn_ffn_workspace_bytes
     assert size(_ffn(), AT) == 0
-    assert size(_ffn(), AT + 2) > 0 and size(_ffn(in_s=7, x_ld=16), AT) > 0 and size(_ffn(W=AT + 2), AT) > 0 and size(_ffn(out_s=9), AT) > 0
-    assert size(_ffn(dtype=B.F32), AT) >= 3 * 2 * (40 * 16 + 2 * 8 * 16)
+    assert size(_ffn(), AT + 2) > 0 and size(_ffn(in_s=39, x_ld=80), AT) > 0 and size(_ffn(W=AT + 2), AT) > 0 and size(_ffn(out_s=9), AT) > 0
+    assert size(_ffn(dtype=B.F32), AT) >= 3 * 2 * (40 * 80 + 2 * 40 * 16)
     assert size(_ffn(n=0), None) == 0
     assert size(_ffn(n=4, in_s=7, out_s=9, dtype=B.F32), AT + 4) == 0     # a few rows need none, whatever their layout
     assert size(_ffn(n=4), AT, AT) > 0

@@ -220,3 +220,15 @@ def test_products_in_pieces(shape, types):
         q = Problem(*shape, gated, act, dtype, grad, pad=pad, residual=residual)
         q.check_forward(q.forward())
         q.check_backward(q.backward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("types", ["bf16", "fp32", "bf16/fp32"])
+@pytest.mark.parametrize("shape", [(3000, 8, 14, 23), (777, 8, 4, 193), (5000, 6, 20, 64), (1000, 64, 1, 3), (2000, 4, 32, 32), (300, 12, 5, 1), (20_001, 8, 32, 64)], ids=str)
+def test_narrow_slices(shape, types):
+    """Slices of few columns are computed several at a time."""
+    dtype, grad = types.split("/") if "/" in types else (types, "same")
+    for gated, act, pad, residual in ((False, "silu", 1, True), (True, "gelu", 0, False), (False, "none", 5, True)):
+        q = Problem(*shape, gated, act, dtype, grad, pad=pad, residual=residual)
+        q.check_forward(q.forward())
+        q.check_backward(q.backward())
