@@ -569,8 +569,8 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
  * elements of a tensor (the block's largest magnitude times fp32's 1/127, 1/255; 0 when that is below the least normal number).  What a code
  * stands for is code * scale.  A code is rounded up where its fraction reaches a threshold that a hash of the element's index and t gives:
  * a state that moves by less than a code a step moves on average as it should, where rounding to nearest would leave it.  sqrt(v) > 0 never
- * becomes code 0.  The update uses m and v before they are rounded.  An eps below the least normal fp32 number counts as that number.  A gradient that is infinite or NaN makes the whole block's
- * states NaN.
+ * becomes code 0.  The update uses m and v before they are rounded.  An eps below the least normal fp32 number counts as that number.  A gradient that is infinite or NaN leaves no finite
+ * state in its whole block.
  */
 enum { SLICEGCN_Q8 = 2 };
 #define SLICEGCN_ADAMW_BLOCK 256

@@ -57,7 +57,7 @@ struct Params {
     int p, slices;                 // slices; slices times parts of the output (kDw), else the same
     int tiles_m, tiles_n, group;   // per slice; m tiles that follow one another before the next n tile
     Divide by_split, by_group, by_n, by_m, by_last;   // what item_of divides by
-    int items;
+    int items, clusters;
     int nt;                        // columns of B per CTA: 64 or 128
     int kb_total, kb_part, k_part; // 64-wide steps of an item, of one part of k, and that part's extent
     int chunk;                     // steps between emptyings of the accumulator
@@ -76,8 +76,9 @@ struct Params {
     void* out;
     int out_ld;
     int out_bf16, out_vec;
-    // kDz: sums over 32 rows each
-    float* sums;                   // [ceil(n/32)][parts * p][cols], or NULL
+    int fixed;                     // every pair of SMs stays with one column tile
+    // kDz: sums over 32 rows each, or (fixed) over all rows that an epilogue warp has seen
+    float* sums;                   // [ceil(n/32) or epilogue warps per column tile][parts * p][cols], or NULL
     float* partial;                // pieces' products, where they are joined by another kernel; kDw: [splits][slices][in_s][out_s], else [splits][slices][n][cols]
     int matrices;                  // kDw: slices times parts
     void *dw, *dw2;                // kDw, splits == 1
@@ -477,10 +478,10 @@ __device__ __forceinline__ void planes_out(const Params& P, const Where& w, int 
         }
     }
 }
-__device__ __forceinline__ void sums_out(const Params& P, const Where& w, int part, int col, float (&s)[8], int lane) {
+__device__ __forceinline__ void sums_out(const Params& P, int row, int matrix, int col, float (&s)[8], int lane) {
     const float t = sum_lanes(s, lane);
     const int c = col + sum_column(lane);
-    if (c < P.cols && w.rows > 0) P.sums[((int64_t)(w.row >> 5) * P.slices + part * P.p + w.slice) * P.cols + c] = t;
+    if (c < P.cols) P.sums[((int64_t)row * P.slices + matrix) * P.cols + c] = t;
 }
 
 // ------------------------------------------------------------------------------------------ the product
@@ -658,6 +659,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
         const int second = kGated ? P.nt : 32;   // columns from the first 32 to the other 32
         bool ok = true;
         int turn = 0, halves = 0;
+        float bias[8], bias2[8], s[8], s2[8];   // s, s2: column sums of da and dc; not gated: of da's two units
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = s2[j] = 0.f;
         Item ahead;   // of turn / 32 * 32 + lane: 32 tiles are worked out at once, each lane one, and passed around when their turn comes
         for (int i = first; ok && i < P.items; i += stride, ++turn) {
             if ((turn & 31) == 0) ahead = item_of<MODE>(P, min(i + lane * stride, P.items - 1));
@@ -782,27 +786,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                         }
                     }
                     if (kIsDz && P.sums) {
-                        sums_out(P, w, 0, col, s, lane);
-                        if (kGated) sums_out(P, w, 1, col, s2, lane);
+                        sums_out(P, w.row >> 5, w.slice, col, s, lane);
+                        if (kGated) sums_out(P, w.row >> 5, P.p + w.slice, col, s2, lane);
                     }
                 }
             } else {
                 // what a unit needs besides the product is on its way while the product is waited for
                 const bool with_in = kIsDz || (MODE != kDx && P.in);
-                float bias[8], bias2[8];
                 uint4 raw[4];
-                load_bias(P, MODE == kDx ? nullptr : P.b, w.slice, col0, bias, lane);
-                if (kGated) load_bias(P, P.b2, w.slice, col0, bias2, lane);
+                if (!kGated || !P.fixed || turn == group) {
+                    load_bias(P, MODE == kDx ? nullptr : P.b, w.slice, col0, bias, lane);
+                    if (kGated) load_bias(P, P.b2, w.slice, col0, bias2, lane);
+                }
                 if (with_in) load_in(P, w, col0, raw, lane);
                 ok = __all_sync(0xffffffffu, mbar_wait(tfull + group * 2 + (use & 1), (use >> 1) & 1));
                 if (!ok) break;
                 fence_after();
                 const uint32_t d = mine + (group * 2 + (use & 1)) * (2 * P.nt);
-#pragma unroll 1
+                if (kIsDz && !P.fixed) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s[j] = s2[j] = 0.f;
+                }
+#pragma unroll(kIsDz ? 2 : 1)
                 for (int u = 0; u < (kGated ? 1 : 2); ++u) {
                     const int col = col0 + u * 32;
                     const bool last = kGated || u == 1;
-                    float a[16], c[16], s[8], s2[8];
+                    float a[16], c[16];
                     // da and dc need both slabs, else the two take turns, so that one leaves while the other is filled
                     const uint32_t to = kIsDz && kGated ? slab : slab + (halves++ & 1) * 2048;
                     tmem_fragments(d + u * 32, a);
@@ -813,8 +822,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                         put_in(P, w, col, raw, to, lane);
                         __syncwarp();
                     }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) s[j] = s2[j] = 0.f;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (h) {
@@ -836,7 +843,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                         if constexpr (kIsDz) {
                             backward_as<ACT, kGated, false>(P.scale, in, a, c);
                             if (P.sums) {
-                                sum_half(a, s);
+                                if (u == 0)
+                                    sum_half(a, s);
+                                else
+                                    sum_half(a, s2);
                                 if (kGated) sum_half(c, s2);
                             }
                             if (kGated) {
@@ -870,15 +880,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     } else if (there) {
                         slab_out(static_cast<__nv_bfloat16*>(P.out) + (int64_t)w.row * P.out_ld + (w.slice * P.cols + col), P.out_ld, w.rows, P.cols - col, to, lane);
                     }
-                    if (kIsDz && P.sums && there) {
-                        sums_out(P, w, 0, col, s, lane);
-                        if (kGated) sums_out(P, w, 1, col, s2, lane);
+                    if (kIsDz && P.sums && !P.fixed && there) {
+                        sums_out(P, w.row >> 5, w.slice, col, u == 0 ? s : s2, lane);
+                        if (kGated) sums_out(P, w.row >> 5, P.p + w.slice, col, s2, lane);
                     }
                     if (!last) {
                         load_bias(P, MODE == kDx ? nullptr : P.b, w.slice, col + 32, bias, lane);
                         if (with_in) load_in(P, w, col + 32, raw, lane);
                     }
                 }
+            }
+        }
+        if constexpr (kIsDz && !PROMO) {
+            if (ok && P.sums && P.fixed) {   // the first item's columns are all items' columns; a warp without an item adds zeros
+                const Item t = item_of<MODE>(P, first);
+                const int per = P.slices / (kGated ? 2 : 1) * P.tiles_n;   // column tiles; pairs of SMs `per` apart share one
+                const int row = ((first / per * 2 + (int)rank) * 4 + quarter) * groups + group, col = t.n + part * share;
+                sums_out(P, row, t.slice, col, s, lane);
+                sums_out(P, row, kGated ? P.p + t.slice : t.slice, kGated ? col : col + 32, s2, lane);
             }
         }
         if (lane == 0) stores_done();
@@ -1385,6 +1404,7 @@ constexpr int kChunkF32 = 4, kChunkLong = 64;
 struct Cut {
     int nt = 128, tiles_m = 1, tiles_n = 1, splits = 1, kb = 1, chunk = 1;   // kb: steps of a piece of k, the same for each
     bool swapped = false, pair = false;
+    int fixed = 0;   // pairs of SMs that work, where each stays with one column tile
     double cost = 1e300;
 };
 // SM cycles of `items` tiles: a 64-wide step takes its MMAs' time, or with half-width tiles rather what its copies take; a tile's start
@@ -1420,6 +1440,14 @@ Cut cut_rows(int64_t n, int p, int cols, bool gated, int64_t kb, int pairs) {
     }
     return best;
 }
+// Pairs of SMs that stay with a column tile each, item after item: their biases and column sums stay in registers (gradients of
+// 169,343 x 256 -> 2 x 1,024: 610 -> 580 us).  Where that leaves no more than two idle, else 0.
+int fixed_pairs(const Cut& c, int p) {
+    const int64_t per = (int64_t)p * c.tiles_n;
+    if (c.splits > 1 || per > kPairs) return 0;
+    const int64_t used = std::min<int64_t>(kPairs / per, c.tiles_m) * per;
+    return used >= 72 ? (int)used : 0;
+}
 // Pieces of the rows for dW; which of the two operands gives the tile's 256 rows.
 Cut cut_dw(int64_t n, int p, int parts, int in_s, int out_s, int pairs) {
     Cut best;
@@ -1453,6 +1481,7 @@ struct Plan {
     int x_planes = 1, w_planes = 1, z_planes = 1;
     int in_pad = 0, out_pad = 0, parts = 1, sum_chunks = 1;
     Cut product, dx, dw;
+    int64_t sum_rows = 0;   // of what the column sums are taken of
     int64_t x_at = 0, w_at = 0, w2_at = 0, z_at = 0, sums_at = 0, chunks_at = 0, partial_at = 0, bytes = 0;
 };
 
@@ -1510,8 +1539,10 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
     }
     if (back) {
         if (q.dz || q.pack_g) q.z_at = take(2 * q.z_planes * n * q.parts * p * q.out_pad);
-        if (q.dz) q.sums_at = take(4 * ceil_div(n, 32) * cols);
-        const int64_t rows = q.dz ? ceil_div(n, 32) : n;
+        if (q.dz && !f32 && q.z_planes == 1) q.product.fixed = fixed_pairs(q.product, p);
+        q.sum_rows = !q.dz ? n : !q.product.fixed ? ceil_div(n, 32) : q.product.fixed / (p * q.product.tiles_n) * (q.product.nt == 64 ? 16 : 8);
+        if (q.dz) q.sums_at = take(4 * q.sum_rows * cols);
+        const int64_t rows = q.sum_rows;
         q.sum_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({kSumChunks, ceil_div(148 * 6, ceil_div(cols, 128)), rows / 64}));
         q.chunks_at = take(4 * q.sum_chunks * cols);
         q.dx = cut_rows(n, p, q.in_s, false, q.parts * ceil_div(q.out_s, 64), pairs_of(q.z_planes, q.w_planes));
@@ -1597,7 +1628,7 @@ template <int MODE, bool PROMO, int ACT>
 slicegcn_status_t launch_as(const Params& P, cudaStream_t st) {
     static SmemLimit limit;
     SGCN_TRY(limit.set((const void*)ffn_kernel<MODE, PROMO, ACT>, kSmem));
-    return launch_after(ffn_kernel<MODE, PROMO, ACT>, dim3(2 * std::min(P.items, kPairs)), kThreads, kSmem, st, P);
+    return launch_after(ffn_kernel<MODE, PROMO, ACT>, dim3(2 * P.clusters), kThreads, kSmem, st, P);
 }
 template <int MODE, bool PROMO>
 slicegcn_status_t launch(const Params& P, int act, cudaStream_t st) {
@@ -1611,7 +1642,9 @@ slicegcn_status_t launch(const Params& P, int act, cudaStream_t st) {
 
 slicegcn_status_t set_cut(Params& P, const Cut& c, bool dw) {
     P.nt = c.nt, P.tiles_m = c.tiles_m, P.tiles_n = c.tiles_n, P.splits = c.splits, P.kb_total = c.kb, P.chunk = c.chunk;
-    P.group = dw ? 1 : std::min(c.tiles_m, 8);
+    P.clusters = c.fixed ? c.fixed : (int)std::min<int64_t>((int64_t)P.slices * P.tiles_m * P.tiles_n * P.splits, kPairs);
+    P.fixed = c.fixed > 0;
+    P.group = dw || P.fixed ? 1 : std::min(c.tiles_m, 8);
     const int64_t tiles = (int64_t)P.slices * P.tiles_m * P.tiles_n;
     if (tiles * P.splits > (1 << 30)) SGCN_FAIL(SLICEGCN_ERR_OVERFLOW, "ffn: too many tiles");
     P.items = (int)tiles * P.splits;
@@ -1876,7 +1909,7 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
     if (sums) {
         SumArgs A;
         A.src = q.dz ? (const void*)(ws + q.sums_at) : dout;
-        A.rows = q.dz ? ceil_div(n, 32) : n;
+        A.rows = q.sum_rows;
         A.cols = (int)(q.parts * outs);
         A.ld = q.dz ? A.cols : d->dout_ld;
         A.bf16 = !q.dz && ge == 2;
