@@ -4,9 +4,10 @@
 // States in 32 bits, or in 8: int8 codes of m and uint8 codes of sqrt(v), a scale each per block of 256 elements.  sqrt(v) instead
 // of v, since the update needs no more of v and a linear code of the root reaches 255^2 down in v.
 //
-// Bound by HBM: 28 bytes an element with 32-bit states, 16 with 8-bit ones (fp32 gradients; 2 more for a bf16 copy).  A warp takes
-// a block of 256 elements, eight per lane, all its loads on their way together: the block's largest magnitudes are then five
-// shuffles away, and no shared memory or barrier is needed.
+// Bound by HBM: 28 bytes an element with 32-bit states (245 M elements in 1,095 us, 6.3 TB/s), 16 with 8-bit ones (fp32 gradients; 2
+// more for a bf16 copy), where instructions come before it (95 an element: 245 M with bf16 gradients and copies in 840 us, 4.7
+// TB/s).  A warp takes a block of 256 elements, eight per lane, all its loads on their way together: the block's largest
+// magnitudes are then one reduction of the warp away, and no shared memory or barrier is needed.
 #include <algorithm>
 #include <cmath>
 
@@ -40,7 +41,7 @@ struct Table {
 };
 struct Hyper {
     float beta1, one_minus_beta1, beta2, one_minus_beta2, eps;
-    double lr, beta1d, beta2d, weight_decay, max_norm;
+    double lr, log_beta1, log_beta2, weight_decay, max_norm;
     const float *grad_norm, *lr_scale;
     int64_t* step;
     int last;        // this launch is the call's last: it advances the step
@@ -106,8 +107,7 @@ __device__ __forceinline__ void store_bf16(__nv_bfloat16* t, int lane, int left,
     }
 }
 // Conversions between codes and floats go through the significand of a number whose last bit counts one (or 2^-16): the conversion
-// instructions share a unit of a sixteenth of the rate with roots and quotients, and six of them for each element paced the kernel
-// (837 us for 245 M elements; see below for now).
+// instructions share a unit of an eighth of the rate with roots and quotients.
 constexpr float kTwo23 = 8388608.f;
 // Codes as they lie in memory, one byte each, in the lowest byte of 2^23's pattern.
 template <bool VEC>
@@ -168,25 +168,29 @@ __device__ __forceinline__ void update_block(const Entry& e, int64_t block, int 
     const int64_t at = block * kBlock;
     const int left = (int)min(e.elems - at, (int64_t)kBlock);
     float p[kPerLane], g[kPerLane], m[kPerLane], v[kPerLane];
+    uint32_t mc[kPerLane], vc[kPerLane];
+    float ms0 = 0.f, vs0 = 0.f;
+    load_f32<VEC>(e.p + at, lane, left, p);
+    if (Q8) {
+        load_codes<VEC>(static_cast<const uint8_t*>(e.m) + at, lane, left, mc);
+        load_codes<VEC>(static_cast<const uint8_t*>(e.v) + at, lane, left, vc);
+        ms0 = e.m_scale[block], vs0 = e.v_scale[block];
+    } else {
+        load_f32<VEC>(static_cast<const float*>(e.m) + at, lane, left, m);
+        load_f32<VEC>(static_cast<const float*>(e.v) + at, lane, left, v);
+    }
+    // last, since the two cases' loads are waited for where they meet
     if (e.g_bf16)
         load_bf16<VEC>(static_cast<const __nv_bfloat16*>(e.g) + at, lane, left, g);
     else
         load_f32<VEC>(static_cast<const float*>(e.g) + at, lane, left, g);
-    load_f32<VEC>(e.p + at, lane, left, p);
     if (Q8) {
-        uint32_t mc[kPerLane], vc[kPerLane];
-        load_codes<VEC>(static_cast<const uint8_t*>(e.m) + at, lane, left, mc);
-        load_codes<VEC>(static_cast<const uint8_t*>(e.v) + at, lane, left, vc);
-        const float ms = e.m_scale[block], vs = e.v_scale[block];
 #pragma unroll
         for (int k = 0; k < kPerLane; ++k) {
-            m[k] = __fmul_rn(__uint_as_float(mc[k] ^ 0x80u) - (kTwo23 + 128.f), ms);   // a signed code plus 128 is unsigned
-            const float root = __fmul_rn(__uint_as_float(vc[k]) - kTwo23, vs);
+            m[k] = __fmul_rn(__uint_as_float(mc[k] ^ 0x80u) - (kTwo23 + 128.f), ms0);   // a signed code plus 128 is unsigned
+            const float root = __fmul_rn(__uint_as_float(vc[k]) - kTwo23, vs0);
             v[k] = __fmul_rn(root, root);
         }
-    } else {
-        load_f32<VEC>(static_cast<const float*>(e.m) + at, lane, left, m);
-        load_f32<VEC>(static_cast<const float*>(e.v) + at, lane, left, v);
     }
     const float shrink = e.decayed ? s.decay : 1.f;
     if (s.factor64 != 0.0) {
@@ -217,7 +221,6 @@ __device__ __forceinline__ void update_block(const Entry& e, int64_t block, int 
     if (ms < kLeastNormal) ms = 0.f;
     if (vs < kLeastNormal) vs = 0.f;
     const float mi = ms > 0.f ? __fdiv_rn(1.f, ms) : 0.f, vi = vs > 0.f ? __fdiv_rn(1.f, vs) : 0.f;
-    uint32_t mc[kPerLane], vc[kPerLane];
 #pragma unroll
     for (int k = 0; k < kPerLane; ++k) {
         const uint32_t u = thresholds((uint32_t)(at + place<VEC>(lane, k)), s.t_mixed);
@@ -237,10 +240,10 @@ __device__ __forceinline__ void update_block(const Entry& e, int64_t block, int 
 template <bool Q8, int N>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table<N> t, const __grid_constant__ Hyper h) {
     __shared__ Step shared;
-    __shared__ double power[2];
+    __shared__ double corr[2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t step = h.step[0] + 1;
-    if (threadIdx.x < 2) power[threadIdx.x] = pow(threadIdx.x ? h.beta2d : h.beta1d, (double)step);   // two lanes side by side
+    if (threadIdx.x < 2) corr[threadIdx.x] = -expm1((double)step * (threadIdx.x ? h.log_beta2 : h.log_beta1));   // 1 - beta^t, two lanes side by side
     __syncwarp();
     if (threadIdx.x == 0) {
         const double rate = h.lr * (h.lr_scale ? (double)*h.lr_scale : 1.0);
@@ -251,8 +254,8 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
         }
         shared.factor = (float)factor;
         shared.factor64 = factor < (double)kLeastNormal ? factor : 0.0;
-        shared.rate = (float)(rate / (1.0 - power[0]));
-        shared.inv_root_corr = (float)(1.0 / sqrt(1.0 - power[1]));
+        shared.rate = (float)(rate / corr[0]);
+        shared.inv_root_corr = (float)(1.0 / sqrt(corr[1]));
         shared.decay = (float)(1.0 - rate * h.weight_decay);
         shared.t_mixed = (uint32_t)step * 0x85EBCA6Bu;
     }
@@ -358,7 +361,7 @@ slicegcn_status_t slicegcn_adamw_step(const slicegcn_adamw_desc* d, int64_t* ste
     h.beta1 = (float)d->beta1, h.one_minus_beta1 = (float)(1.0 - d->beta1);
     h.beta2 = (float)d->beta2, h.one_minus_beta2 = (float)(1.0 - d->beta2);
     h.eps = std::max((float)d->eps, kLeastNormal);   // 0 / 0 otherwise, where gradients have been zero
-    h.lr = d->lr, h.beta1d = d->beta1, h.beta2d = d->beta2, h.weight_decay = d->weight_decay, h.max_norm = d->max_norm;
+    h.lr = d->lr, h.log_beta1 = std::log(d->beta1), h.log_beta2 = std::log(d->beta2), h.weight_decay = d->weight_decay, h.max_norm = d->max_norm;
     h.grad_norm = grad_norm, h.lr_scale = d->lr_scale;
     h.step = step;
     h.last = 1;
