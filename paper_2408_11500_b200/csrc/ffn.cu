@@ -212,6 +212,19 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, bool k_contiguous) 
 // and 136 instructions per 32 columns' sums; the gated forward's epilogue fell from 552 instructions a unit to under 400), and 8x8
 // matrix loads and stores bring bf16 fragments to shared memory, from where they leave in whole lines.
 
+// Two fp32 operations in one instruction, each rounded as the single one is: half the issue slots of the epilogue's sums and products.
+__device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tadd.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void mul2(float& x, float& y, float a, float b) {
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tmul.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+// x, y = x a + c, y b + d
+__device__ __forceinline__ void fma2(float& x, float& y, float a, float b, float c, float d) {
+    asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tmov.b64 r, {%4, %5};\n\tfma.rn.f32x2 p, p, q, r;\n\tmov.b64 {%0, %1}, p;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b), "f"(c), "f"(d));
+}
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&t);
@@ -359,12 +372,12 @@ __device__ __forceinline__ void load_bias(const Params& P, const float* b, int s
 }
 __device__ __forceinline__ void add_bias(float (&v)[16], const float (&b)[8]) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] += b[(k >> 2) * 2 + (k & 1)];
+    for (int k = 0; k < 16; k += 2) add2(v[k], v[k + 1], b[(k >> 2) * 2], b[(k >> 2) * 2 + 1]);
 }
 // Column sums of a unit: each lane's over its rows, then over the eight lanes that hold the same columns, each of which ends with one.
 __device__ __forceinline__ void sum_half(const float (&v)[16], float (&s)[8]) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s[(k >> 2) * 2 + (k & 1)] += v[k];
+    for (int k = 0; k < 16; k += 2) add2(s[(k >> 2) * 2], s[(k >> 2) * 2 + 1], v[k], v[k + 1]);
 }
 __device__ __forceinline__ float sum_lanes(float (&s)[8], int lane) {   // of column 8 (k >> 1) + 2 (lane % 4) + (k & 1), k = sum_column(lane)
 #pragma unroll
@@ -383,71 +396,108 @@ __device__ __forceinline__ int sum_column(int lane) {
     return 8 * (k >> 1) + 2 * (lane & 3) + (k & 1);
 }
 
-// 1 / (1 + exp(-w)).  Where results are rounded to bf16 the hardware's exponential and reciprocal (2^-22 each, and 2^-24 |w| of the
-// argument) are exact enough (one reciprocal for two numbers, 1/x = y/(xy), gained nothing); `t` is -w log2(e).
-__device__ __forceinline__ float sigmoid_of(float t) {
-    float e, q;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(1.f + e));
-    return q;
-}
+// SILU and GELU multiply a by a gate 1 / (1 + exp(-w)): w = a, or 2 u with (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)).
 constexpr float kLog2e = 1.4426950408889634f, kGeluA = 0.7978845608028654f, kGeluB = 0.044715f;
-template <bool ACCURATE>
-__device__ __forceinline__ float sigmoid(float w) {
-    return ACCURATE ? 1.f / (1.f + expf(-w)) : sigmoid_of(-kLog2e * w);
+template <int ACT>
+__device__ __forceinline__ float gate_of(float a) {
+    return 1.f / (1.f + expf(ACT == SLICEGCN_ACT_SILU ? -a : -2.f * kGeluA * a * fmaf(kGeluB, a * a, 1.f)));
 }
-template <bool ACCURATE>
-__device__ __forceinline__ float gelu_gate(float a) {   // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u))
-    const float s = a * a;
-    return ACCURATE ? sigmoid<true>(2.f * kGeluA * a * fmaf(kGeluB, s, 1.f)) : sigmoid_of(a * fmaf(-2.f * kLog2e * kGeluA * kGeluB, s, -2.f * kLog2e * kGeluA));
-}
-// act(a)
-template <int ACT, bool ACCURATE>
-__device__ __forceinline__ float act_of(float a) {
-    if (ACT == SLICEGCN_ACT_SILU) return a * sigmoid<ACCURATE>(a);
-    if (ACT == SLICEGCN_ACT_GELU) return a * gelu_gate<ACCURATE>(a);
-    if (ACT == SLICEGCN_ACT_RELU) return a > 0.f || isnan(a) ? a : 0.f;
-    return a;
-}
-// act(a) and act'(a)
-template <int ACT, bool ACCURATE>
-__device__ __forceinline__ void act_both(float a, float& y, float& dy) {
+// Where results are rounded to bf16 the hardware's exponential and reciprocal (2^-22 each, and 2^-24 |w| of the argument) are exact
+// enough (one reciprocal for two numbers, 1/x = y/(xy), gained nothing).  Two numbers at a time; s = a^2.
+template <int ACT>
+__device__ __forceinline__ void gates_of(float a0, float a1, float s0, float s1, float& q0, float& q1) {
     if (ACT == SLICEGCN_ACT_SILU) {
-        const float q = sigmoid<ACCURATE>(a);
-        y = a * q;
-        dy = fmaf(y, 1.f - q, q);
-    } else if (ACT == SLICEGCN_ACT_GELU) {
-        const float q = gelu_gate<ACCURATE>(a);
-        y = a * q;
-        dy = fmaf(y * (1.f - q), 2.f * kGeluA * fmaf(3.f * kGeluB, a * a, 1.f), q);
-    } else if (ACT == SLICEGCN_ACT_RELU) {
-        y = a > 0.f || isnan(a) ? a : 0.f;
-        dy = a > 0.f ? 1.f : 0.f;
+        q0 = a0, q1 = a1;
+        mul2(q0, q1, -kLog2e, -kLog2e);
     } else {
-        y = a;
-        dy = 1.f;
+        constexpr float c0 = -2.f * kLog2e * kGeluA, c1 = c0 * kGeluB;
+        q0 = s0, q1 = s1;
+        fma2(q0, q1, c1, c1, c0, c0);
+        mul2(q0, q1, a0, a1);
     }
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(q0));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(q1));
+    add2(q0, q1, 1.f, 1.f);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(q0));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(q1));
 }
+__device__ __forceinline__ float relu(float a) { return a > 0.f || isnan(a) ? a : 0.f; }
+// a -> act(a) [* c]
 template <int ACT, bool GATED, bool ACCURATE, int N>
 __device__ __forceinline__ void forward_as(float (&a)[N], const float (&c)[N]) {
+    constexpr bool kSmooth = ACT == SLICEGCN_ACT_SILU || ACT == SLICEGCN_ACT_GELU;
+    if constexpr (ACCURATE) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        a[k] = act_of<ACT, ACCURATE>(a[k]);
-        if (GATED) a[k] *= c[k];
+        for (int k = 0; k < N; ++k) {
+            if (kSmooth) a[k] *= gate_of<ACT>(a[k]);
+            if (ACT == SLICEGCN_ACT_RELU) a[k] = relu(a[k]);
+            if (GATED) a[k] *= c[k];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; k += 2) {
+            if (kSmooth) {
+                float s0 = a[k], s1 = a[k + 1], q0, q1;
+                if (ACT == SLICEGCN_ACT_GELU) mul2(s0, s1, a[k], a[k + 1]);
+                gates_of<ACT>(a[k], a[k + 1], s0, s1, q0, q1);
+                mul2(a[k], a[k + 1], q0, q1);
+            }
+            if (ACT == SLICEGCN_ACT_RELU) a[k] = relu(a[k]), a[k + 1] = relu(a[k + 1]);
+            if (GATED) mul2(a[k], a[k + 1], c[k], c[k + 1]);
+        }
     }
 }
-// a, c -> da, dc
+// a, c -> da, dc:  SILU' = q + y (1 - q),  GELU' = q + y (1 - q) 2 A (1 + 3 B a^2)  with the gate q and y = a q
 template <int ACT, bool GATED, bool ACCURATE, int N>
 __device__ __forceinline__ void backward_as(float scale, const float (&g)[N], float (&a)[N], float (&c)[N]) {
+    constexpr bool kSmooth = ACT == SLICEGCN_ACT_SILU || ACT == SLICEGCN_ACT_GELU;
+    if constexpr (ACCURATE) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        float y, dy;
-        act_both<ACT, ACCURATE>(a[k], y, dy);
-        const float gk = g[k] * scale;
-        a[k] = GATED ? gk * c[k] * dy : gk * dy;
-        if (GATED) c[k] = gk * y;
+        for (int k = 0; k < N; ++k) {
+            float y = a[k], dy = 1.f;
+            if (kSmooth) {
+                const float q = gate_of<ACT>(a[k]);
+                y *= q;
+                dy = fmaf(y * (1.f - q), ACT == SLICEGCN_ACT_GELU ? 2.f * kGeluA * fmaf(3.f * kGeluB, a[k] * a[k], 1.f) : 1.f, q);
+            }
+            if (ACT == SLICEGCN_ACT_RELU) y = relu(a[k]), dy = a[k] > 0.f ? 1.f : 0.f;
+            const float gk = g[k] * scale;
+            a[k] = GATED ? gk * c[k] * dy : gk * dy;
+            if (GATED) c[k] = gk * y;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; k += 2) {
+            float y0 = a[k], y1 = a[k + 1], d0 = 1.f, d1 = 1.f, g0 = g[k], g1 = g[k + 1];
+            mul2(g0, g1, scale, scale);
+            if (kSmooth) {
+                float s0 = a[k], s1 = a[k + 1], q0, q1;
+                if (ACT == SLICEGCN_ACT_GELU) mul2(s0, s1, a[k], a[k + 1]);
+                gates_of<ACT>(a[k], a[k + 1], s0, s1, q0, q1);
+                mul2(y0, y1, q0, q1);
+                d0 = q0, d1 = q1;
+                fma2(d0, d1, -1.f, -1.f, 1.f, 1.f);
+                if (ACT == SLICEGCN_ACT_GELU) {
+                    fma2(s0, s1, 6.f * kGeluA * kGeluB, 6.f * kGeluA * kGeluB, 2.f * kGeluA, 2.f * kGeluA);
+                    mul2(d0, d1, s0, s1);
+                }
+                fma2(d0, d1, y0, y1, q0, q1);
+            }
+            if (ACT == SLICEGCN_ACT_RELU) {
+                y0 = relu(a[k]), y1 = relu(a[k + 1]);
+                d0 = a[k] > 0.f ? 1.f : 0.f, d1 = a[k + 1] > 0.f ? 1.f : 0.f;
+            }
+            a[k] = g0, a[k + 1] = g1;
+            if (GATED) mul2(a[k], a[k + 1], c[k], c[k + 1]);
+            if (ACT != SLICEGCN_ACT_NONE) mul2(a[k], a[k + 1], d0, d1);
+            if (GATED) {
+                c[k] = y0, c[k + 1] = y1;
+                mul2(c[k], c[k + 1], g0, g1);
+            }
+        }
     }
 }
+
 // Parts of an fp32 number whose sum it is: 8 bits each.  Cut, not rounded: no part leaves the range, and each is exact.  Takes the
 // next part off x.
 __device__ __forceinline__ uint32_t next_part(float& x) {
@@ -857,10 +907,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                             if (MODE != kDx) forward_as<ACT, kGated, false>(a, c);
                             if (with_in) {
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) a[j] = fmaf(a[j], P.scale, in[j]);
+                                for (int j = 0; j < 16; j += 2) fma2(a[j], a[j + 1], P.scale, P.scale, in[j], in[j + 1]);
                             } else if (P.scale != 1.f) {
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) a[j] *= P.scale;
+                                for (int j = 0; j < 16; j += 2) mul2(a[j], a[j + 1], P.scale, P.scale);
                             }
                         }
                         pack_half(a, words);
@@ -1536,6 +1586,8 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
     if (!back || q.dz) {
         q.product = cut_rows(n, p, q.out_s, d->W2 != nullptr, ceil_div(q.in_s, 64), pairs_of(q.x_planes, q.w_planes));
         if (q.product.splits > 1) partial = 4LL * q.product.splits * n * cols;
+        // a long k leaves little to gain, and idle pairs of SMs to lose
+        if (!back && d->W2 && !f32 && q.in_s <= 512) q.product.fixed = fixed_pairs(q.product, p);
     }
     if (back) {
         if (q.dz || q.pack_g) q.z_at = take(2 * q.z_planes * n * q.parts * p * q.out_pad);
