@@ -400,7 +400,7 @@ __device__ __forceinline__ int sum_column(int lane) {
 constexpr float kLog2e = 1.4426950408889634f, kGeluA = 0.7978845608028654f, kGeluB = 0.044715f;
 template <int ACT>
 __device__ __forceinline__ float gate_of(float a) {
-    return 1.f / (1.f + expf(ACT == SLICEGCN_ACT_SILU ? -a : -2.f * kGeluA * a * fmaf(kGeluB, a * a, 1.f)));
+    return __fdividef(1.f, 1.f + expf(ACT == SLICEGCN_ACT_SILU ? -a : -2.f * kGeluA * a * fmaf(kGeluB, a * a, 1.f)));   // 2 units of the last place each
 }
 // Where results are rounded to bf16 the hardware's exponential and reciprocal (2^-22 each, and 2^-24 |w| of the argument) are exact
 // enough (one reciprocal for two numbers, 1/x = y/(xy), gained nothing).  Two numbers at a time; s = a^2.
@@ -1413,6 +1413,117 @@ __global__ void __launch_bounds__(kRowsThreads) ffn_rows_kernel(const __grid_con
     if (parts > 1) cluster_sync();                // no CTA's memory goes while another reads it
 }
 
+// ------------------------------------------------------------------------------------------ little work in awkward layouts
+//
+// Forward products of fp32, or of bf16 rows off 16 bytes, would be laid out anew before the tensor cores can read them; where there is
+// little arithmetic that costs more than plain fp32 multiply-adds (19,697 x 25 -> 14 fp32: 16.5 us by way of the tensor cores).  Tiles
+// of 64 x 64, sixteen k at a time through shared memory, 4 x 4 results a thread (gated: of both products); one launch, no workspace.
+constexpr int kLittleK = 16, kLittleTile = 64;
+struct LittleArgs {
+    const void* x;
+    int64_t x_ld;
+    const void *W, *W2;
+    const float *b, *b2;
+    const void* r;
+    int64_t r_ld;
+    void* out;
+    int64_t out_ld;
+    int n, in_s, out_s, act, tiles_n;
+    float scale;
+};
+template <bool GATED, bool BF16>
+__global__ void __launch_bounds__(256) ffn_little_kernel(const __grid_constant__ LittleArgs A) {
+    __shared__ __align__(16) float xs[2][kLittleK][kLittleTile + 4];
+    __shared__ __align__(16) float ws[2][1 + GATED][kLittleK][kLittleTile];
+    cudaGridDependencySynchronize();
+    cudaTriggerProgrammaticLaunchCompletion();
+    const int tile_n = blockIdx.x % A.tiles_n, slice = blockIdx.x / A.tiles_n, row0 = blockIdx.y * kLittleTile, col0 = tile_n * kLittleTile;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int64_t wat = (int64_t)slice * A.in_s * A.out_s;
+    float fx[4], fw[1 + GATED][4];
+    // of x: row threadIdx / 16 + 16 q, k threadIdx % 16; of W: k threadIdx / 64 + 4 q, column threadIdx % 64
+    auto fetch = [&](int k0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int row = row0 + (threadIdx.x >> 4) + 16 * q, k = k0 + (threadIdx.x & 15);
+            fx[q] = row < A.n && k < A.in_s ? load_one<BF16>(A.x, row * A.x_ld + (int64_t)slice * A.in_s + k) : 0.f;
+            const int wk = k0 + (threadIdx.x >> 6) + 4 * q, col = col0 + (threadIdx.x & 63);
+            const bool there = wk < A.in_s && col < A.out_s;
+            fw[0][q] = there ? load_one<BF16>(A.W, wat + (int64_t)wk * A.out_s + col) : 0.f;
+            if (GATED) fw[GATED][q] = there ? load_one<BF16>(A.W2, wat + (int64_t)wk * A.out_s + col) : 0.f;
+        }
+    };
+    auto put = [&](int to) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            xs[to][threadIdx.x & 15][(threadIdx.x >> 4) + 16 * q] = fx[q];
+#pragma unroll
+            for (int g = 0; g < 1 + GATED; ++g) ws[to][g][(threadIdx.x >> 6) + 4 * q][threadIdx.x & 63] = fw[g][q];
+        }
+    };
+    float a[16], c[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) a[j] = c[j] = 0.f;
+    fetch(0);
+    put(0);
+    __syncthreads();
+    int at = 0;
+    for (int k0 = 0; k0 < A.in_s; k0 += kLittleK, at ^= 1) {
+        const bool more = k0 + kLittleK < A.in_s;
+        if (more) fetch(k0 + kLittleK);   // on its way while this step is worked on
+#pragma unroll
+        for (int k = 0; k < kLittleK; ++k) {
+            const float4 xv = *reinterpret_cast<const float4*>(&xs[at][k][ty * 4]);
+            const float xr[4] = {xv.x, xv.y, xv.z, xv.w};
+#pragma unroll
+            for (int g = 0; g < 1 + GATED; ++g) {
+                const float4 wv = *reinterpret_cast<const float4*>(&ws[at][g][k][tx * 4]);
+                const float wr[4] = {wv.x, wv.y, wv.z, wv.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float& to = g ? c[i * 4 + j] : a[i * 4 + j];
+                        to = fmaf(xr[i], wr[j], to);
+                    }
+            }
+        }
+        if (more) put(at ^ 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int col = col0 + tx * 4 + j;
+        const float b = A.b && col < A.out_s ? A.b[slice * A.out_s + col] : 0.f, b2 = GATED && A.b2 && col < A.out_s ? A.b2[slice * A.out_s + col] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i * 4 + j] += b, c[i * 4 + j] += b2;
+    }
+    if (A.act == SLICEGCN_ACT_SILU)
+        forward_as<SLICEGCN_ACT_SILU, GATED, true>(a, c);
+    else if (A.act == SLICEGCN_ACT_GELU)
+        forward_as<SLICEGCN_ACT_GELU, GATED, true>(a, c);
+    else if (A.act == SLICEGCN_ACT_RELU)
+        forward_as<SLICEGCN_ACT_RELU, GATED, true>(a, c);
+    else
+        forward_as<SLICEGCN_ACT_NONE, GATED, true>(a, c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = row0 + ty * 4 + i;
+        if (row >= A.n) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int col = col0 + tx * 4 + j;
+            if (col >= A.out_s) break;
+            const int64_t o = (int64_t)slice * A.out_s + col;
+            const float v = A.r ? fmaf(a[i * 4 + j], A.scale, load_one<BF16>(A.r, row * A.r_ld + o)) : a[i * 4 + j] * A.scale;
+            if (BF16)
+                static_cast<__nv_bfloat16*>(A.out)[row * A.out_ld + o] = __float2bfloat16_rn(v);
+            else
+                static_cast<float*>(A.out)[row * A.out_ld + o] = v;
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------ host
 
 typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -1527,7 +1638,7 @@ Cut cut_dw(int64_t n, int p, int parts, int in_s, int out_s, int pairs) {
 // block-diagonal matrix cost no MMA more, and there are fewer and wider tiles (8 slices of 14 -> 23 columns: half the time).
 struct Plan {
     int p = 1, in_s = 1, out_s = 1, merge = 1;   // slices and their columns as the products see them
-    bool rows = false, pack_x = false, pack_w = false, pack_g = false, dz = false;
+    bool rows = false, little = false, pack_x = false, pack_w = false, pack_g = false, dz = false;
     int x_planes = 1, w_planes = 1, z_planes = 1;
     int in_pad = 0, out_pad = 0, parts = 1, sum_chunks = 1;
     Cut product, dx, dw;
@@ -1583,6 +1694,20 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
         if (d->W2) q.w2_at = take(2LL * q.w_planes * p * q.in_s * q.out_pad);
     }
     const int64_t cols = (int64_t)q.parts * p * q.out_s;
+    if (!back && (q.pack_x || q.pack_w)) {
+        // SM cycles, as measured: a tile over all SMs, the latency of its steps, a launch; against the tensor cores' tiles, the
+        // matrices' way through the workspace and the packing launch
+        const int64_t tiles = ceil_div(n, kLittleTile) * ceil_div(d->out_s, kLittleTile) * d->num_slices;
+        const double steps = (double)ceil_div(d->in_s, kLittleK);
+        const double little = (double)tiles * (1600.0 * q.parts * steps + 1200.0) / 148 + steps * 1800 + 4000;
+        const double packed = (double)n * p * q.in_s * (f32 ? 16 : 6) + (double)q.parts * p * q.in_s * q.out_s * (f32 ? 16 : 6);
+        const Cut c = cut_rows(n, p, q.out_s, d->W2 != nullptr, ceil_div(q.in_s, 64), pairs_of(q.x_planes, q.w_planes));
+        if (ceil_div(n, kLittleTile) <= 65535 && little < c.cost + packed / 3400 + 10000) {
+            q.little = true;
+            q.bytes = 0;
+            return;
+        }
+    }
     if (!back || q.dz) {
         q.product = cut_rows(n, p, q.out_s, d->W2 != nullptr, ceil_div(q.in_s, 64), pairs_of(q.x_planes, q.w_planes));
         if (q.product.splits > 1) partial = 4LL * q.product.splits * n * cols;
@@ -1818,6 +1943,15 @@ slicegcn_status_t rows_forward(const slicegcn_ffn_desc* d, const void* x, const 
     return launch_rows<8>(A, bf16, vec, parts, d->num_slices, st);
 }
 
+slicegcn_status_t little_forward(const slicegcn_ffn_desc* d, const void* x, const void* r, void* out, cudaStream_t st) {
+    LittleArgs A = {x, d->x_ld, d->W, d->W2, d->b, d->b2, r, d->r_ld, out, d->out_ld, (int)d->n, d->in_s, d->out_s, d->act,
+                    (int)ceil_div(d->out_s, kLittleTile), (float)d->scale};
+    const dim3 grid((unsigned)(A.tiles_n * d->num_slices), (unsigned)ceil_div(d->n, kLittleTile));
+    if (d->dtype == SLICEGCN_BF16)
+        return d->W2 ? launch_after(ffn_little_kernel<true, true>, grid, 256, 0, st, A) : launch_after(ffn_little_kernel<false, true>, grid, 256, 0, st, A);
+    return d->W2 ? launch_after(ffn_little_kernel<true, false>, grid, 256, 0, st, A) : launch_after(ffn_little_kernel<false, false>, grid, 256, 0, st, A);
+}
+
 }  // namespace
 }  // namespace sgcn
 
@@ -1853,6 +1987,7 @@ slicegcn_status_t slicegcn_ffn_forward(const slicegcn_ffn_desc* d, const void* x
     if (!some) return SLICEGCN_OK;
     cudaStream_t st = (cudaStream_t)stream;
     if (q.rows) return rows_forward(d, x, r, out, st);
+    if (q.little) return little_forward(d, x, r, out, st);
     char* ws = static_cast<char*>(workspace);
     Operand ox, ow[2];
     PackArgs packs = {};

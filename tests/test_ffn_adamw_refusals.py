@@ -55,21 +55,23 @@ def test_ffn_matrices():
     assert _status(bwd) == B.ERR_INVALID_ARG
     d.dout_ld, d.out_ld = 32, 31
     assert _status(fwd) == B.ERR_INVALID_ARG
-    d.out_ld, d.x_ld = 32, 81                            # rows off 16 bytes are laid out anew and need room for it
+    d.out_ld, d.n, d.in_s, d.out_s, d.x_ld = 1024, 40_000, 400, 512, 801     # rows off 16 bytes are laid out anew and need room for it
     assert _status(lambda: fwd(n=0)) == B.ERR_ALLOC
-    assert B.slicegcn_ffn_workspace_bytes(d, AT) >= 2 * 40 * 80
+    assert B.slicegcn_ffn_workspace_bytes(d, AT) >= 2 * 40_000 * 800
     with pytest.raises(B.SliceGCNError):
         B.slicegcn_ffn_workspace_bytes(d, None)
 
 
 def test_ffn_workspace_follows_what_is_laid_out():
     from paper_2408_11500_b200 import binding as B
-    size = B.slicegcn_ffn_workspace_bytes
-    assert size(_ffn(), AT) == 0
-    assert size(_ffn(), AT + 2) > 0 and size(_ffn(in_s=39, x_ld=80), AT) > 0 and size(_ffn(W=AT + 2), AT) > 0 and size(_ffn(out_s=9), AT) > 0
-    assert size(_ffn(dtype=B.F32), AT) >= 3 * 2 * (40 * 80 + 2 * 40 * 16)
+    size, large = B.slicegcn_ffn_workspace_bytes, dict(n=40_000, in_s=400, out_s=512)
+    assert size(_ffn(**large), AT) == 0
+    assert size(_ffn(**large), AT + 2) > 0 and size(_ffn(**{**large, "in_s": 399}, x_ld=800), AT) > 0 and size(_ffn(**large, W=AT + 2), AT) > 0
+    assert size(_ffn(**{**large, "out_s": 509}), AT) > 0
+    assert size(_ffn(**large, dtype=B.F32), AT) >= 3 * 2 * (40_000 * 800 + 2 * 400 * 512)
     assert size(_ffn(n=0), None) == 0
     assert size(_ffn(n=4, in_s=7, out_s=9, dtype=B.F32), AT + 4) == 0     # a few rows need none, whatever their layout
+    assert size(_ffn(dtype=B.F32), AT) == 0                               # nor does little work
     assert size(_ffn(n=4), AT, AT) > 0
     with pytest.raises(TypeError):
         _ffn(y_ld=3)
