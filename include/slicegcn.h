@@ -516,8 +516,11 @@ slicegcn_status_t slicegcn_clip_grads(const slicegcn_tensor_list* list, double m
  *   out_s = r_s + scale * act(a) * c      (gated)
  * num_slices = 1 is the ordinary matrix product.  act: NONE a;  RELU max(a, 0);  SILU a / (1 + exp(-a));
  * GELU a/2 * (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))).  ReLU'(0) = 0.
- * x, W, W2, r and out are stored as `dtype` (bf16 weights: the copies that slicegcn_adamw_step keeps), biases are fp32.  All
- * arithmetic is fp32-accurate from the stored values, with one rounding of out; sums over long axes are added in pieces.
+ * x, W, W2, r and out are stored as `dtype` (bf16 weights: the copies that slicegcn_adamw_step keeps), biases are fp32.  Products
+ * and activations are computed from the stored values with fp32's digits and rounded once, as out; with bf16 storage sums over long
+ * axes keep about 2^-28 of relative accuracy per column added, at worst (2^-16 at 4,096).  A row of x with infinite or NaN
+ * elements has no finite results where such an element enters, and may have NaN in its other slices too (narrow slices are
+ * computed together); other rows are not touched.
  */
 enum { SLICEGCN_ACT_NONE = 0, SLICEGCN_ACT_RELU = 1, SLICEGCN_ACT_SILU = 2, SLICEGCN_ACT_GELU = 3 };
 #define SLICEGCN_MAX_FFN_WIDTH 65536

@@ -1585,20 +1585,29 @@ int pairs_of(int pa, int pb) {
 // would leave pairs of SMs idle; pieces of k where there are few tiles (as two separate products then, if gated).
 Cut cut_rows(int64_t n, int p, int cols, bool gated, int64_t kb, int pairs) {
     Cut best;
-    for (int s = 1; s <= 32; ++s) {
+    const int chunk = pairs > 1 ? kChunkF32 : 1;
+    auto consider = [&](int s) {
         Cut c;
-        const int chunk = pairs > 1 ? kChunkF32 : 1, per = s > 1 ? (int)up(ceil_div(kb, s), chunk) : (int)kb;
-        if (s > 1 && ceil_div(kb, per) != s) continue;
+        const int per = s > 1 ? (int)up(ceil_div(kb, s), chunk) : (int)kb;
+        s = (int)ceil_div(kb, per);
         const bool two = gated && s == 1;
         const int one = two ? 64 : 128, slices = p * (gated && !two ? 2 : 1);
         c.tiles_m = (int)ceil_div(n, 256);
         c.nt = cols <= one || (int64_t)c.tiles_m * slices * ceil_div(cols, 2 * one) * s * 2 <= kPairs ? 64 : 128;
         c.tiles_n = (int)ceil_div(cols, two ? c.nt : 2 * c.nt);
         c.splits = s, c.kb = per, c.chunk = pairs > 1 ? kChunkF32 : per;
-        c.cost = cost_of((int64_t)slices * c.tiles_m * c.tiles_n, s, per, pairs, c.nt, 4.0 * n * slices * cols);
+        const int64_t tiles = (int64_t)slices * c.tiles_m * c.tiles_n;
+        c.cost = cost_of(tiles, s, per, pairs, c.nt, 4.0 * n * slices * cols);
         if (c.cost < best.cost) best = c;
-        if (n > 74 * 256) break;   // the SMs have work anyway
-    }
+        return tiles;
+    };
+    const int64_t tiles = consider(1);
+    if (tiles < kPairs)   // else the SMs have work anyway
+        for (int r = 1; r <= 2; ++r)
+            for (int wide = 1; wide <= 4; wide *= 2) {   // the pieces' tiles are other ones, to be met once or twice by each pair of SMs
+                const int64_t s = std::min<int64_t>(32, kPairs * r / std::max<int64_t>(1, tiles * wide / 2));
+                if (s > 1) consider((int)s);
+            }
     return best;
 }
 // Pairs of SMs that stay with a column tile each, item after item: their biases and column sums stay in registers (gradients of
@@ -1615,17 +1624,16 @@ Cut cut_dw(int64_t n, int p, int parts, int in_s, int out_s, int pairs) {
     for (int swapped = 0; swapped < 2; ++swapped) {
         const int m = swapped ? in_s : out_s, k = swapped ? out_s : in_s;
         const int64_t all = ceil_div(n, 64);
-        for (int s = 1; s <= 2 * kPairs; ++s) {
+        const bool pair = swapped && parts == 2;
+        const int one = pair ? 64 : 128, slices = pair ? p : parts * p, nt = k <= one ? 64 : 128;
+        const int64_t tiles_m = ceil_div(m, 256), tiles_n = ceil_div(k, pair ? nt : 2 * nt), tiles = slices * tiles_m * tiles_n;
+        for (int r : {0, 1, 2, 4, 8, 12, 16}) {   // pieces that fill a quarter, a half of the pairs of SMs, all once, twice ...
             Cut c;
-            c.swapped = swapped, c.splits = s;
-            c.kb = (int)ceil_div(all, s);
-            if (ceil_div(all, c.kb) != s) continue;
-            c.pair = swapped && parts == 2;
-            const int one = c.pair ? 64 : 128, slices = c.pair ? p : parts * p;
-            c.nt = k <= one ? 64 : 128;
-            c.tiles_m = (int)ceil_div(m, 256), c.tiles_n = (int)ceil_div(k, c.pair ? c.nt : 2 * c.nt);
+            c.swapped = swapped, c.pair = pair, c.nt = nt, c.tiles_m = (int)tiles_m, c.tiles_n = (int)tiles_n;
+            c.kb = (int)ceil_div(all, std::max<int64_t>(1, std::min<int64_t>(2 * kPairs, kPairs * r / (4 * tiles))));
+            c.splits = (int)ceil_div(all, c.kb);
             c.chunk = pairs > 1 ? kChunkF32 : kChunkLong;
-            c.cost = cost_of((int64_t)slices * c.tiles_m * c.tiles_n, s, c.kb, pairs, c.nt, 4.0 * parts * p * in_s * out_s);
+            c.cost = cost_of(tiles, c.splits, c.kb, pairs, c.nt, 4.0 * parts * p * in_s * out_s);
             if (c.cost < best.cost) best = c;
         }
     }
@@ -1634,8 +1642,8 @@ Cut cut_dw(int64_t n, int p, int parts, int in_s, int out_s, int pairs) {
 
 // What a call needs in the workspace, and where.
 //
-// Slices of few columns are taken together, as long as their columns of x stay within one 64-wide step of k: their weights as one
-// block-diagonal matrix cost no MMA more, and there are fewer and wider tiles (8 slices of 14 -> 23 columns: half the time).
+// Slices are taken together, their weights as one block-diagonal matrix, where that costs less: tiles and 64-wide steps of k have room for
+// columns of several narrow slices (8 slices of 14 -> 23 columns: a third of the time).
 struct Plan {
     int p = 1, in_s = 1, out_s = 1, merge = 1;   // slices and their columns as the products see them
     bool rows = false, little = false, pack_x = false, pack_w = false, pack_g = false, dz = false;
@@ -1669,18 +1677,27 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
         q.rows = true;
         return;
     }
-    for (int m = d->num_slices; m > 1; --m)
-        if (d->num_slices % m == 0 && m * d->in_s <= 64 && (int64_t)m * d->out_s <= SLICEGCN_MAX_FFN_WIDTH) {
-            q.merge = m;
-            break;
-        }
-    q.p = d->num_slices / q.merge, q.in_s = d->in_s * q.merge, q.out_s = d->out_s * q.merge;
+    const bool dz = back && (d->act != SLICEGCN_ACT_NONE || d->W2), gated = d->W2 != nullptr;
+    const int pairs = pairs_of(q.x_planes, q.w_planes), dx_pairs = pairs_of(q.z_planes, q.w_planes), dw_pairs = pairs_of(q.z_planes, q.x_planes);
+    double least = 1e300;
+    for (int m = 1; m <= d->num_slices; ++m) {
+        const int64_t ins = (int64_t)m * d->in_s, outs = (int64_t)m * d->out_s;
+        if (d->num_slices % m || (m > 1 && (ins > 2048 || outs > 8192))) continue;
+        const int p = d->num_slices / m;
+        Cut c[3];
+        if (!back || dz) c[0] = cut_rows(n, p, (int)outs, gated, ceil_div(ins, 64), pairs);
+        if (back) c[1] = cut_rows(n, p, (int)ins, false, q.parts * ceil_div(outs, 64), dx_pairs), c[2] = cut_dw(n, p, q.parts, (int)ins, (int)outs, dw_pairs);
+        double cost = (!back || dz ? c[0].cost : 0.0) + (back ? c[1].cost + c[2].cost : 0.0);
+        if (m > 1) cost += 0.1 * cost + 4000 + (double)q.parts * p * ins * outs * (f32 ? 10 : 4) / 3400;            // weights are laid out anew; the model's margin
+        if (!f32 && unaligned(x, d->x_ld, p, (int)ins)) cost += 4000 + (double)n * p * ins * 6 / 3400;              // x is, or needs not to be
+        if (cost < least) least = cost, q.merge = m, q.p = p, q.in_s = (int)ins, q.out_s = (int)outs, q.product = c[0], q.dx = c[1], q.dw = c[2];
+    }
     q.in_pad = (int)up(q.in_s, 8);
     q.out_pad = (int)up(q.out_s, 8);
     const int p = q.p;
     q.pack_x = f32 || unaligned(x, d->x_ld, p, q.in_s);
     q.pack_w = f32 || q.merge > 1 || unaligned(d->W, d->out_s, 1, 8) || unaligned(d->W2, d->out_s, 1, 8);
-    q.dz = back && (d->act != SLICEGCN_ACT_NONE || d->W2);
+    q.dz = dz;
     q.pack_g = back && !q.dz && (q.z_planes == 3 || unaligned(dout, d->dout_ld, p, q.out_s));
     int64_t at = 0, partial = 0;
     auto take = [&](int64_t bytes) {
@@ -1701,15 +1718,13 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
         const double steps = (double)ceil_div(d->in_s, kLittleK);
         const double little = (double)tiles * (1600.0 * q.parts * steps + 1200.0) / 148 + steps * 1800 + 4000;
         const double packed = (double)n * p * q.in_s * (f32 ? 16 : 6) + (double)q.parts * p * q.in_s * q.out_s * (f32 ? 16 : 6);
-        const Cut c = cut_rows(n, p, q.out_s, d->W2 != nullptr, ceil_div(q.in_s, 64), pairs_of(q.x_planes, q.w_planes));
-        if (ceil_div(n, kLittleTile) <= 65535 && little < c.cost + packed / 3400 + 10000) {
+        if (ceil_div(n, kLittleTile) <= 65535 && little < q.product.cost + packed / 3400 + 10000) {
             q.little = true;
             q.bytes = 0;
             return;
         }
     }
     if (!back || q.dz) {
-        q.product = cut_rows(n, p, q.out_s, d->W2 != nullptr, ceil_div(q.in_s, 64), pairs_of(q.x_planes, q.w_planes));
         if (q.product.splits > 1) partial = 4LL * q.product.splits * n * cols;
         // a long k leaves little to gain, and idle pairs of SMs to lose
         if (!back && d->W2 && !f32 && q.in_s <= 512) q.product.fixed = fixed_pairs(q.product, p);
@@ -1722,9 +1737,7 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
         const int64_t rows = q.sum_rows;
         q.sum_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({kSumChunks, ceil_div(148 * 6, ceil_div(cols, 128)), rows / 64}));
         q.chunks_at = take(4 * q.sum_chunks * cols);
-        q.dx = cut_rows(n, p, q.in_s, false, q.parts * ceil_div(q.out_s, 64), pairs_of(q.z_planes, q.w_planes));
         if (q.dx.splits > 1) partial = std::max<int64_t>(partial, 4LL * q.dx.splits * n * p * q.in_s);
-        q.dw = cut_dw(n, p, q.parts, q.in_s, q.out_s, pairs_of(q.z_planes, q.x_planes));
         if (q.dw.splits > 1 || q.merge > 1) partial = std::max<int64_t>(partial, 4LL * q.dw.splits * q.in_s * cols);
     }
     if (partial) q.partial_at = take(partial);
