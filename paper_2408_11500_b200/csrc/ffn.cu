@@ -1416,8 +1416,9 @@ __global__ void __launch_bounds__(kRowsThreads) ffn_rows_kernel(const __grid_con
 // ------------------------------------------------------------------------------------------ little work in awkward layouts
 //
 // Forward products of fp32, or of bf16 rows off 16 bytes, would be laid out anew before the tensor cores can read them; where there is
-// little arithmetic that costs more than plain fp32 multiply-adds (19,697 x 25 -> 14 fp32: 16.5 us by way of the tensor cores).  Tiles
-// of 64 x 64, sixteen k at a time through shared memory, 4 x 4 results a thread (gated: of both products); one launch, no workspace.
+// little arithmetic, or few columns for much of x, that costs more than plain fp32 multiply-adds (19,697 x 25 -> 14 fp32: 7 us, by
+// way of the tensor cores 16; 200,000 x 600 -> 8: 179 and 543).  Tiles of 64 x 64, sixteen k at a time through shared memory, 4 x 4
+// results a thread (gated: of both products); one launch, no workspace.
 constexpr int kLittleK = 16, kLittleTile = 64;
 struct LittleArgs {
     const void* x;
@@ -1430,7 +1431,43 @@ struct LittleArgs {
     int64_t out_ld;
     int n, in_s, out_s, act, tiles_n;
     float scale;
+    int x_vec, w_vec;   // fp32: 16 bytes at a time are aligned
 };
+// Bias, activation, gate, scale, residual and store of a thread's R rows x 4 columns.
+template <bool GATED, bool BF16, int R>
+__device__ __forceinline__ void little_finish(const LittleArgs& A, int slice, int row0, int col0, float (&a)[R * 4], float (&c)[R * 4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int col = col0 + j;
+        const float b = A.b && col < A.out_s ? A.b[slice * A.out_s + col] : 0.f, b2 = GATED && A.b2 && col < A.out_s ? A.b2[slice * A.out_s + col] : 0.f;
+#pragma unroll
+        for (int i = 0; i < R; ++i) a[i * 4 + j] += b, c[i * 4 + j] += b2;
+    }
+    if (A.act == SLICEGCN_ACT_SILU)
+        forward_as<SLICEGCN_ACT_SILU, GATED, true>(a, c);
+    else if (A.act == SLICEGCN_ACT_GELU)
+        forward_as<SLICEGCN_ACT_GELU, GATED, true>(a, c);
+    else if (A.act == SLICEGCN_ACT_RELU)
+        forward_as<SLICEGCN_ACT_RELU, GATED, true>(a, c);
+    else
+        forward_as<SLICEGCN_ACT_NONE, GATED, true>(a, c);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int row = row0 + i;
+        if (row >= A.n) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int col = col0 + j;
+            if (col >= A.out_s) break;
+            const int64_t o = (int64_t)slice * A.out_s + col;
+            const float v = A.r ? fmaf(a[i * 4 + j], A.scale, load_one<BF16>(A.r, row * A.r_ld + o)) : a[i * 4 + j] * A.scale;
+            if (BF16)
+                static_cast<__nv_bfloat16*>(A.out)[row * A.out_ld + o] = __float2bfloat16_rn(v);
+            else
+                static_cast<float*>(A.out)[row * A.out_ld + o] = v;
+        }
+    }
+}
 template <bool GATED, bool BF16>
 __global__ void __launch_bounds__(256) ffn_little_kernel(const __grid_constant__ LittleArgs A) {
     __shared__ __align__(16) float xs[2][kLittleK][kLittleTile + 4];
@@ -1491,37 +1528,104 @@ __global__ void __launch_bounds__(256) ffn_little_kernel(const __grid_constant__
         if (more) put(at ^ 1);
         __syncthreads();
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int col = col0 + tx * 4 + j;
-        const float b = A.b && col < A.out_s ? A.b[slice * A.out_s + col] : 0.f, b2 = GATED && A.b2 && col < A.out_s ? A.b2[slice * A.out_s + col] : 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i * 4 + j] += b, c[i * 4 + j] += b2;
-    }
-    if (A.act == SLICEGCN_ACT_SILU)
-        forward_as<SLICEGCN_ACT_SILU, GATED, true>(a, c);
-    else if (A.act == SLICEGCN_ACT_GELU)
-        forward_as<SLICEGCN_ACT_GELU, GATED, true>(a, c);
-    else if (A.act == SLICEGCN_ACT_RELU)
-        forward_as<SLICEGCN_ACT_RELU, GATED, true>(a, c);
+    little_finish<GATED, BF16, 4>(A, slice, row0 + ty * 4, col0 + tx * 4, a, c);
+}
+
+// The same for fp32, by asynchronous copies of 16 bytes or (other alignments) 4, two steps ahead.  TN: columns of a tile; with 16 it
+// has 128 rows, since few columns make x the main traffic.
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there, int bytes) {   // zeros where nothing is there
+    const int have = there ? bytes : 0;
+    if (bytes == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(have) : "memory");
     else
-        forward_as<SLICEGCN_ACT_NONE, GATED, true>(a, c);
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(have) : "memory");
+}
+template <bool GATED, int TN>
+__global__ void __launch_bounds__(256) ffn_little_f32_kernel(const __grid_constant__ LittleArgs A) {
+    constexpr int TM = TN == 16 ? 128 : 64, R = TM * TN / 1024, XS = kLittleK + 4, kDeep = 3, kTx = TN / 4;
+    __shared__ __align__(16) float xs[kDeep][TM][XS];
+    __shared__ __align__(16) float ws[kDeep][1 + GATED][kLittleK][TN];
+    cudaGridDependencySynchronize();
+    cudaTriggerProgrammaticLaunchCompletion();
+    const int tile_n = blockIdx.x % A.tiles_n, slice = blockIdx.x / A.tiles_n, row0 = blockIdx.y * TM, col0 = tile_n * TN;
+    const int tx = threadIdx.x % kTx, ty = threadIdx.x / kTx, tid = threadIdx.x;
+    const float* x = static_cast<const float*>(A.x) + (int64_t)slice * A.in_s;
+    const float* W[2] = {static_cast<const float*>(A.W) + (int64_t)slice * A.in_s * A.out_s,
+                         GATED ? static_cast<const float*>(A.W2) + (int64_t)slice * A.in_s * A.out_s : nullptr};
+    const int steps = (A.in_s + kLittleK - 1) / kLittleK;
+    auto fetch = [&](int step) {
+        const int k0 = step * kLittleK, to = step % kDeep;
+        if (step < steps) {
+            if (A.x_vec) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = row0 + ty * 4 + i;
-        if (row >= A.n) break;
+                for (int q = 0; q < TM / 64; ++q) {
+                    const int r = q * 64 + (tid >> 2), k = (tid & 3) * 4;
+                    const bool there = row0 + r < A.n && k0 + k < A.in_s;   // in_s is a multiple of 4
+                    copy_async(smem_u32(&xs[to][r][k]), there ? x + (row0 + r) * A.x_ld + k0 + k : x, there, 16);
+                }
+            } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int col = col0 + tx * 4 + j;
-            if (col >= A.out_s) break;
-            const int64_t o = (int64_t)slice * A.out_s + col;
-            const float v = A.r ? fmaf(a[i * 4 + j], A.scale, load_one<BF16>(A.r, row * A.r_ld + o)) : a[i * 4 + j] * A.scale;
-            if (BF16)
-                static_cast<__nv_bfloat16*>(A.out)[row * A.out_ld + o] = __float2bfloat16_rn(v);
-            else
-                static_cast<float*>(A.out)[row * A.out_ld + o] = v;
+                for (int q = 0; q < TM / 16; ++q) {
+                    const int r = q * 16 + (tid >> 4), k = tid & 15;
+                    const bool there = row0 + r < A.n && k0 + k < A.in_s;
+                    copy_async(smem_u32(&xs[to][r][k]), there ? x + (row0 + r) * A.x_ld + k0 + k : x, there, 4);
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < 1 + GATED; ++g) {
+                if (A.w_vec) {
+                    if (tid < kLittleK * kTx) {
+                        const int k = tid / kTx, c = tid % kTx * 4;
+                        const bool there = k0 + k < A.in_s && col0 + c < A.out_s;   // out_s is a multiple of 4
+                        copy_async(smem_u32(&ws[to][g][k][c]), there ? W[g] + (int64_t)(k0 + k) * A.out_s + col0 + c : W[g], there, 16);
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < TN / 16; ++q) {
+                        const int e = q * 256 + tid, k = e / TN, c = e % TN;
+                        const bool there = k0 + k < A.in_s && col0 + c < A.out_s;
+                        copy_async(smem_u32(&ws[to][g][k][c]), there ? W[g] + (int64_t)(k0 + k) * A.out_s + col0 + c : W[g], there, 4);
+                    }
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    float a[R * 4], c[R * 4];
+#pragma unroll
+    for (int j = 0; j < R * 4; ++j) a[j] = c[j] = 0.f;
+    fetch(0);
+    fetch(1);
+    for (int step = 0; step < steps; ++step) {
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncthreads();   // this step has come, and the one before is no longer read
+        fetch(step + 2);
+        const int at = step % kDeep;
+#pragma unroll
+        for (int k0 = 0; k0 < kLittleK; k0 += 4) {
+            float xr[R][4];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const float4 t = *reinterpret_cast<const float4*>(&xs[at][ty * R + i][k0]);
+                xr[i][0] = t.x, xr[i][1] = t.y, xr[i][2] = t.z, xr[i][3] = t.w;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int g = 0; g < 1 + GATED; ++g) {
+                    const float4 t = *reinterpret_cast<const float4*>(&ws[at][g][k0 + k][tx * 4]);
+                    const float wr[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+                    for (int i = 0; i < R; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float& to = g ? c[i * 4 + j] : a[i * 4 + j];
+                            to = fmaf(xr[i][k], wr[j], to);
+                        }
+                }
         }
     }
+    little_finish<GATED, false, R>(A, slice, row0 + ty * R, col0 + tx * 4, a, c);
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -1712,13 +1816,16 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
     }
     const int64_t cols = (int64_t)q.parts * p * q.out_s;
     if (!back && (q.pack_x || q.pack_w)) {
-        // SM cycles, as measured: a tile over all SMs, the latency of its steps, a launch; against the tensor cores' tiles, the
-        // matrices' way through the workspace and the packing launch
-        const int64_t tiles = ceil_div(n, kLittleTile) * ceil_div(d->out_s, kLittleTile) * d->num_slices;
-        const double steps = (double)ceil_div(d->in_s, kLittleK);
-        const double little = (double)tiles * (1600.0 * q.parts * steps + 1200.0) / 148 + steps * 1800 + 4000;
+        // SM cycles, as measured: a step of a tile where there are tiles enough for all SMs, and where there is one; against the tensor
+        // cores' tiles, the matrices' way through the workspace and the packing launch
+        const bool narrow = f32 && d->out_s <= 16;
+        const int64_t tiles = ceil_div(n, narrow ? 128 : kLittleTile) * ceil_div(d->out_s, narrow ? 16 : kLittleTile) * d->num_slices;
+        const double steps = (double)ceil_div(d->in_s, kLittleK), wave = (double)tiles / 148;
+        const double step = narrow ? (gated ? 1070 : 825) : f32 ? (gated ? 2280 : 1180) : (gated ? 3200 : 1600);
+        const double least_step = narrow ? 1270 : f32 ? (gated ? 2050 : 1400) : (gated ? 2600 : 1800);
+        const double little = 1.2 * steps * std::max(least_step, step * wave) + 1200 * wave + 6000;
         const double packed = (double)n * p * q.in_s * (f32 ? 16 : 6) + (double)q.parts * p * q.in_s * q.out_s * (f32 ? 16 : 6);
-        if (ceil_div(n, kLittleTile) <= 65535 && little < q.product.cost + packed / 3400 + 10000) {
+        if (ceil_div(n, narrow ? 128 : kLittleTile) <= 65535 && little < q.product.cost + packed / 3400 + 10000) {
             q.little = true;
             q.bytes = 0;
             return;
@@ -1957,12 +2064,17 @@ slicegcn_status_t rows_forward(const slicegcn_ffn_desc* d, const void* x, const 
 }
 
 slicegcn_status_t little_forward(const slicegcn_ffn_desc* d, const void* x, const void* r, void* out, cudaStream_t st) {
-    LittleArgs A = {x, d->x_ld, d->W, d->W2, d->b, d->b2, r, d->r_ld, out, d->out_ld, (int)d->n, d->in_s, d->out_s, d->act,
-                    (int)ceil_div(d->out_s, kLittleTile), (float)d->scale};
-    const dim3 grid((unsigned)(A.tiles_n * d->num_slices), (unsigned)ceil_div(d->n, kLittleTile));
+    LittleArgs A = {x, d->x_ld, d->W, d->W2, d->b, d->b2, r, d->r_ld, out, d->out_ld, (int)d->n, d->in_s, d->out_s, d->act, 0, (float)d->scale, 0, 0};
+    const bool narrow = d->dtype == SLICEGCN_F32 && d->out_s <= 16;
+    A.tiles_n = (int)ceil_div(d->out_s, narrow ? 16 : kLittleTile);
+    const dim3 grid((unsigned)(A.tiles_n * d->num_slices), (unsigned)ceil_div(d->n, narrow ? 128 : kLittleTile));
     if (d->dtype == SLICEGCN_BF16)
         return d->W2 ? launch_after(ffn_little_kernel<true, true>, grid, 256, 0, st, A) : launch_after(ffn_little_kernel<false, true>, grid, 256, 0, st, A);
-    return d->W2 ? launch_after(ffn_little_kernel<true, false>, grid, 256, 0, st, A) : launch_after(ffn_little_kernel<false, false>, grid, 256, 0, st, A);
+    A.x_vec = (uintptr_t)x % 16 == 0 && d->x_ld % 4 == 0 && d->in_s % 4 == 0;
+    A.w_vec = (uintptr_t)d->W % 16 == 0 && (uintptr_t)d->W2 % 16 == 0 && d->out_s % 4 == 0;
+    if (narrow)
+        return d->W2 ? launch_after(ffn_little_f32_kernel<true, 16>, grid, 256, 0, st, A) : launch_after(ffn_little_f32_kernel<false, 16>, grid, 256, 0, st, A);
+    return d->W2 ? launch_after(ffn_little_f32_kernel<true, 64>, grid, 256, 0, st, A) : launch_after(ffn_little_f32_kernel<false, 64>, grid, 256, 0, st, A);
 }
 
 }  // namespace

@@ -232,3 +232,13 @@ def test_narrow_slices(shape, types):
         q = Problem(*shape, gated, act, dtype, grad, pad=pad, residual=residual)
         q.check_forward(q.forward())
         q.check_backward(q.backward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(1000, 1, 25, 14), (513, 2, 300, 9), (3000, 1, 16, 16), (129, 8, 13, 10), (70, 4, 7, 375), (65, 1, 100, 100), (10, 1, 4, 64), (20_000, 1, 1213, 5), (999, 1, 64, 61)], ids=str)
+def test_little_work(shape, dtype):
+    """Sizes and layouts that plain multiply-adds take, aligned (pad 4) and not."""
+    for gated, act, pad, residual in ((False, "silu", 1, True), (True, "gelu", 4, False), (False, "none", 0, False), (True, "relu", 3, True)):
+        q = Problem(*shape, gated, act, dtype, pad=pad, residual=residual, offset=pad)
+        q.check_forward(q.forward())
