@@ -517,10 +517,10 @@ slicegcn_status_t slicegcn_clip_grads(const slicegcn_tensor_list* list, double m
  * num_slices = 1 is the ordinary matrix product.  act: NONE a;  RELU max(a, 0);  SILU a / (1 + exp(-a));
  * GELU a/2 * (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))).  ReLU'(0) = 0.
  * x, W, W2, r and out are stored as `dtype` (bf16 weights: the copies that slicegcn_adamw_step keeps), biases are fp32.  Products
- * and activations are computed from the stored values with fp32's digits and rounded once, as out; with bf16 storage sums over long
- * axes keep about 2^-28 of relative accuracy per column added, at worst (2^-16 at 4,096).  A row of x with infinite or NaN
- * elements has no finite results where such an element enters, and may have NaN in its other slices too (narrow slices are
- * computed together); other rows are not touched.
+ * and activations are computed from the stored values with fp32's digits and rounded once, as out; sums whose only results are bf16
+ * keep 2^-28 of relative accuracy per column added, at worst (2^-16 at 4,096).  An infinite or NaN element of x, W or dout
+ * leaves no finite results where it enters (infinities may become NaN there); one of x or dout may do the same in the other slices
+ * of its row (narrow slices are computed together), and so in what is summed over rows.  Other rows of out and dx are not touched.
  */
 enum { SLICEGCN_ACT_NONE = 0, SLICEGCN_ACT_RELU = 1, SLICEGCN_ACT_SILU = 2, SLICEGCN_ACT_GELU = 3 };
 #define SLICEGCN_MAX_FFN_WIDTH 65536
@@ -572,8 +572,9 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
  * elements of a tensor (the block's largest magnitude times fp32's 1/127, 1/255; 0 when that is below the least normal number).  What a code
  * stands for is code * scale.  A code is rounded up where its fraction reaches a threshold that a hash of the element's index and t gives:
  * a state that moves by less than a code a step moves on average as it should, where rounding to nearest would leave it.  sqrt(v) > 0 never
- * becomes code 0.  The update uses m and v before they are rounded.  An eps below the least normal fp32 number counts as that number.  A gradient that is infinite or NaN leaves no finite
- * state in its whole block.
+ * becomes code 0.  The update uses m and v before they are rounded.  An eps below the least normal fp32 number
+ * counts as that number.  A gradient that is infinite or NaN, or whose square is past fp32's range, leaves no finite state in its
+ * whole block (fp32 states: of its own element).
  */
 enum { SLICEGCN_Q8 = 2 };
 #define SLICEGCN_ADAMW_BLOCK 256

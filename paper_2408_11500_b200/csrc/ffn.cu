@@ -10,13 +10,15 @@
 //   * Both operands come by tensor copy from where they lie, whichever of their axes is contiguous (x and dW's operands along
 //     rows, W along columns): nothing is transposed.  Odd strides, and fp32, are laid out in the workspace first.
 //   * fp32 values are three bf16 numbers (8 bits of the significand each), and a product of two of them is the six products
-//     of parts that reach fp32's last digit, the small ones first.  One code path, at a sixth of the bf16 rate.
+//     of parts that reach fp32's last digit, the small ones first, each tile of parts copied once.  A sixth of the bf16 rate.
 //   * Tensor memory's accumulation cuts digits off; over k in the hundreds of 16-wide steps that would show in fp32.  There the
-//     accumulator is emptied into registers every few hundred k ("chunk"), and the registers are added to with rounding.
+//     accumulator is emptied into registers every few steps ("chunk"), and the registers are added to with rounding.
 //   * Two accumulators: the sixteen epilogue warps work on one while the MMA fills the other.
 //   * The gate needs no second pass: the two halves of B are columns of W and of W2, so a and c of the same columns
 //     meet in the same thread.
 //   * dW = x^T da runs over rows; they are split over the SMs, and the pieces' sums are added in a fixed order.
+//   * Narrow slices are computed together, their weights as one block-diagonal matrix.  Up to eight rows, and little work in
+//     layouts that the tensor cores cannot read, go by plain multiply-adds (further down).
 #include <cuda.h>
 
 #include <algorithm>
@@ -61,8 +63,7 @@ struct Params {
     int nt;                        // columns of B per CTA: 64 or 128
     int kb_total, kb_part, k_part; // 64-wide steps of an item, of one part of k, and that part's extent
     int chunk;                     // steps between emptyings of the accumulator
-    int pairs;                     // products of operand parts
-    int8_t ia[6], ib[6];
+    int a_planes, b_planes;        // 3: parts of fp32
     int splits;                    // pieces of k (kDw: of the rows), kb_total steps each
     int swapped, pair;             // kDw: a tile's rows are dW's; and its column halves are dW's and dW2's
     // epilogue
@@ -72,10 +73,13 @@ struct Params {
     int bias_vec;                  // two of them at a time are aligned
     const void* in;                // r or dout
     int in_ld;
-    int in_vec;
+    int in_bf16, in_vec, in_pairs; // vec: 16 bytes at a time are aligned; pairs: 8
     void* out;
     int out_ld;
-    int out_bf16, out_vec;
+    int out_bf16, out_vec, out_pairs;   // vec: tensor copies reach it; pairs: 8 bytes at a time are aligned
+    __nv_bfloat16* dz;             // kDz, emptied into registers: da and dc, planes, strides of a row and a slice
+    int64_t dz_plane;
+    int planes, dz_row, dz_pad;
     int fixed;                     // every pair of SMs stays with one column tile
     // kDz: sums over 32 rows each, or (fixed) over all rows that an epilogue warp has seen
     float* sums;                   // [ceil(n/32) or epilogue warps per column tile][parts * p][cols], or NULL
@@ -209,7 +213,7 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, bool k_contiguous) 
 // A warp works on units of 32 rows x 32 columns, in halves of 16 rows.  Its registers hold them as tensor memory's 16x256b form, the
 // form of 8x8 matrix fragments, gives them: v[4 j + 2 q + e] is row 8 q + lane / 4, column 8 j + 2 (lane % 4) + e.  A lane then
 // needs the biases of eight columns only and adds up columns mostly within itself (a row per lane took 64 broadcast reads of biases
-// and 136 instructions per 32 columns' sums; the gated forward's epilogue fell from 552 instructions a unit to under 400), and 8x8
+// and 136 instructions per 32 columns' sums; the gated forward's epilogue fell from 552 instructions a unit to 419), and 8x8
 // matrix loads and stores bring bf16 fragments to shared memory, from where they leave in whole lines.
 
 // Two fp32 operations in one instruction, each rounded as the single one is: half the issue slots of the epilogue's sums and products.
@@ -316,38 +320,64 @@ __device__ __forceinline__ void put_in(const Params& P, const Where& w, int col,
         }
     }
 }
-// fp32 fragments and memory: four lanes share an aligned 32 bytes, so that no detour pays.
-__device__ __forceinline__ void load_half_f32(const Params& P, const Where& w, int col, int h, float (&v)[16], int lane) {
-    const float* at = static_cast<const float*>(P.in) + (int64_t)w.row * P.in_ld + (int64_t)w.slice * P.cols;
+// Where the accumulator is emptied into registers, r or dout come into the slab by asynchronous copies that are asked for before the
+// product is there (loads of fragments from memory took 4,800 cycles a half where the MMAs run 12,000 ahead): halves of 16 rows, 2 KB apart, rows of
+// 64 bytes of bf16 or 128 of fp32, chunks exchanged as tensor copies with that swizzle do.  Zeros where nothing is there.
+__device__ __forceinline__ void fetch_in(const Params& P, const Where& w, int col, uint32_t slab, int lane) {
+    const int elem = P.in_bf16 ? 2 : 4, chunks_log = P.in_bf16 ? 2 : 3;
+    const char* at = static_cast<const char*>(P.in) + ((int64_t)w.row * P.in_ld + (w.slice * P.cols + col)) * elem;
+    const int64_t step = (int64_t)P.in_ld * elem;
+    const int have = min(32, P.cols - col) * elem;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= 4 && P.in_bf16) break;
+        const int id = i * 32 + lane, row = id >> chunks_log, c = id & ((1 << chunks_log) - 1), left = row < w.rows ? max(0, min(16, have - c * 16)) : 0;
+        const uint32_t dst = slab + (row >> 4) * 2048 + ((row & 15) << (chunks_log + 4)) + ((c ^ (P.in_bf16 ? (row >> 1) & 3 : row & 7)) << 4);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(left ? at + row * step + c * 16 : static_cast<const char*>(P.in)), "r"(left) : "memory");
+    }
+}
+__device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// Element pair k of a lane's half of fp32.
+__device__ __forceinline__ uint32_t pair_at(uint32_t slab, int lane, int h, int k) {
+    return slab + h * 2048 + (8 * (k & 1) + (lane >> 2)) * 128 + (((2 * (k >> 1) + ((lane >> 1) & 1)) ^ (lane >> 2)) << 4) + (lane & 1) * 8;
+}
+__device__ __forceinline__ void half_of_in(const Params& P, uint32_t slab, int lane, int h, float (&v)[16]) {
+    if (P.in_bf16) return half_from_slab(v, slab + h * 1024, lane, h);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v[2 * k]), "=f"(v[2 * k + 1]) : "r"(pair_at(slab, lane, h, k)) : "memory");
+}
+// The same from and to memory whose rows no such copy can reach; fp32 in pairs, where they are aligned.
+__device__ __forceinline__ void load_half(const Params& P, const Where& w, int col, int h, float (&v)[16], int lane) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int c = col + 8 * (k >> 1) + 2 * (lane & 3), row = 16 * h + 8 * (k & 1) + (lane >> 2);
-        const float* p = at + (int64_t)row * P.in_ld + c;
+        const int64_t at = (int64_t)(w.row + row) * P.in_ld + (w.slice * P.cols + c);
         v[2 * k] = v[2 * k + 1] = 0.f;
-        if (row < w.rows) {
-            if (P.in_vec && c + 1 < P.cols) {
-                const float2 t = *reinterpret_cast<const float2*>(p);
-                v[2 * k] = t.x, v[2 * k + 1] = t.y;
-            } else {
-                if (c < P.cols) v[2 * k] = p[0];
-                if (c + 1 < P.cols) v[2 * k + 1] = p[1];
-            }
+        if (row >= w.rows) continue;
+        if (P.in_bf16) {
+            if (c < P.cols) v[2 * k] = __bfloat162float(static_cast<const __nv_bfloat16*>(P.in)[at]);
+            if (c + 1 < P.cols) v[2 * k + 1] = __bfloat162float(static_cast<const __nv_bfloat16*>(P.in)[at + 1]);
+        } else if (P.in_pairs && c + 1 < P.cols) {
+            const float2 t = *reinterpret_cast<const float2*>(static_cast<const float*>(P.in) + at);
+            v[2 * k] = t.x, v[2 * k + 1] = t.y;
+        } else {
+            if (c < P.cols) v[2 * k] = static_cast<const float*>(P.in)[at];
+            if (c + 1 < P.cols) v[2 * k + 1] = static_cast<const float*>(P.in)[at + 1];
         }
     }
 }
-__device__ __forceinline__ void store_half_f32(const Params& P, const Where& w, int col, int h, const float (&v)[16], int lane) {
-    float* at = static_cast<float*>(P.out) + (int64_t)w.row * P.out_ld + (int64_t)w.slice * P.cols;
+__device__ __forceinline__ void store_half(const Params& P, const Where& w, int col, int h, const float (&v)[16], int lane) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int c = col + 8 * (k >> 1) + 2 * (lane & 3), row = 16 * h + 8 * (k & 1) + (lane >> 2);
-        float* p = at + (int64_t)row * P.out_ld + c;
-        if (row < w.rows) {
-            if (P.out_vec && c + 1 < P.cols) {
-                *reinterpret_cast<float2*>(p) = make_float2(v[2 * k], v[2 * k + 1]);
-            } else {
-                if (c < P.cols) p[0] = v[2 * k];
-                if (c + 1 < P.cols) p[1] = v[2 * k + 1];
-            }
+        float* p = static_cast<float*>(P.out) + (int64_t)(w.row + row) * P.out_ld + (w.slice * P.cols + c);
+        if (row >= w.rows) continue;
+        if (P.out_pairs && c + 1 < P.cols) {
+            *reinterpret_cast<float2*>(p) = make_float2(v[2 * k], v[2 * k + 1]);
+        } else {
+            if (c < P.cols) p[0] = v[2 * k];
+            if (c + 1 < P.cols) p[1] = v[2 * k + 1];
         }
     }
 }
@@ -499,26 +529,32 @@ __device__ __forceinline__ void backward_as(float scale, const float (&g)[N], fl
 }
 
 // Parts of an fp32 number whose sum it is: 8 bits each.  Cut, not rounded: no part leaves the range, and each is exact.  Takes the
-// next part off x.
+// next part off x (off an infinity or a NaN: NaN is left).
 __device__ __forceinline__ uint32_t next_part(float& x) {
     const uint32_t part = __float_as_uint(x) & 0xffff0000u;
-    x = isfinite(x) ? x - __uint_as_float(part) : 0.f;
+    x -= __uint_as_float(part);
     return part;
 }
-// Half h of da or dc as three planes, by way of the slabs' four halves in turn.
-__device__ __forceinline__ void planes_out(const Params& P, const Where& w, int part, int col, int h, float (&v)[16], uint32_t slab, int& halves, int lane) {
+// Half h of da or dc as three planes, or rounded as one, by way of two slots in turn in the half's place.
+__device__ __forceinline__ void planes_out(const Params& P, const Where& w, int part, int col, int h, float (&v)[16], uint32_t slab, int& slots, int lane) {
 #pragma unroll
     for (int q = 0; q < 3; ++q) {
+        if (q >= P.planes) break;
         uint32_t words[8];
+        if (P.planes == 1) {
+            pack_half(v, words);
+        } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t lo = next_part(v[2 * k]), hi = next_part(v[2 * k + 1]);
-            words[k] = lo >> 16 | hi;
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t lo = __float_as_uint(v[2 * k]), hi = __float_as_uint(v[2 * k + 1]);
+                words[k] = __byte_perm(lo, hi, 0x7632);
+                if (q < 2) add2(v[2 * k], v[2 * k + 1], __uint_as_float((lo & 0xffff0000u) ^ 0x80000000u), __uint_as_float((hi & 0xffff0000u) ^ 0x80000000u));
+            }
         }
-        if (lane == 0) stores_read<3>();
+        if (lane == 0) stores_read<1>();
         __syncwarp();
-        const uint32_t at = slab + (halves & 3) * 1024;
-        ++halves;
+        const uint32_t at = slab + h * 2048 + (slots & 1) * 1024;
+        ++slots;
         half_to_slab(words, at, lane, 0);
         proxy_fence();
         __syncwarp();
@@ -601,6 +637,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
     cudaTriggerProgrammaticLaunchCompletion();
 
     const int chunks = (P.kb_total + P.chunk - 1) / P.chunk;
+    // Two operands in parts of fp32 come in three stages for 64 k -- parts 2 of both, then 0, then 1 -- and each is multiplied with all
+    // of the others that it is needed with: six products from six tiles, where a pair of tiles for each is twice the traffic
+    // from L2 (gradients of 232,965 x 600 -> 2 x 128: 1,620 -> 1,510 us).  Small products come first, since every addition cuts digits
+    // off the sum: the product of parts 0, which makes it large, is put off until the next 64 k's parts 2 are done; by then its
+    // stage's place in the ring is not needed yet.  One operand in parts: three products one after another over a chunk of k (in
+    // this way of three stages 480 instead of 340 us for dx of 169,343 x 256 -> 2 x 1,024, since two of three stages then are half empty).
+    const bool six = P.a_planes == 3 && P.b_planes == 3;
+    const int products = six ? 1 : max(P.a_planes, P.b_planes);
     // The two issuing warps walk their loops as whole warps, and one lane issues: what copies and MMAs are given then stays in
     // uniform registers.  (One lane in a loop of its own: 880 cycles per 64-wide step where the MMAs take 512.)
     if (warp == kEpiWarps) {
@@ -619,32 +663,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
             const CUtensorMap* bmap = (kGated && rank) || (MODE == kFwd && upper) ? &P.b1 : &P.b0;
             const int bcol = kGated || (MODE == kDw && P.pair) ? t.n : t.n + (int)rank * P.nt;
             const int first_kb = t.split * P.kb_total;
+            const auto fetch = [&](int kb, int plane) {   // of the operands that have it, else plane 0
+                ok = __all_sync(0xffffffffu, mbar_wait(empty + st, phase));
+                if (!ok) return;
+                const uint32_t a = base + st * kStageBytes, b = a + 16384u;
+                const bool second = MODE == kDx && first_kb + kb >= P.kb_part;
+                const int k = (first_kb + kb - (second ? P.kb_part : 0)) * 64;   // past the end there are only zeros
+                const int a_plane = min(plane, P.a_planes - 1), b_plane = min(plane, P.b_planes - 1);
+                if (one) {
+                    if (rank == 0) mbar_expect(full + st, bytes);
+                    if (kAK) {
+                        tma_load(a, &P.a, k, row0, second ? P.p + slice : slice, a_plane, full + st);
+                    } else {
+                        tma_load(a, &P.a, row0, k, aslice, a_plane, full + st);
+                        tma_load(a + 8192, &P.a, row0 + 64, k, aslice, a_plane, full + st);
+                    }
+                    if (kBK) {
+                        tma_load(b, second ? &P.b1 : &P.b0, k, bcol, slice, b_plane, full + st);
+                    } else {
+                        tma_load(b, bmap, bcol, k, bslice, b_plane, full + st);
+                        if (P.nt > 64) tma_load(b + 8192, bmap, bcol + 64, k, bslice, b_plane, full + st);
+                    }
+                }
+                __syncwarp();
+                ++fill;
+                if (++st == kStages) st = 0, phase ^= 1;
+            };
             for (int c = 0; ok && c < chunks; ++c) {
                 const int kb0 = c * P.chunk, kb1 = min(kb0 + P.chunk, P.kb_total);
-                for (int q = 0; ok && q < P.pairs; ++q)
-                    for (int kb = kb0; kb < kb1; ++kb, ++fill) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(empty + st, phase));
-                        if (!ok) break;
-                        const uint32_t a = base + st * kStageBytes, b = a + 16384u;
-                        const bool second = MODE == kDx && first_kb + kb >= P.kb_part;
-                        const int k = (first_kb + kb - (second ? P.kb_part : 0)) * 64;   // past the end there are only zeros
-                        if (one) {
-                            if (rank == 0) mbar_expect(full + st, bytes);
-                            if (kAK) {
-                                tma_load(a, &P.a, k, row0, second ? P.p + slice : slice, P.ia[q], full + st);
-                            } else {
-                                tma_load(a, &P.a, row0, k, aslice, P.ia[q], full + st);
-                                tma_load(a + 8192, &P.a, row0 + 64, k, aslice, P.ia[q], full + st);
-                            }
-                            if (kBK) {
-                                tma_load(b, second ? &P.b1 : &P.b0, k, bcol, slice, P.ib[q], full + st);
-                            } else {
-                                tma_load(b, bmap, bcol, k, bslice, P.ib[q], full + st);
-                                if (P.nt > 64) tma_load(b + 8192, bmap, bcol + 64, k, bslice, P.ib[q], full + st);
-                            }
+                for (int q = products - 1; ok && q >= 0; --q)
+                    for (int kb = kb0; ok && kb < kb1; ++kb) {
+                        if (six) {
+                            fetch(kb, 2);
+                            if (ok) fetch(kb, 0);
+                            if (ok) fetch(kb, 1);
+                        } else {
+                            fetch(kb, q);
                         }
-                        __syncwarp();
-                        if (++st == kStages) st = 0, phase ^= 1;
                     }
             }
         }
@@ -669,25 +724,56 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     if (!ok) break;
                     fence_after();
                     bool more = false;
-                    for (int q = 0; ok && q < P.pairs; ++q)
-                        for (int kb = kb0; kb < kb1; ++kb) {
-                            ok = __all_sync(0xffffffffu, mbar_wait(full + st, phase));
-                            if (!ok) break;
-                            fence_after();
-                            const uint32_t at = base + st * kStageBytes;
-                            const uint64_t ad = tile_desc(at, kAK), bd = tile_desc(at + 16384u, kBK);
-                            const int at_kb = first_kb + kb;
-                            const int left = MODE == kDw ? 64 : P.k_part - (at_kb >= P.kb_part ? at_kb - P.kb_part : at_kb) * 64;   // past the end there are only zeros
-                            if (one) {
+                    const auto arrived = [&](int& s) {   // the next stage of the ring
+                        s = st;
+                        ok = ok && __all_sync(0xffffffffu, mbar_wait(full + st, phase));
+                        fence_after();
+                        if (++st == kStages) st = 0, phase ^= 1;
+                        return ok;
+                    };
+                    const auto multiply = [&](int kb, int sa, int sb) {
+                        const uint64_t ad = tile_desc(base + sa * kStageBytes, kAK), bd = tile_desc(base + sb * kStageBytes + 16384u, kBK);
+                        const int at_kb = first_kb + kb;
+                        const int left = MODE == kDw ? 64 : P.k_part - (at_kb >= P.kb_part ? at_kb - P.kb_part : at_kb) * 64;   // past the end there are only zeros
+                        if (one) {
 #pragma unroll
-                                for (int s = 0; s < 4; ++s)
-                                    if (s == 0 || s * 16 < left) umma(d, ad + (uint64_t)(s * (kAK ? 2 : 128)), bd + (uint64_t)(s * (kBK ? 2 : 128)), idesc, s > 0 || more);
-                                umma_commit(empty + st);
-                            }
-                            __syncwarp();
-                            more = true;
-                            if (++st == kStages) st = 0, phase ^= 1;
+                            for (int s = 0; s < 4; ++s)
+                                if (s == 0 || s * 16 < left) umma(d, ad + (uint64_t)(s * (kAK ? 2 : 128)), bd + (uint64_t)(s * (kBK ? 2 : 128)), idesc, s > 0 || more);
                         }
+                        more = true;
+                    };
+                    const auto done_with = [&](int s) {
+                        if (one) umma_commit(empty + s);
+                        __syncwarp();
+                    };
+                    int x, y, z, held = -1;
+                    for (int q = 0; ok && q < products; ++q)
+                        for (int kb = kb0; kb < kb1; ++kb) {
+                            if (!six) {
+                                if (!arrived(z)) break;
+                                multiply(kb, z, z);
+                                done_with(z);
+                                continue;
+                            }
+                            if (!arrived(x) || !arrived(z)) break;
+                            multiply(kb, x, z);
+                            multiply(kb, z, x);
+                            done_with(x);
+                            if (held >= 0) {
+                                multiply(kb - 1, held, held);
+                                done_with(held);
+                            }
+                            if (!arrived(y)) break;
+                            multiply(kb, y, y);
+                            multiply(kb, y, z);
+                            multiply(kb, z, y);
+                            done_with(y);
+                            held = z;
+                        }
+                    if (ok && held >= 0) {
+                        multiply(kb1 - 1, held, held);
+                        done_with(held);
+                    }
                     if (one) umma_commit(tfull + acc);
                     __syncwarp();
                 }
@@ -777,6 +863,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                 float acc[64];   // half h of the first 32 columns at 16 h, of the other 32 at 32 + 16 h
 #pragma unroll
                 for (int j = 0; j < 64; ++j) acc[j] = 0.f;
+                const bool with_in = P.splits == 1 && (kIsDz || (MODE != kDx && P.in)), staged = with_in && P.in_vec;
+                if (staged) {
+                    if (lane == 0) stores_read<0>();
+                    __syncwarp();
+                    fetch_in(P, w, col0, slab, lane);
+                }
+                // a column's bias each, passed around later: loads in the epilogue took 4,000 cycles
+                float lower_bias = 0.f, upper_bias = 0.f;
+                if (MODE != kDx) {
+                    if (P.b && col0 + lane < P.cols) lower_bias = __ldg(P.b + (w.slice * P.cols + col0 + lane));
+                    const float* b = kGated ? P.b2 : P.b;
+                    const int c = kGated ? col0 + lane : col0 + 32 + lane;
+                    if (b && c < P.cols) upper_bias = __ldg(b + (w.slice * P.cols + c));
+                }
                 for (int c = 0; c < chunks; ++c, ++use) {
                     ok = __all_sync(0xffffffffu, mbar_wait(tfull + group * 2 + (use & 1), (use >> 1) & 1));
                     if (!ok) break;
@@ -794,6 +894,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     __syncwarp();
                     if (lane == 0) mbar_arrive_first(tempty + group * 2 + (use & 1));
                 }
+                if (staged) fetched();
+                __syncwarp();
                 if (!ok) break;
 #pragma unroll
                 for (int u = 0; u < (kGated ? 1 : 2); ++u) {
@@ -808,11 +910,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                         }
                         continue;
                     }
+                    if (u && staged) {
+                        if (lane == 0) stores_read<0>();
+                        __syncwarp();
+                        fetch_in(P, w, col, slab, lane);
+                        fetched();
+                        __syncwarp();
+                    }
                     float bias[8], bias2[8], s[8], s2[8];
-                    load_bias(P, MODE == kDx ? nullptr : P.b, w.slice, col, bias, lane);
-                    if (kGated) load_bias(P, P.b2, w.slice, col, bias2, lane);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s[j] = s2[j] = 0.f;
+                    for (int j = 0; j < 8; ++j) {
+                        const int from = 8 * (j >> 1) + 2 * (lane & 3) + (j & 1);
+                        if (MODE != kDx) bias[j] = __shfl_sync(0xffffffffu, u ? upper_bias : lower_bias, from);
+                        if (kGated) bias2[j] = __shfl_sync(0xffffffffu, upper_bias, from);
+                        s[j] = s2[j] = 0.f;
+                    }
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float a[16], c[16];
@@ -821,9 +933,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                         if (MODE != kDx) add_bias(a, bias);
                         if (kGated) add_bias(c, bias2);
                         float in[16];
-                        if (kIsDz || (MODE != kDx && P.in)) load_half_f32(P, w, col, h, in, lane);
+                        if (staged) {
+                            half_of_in(P, slab, lane, h, in);
+                            __syncwarp();   // its place is used from here on
+                        } else if (with_in) {
+                            load_half(P, w, col, h, in, lane);
+                        }
                         if constexpr (kIsDz) {
-                            backward_as<ACT, kGated, true>(P.scale, in, a, c);
+                            if (P.planes == 1)
+                                backward_as<ACT, kGated, false>(P.scale, in, a, c);
+                            else
+                                backward_as<ACT, kGated, true>(P.scale, in, a, c);
                             sum_half(a, s);
                             if (kGated) sum_half(c, s2);
                             planes_out(P, w, 0, col, h, a, slab, halves, lane);
@@ -831,8 +951,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                         } else {
                             if (MODE != kDx) forward_as<ACT, kGated, true>(a, c);
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) a[j] = MODE != kDx && P.in ? fmaf(a[j], P.scale, in[j]) : a[j] * P.scale;
-                            store_half_f32(P, w, col, h, a, lane);
+                            for (int j = 0; j < 16; ++j) a[j] = with_in ? fmaf(a[j], P.scale, in[j]) : a[j] * P.scale;
+                            if (P.out_vec) {
+                                if (lane == 0) stores_read<1>();   // of the same half before
+                                __syncwarp();
+#pragma unroll
+                                for (int k = 0; k < 8; ++k)
+                                    asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(pair_at(slab, lane, h, k)), "f"(a[2 * k]), "f"(a[2 * k + 1]) : "memory");
+                                proxy_fence();
+                                __syncwarp();
+                                if (lane == 0) {
+                                    if (w.rows > 16 * h) tma_store(&P.o, slab + h * 2048, col, w.row + 16 * h, w.slice, 0);
+                                    stores_commit();
+                                }
+                            } else {
+                                store_half(P, w, col, h, a, lane);
+                            }
                         }
                     }
                     if (kIsDz && P.sums) {
@@ -1014,9 +1148,6 @@ __global__ void __launch_bounds__(256) ffn_pack_kernel(const __grid_constant__ P
                 for (int q = 0; q < 8; ++q) v[q] = q >= first && q < left ? s[q] : 0.f;
             }
             uint32_t w[3][4];
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                if (isnan(v[q])) v[q] = __int_as_float(0x7fc00000);   // one whose upper half alone is a NaN too
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -1633,11 +1764,12 @@ __global__ void __launch_bounds__(256) ffn_little_f32_kernel(const __grid_consta
 typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// An operand: bf16, [plane][row][group][width] by strides in elements (multiples of 8 where there is more than one).
+// An operand (bf16) or a result: [plane][row][group][width] by strides in elements (multiples of 16 bytes where there is more than one).
 struct Operand {
     const void* base = nullptr;
     int64_t rows = 0, ld = 0, group_stride = 0, plane_stride = 0;
     int width = 0, groups = 1, planes = 1;
+    bool f32 = false;      // a result of fp32
 };
 slicegcn_status_t make_map(CUtensorMap* map, const Operand& o, int box_rows, bool result = false) {
     static EncodeFn encode = [] {
@@ -1649,11 +1781,12 @@ slicegcn_status_t make_map(CUtensorMap* map, const Operand& o, int box_rows, boo
     }();
     if (!encode) SGCN_FAIL(SLICEGCN_ERR_CUDA, "ffn: the driver has no tensor map encoder");
     const cuuint64_t dims[4] = {(cuuint64_t)o.width, (cuuint64_t)o.rows, (cuuint64_t)o.groups, (cuuint64_t)o.planes};
-    const cuuint64_t strides[3] = {(cuuint64_t)(o.rows > 1 ? o.ld : 8) * 2, (cuuint64_t)(o.groups > 1 ? o.group_stride : 8) * 2,
-                                   (cuuint64_t)(o.planes > 1 ? o.plane_stride : 8) * 2};
+    const int elem = o.f32 ? 4 : 2;
+    const cuuint64_t strides[3] = {(cuuint64_t)(o.rows > 1 ? o.ld : 8) * elem, (cuuint64_t)(o.groups > 1 ? o.group_stride : 8) * elem,
+                                   (cuuint64_t)(o.planes > 1 ? o.plane_stride : 8) * elem};
     const cuuint32_t box[4] = {result ? 32u : 64u, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
-    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(o.base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              result ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    const CUresult r = encode(map, o.f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(o.base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              result && !o.f32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) SGCN_FAIL(SLICEGCN_ERR_CUDA, "ffn: tensor map refused (%d)", (int)r);
     return SLICEGCN_OK;
@@ -1662,8 +1795,15 @@ slicegcn_status_t make_map(CUtensorMap* map, const Operand& o, int box_rows, boo
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Steps between emptyings: fp32's digits allow 256 k (16 additions in tensor memory); bf16 results only need it for long sums.
-constexpr int kChunkF32 = 4, kChunkLong = 64;
+// Steps between emptyings.  fp32's digits allow some twenty additions in tensor memory at the sum's full size: of six products two
+// steps' (those of parts 0 and four between them), else the last product of four steps.  For biases' gradients beside results of bf16: 512 k.
+// bf16 results only need it for long sums.
+constexpr int kChunkLong = 64;
+int chunk_of(int pairs) { return pairs == 6 ? 2 : 4; }
+constexpr int kChunkBiases = 8;
+// Biases' gradients are fp32 sums over da, whatever its type: with more than this many steps of k the accumulator's 2^-28 a column
+// would pass 2^-20 (they cut in one direction, so that sums over rows do not average it out), and it is emptied as for fp32.
+constexpr int kLongSteps = 12;
 
 // How a product is cut up.
 struct Cut {
@@ -1686,10 +1826,11 @@ int pairs_of(int pa, int pb) {
     return n;
 }
 // Tiles of a product over the rows of x (gated: of two at once); half-width ones where they cover the columns, or where whole ones
-// would leave pairs of SMs idle; pieces of k where there are few tiles (as two separate products then, if gated).
-Cut cut_rows(int64_t n, int p, int cols, bool gated, int64_t kb, int pairs) {
+// would leave pairs of SMs idle; pieces of k where there are few tiles (as two separate products then, if gated).  emptied: steps between
+// emptyings, 0: none but those of pieces.
+Cut cut_rows(int64_t n, int p, int cols, bool gated, int64_t kb, int pairs, int emptied) {
     Cut best;
-    const int chunk = pairs > 1 ? kChunkF32 : 1;
+    const int chunk = pairs > 1 ? chunk_of(pairs) : 1;
     auto consider = [&](int s) {
         Cut c;
         const int per = s > 1 ? (int)up(ceil_div(kb, s), chunk) : (int)kb;
@@ -1699,7 +1840,7 @@ Cut cut_rows(int64_t n, int p, int cols, bool gated, int64_t kb, int pairs) {
         c.tiles_m = (int)ceil_div(n, 256);
         c.nt = cols <= one || (int64_t)c.tiles_m * slices * ceil_div(cols, 2 * one) * s * 2 <= kPairs ? 64 : 128;
         c.tiles_n = (int)ceil_div(cols, two ? c.nt : 2 * c.nt);
-        c.splits = s, c.kb = per, c.chunk = pairs > 1 ? kChunkF32 : per;
+        c.splits = s, c.kb = per, c.chunk = emptied ? emptied : s > 1 ? chunk_of(pairs) : per;
         const int64_t tiles = (int64_t)slices * c.tiles_m * c.tiles_n;
         c.cost = cost_of(tiles, s, per, pairs, c.nt, 4.0 * n * slices * cols);
         if (c.cost < best.cost) best = c;
@@ -1736,7 +1877,7 @@ Cut cut_dw(int64_t n, int p, int parts, int in_s, int out_s, int pairs) {
             c.swapped = swapped, c.pair = pair, c.nt = nt, c.tiles_m = (int)tiles_m, c.tiles_n = (int)tiles_n;
             c.kb = (int)ceil_div(all, std::max<int64_t>(1, std::min<int64_t>(2 * kPairs, kPairs * r / (4 * tiles))));
             c.splits = (int)ceil_div(all, c.kb);
-            c.chunk = pairs > 1 ? kChunkF32 : kChunkLong;
+            c.chunk = pairs > 1 ? chunk_of(pairs) : kChunkLong;
             c.cost = cost_of(tiles, c.splits, c.kb, pairs, c.nt, 4.0 * parts * p * in_s * out_s);
             if (c.cost < best.cost) best = c;
         }
@@ -1750,6 +1891,7 @@ Cut cut_dw(int64_t n, int p, int parts, int in_s, int out_s, int pairs) {
 // columns of several narrow slices (8 slices of 14 -> 23 columns: a third of the time).
 struct Plan {
     int p = 1, in_s = 1, out_s = 1, merge = 1;   // slices and their columns as the products see them
+    bool digits = false;    // of the product that gives da and dc: those of fp32
     bool rows = false, little = false, pack_x = false, pack_w = false, pack_g = false, dz = false;
     int x_planes = 1, w_planes = 1, z_planes = 1;
     int in_pad = 0, out_pad = 0, parts = 1, sum_chunks = 1;
@@ -1782,19 +1924,21 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
         return;
     }
     const bool dz = back && (d->act != SLICEGCN_ACT_NONE || d->W2), gated = d->W2 != nullptr;
-    const int pairs = pairs_of(q.x_planes, q.w_planes), dx_pairs = pairs_of(q.z_planes, q.w_planes), dw_pairs = pairs_of(q.z_planes, q.x_planes);
+    const int pairs = pairs_of(q.x_planes, q.w_planes);
     double least = 1e300;
+    const int dx_pairs = pairs_of(q.z_planes, q.w_planes), dw_pairs = pairs_of(q.z_planes, q.x_planes);
     for (int m = 1; m <= d->num_slices; ++m) {
         const int64_t ins = (int64_t)m * d->in_s, outs = (int64_t)m * d->out_s;
         if (d->num_slices % m || (m > 1 && (ins > 2048 || outs > 8192))) continue;
         const int p = d->num_slices / m;
+        const bool digits = f32 || (back && (q.z_planes == 3 || ceil_div(ins, 64) > kLongSteps));
         Cut c[3];
-        if (!back || dz) c[0] = cut_rows(n, p, (int)outs, gated, ceil_div(ins, 64), pairs);
-        if (back) c[1] = cut_rows(n, p, (int)ins, false, q.parts * ceil_div(outs, 64), dx_pairs), c[2] = cut_dw(n, p, q.parts, (int)ins, (int)outs, dw_pairs);
+        if (!back || dz) c[0] = cut_rows(n, p, (int)outs, gated, ceil_div(ins, 64), pairs, !digits ? 0 : f32 || q.z_planes == 3 ? chunk_of(pairs) : kChunkBiases);
+        if (back) c[1] = cut_rows(n, p, (int)ins, false, q.parts * ceil_div(outs, 64), dx_pairs, dx_pairs > 1 ? chunk_of(dx_pairs) : 0), c[2] = cut_dw(n, p, q.parts, (int)ins, (int)outs, dw_pairs);
         double cost = (!back || dz ? c[0].cost : 0.0) + (back ? c[1].cost + c[2].cost : 0.0);
         if (m > 1) cost += 0.1 * cost + 4000 + (double)q.parts * p * ins * outs * (f32 ? 10 : 4) / 3400;            // weights are laid out anew; the model's margin
         if (!f32 && unaligned(x, d->x_ld, p, (int)ins)) cost += 4000 + (double)n * p * ins * 6 / 3400;              // x is, or needs not to be
-        if (cost < least) least = cost, q.merge = m, q.p = p, q.in_s = (int)ins, q.out_s = (int)outs, q.product = c[0], q.dx = c[1], q.dw = c[2];
+        if (cost < least) least = cost, q.merge = m, q.p = p, q.in_s = (int)ins, q.out_s = (int)outs, q.digits = digits, q.product = c[0], q.dx = c[1], q.dw = c[2];
     }
     q.in_pad = (int)up(q.in_s, 8);
     q.out_pad = (int)up(q.out_s, 8);
@@ -1838,7 +1982,7 @@ void plan(const slicegcn_ffn_desc* d, const void* x, const void* dout, Plan& q) 
     }
     if (back) {
         if (q.dz || q.pack_g) q.z_at = take(2 * q.z_planes * n * q.parts * p * q.out_pad);
-        if (q.dz && !f32 && q.z_planes == 1) q.product.fixed = fixed_pairs(q.product, p);
+        if (q.dz && !q.digits) q.product.fixed = fixed_pairs(q.product, p);
         q.sum_rows = !q.dz ? n : !q.product.fixed ? ceil_div(n, 32) : q.product.fixed / (p * q.product.tiles_n) * (q.product.nt == 64 ? 16 : 8);
         if (q.dz) q.sums_at = take(4 * q.sum_rows * cols);
         const int64_t rows = q.sum_rows;
@@ -1897,14 +2041,6 @@ slicegcn_status_t run_packs(const PackArgs& args, cudaStream_t st) {
     int ctas = 0;
     for (int k = 0; k < args.count; ++k) ctas += args.job[k].ctas;
     return ctas ? launch_after(ffn_pack_kernel, dim3(ctas), 256, 0, st, args) : SLICEGCN_OK;
-}
-
-// Products of operand parts, the smallest first.
-void set_pairs(Params& P, int pa, int pb) {
-    P.pairs = 0;
-    for (int order = 2; order >= 0; --order)
-        for (int i = std::min(order, pa - 1); i >= 0; --i)
-            if (order - i < pb) P.ia[P.pairs] = (int8_t)i, P.ib[P.pairs] = (int8_t)(order - i), ++P.pairs;
 }
 
 // A kernel's limit of dynamic shared memory, a constant of the kernel, set at its first launch on each device (a call costs a
@@ -1980,14 +2116,14 @@ void operands(const slicegcn_ffn_desc* d, const Plan& q, const void* x, char* ws
 slicegcn_status_t forward_product(Params& P, FinishArgs& F, const slicegcn_ffn_desc* d, const Plan& q, const Operand& ox, const Operand (&ow)[2], char* ws, bool back,
                                   cudaStream_t st) {
     const bool gated = d->W2 != nullptr, split = q.product.splits > 1;
-    const bool promo = d->dtype == SLICEGCN_F32 || (back && d->grad_dtype == SLICEGCN_F32) || split;
+    const bool promo = q.digits || split;
     P.n = (int)d->n, P.p = q.p, P.slices = split ? q.parts * q.p : q.p, P.cols = q.out_s;
     SGCN_TRY(set_cut(P, q.product, false));
     SGCN_TRY(make_map(&P.a, ox, 128));
     SGCN_TRY(make_map(&P.b0, ow[0], 64));
     SGCN_TRY(make_map(&P.b1, ow[1], 64));
     P.kb_part = (int)ceil_div(q.in_s, 64), P.k_part = q.in_s;
-    set_pairs(P, q.x_planes, q.w_planes);
+    P.a_planes = q.x_planes, P.b_planes = q.w_planes;
     P.scale = (float)d->scale, P.b = d->b, P.b2 = d->b2;
     P.bias_vec = q.out_s % 2 == 0 && (uintptr_t)d->b % 8 == 0 && (uintptr_t)d->b2 % 8 == 0;
     if (split) {
@@ -2006,21 +2142,22 @@ slicegcn_status_t forward_product(Params& P, FinishArgs& F, const slicegcn_ffn_d
     return promo ? launch<kFwd, true>(P, d->act, st) : launch<kFwd, false>(P, d->act, st);
 }
 
-// 16 bytes at a time of bf16, 8 of fp32 (as the epilogue reads and writes them)
-bool wide_access(const void* p, int64_t ld, int elem, int groups, int width) {
-    const int unit = elem == 2 ? 16 : 8;
+// `unit` bytes at a time are aligned, in every row and slice.
+bool wide_access(const void* p, int64_t ld, int elem, int groups, int width, int unit = 16) {
     return (uintptr_t)p % unit == 0 && ld * elem % unit == 0 && (groups == 1 || width * elem % unit == 0);
 }
-// Where a product's result goes: bf16 by tensor copies, where they can reach it.
+// Where a product's result goes: by tensor copies, where they can reach it.
 slicegcn_status_t set_result(Params& P, FinishArgs& F, void* out, int64_t ld, int elem, int groups, int width, int64_t rows) {
     P.out = F.out = out, P.out_ld = (int)ld, F.out_ld = ld, P.out_bf16 = F.out_bf16 = elem == 2, P.out_vec = wide_access(out, ld, elem, groups, width);
-    if (elem != 2 || !P.out_vec) return SLICEGCN_OK;
+    P.out_pairs = wide_access(out, ld, elem, groups, width, 8);
+    if (!P.out_vec) return SLICEGCN_OK;
     Operand o;
-    o.base = out, o.rows = rows, o.ld = ld, o.group_stride = width, o.width = width, o.groups = groups;
-    return make_map(&P.o, o, 32, true);
+    o.base = out, o.rows = rows, o.ld = ld, o.group_stride = width, o.width = width, o.groups = groups, o.f32 = elem == 4;
+    return make_map(&P.o, o, elem == 4 ? 16 : 32, true);
 }
 void set_input(Params& P, FinishArgs& F, const void* in, int64_t ld, int elem, int groups, int width) {
-    P.in = F.in = in, P.in_ld = (int)ld, F.in_ld = ld, F.in_bf16 = elem == 2, P.in_vec = in && wide_access(in, ld, elem, groups, width);
+    P.in = F.in = in, P.in_ld = (int)ld, F.in_ld = ld, P.in_bf16 = F.in_bf16 = elem == 2, P.in_vec = in && wide_access(in, ld, elem, groups, width);
+    P.in_pairs = in && wide_access(in, ld, elem, groups, width, 8);
 }
 
 template <int R, bool GATED, bool BF16, bool VEC>
@@ -2171,7 +2308,8 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         oz.width = q.out_s, oz.groups = q.parts * p, oz.planes = q.z_planes;
         F.dz = reinterpret_cast<__nv_bfloat16*>(ws + q.z_at);
         F.dz_plane = oz.plane_stride, F.dz_row = (int)oz.ld, F.dz_pad = q.out_pad, F.dz_planes = q.z_planes;
-        SGCN_TRY(make_map(&P.o, oz, q.z_planes == 1 ? 32 : 16, true));
+        P.dz = F.dz, P.dz_plane = F.dz_plane, P.dz_row = F.dz_row, P.dz_pad = F.dz_pad, P.planes = q.z_planes;
+        SGCN_TRY(make_map(&P.o, oz, q.digits ? 16 : 32, true));
         SGCN_TRY(forward_product(P, F, d, q, ox, ow, ws, true, st));
     }
     if (dx) {
@@ -2184,12 +2322,12 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         SGCN_TRY(make_map(&P.b0, ow[0], P.nt));
         SGCN_TRY(make_map(&P.b1, ow[1], P.nt));
         P.kb_part = (int)ceil_div(q.out_s, 64), P.k_part = q.out_s;
-        set_pairs(P, q.z_planes, q.w_planes);
+        P.a_planes = q.z_planes, P.b_planes = q.w_planes;
         P.scale = scale;
         SGCN_TRY(set_result(P, F, dx, d->dx_ld, ge, p, q.in_s, n));
         const bool split = P.splits > 1;
         if (split) P.partial = reinterpret_cast<float*>(ws + q.partial_at);
-        SGCN_TRY((P.pairs > 1 || split ? launch_as<kDx, true, SLICEGCN_ACT_NONE>(P, st) : launch_as<kDx, false, SLICEGCN_ACT_NONE>(P, st)));
+        SGCN_TRY((P.a_planes > 1 || split ? launch_as<kDx, true, SLICEGCN_ACT_NONE>(P, st) : launch_as<kDx, false, SLICEGCN_ACT_NONE>(P, st)));
         if (split) {
             F.partial = P.partial, F.splits = P.splits, F.n = P.n, F.p = p, F.cols = P.cols, F.act = SLICEGCN_ACT_NONE, F.scale = scale;
             SGCN_TRY(launch_after(ffn_finish_kernel, dim3((unsigned)(ceil_div(P.cols, 32) * p), (unsigned)ceil_div(n, 32)), 256, 0, st, F));
@@ -2206,7 +2344,7 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         SGCN_TRY(make_map(&P.a, P.swapped ? ox : oz, 64));
         SGCN_TRY(make_map(&P.b0, P.swapped ? oz : ox, 64));
         P.b1 = P.b0;
-        set_pairs(P, P.swapped ? q.x_planes : q.z_planes, P.swapped ? q.z_planes : q.x_planes);
+        P.a_planes = P.swapped ? q.x_planes : q.z_planes, P.b_planes = P.swapped ? q.z_planes : q.x_planes;
         P.scale = scale, P.out_bf16 = ge == 2;
         const bool join = P.splits > 1 || q.merge > 1;
         if (join) P.partial = reinterpret_cast<float*>(ws + q.partial_at);

@@ -2,9 +2,9 @@
 
 Tolerances.  With K terms of a sum the error is bounded against the sum of magnitudes, not the result: by S below, the
 definition with |x|, |W|, |b| and the activation's largest slope.  fp32: operands are exact sums of three parts, products of
-parts beyond the 24th bit are left out (2^-24 each, three of them at most 2^-22 in all), and the tensor cores' and registers' additions cut
-off up to 2^-23 of the running sum each: 16 of them per chunk of 256 (six products: the five small ones lie 2^-7 down), plus one per chunk, so
-(16 + 8 + K / 256) 2^-23 S covers them; activations add 8 * 2^-24.  bf16: products are exact, additions as above without chunks
+parts beyond the 24th bit are left out (2^-24 each, three of them at most 2^-22 in all), and the tensor cores' additions cut off up to
+2^-23 of the running sum each: 20 of them at its full size per chunk of 128 (six products: the five small ones lie 2^-7 down), and half as
+much for each of the K / 128 additions in registers, so (16 + 8 + K / 256) 2^-23 S covers them; activations add 8 * 2^-24.  bf16: products are exact, additions as above without chunks
 (K / 16) 2^-23 S, and results are rounded once, half a step or 2^-8 of the value at most.
 Gradients in bf16 round da and dc first: another 2^-8 of the sum of magnitudes.
 """
@@ -242,3 +242,30 @@ def test_little_work(shape, dtype):
     for gated, act, pad, residual in ((False, "silu", 1, True), (True, "gelu", 4, False), (False, "none", 0, False), (True, "relu", 3, True)):
         q = Problem(*shape, gated, act, dtype, pad=pad, residual=residual, offset=pad)
         q.check_forward(q.forward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pad,offset", [(0, 0), (4, 4), (2, 2), (1, 0), (8, 8), (4, 2)], ids=str)
+@pytest.mark.parametrize("shape,types", [((700, 1, 300, 132), ("fp32", "fp32")), ((333, 2, 260, 96), ("fp32", "fp32")), ((260, 3, 150, 70), ("fp32", "fp32")),
+                                         ((700, 1, 900, 136), ("bf16", "bf16")), ((300, 1, 1000, 131), ("bf16", "fp32"))], ids=str)
+def test_layouts_of_sums_emptied_into_registers(shape, types, pad, offset):
+    """r, dout and results by 16, 8 and single elements at a time."""
+    for gated, act, residual in ((False, "gelu", True), (True, "silu", False), (True, "relu", True)):
+        q = Problem(*shape, gated, act, types[0], grad=types[1], pad=pad, residual=residual, offset=offset)
+        q.check_forward(q.forward())
+        q.check_backward(q.backward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ins", [1024, 4096])
+def test_biases_gradients_of_long_sums(ins):
+    """Additions cut in one direction, so that a sum over rows keeps a relative error that stays what an element's is.  512 k are 32
+    additions that cut half of 2^-23 of a running sum that grows to the whole: 32 * 2^-24 / 2 = 2^-20 on average; twice that is allowed."""
+    import torch
+    q = Problem(300, 1, ins, 64, True, "silu", "bf16")
+    got = q.backward(("db", "db2"))
+    x, a, _, c, _ = q._pre()
+    y, dy = act64("silu", a)
+    g = q.dout.double()[None] * q.scale
+    for name, want in (("db", (g * dy * c).sum(1)), ("db2", (g * y).sum(1))):
+        assert float((got[name].double() - want).norm() / want.norm()) < 2.0 ** -19
