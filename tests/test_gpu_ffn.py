@@ -269,3 +269,14 @@ def test_biases_gradients_of_long_sums(ins):
     g = q.dout.double()[None] * q.scale
     for name, want in (("db", (g * dy * c).sum(1)), ("db2", (g * y).sum(1))):
         assert float((got[name].double() - want).norm() / want.norm()) < 2.0 ** -19
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 31, 33, 512, 513])
+@pytest.mark.parametrize("types", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32")], ids=str)
+def test_biases_gradients_of_few_rows(n, types):
+    for p, gated in ((1, True), (3, False)):
+        q = Problem(n, p, 72, 200, gated, "gelu", types[0], grad=types[1])
+        q.check_backward(q.backward())
+        for want in (("db",), ("dW", "db"), ("dx",)):
+            q.check_backward(q.backward(want))
