@@ -77,6 +77,7 @@ struct Params {
     void* out;
     int out_ld;
     int out_bf16, out_vec, out_pairs;   // vec: tensor copies reach it; pairs: 8 bytes at a time are aligned
+    int out_edge;                  // columns from here on are stored one by one: a tensor copy writes whole 16 bytes
     __nv_bfloat16* dz;             // kDz, emptied into registers: da and dc, planes, strides of a row and a slice
     int64_t dz_plane;
     int planes, dz_row, dz_pad;
@@ -148,7 +149,7 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar) & 0xFEFFFFFFu)
         : "memory");
 }
-// One box of shared memory to a tensor map; what lies outside the tensor is left out.  Groups of them are waited for by the lane that
+// One box of shared memory to a tensor map; what lies outside the tensor is left out, but a row's end only from the next 16 bytes on.  Groups of them are waited for by the lane that
 // issued them; a turn without a box commits its (empty) group too, since the waits count groups.
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int x, int y, int z, int w) {
     asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map), "r"(src),
@@ -952,7 +953,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                             if (MODE != kDx) forward_as<ACT, kGated, true>(a, c);
 #pragma unroll
                             for (int j = 0; j < 16; ++j) a[j] = with_in ? fmaf(a[j], P.scale, in[j]) : a[j] * P.scale;
-                            if (P.out_vec) {
+                            if (P.out_vec && col < P.out_edge) {
                                 if (lane == 0) stores_read<1>();   // of the same half before
                                 __syncwarp();
 #pragma unroll
@@ -1053,7 +1054,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     proxy_fence();
                     __syncwarp();
                     const bool there = col < P.cols && w.rows > 0;
-                    if (kIsDz || P.out_vec) {
+                    if (kIsDz || (P.out_vec && col < P.out_edge)) {
                         if (lane == 0) {
                             if (there) {
                                 tma_store(&P.o, to, col, w.row, w.slice, 0);
@@ -1061,8 +1062,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                             }
                             stores_commit();
                         }
-                    } else if (there) {
-                        slab_out(static_cast<__nv_bfloat16*>(P.out) + (int64_t)w.row * P.out_ld + (w.slice * P.cols + col), P.out_ld, w.rows, P.cols - col, to, lane);
+                    } else {
+                        if (lane == 0) stores_commit();
+                        if (there) slab_out(static_cast<__nv_bfloat16*>(P.out) + (int64_t)w.row * P.out_ld + (w.slice * P.cols + col), P.out_ld, w.rows, P.cols - col, to, lane);
                     }
                     if (kIsDz && P.sums && !P.fixed && there) {
                         sums_out(P, w.row >> 5, w.slice, col, u == 0 ? s : s2, lane);
@@ -2153,6 +2155,7 @@ bool wide_access(const void* p, int64_t ld, int elem, int groups, int width, int
 slicegcn_status_t set_result(Params& P, FinishArgs& F, void* out, int64_t ld, int elem, int groups, int width, int64_t rows) {
     P.out = F.out = out, P.out_ld = (int)ld, F.out_ld = ld, P.out_bf16 = F.out_bf16 = elem == 2, P.out_vec = wide_access(out, ld, elem, groups, width);
     P.out_pairs = wide_access(out, ld, elem, groups, width, 8);
+    P.out_edge = width * elem % 16 ? width / 32 * 32 : width;
     if (!P.out_vec) return SLICEGCN_OK;
     Operand o;
     o.base = out, o.rows = rows, o.ld = ld, o.group_stride = width, o.width = width, o.groups = groups, o.f32 = elem == 4;

@@ -233,6 +233,34 @@ def test_offsets_past_32_bits():
     assert float((dW2[0].double() - total).norm() / total.norm()) <= 2 * 2.0 ** -8
 
 
+@pytest.mark.parametrize("types", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32")], ids=str)
+@pytest.mark.parametrize("shape", [(3001, 1, 300, 132), (2500, 2, 1000, 76), (700, 1, 64, 40)], ids=str)
+def test_neighbours_of_aligned_rows_keep_their_values(shape, types):
+    """The same where rows start on 16 bytes, widths do not end there, and results leave by tensor copies."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    n, p, ins, outs = shape
+    t, gt = (torch.bfloat16 if k == "bf16" else torch.float32 for k in types)
+    code = lambda k: B.BF16 if k == torch.bfloat16 else B.F32   # noqa: E731
+    wide = lambda cols: (cols + 7) // 8 * 8 + 16   # noqa: E731
+    W, W2 = (torch.randn((p, ins, outs), device="cuda").to(t) for _ in range(2))
+    x, g = torch.randn((n, wide(p * ins)), device="cuda").to(t), torch.randn((n, wide(p * outs)), device="cuda").to(gt)
+    x[:, p * ins:], g[:, p * outs:] = float("nan"), float("nan")
+    out, dx = torch.full((n + 2, wide(p * outs)), 9.0, device="cuda", dtype=t), torch.full((n + 2, wide(p * ins)), 9.0, device="cuda", dtype=gt)
+    r = torch.full((n, wide(p * outs)), float("nan"), device="cuda", dtype=t)
+    r[:, :p * outs] = 1.0
+    d = B.make_ffn_desc(n, p, ins, outs, W, W2, act=B.ACT_SILU, dtype=code(t), grad_dtype=code(gt), x_ld=x.stride(0), r_ld=r.stride(0), out_ld=out.stride(0),
+                        dout_ld=g.stride(0), dx_ld=dx.stride(0))
+    need = max(B.slicegcn_ffn_workspace_bytes(d, x), B.slicegcn_ffn_workspace_bytes(d, x, g))
+    ws = torch.full((need + 256,), 9, device="cuda", dtype=torch.uint8)
+    dW, dW2 = (torch.empty((p, ins, outs), device="cuda", dtype=gt) for _ in range(2))
+    B.slicegcn_ffn_forward(d, x, r, out, None, ws, need)
+    B.slicegcn_ffn_backward(d, x, g, dx, dW, dW2, None, None, None, ws, need)
+    for m, cols in ((out, p * outs), (dx, p * ins)):
+        assert bool((m[n:] == 9).all()) and bool((m[:, cols:] == 9).all()) and bool(torch.isfinite(m[:n, :cols]).all())
+    assert bool(torch.isfinite(dW).all()) and bool(torch.isfinite(dW2).all()) and bool((ws[need:] == 9).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_rows_with_infinities_and_nan_stay_in_their_rows(dtype):
     import torch
