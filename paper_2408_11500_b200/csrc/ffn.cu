@@ -2129,7 +2129,9 @@ slicegcn_status_t forward_product(Params& P, FinishArgs& F, const slicegcn_ffn_d
     SGCN_TRY(make_map(&P.b1, ow[1], 64));
     P.kb_part = (int)ceil_div(q.in_s, 64), P.k_part = q.in_s;
     P.a_planes = q.x_planes, P.b_planes = q.w_planes;
-    P.scale = (float)d->scale, P.b = d->b, P.b2 = d->b2;
+    P.scale = (float)d->scale;
+    // a product in pieces has the second projection's columns as slices of their own, which no array of biases has: they are the finishing kernel's
+    if (!split) P.b = d->b, P.b2 = d->b2;
     P.bias_vec = q.out_s % 2 == 0 && (uintptr_t)d->b % 8 == 0 && (uintptr_t)d->b2 % 8 == 0;
     if (split) {
         P.partial = reinterpret_cast<float*>(ws + q.partial_at);
