@@ -9,7 +9,7 @@
 //     single CTAs with the same tile would copy 48 KB, and shared memory would pace the MMA.
 //   * Both operands come by tensor copy from where they lie, whichever of their axes is contiguous (x and dW's operands along
 //     rows, W along columns): nothing is transposed.  Odd strides, and fp32, are laid out in the workspace first.
-//   * fp32 values are three bf16 numbers (8 bits of the significand each), and a product of two of them is the six products
+//   * fp32 values are three bf16 numbers (8 bits of the significand each, all 24 from 2^-110 up), and a product of two of them is the six products
 //     of parts that reach fp32's last digit, the small ones first, each tile of parts copied once.  A sixth of the bf16 rate.
 //   * Tensor memory's accumulation cuts digits off; over k in the hundreds of 16-wide steps that would show in fp32.  There the
 //     accumulator is emptied into registers every few steps ("chunk"), and the registers are added to with rounding.
@@ -529,8 +529,10 @@ __device__ __forceinline__ void backward_as(float scale, const float (&g)[N], fl
     }
 }
 
-// Parts of an fp32 number whose sum it is: 8 bits each.  Cut, not rounded: no part leaves the range, and each is exact.  Takes the
-// next part off x (off an infinity or a NaN: NaN is left).
+// Parts of an fp32 number: 8 bits each, cut, not rounded, so that none leaves the range at its upper end.  From 2^-110 up their sum is
+// the number; below that the third part's last bits fall under bf16's least number, 2^-133, and are left out.  (A power of two in front
+// of tiny operands would need their largest magnitude first, a pass over them.)  Takes the next part off x (off an infinity or a NaN:
+// NaN is left).
 __device__ __forceinline__ uint32_t next_part(float& x) {
     const uint32_t part = __float_as_uint(x) & 0xffff0000u;
     x -= __uint_as_float(part);

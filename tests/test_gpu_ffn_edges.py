@@ -1,0 +1,67 @@
+"""Feed-forward projections at the edges of their number ranges: tiny and large fp32 numbers in the form that the tensor cores take."""
+import pytest
+
+from test_gpu_ffn import U32
+
+pytestmark = pytest.mark.gpu
+
+LOST = 2.0 ** -133     # what the three bf16 parts of an fp32 number leave out at most: the last bit of the least of them
+
+
+def _adds(k):
+    """Relative error of a sum of k fp32 products against the sum of magnitudes, as `test_gpu_ffn.py` derives it."""
+    return (24 + k / 256) * 2 * U32
+
+
+def _ranged(n, cols, lo, hi, seed):
+    """Rows of normal numbers times powers of two from 2^lo to 2^hi."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(seed)
+    scale = torch.linspace(lo, hi, n, device="cuda", dtype=torch.float64).round().exp2()
+    return (torch.randn((n, cols), generator=g, device="cuda", dtype=torch.float64) * scale[:, None]).float()
+
+
+def test_fp32_numbers_of_every_magnitude_in_three_parts():
+    """Rows from 2^-120 (and single numbers below the normal ones) to 2^90; the weights are large enough for the products to be normal.
+    A number keeps its 24 bits from 2^-110 up; below that what it loses is less than 2^-133."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    n, ins, outs = 3000, 512, 256
+    g = torch.Generator("cuda").manual_seed(1)
+    x, dout = _ranged(n, ins, -120, 90, 2), _ranged(n, outs, -120, 90, 3)
+    W = torch.randn((1, ins, outs), generator=g, device="cuda") * 2.0 ** 16
+    out, dx = torch.empty((n, outs), device="cuda"), torch.empty((n, ins), device="cuda")
+    d = B.make_ffn_desc(n, 1, ins, outs, W)
+    need = B.slicegcn_ffn_workspace_bytes(d, x)
+    assert need >= 6 * n * ins                       # parts of x are laid out: this is no plain product
+    ws = torch.empty(max(need, B.slicegcn_ffn_workspace_bytes(d, x, dout)), dtype=torch.uint8, device="cuda")
+    B.slicegcn_ffn_forward(d, x, None, out, None, ws, ws.numel())
+    B.slicegcn_ffn_backward(d, x, dout, dx, None, None, None, None, None, ws, ws.numel())
+    w = W[0].double()
+    for got, a, b in ((out, x.double(), w), (dx, dout.double(), w.t())):
+        want, mag, lost = a @ b, a.abs() @ b.abs(), LOST * b.abs().sum(0)
+        bound = (_adds(a.shape[1]) + 2 * U32) * mag + lost
+        off = (got.double() - want).abs()
+        assert bool((off <= bound).all()), float((off / bound).max())
+
+
+def test_tiny_gradients_in_three_parts():
+    """da and dc of rows from 2^-120 to 2^60 on their way through memory, gated without an activation: da = g c, dc = g a."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    n, ins, outs = 2000, 256, 320
+    g = torch.Generator("cuda").manual_seed(4)
+    x, dout = torch.randn((n, ins), generator=g, device="cuda"), _ranged(n, outs, -120, 60, 5)
+    W, W2 = (torch.randn((1, ins, outs), generator=g, device="cuda") * 16 for _ in range(2))
+    dx = torch.empty((n, ins), device="cuda")
+    d = B.make_ffn_desc(n, 1, ins, outs, W, W2)
+    ws = torch.empty(B.slicegcn_ffn_workspace_bytes(d, x, dout), dtype=torch.uint8, device="cuda")
+    B.slicegcn_ffn_backward(d, x, dout, dx, None, None, None, None, None, ws, ws.numel())
+    X, G, w, w2 = x.double(), dout.double(), W[0].double(), W2[0].double()
+    want, bound = 0.0, 0.0
+    for here, other in ((w, w2), (w2, w)):
+        z, s = G * (X @ other), G.abs() * (X.abs() @ other.abs())
+        want = want + z @ here.t()
+        bound = bound + ((_adds(ins) + 4 * U32) * s + LOST) @ here.abs().t() + (_adds(2 * outs) + 2 * U32) * (z.abs() @ here.abs().t())
+    off = (dx.double() - want).abs()
+    assert bool((off <= bound).all()), float((off / bound).max())
