@@ -520,8 +520,9 @@ slicegcn_status_t slicegcn_clip_grads(const slicegcn_tensor_list* list, double m
  * and activations are computed from the stored values with fp32's digits and rounded once, as out; sums whose only results are bf16
  * keep 2^-28 of relative accuracy per column added, at worst (2^-16 at 4,096).  Elements of fp32 keep their 24 bits from 2^-110 up; of
  * smaller ones, what lies below 2^-133 may be left out.  An infinite or NaN element of x, W or dout
- * leaves no finite results where it enters (infinities may become NaN there); one of x or dout may do the same in the other slices
- * of its row (narrow slices are computed together), and so in what is summed over rows.  Other rows of out and dx are not touched.
+ * leaves no finite results where it enters (infinities may become NaN there; RELU's value below and its slope are finite at an
+ * infinity, and NaN at NaN); one of x or dout may do the same in the other slices of its row (narrow slices are computed together),
+ * and so in what is summed over rows.  Other rows of out and dx are not touched.
  */
 enum { SLICEGCN_ACT_NONE = 0, SLICEGCN_ACT_RELU = 1, SLICEGCN_ACT_SILU = 2, SLICEGCN_ACT_GELU = 3 };
 #define SLICEGCN_MAX_FFN_WIDTH 65536

@@ -453,6 +453,7 @@ __device__ __forceinline__ void gates_of(float a0, float a1, float s0, float s1,
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(q1));
 }
 __device__ __forceinline__ float relu(float a) { return a > 0.f || isnan(a) ? a : 0.f; }
+__device__ __forceinline__ float relu_slope(float a) { return a > 0.f ? 1.f : isnan(a) ? a : 0.f; }   // a NaN stays one
 // a -> act(a) [* c]
 template <int ACT, bool GATED, bool ACCURATE, int N>
 __device__ __forceinline__ void forward_as(float (&a)[N], const float (&c)[N]) {
@@ -491,7 +492,7 @@ __device__ __forceinline__ void backward_as(float scale, const float (&g)[N], fl
                 y *= q;
                 dy = fmaf(y * (1.f - q), ACT == SLICEGCN_ACT_GELU ? 2.f * kGeluA * fmaf(3.f * kGeluB, a[k] * a[k], 1.f) : 1.f, q);
             }
-            if (ACT == SLICEGCN_ACT_RELU) y = relu(a[k]), dy = a[k] > 0.f ? 1.f : 0.f;
+            if (ACT == SLICEGCN_ACT_RELU) y = relu(a[k]), dy = relu_slope(a[k]);
             const float gk = g[k] * scale;
             a[k] = GATED ? gk * c[k] * dy : gk * dy;
             if (GATED) c[k] = gk * y;
@@ -516,7 +517,7 @@ __device__ __forceinline__ void backward_as(float scale, const float (&g)[N], fl
             }
             if (ACT == SLICEGCN_ACT_RELU) {
                 y0 = relu(a[k]), y1 = relu(a[k + 1]);
-                d0 = a[k] > 0.f ? 1.f : 0.f, d1 = a[k + 1] > 0.f ? 1.f : 0.f;
+                d0 = relu_slope(a[k]), d1 = relu_slope(a[k + 1]);
             }
             a[k] = g0, a[k + 1] = g1;
             if (GATED) mul2(a[k], a[k + 1], c[k], c[k + 1]);

@@ -1,7 +1,8 @@
-"""Feed-forward projections at the edges of their number ranges: tiny and large fp32 numbers in the form that the tensor cores take."""
+"""Feed-forward projections at the edges of their number ranges: tiny and large fp32 numbers in the form that the tensor cores
+take, NaN before an activation."""
 import pytest
 
-from test_gpu_ffn import U32
+from test_gpu_ffn import U32, Problem
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +66,24 @@ def test_tiny_gradients_in_three_parts():
         bound = bound + ((_adds(ins) + 4 * U32) * s + LOST) @ here.abs().t() + (_adds(2 * outs) + 2 * U32) * (z.abs() @ here.abs().t())
     off = (dx.double() - want).abs()
     assert bool((off <= bound).all()), float((off / bound).max())
+
+
+#: rows, columns: tiles; pieces of k and the kernel that ends them
+GRAD_PATHS = [(600, 64), (16, 2048), (300, 1024)]
+TYPES = [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32")]
+
+
+@pytest.mark.parametrize("types", TYPES, ids=str)
+@pytest.mark.parametrize("n,ins", GRAD_PATHS, ids=str)
+@pytest.mark.parametrize("gated", [False, True], ids=["plain", "gated"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_nan_before_an_activation_leaves_no_finite_gradient(act, gated, n, ins, types):
+    """Of its row in dx, and of the biases' and weights' sums that it enters; other rows keep theirs."""
+    import torch
+    q = Problem(n, 1, ins, 72, gated, act, types[0], grad=types[1])
+    clean = q.backward()["dx"].clone()
+    q.x[4, 7] = float("nan")
+    got = q.backward()
+    keep = torch.arange(n, device="cuda") != 4
+    assert torch.equal(got["dx"][keep], clean[keep])
+    assert bool(torch.isnan(got["dx"][4]).all()) and bool(torch.isnan(got["db"]).all()) and bool(torch.isnan(got["dW"]).all())
