@@ -479,7 +479,9 @@ __device__ __forceinline__ void forward_as(float (&a)[N], const float (&c)[N]) {
         }
     }
 }
-// a, c -> da, dc:  SILU' = q + y (1 - q),  GELU' = q + y (1 - q) 2 A (1 + 3 B a^2)  with the gate q and y = a q
+// a, c -> da, dc:  SILU' = q + y (1 - q),  GELU' = q + y (1 - q) 2 A (1 + 3 B a^2)  with the gate q and y = a q.  Far from zero
+// y (1 - q) is 0, and a^2 is kept from infinity, since 0 times that is none.
+constexpr float kGeluFar = 1e30f;
 template <int ACT, bool GATED, bool ACCURATE, int N>
 __device__ __forceinline__ void backward_as(float scale, const float (&g)[N], float (&a)[N], float (&c)[N]) {
     constexpr bool kSmooth = ACT == SLICEGCN_ACT_SILU || ACT == SLICEGCN_ACT_GELU;
@@ -490,7 +492,7 @@ __device__ __forceinline__ void backward_as(float scale, const float (&g)[N], fl
             if (kSmooth) {
                 const float q = gate_of<ACT>(a[k]);
                 y *= q;
-                dy = fmaf(y * (1.f - q), ACT == SLICEGCN_ACT_GELU ? 2.f * kGeluA * fmaf(3.f * kGeluB, a[k] * a[k], 1.f) : 1.f, q);
+                dy = fmaf(y * (1.f - q), ACT == SLICEGCN_ACT_GELU ? 2.f * kGeluA * fmaf(3.f * kGeluB, fminf(a[k] * a[k], kGeluFar), 1.f) : 1.f, q);
             }
             if (ACT == SLICEGCN_ACT_RELU) y = relu(a[k]), dy = relu_slope(a[k]);
             const float gk = g[k] * scale;
@@ -510,6 +512,7 @@ __device__ __forceinline__ void backward_as(float scale, const float (&g)[N], fl
                 d0 = q0, d1 = q1;
                 fma2(d0, d1, -1.f, -1.f, 1.f, 1.f);
                 if (ACT == SLICEGCN_ACT_GELU) {
+                    s0 = fminf(s0, kGeluFar), s1 = fminf(s1, kGeluFar);
                     fma2(s0, s1, 6.f * kGeluA * kGeluB, 6.f * kGeluA * kGeluB, 2.f * kGeluA, 2.f * kGeluA);
                     mul2(d0, d1, s0, s1);
                 }

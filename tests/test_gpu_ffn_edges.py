@@ -1,8 +1,8 @@
 """Feed-forward projections at the edges of their number ranges: tiny and large fp32 numbers in the form that the tensor cores
-take, NaN before an activation."""
+take, derivatives far from zero, NaN before an activation."""
 import pytest
 
-from test_gpu_ffn import U32, Problem
+from test_gpu_ffn import U32, UBF, Problem
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +87,36 @@ def test_nan_before_an_activation_leaves_no_finite_gradient(act, gated, n, ins, 
     keep = torch.arange(n, device="cuda") != 4
     assert torch.equal(got["dx"][keep], clean[keep])
     assert bool(torch.isnan(got["dx"][4]).all()) and bool(torch.isnan(got["db"]).all()) and bool(torch.isnan(got["dW"]).all())
+
+
+@pytest.mark.parametrize("types", TYPES, ids=str)
+@pytest.mark.parametrize("n,ins", GRAD_PATHS, ids=str)
+@pytest.mark.parametrize("gated", [False, True], ids=["plain", "gated"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_derivatives_far_from_zero(act, gated, n, ins, types):
+    """W is the unit matrix in its first rows, so that x's first columns are the pre-activations: the derivative is 1 far above zero and
+    0 far below.  Everything is a power of two or a sum of two, so that results are exact."""
+    import torch
+    outs = 64
+    q = Problem(n, 1, ins, outs, gated, act, types[0], grad=types[1], scale=1.0, bias=False)
+    q.x.zero_(), q.W.zero_(), q.dout.fill_(0.5)
+    q.W[0, :outs] = torch.eye(outs, device="cuda", dtype=q.dt)
+    e = torch.arange(20, 20 + outs, device="cuda")                       # 2^20 .. 2^83; squares pass fp32's range from 2^64 on
+    sign = torch.where(torch.arange(n, device="cuda") % 2 == 0, 1.0, -1.0)[:, None]
+    q.x[:, :outs] = (sign * torch.exp2(e.double())).to(q.dt)
+    if gated:                                                            # c = 4 x_0 2^-20 = +-4
+        q.W2.zero_()
+        q.W2[0, 0] = 2.0 ** -18
+    got = q.backward(("dx",))["dx"].double()
+    c = 4.0 * sign.double() if gated else torch.ones_like(sign, dtype=torch.float64)
+    want = torch.zeros_like(got)
+    want[:, :outs] = 0.5 * c * (sign > 0)
+    if gated:                                                            # dc = g act(a), all of it to x_0
+        total = (0.5 * torch.exp2(e.double())).sum() * 2.0 ** -18
+        want[:, :1] += total * (sign > 0)
+        # the sum of 64 powers of two is rounded: additions as in every product, and dc's own roundings
+        slack = (_adds(outs) if q.dt == torch.float32 or q.gt == torch.float32 else (2 + outs / 16) * 2 * U32) + (2 * UBF if q.gt == torch.bfloat16 else 8 * U32)
+        off = (got[:, 0] - want[:, 0]).abs()
+        assert bool((off <= slack * want[:, 0].abs()).all())
+        got, want = got[:, 1:], want[:, 1:]
+    assert torch.equal(got, want), (got - want).abs().max()
