@@ -430,11 +430,13 @@ __device__ __forceinline__ int sum_column(int lane) {
 // SILU and GELU multiply a by a gate 1 / (1 + exp(-w)): w = a, or 2 u with (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)).
 constexpr float kLog2e = 1.4426950408889634f, kGeluA = 0.7978845608028654f, kGeluB = 0.044715f;
 template <int ACT>
-__device__ __forceinline__ float gate_of(float a) {
-    return __fdividef(1.f, 1.f + expf(ACT == SLICEGCN_ACT_SILU ? -a : -2.f * kGeluA * a * fmaf(kGeluB, a * a, 1.f)));   // 2 units of the last place each
+__device__ __forceinline__ float gate_of(float a) {   // by the exponential of -|w|, which passes no range's end: 1 / (1 + t) or t / (1 + t)
+    const float w = ACT == SLICEGCN_ACT_SILU ? a : 2.f * kGeluA * a * fmaf(kGeluB, a * a, 1.f);
+    const float t = expf(-fabsf(w)), r = __fdividef(1.f, 1.f + t);   // 2 units of the last place each
+    return w < 0.f ? t * r : r;
 }
 // Where results are rounded to bf16 the hardware's exponential and reciprocal (2^-22 each, and 2^-24 |w| of the argument) are exact
-// enough (one reciprocal for two numbers, 1/x = y/(xy), gained nothing).  Two numbers at a time; s = a^2.
+// enough (one reciprocal for two numbers, 1/x = y/(xy), gained nothing); a gate below 2^-126 is 0.  Two numbers at a time; s = a^2.
 template <int ACT>
 __device__ __forceinline__ void gates_of(float a0, float a1, float s0, float s1, float& q0, float& q1) {
     if (ACT == SLICEGCN_ACT_SILU) {

@@ -1,5 +1,7 @@
 """Feed-forward projections at the edges of their number ranges: tiny and large fp32 numbers in the form that the tensor cores
-take, derivatives far from zero, NaN before an activation."""
+take, activations and derivatives far from zero, NaN before an activation."""
+import math
+
 import pytest
 
 from test_gpu_ffn import U32, UBF, Problem
@@ -120,3 +122,30 @@ def test_derivatives_far_from_zero(act, gated, n, ins, types):
         assert bool((off <= slack * want[:, 0].abs()).all())
         got, want = got[:, 1:], want[:, 1:]
     assert torch.equal(got, want), (got - want).abs().max()
+
+
+#: rows, columns: a few rows; plain multiply-adds; tiles; pieces of k and the kernel that ends them
+PATHS = [(5, 64), (200, 25), (40_000, 400), (100, 4096)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,ins", PATHS, ids=str)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_activations_far_below_zero(act, n, ins, dtype):
+    """Where 1 + exp(-w) passes fp32's range the activation is still a normal number.  x is zero, so that the biases are the
+    pre-activations.  The exponential and the quotient are off by 2 units each; w by 4 of its own roundings.  Results of bf16 may take a
+    gate below 2^-126 for zero."""
+    import torch
+    outs = 256
+    q = Problem(n, 1, ins, outs, False, act, dtype, scale=1.0)
+    q.x.zero_()
+    q.b.copy_(torch.linspace(-100.0, -60.0, outs, device="cuda") if act == "silu" else torch.linspace(-11.0, -7.0, outs, device="cuda"))
+    a = q.b[0].double()
+    w = -a if act == "silu" else -2 * math.sqrt(2 / math.pi) * (a + 0.044715 * a ** 3)
+    want = a * torch.exp(-w) / (1 + torch.exp(-w))
+    got = q.forward().double()
+    bound = (16 + 4 * w.abs()) * U32 * want.abs() + 2 * a.abs() * 2.0 ** -149
+    if dtype == "bf16":
+        bound = bound + UBF * want.abs() + a.abs() * 2.0 ** -126
+    off = (got - want).abs()
+    assert bool((off <= bound).all()), float((off / bound).max())
