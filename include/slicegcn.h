@@ -557,7 +557,8 @@ slicegcn_status_t slicegcn_ffn_forward(const slicegcn_ffn_desc* d, const void* x
  * Outputs (OVERWRITTEN, each may be NULL to skip): dx [n x num_slices*in_s], dW, dW2 [num_slices x in_s x out_s] of
  * grad_dtype; db, db2 [num_slices x out_s] fp32.  dW2 and db2 only with W2.  No overlap.  Deterministic: sums over rows are
  * taken in a fixed order.  With grad_dtype BF16 the gradients w.r.t. a and c are rounded to bf16 once, as operands of the
- * products that give dx, dW and dW2 (db and db2 are summed before that); with F32 they keep fp32's digits.
+ * products that give dx, dW and dW2 (db and db2 are summed before that, from pre-activations that keep 2^-28 per column added, 2^-18.4
+ * at worst); with F32 they keep fp32's digits.
  * Errors: as slicegcn_ffn_forward. */
 slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* x, const void* dout, void* dx, void* dW,
                                         void* dW2, float* db, float* db2, int32_t* status, void* workspace,

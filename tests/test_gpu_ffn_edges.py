@@ -1,10 +1,10 @@
 """Feed-forward projections at the edges of their number ranges: tiny and large fp32 numbers in the form that the tensor cores
-take, activations and derivatives far from zero, NaN before an activation."""
+take, activations and derivatives far from zero, NaN before an activation, biases' gradients of middling sums."""
 import math
 
 import pytest
 
-from test_gpu_ffn import U32, UBF, Problem
+from test_gpu_ffn import U32, UBF, Problem, act64
 
 pytestmark = pytest.mark.gpu
 
@@ -149,3 +149,18 @@ def test_activations_far_below_zero(act, n, ins, dtype):
         bound = bound + UBF * want.abs() + a.abs() * 2.0 ** -126
     off = (got - want).abs()
     assert bool((off <= bound).all()), float((off / bound).max())
+
+
+@pytest.mark.parametrize("ins", [256, 320, 512, 768, 1024])
+def test_biases_gradients_of_middling_sums(ins):
+    """Biases' gradients are fp32 beside gradients of bf16 too.  An addition of 16 columns in tensor memory cuts half of 2^-23 of a running
+    sum that grows to the whole: ins / 16 * 2^-24 / 2 on average, up to 768 columns; longer sums are emptied every 512.  Twice that is
+    allowed."""
+    q = Problem(300, 1, ins, 64, True, "silu", "bf16")
+    got = q.backward(("db", "db2"))
+    x, a, _, c, _ = q._pre()
+    y, dy = act64("silu", a)
+    g = q.dout.double()[None] * q.scale
+    columns = ins if ins <= 768 else 512
+    for name, want in (("db", (g * dy * c).sum(1)), ("db2", (g * y).sum(1))):
+        assert float((got[name].double() - want).norm() / want.norm()) < columns / 16 * 2.0 ** -24, name
