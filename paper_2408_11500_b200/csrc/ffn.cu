@@ -78,9 +78,7 @@ struct Params {
     int out_ld;
     int out_bf16, out_vec, out_pairs;   // vec: tensor copies reach it; pairs: 8 bytes at a time are aligned
     int out_edge;                  // columns from here on are stored one by one: a tensor copy writes whole 16 bytes
-    __nv_bfloat16* dz;             // kDz, emptied into registers: da and dc, planes, strides of a row and a slice
-    int64_t dz_plane;
-    int planes, dz_row, dz_pad;
+    int planes;                    // kDz, emptied into registers: of da and dc
     int fixed;                     // every pair of SMs stays with one column tile
     // kDz: sums over 32 rows each, or (fixed) over all rows that an epilogue warp has seen
     float* sums;                   // [ceil(n/32) or epilogue warps per column tile][parts * p][cols], or NULL
@@ -2326,7 +2324,7 @@ slicegcn_status_t slicegcn_ffn_backward(const slicegcn_ffn_desc* d, const void* 
         oz.width = q.out_s, oz.groups = q.parts * p, oz.planes = q.z_planes;
         F.dz = reinterpret_cast<__nv_bfloat16*>(ws + q.z_at);
         F.dz_plane = oz.plane_stride, F.dz_row = (int)oz.ld, F.dz_pad = q.out_pad, F.dz_planes = q.z_planes;
-        P.dz = F.dz, P.dz_plane = F.dz_plane, P.dz_row = F.dz_row, P.dz_pad = F.dz_pad, P.planes = q.z_planes;
+        P.planes = q.z_planes;
         SGCN_TRY(make_map(&P.o, oz, q.digits ? 16 : 32, true));
         SGCN_TRY(forward_product(P, F, d, q, ox, ow, ws, true, st));
     }
