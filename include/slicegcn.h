@@ -409,8 +409,8 @@ slicegcn_status_t slicegcn_train_epochs_host(const slicegcn_model* m, const slic
  *   forward    out[i, 0:width] = scale * table[ids[i], 0:width]
  *   backward   dtable[v, 0:width] = sum over i with ids[i] = v of scale * dout[i, 0:width]
  * An id of -1 means "none": a row of zeros forward, no gradient.  Any other id outside [0, vocab) is treated the same way
- * and reported: *status [device, one int32, caller-owned, may be NULL] receives SLICEGCN_DEVSTATUS_BAD_ID (the word is
- * only ever set, never cleared).  Several fields side by side are several calls whose out / dout start at the field's
+ * and reported: *status [device, one int32, caller-owned, may be NULL] receives the bits of SLICEGCN_DEVSTATUS_BAD_ID (bits are
+ * only ever set, never cleared, so that one word can serve these calls and slicegcn_ffn_*).  Several fields side by side are several calls whose out / dout start at the field's
  * first column, with the leading dimension of the whole matrix.
  */
 enum { SLICEGCN_DEVSTATUS_BAD_ID = 33 };
@@ -527,7 +527,8 @@ slicegcn_status_t slicegcn_clip_grads(const slicegcn_tensor_list* list, double m
  */
 enum { SLICEGCN_ACT_NONE = 0, SLICEGCN_ACT_RELU = 1, SLICEGCN_ACT_SILU = 2, SLICEGCN_ACT_GELU = 3 };
 #define SLICEGCN_MAX_FFN_WIDTH 65536
-/* Bit of the status word that a bounded wait inside a kernel sets when it runs out (the outputs are then undefined). */
+/* Bit of the status word that a bounded wait inside a kernel sets when it runs out (the outputs are then undefined).  Other bits of the
+ * word stay as they are, so that SLICEGCN_DEVSTATUS_BAD_ID in the same word is still seen: status & WAIT, and the rest. */
 enum { SLICEGCN_DEVSTATUS_WAIT = 64 };
 typedef struct slicegcn_ffn_desc {
     int64_t n;                   /* rows, 0 .. 2^31 - 16385 */
@@ -547,7 +548,8 @@ typedef struct slicegcn_ffn_desc {
  * laid out in the workspace first. */
 slicegcn_status_t slicegcn_ffn_workspace_bytes(const slicegcn_ffn_desc* d, const void* x, const void* dout, int64_t* bytes);
 /* x [device, n x num_slices*in_s], r [device, n x num_slices*out_s] or NULL, out like r; out may be r (same pointer and leading
- * dimension), no other overlap.  status [device, one int32, caller-owned, may be NULL]: SLICEGCN_DEVSTATUS_WAIT or nothing.
+ * dimension), no other overlap.  status [device, one int32, caller-owned, may be NULL, and then a wait that ran out
+ * goes unseen]: SLICEGCN_DEVSTATUS_WAIT is set, or nothing.
  * workspace [device, 128-byte aligned], contents undefined before and after.
  * Errors: INVALID_ARG, OVERFLOW, UNSUPPORTED, ALLOC (workspace too small), CUDA. */
 slicegcn_status_t slicegcn_ffn_forward(const slicegcn_ffn_desc* d, const void* x, const void* r, void* out, int32_t* status,

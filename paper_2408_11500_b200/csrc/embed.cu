@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(int64_t n, int64_t v
 #pragma unroll
     for (int k = 0; k < ROWS; ++k) {
         const bool known = (uint32_t)id[k] < (uint32_t)vocab;
-        if (!known && id[k] != -1 && status) atomicExch(status, SLICEGCN_DEVSTATUS_BAD_ID);
+        if (!known && id[k] != -1 && status) atomicOr(status, SLICEGCN_DEVSTATUS_BAD_ID);
         part[k].load(table + (int64_t)(known ? id[k] : 0) * table_ld, live_col ? col : 0, L, width);
     }
 #pragma unroll
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
 #pragma unroll 8
     for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads) {
         const uint32_t key = sort_load<FIRST>(a, (int32_t)i).x;
-        if (FIRST && key == (uint32_t)a.vocab && a.status && a.ids[i] != -1) atomicExch(a.status, SLICEGCN_DEVSTATUS_BAD_ID);
+        if (FIRST && key == (uint32_t)a.vocab && a.status && a.ids[i] != -1) atomicOr(a.status, SLICEGCN_DEVSTATUS_BAD_ID);
         atomicAdd(&hist[(key >> a.shift) & mask], 1u);
     }
     __syncthreads();
@@ -924,7 +924,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_small_kernel(const SumArgs 
     uint32_t mine[K];   // lanes of the warp that found one of the CTA's ids
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        if (blockIdx.x == 0 && blockIdx.y == 0 && status && id[k] != -1 && (uint32_t)id[k] >= (uint32_t)a.vocab) atomicExch(status, SLICEGCN_DEVSTATUS_BAD_ID);
+        if (blockIdx.x == 0 && blockIdx.y == 0 && status && id[k] != -1 && (uint32_t)id[k] >= (uint32_t)a.vocab) atomicOr(status, SLICEGCN_DEVSTATUS_BAD_ID);
         mine[k] = __ballot_sync(0xffffffffu, (uint32_t)id[k] < (uint32_t)a.vocab && (uint32_t)id[k] - turn(id[k]) * gridDim.x == blockIdx.x);
         if (lane == 0) sh.before[k][w] = __popc(mine[k]);
     }

@@ -712,7 +712,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
         }
         // the pair's last arrivals at this CTA's barriers, before its memory is given up
         for (int s = max(0, fill - kStages); ok && s < fill; ++s) ok = mbar_wait(empty + s % kStages, (s / kStages) & 1);
-        if (!ok && P.status) atomicExch(P.status, SLICEGCN_DEVSTATUS_WAIT);
+        if (!ok && P.status) atomicOr(P.status, SLICEGCN_DEVSTATUS_WAIT);
     } else if (warp == kEpiWarps + 1) {
         if (rank == 0) {
             const bool one = elect_one();
@@ -790,7 +790,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
                     mbar_wait(full + st, phase);
                     if (++st == kStages) st = 0, phase ^= 1;
                 }
-                if (P.status) atomicExch(P.status, SLICEGCN_DEVSTATUS_WAIT);
+                if (P.status) atomicOr(P.status, SLICEGCN_DEVSTATUS_WAIT);
             }
         }
     } else {
@@ -1093,7 +1093,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ffn_ker
             }
         }
         if (lane == 0) stores_done();
-        if (!ok && lane == 0 && P.status) atomicExch(P.status, SLICEGCN_DEVSTATUS_WAIT);
+        if (!ok && lane == 0 && P.status) atomicOr(P.status, SLICEGCN_DEVSTATUS_WAIT);
     }
     __syncwarp();
     fence_before();

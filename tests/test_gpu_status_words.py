@@ -1,0 +1,36 @@
+"""A status word that several calls share keeps what each of them has set."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n,vocab", [(300, 40), (200_000, 1000)], ids=str)
+def test_bad_ids_leave_an_expired_wait_in_the_word(n, vocab):
+    """Lookup and gradient, small and sorted forms, in a word that holds the bit of a wait that ran out."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    ids = torch.randint(0, vocab, (n,), dtype=torch.int32, device="cuda")
+    ids[n // 2] = vocab
+    table, out = torch.randn((vocab, 8), device="cuda"), torch.empty((n, 8), device="cuda")
+    d = B.make_embed_desc(n, vocab, 8)
+    ws = torch.empty(B.slicegcn_embed_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    status = torch.tensor([B.DEVSTATUS_WAIT], dtype=torch.int32, device="cuda")
+    B.slicegcn_embed_forward(d, ids, table, out, status)
+    assert int(status) == B.DEVSTATUS_WAIT | B.DEVSTATUS_BAD_ID
+    status.fill_(B.DEVSTATUS_WAIT)
+    B.slicegcn_embed_backward(d, ids, out, table, status, ws, ws.numel())
+    assert int(status) == B.DEVSTATUS_WAIT | B.DEVSTATUS_BAD_ID
+    assert B.DEVSTATUS_WAIT & B.DEVSTATUS_BAD_ID == 0
+
+
+def test_feed_forward_calls_leave_bad_ids_in_the_word():
+    from paper_2408_11500_b200 import binding as B
+    import torch
+    n, k = 500, 96
+    x, W, out = torch.randn((n, k), device="cuda"), torch.randn((1, k, k), device="cuda"), torch.empty((n, k), device="cuda")
+    d = B.make_ffn_desc(n, 1, k, k, W, act=B.ACT_SILU)
+    need = max(B.slicegcn_ffn_workspace_bytes(d, x), B.slicegcn_ffn_workspace_bytes(d, x, out))
+    ws, status = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.tensor([B.DEVSTATUS_BAD_ID], dtype=torch.int32, device="cuda")
+    B.slicegcn_ffn_forward(d, x, None, out, status, ws, need)
+    B.slicegcn_ffn_backward(d, x, out, torch.empty_like(x), torch.empty_like(W), None, None, None, status, ws, need)
+    assert int(status) == B.DEVSTATUS_BAD_ID
