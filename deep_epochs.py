@@ -58,7 +58,7 @@ class DeepSlicedGCN:
         self.y = [mat() for _ in range(layers)]              # layer outputs
         self.dx, self.du, self.dy, self.dgate = mat(), mat(), mat(), mat()
         self.norm = torch.zeros(1, device="cuda")
-        self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        self.status, self.waits = (torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(2))   # of the ids; of the blocks
         P = self.params
         self.embed = B.make_embed_desc(self.n, vocab, self.width, scale=self.scale)
         self.first_norm = B.make_residual_norm_desc(self.n, self.p, self.h_s, w_pre=P["w_pre.0"])
@@ -107,8 +107,8 @@ class DeepSlicedGCN:
                 B.slicegcn_residual_norm_forward(self.norms[i], self.x[i], self.y[i], self.u[i], self.x[i + 1], self.u[i + 1], st)
                 continue
             B.slicegcn_residual_norm_forward(self.norms[i], self.x[i], self.y[i], self.u[i], self.xl[i], self.ul[i], st)
-            B.slicegcn_ffn_forward(self.inner[i], self.ul[i], None, self.hidden[i], self.status, self.ws, self.ws_bytes, st)
-            B.slicegcn_ffn_forward(self.outer[i], self.hidden[i], self.xl[i], self.x[i + 1], self.status, self.ws, self.ws_bytes, st)
+            B.slicegcn_ffn_forward(self.inner[i], self.ul[i], None, self.hidden[i], self.waits, self.ws, self.ws_bytes, st)
+            B.slicegcn_ffn_forward(self.outer[i], self.hidden[i], self.xl[i], self.x[i + 1], self.waits, self.ws, self.ws_bytes, st)
             B.slicegcn_residual_norm_forward(self.ends[i], self.x[i + 1], None, None, None, self.u[i + 1], st)
         return self.u[-1] @ self.params["Wc"] + self.params["bc"]
 
@@ -130,9 +130,9 @@ class DeepSlicedGCN:
             if self.ff:                                      # dxl: of the block's end, which is that of the stream before it too
                 B.slicegcn_residual_norm_backward(self.ends[i], None, None, self.x[i + 1], dh, self.du, self.dxl, None, None, None, None, w_pre, None,
                                                   self.ws, self.ws_bytes, st)
-                B.slicegcn_ffn_backward(self.outer[i], self.hidden[i], self.dxl, self.dhidden, G[f"F_out.{i}"], None, G[f"f_out.{i}"], None, self.status,
+                B.slicegcn_ffn_backward(self.outer[i], self.hidden[i], self.dxl, self.dhidden, G[f"F_out.{i}"], None, G[f"f_out.{i}"], None, self.waits,
                                         self.ws, self.ws_bytes, st)
-                B.slicegcn_ffn_backward(self.inner[i], self.ul[i], self.dhidden, self.du, G[f"F_gate.{i}"], G[f"F_up.{i}"], G[f"f.{i}"], None, self.status,
+                B.slicegcn_ffn_backward(self.inner[i], self.ul[i], self.dhidden, self.du, G[f"F_gate.{i}"], G[f"F_up.{i}"], G[f"f.{i}"], None, self.waits,
                                         self.ws, self.ws_bytes, st)
                 dh, w_pre, end = self.dxl, G[f"w_ff.{i}"], self.xl[i]
             B.slicegcn_residual_norm_backward(self.norms[i], self.y[i], self.u[i], end, dh, self.du, self.dx, self.dy, self.dgate,
@@ -158,6 +158,11 @@ class DeepSlicedGCN:
         else:
             self.torch._foreach_add_(list(self.params.values()), list(self.clipped.values()), alpha=-lr)
         return loss
+
+    def check(self):
+        """Raises where a block's kernel gave up waiting: what was computed since is undefined.  Waits for the device."""
+        if int(self.waits):
+            raise RuntimeError(f"a feed-forward call gave up a wait on the device (status {int(self.waits)}): the results are undefined")
 
 
 def main() -> None:
@@ -193,6 +198,7 @@ def main() -> None:
         losses.append(model.step(args.lr))
     t1.record()
     torch.cuda.synchronize()
+    model.check()
     ms = t0.elapsed_time(t1) / args.epochs
     print(json.dumps({"metric": "full-graph training throughput of a deep sliced GCN from ids", "unit": "epochs/s", "value": 1e3 / ms,
                       "ms_per_epoch": ms, "workload": args.workload, "nodes": w["n"], "layers": args.layers, "vocab": vocab,

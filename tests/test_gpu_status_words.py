@@ -34,3 +34,21 @@ def test_feed_forward_calls_leave_bad_ids_in_the_word():
     B.slicegcn_ffn_forward(d, x, None, out, status, ws, need)
     B.slicegcn_ffn_backward(d, x, out, torch.empty_like(x), torch.empty_like(W), None, None, None, status, ws, need)
     assert int(status) == B.DEVSTATUS_BAD_ID
+
+
+def test_the_deep_model_reports_an_expired_wait_as_such():
+    """Not as bad ids, and not silently."""
+    from test_gpu_ffn_deep import _ff_model
+    from paper_2408_11500_b200 import binding as B
+    m, _ = _ff_model(100, 20, 32, 4, 1, 5, 2)
+    m.step(0.1)
+    m.check()
+    assert int(m.waits) == 0 and int(m.status) == 0
+    m.ids[3] = 20
+    m.step(0.1)
+    m.check()
+    assert int(m.waits) == 0 and int(m.status) == B.DEVSTATUS_BAD_ID
+    m.waits.fill_(B.DEVSTATUS_WAIT)                  # as a kernel leaves it
+    with pytest.raises(RuntimeError, match="gave up a wait"):
+        m.check()
+    m.B.slicegcn_graph_destroy(m.g)
