@@ -165,9 +165,8 @@ class DeepSlicedGCN:
             raise RuntimeError(f"a feed-forward call gave up a wait on the device (status {int(self.waits)}): the results are undefined")
 
 
-def main() -> None:
-    import torch
-    from paper_2408_11500_b200 import binding as B, synth
+def arguments(argv=None):
+    from paper_2408_11500_b200 import synth
     ap = argparse.ArgumentParser()
     ap.add_argument("--workload", default="citation", choices=sorted(synth.WORKLOADS))
     ap.add_argument("--fraction", type=float, default=1.0, help="scale the workload's nodes and edges")
@@ -175,10 +174,19 @@ def main() -> None:
     ap.add_argument("--vocab", type=int, default=0, help="categories (0: a vector of its own for every node)")
     ap.add_argument("--epochs", type=int, default=20)
     ap.add_argument("--warmup", type=int, default=3)
-    ap.add_argument("--lr", type=float, default=0.5)
+    ap.add_argument("--lr", type=float, help="learning rate (0.5 for plain gradient descent, 1e-3 for AdamW)")
     ap.add_argument("--ff", type=int, default=0, help="inner columns of a feed-forward block per column of its slice (0: no blocks)")
     ap.add_argument("--adamw", default="", choices=["", "32bit", "8bit"], help="AdamW with states of 32 or 8 bits instead of plain gradient descent")
-    args = ap.parse_args()
+    args = ap.parse_args(argv)
+    if args.lr is None:                       # AdamW moves every parameter by about the rate a step, whatever its gradient
+        args.lr = 1e-3 if args.adamw else 0.5
+    return args
+
+
+def main() -> None:
+    import torch
+    from paper_2408_11500_b200 import binding as B, synth
+    args = arguments()
     w = dict(synth.WORKLOADS[args.workload])
     if args.fraction < 1.0:
         w["n"], w["m"] = max(int(w["n"] * args.fraction), 64), max(int(w["m"] * args.fraction), 64)
