@@ -578,13 +578,13 @@ def make_adamw_desc(params: Sequence, grads: Sequence, m: Sequence, v: Sequence,
             ([list(copies)] if copies is not None else [])
     if any(len(t) != n for t in lists) or (decayed is not None and len(decayed) != n):
         raise ValueError("the lists must have one entry for each parameter tensor")
-    wants = ["float32", None, "int8" if q8 else "float32", "uint8" if q8 else "float32"] + (["float32"] * 2 if q8 else []) + ["bfloat16"]
+    wants = [("float32",), ("float32", "bfloat16"), ("int8" if q8 else "float32",), ("uint8" if q8 else "float32",)] + [("float32",)] * (2 * q8) + [("bfloat16",)]
     for k, (tensors, want) in enumerate(zip(lists, wants)):
         for t, p in zip(tensors, lists[0]):
             if t is None and copies is not None and k == len(lists) - 1:
                 continue
             size = -(-p.numel() // ADAMW_BLOCK) if q8 and k in (4, 5) else p.numel()
-            if t.numel() != size or not t.is_contiguous() or (want and str(t.dtype) != "torch." + want):
+            if t.numel() != size or not t.is_contiguous() or str(t.dtype)[6:] not in want:
                 raise ValueError("the tensors of a list must be dense, of the list's type and of the parameter's size")
     codes = {"torch.float32": F32, "torch.bfloat16": BF16}
     pointers = [(c_void_p * max(n, 1))(*[_ptr(t) for t in tensors]) for tensors in lists]
