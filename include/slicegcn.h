@@ -537,7 +537,7 @@ typedef struct slicegcn_ffn_desc {
     int32_t act;                 /* SLICEGCN_ACT_* */
     int32_t dtype;               /* storage type of x, W, W2, r and out */
     int32_t grad_dtype;          /* storage type of dout, dx, dW and dW2: SLICEGCN_F32, or SLICEGCN_BF16 with dtype BF16 */
-    double scale;
+    double scale;                /* finite as fp32 */
     int64_t x_ld, r_ld, out_ld;  /* leading dimensions of the matrices a call is given */
     int64_t dout_ld, dx_ld;      /* (>= num_slices * in_s or out_s; those of others are ignored) */
     const void *W, *W2;          /* [device, num_slices x in_s x out_s, dense, slice-major]; W2 NULL: no gate */

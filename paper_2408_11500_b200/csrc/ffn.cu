@@ -2018,7 +2018,7 @@ slicegcn_status_t check(const slicegcn_ffn_desc* d) {
     if ((d->dtype != SLICEGCN_F32 && d->dtype != SLICEGCN_BF16) || (d->grad_dtype != SLICEGCN_F32 && d->grad_dtype != SLICEGCN_BF16))
         SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "ffn: bad dtype");
     if (d->dtype == SLICEGCN_F32 && d->grad_dtype != SLICEGCN_F32) SGCN_FAIL(SLICEGCN_ERR_UNSUPPORTED, "ffn: fp32 with bf16 gradients");
-    if (!std::isfinite(d->scale)) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "ffn: scale is not finite");
+    if (!std::isfinite((float)d->scale)) SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "ffn: scale is not finite, or past the range of fp32");
     const uintptr_t e = d->dtype == SLICEGCN_F32 ? 4 : 2;
     if (!d->W || (uintptr_t)d->W % e || (uintptr_t)d->W2 % e || (uintptr_t)d->b % 4 || (uintptr_t)d->b2 % 4)
         SGCN_FAIL(SLICEGCN_ERR_INVALID_ARG, "ffn: W is NULL, or a weight or bias is not aligned to its type");
