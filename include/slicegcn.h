@@ -517,13 +517,14 @@ slicegcn_status_t slicegcn_clip_grads(const slicegcn_tensor_list* list, double m
  * num_slices = 1 is the ordinary matrix product.  act: NONE a;  RELU max(a, 0);  SILU a / (1 + exp(-a));
  * GELU a/2 * (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))).  ReLU'(0) = 0.
  * x, W, W2, r and out are stored as `dtype` (bf16 weights: the copies that slicegcn_adamw_step keeps), biases are fp32.  Products
- * and activations are computed from the stored values with fp32's digits and rounded once, as out; sums whose only results are bf16
- * keep 2^-28 of relative accuracy per column added, at worst (2^-16 at 4,096).  Elements of fp32 keep their 24 bits from 2^-110 up; of
- * smaller ones, what lies below 2^-133 may be left out.  SILU and GELU are a times a gate 1 / (1 + exp(-w)); a gate below 2^-126 (SILU:
- * a < -87.3, GELU: a < -10) keeps the bits down to 2^-149 in fp32, and may count as 0 in sums and results of bf16.  An infinite or NaN element of x, W or dout
- * leaves no finite results where it enters (infinities may become NaN there; RELU's value below and its slope are finite at an
- * infinity, and NaN at NaN); one of x or dout may do the same in the other slices of its row (narrow slices are computed together),
- * and so in what is summed over rows.  Other rows of out and dx are not touched.
+ * and activations are computed from the stored values with fp32's digits and rounded once, as out; sums whose only results are
+ * bf16 keep 2^-28 of relative accuracy per column added, at worst (2^-16 at 4,096; sums over rows 2^-19).  Elements of fp32 keep
+ * their 24 bits from 2^-110 up; of smaller ones, what lies below 2^-133 may be left out.  SILU and GELU are a times a gate 1 / (1
+ * + exp(-w)); a gate below 2^-126 (SILU: a < -87.3, GELU: a < -10) keeps the bits down to 2^-149 in fp32, and may count as 0 in
+ * sums and results of bf16.  An infinite or NaN element of x, W or dout leaves no finite results where it enters (infinities may
+ * become NaN there; RELU's value below and its slope are finite at an infinity, and NaN at NaN); one of x or dout may do the same
+ * in the other slices of its row (narrow slices are computed together), and so in what is summed over rows.  Other rows of out and
+ * dx are not touched.
  */
 enum { SLICEGCN_ACT_NONE = 0, SLICEGCN_ACT_RELU = 1, SLICEGCN_ACT_SILU = 2, SLICEGCN_ACT_GELU = 3 };
 #define SLICEGCN_MAX_FFN_WIDTH 65536

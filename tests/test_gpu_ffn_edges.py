@@ -164,3 +164,27 @@ def test_biases_gradients_of_middling_sums(ins):
     columns = ins if ins <= 768 else 512
     for name, want in (("db", (g * dy * c).sum(1)), ("db2", (g * y).sum(1))):
         assert float((got[name].double() - want).norm() / want.norm()) < columns / 16 * 2.0 ** -24, name
+
+
+def test_weights_gradients_of_many_rows_are_not_cut_short():
+    """Additions in tensor memory cut in one direction: 512 rows are 32 of them, half of 2^-24 each of a sum that grows to the whole, 2^-20 on
+    average; what 512 rows give is then added with rounding.  The mean of a bf16 result's distance to the rightly rounded one is
+    that shift (results on the other side of a rounding's border make up for those that did not move); twice 2^-20 is allowed."""
+    import torch
+    from paper_2408_11500_b200 import binding as B
+    n, ins, outs = 300_000, 1024, 512
+    g = torch.Generator("cuda").manual_seed(6)
+
+    def positive(cols):
+        t = torch.rand((n, cols), generator=g, device="cuda").add_(0.5).mul_(torch.rand(cols, generator=g, device="cuda").add_(1.0))
+        return t.to(torch.bfloat16)
+    x, dout = positive(ins), positive(outs)
+    W, dW = (torch.zeros((1, ins, outs), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    d = B.make_ffn_desc(n, 1, ins, outs, W, dtype=B.BF16)
+    ws = torch.empty(B.slicegcn_ffn_workspace_bytes(d, x, dout), dtype=torch.uint8, device="cuda")
+    B.slicegcn_ffn_backward(d, x, dout, None, dW, None, None, None, None, ws, ws.numel())
+    want = torch.zeros((ins, outs), device="cuda", dtype=torch.float64)
+    for s in range(0, n, 50_000):
+        want += x[s:s + 50_000].double().t() @ dout[s:s + 50_000].double()
+    short = ((want.to(torch.bfloat16).double() - dW[0].double()) / want).mean()
+    assert abs(float(short)) < 2 * 2.0 ** -20, float(short)
