@@ -206,6 +206,7 @@ __device__ __forceinline__ void update_block(const Entry& e, int64_t block, int 
         m[k] = __fadd_rn(__fmul_rn(m[k], h.beta1), __fmul_rn(gk, h.one_minus_beta1));
         v[k] = __fadd_rn(__fmul_rn(v[k], h.beta2), __fmul_rn(__fmul_rn(gk, h.one_minus_beta2), gk));
         const float root = __fsqrt_rn(v[k]);
+        // the quotient is off by 2 units of the last place, of an update that is small beside the parameter
         p[k] = p[k] * shrink - s.rate * __fdividef(m[k], root * s.inv_root_corr + h.eps);
         if (Q8) v[k] = root;
     }

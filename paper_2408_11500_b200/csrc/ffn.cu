@@ -131,8 +131,9 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
 __device__ __forceinline__ void mbar_expect(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
-// Arrives at the same barrier of the pair's first CTA.  Relaxed: what it hands over are accumulators that have been read (the wait for
-// those reads is behind this thread); a release would first wait for all results the warp has stored (17 % of all warp stalls).
+// Arrives at the same barrier of the pair's first CTA.  Relaxed: what it hands over are accumulators that have been read into registers (the
+// wait for those reads is behind this thread, and so is its tcgen05 fence, whose other half follows the issuing warp's wait); no data in
+// memory goes with it.  A release would first wait for all results the warp has stored (17 % of all warp stalls).
 __device__ __forceinline__ void mbar_arrive_first(uint64_t* bar) {
     asm volatile(
         "{\n\t.reg .b32 a;\n\t"
@@ -434,7 +435,8 @@ __device__ __forceinline__ float gate_of(float a) {   // by the exponential of -
     return w < 0.f ? t * r : r;
 }
 // Where results are rounded to bf16 the hardware's exponential and reciprocal (2^-22 each, and 2^-24 |w| of the argument) are exact
-// enough (one reciprocal for two numbers, 1/x = y/(xy), gained nothing); a gate below 2^-126 is 0.  Two numbers at a time; s = a^2.
+// enough (one reciprocal for two numbers, 1/x = y/(xy), gained nothing); a gate below 2^-126 is 0.  These two operations keep the
+// special-function unit busy for 63 % of the gated forward kernels' time.  Two numbers at a time; s = a^2.
 template <int ACT>
 __device__ __forceinline__ void gates_of(float a0, float a1, float s0, float s1, float& q0, float& q1) {
     if (ACT == SLICEGCN_ACT_SILU) {
