@@ -133,7 +133,8 @@ __device__ __forceinline__ void mbar_expect(uint64_t* bar, uint32_t bytes) {
 }
 // Arrives at the same barrier of the pair's first CTA.  Relaxed: what it hands over are accumulators that have been read into registers (the
 // wait for those reads is behind this thread, and so is its tcgen05 fence, whose other half follows the issuing warp's wait); no data in
-// memory goes with it.  A release would first wait for all results the warp has stored (17 % of all warp stalls).
+// memory goes with it.  A release would first wait for all results the warp has stored (17 % of all warp stalls; 157 and 219 us for the gated
+// forward of 169,343 x 256 -> 2 x 1,024).
 __device__ __forceinline__ void mbar_arrive_first(uint64_t* bar) {
     asm volatile(
         "{\n\t.reg .b32 a;\n\t"
